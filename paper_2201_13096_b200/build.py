@@ -2,8 +2,9 @@
 
 Three shared objects come out of ``csrc/``:
 
-* ``libspdy_dp.so``        - the product: host plan (g++) + kernels and launch code (nvcc);
-* ``libspdy_dp_debug.so``  - the same sources with ``-DSPDY_DEBUG_CHECKS``: every row and table access of
+* ``libspdy_dp.so``        - the product: host plan (g++) + kernels and launch code (nvcc), and the evaluation operators
+  (``eval_*.cu``, declared in ``include/spdy_eval.h``);
+* ``libspdy_dp_debug.so``  - the solver's sources with ``-DSPDY_DEBUG_CHECKS``: every row and table access of
   the forward kernels checks its index and reports through the plan's status word (for tests);
 * ``libspdy_plan_host.so`` - ``spdy_plan.cpp`` and ``spdy_search.cpp`` alone, built with the host compiler:
   plans, their verification, the host helpers and the search loop, for machines and tests without nvcc.
@@ -22,6 +23,10 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 HEADERS = [os.path.join(os.path.dirname(PKG), "include", "spdy_dp.h"),
            os.path.join(CSRC, "spdy_plan.h"), os.path.join(CSRC, "spdy_device.cuh")]
+# The evaluation operators (eval_*.cu) share the library but none of the solver's device code.
+EVAL_HEADERS = [os.path.join(os.path.dirname(PKG), "include", "spdy_dp.h"),
+                os.path.join(os.path.dirname(PKG), "include", "spdy_eval.h"),
+                os.path.join(CSRC, "eval_common.cuh"), os.path.join(CSRC, "eval_loss.cuh")]
 HOST_SOURCES = [os.path.join(CSRC, "spdy_plan.cpp"), os.path.join(CSRC, "spdy_search.cpp")]
 LIB = os.path.join(PKG, "libspdy_dp.so")
 LIB_DEBUG = os.path.join(PKG, "libspdy_dp_debug.so")
@@ -43,7 +48,12 @@ def _nvcc() -> str:
 
 
 def cuda_sources() -> list:
-    return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
+    return sorted(glob.glob(os.path.join(CSRC, "spdy_*.cu")))
+
+
+def eval_sources() -> list:
+    """The evaluation operators' translation units: in the product library only (they have no debug variant)."""
+    return sorted(glob.glob(os.path.join(CSRC, "eval_*.cu")))
 
 
 def _newest(paths) -> float:
@@ -77,8 +87,9 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     sources.  Returns the library's path; with ``verbose`` the compilers' output (``-Xptxas -v``) goes
     to stdout."""
     lib = LIB_DEBUG if debug else LIB
-    sources = cuda_sources()
-    if not force and not _stale(lib, sources + HOST_SOURCES + HEADERS):
+    sources = cuda_sources() + ([] if debug else eval_sources())
+    headers = HEADERS + ([] if debug else EVAL_HEADERS)
+    if not force and not _stale(lib, sources + HOST_SOURCES + headers):
         return lib
     objdir = os.path.join(OBJ_ROOT, "debug" if debug else "release")
     os.makedirs(objdir, exist_ok=True)
@@ -88,7 +99,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     for src in sources:
         obj = os.path.join(objdir, os.path.basename(src) + ".o")
         objects.append(obj)
-        if force or verbose or _stale(obj, [src] + HEADERS):
+        if force or verbose or _stale(obj, [src] + (EVAL_HEADERS if os.path.basename(src).startswith("eval_") else HEADERS)):
             jobs.append([_nvcc(), *NVCC_FLAGS, *defines, *ptxas_opt, *(["-Xptxas", "-v"] if verbose else []), "-c", "-o", obj, src])
     for src in HOST_SOURCES:
         host_obj = os.path.join(objdir, os.path.basename(src) + ".o")

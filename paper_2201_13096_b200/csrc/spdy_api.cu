@@ -12,6 +12,10 @@
 
 using namespace spdy;
 
+namespace spdy {
+void note_cuda_error(int err);
+}
+
 namespace {
 
 thread_local int g_last_cuda_error = 0;
@@ -44,6 +48,9 @@ struct DeviceGuard {
 };
 
 }  // namespace
+
+// For the other translation units of the library (eval_*.cu).
+void spdy::note_cuda_error(int err) { g_last_cuda_error = err; }
 
 // Everything a plan owns on the device (spdy_plan::dev).
 struct spdy::DeviceSide {
