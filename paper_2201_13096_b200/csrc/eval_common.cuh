@@ -36,6 +36,29 @@ __device__ __forceinline__ float max_nan(float a, float b)
     return y;
 }
 
+// Two fp32 operations per instruction (each rounded as its scalar form).
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long &>(r)) : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long &>(r)) : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long &>(r))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)), "l"(reinterpret_cast<unsigned long long &>(c)));
+    return r;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 __device__ __forceinline__ float quiet_nan() { return __int_as_float(0x7fc00000); }
 
@@ -58,6 +81,14 @@ template <> struct Elem<float> {
     static constexpr uint32_t kNegInfWord = 0xff800000u;
     static __device__ __forceinline__ float to_float(float x) { return x; }
     static __device__ __forceinline__ float from_float(float x) { return x; }
+    static __device__ __forceinline__ void pairs(uint4 r, float2 *f)
+    {
+        f[0] = make_float2(__uint_as_float(r.x), __uint_as_float(r.y)), f[1] = make_float2(__uint_as_float(r.z), __uint_as_float(r.w));
+    }
+    static __device__ __forceinline__ uint4 pack(const float2 *f)
+    {
+        return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
+    }
     static __device__ __forceinline__ void unpack(uint4 r, float *f)
     {
         f[0] = __uint_as_float(r.x), f[1] = __uint_as_float(r.y), f[2] = __uint_as_float(r.z), f[3] = __uint_as_float(r.w);
@@ -86,6 +117,11 @@ template <> struct Elem<__nv_bfloat16> {
     {
         two(r.x, f[0], f[1]), two(r.y, f[2], f[3]), two(r.z, f[4], f[5]), two(r.w, f[6], f[7]);
     }
+    static __device__ __forceinline__ void pairs(uint4 r, float2 *f)
+    {
+        two(r.x, f[0].x, f[0].y), two(r.y, f[1].x, f[1].y), two(r.z, f[2].x, f[2].y), two(r.w, f[3].x, f[3].y);
+    }
+    static __device__ __forceinline__ uint4 pack(const float2 *f) { return make_uint4(join(f[0].x, f[0].y), join(f[1].x, f[1].y), join(f[2].x, f[2].y), join(f[3].x, f[3].y)); }
     static __device__ __forceinline__ uint32_t join(float lo, float hi)
     {
         __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -113,6 +149,11 @@ template <> struct Elem<__half> {
     {
         two(r.x, f[0], f[1]), two(r.y, f[2], f[3]), two(r.z, f[4], f[5]), two(r.w, f[6], f[7]);
     }
+    static __device__ __forceinline__ void pairs(uint4 r, float2 *f)
+    {
+        two(r.x, f[0].x, f[0].y), two(r.y, f[1].x, f[1].y), two(r.z, f[2].x, f[2].y), two(r.w, f[3].x, f[3].y);
+    }
+    static __device__ __forceinline__ uint4 pack(const float2 *f) { return make_uint4(join(f[0].x, f[0].y), join(f[1].x, f[1].y), join(f[2].x, f[2].y), join(f[3].x, f[3].y)); }
     static __device__ __forceinline__ uint32_t join(float lo, float hi)
     {
         __half2 v = __floats2half2_rn(lo, hi);
@@ -128,35 +169,59 @@ template <> struct Elem<__half> {
 };
 
 // A row that may start anywhere: granule g is the g-th aligned 16 bytes that hold a part of it, elements
-// g * kVec - lead .. + kVec - 1.  Only granules that lie wholly inside the row are moved 16 bytes at a time.
+// g * kVec - lead .. + kVec - 1.  Only granules that lie wholly inside the row (lo <= g < hi) are moved 16 bytes at a time.
 template <class T> struct Row {
     const T *p;
-    int n;      // elements, at most 2^31 - 64 (positions inside a row are 32-bit)
-    int lead;   // elements of granule 0 that lie before the row
+    int n;       // elements, at most 2^31 - 65 (positions inside a row are 32-bit)
+    int lead;    // elements of granule 0 that lie before the row
+    int lo, hi;  // the whole granules
 
-    __device__ __forceinline__ Row(const T *row, int64_t count) : p(row), n(static_cast<int>(count)), lead(static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T))) {}
+    __device__ __forceinline__ Row(const T *row, int64_t count) : p(row), n(static_cast<int>(count)), lead(static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)))
+    {
+        lo = lead ? 1 : 0;
+        hi = (n + lead) / Elem<T>::kVec;
+    }
     __device__ __forceinline__ int granules() const { return (n + lead + Elem<T>::kVec - 1) / Elem<T>::kVec; }
     __device__ __forceinline__ int first(int g) const { return g * Elem<T>::kVec - lead; }
-    // elements outside the row read as -inf
-    __device__ __forceinline__ uint4 load(int g) const
+    __device__ __forceinline__ bool whole(int g) const { return static_cast<unsigned>(g - lo) < static_cast<unsigned>(max(hi - lo, 0)); }
+    __device__ __noinline__ uint4 load_part(int g) const
     {
         const int e = first(g);
-        if (e >= 0 && e + Elem<T>::kVec <= n) return load_stream(p + e);
         float f[Elem<T>::kVec];
 #pragma unroll
         for (int i = 0; i < Elem<T>::kVec; ++i) f[i] = (e + i >= 0 && e + i < n) ? Elem<T>::to_float(p[e + i]) : neg_inf();
         return Elem<T>::pack(f);
     }
-    // f[0..kVec) to the same elements of `q`, a row of as many elements that may start elsewhere
-    static __device__ __forceinline__ void store(T *q, int n, int e, const float *f)
+    // elements outside the row read as -inf
+    __device__ __forceinline__ uint4 load(int g) const
     {
-        if (e >= 0 && e + Elem<T>::kVec <= n && (reinterpret_cast<uintptr_t>(q + e) & 15) == 0) {
-            store_stream(q + e, Elem<T>::pack(f));
-            return;
-        }
+        if (whole(g)) return load_stream(p + first(g));
+        return load_part(g);
+    }
+    // the same, nothing but -inf from granule `limit` on
+    __device__ __forceinline__ uint4 load_below(int g, int limit) const
+    {
+        constexpr uint32_t NI = Elem<T>::kNegInfWord;
+        if (whole(g) && g < limit) return load_stream(p + first(g));
+        if (g < limit) return load_part(g);
+        return make_uint4(NI, NI, NI, NI);
+    }
+    // v, converted already, to granule g's elements of `q`, a row of as many elements that may start elsewhere
+    __device__ __noinline__ void store_part(T *q, int g, uint4 v) const
+    {
+        const int e = first(g);
+        float f[Elem<T>::kVec];
+        Elem<T>::unpack(v, f);
 #pragma unroll
         for (int i = 0; i < Elem<T>::kVec; ++i)
             if (e + i >= 0 && e + i < n) q[e + i] = Elem<T>::from_float(f[i]);
+    }
+    __device__ __forceinline__ bool same_lead(const T *q) const { return (reinterpret_cast<uintptr_t>(q) & 15) == (reinterpret_cast<uintptr_t>(p) & 15); }
+    // `same`: same_lead(q)
+    __device__ __forceinline__ void store(T *q, bool same, int g, uint4 v) const
+    {
+        if (same && whole(g)) store_stream(q + first(g), v);
+        else store_part(q, g, v);
     }
 };
 

@@ -140,7 +140,7 @@ template <class T, int TPR, int VPT, int NT> __global__ void __launch_bounds__(N
         params<VEC>(a.bias, a.param_type, e, a.D, 0.f, b);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) f[i] = fmaf((f[i] - mean) * rstd, w[i], b[i]);
-        Row<T>::store(out, row.n, e, f);
+        row.store(out, row.same_lead(out), g, Elem<T>::pack(f));
     }
 }
 
@@ -184,7 +184,13 @@ template <class T, int VEC> __device__ __forceinline__ void load_some(const T *p
 template <class T, int VEC> __device__ __forceinline__ void store_some(T *p, int64_t e, int64_t n, const float *f)
 {
     if (VEC > 1) {
-        Row<T>::store(p, static_cast<int>(n), static_cast<int>(e), f);
+        if (e + VEC <= n && (reinterpret_cast<uintptr_t>(p + e) & 15) == 0) {
+            store_stream(p + e, Elem<T>::pack(f));
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (e + i < n) p[e + i] = Elem<T>::from_float(f[i]);
+        }
     } else if (e < n) {
         p[e] = Elem<T>::from_float(f[0]);
     }

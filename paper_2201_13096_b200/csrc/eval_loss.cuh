@@ -2,9 +2,11 @@
 // loss, and their gradients.  Instantiated in eval_token_logprobs.cu and eval_distill.cu.
 //
 // Mathematics.  Everything is kept in base 2: with c = log2(e) / T and the running maximum m of the logits, d_v = (x_v - m) c
-// and s = sum 2^d, a probability is 2^d_v / s.  d is one fused multiply-add x c - (m c), but where m c is so large that the
-// product could overflow (rows of the type's lowest value) m is subtracted first.  The entropy needs t = sum 2^d d beside
-// s: H = ln 2 (log2 s - t / s).  When the maximum rises by delta / c, s becomes s 2^-delta and t (t - s delta) 2^-delta.
+// and s = sum 2^d, a probability is 2^d_v / s.  The difference is taken before the scaling: for 16-bit logits it is exact,
+// and rows of the type's lowest value do not overflow.  The entropy needs t = sum 2^d d beside s: H = ln 2 (log2 s - t / s).
+// When the maximum rises by delta / c, s becomes s 2^-delta and t becomes (t - s delta) 2^-delta.
+// An element costs half an instruction each for difference, scaling and sum (two to an instruction), one to unpack and one
+// for the special-function unit, whose 16 results a cycle and multiprocessor are the next limit behind memory.
 #ifndef SPDY_EVAL_LOSS_CUH
 #define SPDY_EVAL_LOSS_CUH
 
@@ -47,7 +49,20 @@ __device__ __forceinline__ int token_at(const LossArgs &a, int64_t r)
     return t < 0 ? -1 : static_cast<int>(t < a.V ? t : a.V);
 }
 
-// Softmax sums of one thread, block or cluster.
+__device__ __forceinline__ float warp_sum(float x)
+{
+#pragma unroll
+    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    return x;
+}
+__device__ __forceinline__ float warp_max(float x)
+{
+#pragma unroll
+    for (int d = 16; d; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+    return x;
+}
+
+// Softmax sums of a warp, block or cluster.
 struct Stats {
     float m, s, t;  // sums over everything (or, with a teacher's tail, over what lies outside its set; t: entropy only)
     float mi, si;   // sums over the teacher's set
@@ -87,55 +102,38 @@ template <bool ENT, bool TAIL> __device__ __forceinline__ Stats shuffle_xor(cons
     return b;
 }
 
-// How a thread forms d = (x - m) c: x c - base, after subtracting `sub` where m c is beyond what x c - m c can carry.
-struct Shift {
-    float base, sub;
-    bool far;
-    __device__ __forceinline__ Shift(float m, float c)
-    {
-        base = m * c;
-        far = !(fabsf(base) < 1e35f);  // also m = -inf, +inf
-        sub = far && m != neg_inf() ? m : 0.f;
-        if (far) base = 0.f;
-    }
-    template <int N> __device__ __forceinline__ void apply(float *f) const
-    {
-        if (far) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) f[i] -= sub;
-        }
-    }
+// What a thread has added up: s and t in two halves, even and odd elements.
+struct Running {
+    float m;
+    float2 s, t;
 };
 
-// Adds U granules, whose largest element is `top`, to (m, s, t); the sums are rescaled at most once per call.
-template <class T, int U, bool ENT> __device__ __forceinline__ void accumulate(const uint4 *raw, float top, float c, Stats &st)
+// Makes `top` the maximum the sums are relative to, if it is larger.
+template <bool ENT> __device__ __forceinline__ void raise(Running &st, float top, float c)
 {
     if (top > st.m) {
-        if (st.s != 0.f) {
+        if (st.s.x + st.s.y != 0.f) {
             const float d = max_nan((st.m - top) * c, -1000.f), f = ex2(d);
-            if (ENT) st.t = f * fmaf(st.s, d, st.t);
-            st.s *= f;
+            if (ENT) st.t = mul2(both(f), fma2(st.s, both(d), st.t));
+            st.s = mul2(st.s, both(f));
         }
         st.m = top;
     }
-    const Shift shift(st.m, c);
+}
+
+// Adds a granule; no element is larger than the maximum.
+template <class T, bool ENT> __device__ __forceinline__ void accumulate(uint4 raw, float c, Running &st)
+{
+    const float2 minus = both(st.m == neg_inf() ? 0.f : -st.m), scale = both(c);
+    float2 f[Elem<T>::kVec / 2];
+    Elem<T>::pairs(raw, f);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        float f[Elem<T>::kVec];
-        Elem<T>::unpack(raw[u], f);
-        shift.apply<Elem<T>::kVec>(f);
-#pragma unroll
-        for (int i = 0; i < Elem<T>::kVec; ++i) {
-            float d = fmaf(f[i], c, -shift.base);
-            if (ENT) {
-                d = max_nan(d, -1000.f);  // an id that is not allowed adds 2^-1000 = 0 rather than 0 times -inf
-                const float e = ex2(d);
-                st.s += e;
-                st.t = fmaf(e, d, st.t);
-            } else {
-                st.s += ex2(d);
-            }
-        }
+    for (int i = 0; i < Elem<T>::kVec / 2; ++i) {
+        float2 d = mul2(add2(f[i], minus), scale);
+        if (ENT) d = make_float2(max_nan(d.x, -1000.f), max_nan(d.y, -1000.f));  // an id that is not allowed adds 0 rather than 0 times -inf
+        const float2 e = make_float2(ex2(d.x), ex2(d.y));
+        st.s = add2(st.s, e);
+        if (ENT) st.t = fma2(e, d, st.t);
     }
 }
 
@@ -187,67 +185,55 @@ __device__ __forceinline__ uint64_t warp_nth_key(uint32_t value, uint32_t index,
     return last;
 }
 
-constexpr int kPruned = 512;
+constexpr int kCandidates = 2048;
 
 struct TopShared {
-    uint64_t tau[2][32];
-    uint64_t best[SPDY_TOP_MAX];  // this block's result, descending
-    uint64_t pruned[kPruned];
+    uint64_t cand[kCandidates];
+    uint64_t best[SPDY_TOP_MAX];  // the result, descending
+    uint64_t tau[32];
     uint32_t count, count2;
     uint32_t hist[256];
     uint64_t prefix;
     uint32_t want;
 };
 
-// Writes the `want` largest of cand[0..n) in descending order to sh.best (want <= n).  All threads of the block.
-template <int NT> __device__ void select_top(TopShared &sh, const uint64_t *cand, int n, int want, uint64_t floor_key)
+template <int NT> __device__ __forceinline__ int block_count(TopShared &sh, int mine)
 {
-    const int tid = threadIdx.x;
-    if (tid == 0) sh.count2 = 0;
+    mine = __reduce_add_sync(0xffffffffu, mine);
+    if (threadIdx.x == 0) sh.count2 = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += NT) {
-        const uint64_t k = cand[i];
-        if (k >= floor_key) {
-            const uint32_t at = atomicAdd(&sh.count2, 1u);
-            if (at < kPruned) sh.pruned[at] = k;
-        }
-    }
+    if ((threadIdx.x & 31) == 0) atomicAdd(&sh.count2, static_cast<uint32_t>(mine));
     __syncthreads();
-    int left = static_cast<int>(sh.count2);
-    if (left > kPruned) {
-        // too many to rank by counting: the want-th largest key bit by bit, then exactly `want` keys are left
-        uint64_t key = 0;
+    const int total = static_cast<int>(sh.count2);
+    __syncthreads();
+    return total;
+}
+
+// Writes the `want` largest of sh.cand[0..n) in descending order to sh.best (want <= n).  All threads of the block.
+template <int NT> __device__ __noinline__ void select_top(TopShared &sh, int n, int want)
+{
+    uint64_t least = 0;
+    if (n > 512) {  // too many to rank all by counting: the want-th largest key first, bit by bit
         for (int b = 63; b >= 0; --b) {
-            const uint64_t trial = key | 1ull << b;
+            const uint64_t trial = least | 1ull << b;
             int mine = 0;
-            for (int i = tid; i < n; i += NT) mine += cand[i] >= trial;
-            mine = __reduce_add_sync(0xffffffffu, mine);
-            if (tid == 0) sh.count2 = 0;
-            __syncthreads();
-            if ((tid & 31) == 0) atomicAdd(&sh.count2, static_cast<uint32_t>(mine));
-            __syncthreads();
-            if (static_cast<int>(sh.count2) >= want) key = trial;
-            __syncthreads();
+            for (int i = threadIdx.x; i < n; i += NT) mine += sh.cand[i] >= trial;
+            if (block_count<NT>(sh, mine) >= want) least = trial;
         }
-        if (tid == 0) sh.count2 = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += NT)
-            if (cand[i] >= key) sh.pruned[atomicAdd(&sh.count2, 1u)] = cand[i];
-        __syncthreads();
-        left = static_cast<int>(sh.count2);
     }
-    for (int i = tid; i < left; i += NT) {
-        const uint64_t k = sh.pruned[i];
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const uint64_t k = sh.cand[i];
+        if (k < least) continue;
         int rank = 0;
-        for (int j = 0; j < left; ++j) rank += sh.pruned[j] > k;
+        for (int j = 0; j < n; ++j) rank += sh.cand[j] > k;
         if (rank < want) sh.best[rank] = k;
     }
     __syncthreads();
 }
 
-// The `want` largest keys of granules [g0, g1) of a row into cand[0..want), by reading the row once per key byte: for rows
-// whose order defeats the running bound (rising rows, long runs of one value).  All threads of the block.
-template <class T, int NT> __device__ void radix_top(TopShared &sh, const Row<T> &row, int g0, int g1, int want, uint64_t *cand)
+// The `want` largest keys of granules [g0, g1) of a row into sh.cand, by reading the row once per key byte: for rows whose
+// order defeats the bound below.  All threads of the block.
+template <class T, int NT> __device__ __noinline__ void radix_top(TopShared &sh, const Row<T> &row, int g0, int g1, int want)
 {
     const int tid = threadIdx.x;
     uint64_t prefix = 0, mask = 0;
@@ -259,6 +245,7 @@ template <class T, int NT> __device__ void radix_top(TopShared &sh, const Row<T>
             const int e = row.first(g);
             float f[Elem<T>::kVec];
             Elem<T>::unpack(row.load(g), f);
+#pragma unroll
             for (int i = 0; i < Elem<T>::kVec; ++i) {
                 if (e + i < 0 || e + i >= row.n) continue;
                 const uint64_t k = rank_key(f[i], static_cast<uint32_t>(e + i));
@@ -284,16 +271,157 @@ template <class T, int NT> __device__ void radix_top(TopShared &sh, const Row<T>
         const int e = row.first(g);
         float f[Elem<T>::kVec];
         Elem<T>::unpack(row.load(g), f);
+#pragma unroll
         for (int i = 0; i < Elem<T>::kVec; ++i) {
             if (e + i < 0 || e + i >= row.n) continue;
             const uint64_t k = rank_key(f[i], static_cast<uint32_t>(e + i));
             if (k >= prefix) {
                 const uint32_t at = atomicAdd(&sh.count, 1u);
-                if (at < static_cast<uint32_t>(want)) cand[at] = k;
+                if (at < static_cast<uint32_t>(want)) sh.cand[at] = k;
             }
         }
     }
     __syncthreads();
+}
+
+// While a block streams its part of a row, each thread notes the largest element of each of its groups (the U granules of
+// one step, or of 2^shift steps in a row too long for `groups`) as an ordered 32-bit value, 0 for a group without elements.
+// Then the K-th largest group value v bounds the K-th largest element from below: elements above v lie in fewer than K
+// groups, which are read again; what is still missing are elements equal to v, those with the lowest ids.
+// `lane_best` is the thread's largest value over all its groups.  Result in sh.best[0..want).
+template <class T, int NT, int U>
+__device__ __noinline__ void find_top(TopShared &sh, const uint32_t *groups, int n_groups, int shift, uint32_t lane_best, const Row<T> &row, int g0, int g1, int want)
+{
+    constexpr int NW = NT / 32, STEP = NT * U;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // a cheap bound first: the r-th largest lane of every warp, r such that the warps together have `want` lanes above it
+    const uint64_t mine = warp_nth_key(lane_best, static_cast<uint32_t>(lane), (want + NW - 1) / NW);
+    if (lane == 0) sh.tau[warp] = mine >> 32;
+    if (tid == 0) sh.count = 0;
+    __syncthreads();
+    const uint32_t tau = max(1u, __reduce_min_sync(0xffffffffu, lane < NW ? static_cast<uint32_t>(sh.tau[lane]) : 0xffffffffu));
+    const int total = n_groups * NT;
+    for (int i = tid; i < total; i += NT)
+        if (groups[i] >= tau) {
+            const uint32_t at = atomicAdd(&sh.count, 1u);
+            if (at < 512) sh.cand[at] = static_cast<uint64_t>(groups[i]) << 32 | static_cast<uint32_t>(~i);
+        }
+    __syncthreads();
+    const int listed = static_cast<int>(sh.count);
+    uint32_t v = 0;
+    if (listed > 512) {
+        for (int b = 31; b >= 0; --b) {
+            const uint32_t trial = v | 1u << b;
+            int count = 0;
+            for (int i = tid; i < total; i += NT) count += groups[i] >= trial;
+            if (block_count<NT>(sh, count) >= want) v = trial;
+        }
+    } else {
+        if (tid == 0) sh.want = 0;  // fewer groups than `want`: every element is wanted or nearly
+        __syncthreads();
+        for (int i = tid; i < listed; i += NT) {
+            const uint64_t k = sh.cand[i];
+            int rank = 0;
+            for (int j = 0; j < listed; ++j) rank += sh.cand[j] > k;
+            if (rank == want - 1) sh.want = static_cast<uint32_t>(k >> 32);
+        }
+        __syncthreads();
+        v = sh.want;
+    }
+    __syncthreads();
+    if (tid == 0) sh.count = 0;
+    __syncthreads();
+    // elements above v, and the number of groups whose largest is v
+    int ties = 0;
+    for (int i = tid; i < total; i += NT) {
+        if (groups[i] < v) continue;
+        ties += groups[i] == v;
+        if (groups[i] == v) continue;
+        const int base = g0 + (i / NT << shift) * STEP + i % NT;
+        for (int k = 0; k < (U << shift); ++k) {
+            const int g = base + k * NT;
+            if (g >= g1) break;
+            const int e = row.first(g);
+            float f[Elem<T>::kVec];
+            Elem<T>::unpack(row.load(g), f);
+#pragma unroll
+            for (int j = 0; j < Elem<T>::kVec; ++j) {
+                if (ordered(f[j]) <= v || e + j < 0 || e + j >= row.n) continue;
+                const uint32_t at = atomicAdd(&sh.count, 1u);
+                if (at < kCandidates) sh.cand[at] = rank_key(f[j], static_cast<uint32_t>(e + j));
+            }
+        }
+    }
+    ties = block_count<NT>(sh, ties);
+    const int above = static_cast<int>(sh.count);
+    __syncthreads();
+    if (above < want && ties <= 64) {
+        // few groups can hold an element equal to v: take them all
+        for (int i = tid; i < total; i += NT) {
+            if (groups[i] < v) continue;
+            const int base = g0 + (i / NT << shift) * STEP + i % NT;
+            for (int k = 0; k < (U << shift); ++k) {
+                const int g = base + k * NT;
+                if (g >= g1) break;
+                const int e = row.first(g);
+                float f[Elem<T>::kVec];
+                Elem<T>::unpack(row.load(g), f);
+#pragma unroll
+                for (int j = 0; j < Elem<T>::kVec; ++j) {
+                    if (ordered(f[j]) != v || e + j < 0 || e + j >= row.n) continue;
+                    const uint32_t at = atomicAdd(&sh.count, 1u);
+                    if (at < kCandidates) sh.cand[at] = rank_key(f[j], static_cast<uint32_t>(e + j));
+                }
+            }
+        }
+        __syncthreads();
+    } else if (above < want) {
+        // many (a masked or constant row): in ascending order from the row's start until there are enough
+        int have = above;
+        for (int base = g0; base < g1 && have < want; base += NT) {
+            const int g = base + tid;
+            uint32_t bits = 0;
+            float f[Elem<T>::kVec];
+            const int e = row.first(g);
+            if (g < g1) {
+                Elem<T>::unpack(row.load(g), f);
+#pragma unroll
+                for (int j = 0; j < Elem<T>::kVec; ++j)
+                    if (ordered(f[j]) == v && e + j >= 0 && e + j < row.n) bits |= 1u << j;
+            }
+            int before = __popc(bits);
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int other = __shfl_up_sync(0xffffffffu, before, d);
+                if (lane >= d) before += other;
+            }
+            if (lane == 31) sh.tau[warp] = before;
+            __syncthreads();
+            int total_here = 0;
+            for (int w = 0; w < NW; ++w) {
+                if (w == warp) before += total_here;
+                total_here += static_cast<int>(sh.tau[w]);
+            }
+            int at = have + before - __popc(bits);
+#pragma unroll
+            for (int j = 0; j < Elem<T>::kVec; ++j)
+                if (bits >> j & 1) {
+                    if (at < want) sh.cand[at] = rank_key(f[j], static_cast<uint32_t>(e + j));
+                    ++at;
+                }
+            have += total_here;
+            __syncthreads();
+        }
+        if (tid == 0) sh.count = static_cast<uint32_t>(min(have, want));
+        __syncthreads();
+    }
+    int n = static_cast<int>(sh.count);
+    __syncthreads();
+    if (n > kCandidates || n < want) {
+        radix_top<T, NT>(sh, row, g0, g1, want);
+        n = want;
+    }
+    select_top<NT>(sh, n, want);
 }
 
 // ------------------------------------------------------------------------------------------ teacher's entries
@@ -318,19 +446,6 @@ template <class T, int NT> __device__ __forceinline__ void teacher_read(TeacherS
         sh.logq[j] = here ? a.top_lp[row * a.K + j] : neg_inf();
         sh.x[j] = here && id >= e0 && id < e1 ? Elem<T>::to_float(static_cast<const T *>(a.logits)[row * a.ld + id]) : neg_inf();
     }
-}
-
-__device__ __forceinline__ float warp_sum(float x)
-{
-#pragma unroll
-    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    return x;
-}
-__device__ __forceinline__ float warp_max(float x)
-{
-#pragma unroll
-    for (int d = 16; d; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-    return x;
 }
 
 // q, log q, left and mass from the entries; one warp, after a barrier behind teacher_read.
@@ -403,6 +518,7 @@ template <bool TAIL> __device__ __forceinline__ float teacher_loss(const Teacher
 enum { kLogprobs = 0, kLogprobsTop = 1, kDistill = 2, kDistillTail = 3 };
 
 constexpr int kBitmapWords = 4096;  // ids of one segment of a row: 2^17 bits
+constexpr int kGroupSteps = 32;     // groups a thread notes at most
 
 template <int NT> struct ForwardShared {
     Stats part[NT / 32];
@@ -410,24 +526,50 @@ template <int NT> struct ForwardShared {
     uint32_t found;      // entries of top.best
 };
 
+// Sums of a warp's threads, then of the block's warps (in warp 0 afterwards).
+template <bool ENT, bool TAIL, int NT> __device__ __forceinline__ Stats block_stats(const Running &run, float mi, float si, Stats *part, float c)
+{
+    constexpr int NW = NT / 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // the warp's maximum first, so that every lane rescales once and the rest are additions
+    Stats st = {warp_max(run.m), run.s.x + run.s.y, ENT ? run.t.x + run.t.y : 0.f, mi, si};
+    if (st.s != 0.f) {
+        const float d = max_nan((run.m - st.m) * c, -1000.f), f = ex2(d);
+        if (ENT) st.t = f * fmaf(st.s, d, st.t);
+        st.s *= f;
+    }
+    st.s = warp_sum(st.s);
+    if (ENT) st.t = warp_sum(st.t);
+    if (TAIL) {
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            const float om = __shfl_xor_sync(0xffffffffu, st.mi, d), os = __shfl_xor_sync(0xffffffffu, st.si, d);
+            join_sums(st.mi, st.si, om, os, c);
+        }
+    }
+    if (lane == 0) part[warp] = st;
+    __syncthreads();
+    if (warp == 0) {
+        st = lane < NW ? part[lane] : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
+#pragma unroll
+        for (int d = NW / 2; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), c);
+    }
+    return st;
+}
+
 // One row per cluster of blocks (of one block when there are rows enough), the row's granules divided among the blocks and
 // read once, the next U granules of a thread in flight while the present ones are added up.
-//
-// Alternatives: each lane remembers the largest granule it has seen; with r = ceil(K / warps), the r-th largest of a warp's
-// lanes, minimised over the warps, bounds the K-th largest element from below.  Elements under the bound cannot matter; the
-// few others are appended to a list in shared memory, of which the K largest are sorted out at the end.
 template <class T, int NT, int U, int MODE>
 __global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossArgs a)
 {
     constexpr bool ENT = MODE == kLogprobs || MODE == kLogprobsTop, TOP = MODE == kLogprobsTop;
     constexpr bool TEACHER = MODE >= kDistill, TAIL = MODE == kDistillTail;
-    constexpr int NW = NT / 32, kCand = NT * 8 + 512;
     extern __shared__ __align__(16) unsigned char dynamic[];
     __shared__ ForwardShared<NT> sh;
-    uint64_t *cand = reinterpret_cast<uint64_t *>(dynamic);                      // TOP
-    TopShared &top = *reinterpret_cast<TopShared *>(dynamic + sizeof(uint64_t) * kCand);
-    TeacherShared &teacher = *reinterpret_cast<TeacherShared *>(dynamic);        // TEACHER
-    uint32_t *bitmap = reinterpret_cast<uint32_t *>(dynamic + sizeof(TeacherShared));  // TAIL
+    TopShared &top = *reinterpret_cast<TopShared *>(dynamic);                               // TOP
+    uint32_t *groups = reinterpret_cast<uint32_t *>(dynamic + sizeof(TopShared));           // TOP
+    TeacherShared &teacher = *reinterpret_cast<TeacherShared *>(dynamic);                   // TEACHER
+    uint32_t *bitmap = reinterpret_cast<uint32_t *>(dynamic + sizeof(TeacherShared));       // TAIL
 
     cg::cluster_group cluster = cg::this_cluster();
     const int C = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
@@ -436,19 +578,12 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossAr
     const Row<T> row(static_cast<const T *>(a.logits) + r * a.ld, a.V);
     const int G = row.granules(), per = (G + C - 1) / C;
     const int g0 = min(G, rank * per), g1 = min(G, g0 + per);
-    constexpr uint32_t NI = Elem<T>::kNegInfWord;
 
-    Stats st = {neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
+    Running run = {neg_inf(), both(0.f), both(0.f)};
+    float mi = neg_inf(), si = 0.f;
     uint4 next[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int g = g0 + u * NT + tid;
-        next[u] = g < g1 ? row.load(g) : make_uint4(NI, NI, NI, NI);
-    }
-    if (TOP) {
-        if (tid == 0) top.count = 0;
-        __syncthreads();
-    }
+    for (int u = 0; u < U; ++u) next[u] = row.load_below(g0 + u * NT + tid, g1);
     if (TEACHER) {
         teacher_read<T, NT>(teacher, a, r, rank == 0 ? 0 : row.first(g0), rank == 0 ? a.V : row.first(g1));
         if (TAIL) {
@@ -459,14 +594,14 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossAr
         if (warp == 0 && rank == 0) teacher_weights<TAIL>(teacher, a.K);
     }
 
-    float best = neg_inf();
-    uint32_t best_at = 0xffffffffu;
-    bool have = false;
-    uint64_t warp_tau = 0;
-    const int nth = TOP ? (a.K + NW - 1) / NW : 1;
-    int phase = 0;
     constexpr int kSegment = kBitmapWords * 32 / Elem<T>::kVec;  // granules
     static_assert(kSegment % (NT * U) == 0, "a segment is whole steps");
+    const int steps = (g1 - g0 + NT * U - 1) / (NT * U);
+    int shift = 0;
+    if (TOP)
+        while (steps >> shift >= kGroupSteps) ++shift;
+    int step = 0;
+    uint32_t lane_best = 0;
 
     for (int seg = g0; seg < g1; seg = TAIL ? seg + kSegment : g1) {
         const int seg_end = TAIL ? min(g1, seg + kSegment) : g1;
@@ -475,20 +610,17 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossAr
                 const int pos = teacher.id[j] - row.first(seg);
                 if (teacher.id[j] >= 0 && pos >= 0 && pos < (seg_end - seg) * Elem<T>::kVec) {
                     const uint32_t bit = 1u << (pos & 31);
-                    if (!(atomicOr(&bitmap[pos >> 5], bit) & bit)) add_logit(st.mi, st.si, teacher.x[j], a.c);
+                    if (!(atomicOr(&bitmap[pos >> 5], bit) & bit)) add_logit(mi, si, teacher.x[j], a.c);
                 }
             }
             __syncthreads();
         }
-        for (int base = seg; base < seg_end; base += NT * U) {
+        for (int base = seg; base < seg_end; base += NT * U, ++step) {
             uint4 cur[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) cur[u] = next[u];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int g = base + NT * U + u * NT + tid;
-                next[u] = g < g1 ? row.load(g) : make_uint4(NI, NI, NI, NI);
-            }
+            for (int u = 0; u < U; ++u) next[u] = row.load_below(base + NT * U + u * NT + tid, g1);
             if (TAIL) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -497,47 +629,19 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossAr
                     if (bits) cur[u] = without<T>(cur[u], bits);
                 }
             }
-            float largest[U], all = neg_inf();
+            float all = Elem<T>::max_of(cur[0]);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                largest[u] = Elem<T>::max_of(cur[u]);
-                all = fmaxf(all, largest[u]);
-            }
-            accumulate<T, U, ENT>(cur, all, a.c, st);
+            for (int u = 1; u < U; ++u) all = fmaxf(all, Elem<T>::max_of(cur[u]));
             if (TOP) {
-                bool better = false;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int g = base + u * NT + tid;
-                    if (g < g1 && (largest[u] > best || (!have && largest[u] == neg_inf()))) {
-                        best = largest[u];
-                        best_at = static_cast<uint32_t>(row.first(g) + Elem<T>::kVec - 1);  // no element of the granule ranks below this
-                        have = better = true;
-                    }
-                }
-                if (__any_sync(0xffffffffu, better)) warp_tau = warp_nth_key(have ? ordered(best) : 0u, best_at, nth);
-                if (lane == 0) top.tau[phase][warp] = warp_tau;
-                __syncthreads();
-                const uint64_t w = lane < NW ? top.tau[phase][lane] : ~0ull;
-                const uint32_t tv = __reduce_min_sync(0xffffffffu, static_cast<uint32_t>(w >> 32));
-                const uint32_t ti = ~__reduce_min_sync(0xffffffffu, static_cast<uint32_t>(w >> 32) == tv ? static_cast<uint32_t>(w) : 0xffffffffu);
-                const float tau = tv == 0u ? neg_inf() : unordered(tv);
-                phase ^= 1;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int g = base + u * NT + tid;
-                    const int e = row.first(g);
-                    if (g >= g1 || largest[u] < tau || (largest[u] == tau && e > 0 && static_cast<uint32_t>(e) > ti)) continue;
-                    float f[Elem<T>::kVec];
-                    Elem<T>::unpack(cur[u], f);
-#pragma unroll
-                    for (int i = 0; i < Elem<T>::kVec; ++i) {
-                        if (f[i] < tau || e + i < 0 || e + i >= row.n || (f[i] == tau && static_cast<uint32_t>(e + i) > ti)) continue;
-                        const uint32_t at = atomicAdd(&top.count, 1u);
-                        if (at < kCand) cand[at] = rank_key(f[i], static_cast<uint32_t>(e + i));
-                    }
-                }
+                uint32_t key = base + tid < g1 ? ordered(all) : 0u;
+                lane_best = max(lane_best, key);
+                uint32_t *slot = groups + (step >> shift) * NT + tid;
+                if (step & ((1 << shift) - 1)) key = max(key, *slot);
+                *slot = key;
             }
+            raise<ENT>(run, all, a.c);
+#pragma unroll
+            for (int u = 0; u < U; ++u) accumulate<T, ENT>(cur[u], a.c, run);
         }
         if (TAIL) {
             __syncthreads();
@@ -549,32 +653,12 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossAr
         }
     }
 
-    // sums of the block
-#pragma unroll
-    for (int d = 16; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-    if (lane == 0) sh.part[warp] = st;
-    __syncthreads();
-    if (warp == 0) {
-        st = lane < NW ? sh.part[lane] : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
-#pragma unroll
-        for (int d = NW / 2; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-        if (lane == 0) sh.pub = st;
-    }
+    Stats st = block_stats<ENT, TAIL, NT>(run, mi, si, sh.part, a.c);
+    if (tid == 0) sh.pub = st;
     if (TOP) {
         const int e0 = max(0, row.first(g0)), e1 = min(row.n, row.first(g1));
         const int want = max(0, min(a.K, e1 - e0));
-        int n = static_cast<int>(top.count);
-        uint64_t floor_key = 0;
-        if (n > kCand || n < want) {
-            __syncthreads();
-            radix_top<T, NT>(top, row, g0, g1, want, cand);
-            n = want;
-        } else {
-            const uint64_t w = lane < NW ? top.tau[phase ^ 1][lane] : ~0ull;
-            const uint32_t tv = __reduce_min_sync(0xffffffffu, static_cast<uint32_t>(w >> 32));
-            floor_key = static_cast<uint64_t>(tv) << 32 | __reduce_min_sync(0xffffffffu, static_cast<uint32_t>(w >> 32) == tv ? static_cast<uint32_t>(w) : 0xffffffffu);
-        }
-        select_top<NT>(top, cand, n, want, floor_key);
+        if (want > 0) find_top<T, NT, U>(top, groups, (steps + (1 << shift) - 1) >> shift, shift, lane_best, row, g0, g1, want);
         if (tid == 0) sh.found = static_cast<uint32_t>(want);
     }
     if (C > 1) {
@@ -586,21 +670,20 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossAr
                 for (int d = 4; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
             }
             if (TOP) {
-                // the blocks' lists side by side in cand
-                int n = 0;
+                int n = 0;  // the blocks' lists side by side
                 for (int b = 0; b < C; ++b) {
                     const int m = static_cast<int>(*cluster.map_shared_rank(&sh.found, b));
                     const TopShared *other = cluster.map_shared_rank(&top, b);
-                    for (int i = tid; i < m; i += NT) cand[n + i] = other->best[i];
+                    for (int i = tid; i < m; i += NT) top.cand[n + i] = other->best[i];
                     n += m;
                 }
                 __syncthreads();
-                select_top<NT>(top, cand, n, a.K, 0);
+                select_top<NT>(top, n, a.K);
             }
         }
         cluster.sync();  // no block leaves while its shared memory is read
         if (rank != 0) return;
-        if (warp == 0 && lane == 0) sh.pub = st;
+        if (tid == 0) sh.pub = st;
     }
     __syncthreads();
     st = sh.pub;
@@ -638,36 +721,37 @@ struct RowGrad {
     float m, k0, k1;
 };
 
-template <class T, int U, bool ENT>
-__device__ __forceinline__ void write_gradient(const uint4 *raw, const Row<T> &row, T *out, int g, int step, int limit, float c, const RowGrad &k,
-                                               int token, float hit)
+template <class T, bool ENT> __device__ __forceinline__ uint4 gradient_of(uint4 raw, float c, const RowGrad &k)
 {
-    const Shift shift(k.m, c);
+    const float2 minus = both(-k.m), scale = both(c), k0 = both(k.k0), k1 = both(k.k1);
+    float2 f[Elem<T>::kVec / 2];
+    Elem<T>::pairs(raw, f);
+#pragma unroll
+    for (int i = 0; i < Elem<T>::kVec / 2; ++i) {
+        float2 d = mul2(add2(f[i], minus), scale);
+        if (ENT) d = make_float2(max_nan(d.x, -1000.f), max_nan(d.y, -1000.f));
+        f[i] = mul2(make_float2(ex2(d.x), ex2(d.y)), ENT ? fma2(k1, d, k0) : k0);
+    }
+    return Elem<T>::pack(f);
+}
+
+// Granules g, g + step, ... of a row below `limit`; `entropy`: k1 is not zero (the same for the whole block).
+template <class T, int U>
+__device__ __forceinline__ void write_gradient(const uint4 *raw, const Row<T> &row, T *out, bool same, int g, int step, int limit, float c, const RowGrad &k, bool entropy)
+{
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int gu = g + u * step;
         if (gu >= limit) continue;
-        const int e = row.first(gu);
-        float f[Elem<T>::kVec];
-        Elem<T>::unpack(raw[u], f);
-        shift.apply<Elem<T>::kVec>(f);
-#pragma unroll
-        for (int i = 0; i < Elem<T>::kVec; ++i) {
-            float d = fmaf(f[i], c, -shift.base);
-            if (ENT) {
-                d = max_nan(d, -1000.f);
-                f[i] = ex2(d) * fmaf(k.k1, d, k.k0);
-            } else {
-                f[i] = ex2(d) * k.k0;
-            }
-        }
-        if (ENT && token >= e && token < e + Elem<T>::kVec) {
-#pragma unroll
-            for (int i = 0; i < Elem<T>::kVec; ++i)
-                if (token == e + i) f[i] += hit;
-        }
-        Row<T>::store(out, row.n, e, f);
+        row.store(out, same, gu, entropy ? gradient_of<T, true>(raw[u], c, k) : gradient_of<T, false>(raw[u], c, k));
     }
+}
+
+// The given token's element: its share of 2^d (k0 + k1 d) plus `hit`, written again by one thread behind a barrier.
+template <class T> __device__ __forceinline__ void write_token_gradient(T *out, int token, float x, float c, const RowGrad &k, float hit)
+{
+    const float d = max_nan((x - k.m) * c, -1000.f);
+    out[token] = Elem<T>::from_float(fmaf(ex2(d), fmaf(k.k1, d, k.k0), hit));
 }
 
 // The elements of the teacher's set that lie in [e0, e1): A p - (sum of q with this id), written by the thread of the id's
@@ -744,16 +828,22 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
             k.k1 = -gh * kLn2;
         }
     }
-    constexpr uint32_t NI = Elem<T>::kNegInfWord;
+    const bool same = row.same_lead(out), entropy = k.k1 != 0.f;
+    float token_x = 0.f;
+    const bool token_here = token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1);
+    if (!TEACHER && token_here && threadIdx.x == 0) token_x = Elem<T>::to_float(row.p[token]);
+    if (!TEACHER) __syncthreads();  // read before it is overwritten in place
     for (int g = g0 + threadIdx.x; g < g1; g += NT * U) {
         uint4 raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = g + u * NT < g1 ? row.load(g + u * NT) : make_uint4(NI, NI, NI, NI);
-        write_gradient<T, U, !TEACHER>(raw, row, out, g, NT, g1, a.c, k, token, hit);
+        for (int u = 0; u < U; ++u) raw[u] = row.load_below(g + u * NT, g1);
+        write_gradient<T, U>(raw, row, out, same, g, NT, g1, a.c, k, entropy);
     }
+    __syncthreads();
     if constexpr (TEACHER) {
-        __syncthreads();
         write_set_gradient<T, NT>(shared, a.K, out, row.first(g0), row.first(g1), a.c, p_m, p_scale, q_scale);
+    } else {
+        if (token_here && threadIdx.x == 0) write_token_gradient<T>(out, token, token_x, a.c, k, hit);
     }
 }
 
@@ -769,7 +859,6 @@ template <class T, int NT, int U, bool TEACHER, bool TAIL>
 __global__ void __launch_bounds__(NT, 768 / NT) loss_resident_kernel(const LossArgs a)
 {
     constexpr bool ENT = !TEACHER;
-    constexpr int NW = NT / 32;
     __shared__ ResidentShared<NT> sh;
     __shared__ typename std::conditional<TEACHER, TeacherShared, int>::type teacher;
     __shared__ uint32_t bitmap[TAIL ? NT * U * Elem<T>::kVec / 32 : 1];
@@ -781,15 +870,12 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_resident_kernel(const LossA
     T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
     const int G = row.granules(), per = (G + C - 1) / C;
     const int g0 = min(G, rank * per), g1 = min(G, g0 + per);
-    constexpr uint32_t NI = Elem<T>::kNegInfWord;
 
     uint4 raw[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int g = g0 + u * NT + tid;
-        raw[u] = g < g1 ? row.load(g) : make_uint4(NI, NI, NI, NI);
-    }
-    Stats st = {neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
+    for (int u = 0; u < U; ++u) raw[u] = row.load_below(g0 + u * NT + tid, g1);
+    Running run = {neg_inf(), both(0.f), both(0.f)};
+    float mi = neg_inf(), si = 0.f;
     int token = -1;
     float token_x = 0.f;
     if constexpr (TEACHER) {
@@ -803,7 +889,7 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_resident_kernel(const LossA
                 const int pos = teacher.id[j] - row.first(g0);
                 if (teacher.id[j] >= 0 && pos >= 0 && pos < (g1 - g0) * Elem<T>::kVec) {
                     const uint32_t bit = 1u << (pos & 31);
-                    if (!(atomicOr(&bitmap[pos >> 5], bit) & bit)) add_logit(st.mi, st.si, teacher.x[j], a.c);
+                    if (!(atomicOr(&bitmap[pos >> 5], bit) & bit)) add_logit(mi, si, teacher.x[j], a.c);
                 }
             }
         }
@@ -822,20 +908,15 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_resident_kernel(const LossA
             if (token >= 0 && token < a.V) token_x = Elem<T>::to_float(row.p[token]);
         }
     }
-    float all = neg_inf();
+    float all = Elem<T>::max_of(raw[0]);
 #pragma unroll
-    for (int u = 0; u < U; ++u) all = fmaxf(all, Elem<T>::max_of(raw[u]));
-    accumulate<T, U, ENT>(raw, all, a.c, st);
+    for (int u = 1; u < U; ++u) all = fmaxf(all, Elem<T>::max_of(raw[u]));
+    raise<ENT>(run, all, a.c);
 #pragma unroll
-    for (int d = 16; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-    if (lane == 0) sh.part[warp] = st;
-    __syncthreads();
-    if (warp == 0) {
-        st = lane < NW ? sh.part[lane] : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
-#pragma unroll
-        for (int d = NW / 2; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-        if (lane == 0) sh.pub = st, sh.total = st;
-    }
+    for (int u = 0; u < U; ++u)
+        if (g0 + u * NT + (warp << 5) < g1) accumulate<T, ENT>(raw[u], a.c, run);
+    Stats st = block_stats<ENT, TAIL, NT>(run, mi, si, sh.part, a.c);
+    if (tid == 0) sh.pub = st, sh.total = st;
     if (C > 1) {
         cluster.sync();
         if (warp == 0) {
@@ -904,10 +985,12 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_resident_kernel(const LossA
     // the elements are unpacked again rather than kept unpacked in twice the registers
 #pragma unroll
     for (int u = 0; u < U; ++u) asm volatile("" : "+r"(raw[u].x), "+r"(raw[u].y), "+r"(raw[u].z), "+r"(raw[u].w));
-    write_gradient<T, U, ENT>(raw, row, out, g0 + tid, NT, g1, a.c, k, token, hit);
+    write_gradient<T, U>(raw, row, out, row.same_lead(out), g0 + tid, NT, g1, a.c, k, k.k1 != 0.f);
+    __syncthreads();
     if constexpr (TEACHER) {
-        __syncthreads();
         write_set_gradient<T, NT>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, p_m, p_scale, q_scale);
+    } else {
+        if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, k, hit);
     }
 }
 
@@ -935,9 +1018,15 @@ constexpr int64_t kMostBlocks = 0x7fffffff;
 
 template <class T, int NT, int MODE> inline int forward_with(const LossArgs &a, int cluster, cudaStream_t stream)
 {
-    constexpr size_t smem = MODE == kLogprobsTop ? sizeof(uint64_t) * (NT * 8 + 512) + sizeof(TopShared)
-                            : MODE == kDistillTail ? sizeof(TeacherShared) + 4 * kBitmapWords
-                            : MODE == kDistill     ? sizeof(TeacherShared) : 0;
+    size_t smem = 0;
+    if (MODE == kDistill) smem = sizeof(TeacherShared);
+    if (MODE == kDistillTail) smem = sizeof(TeacherShared) + 4 * kBitmapWords;
+    if (MODE == kLogprobsTop) {
+        const int64_t steps = (most_granules<T>(a.V) / cluster + NT * 4) / (NT * 4);
+        smem = sizeof(TopShared) + sizeof(uint32_t) * NT * static_cast<size_t>(steps < kGroupSteps ? steps + 1 : kGroupSteps + 1);
+        SPDY_EVAL_TRY(cudaFuncSetAttribute(loss_forward_kernel<T, NT, 4, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           static_cast<int>(sizeof(TopShared) + sizeof(uint32_t) * NT * (kGroupSteps + 1))));
+    }
     return launch_clusters(loss_forward_kernel<T, NT, 4, MODE>, a.R, cluster, NT, smem, stream, a);
 }
 
