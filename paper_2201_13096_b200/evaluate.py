@@ -54,6 +54,7 @@ def _load():
     """The product library, whichever build ``binding`` has selected for the solver."""
     global _lib
     if _lib is None:
+        _import_torch()
         lib = binding.open_library(binding.LIB_PATH)
         vp, i32, i64, f32, size, cint = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t,
                                          ctypes.c_int)
@@ -83,76 +84,82 @@ def library():
     return _load()
 
 
-_TYPES = None
+# PyTorch, imported with the library (the package itself imports without it).
+torch = None
+_TYPES = {}
+_current_stream = _current_device = None
+
+
+def _import_torch():
+    global torch, _current_stream, _current_device
+    import torch as t
+
+    _TYPES.update({t.float32: 0, t.bfloat16: 1, t.float16: 2})
+    # the handle of the current stream as a number, without an object around it (small calls are bound by the host)
+    _current_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda i: t.cuda.current_stream(i).cuda_stream)
+    _current_device = getattr(t._C, "_cuda_getDevice", None) or t.cuda.current_device
+    torch = t
 
 
 def _dtype(t, what: str) -> int:
-    global _TYPES
-    if _TYPES is None:
-        import torch
-
-        _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
     code = _TYPES.get(t.dtype)
     if code is None:
         raise ValueError(f"{what} must be float32, bfloat16 or float16")
     return code
 
 
-def _matrix(t, what: str, rows: Optional[int] = None, cols: Optional[int] = None, dtype=None, device=None) -> int:
-    """Checks a 2-D CUDA tensor with unit column stride; its row stride in elements."""
-    if not t.is_cuda or t.dim() != 2:
+def _rows(t, what: str):
+    """(rows, columns, row stride in elements, device index) of a 2-D CUDA tensor with unit column stride."""
+    if not t.is_cuda or t.ndim != 2:
         raise ValueError(f"{what} must be a 2-D CUDA tensor")
-    r, c = t.shape
-    if (rows is not None and r != rows) or (cols is not None and c != cols):
-        raise ValueError(f"{what} must be [{'*' if rows is None else rows}][{'*' if cols is None else cols}]")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{what} must be {dtype}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{what} must be on {device}")
-    s0, s1 = t.stride()
-    if c > 1 and s1 != 1:
+    (r, c), (s0, s1) = t.shape, t.stride()
+    if s1 != 1 and c > 1:
         raise ValueError(f"{what} must have unit column stride")
-    if r <= 1:
-        return c if s0 < c else s0
     if s0 < c:
-        raise ValueError(f"{what} must not have overlapping rows")
-    return s0
+        if r > 1:
+            raise ValueError(f"{what} must not have overlapping rows")
+        s0 = c
+    return r, c, s0, t.get_device()
 
 
-def _vector(t, what: str, n: int, device, dtype=None):
-    if not t.is_cuda or t.dim() != 1 or t.shape[0] != n or t.device != device or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{what} must be a contiguous [{n}] tensor on {device}")
+def _like(t, what: str, rows: int, cols: int, dtype, device: int) -> int:
+    """The row stride of a matrix that has to have this shape, type and device."""
+    r, c, ld, dev = _rows(t, what)
+    if r != rows or c != cols or dev != device or t.dtype != dtype:
+        raise ValueError(f"{what} must be [{rows}][{cols}] of {dtype} on cuda:{device}")
+    return ld
+
+
+def _vector(t, what: str, n: int, device: int, dtype=None):
+    if t.ndim != 1 or t.shape[0] != n or t.get_device() != device or (n > 1 and not t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous [{n}] tensor on cuda:{device}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}")
     return t.data_ptr()
 
 
-def _ids(t, what: str, shape, device) -> int:
-    import torch
-
-    if t.dtype not in (torch.int64, torch.int32):
+def _ids(t, what: str, shape, device: int) -> int:
+    bits = 64 if t.dtype == torch.int64 else 32 if t.dtype == torch.int32 else 0
+    if not bits:
         raise ValueError(f"{what} must be int32 or int64")
-    if tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous {list(shape)} tensor on {device}")
-    return 64 if t.dtype == torch.int64 else 32
+    if t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {list(shape)} tensor on cuda:{device}")
+    return bits
 
 
 class _Scope:
     """Current device and stream for the duration of a call: memory comes from the stream the work runs on."""
 
-    def __init__(self, device, stream):
-        import torch
+    __slots__ = ("_stack", "handle")
 
+    def __init__(self, device: int, stream):
         self._stack = None
-        if torch.cuda.current_device() != device.index or stream is not None:
+        if stream is not None or _current_device() != device:
+            if stream is not None and stream.device_index != device:
+                raise ValueError("the stream must be on the tensors' device")
             self._stack = contextlib.ExitStack()
-            self._stack.enter_context(torch.cuda.device(device))
-            if stream is not None:
-                if stream.device != device:
-                    self._stack.close()
-                    raise ValueError("the stream must be on the tensors' device")
-                self._stack.enter_context(torch.cuda.stream(stream))
-        self.handle = torch.cuda.current_stream().cuda_stream
+            self._stack.enter_context(torch.cuda.device(device) if stream is None else torch.cuda.stream(stream))
+        self.handle = _current_stream(device)
 
     def __enter__(self):
         return self.handle
@@ -166,49 +173,52 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _workspace(nbytes: int, device):
-    import torch
-
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-
-
 def linear(x, weight, bias=None, residual=None, activation: str = "none", out=None, out_dtype=None, stream=None):
     """``spdy_linear``: ``act(x @ weight.T + bias) + residual``.
 
     ``x`` [M][K] and ``weight`` [N][K] bfloat16 or float16 (the same), ``bias`` [N] of that type or float32, ``residual``
     [M][N] of that type; ``activation`` one of "none", "relu", "gelu" (with erf), "silu".  The result is ``out`` if given,
     else a new tensor of ``out_dtype`` (default: ``x``'s type; float32 is the other choice).  ``out`` may be ``residual``."""
-    import torch
-
-    if activation not in ACTIVATIONS:
+    lib = _lib or _load()
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
-    if x.dtype not in (torch.bfloat16, torch.float16):
+    dtype = x.dtype
+    code = _TYPES.get(dtype, 0)
+    if not code:
         raise ValueError("x must be bfloat16 or float16")
-    ldx = _matrix(x, "x")
-    M, K = x.shape
-    dev = x.device
-    ldw = _matrix(weight, "weight", cols=K, dtype=x.dtype, device=dev)
-    N = weight.shape[0]
+    M, K, ldx, dev = _rows(x, "x")
+    N, k, ldw, wdev = _rows(weight, "weight")
+    if k != K or wdev != dev or weight.dtype != dtype:
+        raise ValueError(f"weight must be [N][{K}] of {dtype} on cuda:{dev}")
+    pb, bcode, pr, ldres = None, 0, None, 0
     if bias is not None:
-        _vector(bias, "bias", N, dev)
-        if bias.dtype not in (x.dtype, torch.float32):
+        pb, bcode = _vector(bias, "bias", N, dev), _TYPES.get(bias.dtype, -1)
+        if bcode and bcode != code:
             raise ValueError("bias must have x's type or be float32")
-    ldres = 0 if residual is None else _matrix(residual, "residual", M, N, x.dtype, dev)
-    lib, code = _load(), _dtype(x, "x")
+    if residual is not None:
+        pr, ldres = residual.data_ptr(), _like(residual, "residual", M, N, dtype, dev)
     with _Scope(dev, stream) as handle:
         if out is None:
-            out = torch.empty((M, N), dtype=x.dtype if out_dtype is None else out_dtype, device=dev)
-        elif out_dtype is not None and out.dtype != out_dtype:
-            raise ValueError("out must have out_dtype")
-        if out.dtype not in (x.dtype, torch.float32):
+            out = x.new_empty((M, N)) if out_dtype is None else x.new_empty((M, N), dtype=out_dtype)
+            ldy = N
+        else:
+            if out_dtype is not None and out.dtype != out_dtype:
+                raise ValueError("out must have out_dtype")
+            ldy = _like(out, "out", M, N, out.dtype, dev)
+        ocode = _TYPES.get(out.dtype, -1)
+        if ocode and ocode != code:
             raise ValueError("the result must have x's type or be float32")
-        ldy = _matrix(out, "out", M, N, device=dev)
         px, pw = x.data_ptr(), weight.data_ptr()
-        need = lib.spdy_linear_workspace_bytes(px, ldx, pw, ldw, code, M, N, K)
-        ws = _workspace(need, dev)
-        binding._check(lib.spdy_linear(px, ldx, pw, ldw, code, _ptr(bias), 0 if bias is None else _dtype(bias, "bias"),
-                                       _ptr(residual), ldres, ACTIVATIONS[activation], M, N, K, out.data_ptr(), ldy,
-                                       _dtype(out, "out"), _ptr(ws), need, handle), "spdy_linear")
+        pws, need = None, 0
+        if (px | pw | ldx * 2 | ldw * 2) & 15 or M > 8:
+            need = lib.spdy_linear_workspace_bytes(px, ldx, pw, ldw, code, M, N, K)
+            if need:
+                ws = x.new_empty(need, dtype=torch.uint8)
+                pws = ws.data_ptr()
+        rc = lib.spdy_linear(px, ldx, pw, ldw, code, pb, bcode, pr, ldres, act, M, N, K, out.data_ptr(), ldy, ocode, pws, need, handle)
+    if rc:
+        binding._check(rc, "spdy_linear")
     return out
 
 
@@ -217,121 +227,124 @@ def linear_check_status(stream=None):
     binding._check(_load().spdy_linear_check_status(binding._stream_handle(stream)), "spdy_linear_check_status")
 
 
-def _norm_params(x, weight, bias):
-    import torch
-
+def _norm_params(x, weight, bias, D, dev, code):
     kind = None
     for name, p in (("weight", weight), ("bias", bias)):
         if p is None:
             continue
-        _vector(p, name, x.shape[1], x.device)
-        if p.dtype not in (x.dtype, torch.float32) or (kind is not None and p.dtype != kind):
+        _vector(p, name, D, dev)
+        c = _TYPES.get(p.dtype, -1)
+        if (c and c != code) or (kind is not None and c != kind):
             raise ValueError("weight and bias must both have x's type or both be float32")
-        kind = p.dtype
-    return 0 if kind is None else (0 if kind == torch.float32 else _dtype(x, "x"))
+        kind = c
+    return kind or 0
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=None):
     """``spdy_layer_norm``: (y, mean, rstd) of ``x`` [R][D] (float32, bfloat16 or float16); ``weight`` and ``bias`` [D] of
     ``x``'s type or float32, or None.  ``mean`` and ``rstd`` [R] are float32.  ``out`` may be ``x``."""
-    import torch
-
-    code, ldx = _dtype(x, "x"), _matrix(x, "x")
-    R, D = x.shape
-    kind = _norm_params(x, weight, bias)
-    lib = _load()
-    with _Scope(x.device, stream) as handle:
+    lib = _lib or _load()
+    R, D, ldx, dev = _rows(x, "x")
+    code = _dtype(x, "x")
+    kind = _norm_params(x, weight, bias, D, dev, code)
+    with _Scope(dev, stream) as handle:
         if out is None:
-            out = torch.empty((R, D), dtype=x.dtype, device=x.device)
-        ldy = _matrix(out, "out", R, D, x.dtype, x.device)
-        stats = torch.empty((2, R), dtype=torch.float32, device=x.device)
-        mean, rstd = stats.unbind(0)
-        binding._check(lib.spdy_layer_norm(x.data_ptr(), ldx, code, _ptr(weight), _ptr(bias), kind, R, D, eps, out.data_ptr(), ldy,
-                                           mean.data_ptr(), rstd.data_ptr(), handle), "spdy_layer_norm")
-    return out, mean, rstd
+            out, ldy = x.new_empty((R, D)), D
+        else:
+            ldy = _like(out, "out", R, D, x.dtype, dev)
+        stats = x.new_empty((2, R), dtype=torch.float32)
+        p = stats.data_ptr()
+        rc = lib.spdy_layer_norm(x.data_ptr(), ldx, code, _ptr(weight), _ptr(bias), kind, R, D, eps, out.data_ptr(), ldy, p, p + 4 * R,
+                                 handle)
+    if rc:
+        binding._check(rc, "spdy_layer_norm")
+    return (out, *stats.unbind(0))
 
 
 def layer_norm_backward(dy, x, weight, mean, rstd, out=None, params: bool = True, stream=None):
     """``spdy_layer_norm_backward``: (dx, dweight, dbias) from the gradient ``dy`` [R][D] of ``layer_norm``'s result, its input
     ``x`` and its ``mean`` and ``rstd``.  ``dx`` has ``x``'s type, ``dweight`` and ``dbias`` [D] are float32 (None with
     ``params=False``).  ``out`` receives ``dx`` and may be ``dy`` or ``x``."""
-    import torch
-
-    code, ldx = _dtype(x, "x"), _matrix(x, "x")
-    R, D = x.shape
-    dev = x.device
-    lddy = _matrix(dy, "dy", R, D, x.dtype, dev)
-    kind = _norm_params(x, weight, None)
+    lib = _lib or _load()
+    R, D, ldx, dev = _rows(x, "x")
+    code = _dtype(x, "x")
+    lddy = _like(dy, "dy", R, D, x.dtype, dev)
+    kind = _norm_params(x, weight, None, D, dev, code)
     pm, pr = _vector(mean, "mean", R, dev, torch.float32), _vector(rstd, "rstd", R, dev, torch.float32)
-    lib = _load()
     with _Scope(dev, stream) as handle:
         if out is None:
-            out = torch.empty((R, D), dtype=x.dtype, device=dev)
-        lddx = _matrix(out, "out", R, D, x.dtype, dev)
-        dw = db = ws = None
+            out, lddx = x.new_empty((R, D)), D
+        else:
+            lddx = _like(out, "out", R, D, x.dtype, dev)
+        dw = db = pw = pb = pws = None
         need = 0
         if params:
-            dw, db = torch.empty((2, D), dtype=torch.float32, device=dev).unbind(0)
+            grads = x.new_empty((2, D), dtype=torch.float32)
+            dw, db = grads.unbind(0)
+            pw = grads.data_ptr()
+            pb = pw + 4 * D
             need = lib.spdy_layer_norm_backward_workspace_bytes(R, D, code)
-            ws = _workspace(need, dev)
-        binding._check(lib.spdy_layer_norm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, code, _ptr(weight), kind, pm, pr, R, D,
-                                                    out.data_ptr(), lddx, _ptr(dw), _ptr(db), _ptr(ws), need, handle),
-                       "spdy_layer_norm_backward")
+            if need:
+                ws = x.new_empty(need, dtype=torch.uint8)
+                pws = ws.data_ptr()
+        rc = lib.spdy_layer_norm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, code, _ptr(weight), kind, pm, pr, R, D, out.data_ptr(),
+                                          lddx, pw, pb, pws, need, handle)
+    if rc:
+        binding._check(rc, "spdy_layer_norm_backward")
     return out, dw, db
 
 
 def _logits(logits):
-    code, ld = _dtype(logits, "logits"), _matrix(logits, "logits")
-    return code, ld, logits.shape[0], logits.shape[1], logits.device
+    """(pointer, row stride, type) as the C calls take them, and (rows, columns, device index)."""
+    R, V, ld, dev = _rows(logits, "logits")
+    return (logits.data_ptr(), ld, _dtype(logits, "logits")), R, V, dev
 
 
 def _grads_out(out, logits, R, V, dev):
-    import torch
-
     if out is None:
-        out = torch.empty((R, V), dtype=logits.dtype, device=dev)
-    return out, _matrix(out, "out", R, V, logits.dtype, dev)
+        return logits.new_empty((R, V)), V
+    return out, _like(out, "out", R, V, logits.dtype, dev)
+
+
+def _optional(R, dev, **vectors):
+    return [None if t is None else _vector(t, name, R, dev, torch.float32) for name, t in vectors.items()]
 
 
 def token_logprobs(logits, tokens, top_k: int = 0, temperature: float = 1.0, stream=None) -> TokenLogprobs:
     """``spdy_token_logprobs``: log probability of ``tokens`` [R] (int32 or int64; negative = none) under
     softmax(``logits`` [R][V] / ``temperature``), entropy and lse of each row, and with ``top_k`` > 0 the ids (int32) and log
     probabilities of its most probable ids, best first, equal logits by ascending id."""
-    import torch
-
-    code, ld, R, V, dev = _logits(logits)
+    lib = _lib or _load()
+    head, R, V, dev = _logits(logits)
     bits = _ids(tokens, "tokens", (R,), dev)
     top_k = int(top_k)
-    lib = _load()
     with _Scope(dev, stream) as handle:
-        logprob, entropy, lse = torch.empty((3, R), dtype=torch.float32, device=dev).unbind(0)
-        ids = lps = None
+        stats = logits.new_empty((3, R), dtype=torch.float32)
+        p = stats.data_ptr()
+        ids = lps = pi = pl = None
         if top_k > 0:
-            ids = torch.empty((R, top_k), dtype=torch.int32, device=dev)
-            lps = torch.empty((R, top_k), dtype=torch.float32, device=dev)
-        binding._check(lib.spdy_token_logprobs(logits.data_ptr(), ld, code, tokens.data_ptr(), bits, R, V, temperature, top_k,
-                                               logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), _ptr(ids), _ptr(lps),
-                                               handle), "spdy_token_logprobs")
-    return TokenLogprobs(logprob, entropy, lse, ids, lps)
+            ids = logits.new_empty((R, top_k), dtype=torch.int32)
+            lps = logits.new_empty((R, top_k), dtype=torch.float32)
+            pi, pl = ids.data_ptr(), lps.data_ptr()
+        rc = lib.spdy_token_logprobs(*head, tokens.data_ptr(), bits, R, V, temperature, top_k, p, p + 4 * R, p + 8 * R, pi, pl, handle)
+    if rc:
+        binding._check(rc, "spdy_token_logprobs")
+    return TokenLogprobs(*stats.unbind(0), ids, lps)
 
 
 def token_logprobs_backward(logits, tokens, lse, entropy=None, grad_logprob=None, grad_entropy=None, temperature: float = 1.0,
                             out=None, stream=None):
     """``spdy_token_logprobs_backward``: the gradient [R][V] (``logits``' type) of ``sum(grad_logprob * logprob + grad_entropy *
     entropy)``, from the forward call's ``lse`` and (with ``grad_entropy``) ``entropy``.  ``out`` may be ``logits``."""
-    import torch
-
-    code, ld, R, V, dev = _logits(logits)
+    lib = _lib or _load()
+    head, R, V, dev = _logits(logits)
     bits = _ids(tokens, "tokens", (R,), dev)
-    for name, t in (("lse", lse), ("entropy", entropy), ("grad_logprob", grad_logprob), ("grad_entropy", grad_entropy)):
-        if t is not None:
-            _vector(t, name, R, dev, torch.float32)
-    lib = _load()
+    vectors = _optional(R, dev, lse=lse, entropy=entropy, grad_logprob=grad_logprob, grad_entropy=grad_entropy)
     with _Scope(dev, stream) as handle:
         out, ldo = _grads_out(out, logits, R, V, dev)
-        binding._check(lib.spdy_token_logprobs_backward(logits.data_ptr(), ld, code, tokens.data_ptr(), bits, R, V, temperature,
-                                                        _ptr(lse), _ptr(entropy), _ptr(grad_logprob), _ptr(grad_entropy),
-                                                        out.data_ptr(), ldo, handle), "spdy_token_logprobs_backward")
+        rc = lib.spdy_token_logprobs_backward(*head, tokens.data_ptr(), bits, R, V, temperature, *vectors, out.data_ptr(), ldo, handle)
+    if rc:
+        binding._check(rc, "spdy_token_logprobs_backward")
     return out
 
 
@@ -339,34 +352,31 @@ def token_logprobs_with_grad(logits, tokens, grad_logprob=None, grad_entropy=Non
                              stream=None):
     """``spdy_token_logprobs_with_grad``: (``TokenLogprobs``, gradient) in one call, for a loss whose weights per row are known
     beforehand.  ``out`` receives the gradient and may be ``logits``."""
-    import torch
-
-    code, ld, R, V, dev = _logits(logits)
+    lib = _lib or _load()
+    head, R, V, dev = _logits(logits)
     bits = _ids(tokens, "tokens", (R,), dev)
-    for name, t in (("grad_logprob", grad_logprob), ("grad_entropy", grad_entropy)):
-        if t is not None:
-            _vector(t, name, R, dev, torch.float32)
-    lib = _load()
+    vectors = _optional(R, dev, grad_logprob=grad_logprob, grad_entropy=grad_entropy)
     with _Scope(dev, stream) as handle:
         out, ldo = _grads_out(out, logits, R, V, dev)
-        logprob, entropy, lse = torch.empty((3, R), dtype=torch.float32, device=dev).unbind(0)
-        binding._check(lib.spdy_token_logprobs_with_grad(logits.data_ptr(), ld, code, tokens.data_ptr(), bits, R, V, temperature,
-                                                         _ptr(grad_logprob), _ptr(grad_entropy), logprob.data_ptr(),
-                                                         entropy.data_ptr(), lse.data_ptr(), out.data_ptr(), ldo, handle),
-                       "spdy_token_logprobs_with_grad")
-    return TokenLogprobs(logprob, entropy, lse), out
+        stats = logits.new_empty((3, R), dtype=torch.float32)
+        p = stats.data_ptr()
+        rc = lib.spdy_token_logprobs_with_grad(*head, tokens.data_ptr(), bits, R, V, temperature, *vectors, p, p + 4 * R, p + 8 * R,
+                                               out.data_ptr(), ldo, handle)
+    if rc:
+        binding._check(rc, "spdy_token_logprobs_with_grad")
+    return TokenLogprobs(*stats.unbind(0)), out
 
 
 def _teacher(top_ids, top_logprobs, R, dev):
-    import torch
-
-    if top_ids.dim() != 2:
+    """(ids' pointer, their bits, log probabilities' pointer) as the C calls take them, and K."""
+    if top_ids.ndim != 2:
         raise ValueError("top_ids must be [R][K]")
     K = top_ids.shape[1]
     bits = _ids(top_ids, "top_ids", (R, K), dev)
-    if tuple(top_logprobs.shape) != (R, K) or top_logprobs.dtype != torch.float32 or top_logprobs.device != dev or not top_logprobs.is_contiguous():
+    if (top_logprobs.shape != (R, K) or top_logprobs.dtype != torch.float32 or top_logprobs.get_device() != dev
+            or not top_logprobs.is_contiguous()):
         raise ValueError("top_logprobs must be a contiguous float32 tensor like top_ids")
-    return bits, K
+    return (top_ids.data_ptr(), bits, top_logprobs.data_ptr()), K
 
 
 def distill_loss(logits, top_ids, top_logprobs, temperature: float = 1.0, tail: bool = True, stream=None) -> DistillLoss:
@@ -374,38 +384,33 @@ def distill_loss(logits, top_ids, top_logprobs, temperature: float = 1.0, tail: 
     probabilities [R][K] (float32, at the same temperature) at ``top_ids`` [R][K] (negative = no entry).  With ``tail`` the
     teacher's remaining mass is compared with the student's mass outside the ids; without, the teacher is renormalised over
     them.  Rows are not averaged."""
-    import torch
-
-    code, ld, R, V, dev = _logits(logits)
-    bits, K = _teacher(top_ids, top_logprobs, R, dev)
-    lib = _load()
+    lib = _lib or _load()
+    head, R, V, dev = _logits(logits)
+    teacher, K = _teacher(top_ids, top_logprobs, R, dev)
     with _Scope(dev, stream) as handle:
-        loss, lse, rest = torch.empty((3, R), dtype=torch.float32, device=dev).unbind(0)
-        binding._check(lib.spdy_distill_loss(logits.data_ptr(), ld, code, top_ids.data_ptr(), bits, top_logprobs.data_ptr(), R, V, K,
-                                             temperature, bool(tail), loss.data_ptr(), lse.data_ptr(),
-                                             rest.data_ptr() if tail else None, handle), "spdy_distill_loss")
-    return DistillLoss(loss, lse, rest if tail else None)
+        stats = logits.new_empty((3, R) if tail else (2, R), dtype=torch.float32)
+        p = stats.data_ptr()
+        rc = lib.spdy_distill_loss(*head, *teacher, R, V, K, temperature, bool(tail), p, p + 4 * R, p + 8 * R if tail else None, handle)
+    if rc:
+        binding._check(rc, "spdy_distill_loss")
+    return DistillLoss(*stats.unbind(0))
 
 
 def distill_loss_backward(logits, top_ids, top_logprobs, lse, rest, grad_loss, temperature: float = 1.0, tail: bool = True,
                           out=None, stream=None):
     """``spdy_distill_loss_backward``: the gradient [R][V] (``logits``' type) of ``sum(grad_loss * loss)`` from the forward call's
     ``lse`` and ``rest`` (None without ``tail``).  ``out`` may be ``logits``."""
-    import torch
-
-    code, ld, R, V, dev = _logits(logits)
-    bits, K = _teacher(top_ids, top_logprobs, R, dev)
+    lib = _lib or _load()
+    head, R, V, dev = _logits(logits)
+    teacher, K = _teacher(top_ids, top_logprobs, R, dev)
     if tail and rest is None:
         raise ValueError("rest is needed with tail")
-    for name, t in (("lse", lse), ("rest", rest if tail else None), ("grad_loss", grad_loss)):
-        if t is not None:
-            _vector(t, name, R, dev, torch.float32)
-    lib = _load()
+    vectors = _optional(R, dev, lse=lse, rest=rest if tail else None, grad_loss=grad_loss)
     with _Scope(dev, stream) as handle:
         out, ldo = _grads_out(out, logits, R, V, dev)
-        binding._check(lib.spdy_distill_loss_backward(logits.data_ptr(), ld, code, top_ids.data_ptr(), bits, top_logprobs.data_ptr(), R,
-                                                      V, K, temperature, bool(tail), _ptr(lse), _ptr(rest) if tail else None,
-                                                      _ptr(grad_loss), out.data_ptr(), ldo, handle), "spdy_distill_loss_backward")
+        rc = lib.spdy_distill_loss_backward(*head, *teacher, R, V, K, temperature, bool(tail), *vectors, out.data_ptr(), ldo, handle)
+    if rc:
+        binding._check(rc, "spdy_distill_loss_backward")
     return out
 
 
@@ -413,17 +418,16 @@ def distill_loss_with_grad(logits, top_ids, top_logprobs, grad_loss, temperature
                            stream=None):
     """``spdy_distill_loss_with_grad``: (``DistillLoss``, gradient) in one call.  ``out`` receives the gradient and may be
     ``logits``."""
-    import torch
-
-    code, ld, R, V, dev = _logits(logits)
-    bits, K = _teacher(top_ids, top_logprobs, R, dev)
-    _vector(grad_loss, "grad_loss", R, dev, torch.float32)
-    lib = _load()
+    lib = _lib or _load()
+    head, R, V, dev = _logits(logits)
+    teacher, K = _teacher(top_ids, top_logprobs, R, dev)
+    pg = _vector(grad_loss, "grad_loss", R, dev, torch.float32)
     with _Scope(dev, stream) as handle:
         out, ldo = _grads_out(out, logits, R, V, dev)
-        loss, lse, rest = torch.empty((3, R), dtype=torch.float32, device=dev).unbind(0)
-        binding._check(lib.spdy_distill_loss_with_grad(logits.data_ptr(), ld, code, top_ids.data_ptr(), bits, top_logprobs.data_ptr(),
-                                                       R, V, K, temperature, bool(tail), grad_loss.data_ptr(), loss.data_ptr(),
-                                                       lse.data_ptr(), rest.data_ptr() if tail else None, out.data_ptr(), ldo,
-                                                       handle), "spdy_distill_loss_with_grad")
-    return DistillLoss(loss, lse, rest if tail else None), out
+        stats = logits.new_empty((3, R) if tail else (2, R), dtype=torch.float32)
+        p = stats.data_ptr()
+        rc = lib.spdy_distill_loss_with_grad(*head, *teacher, R, V, K, temperature, bool(tail), pg, p, p + 4 * R,
+                                             p + 8 * R if tail else None, out.data_ptr(), ldo, handle)
+    if rc:
+        binding._check(rc, "spdy_distill_loss_with_grad")
+    return DistillLoss(*stats.unbind(0)), out
