@@ -168,6 +168,36 @@ template <> struct Elem<__half> {
     }
 };
 
+// Granules that lie only partly inside a row of n elements, from element e (of row p or q) on: kept out of line, they are few.
+template <class T> __device__ __noinline__ uint4 load_part(const T *p, int n, int e)
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j, e += 4 / static_cast<int>(sizeof(T))) {
+        w[j] = Elem<T>::kNegInfWord;
+        if (sizeof(T) == 4) {
+            if (e >= 0 && e < n) w[j] = reinterpret_cast<const uint32_t *>(p)[e];
+        } else {
+            if (e >= 0 && e < n) w[j] = (w[j] & 0xffff0000u) | reinterpret_cast<const uint16_t *>(p)[e];
+            if (e + 1 >= 0 && e + 1 < n) w[j] = (w[j] & 0xffffu) | static_cast<uint32_t>(reinterpret_cast<const uint16_t *>(p)[e + 1]) << 16;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <class T> __device__ __noinline__ void store_part(T *q, int n, int e, uint4 v)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j, e += 4 / static_cast<int>(sizeof(T))) {
+        if (sizeof(T) == 4) {
+            if (e >= 0 && e < n) reinterpret_cast<uint32_t *>(q)[e] = w[j];
+        } else {
+            if (e >= 0 && e < n) reinterpret_cast<uint16_t *>(q)[e] = static_cast<uint16_t>(w[j]);
+            if (e + 1 >= 0 && e + 1 < n) reinterpret_cast<uint16_t *>(q)[e + 1] = static_cast<uint16_t>(w[j] >> 16);
+        }
+    }
+}
+
 // A row that may start anywhere: granule g is the g-th aligned 16 bytes that hold a part of it, elements
 // g * kVec - lead .. + kVec - 1.  Only granules that lie wholly inside the row (lo <= g < hi) are moved 16 bytes at a time.
 template <class T> struct Row {
@@ -184,44 +214,26 @@ template <class T> struct Row {
     __device__ __forceinline__ int granules() const { return (n + lead + Elem<T>::kVec - 1) / Elem<T>::kVec; }
     __device__ __forceinline__ int first(int g) const { return g * Elem<T>::kVec - lead; }
     __device__ __forceinline__ bool whole(int g) const { return static_cast<unsigned>(g - lo) < static_cast<unsigned>(max(hi - lo, 0)); }
-    __device__ __noinline__ uint4 load_part(int g) const
-    {
-        const int e = first(g);
-        float f[Elem<T>::kVec];
-#pragma unroll
-        for (int i = 0; i < Elem<T>::kVec; ++i) f[i] = (e + i >= 0 && e + i < n) ? Elem<T>::to_float(p[e + i]) : neg_inf();
-        return Elem<T>::pack(f);
-    }
     // elements outside the row read as -inf
     __device__ __forceinline__ uint4 load(int g) const
     {
         if (whole(g)) return load_stream(p + first(g));
-        return load_part(g);
+        return load_part(p, n, first(g));
     }
     // the same, nothing but -inf from granule `limit` on
     __device__ __forceinline__ uint4 load_below(int g, int limit) const
     {
         constexpr uint32_t NI = Elem<T>::kNegInfWord;
         if (whole(g) && g < limit) return load_stream(p + first(g));
-        if (g < limit) return load_part(g);
+        if (g < limit) return load_part(p, n, first(g));
         return make_uint4(NI, NI, NI, NI);
     }
-    // v, converted already, to granule g's elements of `q`, a row of as many elements that may start elsewhere
-    __device__ __noinline__ void store_part(T *q, int g, uint4 v) const
-    {
-        const int e = first(g);
-        float f[Elem<T>::kVec];
-        Elem<T>::unpack(v, f);
-#pragma unroll
-        for (int i = 0; i < Elem<T>::kVec; ++i)
-            if (e + i >= 0 && e + i < n) q[e + i] = Elem<T>::from_float(f[i]);
-    }
     __device__ __forceinline__ bool same_lead(const T *q) const { return (reinterpret_cast<uintptr_t>(q) & 15) == (reinterpret_cast<uintptr_t>(p) & 15); }
-    // `same`: same_lead(q)
+    // v, converted already, to granule g's elements of `q`, a row of as many elements that may start elsewhere; `same`: same_lead(q)
     __device__ __forceinline__ void store(T *q, bool same, int g, uint4 v) const
     {
         if (same && whole(g)) store_stream(q + first(g), v);
-        else store_part(q, g, v);
+        else store_part(q, n, first(g), v);
     }
 };
 

@@ -21,14 +21,14 @@ LossArgs base_args(const void *logits, int64_t ld, const void *ids, int bits, co
 
 int run_forward(const LossArgs &a, int dtype, int tail, cudaStream_t stream)
 {
-    if (tail) return SPDY_EVAL_BY_TYPE(dtype, (forward<T, kDistillTail>(a, stream)));
-    return SPDY_EVAL_BY_TYPE(dtype, (forward<T, kDistill>(a, stream)));
+    if (tail) return SPDY_EVAL_BY_TYPE(dtype, (rows<T, kDistillTail, kNoGrad>(a, stream)));
+    return SPDY_EVAL_BY_TYPE(dtype, (rows<T, kDistill, kNoGrad>(a, stream)));
 }
 
 int run_backward(const LossArgs &a, int dtype, int tail, cudaStream_t stream)
 {
-    if (tail) return SPDY_EVAL_BY_TYPE(dtype, (backward<T, true, true>(a, stream)));
-    return SPDY_EVAL_BY_TYPE(dtype, (backward<T, true, false>(a, stream)));
+    if (tail) return SPDY_EVAL_BY_TYPE(dtype, (backward<T, kDistillTail>(a, stream)));
+    return SPDY_EVAL_BY_TYPE(dtype, (backward<T, kDistill>(a, stream)));
 }
 
 }  // namespace
@@ -71,13 +71,8 @@ int spdy_distill_loss_with_grad(const void *logits, int64_t ld, int dtype, const
     LossArgs a = base_args(logits, ld, ids, index_bits, top_logprobs, R, V, K, temperature);
     a.loss = loss, a.lse = lse, a.rest = rest, a.grad = grad_loss, a.dlogits = dlogits, a.lddl = lddl;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    bool fits = false;
-    const int rc = tail ? SPDY_EVAL_BY_TYPE(dtype, (resident<T, true, true>(a, stream, fits))) : SPDY_EVAL_BY_TYPE(dtype, (resident<T, true, false>(a, stream, fits)));
-    if (rc != SPDY_OK || fits) return rc;
-    const int fwd = run_forward(a, dtype, tail, stream);
-    if (fwd != SPDY_OK) return fwd;
-    a.in_lse = lse, a.in_rest = rest;
-    return run_backward(a, dtype, tail, stream);
+    if (tail) return SPDY_EVAL_BY_TYPE(dtype, (rows<T, kDistillTail, kGrad>(a, stream)));
+    return SPDY_EVAL_BY_TYPE(dtype, (rows<T, kDistill, kGrad>(a, stream)));
 }
 
 }  // extern "C"

@@ -185,10 +185,11 @@ __device__ __forceinline__ uint64_t warp_nth_key(uint32_t value, uint32_t index,
     return last;
 }
 
-constexpr int kCandidates = 2048;
+constexpr int kCandidates = 1536, kListed = 512;
 
 struct TopShared {
     uint64_t cand[kCandidates];
+    uint64_t list[kListed];
     uint64_t best[SPDY_TOP_MAX];  // the result, descending
     uint64_t tau[32];
     uint32_t count, count2;
@@ -225,6 +226,7 @@ template <int NT> __device__ __noinline__ void select_top(TopShared &sh, int n, 
         const uint64_t k = sh.cand[i];
         if (k < least) continue;
         int rank = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) rank += sh.cand[j] > k;
         if (rank < want) sh.best[rank] = k;
     }
@@ -287,106 +289,89 @@ template <class T, int NT> __device__ __noinline__ void radix_top(TopShared &sh,
 // While a block streams its part of a row, each thread notes the largest element of each of its groups (the U granules of
 // one step, or of 2^shift steps in a row too long for `groups`) as an ordered 32-bit value, 0 for a group without elements.
 // Then the K-th largest group value v bounds the K-th largest element from below: elements above v lie in fewer than K
-// groups, which are read again; what is still missing are elements equal to v, those with the lowest ids.
+// groups, which are read again; what may still be missing are elements equal to v, those with the lowest ids.
 // `lane_best` is the thread's largest value over all its groups.  Result in sh.best[0..want).
 template <class T, int NT, int U>
 __device__ __noinline__ void find_top(TopShared &sh, const uint32_t *groups, int n_groups, int shift, uint32_t lane_best, const Row<T> &row, int g0, int g1, int want)
 {
-    constexpr int NW = NT / 32, STEP = NT * U;
+    constexpr int NW = NT / 32, STEP = NT * U, VEC = Elem<T>::kVec;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     // a cheap bound first: the r-th largest lane of every warp, r such that the warps together have `want` lanes above it
     const uint64_t mine = warp_nth_key(lane_best, static_cast<uint32_t>(lane), (want + NW - 1) / NW);
     if (lane == 0) sh.tau[warp] = mine >> 32;
-    if (tid == 0) sh.count = 0;
+    if (tid == 0) sh.count = 0, sh.want = 0;
     __syncthreads();
     const uint32_t tau = max(1u, __reduce_min_sync(0xffffffffu, lane < NW ? static_cast<uint32_t>(sh.tau[lane]) : 0xffffffffu));
     const int total = n_groups * NT;
+#pragma unroll 4
     for (int i = tid; i < total; i += NT)
         if (groups[i] >= tau) {
             const uint32_t at = atomicAdd(&sh.count, 1u);
-            if (at < 512) sh.cand[at] = static_cast<uint64_t>(groups[i]) << 32 | static_cast<uint32_t>(~i);
+            if (at < kListed) sh.list[at] = static_cast<uint64_t>(groups[i]) << 32 | static_cast<uint32_t>(~i);
         }
     __syncthreads();
-    const int listed = static_cast<int>(sh.count);
-    uint32_t v = 0;
-    if (listed > 512) {
+    int listed = static_cast<int>(sh.count);
+    uint32_t v = 0;  // stays 0 with fewer groups than `want`: every element is looked at
+    if (listed <= kListed) {
+        for (int i = tid; i < listed; i += NT) {
+            const uint64_t k = sh.list[i];
+            int rank = 0;
+#pragma unroll 8
+            for (int j = 0; j < listed; ++j) rank += sh.list[j] > k;
+            if (rank == want - 1) sh.want = static_cast<uint32_t>(k >> 32);
+        }
+        __syncthreads();
+        v = sh.want;
+    } else {
         for (int b = 31; b >= 0; --b) {
             const uint32_t trial = v | 1u << b;
             int count = 0;
             for (int i = tid; i < total; i += NT) count += groups[i] >= trial;
             if (block_count<NT>(sh, count) >= want) v = trial;
         }
-    } else {
-        if (tid == 0) sh.want = 0;  // fewer groups than `want`: every element is wanted or nearly
-        __syncthreads();
-        for (int i = tid; i < listed; i += NT) {
-            const uint64_t k = sh.cand[i];
-            int rank = 0;
-            for (int j = 0; j < listed; ++j) rank += sh.cand[j] > k;
-            if (rank == want - 1) sh.want = static_cast<uint32_t>(k >> 32);
-        }
-        __syncthreads();
-        v = sh.want;
     }
-    __syncthreads();
-    if (tid == 0) sh.count = 0;
-    __syncthreads();
-    // elements above v, and the number of groups whose largest is v
-    int ties = 0;
-    for (int i = tid; i < total; i += NT) {
-        if (groups[i] < v) continue;
-        ties += groups[i] == v;
-        if (groups[i] == v) continue;
-        const int base = g0 + (i / NT << shift) * STEP + i % NT;
-        for (int k = 0; k < (U << shift); ++k) {
-            const int g = base + k * NT;
-            if (g >= g1) break;
-            const int e = row.first(g);
-            float f[Elem<T>::kVec];
-            Elem<T>::unpack(row.load(g), f);
-#pragma unroll
-            for (int j = 0; j < Elem<T>::kVec; ++j) {
-                if (ordered(f[j]) <= v || e + j < 0 || e + j >= row.n) continue;
-                const uint32_t at = atomicAdd(&sh.count, 1u);
-                if (at < kCandidates) sh.cand[at] = rank_key(f[j], static_cast<uint32_t>(e + j));
-            }
-        }
-    }
+    // the groups that can hold one of the best: those above v, and those equal to v unless they are many
+    int ties = 0, above = 0;
+    for (int i = tid; i < total; i += NT) ties += groups[i] == v, above += groups[i] > v;
     ties = block_count<NT>(sh, ties);
-    const int above = static_cast<int>(sh.count);
+    above = block_count<NT>(sh, above);
+    const bool few = ties + above <= kListed && ties <= 64 + want;
+    const uint32_t least = few ? v : v + 1;
+    if (tid == 0) sh.count = sh.count2 = 0;
     __syncthreads();
-    if (above < want && ties <= 64) {
-        // few groups can hold an element equal to v: take them all
-        for (int i = tid; i < total; i += NT) {
-            if (groups[i] < v) continue;
-            const int base = g0 + (i / NT << shift) * STEP + i % NT;
-            for (int k = 0; k < (U << shift); ++k) {
-                const int g = base + k * NT;
-                if (g >= g1) break;
-                const int e = row.first(g);
-                float f[Elem<T>::kVec];
-                Elem<T>::unpack(row.load(g), f);
+    for (int i = tid; i < total; i += NT)
+        if (groups[i] >= least) sh.list[atomicAdd(&sh.count2, 1u)] = i;
+    __syncthreads();
+    listed = static_cast<int>(sh.count2);
+    const int each = U << shift;
+    for (int i = tid; i < listed * each; i += NT) {
+        const int slot = static_cast<int>(sh.list[i / each]);
+        const int g = g0 + (slot / NT << shift) * STEP + slot % NT + i % each * NT;
+        if (g >= g1) continue;
+        const int e = row.first(g);
+        float f[VEC];
+        Elem<T>::unpack(row.load(g), f);
 #pragma unroll
-                for (int j = 0; j < Elem<T>::kVec; ++j) {
-                    if (ordered(f[j]) != v || e + j < 0 || e + j >= row.n) continue;
-                    const uint32_t at = atomicAdd(&sh.count, 1u);
-                    if (at < kCandidates) sh.cand[at] = rank_key(f[j], static_cast<uint32_t>(e + j));
-                }
-            }
+        for (int j = 0; j < VEC; ++j) {
+            if (ordered(f[j]) < least || e + j < 0 || e + j >= row.n) continue;
+            const uint32_t at = atomicAdd(&sh.count, 1u);
+            if (at < kCandidates) sh.cand[at] = rank_key(f[j], static_cast<uint32_t>(e + j));
         }
-        __syncthreads();
-    } else if (above < want) {
-        // many (a masked or constant row): in ascending order from the row's start until there are enough
-        int have = above;
+    }
+    __syncthreads();
+    int have = static_cast<int>(sh.count);
+    __syncthreads();
+    if (!few && have < want) {
+        // many groups equal to v (a masked or constant row): its elements in ascending order until there are enough
         for (int base = g0; base < g1 && have < want; base += NT) {
             const int g = base + tid;
             uint32_t bits = 0;
-            float f[Elem<T>::kVec];
+            float f[VEC];
             const int e = row.first(g);
             if (g < g1) {
                 Elem<T>::unpack(row.load(g), f);
 #pragma unroll
-                for (int j = 0; j < Elem<T>::kVec; ++j)
+                for (int j = 0; j < VEC; ++j)
                     if (ordered(f[j]) == v && e + j >= 0 && e + j < row.n) bits |= 1u << j;
             }
             int before = __popc(bits);
@@ -404,7 +389,7 @@ __device__ __noinline__ void find_top(TopShared &sh, const uint32_t *groups, int
             }
             int at = have + before - __popc(bits);
 #pragma unroll
-            for (int j = 0; j < Elem<T>::kVec; ++j)
+            for (int j = 0; j < VEC; ++j)
                 if (bits >> j & 1) {
                     if (at < want) sh.cand[at] = rank_key(f[j], static_cast<uint32_t>(e + j));
                     ++at;
@@ -412,16 +397,13 @@ __device__ __noinline__ void find_top(TopShared &sh, const uint32_t *groups, int
             have += total_here;
             __syncthreads();
         }
-        if (tid == 0) sh.count = static_cast<uint32_t>(min(have, want));
-        __syncthreads();
+        have = min(have, want);
     }
-    int n = static_cast<int>(sh.count);
-    __syncthreads();
-    if (n > kCandidates || n < want) {
+    if (have > kCandidates || have < want) {
         radix_top<T, NT>(sh, row, g0, g1, want);
-        n = want;
+        have = want;
     }
-    select_top<NT>(sh, n, want);
+    select_top<NT>(sh, have, want);
 }
 
 // ------------------------------------------------------------------------------------------ teacher's entries
@@ -433,12 +415,11 @@ struct TeacherShared {
     int bad;                       // an id >= V
 };
 
-// The entries of a row; the student's logits only for ids in [e0, e1) (another block may be overwriting the rest in place).
-template <class T, int NT> __device__ __forceinline__ void teacher_read(TeacherShared &sh, const LossArgs &a, int64_t row, int64_t e0, int64_t e1)
+// The entries of a row, by `n` threads; the student's logits only for ids in [e0, e1) (another block may be overwriting the
+// rest in place).  `bad` is zero before.
+template <class T> __device__ __forceinline__ void teacher_read(TeacherShared &sh, const LossArgs &a, int64_t row, int e0, int e1, int t, int n)
 {
-    if (threadIdx.x == 0) sh.bad = 0;
-    __syncthreads();
-    for (int j = threadIdx.x; j < a.K; j += NT) {
+    for (int j = t; j < a.K; j += n) {
         const int64_t id = index_at(a.ids, a.index_bits, row * a.K + j);
         if (id >= a.V) sh.bad = 1;
         const bool here = id >= 0 && id < a.V;
@@ -514,23 +495,12 @@ template <bool TAIL> __device__ __forceinline__ float teacher_loss(const Teacher
     return sh.bad ? quiet_nan() : sum;
 }
 
-// ------------------------------------------------------------------------------------------ forward
+// ------------------------------------------------------------------------------------------ results and gradients of a row
 enum { kLogprobs = 0, kLogprobsTop = 1, kDistill = 2, kDistillTail = 3 };
+enum { kNoGrad = 0, kGrad = 1, kGradSaved = 2 };  // no gradient; from this call's sums; from a forward call's
 
-constexpr int kBitmapWords = 4096;  // ids of one segment of a row: 2^17 bits
-constexpr int kGroupSteps = 32;     // groups a thread notes at most
-
-template <int NT> struct ForwardShared {
-    Stats part[NT / 32];
-    Stats pub;           // this block's sums, read by the cluster's first block
-    uint32_t found;      // entries of top.best
-};
-
-// Sums of a warp's threads, then of the block's warps (in warp 0 afterwards).
-template <bool ENT, bool TAIL, int NT> __device__ __forceinline__ Stats block_stats(const Running &run, float mi, float si, Stats *part, float c)
+template <bool ENT, bool TAIL> __device__ __forceinline__ Stats warp_stats(const Running &run, float mi, float si, float c)
 {
-    constexpr int NW = NT / 32;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // the warp's maximum first, so that every lane rescales once and the rest are additions
     Stats st = {warp_max(run.m), run.s.x + run.s.y, ENT ? run.t.x + run.t.y : 0.f, mi, si};
     if (st.s != 0.f) {
@@ -547,25 +517,373 @@ template <bool ENT, bool TAIL, int NT> __device__ __forceinline__ Stats block_st
             join_sums(st.mi, st.si, om, os, c);
         }
     }
-    if (lane == 0) part[warp] = st;
-    __syncthreads();
-    if (warp == 0) {
-        st = lane < NW ? part[lane] : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
-#pragma unroll
-        for (int d = NW / 2; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), c);
-    }
     return st;
 }
 
+// One thread writes a row's sums; `token_x` is the given token's logit.
+template <bool ENT, bool TAIL> __device__ __forceinline__ void write_sums(const LossArgs &a, int64_t r, const Stats &st, const RowEnd &e, int token, float token_x)
+{
+    if (a.lse) a.lse[r] = lse_of(e.m, e.ls, e.empty, a.inv_t);
+    if (ENT) {
+        if (a.entropy) a.entropy[r] = e.empty ? 0.f : kLn2 * (e.ls - st.t / st.s);
+        if (a.logprob) a.logprob[r] = token < 0 ? 0.f : token >= a.V ? quiet_nan() : log_prob(token_x, e, a.inv_t);
+    }
+    if (TAIL && a.rest) a.rest[r] = lse_of(e.mr, e.lsr, e.rest_empty, a.inv_t);
+}
+
+// A row's gradient: 2^d (k0 + k1 d) with d = (x - m) c for every element, `hit` more for the given token, and for the
+// teacher's ids 2^((x - p_m) c) p_scale - q q_scale instead.
+struct RowGrad {
+    float m, k0, k1, hit;
+    float p_m, p_scale, q_scale;
+};
+
+template <bool TAIL> __device__ __forceinline__ RowGrad teacher_gradient(const LossArgs &a, int64_t r, const RowEnd &e, const TeacherShared &teacher)
+{
+    RowGrad k = {};
+    const float g = teacher.bad ? quiet_nan() : a.grad[r] * a.inv_t;
+    const float inv_s = 1.f / e.s;
+    const float mass = teacher.mass + (TAIL && !e.rest_empty ? teacher.left : 0.f);
+    k.p_m = e.empty ? 0.f : e.m;
+    k.p_scale = g * mass * inv_s;
+    k.q_scale = g;
+    if (TAIL) {
+        k.m = e.rest_empty ? 0.f : e.mr;
+        k.k0 = e.rest_empty ? 0.f : g * fmaf(mass, ex2((e.mr - e.m) * a.c) * e.sr * inv_s, -teacher.left) / e.sr;
+    } else {
+        k.m = k.p_m, k.k0 = k.p_scale;
+    }
+    if (e.empty) k.k0 = k.p_scale = k.q_scale = 0.f;
+    if (teacher.bad) k.k0 = k.p_scale = k.q_scale = quiet_nan();
+    return k;
+}
+
+template <bool TAIL> __device__ __forceinline__ RowGrad teacher_gradient_saved(const LossArgs &a, int64_t r, const TeacherShared &teacher)
+{
+    RowGrad k = {};
+    const float lse = a.in_lse[r], g = teacher.bad ? quiet_nan() : a.grad[r] * a.inv_t;
+    const bool empty = lse == neg_inf();
+    k.p_m = empty ? 0.f : lse * a.temperature;
+    if (TAIL) {
+        const float rest = a.in_rest[r];
+        const bool none = rest == neg_inf();
+        const float mass = teacher.mass + (none ? 0.f : teacher.left);
+        k.m = none ? 0.f : rest * a.temperature;
+        k.k0 = none ? 0.f : g * fmaf(mass, expf(rest - lse), -teacher.left);
+        k.p_scale = g * mass;
+    } else {
+        k.m = k.p_m;
+        k.k0 = k.p_scale = g * teacher.mass;
+    }
+    k.q_scale = g;
+    if (empty) k.k0 = k.p_scale = k.q_scale = 0.f;
+    if (teacher.bad) k.k0 = k.p_scale = k.q_scale = quiet_nan();
+    return k;
+}
+
+__device__ __forceinline__ float token_weight(const LossArgs &a, int64_t r, int token)
+{
+    if (!a.grad || token < 0) return 0.f;
+    return token >= a.V ? quiet_nan() : a.grad[r] * a.inv_t;
+}
+
+// p (gl + gh (log p + H)) with log p + H = ln 2 (d - sum p d)
+__device__ __forceinline__ RowGrad token_gradient(const LossArgs &a, int64_t r, const Stats &st, const RowEnd &e, int token)
+{
+    RowGrad k = {};
+    const float gh = a.grad_entropy ? a.grad_entropy[r] * a.inv_t : 0.f, gl = token_weight(a, r, token);
+    k.hit = gl;
+    if (e.empty) {
+        k.k0 = k.hit = gl != gl ? gl : 0.f;
+    } else {
+        const float inv_s = 1.f / st.s;
+        k.m = e.m;
+        k.k0 = -fmaf(-gh * kLn2, st.t * inv_s, gl) * inv_s;
+        k.k1 = -gh * kLn2 * inv_s;
+    }
+    return k;
+}
+
+__device__ __forceinline__ RowGrad token_gradient_saved(const LossArgs &a, int64_t r, int token)
+{
+    RowGrad k = {};
+    const float lse = a.in_lse[r], gh = a.grad_entropy ? a.grad_entropy[r] * a.inv_t : 0.f, gl = token_weight(a, r, token);
+    k.hit = gl;
+    if (lse == neg_inf()) {
+        k.k0 = k.hit = gl != gl ? gl : 0.f;
+    } else {
+        k.m = lse * a.temperature;
+        k.k0 = -(a.grad_entropy ? fmaf(gh, a.in_entropy[r], gl) : gl);
+        k.k1 = -gh * kLn2;
+    }
+    return k;
+}
+
+template <class T, bool ENT> __device__ __forceinline__ uint4 gradient_of(uint4 raw, float c, const RowGrad &k)
+{
+    const float2 minus = both(-k.m), scale = both(c), k0 = both(k.k0), k1 = both(k.k1);
+    float2 f[Elem<T>::kVec / 2];
+    Elem<T>::pairs(raw, f);
+#pragma unroll
+    for (int i = 0; i < Elem<T>::kVec / 2; ++i) {
+        float2 d = mul2(add2(f[i], minus), scale);
+        if (ENT) d = make_float2(max_nan(d.x, -1000.f), max_nan(d.y, -1000.f));
+        f[i] = mul2(make_float2(ex2(d.x), ex2(d.y)), ENT ? fma2(k1, d, k0) : k0);
+    }
+    return Elem<T>::pack(f);
+}
+
+// Granules g, g + step, ... of a row below `limit`; `entropy`: k1 is not zero (the same for all threads of the row).
+template <class T, int U>
+__device__ __forceinline__ void write_gradient(const uint4 *raw, const Row<T> &row, T *out, bool same, int g, int step, int limit, float c, const RowGrad &k, bool entropy)
+{
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int gu = g + u * step;
+        if (gu >= limit) continue;
+        row.store(out, same, gu, entropy ? gradient_of<T, true>(raw[u], c, k) : gradient_of<T, false>(raw[u], c, k));
+    }
+}
+
+// The given token's element, written again by one thread behind a barrier.
+template <class T> __device__ __forceinline__ void write_token_gradient(T *out, int token, float x, float c, const RowGrad &k)
+{
+    const float d = max_nan((x - k.m) * c, -1000.f);
+    out[token] = Elem<T>::from_float(fmaf(ex2(d), fmaf(k.k1, d, k.k0), k.hit));
+}
+
+// The teacher's ids that lie in [e0, e1), written again behind a barrier by the thread of the id's first entry, by `n` threads.
+template <class T> __device__ __forceinline__ void write_set_gradient(const TeacherShared &sh, int K, T *out, int e0, int e1, float c, const RowGrad &k, int t, int n)
+{
+    for (int j = t; j < K; j += n) {
+        const int32_t id = sh.id[j];
+        if (id < 0 || id < e0 || id >= e1) continue;
+        float q = 0.f;
+        bool first = true;
+#pragma unroll 8
+        for (int i = 0; i < K; ++i)
+            if (sh.id[i] == id) {
+                first = first && i >= j;
+                q += sh.q[i];
+            }
+        if (first) out[id] = Elem<T>::from_float(ex2((sh.x[j] - k.p_m) * c) * k.p_scale - q * k.q_scale);
+    }
+}
+
+// Marks the teacher's ids among elements first .. first + count - 1 in a bitmap; the thread that marks one adds it to the sums
+// over the set.
+__device__ __forceinline__ void mark_set(const TeacherShared &sh, int K, uint32_t *bitmap, int first, int count, float c, float &mi, float &si, int t, int n)
+{
+    for (int j = t; j < K; j += n) {
+        const int pos = sh.id[j] - first;
+        if (sh.id[j] < 0 || pos < 0 || pos >= count) continue;
+        const uint32_t bit = 1u << (pos & 31);
+        if (!(atomicOr(&bitmap[pos >> 5], bit) & bit)) add_logit(mi, si, sh.x[j], c);
+    }
+}
+
+// ------------------------------------------------------------------------------------------ short rows: one warp each
+constexpr int kWarpRows = 4;         // rows, and warps, of a block
+constexpr int kWarpCandidates = 256;
+
+template <class T, int U, int MODE> struct WarpShared {
+    TeacherShared teacher[MODE >= kDistill ? kWarpRows : 1];
+    uint32_t bitmap[MODE == kDistillTail ? kWarpRows : 1][U * Elem<T>::kVec];
+    uint64_t cand[MODE == kLogprobsTop ? kWarpRows : 1][kWarpCandidates];
+    uint32_t count[kWarpRows];
+};
+
+// The `want` best of a warp's granules, as keys in cand[0..n), n <= kWarpCandidates; returns n.  The want-th largest granule's
+// largest element bounds the want-th largest element from below.
+template <class T, int U> __device__ __forceinline__ int warp_top(uint4 *raw, const Row<T> &row, int G, int want, uint64_t *cand, uint32_t *count)
+{
+    constexpr int VEC = Elem<T>::kVec;
+    const int lane = threadIdx.x & 31;
+    uint32_t keys[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) keys[u] = u * 32 + lane < G ? ordered(Elem<T>::max_of(raw[u])) : 0u;
+    uint32_t v = 0;
+    for (int b = 31; b >= (VEC == 8 ? 12 : 0); --b) {  // 16-bit types: the low bits of the order are all alike
+        const uint32_t trial = v | 1u << b;
+        int n = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) n += keys[u] >= trial;
+        if (static_cast<int>(__reduce_add_sync(0xffffffffu, n)) >= want) v = trial;
+    }
+    if (lane == 0) *count = 0;
+    __syncwarp();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (v != 0 && keys[u] < v) continue;
+        const int e = row.first(u * 32 + lane);
+        float f[VEC];
+        Elem<T>::unpack(raw[u], f);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            if (ordered(f[i]) < v || e + i < 0 || e + i >= row.n) continue;
+            const uint32_t at = atomicAdd(count, 1u);
+            if (at < kWarpCandidates) cand[at] = rank_key(f[i], static_cast<uint32_t>(e + i));
+        }
+    }
+    __syncwarp();
+    const int n = static_cast<int>(*count);
+    if (n <= kWarpCandidates && n >= want) return n;
+    // many equal or many in few granules (or a bound from beyond the row's end, beside NaN alone): the want-th largest element itself, bit by bit, then those above it and the first
+    // ones equal to it
+    v = 0;
+#pragma unroll 1
+    for (int b = 31; b >= 0; --b) {
+        const uint32_t trial = v | 1u << b;
+        int c = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            asm volatile("" : "+r"(raw[u].x), "+r"(raw[u].y), "+r"(raw[u].z), "+r"(raw[u].w));  // unpacked anew in every round
+            const int e = row.first(u * 32 + lane);
+            float f[VEC];
+            Elem<T>::unpack(raw[u], f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) c += ordered(f[i]) >= trial && e + i >= 0 && e + i < row.n;
+        }
+        if (static_cast<int>(__reduce_add_sync(0xffffffffu, c)) >= want) v = trial;
+    }
+    int have = 0;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            asm volatile("" : "+r"(raw[u].x), "+r"(raw[u].y), "+r"(raw[u].z), "+r"(raw[u].w));
+            const int e = row.first(u * 32 + lane);
+            float f[VEC];
+            Elem<T>::unpack(raw[u], f);
+            uint32_t bits = 0;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if ((pass == 0 ? ordered(f[i]) > v : ordered(f[i]) == v) && e + i >= 0 && e + i < row.n) bits |= 1u << i;
+            int at = __popc(bits);
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int other = __shfl_up_sync(0xffffffffu, at, d);
+                if (lane >= d) at += other;
+            }
+            const int total = __shfl_sync(0xffffffffu, at, 31);
+            at += have - __popc(bits);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (bits >> i & 1) {
+                    if (at < want) cand[at] = rank_key(f[i], static_cast<uint32_t>(e + i));
+                    ++at;
+                }
+            have += total;
+        }
+    }
+    __syncwarp();
+    return want;
+}
+
+// Rows of up to 32 U granules: a warp reads its row once, keeps it in registers and needs no barrier.
+template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(32 * kWarpRows) loss_warp_kernel(const LossArgs a)
+{
+    constexpr bool ENT = MODE == kLogprobs || MODE == kLogprobsTop, TEACHER = MODE >= kDistill, TAIL = MODE == kDistillTail;
+    __shared__ WarpShared<T, U, MODE> sh;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * kWarpRows + warp;
+    if (r >= a.R) return;
+    const Row<T> row(static_cast<const T *>(a.logits) + r * a.ld, a.V);
+    T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
+    const int G = row.granules();
+    TeacherShared &teacher = sh.teacher[TEACHER ? warp : 0];
+    uint4 raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = row.load_below(u * 32 + lane, G);
+    int token = -1;
+    float token_x = 0.f, mi = neg_inf(), si = 0.f;
+    if (TEACHER) {
+        if (lane == 0) teacher.bad = 0;
+        __syncwarp();
+        teacher_read<T>(teacher, a, r, 0, static_cast<int>(a.V), lane, 32);
+        if (TAIL && GRAD != kGradSaved)
+            for (int i = lane; i < U * Elem<T>::kVec; i += 32) sh.bitmap[warp][i] = 0;
+        __syncwarp();
+        teacher_weights<TAIL>(teacher, a.K);
+        if (TAIL && GRAD != kGradSaved) {
+            mark_set(teacher, a.K, sh.bitmap[warp], row.first(0), G * Elem<T>::kVec, a.c, mi, si, lane, 32);
+            __syncwarp();
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t bits = u * 32 + lane < G ? bits_of<T>(sh.bitmap[warp], u * 32 + lane) : 0u;
+                if (bits) raw[u] = without<T>(raw[u], bits);
+            }
+        }
+    } else if (a.ids) {
+        token = token_at(a, r);
+        if (token >= 0 && token < a.V) token_x = Elem<T>::to_float(row.p[token]);
+    }
+    RowGrad k;
+    if (GRAD != kGradSaved) {
+        Running run = {neg_inf(), both(0.f), both(0.f)};
+        float all = Elem<T>::max_of(raw[0]);
+#pragma unroll
+        for (int u = 1; u < U; ++u) all = fmaxf(all, Elem<T>::max_of(raw[u]));
+        raise<ENT>(run, all, a.c);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (u * 32 < G) accumulate<T, ENT>(raw[u], a.c, run);
+        const Stats st = warp_stats<ENT, TAIL>(run, mi, si, a.c);
+        const RowEnd e = row_end<TAIL>(st, a.c);
+        if (lane == 0) write_sums<ENT, TAIL>(a, r, st, e, token, token_x);
+        if (TEACHER && a.loss) {
+            const float loss = teacher_loss<TAIL>(teacher, e, a.inv_t, a.K);
+            if (lane == 0) a.loss[r] = loss;
+        }
+        if (MODE == kLogprobsTop) {
+            uint64_t *cand = sh.cand[warp];
+            const int n = warp_top<T, U>(raw, row, G, a.K, cand, &sh.count[warp]);
+            for (int i = lane; i < n; i += 32) {
+                const uint64_t key = cand[i];
+                int rank = 0;
+#pragma unroll 8
+                for (int j = 0; j < n; ++j) rank += cand[j] > key;
+                if (rank >= a.K) continue;
+                a.top_ids[r * a.K + rank] = static_cast<int32_t>(~static_cast<uint32_t>(key));
+                a.top_logprobs[r * a.K + rank] = log_prob(unordered(static_cast<uint32_t>(key >> 32)), e, a.inv_t);
+            }
+        }
+        if (GRAD == kNoGrad) return;
+        k = TEACHER ? teacher_gradient<TAIL>(a, r, e, teacher) : token_gradient(a, r, st, e, token);
+    } else {
+        k = TEACHER ? teacher_gradient_saved<TAIL>(a, r, teacher) : token_gradient_saved(a, r, token);
+    }
+    // the elements are unpacked again rather than kept unpacked in twice the registers
+#pragma unroll
+    for (int u = 0; u < U; ++u) asm volatile("" : "+r"(raw[u].x), "+r"(raw[u].y), "+r"(raw[u].z), "+r"(raw[u].w));
+    write_gradient<T, U>(raw, row, out, row.same_lead(out), lane, 32, G, a.c, k, k.k1 != 0.f);
+    __syncwarp();
+    if (TEACHER) write_set_gradient<T>(teacher, a.K, out, 0, row.n, a.c, k, lane, 32);
+    else if (lane == 0 && token >= 0 && token < a.V) write_token_gradient<T>(out, token, token_x, a.c, k);
+}
+
+// ------------------------------------------------------------------------------------------ long rows: a block or cluster each
+constexpr int kBitmapWords = 4096;  // ids of one segment of a row: 2^17 bits
+constexpr int kGroupSteps = 32;     // groups a thread notes at most
+
+template <int NT> struct RowShared {
+    Stats part[NT / 32];
+    Stats pub;       // this block's sums, read by the cluster's other blocks
+    Stats total;     // the row's
+    uint32_t found;  // entries of top.best
+};
+
 // One row per cluster of blocks (of one block when there are rows enough), the row's granules divided among the blocks and
-// read once, the next U granules of a thread in flight while the present ones are added up.
-template <class T, int NT, int U, int MODE>
-__global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossArgs a)
+// streamed, the next U granules of a thread in flight while the present ones are added up.  With GRAD the row is then read
+// again, backwards, and its gradient written: rows in flight stay in L2 (see row_cluster), so that memory is read once.
+template <class T, int NT, int U, int MODE, int GRAD>
+__global__ void __launch_bounds__(NT, 768 / NT) loss_row_kernel(const LossArgs a)
 {
     constexpr bool ENT = MODE == kLogprobs || MODE == kLogprobsTop, TOP = MODE == kLogprobsTop;
     constexpr bool TEACHER = MODE >= kDistill, TAIL = MODE == kDistillTail;
+    constexpr int NW = NT / 32, STEP = NT * U;
     extern __shared__ __align__(16) unsigned char dynamic[];
-    __shared__ ForwardShared<NT> sh;
+    __shared__ RowShared<NT> sh;
     TopShared &top = *reinterpret_cast<TopShared *>(dynamic);                               // TOP
     uint32_t *groups = reinterpret_cast<uint32_t *>(dynamic + sizeof(TopShared));           // TOP
     TeacherShared &teacher = *reinterpret_cast<TeacherShared *>(dynamic);                   // TEACHER
@@ -581,22 +899,29 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossAr
 
     Running run = {neg_inf(), both(0.f), both(0.f)};
     float mi = neg_inf(), si = 0.f;
+    int token = -1;
+    float token_x = 0.f;
     uint4 next[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) next[u] = row.load_below(g0 + u * NT + tid, g1);
     if (TEACHER) {
-        teacher_read<T, NT>(teacher, a, r, rank == 0 ? 0 : row.first(g0), rank == 0 ? a.V : row.first(g1));
+        if (tid == 0) teacher.bad = 0;
         if (TAIL) {
             const int words = min(kBitmapWords, ((g1 - g0) * Elem<T>::kVec + 31) / 32);
             for (int i = tid; i < words; i += NT) bitmap[i] = 0;
         }
         __syncthreads();
-        if (warp == 0 && rank == 0) teacher_weights<TAIL>(teacher, a.K);
+        teacher_read<T>(teacher, a, r, rank == 0 ? 0 : row.first(g0), rank == 0 ? row.n : row.first(g1), tid, NT);
+        __syncthreads();
+        if (warp == 0 && (rank == 0 || GRAD)) teacher_weights<TAIL>(teacher, a.K);
+    } else if (a.ids) {
+        token = token_at(a, r);
+        if (token >= 0 && token < a.V && tid == 0) token_x = Elem<T>::to_float(row.p[token]);
     }
 
     constexpr int kSegment = kBitmapWords * 32 / Elem<T>::kVec;  // granules
-    static_assert(kSegment % (NT * U) == 0, "a segment is whole steps");
-    const int steps = (g1 - g0 + NT * U - 1) / (NT * U);
+    static_assert(kSegment % STEP == 0, "a segment is whole steps");
+    const int steps = (g1 - g0 + STEP - 1) / STEP;
     int shift = 0;
     if (TOP)
         while (steps >> shift >= kGroupSteps) ++shift;
@@ -605,22 +930,16 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossAr
 
     for (int seg = g0; seg < g1; seg = TAIL ? seg + kSegment : g1) {
         const int seg_end = TAIL ? min(g1, seg + kSegment) : g1;
-        if (TAIL) {  // mark the set's ids; the thread that marks one adds it to the sums over the set
-            for (int j = tid; j < a.K; j += NT) {
-                const int pos = teacher.id[j] - row.first(seg);
-                if (teacher.id[j] >= 0 && pos >= 0 && pos < (seg_end - seg) * Elem<T>::kVec) {
-                    const uint32_t bit = 1u << (pos & 31);
-                    if (!(atomicOr(&bitmap[pos >> 5], bit) & bit)) add_logit(mi, si, teacher.x[j], a.c);
-                }
-            }
+        if (TAIL) {
+            mark_set(teacher, a.K, bitmap, row.first(seg), (seg_end - seg) * Elem<T>::kVec, a.c, mi, si, tid, NT);
             __syncthreads();
         }
-        for (int base = seg; base < seg_end; base += NT * U, ++step) {
+        for (int base = seg; base < seg_end; base += STEP, ++step) {
             uint4 cur[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) cur[u] = next[u];
 #pragma unroll
-            for (int u = 0; u < U; ++u) next[u] = row.load_below(base + NT * U + u * NT + tid, g1);
+            for (int u = 0; u < U; ++u) next[u] = row.load_below(base + STEP + u * NT + tid, g1);
             if (TAIL) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -641,20 +960,29 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossAr
             }
             raise<ENT>(run, all, a.c);
 #pragma unroll
-            for (int u = 0; u < U; ++u) accumulate<T, ENT>(cur[u], a.c, run);
+            for (int u = 0; u < U; ++u)
+                if (base + u * NT + (warp << 5) < g1) accumulate<T, ENT>(cur[u], a.c, run);
         }
-        if (TAIL) {
+        if (TAIL && seg_end < g1) {
             __syncthreads();
-            for (int j = tid; j < a.K; j += NT) {
-                const int pos = teacher.id[j] - row.first(seg);
-                if (teacher.id[j] >= 0 && pos >= 0 && pos < (seg_end - seg) * Elem<T>::kVec) bitmap[pos >> 5] = 0;
-            }
+            for (int i = tid; i < kBitmapWords; i += NT) bitmap[i] = 0;
             __syncthreads();
         }
     }
+    if (GRAD) {  // the second reading's first granules come while the sums are joined
+#pragma unroll
+        for (int u = 0; u < U; ++u) next[u] = row.load_below(g0 + (steps - 1) * STEP + u * NT + tid, steps ? g1 : 0);
+    }
 
-    Stats st = block_stats<ENT, TAIL, NT>(run, mi, si, sh.part, a.c);
-    if (tid == 0) sh.pub = st;
+    Stats st = warp_stats<ENT, TAIL>(run, mi, si, a.c);
+    if (lane == 0) sh.part[warp] = st;
+    __syncthreads();
+    if (warp == 0) {
+        st = lane < NW ? sh.part[lane] : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
+#pragma unroll
+        for (int d = NW / 2; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
+        if (lane == 0) sh.pub = sh.total = st;
+    }
     if (TOP) {
         const int e0 = max(0, row.first(g0)), e1 = min(row.n, row.first(g1));
         const int want = max(0, min(a.K, e1 - e0));
@@ -663,115 +991,59 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_forward_kernel(const LossAr
     }
     if (C > 1) {
         cluster.sync();
-        if (rank == 0) {
-            if (warp == 0) {
-                st = lane < C ? *cluster.map_shared_rank(&sh.pub, lane) : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
+        if (warp == 0 && (rank == 0 || GRAD)) {
+            st = lane < C ? *cluster.map_shared_rank(&sh.pub, lane) : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
 #pragma unroll
-                for (int d = 4; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-            }
-            if (TOP) {
-                int n = 0;  // the blocks' lists side by side
-                for (int b = 0; b < C; ++b) {
-                    const int m = static_cast<int>(*cluster.map_shared_rank(&sh.found, b));
-                    const TopShared *other = cluster.map_shared_rank(&top, b);
-                    for (int i = tid; i < m; i += NT) top.cand[n + i] = other->best[i];
-                    n += m;
-                }
-                __syncthreads();
-                select_top<NT>(top, n, a.K);
-            }
+            for (int d = 4; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
+            if (lane == 0) sh.total = st;
         }
-        cluster.sync();  // no block leaves while its shared memory is read
-        if (rank != 0) return;
-        if (tid == 0) sh.pub = st;
+        if (TOP && rank == 0) {
+            int n = 0;  // the blocks' lists side by side
+            for (int b = 0; b < C; ++b) {
+                const int m = static_cast<int>(*cluster.map_shared_rank(&sh.found, b));
+                const TopShared *other = cluster.map_shared_rank(&top, b);
+                for (int i = tid; i < m; i += NT) top.cand[n + i] = other->best[i];
+                n += m;
+            }
+            __syncthreads();
+            select_top<NT>(top, n, a.K);
+        }
+        cluster.barrier_arrive();  // its other half stands at the end: no block leaves while its shared memory is read
     }
     __syncthreads();
-    st = sh.pub;
+    st = sh.total;
     const RowEnd e = row_end<TAIL>(st, a.c);
-    if (tid == 0) {
-        if (a.lse) a.lse[r] = lse_of(e.m, e.ls, e.empty, a.inv_t);
-        if (ENT) {
-            if (a.entropy) a.entropy[r] = e.empty ? 0.f : kLn2 * (e.ls - st.t / st.s);
-            if (a.logprob) {
-                const int token = token_at(a, r);
-                float lp = 0.f;
-                if (token >= a.V) lp = quiet_nan();
-                else if (token >= 0) lp = log_prob(Elem<T>::to_float(row.p[token]), e, a.inv_t);
-                a.logprob[r] = lp;
+    if (rank == 0) {
+        if (tid == 0) write_sums<ENT, TAIL>(a, r, st, e, token, token_x);
+        if (TEACHER && warp == NW - 1 && a.loss) {
+            const float loss = teacher_loss<TAIL>(teacher, e, a.inv_t, a.K);
+            if (lane == 0) a.loss[r] = loss;
+        }
+        if (TOP) {
+            for (int i = tid; i < a.K; i += NT) {
+                const uint64_t key = top.best[i];
+                a.top_ids[r * a.K + i] = static_cast<int32_t>(~static_cast<uint32_t>(key));
+                a.top_logprobs[r * a.K + i] = log_prob(unordered(static_cast<uint32_t>(key >> 32)), e, a.inv_t);
             }
         }
-        if (TAIL && a.rest) a.rest[r] = lse_of(e.mr, e.lsr, e.rest_empty, a.inv_t);
     }
-    if (TEACHER && warp == 0 && a.loss) {
-        const float loss = teacher_loss<TAIL>(teacher, e, a.inv_t, a.K);
-        if (lane == 0) a.loss[r] = loss;
-    }
-    if (TOP) {
-        for (int i = tid; i < a.K; i += NT) {
-            const uint64_t k = top.best[i];
-            a.top_ids[r * a.K + i] = static_cast<int32_t>(~static_cast<uint32_t>(k));
-            a.top_logprobs[r * a.K + i] = log_prob(unordered(static_cast<uint32_t>(k >> 32)), e, a.inv_t);
-        }
-    }
-}
-
-// ------------------------------------------------------------------------------------------ gradients
-// A row's gradient is 2^d (k0 + k1 d) per element with d = (x - m) c, plus a few elements that get their own value.
-struct RowGrad {
-    float m, k0, k1;
-};
-
-template <class T, bool ENT> __device__ __forceinline__ uint4 gradient_of(uint4 raw, float c, const RowGrad &k)
-{
-    const float2 minus = both(-k.m), scale = both(c), k0 = both(k.k0), k1 = both(k.k1);
-    float2 f[Elem<T>::kVec / 2];
-    Elem<T>::pairs(raw, f);
+    if (GRAD) {
+        T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
+        const RowGrad k = TEACHER ? teacher_gradient<TAIL>(a, r, e, teacher) : token_gradient(a, r, st, e, token);
+        const bool same = row.same_lead(out), entropy = k.k1 != 0.f;
+        for (int base = g0 + (steps - 1) * STEP; base >= g0; base -= STEP) {
+            uint4 cur[U];
 #pragma unroll
-    for (int i = 0; i < Elem<T>::kVec / 2; ++i) {
-        float2 d = mul2(add2(f[i], minus), scale);
-        if (ENT) d = make_float2(max_nan(d.x, -1000.f), max_nan(d.y, -1000.f));
-        f[i] = mul2(make_float2(ex2(d.x), ex2(d.y)), ENT ? fma2(k1, d, k0) : k0);
-    }
-    return Elem<T>::pack(f);
-}
-
-// Granules g, g + step, ... of a row below `limit`; `entropy`: k1 is not zero (the same for the whole block).
-template <class T, int U>
-__device__ __forceinline__ void write_gradient(const uint4 *raw, const Row<T> &row, T *out, bool same, int g, int step, int limit, float c, const RowGrad &k, bool entropy)
-{
+            for (int u = 0; u < U; ++u) cur[u] = next[u];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int gu = g + u * step;
-        if (gu >= limit) continue;
-        row.store(out, same, gu, entropy ? gradient_of<T, true>(raw[u], c, k) : gradient_of<T, false>(raw[u], c, k));
-    }
-}
-
-// The given token's element: its share of 2^d (k0 + k1 d) plus `hit`, written again by one thread behind a barrier.
-template <class T> __device__ __forceinline__ void write_token_gradient(T *out, int token, float x, float c, const RowGrad &k, float hit)
-{
-    const float d = max_nan((x - k.m) * c, -1000.f);
-    out[token] = Elem<T>::from_float(fmaf(ex2(d), fmaf(k.k1, d, k.k0), hit));
-}
-
-// The elements of the teacher's set that lie in [e0, e1): A p - (sum of q with this id), written by the thread of the id's
-// first entry.  Behind a barrier after the row's other elements were written.
-template <class T, int NT>
-__device__ __forceinline__ void write_set_gradient(const TeacherShared &sh, int K, T *out, int e0, int e1, float c, float m, float p_scale,
-                                                   float q_scale)
-{
-    for (int j = threadIdx.x; j < K; j += NT) {
-        const int32_t id = sh.id[j];
-        if (id < 0 || id < e0 || id >= e1) continue;
-        float q = 0.f;
-        bool first = true;
-        for (int i = 0; i < K; ++i) {
-            if (sh.id[i] != id) continue;
-            if (i < j) first = false;
-            q += sh.q[i];
+            for (int u = 0; u < U; ++u) next[u] = row.load_below(base - STEP + u * NT + tid, base > g0 ? g1 : 0);
+            write_gradient<T, U>(cur, row, out, same, base + tid, NT, g1, a.c, k, entropy);
         }
-        if (first) out[id] = Elem<T>::from_float(ex2((sh.x[j] - m) * c) * p_scale - q * q_scale);
+        __syncthreads();
+        if (TEACHER) write_set_gradient<T>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, k, tid, NT);
+        else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, k);
     }
+    if (C > 1) cluster.barrier_wait();
 }
 
 // Gradients from saved sums: one read and one write of the row, a.segments blocks per row.
@@ -785,223 +1057,62 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
     T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
     const int G = row.granules(), per = (G + a.segments - 1) / a.segments;
     const int g0 = min(G, part * per), g1 = min(G, g0 + per);
-    const float lse = a.in_lse[r];
-    RowGrad k = {0.f, 0.f, 0.f};
-    int token = -1;  // V stands for any id beyond the vocabulary
-    float hit = 0.f, p_m = 0.f, p_scale = 0.f, q_scale = 0.f;
+    RowGrad k;
+    int token = -1;
+    float token_x = 0.f;
+    uint4 next[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = row.load_below(g0 + threadIdx.x + u * NT, g1);
     if constexpr (TEACHER) {
-        teacher_read<T, NT>(shared, a, r, row.first(g0), row.first(g1));
+        if (threadIdx.x == 0) shared.bad = 0;
+        __syncthreads();
+        teacher_read<T>(shared, a, r, row.first(g0), row.first(g1), threadIdx.x, NT);
         __syncthreads();
         if (threadIdx.x < 32) teacher_weights<TAIL>(shared, a.K);
         __syncthreads();
-        float g = a.grad[r] * a.inv_t;
-        if (shared.bad) g = quiet_nan();
-        const bool empty = lse == neg_inf();
-        p_m = empty ? 0.f : lse * a.temperature;
-        if (TAIL) {
-            const float rest = a.in_rest[r];
-            const bool none = rest == neg_inf();
-            const float mass = shared.mass + (none ? 0.f : shared.left);
-            k.m = none ? 0.f : rest * a.temperature;
-            k.k0 = none ? 0.f : g * fmaf(mass, expf(rest - lse), -shared.left);
-            p_scale = g * mass;
-        } else {
-            k.m = p_m;
-            k.k0 = p_scale = g * shared.mass;
-        }
-        q_scale = g;
-        if (empty) k.k0 = p_scale = q_scale = shared.bad ? quiet_nan() : 0.f;
-        if (shared.bad) k.k0 = quiet_nan();
+        k = teacher_gradient_saved<TAIL>(a, r, shared);
     } else {
-        const float gh = a.grad_entropy ? a.grad_entropy[r] * a.inv_t : 0.f;
-        float gl = 0.f;
-        if (a.grad) {
-            token = token_at(a, r);
-            if (token >= 0) gl = token >= a.V ? quiet_nan() : a.grad[r] * a.inv_t;
-            hit = gl;
-        }
-        if (lse == neg_inf()) {
-            k.k0 = hit = token >= a.V ? quiet_nan() : 0.f;
-        } else {
-            k.m = lse * a.temperature;
-            k.k0 = -(a.grad_entropy ? fmaf(gh, a.in_entropy[r], gl) : gl);
-            k.k1 = -gh * kLn2;
-        }
+        if (a.grad) token = token_at(a, r);
+        k = token_gradient_saved(a, r, token);
+        if (token < row.first(g0) || token >= row.first(g1) || token >= a.V) token = -1;  // another block's, or none
+        if (threadIdx.x == 0 && token >= 0) token_x = Elem<T>::to_float(row.p[token]);
+        __syncthreads();  // read before it is overwritten in place
     }
     const bool same = row.same_lead(out), entropy = k.k1 != 0.f;
-    float token_x = 0.f;
-    const bool token_here = token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1);
-    if (!TEACHER && token_here && threadIdx.x == 0) token_x = Elem<T>::to_float(row.p[token]);
-    if (!TEACHER) __syncthreads();  // read before it is overwritten in place
-    for (int g = g0 + threadIdx.x; g < g1; g += NT * U) {
+    for (int g = g0 + threadIdx.x; g - static_cast<int>(threadIdx.x) < g1; g += NT * U) {
         uint4 raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = row.load_below(g + u * NT, g1);
+        for (int u = 0; u < U; ++u) raw[u] = next[u];
+#pragma unroll
+        for (int u = 0; u < U; ++u) next[u] = row.load_below(g + (U + u) * NT, g1);
         write_gradient<T, U>(raw, row, out, same, g, NT, g1, a.c, k, entropy);
     }
     __syncthreads();
-    if constexpr (TEACHER) {
-        write_set_gradient<T, NT>(shared, a.K, out, row.first(g0), row.first(g1), a.c, p_m, p_scale, q_scale);
-    } else {
-        if (token_here && threadIdx.x == 0) write_token_gradient<T>(out, token, token_x, a.c, k, hit);
-    }
-}
-
-// Loss and gradient of rows that a cluster holds in registers: U granules per thread, read once.
-template <int NT> struct ResidentShared {
-    Stats part[NT / 32];
-    Stats pub;
-    Stats total;
-    float loss;
-};
-
-template <class T, int NT, int U, bool TEACHER, bool TAIL>
-__global__ void __launch_bounds__(NT, 768 / NT) loss_resident_kernel(const LossArgs a)
-{
-    constexpr bool ENT = !TEACHER;
-    __shared__ ResidentShared<NT> sh;
-    __shared__ typename std::conditional<TEACHER, TeacherShared, int>::type teacher;
-    __shared__ uint32_t bitmap[TAIL ? NT * U * Elem<T>::kVec / 32 : 1];
-    cg::cluster_group cluster = cg::this_cluster();
-    const int C = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
-    const int64_t r = blockIdx.x / C;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const Row<T> row(static_cast<const T *>(a.logits) + r * a.ld, a.V);
-    T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
-    const int G = row.granules(), per = (G + C - 1) / C;
-    const int g0 = min(G, rank * per), g1 = min(G, g0 + per);
-
-    uint4 raw[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = row.load_below(g0 + u * NT + tid, g1);
-    Running run = {neg_inf(), both(0.f), both(0.f)};
-    float mi = neg_inf(), si = 0.f;
-    int token = -1;
-    float token_x = 0.f;
-    if constexpr (TEACHER) {
-        teacher_read<T, NT>(teacher, a, r, rank == 0 ? 0 : row.first(g0), rank == 0 ? a.V : row.first(g1));
-        if (TAIL)
-            for (int i = tid; i < NT * U * Elem<T>::kVec / 32; i += NT) bitmap[i] = 0;
-        __syncthreads();
-        if (warp == 0) teacher_weights<TAIL>(teacher, a.K);
-        if (TAIL) {
-            for (int j = tid; j < a.K; j += NT) {
-                const int pos = teacher.id[j] - row.first(g0);
-                if (teacher.id[j] >= 0 && pos >= 0 && pos < (g1 - g0) * Elem<T>::kVec) {
-                    const uint32_t bit = 1u << (pos & 31);
-                    if (!(atomicOr(&bitmap[pos >> 5], bit) & bit)) add_logit(mi, si, teacher.x[j], a.c);
-                }
-            }
-        }
-        __syncthreads();
-        if (TAIL) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int g = g0 + u * NT + tid;
-                const uint32_t bits = g < g1 ? bits_of<T>(bitmap, g - g0) : 0u;
-                if (bits) raw[u] = without<T>(raw[u], bits);
-            }
-        }
-    } else {
-        if (a.ids) {
-            token = token_at(a, r);
-            if (token >= 0 && token < a.V) token_x = Elem<T>::to_float(row.p[token]);
-        }
-    }
-    float all = Elem<T>::max_of(raw[0]);
-#pragma unroll
-    for (int u = 1; u < U; ++u) all = fmaxf(all, Elem<T>::max_of(raw[u]));
-    raise<ENT>(run, all, a.c);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (g0 + u * NT + (warp << 5) < g1) accumulate<T, ENT>(raw[u], a.c, run);
-    Stats st = block_stats<ENT, TAIL, NT>(run, mi, si, sh.part, a.c);
-    if (tid == 0) sh.pub = st, sh.total = st;
-    if (C > 1) {
-        cluster.sync();
-        if (warp == 0) {
-            st = lane < C ? *cluster.map_shared_rank(&sh.pub, lane) : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
-#pragma unroll
-            for (int d = 4; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-            if (lane == 0) sh.total = st;
-        }
-        cluster.sync();  // the peers have read; from here on every block is on its own
-    } else {
-        __syncthreads();
-    }
-    st = sh.total;
-    const RowEnd e = row_end<TAIL>(st, a.c);
-    RowGrad k = {0.f, 0.f, 0.f};
-    float hit = 0.f, p_m = 0.f, p_scale = 0.f, q_scale = 0.f;
-    if constexpr (TEACHER) {
-        if (rank == 0 && warp == 0) {
-            const float loss = teacher_loss<TAIL>(teacher, e, a.inv_t, a.K);
-            if (lane == 0) {
-                if (a.loss) a.loss[r] = loss;
-                if (a.lse) a.lse[r] = lse_of(e.m, e.ls, e.empty, a.inv_t);
-                if (TAIL && a.rest) a.rest[r] = lse_of(e.mr, e.lsr, e.rest_empty, a.inv_t);
-            }
-        }
-        const float g = teacher.bad ? quiet_nan() : a.grad[r] * a.inv_t;
-        const float inv_s = 1.f / e.s;
-        p_m = e.empty ? 0.f : e.m;
-        const float mass = teacher.mass + (TAIL && !e.rest_empty ? teacher.left : 0.f);
-        p_scale = g * mass * inv_s;
-        if (TAIL) {
-            k.m = e.rest_empty ? 0.f : e.mr;
-            k.k0 = e.rest_empty ? 0.f : g * fmaf(mass, ex2((e.mr - e.m) * a.c) * e.sr * inv_s, -teacher.left) / e.sr;
-        } else {
-            k.m = p_m, k.k0 = p_scale;
-        }
-        q_scale = g;
-        if (e.empty) k.k0 = p_scale = q_scale = 0.f;
-        if (teacher.bad) k.k0 = p_scale = q_scale = quiet_nan();
-    } else {
-        const float mean_d = e.empty ? 0.f : st.t / st.s;  // sum p d
-        if (rank == 0 && tid == 0) {
-            if (a.lse) a.lse[r] = lse_of(e.m, e.ls, e.empty, a.inv_t);
-            if (a.entropy) a.entropy[r] = e.empty ? 0.f : kLn2 * (e.ls - mean_d);
-            if (a.logprob) {
-                float lp = 0.f;
-                if (token >= a.V) lp = quiet_nan();
-                else if (token >= 0) lp = log_prob(token_x, e, a.inv_t);
-                a.logprob[r] = lp;
-            }
-        }
-        const float gh = a.grad_entropy ? a.grad_entropy[r] * a.inv_t : 0.f;
-        float gl = 0.f;
-        if (a.grad && token >= 0) gl = token >= a.V ? quiet_nan() : a.grad[r] * a.inv_t;
-        hit = gl;
-        if (e.empty) {
-            k.k0 = hit = a.grad && token >= a.V ? quiet_nan() : 0.f;
-        } else {
-            // p (gl + gh (log p + H)) with log p + H = ln 2 (d - mean_d)
-            const float inv_s = 1.f / st.s;
-            k.m = e.m;
-            k.k0 = -fmaf(-gh * kLn2, mean_d, gl) * inv_s;
-            k.k1 = -gh * kLn2 * inv_s;
-        }
-    }
-    // the elements are unpacked again rather than kept unpacked in twice the registers
-#pragma unroll
-    for (int u = 0; u < U; ++u) asm volatile("" : "+r"(raw[u].x), "+r"(raw[u].y), "+r"(raw[u].z), "+r"(raw[u].w));
-    write_gradient<T, U>(raw, row, out, row.same_lead(out), g0 + tid, NT, g1, a.c, k, k.k1 != 0.f);
-    __syncthreads();
-    if constexpr (TEACHER) {
-        write_set_gradient<T, NT>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, p_m, p_scale, q_scale);
-    } else {
-        if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, k, hit);
-    }
+    if constexpr (TEACHER) write_set_gradient<T>(shared, a.K, out, row.first(g0), row.first(g1), a.c, k, threadIdx.x, NT);
+    else if (threadIdx.x == 0 && token >= 0) write_token_gradient<T>(out, token, token_x, a.c, k);
 }
 
 // ------------------------------------------------------------------------------------------ launches
 template <class T> inline int64_t most_granules(int64_t V) { return (V + Elem<T>::kVec - 1) / Elem<T>::kVec + 1; }
 
-template <class Kernel> inline int launch_clusters(Kernel kernel, int64_t rows, int cluster, int threads, size_t smem, cudaStream_t stream, const LossArgs &a)
+constexpr int64_t kMostBlocks = 0x7fffffff;
+constexpr int kSteps = 4;  // granules per thread and step of the long rows' kernels
+
+template <class T, int NT, int MODE, int GRAD> inline int launch_row(const LossArgs &a, int cluster, cudaStream_t stream)
 {
+    auto *kernel = loss_row_kernel<T, NT, kSteps, MODE, GRAD>;
+    size_t smem = 0;
+    if (MODE == kDistill) smem = sizeof(TeacherShared);
+    if (MODE == kDistillTail) smem = sizeof(TeacherShared) + 4 * kBitmapWords;
+    if (MODE == kLogprobsTop) {
+        const int64_t steps = (most_granules<T>(a.V) / cluster + NT * kSteps) / (NT * kSteps);
+        smem = sizeof(TopShared) + sizeof(uint32_t) * NT * static_cast<size_t>(steps < kGroupSteps ? steps + 1 : kGroupSteps + 1);
+        SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           static_cast<int>(sizeof(TopShared) + sizeof(uint32_t) * NT * (kGroupSteps + 1))));
+    }
     cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(static_cast<unsigned>(rows * cluster));
-    config.blockDim = dim3(static_cast<unsigned>(threads));
+    config.gridDim = dim3(static_cast<unsigned>(a.R * cluster));
+    config.blockDim = dim3(NT);
     config.dynamicSmemBytes = smem;
     config.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -1014,59 +1125,49 @@ template <class Kernel> inline int launch_clusters(Kernel kernel, int64_t rows, 
     return SPDY_OK;
 }
 
-constexpr int64_t kMostBlocks = 0x7fffffff;
-
-template <class T, int NT, int MODE> inline int forward_with(const LossArgs &a, int cluster, cudaStream_t stream)
+// Blocks that share a row: more when the rows alone would not fill the device twice and every block still has a step of
+// work; with a gradient also as many as keep the rows in flight (three blocks per multiprocessor) within 64 MB of L2.
+template <class T> inline int row_cluster(const LossArgs &a, int64_t G, int threads, bool grad)
 {
-    size_t smem = 0;
-    if (MODE == kDistill) smem = sizeof(TeacherShared);
-    if (MODE == kDistillTail) smem = sizeof(TeacherShared) + 4 * kBitmapWords;
-    if (MODE == kLogprobsTop) {
-        const int64_t steps = (most_granules<T>(a.V) / cluster + NT * 4) / (NT * 4);
-        smem = sizeof(TopShared) + sizeof(uint32_t) * NT * static_cast<size_t>(steps < kGroupSteps ? steps + 1 : kGroupSteps + 1);
-        SPDY_EVAL_TRY(cudaFuncSetAttribute(loss_forward_kernel<T, NT, 4, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                           static_cast<int>(sizeof(TopShared) + sizeof(uint32_t) * NT * (kGroupSteps + 1))));
-    }
-    return launch_clusters(loss_forward_kernel<T, NT, 4, MODE>, a.R, cluster, NT, smem, stream, a);
-}
-
-template <class T, int MODE> int forward(const LossArgs &a, cudaStream_t stream)
-{
-    // Short rows get small blocks, so that many rows are in flight on a multiprocessor; a row is divided among up to eight
-    // blocks when the rows alone would not fill the device twice and every block still has a step of work.
-    const int64_t G = most_granules<T>(a.V);
-    const bool small = G <= 512;
     int cluster = 1;
-    while (cluster < 8 && a.R * cluster < 2 * sm_count() && G > static_cast<int64_t>(cluster) * (small ? 512 : 1024)) cluster *= 2;
-    if (a.R * cluster > kMostBlocks) return SPDY_ERR_UNSUPPORTED;
-    return small ? forward_with<T, 128, MODE>(a, cluster, stream) : forward_with<T, 256, MODE>(a, cluster, stream);
+    if (grad)
+        while (cluster < 8 && 3ll * sm_count() / cluster * G * 16 > (64ll << 20)) cluster *= 2;
+    while (cluster < 8 && a.R * cluster < 2 * sm_count() && G > static_cast<int64_t>(cluster) * threads * kSteps) cluster *= 2;
+    return cluster;
 }
 
-template <class T, bool TEACHER, bool TAIL> int backward(LossArgs a, cudaStream_t stream)
+template <class T, int U, int MODE, int GRAD> inline int launch_warp(const LossArgs &a, cudaStream_t stream)
 {
-    constexpr int NT = 256, U = 4;
+    const int64_t blocks = (a.R + kWarpRows - 1) / kWarpRows;
+    if (blocks > kMostBlocks) return SPDY_ERR_UNSUPPORTED;
+    loss_warp_kernel<T, U, MODE, GRAD><<<static_cast<unsigned>(blocks), 32 * kWarpRows, 0, stream>>>(a);
+    return finish_launch();
+}
+
+// The forward pass, with the gradient too where GRAD says so.
+template <class T, int MODE, int GRAD> int rows(const LossArgs &a, cudaStream_t stream)
+{
     const int64_t G = most_granules<T>(a.V);
+    if (G <= 128) return launch_warp<T, 4, MODE, GRAD>(a, stream);
+    if (G <= 256) return launch_warp<T, 8, MODE, GRAD>(a, stream);
+    const int threads = G <= 1024 ? 128 : 256;
+    const int cluster = row_cluster<T>(a, G, threads, GRAD);
+    if (a.R * cluster > kMostBlocks) return SPDY_ERR_UNSUPPORTED;
+    return threads == 128 ? launch_row<T, 128, MODE, GRAD>(a, cluster, stream) : launch_row<T, 256, MODE, GRAD>(a, cluster, stream);
+}
+
+template <class T, int MODE> int backward(LossArgs a, cudaStream_t stream)
+{
+    constexpr int NT = 256, U = kSteps;
+    constexpr bool TEACHER = MODE >= kDistill, TAIL = MODE == kDistillTail;
+    const int64_t G = most_granules<T>(a.V);
+    if (G <= 128) return launch_warp<T, 4, MODE, kGradSaved>(a, stream);
+    if (G <= 256) return launch_warp<T, 8, MODE, kGradSaved>(a, stream);
     a.segments = static_cast<int>((G + 2 * NT * U - 1) / (2 * NT * U));
     if (a.R * a.segments < 4 * sm_count()) a.segments = static_cast<int>((G + NT - 1) / NT);
     if (a.R * a.segments > kMostBlocks) return SPDY_ERR_UNSUPPORTED;
     loss_backward_kernel<T, NT, U, TEACHER, TAIL><<<static_cast<unsigned>(a.R * a.segments), NT, 0, stream>>>(a);
     return finish_launch();
-}
-
-// Whether a cluster holds the row in registers; if so, loss and gradient in one launch.
-template <class T, bool TEACHER, bool TAIL> int resident(const LossArgs &a, cudaStream_t stream, bool &fits)
-{
-    constexpr int U = 8;
-    const int64_t G = most_granules<T>(a.V);
-    fits = G <= 8 * 512 * U;
-    if (!fits) return SPDY_OK;
-    const int NT = G <= 128 * U ? 128 : G <= 8 * 256 * U ? 256 : 512;
-    int cluster = static_cast<int>((G + NT * U - 1) / (NT * U));
-    while (cluster < 8 && a.R * cluster < sm_count() && G > static_cast<int64_t>(cluster) * NT) ++cluster;
-    if (a.R * cluster > kMostBlocks) return SPDY_ERR_UNSUPPORTED;
-    if (NT == 128) return launch_clusters(loss_resident_kernel<T, 128, U, TEACHER, TAIL>, a.R, cluster, NT, 0, stream, a);
-    if (NT == 256) return launch_clusters(loss_resident_kernel<T, 256, U, TEACHER, TAIL>, a.R, cluster, NT, 0, stream, a);
-    return launch_clusters(loss_resident_kernel<T, 512, U, TEACHER, TAIL>, a.R, cluster, NT, 0, stream, a);
 }
 
 #define SPDY_EVAL_BY_TYPE(dtype, call)                                                          \

@@ -48,8 +48,8 @@ int spdy_token_logprobs(const void *logits, int64_t ld, int dtype, const void *t
     a.K = top_k;
     a.logprob = logprob, a.entropy = entropy, a.lse = lse, a.top_ids = top_ids, a.top_logprobs = top_logprobs;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (top_k) return SPDY_EVAL_BY_TYPE(dtype, (forward<T, kLogprobsTop>(a, stream)));
-    return SPDY_EVAL_BY_TYPE(dtype, (forward<T, kLogprobs>(a, stream)));
+    if (top_k) return SPDY_EVAL_BY_TYPE(dtype, (rows<T, kLogprobsTop, kNoGrad>(a, stream)));
+    return SPDY_EVAL_BY_TYPE(dtype, (rows<T, kLogprobs, kNoGrad>(a, stream)));
 }
 
 int spdy_token_logprobs_backward(const void *logits, int64_t ld, int dtype, const void *tokens, int index_bits, int64_t R, int64_t V, float temperature,
@@ -63,7 +63,7 @@ int spdy_token_logprobs_backward(const void *logits, int64_t ld, int dtype, cons
     LossArgs a = base_args(logits, ld, tokens, index_bits, R, V, temperature);
     a.in_lse = lse, a.in_entropy = entropy, a.grad = grad_logprob, a.grad_entropy = grad_entropy, a.dlogits = dlogits, a.lddl = lddl;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    return SPDY_EVAL_BY_TYPE(dtype, (backward<T, false, false>(a, stream)));
+    return SPDY_EVAL_BY_TYPE(dtype, (backward<T, kLogprobs>(a, stream)));
 }
 
 int spdy_token_logprobs_with_grad(const void *logits, int64_t ld, int dtype, const void *tokens, int index_bits, int64_t R, int64_t V, float temperature,
@@ -77,14 +77,7 @@ int spdy_token_logprobs_with_grad(const void *logits, int64_t ld, int dtype, con
     LossArgs a = base_args(logits, ld, tokens, index_bits, R, V, temperature);
     a.logprob = logprob, a.entropy = entropy, a.lse = lse, a.grad = grad_logprob, a.grad_entropy = grad_entropy, a.dlogits = dlogits, a.lddl = lddl;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    bool fits = false;
-    const int rc = SPDY_EVAL_BY_TYPE(dtype, (resident<T, false, false>(a, stream, fits)));
-    if (rc != SPDY_OK || fits) return rc;
-    // rows longer than a cluster holds: two passes over them
-    const int fwd = SPDY_EVAL_BY_TYPE(dtype, (forward<T, kLogprobs>(a, stream)));
-    if (fwd != SPDY_OK) return fwd;
-    a.in_lse = lse, a.in_entropy = entropy;
-    return SPDY_EVAL_BY_TYPE(dtype, (backward<T, false, false>(a, stream)));
+    return SPDY_EVAL_BY_TYPE(dtype, (rows<T, kLogprobs, kGrad>(a, stream)));
 }
 
 }  // extern "C"
