@@ -69,9 +69,25 @@ __device__ __forceinline__ uint4 load_stream(const void *p)
     return v;
 }
 
+// Read for the last time, or written to be read much later: first to leave L2.
+__device__ __forceinline__ uint64_t leave_first()
+{
+    uint64_t policy;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+    return policy;
+}
+__device__ __forceinline__ uint4 load_last(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p), "l"(leave_first())
+                 : "memory");
+    return v;
+}
 __device__ __forceinline__ void store_stream(void *p, uint4 v)
 {
-    asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+    asm volatile("st.global.L1::no_allocate.L2::cache_hint.v4.u32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "l"(leave_first()) : "memory");
 }
 
 // Element types: how many fit 16 bytes, conversion, and the bit pattern of -inf repeated over a word.
@@ -199,32 +215,27 @@ template <class T> __device__ __noinline__ void store_part(T *q, int n, int e, u
 }
 
 // A row that may start anywhere: granule g is the g-th aligned 16 bytes that hold a part of it, elements
-// g * kVec - lead .. + kVec - 1.  Only granules that lie wholly inside the row (lo <= g < hi) are moved 16 bytes at a time.
+// g * kVec - lead .. + kVec - 1.  Only granules that lie wholly inside the row are moved 16 bytes at a time.
 template <class T> struct Row {
     const T *p;
     int n;       // elements, at most 2^31 - 65 (positions inside a row are 32-bit)
     int lead;    // elements of granule 0 that lie before the row
-    int lo, hi;  // the whole granules
 
-    __device__ __forceinline__ Row(const T *row, int64_t count) : p(row), n(static_cast<int>(count)), lead(static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T)))
-    {
-        lo = lead ? 1 : 0;
-        hi = (n + lead) / Elem<T>::kVec;
-    }
+    __device__ __forceinline__ Row(const T *row, int64_t count) : p(row), n(static_cast<int>(count)), lead(static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T))) {}
     __device__ __forceinline__ int granules() const { return (n + lead + Elem<T>::kVec - 1) / Elem<T>::kVec; }
     __device__ __forceinline__ int first(int g) const { return g * Elem<T>::kVec - lead; }
-    __device__ __forceinline__ bool whole(int g) const { return static_cast<unsigned>(g - lo) < static_cast<unsigned>(max(hi - lo, 0)); }
+    __device__ __forceinline__ bool whole(int g) const { return first(g) >= 0 && first(g) <= n - Elem<T>::kVec; }
     // elements outside the row read as -inf
     __device__ __forceinline__ uint4 load(int g) const
     {
         if (whole(g)) return load_stream(p + first(g));
         return load_part(p, n, first(g));
     }
-    // the same, nothing but -inf from granule `limit` on
-    __device__ __forceinline__ uint4 load_below(int g, int limit) const
+    // the same, nothing but -inf from granule `limit` on; LAST: not to be read again
+    template <bool LAST = false> __device__ __forceinline__ uint4 load_below(int g, int limit) const
     {
         constexpr uint32_t NI = Elem<T>::kNegInfWord;
-        if (whole(g) && g < limit) return load_stream(p + first(g));
+        if (whole(g) && g < limit) return LAST ? load_last(p + first(g)) : load_stream(p + first(g));
         if (g < limit) return load_part(p, n, first(g));
         return make_uint4(NI, NI, NI, NI);
     }

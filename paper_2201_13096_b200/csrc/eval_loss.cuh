@@ -10,6 +10,7 @@
 #ifndef SPDY_EVAL_LOSS_CUH
 #define SPDY_EVAL_LOSS_CUH
 
+#include <algorithm>
 #include <type_traits>
 
 #include "eval_common.cuh"
@@ -235,7 +236,7 @@ template <int NT> __device__ __noinline__ void select_top(TopShared &sh, int n, 
 
 // The `want` largest keys of granules [g0, g1) of a row into sh.cand, by reading the row once per key byte: for rows whose
 // order defeats the bound below.  All threads of the block.
-template <class T, int NT> __device__ __noinline__ void radix_top(TopShared &sh, const Row<T> &row, int g0, int g1, int want)
+template <class T, int NT> __device__ __noinline__ void radix_top(TopShared &sh, const Row<T> row, int g0, int g1, int want)
 {
     const int tid = threadIdx.x;
     uint64_t prefix = 0, mask = 0;
@@ -290,13 +291,15 @@ template <class T, int NT> __device__ __noinline__ void radix_top(TopShared &sh,
 // one step, or of 2^shift steps in a row too long for `groups`) as an ordered 32-bit value, 0 for a group without elements.
 // Then the K-th largest group value v bounds the K-th largest element from below: elements above v lie in fewer than K
 // groups, which are read again; what may still be missing are elements equal to v, those with the lowest ids.
-// `lane_best` is the thread's largest value over all its groups.  Result in sh.best[0..want).
+// Result in sh.best[0..want).
 template <class T, int NT, int U>
-__device__ __noinline__ void find_top(TopShared &sh, const uint32_t *groups, int n_groups, int shift, uint32_t lane_best, const Row<T> &row, int g0, int g1, int want)
+__device__ __forceinline__ void find_top(TopShared &sh, const uint32_t *groups, int n_groups, int shift, const Row<T> row, int g0, int g1, int want)
 {
     constexpr int NW = NT / 32, STEP = NT * U, VEC = Elem<T>::kVec;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     // a cheap bound first: the r-th largest lane of every warp, r such that the warps together have `want` lanes above it
+    uint32_t lane_best = 0;
+    for (int i = 0; i < n_groups; ++i) lane_best = max(lane_best, groups[i * NT + tid]);
     const uint64_t mine = warp_nth_key(lane_best, static_cast<uint32_t>(lane), (want + NW - 1) / NW);
     if (lane == 0) sh.tau[warp] = mine >> 32;
     if (tid == 0) sh.count = 0, sh.want = 0;
@@ -682,6 +685,22 @@ __device__ __forceinline__ void mark_set(const TeacherShared &sh, int K, uint32_
     }
 }
 
+__device__ __forceinline__ void unmark_set(const TeacherShared &sh, int K, uint32_t *bitmap, int first, int count, int t, int n)
+{
+    for (int j = t; j < K; j += n) {
+        const int pos = sh.id[j] - first;
+        if (sh.id[j] >= 0 && pos >= 0 && pos < count) bitmap[pos >> 5] = 0;
+    }
+}
+
+// Entries that block `b` of a row's cluster contributes to its alternatives.
+template <class T> __device__ __forceinline__ int share_count(const Row<T> &row, int blocks, int b, int K)
+{
+    const int G = row.granules(), per = (G + blocks - 1) / blocks;
+    const int g0 = min(G, b * per), g1 = min(G, g0 + per);
+    return max(0, min(K, min(row.n, row.first(g1)) - max(0, row.first(g0))));
+}
+
 // ------------------------------------------------------------------------------------------ short rows: one warp each
 constexpr int kWarpRows = 4;         // rows, and warps, of a block
 constexpr int kWarpCandidates = 256;
@@ -856,7 +875,7 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
     // the elements are unpacked again rather than kept unpacked in twice the registers
 #pragma unroll
     for (int u = 0; u < U; ++u) asm volatile("" : "+r"(raw[u].x), "+r"(raw[u].y), "+r"(raw[u].z), "+r"(raw[u].w));
-    write_gradient<T, U>(raw, row, out, row.same_lead(out), lane, 32, G, a.c, k, k.k1 != 0.f);
+    write_gradient<T, U>(raw, row, out, row.same_lead(out), lane, 32, G, a.c, k, ENT && k.k1 != 0.f);
     __syncwarp();
     if (TEACHER) write_set_gradient<T>(teacher, a.K, out, 0, row.n, a.c, k, lane, 32);
     else if (lane == 0 && token >= 0 && token < a.V) write_token_gradient<T>(out, token, token_x, a.c, k);
@@ -865,6 +884,7 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
 // ------------------------------------------------------------------------------------------ long rows: a block or cluster each
 constexpr int kBitmapWords = 4096;  // ids of one segment of a row: 2^17 bits
 constexpr int kGroupSteps = 32;     // groups a thread notes at most
+constexpr int kRowThreads = 768;    // threads a multiprocessor holds of the long rows' kernels
 
 template <int NT> struct RowShared {
     Stats part[NT / 32];
@@ -873,11 +893,23 @@ template <int NT> struct RowShared {
     uint32_t found;  // entries of top.best
 };
 
-// One row per cluster of blocks (of one block when there are rows enough), the row's granules divided among the blocks and
-// streamed, the next U granules of a thread in flight while the present ones are added up.  With GRAD the row is then read
-// again, backwards, and its gradient written: rows in flight stay in L2 (see row_cluster), so that memory is read once.
+// The granules of a row that a block of a cluster works on.
+template <class T> struct Share {
+    Row<T> row;
+    int g0, g1;
+    __device__ __forceinline__ Share(const LossArgs &a, int64_t r, int blocks, int rank) : row(static_cast<const T *>(a.logits) + r * a.ld, a.V)
+    {
+        const int G = row.granules(), per = (G + blocks - 1) / blocks;
+        g0 = min(G, rank * per), g1 = min(G, g0 + per);
+    }
+};
+
+// Blocks stay and walk over rows; a row belongs to one block, or to a cluster whose blocks divide its granules.  The row is
+// streamed, the next U granules of a thread in flight while the present ones are added up, and the next row's first ones
+// while this row is finished.  With GRAD the row is then read again, backwards, and its gradient written: rows in flight stay
+// in L2 (see row_cluster), so that memory is read once.
 template <class T, int NT, int U, int MODE, int GRAD>
-__global__ void __launch_bounds__(NT, 768 / NT) loss_row_kernel(const LossArgs a)
+__global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const LossArgs a)
 {
     constexpr bool ENT = MODE == kLogprobs || MODE == kLogprobsTop, TOP = MODE == kLogprobsTop;
     constexpr bool TEACHER = MODE >= kDistill, TAIL = MODE == kDistillTail;
@@ -891,159 +923,180 @@ __global__ void __launch_bounds__(NT, 768 / NT) loss_row_kernel(const LossArgs a
 
     cg::cluster_group cluster = cg::this_cluster();
     const int C = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
-    const int64_t r = blockIdx.x / C;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const Row<T> row(static_cast<const T *>(a.logits) + r * a.ld, a.V);
-    const int G = row.granules(), per = (G + C - 1) / C;
-    const int g0 = min(G, rank * per), g1 = min(G, g0 + per);
-
-    Running run = {neg_inf(), both(0.f), both(0.f)};
-    float mi = neg_inf(), si = 0.f;
-    int token = -1;
-    float token_x = 0.f;
+    const int64_t stride = gridDim.x / C;
+    int64_t r = blockIdx.x / C;
     uint4 next[U];
+    const auto begin_row = [&](int64_t at) {  // a row's first granules; nothing beyond the last row
+        if (at >= a.R) return;
+        const Share<T> s(a, at, C, rank);
 #pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = row.load_below(g0 + u * NT + tid, g1);
-    if (TEACHER) {
-        if (tid == 0) teacher.bad = 0;
-        if (TAIL) {
-            const int words = min(kBitmapWords, ((g1 - g0) * Elem<T>::kVec + 31) / 32);
-            for (int i = tid; i < words; i += NT) bitmap[i] = 0;
-        }
+        for (int u = 0; u < U; ++u) next[u] = s.row.load_below(s.g0 + u * NT + tid, s.g1);
+    };
+    begin_row(r);
+    if (TAIL) {
+        for (int i = tid; i < kBitmapWords; i += NT) bitmap[i] = 0;
         __syncthreads();
-        teacher_read<T>(teacher, a, r, rank == 0 ? 0 : row.first(g0), rank == 0 ? row.n : row.first(g1), tid, NT);
-        __syncthreads();
-        if (warp == 0 && (rank == 0 || GRAD)) teacher_weights<TAIL>(teacher, a.K);
-    } else if (a.ids) {
-        token = token_at(a, r);
-        if (token >= 0 && token < a.V && tid == 0) token_x = Elem<T>::to_float(row.p[token]);
     }
 
-    constexpr int kSegment = kBitmapWords * 32 / Elem<T>::kVec;  // granules
-    static_assert(kSegment % STEP == 0, "a segment is whole steps");
-    const int steps = (g1 - g0 + STEP - 1) / STEP;
-    int shift = 0;
-    if (TOP)
-        while (steps >> shift >= kGroupSteps) ++shift;
-    int step = 0;
-    uint32_t lane_best = 0;
-
-    for (int seg = g0; seg < g1; seg = TAIL ? seg + kSegment : g1) {
-        const int seg_end = TAIL ? min(g1, seg + kSegment) : g1;
-        if (TAIL) {
-            mark_set(teacher, a.K, bitmap, row.first(seg), (seg_end - seg) * Elem<T>::kVec, a.c, mi, si, tid, NT);
+    for (; r < a.R; r += stride) {
+        const Share<T> share(a, r, C, rank);
+        const Row<T> &row = share.row;
+        const int g0 = share.g0, g1 = share.g1;
+        Running run = {neg_inf(), both(0.f), both(0.f)};
+        float mi = neg_inf(), si = 0.f;
+        int token = -1;
+        float token_x = 0.f;
+        if (TEACHER) {
+            if (tid == 0) teacher.bad = 0;
             __syncthreads();
+            teacher_read<T>(teacher, a, r, rank == 0 ? 0 : row.first(g0), rank == 0 ? row.n : row.first(g1), tid, NT);
+            __syncthreads();
+            if (warp == 0 && (rank == 0 || GRAD)) teacher_weights<TAIL>(teacher, a.K);
+        } else if (a.ids) {
+            token = token_at(a, r);
+            if (token >= 0 && token < a.V && tid == 0) token_x = Elem<T>::to_float(row.p[token]);
         }
-        for (int base = seg; base < seg_end; base += STEP, ++step) {
-            uint4 cur[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) cur[u] = next[u];
-#pragma unroll
-            for (int u = 0; u < U; ++u) next[u] = row.load_below(base + STEP + u * NT + tid, g1);
+
+        constexpr int kSegment = kBitmapWords * 32 / Elem<T>::kVec;  // granules
+        static_assert(kSegment % STEP == 0, "a segment is whole steps");
+        const int steps = (g1 - g0 + STEP - 1) / STEP;
+        int shift = 0;
+        if (TOP)
+            while (steps >> shift >= kGroupSteps) ++shift;
+        int step = 0;
+
+        for (int seg = g0; seg < g1; seg = TAIL ? seg + kSegment : g1) {
+            const int seg_end = TAIL ? min(g1, seg + kSegment) : g1;
             if (TAIL) {
+                mark_set(teacher, a.K, bitmap, row.first(seg), (seg_end - seg) * Elem<T>::kVec, a.c, mi, si, tid, NT);
+                __syncthreads();
+            }
+            for (int base = seg; base < seg_end; base += STEP, ++step) {
+                uint4 cur[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int g = base + u * NT + tid;
-                    const uint32_t bits = g < seg_end ? bits_of<T>(bitmap, g - seg) : 0u;
-                    if (bits) cur[u] = without<T>(cur[u], bits);
+                for (int u = 0; u < U; ++u) cur[u] = next[u];
+                if (base + STEP < g1) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) next[u] = row.load_below(base + STEP + u * NT + tid, g1);
+                } else if (GRAD) {  // the second reading begins where the first ends
+#pragma unroll
+                    for (int u = 0; u < U; ++u) next[u] = cur[u];
+                } else if (!TOP) {
+                    begin_row(r + stride);
                 }
+                if (TAIL) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int g = base + u * NT + tid;
+                        const uint32_t bits = g < seg_end ? bits_of<T>(bitmap, g - seg) : 0u;
+                        if (bits) cur[u] = without<T>(cur[u], bits);
+                    }
+                }
+                float all = Elem<T>::max_of(cur[0]);
+#pragma unroll
+                for (int u = 1; u < U; ++u) all = fmaxf(all, Elem<T>::max_of(cur[u]));
+                if (TOP) {
+                    uint32_t key = base + tid < g1 ? ordered(all) : 0u;
+                    uint32_t *slot = groups + (step >> shift) * NT + tid;
+                    if (step & ((1 << shift) - 1)) key = max(key, *slot);
+                    *slot = key;
+                }
+                raise<ENT>(run, all, a.c);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (base + u * NT + (warp << 5) < g1) accumulate<T, ENT>(cur[u], a.c, run);
             }
-            float all = Elem<T>::max_of(cur[0]);
-#pragma unroll
-            for (int u = 1; u < U; ++u) all = fmaxf(all, Elem<T>::max_of(cur[u]));
-            if (TOP) {
-                uint32_t key = base + tid < g1 ? ordered(all) : 0u;
-                lane_best = max(lane_best, key);
-                uint32_t *slot = groups + (step >> shift) * NT + tid;
-                if (step & ((1 << shift) - 1)) key = max(key, *slot);
-                *slot = key;
+            if (TAIL) {
+                __syncthreads();
+                unmark_set(teacher, a.K, bitmap, row.first(seg), (seg_end - seg) * Elem<T>::kVec, tid, NT);
+                if (seg_end < g1) __syncthreads();
             }
-            raise<ENT>(run, all, a.c);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (base + u * NT + (warp << 5) < g1) accumulate<T, ENT>(cur[u], a.c, run);
         }
-        if (TAIL && seg_end < g1) {
-            __syncthreads();
-            for (int i = tid; i < kBitmapWords; i += NT) bitmap[i] = 0;
-            __syncthreads();
-        }
-    }
-    if (GRAD) {  // the second reading's first granules come while the sums are joined
-#pragma unroll
-        for (int u = 0; u < U; ++u) next[u] = row.load_below(g0 + (steps - 1) * STEP + u * NT + tid, steps ? g1 : 0);
-    }
 
-    Stats st = warp_stats<ENT, TAIL>(run, mi, si, a.c);
-    if (lane == 0) sh.part[warp] = st;
-    __syncthreads();
-    if (warp == 0) {
-        st = lane < NW ? sh.part[lane] : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
+        Stats st = warp_stats<ENT, TAIL>(run, mi, si, a.c);
+        if (lane == 0) sh.part[warp] = st;
+        __syncthreads();
+        if (warp == 0) {
+            st = lane < NW ? sh.part[lane] : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
 #pragma unroll
-        for (int d = NW / 2; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-        if (lane == 0) sh.pub = sh.total = st;
-    }
-    if (TOP) {
-        const int e0 = max(0, row.first(g0)), e1 = min(row.n, row.first(g1));
-        const int want = max(0, min(a.K, e1 - e0));
-        if (want > 0) find_top<T, NT, U>(top, groups, (steps + (1 << shift) - 1) >> shift, shift, lane_best, row, g0, g1, want);
-        if (tid == 0) sh.found = static_cast<uint32_t>(want);
-    }
-    if (C > 1) {
-        cluster.sync();
-        if (warp == 0 && (rank == 0 || GRAD)) {
-            st = lane < C ? *cluster.map_shared_rank(&sh.pub, lane) : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
-#pragma unroll
-            for (int d = 4; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-            if (lane == 0) sh.total = st;
-        }
-        if (TOP && rank == 0) {
-            int n = 0;  // the blocks' lists side by side
-            for (int b = 0; b < C; ++b) {
-                const int m = static_cast<int>(*cluster.map_shared_rank(&sh.found, b));
-                const TopShared *other = cluster.map_shared_rank(&top, b);
-                for (int i = tid; i < m; i += NT) top.cand[n + i] = other->best[i];
-                n += m;
-            }
-            __syncthreads();
-            select_top<NT>(top, n, a.K);
-        }
-        cluster.barrier_arrive();  // its other half stands at the end: no block leaves while its shared memory is read
-    }
-    __syncthreads();
-    st = sh.total;
-    const RowEnd e = row_end<TAIL>(st, a.c);
-    if (rank == 0) {
-        if (tid == 0) write_sums<ENT, TAIL>(a, r, st, e, token, token_x);
-        if (TEACHER && warp == NW - 1 && a.loss) {
-            const float loss = teacher_loss<TAIL>(teacher, e, a.inv_t, a.K);
-            if (lane == 0) a.loss[r] = loss;
+            for (int d = NW / 2; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
+            if (lane == 0) sh.pub = sh.total = st;
         }
         if (TOP) {
-            for (int i = tid; i < a.K; i += NT) {
-                const uint64_t key = top.best[i];
-                a.top_ids[r * a.K + i] = static_cast<int32_t>(~static_cast<uint32_t>(key));
-                a.top_logprobs[r * a.K + i] = log_prob(unordered(static_cast<uint32_t>(key >> 32)), e, a.inv_t);
+            const int e0 = max(0, row.first(g0)), e1 = min(row.n, row.first(g1));
+            const int want = max(0, min(a.K, e1 - e0));
+            if (want > 0) find_top<T, NT, U>(top, groups, (steps + (1 << shift) - 1) >> shift, shift, row, g0, g1, want);
+            if (tid == 0) sh.found = static_cast<uint32_t>(want);
+        }
+        if (C > 1) {
+            cluster.sync();
+            if (warp == 0 && (rank == 0 || GRAD)) {
+                st = lane < C ? *cluster.map_shared_rank(&sh.pub, lane) : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
+#pragma unroll
+                for (int d = 4; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
+                if (lane == 0) sh.total = st;
+            }
+            if (TOP && rank == 0) {
+                int n = 0;  // the blocks' lists side by side
+                for (int b = 0; b < C; ++b) {
+                    const int m = static_cast<int>(*cluster.map_shared_rank(&sh.found, b));
+                    const TopShared *other = cluster.map_shared_rank(&top, b);
+                    for (int i = tid; i < m; i += NT) top.cand[n + i] = other->best[i];
+                    n += m;
+                }
+            }
+            cluster.barrier_arrive();  // its other half stands at the row's end: shared memory may be read until then
+            if (TOP && rank == 0) {
+                __syncthreads();
+                int n = 0;
+                for (int b = 0; b < C; ++b) n += share_count<T>(row, C, b, a.K);
+                select_top<NT>(top, n, a.K);
             }
         }
-    }
-    if (GRAD) {
-        T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
-        const RowGrad k = TEACHER ? teacher_gradient<TAIL>(a, r, e, teacher) : token_gradient(a, r, st, e, token);
-        const bool same = row.same_lead(out), entropy = k.k1 != 0.f;
-        for (int base = g0 + (steps - 1) * STEP; base >= g0; base -= STEP) {
-            uint4 cur[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) cur[u] = next[u];
-#pragma unroll
-            for (int u = 0; u < U; ++u) next[u] = row.load_below(base - STEP + u * NT + tid, base > g0 ? g1 : 0);
-            write_gradient<T, U>(cur, row, out, same, base + tid, NT, g1, a.c, k, entropy);
-        }
         __syncthreads();
-        if (TEACHER) write_set_gradient<T>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, k, tid, NT);
-        else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, k);
+        st = sh.total;
+        const RowEnd e = row_end<TAIL>(st, a.c);
+        if (rank == 0) {
+            if (tid == 0) write_sums<ENT, TAIL>(a, r, st, e, token, token_x);
+            if (TEACHER && warp == NW - 1 && a.loss) {
+                const float loss = teacher_loss<TAIL>(teacher, e, a.inv_t, a.K);
+                if (lane == 0) a.loss[r] = loss;
+            }
+            if (TOP) {
+                for (int i = tid; i < a.K; i += NT) {
+                    const uint64_t key = top.best[i];
+                    a.top_ids[r * a.K + i] = static_cast<int32_t>(~static_cast<uint32_t>(key));
+                    a.top_logprobs[r * a.K + i] = log_prob(unordered(static_cast<uint32_t>(key >> 32)), e, a.inv_t);
+                }
+            }
+        }
+        if (GRAD) {
+            T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
+            const RowGrad k = TEACHER ? teacher_gradient<TAIL>(a, r, e, teacher) : token_gradient(a, r, st, e, token);
+            const bool same = row.same_lead(out), entropy = !TEACHER && k.k1 != 0.f;
+            for (int base = g0 + (steps - 1) * STEP; base >= g0; base -= STEP) {
+                uint4 cur[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) cur[u] = next[u];
+                if (base > g0) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) next[u] = row.template load_below<true>(base - STEP + u * NT + tid, g1);
+                } else {
+                    begin_row(r + stride);
+                }
+                write_gradient<T, U>(cur, row, out, same, base + tid, NT, g1, a.c, k, entropy);
+            }
+            if (g0 == g1) begin_row(r + stride);
+            __syncthreads();
+            if (TEACHER) write_set_gradient<T>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, k, tid, NT);
+            else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, k);
+        } else if (TOP || g0 == g1) {  // the search for the alternatives needs the registers
+            begin_row(r + stride);
+        }
+        __syncthreads();  // the next row overwrites shared memory
+        if (C > 1) cluster.barrier_wait();
     }
-    if (C > 1) cluster.barrier_wait();
 }
 
 // Gradients from saved sums: one read and one write of the row, a.segments blocks per row.
@@ -1078,7 +1131,7 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
         if (threadIdx.x == 0 && token >= 0) token_x = Elem<T>::to_float(row.p[token]);
         __syncthreads();  // read before it is overwritten in place
     }
-    const bool same = row.same_lead(out), entropy = k.k1 != 0.f;
+    const bool same = row.same_lead(out), entropy = !TEACHER && k.k1 != 0.f;
     for (int g = g0 + threadIdx.x; g - static_cast<int>(threadIdx.x) < g1; g += NT * U) {
         uint4 raw[U];
 #pragma unroll
@@ -1093,7 +1146,11 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
 }
 
 // ------------------------------------------------------------------------------------------ launches
-template <class T> inline int64_t most_granules(int64_t V) { return (V + Elem<T>::kVec - 1) / Elem<T>::kVec + 1; }
+// Granules of the logits' longest row: one more where rows do not start on 16 bytes.
+template <class T> inline int64_t most_granules(const LossArgs &a)
+{
+    return (a.V + Elem<T>::kVec - 1) / Elem<T>::kVec + (aligned(a.logits, 16) && a.ld % Elem<T>::kVec == 0 ? 0 : 1);
+}
 
 constexpr int64_t kMostBlocks = 0x7fffffff;
 constexpr int kSteps = 4;  // granules per thread and step of the long rows' kernels
@@ -1105,13 +1162,17 @@ template <class T, int NT, int MODE, int GRAD> inline int launch_row(const LossA
     if (MODE == kDistill) smem = sizeof(TeacherShared);
     if (MODE == kDistillTail) smem = sizeof(TeacherShared) + 4 * kBitmapWords;
     if (MODE == kLogprobsTop) {
-        const int64_t steps = (most_granules<T>(a.V) / cluster + NT * kSteps) / (NT * kSteps);
+        const int64_t steps = (most_granules<T>(a) / cluster + NT * kSteps) / (NT * kSteps);
         smem = sizeof(TopShared) + sizeof(uint32_t) * NT * static_cast<size_t>(steps < kGroupSteps ? steps + 1 : kGroupSteps + 1);
         SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                            static_cast<int>(sizeof(TopShared) + sizeof(uint32_t) * NT * (kGroupSteps + 1))));
     }
     cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(static_cast<unsigned>(a.R * cluster));
+    // Rows of few steps: blocks that stay, since the next row's first granules hide the start of each (16384 x 8192: 122 ->
+    // 86 us).  Longer ones: a block per row, which the hardware deals out more evenly (4096 x 65536: 122 -> 111 us).
+    const bool stay = most_granules<T>(a) <= 4096;
+    const int64_t held = stay ? std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * (kRowThreads / NT) / cluster) : kMostBlocks / cluster;
+    config.gridDim = dim3(static_cast<unsigned>(std::min(a.R, held) * cluster));
     config.blockDim = dim3(NT);
     config.dynamicSmemBytes = smem;
     config.stream = stream;
@@ -1126,12 +1187,13 @@ template <class T, int NT, int MODE, int GRAD> inline int launch_row(const LossA
 }
 
 // Blocks that share a row: more when the rows alone would not fill the device twice and every block still has a step of
-// work; with a gradient also as many as keep the rows in flight (three blocks per multiprocessor) within 64 MB of L2.
+// work; with a gradient also as many as keep the rows in flight within 64 MB of L2.
 template <class T> inline int row_cluster(const LossArgs &a, int64_t G, int threads, bool grad)
 {
+    const int64_t slots = static_cast<int64_t>(sm_count()) * (kRowThreads / threads);
     int cluster = 1;
     if (grad)
-        while (cluster < 8 && 3ll * sm_count() / cluster * G * 16 > (64ll << 20)) cluster *= 2;
+        while (cluster < 8 && slots / cluster * G * 16 > (64ll << 20)) cluster *= 2;
     while (cluster < 8 && a.R * cluster < 2 * sm_count() && G > static_cast<int64_t>(cluster) * threads * kSteps) cluster *= 2;
     return cluster;
 }
@@ -1147,12 +1209,11 @@ template <class T, int U, int MODE, int GRAD> inline int launch_warp(const LossA
 // The forward pass, with the gradient too where GRAD says so.
 template <class T, int MODE, int GRAD> int rows(const LossArgs &a, cudaStream_t stream)
 {
-    const int64_t G = most_granules<T>(a.V);
+    const int64_t G = most_granules<T>(a);
     if (G <= 128) return launch_warp<T, 4, MODE, GRAD>(a, stream);
     if (G <= 256) return launch_warp<T, 8, MODE, GRAD>(a, stream);
     const int threads = G <= 1024 ? 128 : 256;
     const int cluster = row_cluster<T>(a, G, threads, GRAD);
-    if (a.R * cluster > kMostBlocks) return SPDY_ERR_UNSUPPORTED;
     return threads == 128 ? launch_row<T, 128, MODE, GRAD>(a, cluster, stream) : launch_row<T, 256, MODE, GRAD>(a, cluster, stream);
 }
 
@@ -1160,7 +1221,7 @@ template <class T, int MODE> int backward(LossArgs a, cudaStream_t stream)
 {
     constexpr int NT = 256, U = kSteps;
     constexpr bool TEACHER = MODE >= kDistill, TAIL = MODE == kDistillTail;
-    const int64_t G = most_granules<T>(a.V);
+    const int64_t G = most_granules<T>(a);
     if (G <= 128) return launch_warp<T, 4, MODE, kGradSaved>(a, stream);
     if (G <= 256) return launch_warp<T, 8, MODE, kGradSaved>(a, stream);
     a.segments = static_cast<int>((G + 2 * NT * U - 1) / (2 * NT * U));
