@@ -36,29 +36,6 @@ __device__ __forceinline__ float max_nan(float a, float b)
     return y;
 }
 
-// Two fp32 operations per instruction (each rounded as its scalar form).
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    float2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long &>(r)) : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
-    return r;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    float2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long &>(r)) : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
-    return r;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    float2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(reinterpret_cast<unsigned long long &>(r))
-        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)), "l"(reinterpret_cast<unsigned long long &>(c)));
-    return r;
-}
-__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
-
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 __device__ __forceinline__ float quiet_nan() { return __int_as_float(0x7fc00000); }
 
@@ -69,25 +46,29 @@ __device__ __forceinline__ uint4 load_stream(const void *p)
     return v;
 }
 
-// Read for the last time, or written to be read much later: first to leave L2.
+// L2 policy for what is read for the last time, or written to be read much later: first to leave.
 __device__ __forceinline__ uint64_t leave_first()
 {
     uint64_t policy;
-    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
     return policy;
 }
-__device__ __forceinline__ uint4 load_last(const void *p)
+__device__ __forceinline__ uint4 load_hint(const void *p, uint64_t policy)
 {
     uint4 v;
     asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                 : "l"(p), "l"(leave_first())
+                 : "l"(p), "l"(policy)
                  : "memory");
     return v;
 }
+__device__ __forceinline__ void store_hint(void *p, uint4 v, uint64_t policy)
+{
+    asm volatile("st.global.L1::no_allocate.L2::cache_hint.v4.u32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "l"(policy) : "memory");
+}
 __device__ __forceinline__ void store_stream(void *p, uint4 v)
 {
-    asm volatile("st.global.L1::no_allocate.L2::cache_hint.v4.u32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "l"(leave_first()) : "memory");
+    asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
 // Element types: how many fit 16 bytes, conversion, and the bit pattern of -inf repeated over a word.
@@ -97,14 +78,6 @@ template <> struct Elem<float> {
     static constexpr uint32_t kNegInfWord = 0xff800000u;
     static __device__ __forceinline__ float to_float(float x) { return x; }
     static __device__ __forceinline__ float from_float(float x) { return x; }
-    static __device__ __forceinline__ void pairs(uint4 r, float2 *f)
-    {
-        f[0] = make_float2(__uint_as_float(r.x), __uint_as_float(r.y)), f[1] = make_float2(__uint_as_float(r.z), __uint_as_float(r.w));
-    }
-    static __device__ __forceinline__ uint4 pack(const float2 *f)
-    {
-        return make_uint4(__float_as_uint(f[0].x), __float_as_uint(f[0].y), __float_as_uint(f[1].x), __float_as_uint(f[1].y));
-    }
     static __device__ __forceinline__ void unpack(uint4 r, float *f)
     {
         f[0] = __uint_as_float(r.x), f[1] = __uint_as_float(r.y), f[2] = __uint_as_float(r.z), f[3] = __uint_as_float(r.w);
@@ -133,11 +106,6 @@ template <> struct Elem<__nv_bfloat16> {
     {
         two(r.x, f[0], f[1]), two(r.y, f[2], f[3]), two(r.z, f[4], f[5]), two(r.w, f[6], f[7]);
     }
-    static __device__ __forceinline__ void pairs(uint4 r, float2 *f)
-    {
-        two(r.x, f[0].x, f[0].y), two(r.y, f[1].x, f[1].y), two(r.z, f[2].x, f[2].y), two(r.w, f[3].x, f[3].y);
-    }
-    static __device__ __forceinline__ uint4 pack(const float2 *f) { return make_uint4(join(f[0].x, f[0].y), join(f[1].x, f[1].y), join(f[2].x, f[2].y), join(f[3].x, f[3].y)); }
     static __device__ __forceinline__ uint32_t join(float lo, float hi)
     {
         __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -165,11 +133,6 @@ template <> struct Elem<__half> {
     {
         two(r.x, f[0], f[1]), two(r.y, f[2], f[3]), two(r.z, f[4], f[5]), two(r.w, f[6], f[7]);
     }
-    static __device__ __forceinline__ void pairs(uint4 r, float2 *f)
-    {
-        two(r.x, f[0].x, f[0].y), two(r.y, f[1].x, f[1].y), two(r.z, f[2].x, f[2].y), two(r.w, f[3].x, f[3].y);
-    }
-    static __device__ __forceinline__ uint4 pack(const float2 *f) { return make_uint4(join(f[0].x, f[0].y), join(f[1].x, f[1].y), join(f[2].x, f[2].y), join(f[3].x, f[3].y)); }
     static __device__ __forceinline__ uint32_t join(float lo, float hi)
     {
         __half2 v = __floats2half2_rn(lo, hi);
@@ -231,20 +194,63 @@ template <class T> struct Row {
         if (whole(g)) return load_stream(p + first(g));
         return load_part(p, n, first(g));
     }
-    // the same, nothing but -inf from granule `limit` on; LAST: not to be read again
-    template <bool LAST = false> __device__ __forceinline__ uint4 load_below(int g, int limit) const
-    {
-        constexpr uint32_t NI = Elem<T>::kNegInfWord;
-        if (whole(g) && g < limit) return LAST ? load_last(p + first(g)) : load_stream(p + first(g));
-        if (g < limit) return load_part(p, n, first(g));
-        return make_uint4(NI, NI, NI, NI);
-    }
+    // granules g0 .. g1 - 1 are all whole
+    __device__ __forceinline__ bool inner(int g0, int g1) const { return first(g0) >= 0 && first(g1) <= n; }
     __device__ __forceinline__ bool same_lead(const T *q) const { return (reinterpret_cast<uintptr_t>(q) & 15) == (reinterpret_cast<uintptr_t>(p) & 15); }
     // v, converted already, to granule g's elements of `q`, a row of as many elements that may start elsewhere; `same`: same_lead(q)
     __device__ __forceinline__ void store(T *q, bool same, int g, uint4 v) const
     {
         if (same && whole(g)) store_stream(q + first(g), v);
         else store_part(q, n, first(g), v);
+    }
+};
+
+// The granules base + t, base + t + NT, ... (U of them) of a row, for a block or warp of NT threads: where all are whole and
+// below `limit`, one test serves them all; else each is tested, and reads as -inf from granule `limit` on.
+template <class T, int NT, int U> struct Step {
+    const Row<T> &row;
+    int g, limit;
+    bool plain;
+    __device__ __forceinline__ Step(const Row<T> &r, int base, int t, int limit_) : row(r), g(base + t), limit(limit_)
+    {
+        plain = base + NT * U <= limit_ && r.inner(base, base + NT * U);
+    }
+    __device__ __forceinline__ uint4 load_part_of(int u) const
+    {
+        constexpr uint32_t NI = Elem<T>::kNegInfWord;
+        const int at = g + u * NT;
+        if (at >= limit) return make_uint4(NI, NI, NI, NI);
+        return row.whole(at) ? load_stream(row.p + row.first(at)) : load_part(row.p, row.n, row.first(at));
+    }
+    __device__ __forceinline__ void load(uint4 *v) const
+    {
+        if (plain) {
+            const T *p = row.p + row.first(g);
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load_stream(p + u * NT * Elem<T>::kVec);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load_part_of(u);
+        }
+    }
+    __device__ __forceinline__ void load(uint4 *v, uint64_t policy) const
+    {
+        if (plain) {
+            const T *p = row.p + row.first(g);
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load_hint(p + u * NT * Elem<T>::kVec, policy);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = load_part_of(u);
+        }
+    }
+    // to granule u of `q`, a row of as many elements that may start elsewhere (`same`: it does not)
+    __device__ __forceinline__ void store_part_of(T *q, bool same, int u, uint4 v) const
+    {
+        const int at = g + u * NT;
+        if (at >= limit) return;
+        if (same && row.whole(at)) store_stream(q + row.first(at), v);
+        else store_part(q, row.n, row.first(at), v);
     }
 };
 

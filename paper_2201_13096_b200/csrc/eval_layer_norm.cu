@@ -140,7 +140,8 @@ template <class T, int TPR, int VPT, int NT> __global__ void __launch_bounds__(N
         params<VEC>(a.bias, a.param_type, e, a.D, 0.f, b);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) f[i] = fmaf((f[i] - mean) * rstd, w[i], b[i]);
-        row.store(out, row.same_lead(out), g, Elem<T>::pack(f));
+        if (row.same_lead(out) && row.whole(g)) store_stream(out + e, Elem<T>::pack(f));
+        else store_part(out, row.n, e, Elem<T>::pack(f));
     }
 }
 

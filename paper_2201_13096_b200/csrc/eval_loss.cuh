@@ -2,11 +2,12 @@
 // loss, and their gradients.  Instantiated in eval_token_logprobs.cu and eval_distill.cu.
 //
 // Mathematics.  Everything is kept in base 2: with c = log2(e) / T and the running maximum m of the logits, d_v = (x_v - m) c
-// and s = sum 2^d, a probability is 2^d_v / s.  The difference is taken before the scaling: for 16-bit logits it is exact,
-// and rows of the type's lowest value do not overflow.  The entropy needs t = sum 2^d d beside s: H = ln 2 (log2 s - t / s).
-// When the maximum rises by delta / c, s becomes s 2^-delta and t becomes (t - s delta) 2^-delta.
-// An element costs half an instruction each for difference, scaling and sum (two to an instruction), one to unpack and one
-// for the special-function unit, whose 16 results a cycle and multiprocessor are the next limit behind memory.
+// and s = sum 2^d, a probability is 2^d_v / s.  The entropy needs t = sum 2^d d beside s: H = ln 2 (log2 s - t / s).  When the
+// maximum rises by delta / c, s becomes s 2^-delta and t becomes (t - s delta) 2^-delta.
+// An element costs one fused multiply-add x c - b with b = m c rounded; the rounding r = m c - b is the same for all elements and
+// is taken back once per thread (2^-r s, and t - r s for t).  Where m c is so large that x c could overflow (rows of the type's
+// lowest value) m is subtracted first instead.  Beside that one instruction to unpack, one for the special-function unit
+// (16 results a cycle and multiprocessor, the next limit behind memory) and one or two to add up.
 #ifndef SPDY_EVAL_LOSS_CUH
 #define SPDY_EVAL_LOSS_CUH
 
@@ -103,39 +104,81 @@ template <bool ENT, bool TAIL> __device__ __forceinline__ Stats shuffle_xor(cons
     return b;
 }
 
-// What a thread has added up: s and t in two halves, even and odd elements.
+// What 2^(x c - base) is relative to: base = m c rounded, or 0 after subtracting sub = m where m c is too large for that.
+struct Reference {
+    float base, sub;
+    bool far;
+    __device__ __forceinline__ Reference(float m, float c)
+    {
+        base = m * c;
+        far = !(fabsf(base) < 1e35f);  // also m = -inf, +inf
+        sub = far && m != neg_inf() ? m : 0.f;
+        if (far) base = 0.f;
+    }
+};
+
+// What a thread has added up, relative to Reference(m, c).
 struct Running {
-    float m;
-    float2 s, t;
+    float m, s, t;
 };
 
 // Makes `top` the maximum the sums are relative to, if it is larger.
 template <bool ENT> __device__ __forceinline__ void raise(Running &st, float top, float c)
 {
     if (top > st.m) {
-        if (st.s.x + st.s.y != 0.f) {
-            const float d = max_nan((st.m - top) * c, -1000.f), f = ex2(d);
-            if (ENT) st.t = mul2(both(f), fma2(st.s, both(d), st.t));
-            st.s = mul2(st.s, both(f));
+        if (st.s != 0.f) {
+            const Reference old(st.m, c), now(top, c);
+            const float d = max_nan(old.far || now.far ? (st.m - top) * c : old.base - now.base, -1000.f), f = ex2(d);
+            if (ENT) st.t = f * fmaf(st.s, d, st.t);
+            st.s *= f;
         }
         st.m = top;
     }
 }
 
-// Adds a granule; no element is larger than the maximum.
-template <class T, bool ENT> __device__ __forceinline__ void accumulate(uint4 raw, float c, Running &st)
+// Adds U granules of each thread of a warp; no element is larger than its thread's maximum.
+template <class T, int U, bool ENT> __device__ __forceinline__ void accumulate(const uint4 *raw, float c, Running &st)
 {
-    const float2 minus = both(st.m == neg_inf() ? 0.f : -st.m), scale = both(c);
-    float2 f[Elem<T>::kVec / 2];
-    Elem<T>::pairs(raw, f);
+    const Reference ref(st.m, c);
+    if (__any_sync(0xffffffffu, ref.far)) {
 #pragma unroll
-    for (int i = 0; i < Elem<T>::kVec / 2; ++i) {
-        float2 d = mul2(add2(f[i], minus), scale);
-        if (ENT) d = make_float2(max_nan(d.x, -1000.f), max_nan(d.y, -1000.f));  // an id that is not allowed adds 0 rather than 0 times -inf
-        const float2 e = make_float2(ex2(d.x), ex2(d.y));
-        st.s = add2(st.s, e);
-        if (ENT) st.t = fma2(e, d, st.t);
+        for (int u = 0; u < U; ++u) {
+            float f[Elem<T>::kVec];
+            Elem<T>::unpack(raw[u], f);
+#pragma unroll 1
+            for (int i = 0; i < Elem<T>::kVec; ++i) {
+                const float d = max_nan(ref.far ? (f[0] - ref.sub) * c : fmaf(f[0], c, -ref.base), -1000.f), e = ex2(d);
+                st.s += e;
+                st.t = fmaf(e, d, st.t);
+#pragma unroll
+                for (int j = 0; j + 1 < Elem<T>::kVec; ++j) f[j] = f[j + 1];
+            }
+        }
+        return;
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float f[Elem<T>::kVec];
+        Elem<T>::unpack(raw[u], f);
+#pragma unroll
+        for (int i = 0; i < Elem<T>::kVec; ++i) {
+            float d = fmaf(f[i], c, -ref.base);
+            if (ENT) d = max_nan(d, -1000.f);  // an id that is not allowed adds 0 rather than 0 times -inf
+            const float e = ex2(d);
+            st.s += e;
+            if (ENT) st.t = fmaf(e, d, st.t);
+        }
+    }
+}
+
+// The sums relative to m itself.
+template <bool ENT> __device__ __forceinline__ void settle(Running &st, float c)
+{
+    const Reference ref(st.m, c);
+    if (ref.far || st.s == 0.f) return;
+    const float r = fmaf(st.m, c, -ref.base), f = ex2(-r);
+    if (ENT) st.t = f * fmaf(-r, st.s, st.t);
+    st.s *= f;
 }
 
 // -inf in place of the elements whose bit is set
@@ -502,10 +545,11 @@ template <bool TAIL> __device__ __forceinline__ float teacher_loss(const Teacher
 enum { kLogprobs = 0, kLogprobsTop = 1, kDistill = 2, kDistillTail = 3 };
 enum { kNoGrad = 0, kGrad = 1, kGradSaved = 2 };  // no gradient; from this call's sums; from a forward call's
 
-template <bool ENT, bool TAIL> __device__ __forceinline__ Stats warp_stats(const Running &run, float mi, float si, float c)
+template <bool ENT, bool TAIL> __device__ __forceinline__ Stats warp_stats(Running run, float mi, float si, float c)
 {
+    settle<ENT>(run, c);
     // the warp's maximum first, so that every lane rescales once and the rest are additions
-    Stats st = {warp_max(run.m), run.s.x + run.s.y, ENT ? run.t.x + run.t.y : 0.f, mi, si};
+    Stats st = {warp_max(run.m), run.s, run.t, mi, si};
     if (st.s != 0.f) {
         const float d = max_nan((run.m - st.m) * c, -1000.f), f = ex2(d);
         if (ENT) st.t = f * fmaf(st.s, d, st.t);
@@ -622,31 +666,69 @@ __device__ __forceinline__ RowGrad token_gradient_saved(const LossArgs &a, int64
     return k;
 }
 
-template <class T, bool ENT> __device__ __forceinline__ uint4 gradient_of(uint4 raw, float c, const RowGrad &k)
-{
-    const float2 minus = both(-k.m), scale = both(c), k0 = both(k.k0), k1 = both(k.k1);
-    float2 f[Elem<T>::kVec / 2];
-    Elem<T>::pairs(raw, f);
-#pragma unroll
-    for (int i = 0; i < Elem<T>::kVec / 2; ++i) {
-        float2 d = mul2(add2(f[i], minus), scale);
-        if (ENT) d = make_float2(max_nan(d.x, -1000.f), max_nan(d.y, -1000.f));
-        f[i] = mul2(make_float2(ex2(d.x), ex2(d.y)), ENT ? fma2(k1, d, k0) : k0);
+// How a row's elements are turned into their gradients and written.
+template <class T, bool ENT> struct GradientWriter {
+    T *out;
+    bool same, entropy;
+    Reference ref;
+    float k0, k1;  // relative to `ref` (see settle)
+    uint64_t policy;
+    __device__ __forceinline__ GradientWriter(const Row<T> &row, T *to, const RowGrad &k, float c) : out(to), same(row.same_lead(to)), ref(k.m, c), policy(leave_first())
+    {
+        const float r = ref.far ? 0.f : fmaf(k.m, c, -ref.base), f = ex2(-r);
+        entropy = ENT && k.k1 != 0.f;
+        k0 = f * fmaf(-r, k.k1, k.k0);
+        k1 = f * k.k1;
     }
-    return Elem<T>::pack(f);
-}
-
-// Granules g, g + step, ... of a row below `limit`; `entropy`: k1 is not zero (the same for all threads of the row).
-template <class T, int U>
-__device__ __forceinline__ void write_gradient(const uint4 *raw, const Row<T> &row, T *out, bool same, int g, int step, int limit, float c, const RowGrad &k, bool entropy)
-{
+    template <bool ENTROPY> __device__ __forceinline__ uint4 gradient(uint4 raw, float c) const
+    {
+        float f[Elem<T>::kVec];
+        Elem<T>::unpack(raw, f);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int gu = g + u * step;
-        if (gu >= limit) continue;
-        row.store(out, same, gu, entropy ? gradient_of<T, true>(raw[u], c, k) : gradient_of<T, false>(raw[u], c, k));
+        for (int i = 0; i < Elem<T>::kVec; ++i) {
+            float d = fmaf(f[i], c, -ref.base);
+            if (ENTROPY) {
+                d = max_nan(d, -1000.f);
+                f[i] = ex2(d) * fmaf(k1, d, k0);
+            } else {
+                f[i] = ex2(d) * k0;
+            }
+        }
+        return Elem<T>::pack(f);
     }
-}
+    // Any reference, any factors, any alignment.
+    template <int NT, int U> __device__ __forceinline__ void write_slowly(const Step<T, NT, U> &step, const uint4 *raw, float c) const
+    {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[Elem<T>::kVec];
+            Elem<T>::unpack(raw[u], f);
+#pragma unroll 1
+            for (int i = 0; i < Elem<T>::kVec; ++i) {
+                const float d = max_nan(ref.far ? (f[0] - ref.sub) * c : fmaf(f[0], c, -ref.base), -1000.f), g = ex2(d) * (entropy ? fmaf(k1, d, k0) : k0);
+#pragma unroll
+                for (int j = 0; j + 1 < Elem<T>::kVec; ++j) f[j] = f[j + 1];
+                f[Elem<T>::kVec - 1] = g;
+            }
+            step.store_part_of(out, same, u, Elem<T>::pack(f));
+        }
+    }
+    template <int NT, int U> __device__ __forceinline__ void write(const Step<T, NT, U> &step, const uint4 *raw, float c) const
+    {
+        if (!step.plain || !same || ref.far) {
+            write_slowly<NT, U>(step, raw, c);
+            return;
+        }
+        T *to = out + step.row.first(step.g);
+        if (ENT && entropy) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) store_hint(to + u * NT * Elem<T>::kVec, gradient<true>(raw[u], c), policy);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) store_hint(to + u * NT * Elem<T>::kVec, gradient<false>(raw[u], c), policy);
+        }
+    }
+};
 
 // The given token's element, written again by one thread behind a barrier.
 template <class T> __device__ __forceinline__ void write_token_gradient(T *out, int token, float x, float c, const RowGrad &k)
@@ -812,8 +894,8 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
     const int G = row.granules();
     TeacherShared &teacher = sh.teacher[TEACHER ? warp : 0];
     uint4 raw[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = row.load_below(u * 32 + lane, G);
+    const Step<T, 32, U> step(row, 0, lane, G);
+    step.load(raw);
     int token = -1;
     float token_x = 0.f, mi = neg_inf(), si = 0.f;
     if (TEACHER) {
@@ -839,14 +921,12 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
     }
     RowGrad k;
     if (GRAD != kGradSaved) {
-        Running run = {neg_inf(), both(0.f), both(0.f)};
+        Running run = {neg_inf(), 0.f, 0.f};
         float all = Elem<T>::max_of(raw[0]);
 #pragma unroll
         for (int u = 1; u < U; ++u) all = fmaxf(all, Elem<T>::max_of(raw[u]));
         raise<ENT>(run, all, a.c);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u * 32 < G) accumulate<T, ENT>(raw[u], a.c, run);
+        accumulate<T, U, ENT>(raw, a.c, run);
         const Stats st = warp_stats<ENT, TAIL>(run, mi, si, a.c);
         const RowEnd e = row_end<TAIL>(st, a.c);
         if (lane == 0) write_sums<ENT, TAIL>(a, r, st, e, token, token_x);
@@ -875,7 +955,7 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
     // the elements are unpacked again rather than kept unpacked in twice the registers
 #pragma unroll
     for (int u = 0; u < U; ++u) asm volatile("" : "+r"(raw[u].x), "+r"(raw[u].y), "+r"(raw[u].z), "+r"(raw[u].w));
-    write_gradient<T, U>(raw, row, out, row.same_lead(out), lane, 32, G, a.c, k, ENT && k.k1 != 0.f);
+    GradientWriter<T, ENT>(row, out, k, a.c).write(step, raw, a.c);
     __syncwarp();
     if (TEACHER) write_set_gradient<T>(teacher, a.K, out, 0, row.n, a.c, k, lane, 32);
     else if (lane == 0 && token >= 0 && token < a.V) write_token_gradient<T>(out, token, token_x, a.c, k);
@@ -930,8 +1010,7 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
     const auto begin_row = [&](int64_t at) {  // a row's first granules; nothing beyond the last row
         if (at >= a.R) return;
         const Share<T> s(a, at, C, rank);
-#pragma unroll
-        for (int u = 0; u < U; ++u) next[u] = s.row.load_below(s.g0 + u * NT + tid, s.g1);
+        Step<T, NT, U>(s.row, s.g0, tid, s.g1).load(next);
     };
     begin_row(r);
     if (TAIL) {
@@ -943,7 +1022,7 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
         const Share<T> share(a, r, C, rank);
         const Row<T> &row = share.row;
         const int g0 = share.g0, g1 = share.g1;
-        Running run = {neg_inf(), both(0.f), both(0.f)};
+        Running run = {neg_inf(), 0.f, 0.f};
         float mi = neg_inf(), si = 0.f;
         int token = -1;
         float token_x = 0.f;
@@ -976,15 +1055,9 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
                 uint4 cur[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) cur[u] = next[u];
-                if (base + STEP < g1) {
-#pragma unroll
-                    for (int u = 0; u < U; ++u) next[u] = row.load_below(base + STEP + u * NT + tid, g1);
-                } else if (GRAD) {  // the second reading begins where the first ends
-#pragma unroll
-                    for (int u = 0; u < U; ++u) next[u] = cur[u];
-                } else if (!TOP) {
-                    begin_row(r + stride);
-                }
+                // with a gradient the second reading begins where this one ends: `next` stays
+                if (base + STEP < g1) Step<T, NT, U>(row, base + STEP, tid, g1).load(next);
+                else if (!GRAD && !TOP) begin_row(r + stride);
                 if (TAIL) {
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
@@ -1003,9 +1076,7 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
                     *slot = key;
                 }
                 raise<ENT>(run, all, a.c);
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (base + u * NT + (warp << 5) < g1) accumulate<T, ENT>(cur[u], a.c, run);
+                accumulate<T, U, ENT>(cur, a.c, run);
             }
             if (TAIL) {
                 __syncthreads();
@@ -1074,18 +1145,14 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
         if (GRAD) {
             T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
             const RowGrad k = TEACHER ? teacher_gradient<TAIL>(a, r, e, teacher) : token_gradient(a, r, st, e, token);
-            const bool same = row.same_lead(out), entropy = !TEACHER && k.k1 != 0.f;
+            const GradientWriter<T, ENT> writer(row, out, k, a.c);
             for (int base = g0 + (steps - 1) * STEP; base >= g0; base -= STEP) {
                 uint4 cur[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) cur[u] = next[u];
-                if (base > g0) {
-#pragma unroll
-                    for (int u = 0; u < U; ++u) next[u] = row.template load_below<true>(base - STEP + u * NT + tid, g1);
-                } else {
-                    begin_row(r + stride);
-                }
-                write_gradient<T, U>(cur, row, out, same, base + tid, NT, g1, a.c, k, entropy);
+                if (base > g0) Step<T, NT, U>(row, base - STEP, tid, g1).load(next, writer.policy);
+                else begin_row(r + stride);
+                writer.write(Step<T, NT, U>(row, base, tid, g1), cur, a.c);
             }
             if (g0 == g1) begin_row(r + stride);
             __syncthreads();
@@ -1114,8 +1181,7 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
     int token = -1;
     float token_x = 0.f;
     uint4 next[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) next[u] = row.load_below(g0 + threadIdx.x + u * NT, g1);
+    Step<T, NT, U>(row, g0, threadIdx.x, g1).load(next, leave_first());
     if constexpr (TEACHER) {
         if (threadIdx.x == 0) shared.bad = 0;
         __syncthreads();
@@ -1131,14 +1197,13 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
         if (threadIdx.x == 0 && token >= 0) token_x = Elem<T>::to_float(row.p[token]);
         __syncthreads();  // read before it is overwritten in place
     }
-    const bool same = row.same_lead(out), entropy = !TEACHER && k.k1 != 0.f;
-    for (int g = g0 + threadIdx.x; g - static_cast<int>(threadIdx.x) < g1; g += NT * U) {
-        uint4 raw[U];
+    const GradientWriter<T, !TEACHER> writer(row, out, k, a.c);
+    for (int base = g0; base < g1; base += NT * U) {
+        uint4 cur[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = next[u];
-#pragma unroll
-        for (int u = 0; u < U; ++u) next[u] = row.load_below(g + (U + u) * NT, g1);
-        write_gradient<T, U>(raw, row, out, same, g, NT, g1, a.c, k, entropy);
+        for (int u = 0; u < U; ++u) cur[u] = next[u];
+        if (base + NT * U < g1) Step<T, NT, U>(row, base + NT * U, threadIdx.x, g1).load(next, writer.policy);
+        writer.write(Step<T, NT, U>(row, base, threadIdx.x, g1), cur, a.c);
     }
     __syncthreads();
     if constexpr (TEACHER) write_set_gradient<T>(shared, a.K, out, row.first(g0), row.first(g1), a.c, k, threadIdx.x, NT);
