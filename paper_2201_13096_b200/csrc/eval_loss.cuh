@@ -4,6 +4,7 @@
 // Mathematics.  Everything is kept in base 2: with c = log2(e) / T and the running maximum m of the logits, d_v = (x_v - m) c
 // and s = sum 2^d, a probability is 2^d_v / s.  The entropy needs t = sum 2^d d beside s: H = ln 2 (log2 s - t / s).  When the
 // maximum rises by delta / c, s becomes s 2^-delta and t becomes (t - s delta) 2^-delta.
+// m need not be the maximum: any logit that is at most 2^64 below it does (see raise), so that the sums are rescaled rarely.
 // An element costs one fused multiply-add x c - b with b = m c rounded; the rounding r = m c - b is the same for all elements and
 // is taken back once per thread (2^-r s, and t - r s for t).  Where m c is so large that x c could overflow (rows of the type's
 // lowest value) m is subtracted first instead.  Beside that one instruction to unpack, one for the special-function unit
@@ -117,15 +118,15 @@ struct Reference {
     }
 };
 
-// What a thread has added up, relative to Reference(m, c).
+// What a thread has added up, relative to Reference(m, c): m is some logit, no other is more than 64 / c above it.
 struct Running {
     float m, s, t;
 };
 
-// Makes `top` the maximum the sums are relative to, if it is larger.
+// Makes `top` the logit the sums are relative to, if it is far above the present one (or the first).
 template <bool ENT> __device__ __forceinline__ void raise(Running &st, float top, float c)
 {
-    if (top > st.m) {
+    if (top > st.m && (top - st.m) * c > 64.f) {
         if (st.s != 0.f) {
             const Reference old(st.m, c), now(top, c);
             const float d = max_nan(old.far || now.far ? (st.m - top) * c : old.base - now.base, -1000.f), f = ex2(d);
@@ -136,7 +137,7 @@ template <bool ENT> __device__ __forceinline__ void raise(Running &st, float top
     }
 }
 
-// Adds U granules of each thread of a warp; no element is larger than its thread's maximum.
+// Adds U granules of each thread of a warp, after raise.
 template <class T, int U, bool ENT> __device__ __forceinline__ void accumulate(const uint4 *raw, float c, Running &st)
 {
     const Reference ref(st.m, c);
@@ -548,7 +549,7 @@ enum { kNoGrad = 0, kGrad = 1, kGradSaved = 2 };  // no gradient; from this call
 template <bool ENT, bool TAIL> __device__ __forceinline__ Stats warp_stats(Running run, float mi, float si, float c)
 {
     settle<ENT>(run, c);
-    // the warp's maximum first, so that every lane rescales once and the rest are additions
+    // the warp's largest reference first, so that every lane rescales once and the rest are additions
     Stats st = {warp_max(run.m), run.s, run.t, mi, si};
     if (st.s != 0.f) {
         const float d = max_nan((run.m - st.m) * c, -1000.f), f = ex2(d);
@@ -696,27 +697,25 @@ template <class T, bool ENT> struct GradientWriter {
         }
         return Elem<T>::pack(f);
     }
-    // Any reference, any factors, any alignment.
-    template <int NT, int U> __device__ __forceinline__ void write_slowly(const Step<T, NT, U> &step, const uint4 *raw, float c) const
+    // A granule's elements one by one, with a far reference.
+    static __device__ __noinline__ uint4 far_gradient(uint4 raw, float c, float sub, float k0, float k1)
     {
+        float f[Elem<T>::kVec];
+        Elem<T>::unpack(raw, f);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float f[Elem<T>::kVec];
-            Elem<T>::unpack(raw[u], f);
-#pragma unroll 1
-            for (int i = 0; i < Elem<T>::kVec; ++i) {
-                const float d = max_nan(ref.far ? (f[0] - ref.sub) * c : fmaf(f[0], c, -ref.base), -1000.f), g = ex2(d) * (entropy ? fmaf(k1, d, k0) : k0);
-#pragma unroll
-                for (int j = 0; j + 1 < Elem<T>::kVec; ++j) f[j] = f[j + 1];
-                f[Elem<T>::kVec - 1] = g;
-            }
-            step.store_part_of(out, same, u, Elem<T>::pack(f));
+        for (int i = 0; i < Elem<T>::kVec; ++i) {
+            const float d = max_nan((f[i] - sub) * c, -1000.f);
+            f[i] = ex2(d) * fmaf(k1, d, k0);
         }
+        return Elem<T>::pack(f);
     }
     template <int NT, int U> __device__ __forceinline__ void write(const Step<T, NT, U> &step, const uint4 *raw, float c) const
     {
         if (!step.plain || !same || ref.far) {
-            write_slowly<NT, U>(step, raw, c);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (step.g + u * NT < step.limit)
+                    step.store_part_of(out, same, u, ref.far ? far_gradient(raw[u], c, ref.sub, k0, k1) : ENT && entropy ? gradient<true>(raw[u], c) : gradient<false>(raw[u], c));
             return;
         }
         T *to = out + step.row.first(step.g);
