@@ -667,19 +667,28 @@ __device__ __forceinline__ RowGrad token_gradient_saved(const LossArgs &a, int64
     return k;
 }
 
+// A row's factors relative to Reference(m, c) (compare settle).
+struct Factors {
+    Reference ref;
+    float k0, k1;
+    __device__ __forceinline__ Factors(const RowGrad &k, float c) : ref(k.m, c)
+    {
+        const float r = ref.far ? 0.f : fmaf(k.m, c, -ref.base), f = ex2(-r);
+        k0 = f * fmaf(-r, k.k1, k.k0);
+        k1 = f * k.k1;
+    }
+};
+
 // How a row's elements are turned into their gradients and written.
 template <class T, bool ENT> struct GradientWriter {
     T *out;
     bool same, entropy;
     Reference ref;
-    float k0, k1;  // relative to `ref` (see settle)
+    float k0, k1;
     uint64_t policy;
-    __device__ __forceinline__ GradientWriter(const Row<T> &row, T *to, const RowGrad &k, float c) : out(to), same(row.same_lead(to)), ref(k.m, c), policy(leave_first())
+    __device__ __forceinline__ GradientWriter(const Row<T> &row, T *to, const Factors &f)
+        : out(to), same(row.same_lead(to)), entropy(ENT && f.k1 != 0.f), ref(f.ref), k0(f.k0), k1(f.k1), policy(leave_first())
     {
-        const float r = ref.far ? 0.f : fmaf(k.m, c, -ref.base), f = ex2(-r);
-        entropy = ENT && k.k1 != 0.f;
-        k0 = f * fmaf(-r, k.k1, k.k0);
-        k1 = f * k.k1;
     }
     template <bool ENTROPY> __device__ __forceinline__ uint4 gradient(uint4 raw, float c) const
     {
@@ -954,7 +963,7 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
     // the elements are unpacked again rather than kept unpacked in twice the registers
 #pragma unroll
     for (int u = 0; u < U; ++u) asm volatile("" : "+r"(raw[u].x), "+r"(raw[u].y), "+r"(raw[u].z), "+r"(raw[u].w));
-    GradientWriter<T, ENT>(row, out, k, a.c).write(step, raw, a.c);
+    GradientWriter<T, ENT>(row, out, Factors(k, a.c)).write(step, raw, a.c);
     __syncwarp();
     if (TEACHER) write_set_gradient<T>(teacher, a.K, out, 0, row.n, a.c, k, lane, 32);
     else if (lane == 0 && token >= 0 && token < a.V) write_token_gradient<T>(out, token, token_x, a.c, k);
@@ -968,7 +977,9 @@ constexpr int kRowThreads = 768;    // threads a multiprocessor holds of the lon
 template <int NT> struct RowShared {
     Stats part[NT / 32];
     Stats pub;       // this block's sums, read by the cluster's other blocks
-    Stats total;     // the row's
+    RowEnd end;      // the row's
+    RowGrad grad;
+    Factors factors;
     uint32_t found;  // entries of top.best
 };
 
@@ -994,7 +1005,8 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
     constexpr bool TEACHER = MODE >= kDistill, TAIL = MODE == kDistillTail;
     constexpr int NW = NT / 32, STEP = NT * U;
     extern __shared__ __align__(16) unsigned char dynamic[];
-    __shared__ RowShared<NT> sh;
+    __shared__ __align__(16) unsigned char shared_bytes[sizeof(RowShared<NT>)];
+    RowShared<NT> &sh = *reinterpret_cast<RowShared<NT> *>(shared_bytes);
     TopShared &top = *reinterpret_cast<TopShared *>(dynamic);                               // TOP
     uint32_t *groups = reinterpret_cast<uint32_t *>(dynamic + sizeof(TopShared));           // TOP
     TeacherShared &teacher = *reinterpret_cast<TeacherShared *>(dynamic);                   // TEACHER
@@ -1087,11 +1099,12 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
         Stats st = warp_stats<ENT, TAIL>(run, mi, si, a.c);
         if (lane == 0) sh.part[warp] = st;
         __syncthreads();
+        // The first warp alone joins the sums and works out what the row needs; a row's other threads only read the factors.
         if (warp == 0) {
             st = lane < NW ? sh.part[lane] : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
 #pragma unroll
             for (int d = NW / 2; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-            if (lane == 0) sh.pub = sh.total = st;
+            if (C > 1 && lane == 0) sh.pub = st;
         }
         if (TOP) {
             const int e0 = max(0, row.first(g0)), e1 = min(row.n, row.first(g1));
@@ -1105,7 +1118,6 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
                 st = lane < C ? *cluster.map_shared_rank(&sh.pub, lane) : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
 #pragma unroll
                 for (int d = 4; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-                if (lane == 0) sh.total = st;
             }
             if (TOP && rank == 0) {
                 int n = 0;  // the blocks' lists side by side
@@ -1124,27 +1136,33 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
                 select_top<NT>(top, n, a.K);
             }
         }
-        __syncthreads();
-        st = sh.total;
-        const RowEnd e = row_end<TAIL>(st, a.c);
+        if (warp == 0 && (rank == 0 || GRAD)) {
+            const RowEnd e = row_end<TAIL>(st, a.c);
+            if (GRAD) {
+                const RowGrad k = TEACHER ? teacher_gradient<TAIL>(a, r, e, teacher) : token_gradient(a, r, st, e, token);
+                const Factors f(k, a.c);
+                if (lane == 0) sh.grad = k, sh.factors = f;
+            }
+            if (lane == 0) sh.end = e;
+            if (lane == 0 && rank == 0) write_sums<ENT, TAIL>(a, r, st, e, token, token_x);
+        }
+        if (GRAD || TEACHER || TOP) __syncthreads();
         if (rank == 0) {
-            if (tid == 0) write_sums<ENT, TAIL>(a, r, st, e, token, token_x);
             if (TEACHER && warp == NW - 1 && a.loss) {
-                const float loss = teacher_loss<TAIL>(teacher, e, a.inv_t, a.K);
+                const float loss = teacher_loss<TAIL>(teacher, sh.end, a.inv_t, a.K);
                 if (lane == 0) a.loss[r] = loss;
             }
             if (TOP) {
                 for (int i = tid; i < a.K; i += NT) {
                     const uint64_t key = top.best[i];
                     a.top_ids[r * a.K + i] = static_cast<int32_t>(~static_cast<uint32_t>(key));
-                    a.top_logprobs[r * a.K + i] = log_prob(unordered(static_cast<uint32_t>(key >> 32)), e, a.inv_t);
+                    a.top_logprobs[r * a.K + i] = log_prob(unordered(static_cast<uint32_t>(key >> 32)), sh.end, a.inv_t);
                 }
             }
         }
         if (GRAD) {
             T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
-            const RowGrad k = TEACHER ? teacher_gradient<TAIL>(a, r, e, teacher) : token_gradient(a, r, st, e, token);
-            const GradientWriter<T, ENT> writer(row, out, k, a.c);
+            const GradientWriter<T, ENT> writer(row, out, sh.factors);
             for (int base = g0 + (steps - 1) * STEP; base >= g0; base -= STEP) {
                 uint4 cur[U];
 #pragma unroll
@@ -1155,8 +1173,8 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
             }
             if (g0 == g1) begin_row(r + stride);
             __syncthreads();
-            if (TEACHER) write_set_gradient<T>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, k, tid, NT);
-            else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, k);
+            if (TEACHER) write_set_gradient<T>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, sh.grad, tid, NT);
+            else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, sh.grad);
         } else if (TOP || g0 == g1) {  // the search for the alternatives needs the registers
             begin_row(r + stride);
         }
@@ -1196,7 +1214,7 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
         if (threadIdx.x == 0 && token >= 0) token_x = Elem<T>::to_float(row.p[token]);
         __syncthreads();  // read before it is overwritten in place
     }
-    const GradientWriter<T, !TEACHER> writer(row, out, k, a.c);
+    const GradientWriter<T, !TEACHER> writer(row, out, Factors(k, a.c));
     for (int base = g0; base < g1; base += NT * U) {
         uint4 cur[U];
 #pragma unroll
