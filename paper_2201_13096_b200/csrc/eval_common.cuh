@@ -46,25 +46,17 @@ __device__ __forceinline__ uint4 load_stream(const void *p)
     return v;
 }
 
-// L2 policy for what is read for the last time, or written to be read much later: first to leave.
-__device__ __forceinline__ uint64_t leave_first()
-{
-    uint64_t policy;
-    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
-    return policy;
-}
-__device__ __forceinline__ uint4 load_hint(const void *p, uint64_t policy)
+// Read for the last time, or written to be read much later: first to leave L2 (the streaming forms need no policy register;
+// with an explicit one each access cost two more instructions).
+__device__ __forceinline__ uint4 load_last(const void *p)
 {
     uint4 v;
-    asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
-                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                 : "l"(p), "l"(policy)
-                 : "memory");
+    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
     return v;
 }
-__device__ __forceinline__ void store_hint(void *p, uint4 v, uint64_t policy)
+__device__ __forceinline__ void store_last(void *p, uint4 v)
 {
-    asm volatile("st.global.L1::no_allocate.L2::cache_hint.v4.u32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "l"(policy) : "memory");
+    asm volatile("st.global.cs.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 __device__ __forceinline__ void store_stream(void *p, uint4 v)
 {
@@ -233,12 +225,12 @@ template <class T, int NT, int U> struct Step {
             for (int u = 0; u < U; ++u) v[u] = load_part_of(u);
         }
     }
-    __device__ __forceinline__ void load(uint4 *v, uint64_t policy) const
+    __device__ __forceinline__ void load_again(uint4 *v) const  // not to be read after this
     {
         if (plain) {
             const T *p = row.p + row.first(g);
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = load_hint(p + u * NT * Elem<T>::kVec, policy);
+            for (int u = 0; u < U; ++u) v[u] = load_last(p + u * NT * Elem<T>::kVec);
         } else {
 #pragma unroll
             for (int u = 0; u < U; ++u) v[u] = load_part_of(u);

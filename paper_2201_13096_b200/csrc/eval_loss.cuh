@@ -685,9 +685,8 @@ template <class T, bool ENT> struct GradientWriter {
     bool same, entropy;
     Reference ref;
     float k0, k1;
-    uint64_t policy;
     __device__ __forceinline__ GradientWriter(const Row<T> &row, T *to, const Factors &f)
-        : out(to), same(row.same_lead(to)), entropy(ENT && f.k1 != 0.f), ref(f.ref), k0(f.k0), k1(f.k1), policy(leave_first())
+        : out(to), same(row.same_lead(to)), entropy(ENT && f.k1 != 0.f), ref(f.ref), k0(f.k0), k1(f.k1)
     {
     }
     template <bool ENTROPY> __device__ __forceinline__ uint4 gradient(uint4 raw, float c) const
@@ -730,10 +729,10 @@ template <class T, bool ENT> struct GradientWriter {
         T *to = out + step.row.first(step.g);
         if (ENT && entropy) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) store_hint(to + u * NT * Elem<T>::kVec, gradient<true>(raw[u], c), policy);
+            for (int u = 0; u < U; ++u) store_last(to + u * NT * Elem<T>::kVec, gradient<true>(raw[u], c));
         } else {
 #pragma unroll
-            for (int u = 0; u < U; ++u) store_hint(to + u * NT * Elem<T>::kVec, gradient<false>(raw[u], c), policy);
+            for (int u = 0; u < U; ++u) store_last(to + u * NT * Elem<T>::kVec, gradient<false>(raw[u], c));
         }
     }
 };
@@ -1167,7 +1166,7 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
                 uint4 cur[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) cur[u] = next[u];
-                if (base > g0) Step<T, NT, U>(row, base - STEP, tid, g1).load(next, writer.policy);
+                if (base > g0) Step<T, NT, U>(row, base - STEP, tid, g1).load_again(next);
                 else begin_row(r + stride);
                 writer.write(Step<T, NT, U>(row, base, tid, g1), cur, a.c);
             }
@@ -1198,7 +1197,7 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
     int token = -1;
     float token_x = 0.f;
     uint4 next[U];
-    Step<T, NT, U>(row, g0, threadIdx.x, g1).load(next, leave_first());
+    Step<T, NT, U>(row, g0, threadIdx.x, g1).load_again(next);
     if constexpr (TEACHER) {
         if (threadIdx.x == 0) shared.bad = 0;
         __syncthreads();
@@ -1219,7 +1218,7 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
         uint4 cur[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) cur[u] = next[u];
-        if (base + NT * U < g1) Step<T, NT, U>(row, base + NT * U, threadIdx.x, g1).load(next, writer.policy);
+        if (base + NT * U < g1) Step<T, NT, U>(row, base + NT * U, threadIdx.x, g1).load_again(next);
         writer.write(Step<T, NT, U>(row, base, threadIdx.x, g1), cur, a.c);
     }
     __syncthreads();
