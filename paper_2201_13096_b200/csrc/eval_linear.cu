@@ -2,7 +2,9 @@
 //
 // The product runs on the tensor cores (tcgen05, 16-bit operands, fp32 accumulators in TMEM); one thread feeds it with TMA
 // copies of 64-wide slices of x and w, one issues the matrix instructions, eight warps carry the finished tiles through the
-// epilogue while the next tile is multiplied.  Few rows (single tokens) are a matter of reading w once: a kernel of plain
+// epilogue while the next tile is multiplied.  Large products pair two multiprocessors on a tile of 256 rows (cta_group::2), so
+// that each reads half of the tile's slice of w: with one multiprocessor per 128 x 256 tile the slices took about 15 TB/s out of
+// L2, which was the limit (8192^3: 1.29 PFLOP/s).  Few rows (single tokens) are a matter of reading w once: a kernel of plain
 // multiply-adds streams it.
 #include <cuda.h>
 
@@ -25,7 +27,7 @@ struct LinearArgs {
     int64_t ldx, ldw, ldres, ldy, M, N, K;
     int dtype, bias_type, out_type, activation;
     int tiles_m, tiles_n, k_blocks;
-    int wide_out, wide_res;                // 16-byte accesses are possible on every row of y, of residual
+    int wide_out, wide_res, wide_bias;     // 16-byte accesses are possible on every row of y, of residual, on bias
 };
 
 __device__ int g_timeouts;                 // waits that ran out of time (none in a working run); spdy_linear_check_status
@@ -69,15 +71,54 @@ __device__ __forceinline__ void tma_load(void *to, const CUtensorMap *map, int x
 // Descriptor of a K-major operand whose rows are 128 bytes under the 128-byte swizzle: groups of 8 rows lie 1024 bytes apart.
 __device__ __forceinline__ uint64_t operand(uint32_t addr) { return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | 1ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61; }
 
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+// The address of a shared variable in the first block of the cluster.
+__device__ __forceinline__ uint32_t first_blocks(uint32_t addr)
 {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
-                 "r"(static_cast<uint32_t>(add))
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+__device__ __forceinline__ void barrier_arrive_at(uint32_t addr) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory"); }
+// A copy to this block's shared memory that counts on a barrier of either block of the pair.
+__device__ __forceinline__ void tma_load_pair(void *to, const CUtensorMap *map, int x, int y, uint32_t barrier)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_addr(to)),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(barrier)
                  : "memory");
 }
-__device__ __forceinline__ void mma_commit(uint64_t *b)
+
+template <bool PAIR> __device__ __forceinline__ void tmem_alloc(uint32_t *to, int columns)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(b)) : "memory");
+    if (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+}
+template <bool PAIR> __device__ __forceinline__ void tmem_free(uint32_t tmem, int columns)
+{
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+}
+template <bool PAIR> __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    if (PAIR)
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+                     "r"(static_cast<uint32_t>(add))
+                     : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+                     "r"(static_cast<uint32_t>(add))
+                     : "memory");
+}
+// Signals the barrier (of both blocks of a pair) when the products issued so far are done.
+template <bool PAIR> __device__ __forceinline__ void mma_commit(uint64_t *b)
+{
+    if (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(b)), "h"(static_cast<uint16_t>(3)) : "memory");
+    else asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(b)) : "memory");
 }
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t *v)
 {
@@ -93,12 +134,49 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t *v)
 }
 
 // ---------------------------------------------------------------------------------------------- epilogue
-template <int ACT> __device__ __forceinline__ float activate(float z)
+// Two fp32 operations per instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 {
-    if (ACT == SPDY_ACT_RELU) return max_nan(z, 0.f);
-    if (ACT == SPDY_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    if (ACT == SPDY_ACT_SILU) return z == neg_inf() ? 0.f : __fdividef(z, 1.f + ex2(-z * kLog2e));
-    return z;
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long &>(r))
+        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)), "l"(reinterpret_cast<unsigned long long &>(c)));
+    return r;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// z Phi(z), Phi the normal distribution function.  Phi(z) - 1/2 = z Q(z^2) with Q a polynomial of degree 13 on |z| <= 5 (least
+// maximum of |z Q - (Phi - 1/2)| by reweighted Chebyshev fits, 3e-8; 1.1e-7 with fp32 arithmetic), in the variable
+// 2 z^2 / 25 - 1, where its coefficients' magnitudes sum to 0.4.  Beyond -5 (Phi below 2.9e-7) the result is -0, beyond 5 z.
+// The library's erff costs about 38 instructions here, this 12 in pairs.
+template <int N> __device__ __forceinline__ void gelu(float *f)
+{
+    constexpr float kQ[14] = {-0.000253382081f, 0.000710501277f, -0.000840798195f, 0.00144300074f, -0.00358738378f, 0.00669657066f, -0.0106615145f, 0.0162687358f, -0.0234041531f, 0.0314699598f, -0.0404270627f, 0.0515184402f, -0.0702967867f, 0.141363814f};
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+        const float z0 = f[i], z1 = f[i + (N > 1)];
+        const float2 c = make_float2(fminf(fmaxf(z0, -5.f), 5.f), fminf(fmaxf(z1, -5.f), 5.f));
+        const float2 x = fma2(make_float2(c.x * 0.08f, c.y * 0.08f), c, both(-1.f));
+        float2 q = both(kQ[0]);
+#pragma unroll
+        for (int k = 1; k < 14; ++k) q = fma2(q, x, both(kQ[k]));
+        const float2 phi = fma2(q, c, both(0.5f));
+        f[i] = z0 * (z0 < -5.f ? 0.f : phi.x);
+        if (N > 1) f[i + 1] = z1 * (z1 < -5.f ? 0.f : phi.y);
+    }
+}
+
+template <int ACT, int N> __device__ __forceinline__ void activate(float *f)
+{
+    if constexpr (ACT == SPDY_ACT_GELU) {
+        gelu<N>(f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (ACT == SPDY_ACT_RELU) f[i] = max_nan(f[i], 0.f);
+            if (ACT == SPDY_ACT_SILU) f[i] = f[i] == neg_inf() ? 0.f : __fdividef(f[i], 1.f + ex2(-f[i] * kLog2e));
+        }
+    }
 }
 
 __device__ __forceinline__ float bias_at(const LinearArgs &a, int64_t n)
@@ -108,28 +186,49 @@ __device__ __forceinline__ float bias_at(const LinearArgs &a, int64_t n)
     return __half2float(static_cast<const __half *>(a.bias)[n]);
 }
 
-// Activation, residual and the store of elements n .. n+7 of row m, whose sums (bias included) are in f.
-template <class T, int ACT> __device__ __forceinline__ void finish8(const LinearArgs &a, int64_t m, int64_t n, float *f)
+// bias[n .. n+7], 0 beyond N
+template <class T> __device__ __forceinline__ void bias8(const LinearArgs &a, int64_t n, float *b)
 {
-    const bool whole = n + 8 <= a.N;
-    float res[8];
-    if (a.residual) {
-        const T *p = static_cast<const T *>(a.residual) + m * a.ldres + n;
-        if (whole && a.wide_res) {
-            Elem<T>::unpack(*reinterpret_cast<const uint4 *>(p), res);
+    if (a.bias && a.wide_bias && n + 8 <= a.N) {
+        if (a.bias_type == SPDY_F32) {
+            Elem<float>::unpack(reinterpret_cast<const uint4 *>(static_cast<const float *>(a.bias) + n)[0], b);
+            Elem<float>::unpack(reinterpret_cast<const uint4 *>(static_cast<const float *>(a.bias) + n)[1], b + 4);
         } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) res[i] = n + i < a.N ? Elem<T>::to_float(p[i]) : 0.f;
+            Elem<T>::unpack(*reinterpret_cast<const uint4 *>(static_cast<const T *>(a.bias) + n), b);
         }
+        return;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        f[i] = activate<ACT>(f[i]);
-        if (a.residual) f[i] += res[i];
+    for (int i = 0; i < 8; ++i) b[i] = a.bias && n + i < a.N ? bias_at(a, n + i) : 0.f;
+}
+
+// residual[m][n .. n+7] as they lie, 0 beyond the matrix
+template <class T> __device__ __forceinline__ uint4 residual8(const LinearArgs &a, int64_t m, int64_t n)
+{
+    if (!a.residual || m >= a.M || n >= a.N) return make_uint4(0, 0, 0, 0);
+    const T *p = static_cast<const T *>(a.residual) + m * a.ldres + n;
+    if (a.wide_res && n + 8 <= a.N) return *reinterpret_cast<const uint4 *>(p);
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = n + i < a.N ? Elem<T>::to_float(p[i]) : 0.f;
+    return Elem<T>::pack(f);
+}
+
+// Activation, residual and the store of elements n .. n+7 of row m, whose sums (bias included) are in f.
+template <class T, int ACT> __device__ __forceinline__ void finish8(const LinearArgs &a, int64_t m, int64_t n, float *f, uint4 residual)
+{
+    activate<ACT, 8>(f);
+    if (a.residual) {
+        float res[8];
+        Elem<T>::unpack(residual, res);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] += res[i];
     }
+    if (m >= a.M || n >= a.N) return;
+    const bool whole = n + 8 <= a.N && a.wide_out;
     if (a.out_type == SPDY_F32) {
         float *q = static_cast<float *>(a.y) + m * a.ldy + n;
-        if (whole && a.wide_out) {
+        if (whole) {
             reinterpret_cast<float4 *>(q)[0] = make_float4(f[0], f[1], f[2], f[3]);
             reinterpret_cast<float4 *>(q)[1] = make_float4(f[4], f[5], f[6], f[7]);
         } else {
@@ -140,7 +239,7 @@ template <class T, int ACT> __device__ __forceinline__ void finish8(const Linear
         return;
     }
     T *q = static_cast<T *>(a.y) + m * a.ldy + n;
-    if (whole && a.wide_out) {
+    if (whole) {
         *reinterpret_cast<uint4 *>(q) = Elem<T>::pack(f);
     } else {
 #pragma unroll
@@ -149,10 +248,60 @@ template <class T, int ACT> __device__ __forceinline__ void finish8(const Linear
     }
 }
 
+// One warp carries COLS columns of its 32 rows (from row m0) of an accumulator at `tmem` to y, 32 columns at a time.  A lane
+// reads a row of 32 columns out of TMEM; through shared memory (4 KB, swizzled) they are turned so that four lanes hold a
+// row of eight each, and y and residual are touched in whole sectors.  Bias and residual of the next 32 columns are
+// fetched before the present ones are worked on, those of the first before the accumulator is waited for (`ready`).
+// `release` is called once the last columns have left TMEM.
+template <class T, int ACT, int COLS, class Ready, class Release>
+__device__ __forceinline__ void carry(const LinearArgs &a, uint32_t tmem, int64_t m0, int64_t n0, float4 *mine, Ready ready, Release release)
+{
+    const int lane = threadIdx.x & 31, sub = (lane & 3) * 8;
+    float b[8];
+    uint4 res[4];
+    const auto fetch = [&](int c) {
+        bias8<T>(a, n0 + c + sub, b);
+        if (a.residual)
+#pragma unroll
+            for (int it = 0; it < 4; ++it) res[it] = residual8<T>(a, m0 + it * 8 + (lane >> 2), n0 + c + sub);
+    };
+    fetch(0);
+    if (!ready()) return;
+#pragma unroll 1
+    for (int c = 0; c < COLS; c += 32) {
+        uint32_t v[32];
+        tmem_load32(tmem + c, v);
+        if (c + 32 == COLS) release();
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            mine[lane * 8 + (i ^ (lane & 7))] =
+                make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+        __syncwarp();
+        float bias[8];
+        uint4 residual[4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bias[i] = b[i];
+#pragma unroll
+        for (int it = 0; it < 4; ++it) residual[it] = res[it];
+        if (c + 32 < COLS) fetch(c + 32);
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const int row = it * 8 + (lane >> 2);
+            const float4 lo = mine[row * 8 + ((2 * (lane & 3)) ^ (row & 7))], hi = mine[row * 8 + ((2 * (lane & 3) + 1) ^ (row & 7))];
+            float f[8] = {lo.x + bias[0], lo.y + bias[1], lo.z + bias[2], lo.w + bias[3], hi.x + bias[4], hi.y + bias[5], hi.z + bias[6], hi.w + bias[7]};
+            finish8<T, ACT>(a, m0 + row, n0 + c + sub, f, residual[it]);
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------------------------- tensor-core kernel
-template <int BN> struct Shape {
-    static constexpr int kStageBytes = (BM + BN) * BK * 2;
-    static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : 8;
+enum { kAlone = 0, kSplit = 1, kPair = 2 };
+
+template <int BN, int MODE> struct Shape {
+    static constexpr int kRowsB = MODE == kPair ? BN / 2 : BN;  // rows of w a block holds
+    static constexpr int kStageBytes = (BM + kRowsB) * BK * 2;
+    static constexpr int kStages = kStageBytes >= 32768 ? 6 : 8;
     static constexpr int kTmemColumns = 2 * BN;
     static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpilogueWarps * 4096 + 256;
 };
@@ -162,35 +311,41 @@ struct Control {
     uint32_t tmem;
 };
 
-// SPLIT false: persistent blocks walk over the tiles, two accumulators in TMEM so that a tile's epilogue runs beside the next
-// tile's products.  SPLIT true (few tiles): a cluster of blocks shares one tile, each multiplying a part of K; the parts
-// meet in the shared memory of the block that owns the columns, and are added there in the order of the blocks.
-template <class T, int BN, int ACT, bool SPLIT>
+// Two accumulators in TMEM, so that a tile's epilogue runs beside the next tile's products.
+//   kAlone: persistent blocks walk over tiles of 128 rows.
+//   kPair:  persistent pairs of blocks walk over tiles of 256 rows; each block brings its 128 rows of x and half of the tile's rows
+//           of w, the first block issues the products of both, each block's TMEM receives its own rows.
+//   kSplit (few tiles): a cluster of blocks shares one tile of 128 rows, each multiplying a part of K; the parts meet in the
+//           shared memory of the block that owns the columns, and are added there in the order of the blocks.
+template <class T, int BN, int ACT, int MODE>
 __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const LinearArgs a)
 {
-    using S = Shape<BN>;
+    using S = Shape<BN, MODE>;
     extern __shared__ unsigned char raw_smem[];
     unsigned char *stages = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~static_cast<uintptr_t>(1023));
     unsigned char *staging = stages + S::kStages * S::kStageBytes;
     __shared__ Control ctl;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     cg::cluster_group cluster = cg::this_cluster();
-    const int parts = SPLIT ? static_cast<int>(cluster.num_blocks()) : 1, part = SPLIT ? static_cast<int>(cluster.block_rank()) : 0;
+    const int parts = MODE == kAlone ? 1 : static_cast<int>(cluster.num_blocks()), part = MODE == kAlone ? 0 : static_cast<int>(cluster.block_rank());
     const int tiles = a.tiles_m * a.tiles_n;
-    const int first = SPLIT ? static_cast<int>(blockIdx.x) / parts : static_cast<int>(blockIdx.x), step = SPLIT ? tiles : static_cast<int>(gridDim.x);
-    const int kb0 = static_cast<int>(static_cast<int64_t>(a.k_blocks) * part / parts), kb1 = static_cast<int>(static_cast<int64_t>(a.k_blocks) * (part + 1) / parts);
+    const int first = static_cast<int>(blockIdx.x) / parts, step = MODE == kSplit ? tiles : static_cast<int>(gridDim.x) / parts;
+    const int kb0 = MODE == kSplit ? static_cast<int>(static_cast<int64_t>(a.k_blocks) * part / parts) : 0;
+    const int kb1 = MODE == kSplit ? static_cast<int>(static_cast<int64_t>(a.k_blocks) * (part + 1) / parts) : a.k_blocks;
+    constexpr int TILE_M = MODE == kPair ? 2 * BM : BM;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) barrier_init(&ctl.full[i], 1), barrier_init(&ctl.empty[i], 1);
-        for (int i = 0; i < 2; ++i) barrier_init(&ctl.acc_full[i], 1), barrier_init(&ctl.acc_empty[i], kEpilogueWarps);
+        for (int i = 0; i < 2; ++i) barrier_init(&ctl.acc_full[i], 1), barrier_init(&ctl.acc_empty[i], (MODE == kPair ? 2 : 1) * kEpilogueWarps);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_x)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_w)) : "memory");
     }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&ctl.tmem)), "r"(S::kTmemColumns) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+    __syncwarp();
+    if (warp == 1) tmem_alloc<MODE == kPair>(&ctl.tmem, S::kTmemColumns);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
+    if (MODE == kPair) cluster.sync();  // the peer signals this block's barriers
+    else __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = ctl.tmem;
 
@@ -201,28 +356,35 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
             bool ok = true;
             int issued = 0;
             for (int tile = first; tile < tiles && ok; tile += step) {
-                const int m0 = tile % a.tiles_m * BM, n0 = tile / a.tiles_m * BN;
+                const int m0 = tile % a.tiles_m * TILE_M + (MODE == kPair ? part * BM : 0), n0 = tile / a.tiles_m * BN + (MODE == kPair ? part * S::kRowsB : 0);
                 for (int kb = kb0; kb < kb1; ++kb) {
                     ok = barrier_wait(&ctl.empty[stage], parity ^ 1);
                     if (!ok) break;
                     unsigned char *to = stages + stage * S::kStageBytes;
-                    barrier_expect(&ctl.full[stage], S::kStageBytes);
-                    tma_load(to, &map_x, kb * BK, m0, &ctl.full[stage]);
-                    tma_load(to + BM * BK * 2, &map_w, kb * BK, n0, &ctl.full[stage]);
+                    if (MODE == kPair) {  // both blocks' copies count on the first block's barrier
+                        const uint32_t full = first_blocks(smem_addr(&ctl.full[stage]));
+                        if (part == 0) barrier_expect(&ctl.full[stage], 2 * S::kStageBytes);
+                        tma_load_pair(to, &map_x, kb * BK, m0, full);
+                        tma_load_pair(to + BM * BK * 2, &map_w, kb * BK, n0, full);
+                    } else {
+                        barrier_expect(&ctl.full[stage], S::kStageBytes);
+                        tma_load(to, &map_x, kb * BK, m0, &ctl.full[stage]);
+                        tma_load(to + BM * BK * 2, &map_w, kb * BK, n0, &ctl.full[stage]);
+                    }
                     ++issued;
                     if (++stage == S::kStages) stage = 0, parity ^= 1;
                 }
             }
-            if (!ok)  // copies in flight may not outlive the block
+            if (!ok && part == 0)  // copies in flight may not outlive the block (a peer's are counted on the same barriers)
                 for (int i = 0; i < S::kStages && i < issued; ++i) {
                     const int n = issued - 1 - i;
                     barrier_wait(&ctl.full[n % S::kStages], n / S::kStages & 1);
                 }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (lane == 0 && (MODE != kPair || part == 0)) {
             constexpr uint32_t format = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
-            constexpr uint32_t idesc = 1u << 4 | format << 7 | format << 10 | static_cast<uint32_t>(BN / 8) << 17 | static_cast<uint32_t>(BM / 16) << 24;
+            constexpr uint32_t idesc = 1u << 4 | format << 7 | format << 10 | static_cast<uint32_t>(BN / 8) << 17 | static_cast<uint32_t>(TILE_M / 16) << 24;
             int stage = 0, acc = 0;
             uint32_t parity = 0, acc_parity = 0;
             bool ok = true;
@@ -238,64 +400,50 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                     const uint32_t at = smem_addr(stages + stage * S::kStageBytes);
                     const uint64_t da = operand(at), db = operand(at + BM * BK * 2);
 #pragma unroll
-                    for (int k = 0; k < BK / 16; ++k) mma(d, da + 2 * k, db + 2 * k, idesc, kb > kb0 || k > 0);
-                    mma_commit(&ctl.empty[stage]);
+                    for (int k = 0; k < BK / 16; ++k) mma<MODE == kPair>(d, da + 2 * k, db + 2 * k, idesc, kb > kb0 || k > 0);
+                    mma_commit<MODE == kPair>(&ctl.empty[stage]);
                     if (++stage == S::kStages) stage = 0, parity ^= 1;
                 }
                 if (!ok) break;
-                mma_commit(&ctl.acc_full[acc]);
+                mma_commit<MODE == kPair>(&ctl.acc_full[acc]);
                 if (++acc == 2) acc = 0, acc_parity ^= 1;
             }
         }
-    } else if (!SPLIT) {
+    } else if (MODE != kSplit) {
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         float4 *mine = reinterpret_cast<float4 *>(staging + (warp - 2) * 4096);
         int acc = 0;
         uint32_t acc_parity = 0;
-        for (int tile = first; tile < tiles; tile += step) {
-            if (!barrier_wait(&ctl.acc_full[acc], acc_parity)) break;
-            __syncwarp();
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const int64_t m0 = static_cast<int64_t>(tile % a.tiles_m) * BM + quarter * 32, n0 = static_cast<int64_t>(tile / a.tiles_m) * BN + half * (BN / 2);
-#pragma unroll 1
-            for (int c = 0; c < BN / 2; c += 32) {
-                uint32_t v[32];
-                tmem_load32(tmem + acc * BN + half * (BN / 2) + c + (static_cast<uint32_t>(quarter * 32) << 16), v);
-                if (c + 32 == BN / 2) {  // the accumulator is free once its last columns are out
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) barrier_arrive(&ctl.acc_empty[acc]);
-                }
-                // a lane holds a row of 32 columns; turned so that four lanes hold a row of eight each, for whole sectors
+        bool ok = true;
+        for (int tile = first; tile < tiles && ok; tile += step) {
+            const int64_t m0 = static_cast<int64_t>(tile % a.tiles_m) * TILE_M + (MODE == kPair ? part * BM : 0) + quarter * 32;
+            const int64_t n0 = static_cast<int64_t>(tile / a.tiles_m) * BN + half * (BN / 2);
+            const auto ready = [&] {
+                ok = barrier_wait(&ctl.acc_full[acc], acc_parity);
+                ok = __all_sync(0xffffffffu, ok);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                return ok;
+            };
+            const auto release = [&] {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    mine[lane * 8 + (i ^ (lane & 7))] =
-                        make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
-                __syncwarp();
-                const int64_t n = n0 + c + (lane & 3) * 8;
-                float b[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) b[i] = a.bias && n + i < a.N ? bias_at(a, n + i) : 0.f;
-#pragma unroll
-                for (int it = 0; it < 4; ++it) {
-                    const int row = it * 8 + (lane >> 2);
-                    const float4 lo = mine[row * 8 + ((2 * (lane & 3)) ^ (row & 7))], hi = mine[row * 8 + ((2 * (lane & 3) + 1) ^ (row & 7))];
-                    float f[8] = {lo.x + b[0], lo.y + b[1], lo.z + b[2], lo.w + b[3], hi.x + b[4], hi.y + b[5], hi.z + b[6], hi.w + b[7]};
-                    if (m0 + row < a.M && n < a.N) finish8<T, ACT>(a, m0 + row, n, f);
+                if (lane == 0) {
+                    if (MODE == kPair) barrier_arrive_at(first_blocks(smem_addr(&ctl.acc_empty[acc])));
+                    else barrier_arrive(&ctl.acc_empty[acc]);
                 }
-            }
+            };
+            carry<T, ACT, BN / 2>(a, tmem + acc * BN + half * (BN / 2) + (static_cast<uint32_t>(quarter * 32) << 16), m0, n0, mine, ready, release);
             if (++acc == 2) acc = 0, acc_parity ^= 1;
         }
     }
     __syncwarp();
-    if (SPLIT) {
+    if (MODE == kSplit) {
         const int slice = BN / parts;  // columns this block finishes
         bool ok = true;
         if (warp >= 2) ok = barrier_wait(&ctl.acc_full[0], 0);
         __syncwarp();
         cluster.sync();  // every block's products are done: the stages may be overwritten
-        if (warp >= 2 && ok) {
+        if (warp >= 2 && __all_sync(0xffffffffu, ok)) {
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const int quarter = warp & 3, half = (warp - 2) >> 2;
 #pragma unroll 1
@@ -312,30 +460,39 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         }
-        cluster.sync();
         const int64_t m0 = static_cast<int64_t>(first % a.tiles_m) * BM, n0 = static_cast<int64_t>(first / a.tiles_m) * BN + part * slice;
         const float4 *sums = reinterpret_cast<const float4 *>(stages);
-        for (int i = threadIdx.x; i < BM * (slice / 8); i += kThreads) {
-            const int row = i / (slice / 8), g = i % (slice / 8);
-            const int64_t n = n0 + g * 8;
-            if (m0 + row >= a.M || n >= a.N) continue;
+        const int items = static_cast<int>(min(static_cast<int64_t>(BM), a.M - m0)) * (slice / 8);
+        // the first round's bias and residual come while the parts are exchanged
+        float b[8];
+        uint4 res = make_uint4(0, 0, 0, 0);
+        const auto place = [&](int i, int64_t &m, int64_t &n, int &row, int &g) { row = i / (slice / 8), g = i % (slice / 8), m = m0 + row, n = n0 + g * 8; };
+        int64_t m, n;
+        int row, g;
+        place(static_cast<int>(threadIdx.x), m, n, row, g);
+        if (static_cast<int>(threadIdx.x) < items) bias8<T>(a, n, b), res = residual8<T>(a, m, n);
+        cluster.sync();
+        for (int i = threadIdx.x; i < items; i += kThreads) {
+            if (i >= kThreads) {
+                place(i, m, n, row, g);
+                bias8<T>(a, n, b), res = residual8<T>(a, m, n);
+            }
             float f[8] = {};
             for (int p = 0; p < parts; ++p) {
                 const float4 lo = sums[(p * (slice / 4) + 2 * g) * BM + row], hi = sums[(p * (slice / 4) + 2 * g + 1) * BM + row];
                 f[0] += lo.x, f[1] += lo.y, f[2] += lo.z, f[3] += lo.w, f[4] += hi.x, f[5] += hi.y, f[6] += hi.z, f[7] += hi.w;
             }
-            if (a.bias)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (n + j < a.N) f[j] += bias_at(a, n + j);
-            finish8<T, ACT>(a, m0 + row, n, f);
+            for (int j = 0; j < 8; ++j) f[j] += b[j];
+            finish8<T, ACT>(a, m, n, f, res);
         }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
+    if (MODE == kPair) cluster.sync();  // no block leaves while its barriers are signalled or its operands read
+    else __syncthreads();
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmemColumns) : "memory");
+        tmem_free<MODE == kPair>(tmem, S::kTmemColumns);
     }
 }
 
@@ -399,7 +556,7 @@ template <class T, int ROWS, int COLS, int ACT, bool WIDE> __global__ void __lau
     const int64_t m = m0 + lane / COLS, n = n0 + lane % COLS;
     if (lane >= ROWS * COLS || m >= a.M || n >= a.N) return;
     if (a.bias) z += bias_at(a, n);
-    z = activate<ACT>(z);
+    activate<ACT, 1>(&z);
     if (a.residual) z += Elem<T>::to_float(static_cast<const T *>(a.residual)[m * a.ldres + n]);
     if (a.out_type == SPDY_F32) static_cast<float *>(a.y)[m * a.ldy + n] = z;
     else static_cast<T *>(a.y)[m * a.ldy + n] = Elem<T>::from_float(z);
@@ -453,34 +610,53 @@ bool on_tensor_cores(int64_t M, int64_t K) { return M > kFewRows && K > 0; }
 int64_t packed_ld(int64_t K) { return (K + 7) / 8 * 8; }
 size_t packed_bytes(int64_t rows, int64_t K) { return (static_cast<size_t>(rows) * static_cast<size_t>(packed_ld(K)) * 2 + 255) / 256 * 256; }
 
-template <class T, int BN, int ACT> int launch_tiles(const CUtensorMap &mx, const CUtensorMap &mw, const LinearArgs &a, int parts, cudaStream_t s)
+template <class T, int BN, int ACT, int MODE> int launch_tiles(const CUtensorMap &mx, const CUtensorMap &mw, const LinearArgs &a, int parts, cudaStream_t s)
 {
-    constexpr int smem = Shape<BN>::kSmem;
-    const int tiles = a.tiles_m * a.tiles_n;
+    constexpr int smem = Shape<BN, MODE>::kSmem;
+    const int tiles = a.tiles_m * a.tiles_n, units = sm_count() / parts;
+    auto *kernel = linear_kernel<T, BN, ACT, MODE>;
+    SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(static_cast<unsigned>((MODE == kSplit || tiles < units ? tiles : units) * parts));
     config.blockDim = dim3(kThreads);
     config.dynamicSmemBytes = smem;
     config.stream = s;
     cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(parts);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     config.attrs = attr;
-    if (parts > 1) {
-        if constexpr (BN <= 64) {
-            auto *kernel = linear_kernel<T, BN, ACT, true>;
-            SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-            attr[0].id = cudaLaunchAttributeClusterDimension;
-            attr[0].val.clusterDim.x = static_cast<unsigned>(parts);
-            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-            config.numAttrs = 1;
-            config.gridDim = dim3(static_cast<unsigned>(tiles * parts));
-            SPDY_EVAL_TRY(cudaLaunchKernelEx(&config, kernel, mx, mw, a));
-            return SPDY_OK;
-        }
-    }
-    auto *kernel = linear_kernel<T, BN, ACT, false>;
-    SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    config.gridDim = dim3(static_cast<unsigned>(tiles < sm_count() ? tiles : sm_count()));
+    config.numAttrs = parts > 1 ? 1 : 0;
     SPDY_EVAL_TRY(cudaLaunchKernelEx(&config, kernel, mx, mw, a));
     return SPDY_OK;
+}
+
+// Which tiles carry a product: the shape with the least estimated time, in cycles per multiprocessor.  A round of tiles costs its
+// slices of K (4096 multiply-adds a cycle; narrower tiles wait for L2: measured factors) and an epilogue that no product hides
+// (the last round's).
+struct TilePlan {
+    int mode, width, parts;
+};
+TilePlan choose_tiles(int64_t M, int64_t N, int64_t k_blocks, int sms)
+{
+    const auto div = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+    struct Option {
+        int mode, width, rows, units;
+        double per_slice, fixed;
+    };
+    const Option options[4] = {{kPair, 256, 256, sms / 2, 512, 4000}, {kPair, 128, 256, sms / 2, 290, 2800}, {kAlone, 128, 128, sms, 300, 2500}, {kAlone, 64, 128, sms, 200, 2000}};
+    TilePlan best = {kAlone, 64, 1};
+    double least = 1e300;
+    for (const Option &o : options) {
+        const double time = static_cast<double>(div(div(M, o.rows) * div(N, o.width), o.units)) * o.per_slice * static_cast<double>(k_blocks) + o.fixed;
+        if (time < least) least = time, best = {o.mode, o.width, o.mode == kPair ? 2 : 1};
+    }
+    // Tiles that leave most multiprocessors idle share their K among up to 8 of them.
+    const int64_t tiles = div(M, 128) * div(N, 64);
+    int parts = 1;
+    while (parts < 8 && tiles * parts * 2 <= sms && k_blocks >= parts * 4) parts *= 2;
+    if (parts > 1) best = {kSplit, 64, parts};
+    return best;
 }
 
 template <class T, int ACT> int launch_product(LinearArgs a, void *workspace, cudaStream_t s)
@@ -502,21 +678,18 @@ template <class T, int ACT> int launch_product(LinearArgs a, void *workspace, cu
         const int rc = finish_launch();
         if (rc != SPDY_OK) return rc;
     }
-    // Widest tile that still gives every multiprocessor one; below that, narrow tiles whose K is shared by a cluster.
-    const int64_t tm = (a.M + BM - 1) / BM;
-    const int sms = sm_count();
-    const int BN = tm * ((a.N + 255) / 256) >= sms ? 256 : tm * ((a.N + 127) / 128) >= sms ? 128 : 64;
-    a.tiles_m = static_cast<int>(tm), a.tiles_n = static_cast<int>((a.N + BN - 1) / BN), a.k_blocks = static_cast<int>((a.K + BK - 1) / BK);
-    if (tm * a.tiles_n > 0x7fffffff / 8) return SPDY_ERR_UNSUPPORTED;
-    int parts = 1;
-    while (BN == 64 && parts < 8 && a.tiles_m * a.tiles_n * parts * 2 <= sms && a.k_blocks >= parts * 4) parts *= 2;
+    a.k_blocks = static_cast<int>((a.K + BK - 1) / BK);
+    const TilePlan plan = choose_tiles(a.M, a.N, a.k_blocks, sm_count());
+    const int64_t rows = plan.mode == kPair ? 2 * BM : BM, tm = (a.M + rows - 1) / rows, tn = (a.N + plan.width - 1) / plan.width;
+    if (tm * tn > 0x7fffffff / 8) return SPDY_ERR_UNSUPPORTED;
+    a.tiles_m = static_cast<int>(tm), a.tiles_n = static_cast<int>(tn);
     CUtensorMap mx, mw;
     int rc = make_map(&mx, a.x, a.ldx, a.M, a.K, a.dtype, BM);
-    if (rc == SPDY_OK) rc = make_map(&mw, a.w, a.ldw, a.N, a.K, a.dtype, BN);
+    if (rc == SPDY_OK) rc = make_map(&mw, a.w, a.ldw, a.N, a.K, a.dtype, plan.mode == kPair ? plan.width / 2 : plan.width);
     if (rc != SPDY_OK) return rc;
-    if (BN == 256) return launch_tiles<T, 256, ACT>(mx, mw, a, parts, s);
-    if (BN == 128) return launch_tiles<T, 128, ACT>(mx, mw, a, parts, s);
-    return launch_tiles<T, 64, ACT>(mx, mw, a, parts, s);
+    if (plan.mode == kSplit) return launch_tiles<T, 64, ACT, kSplit>(mx, mw, a, plan.parts, s);
+    if (plan.mode == kPair) return plan.width == 256 ? launch_tiles<T, 256, ACT, kPair>(mx, mw, a, 2, s) : launch_tiles<T, 128, ACT, kPair>(mx, mw, a, 2, s);
+    return plan.width == 128 ? launch_tiles<T, 128, ACT, kAlone>(mx, mw, a, 1, s) : launch_tiles<T, 64, ACT, kAlone>(mx, mw, a, 1, s);
 }
 
 template <class T, int ROWS, int ACT> int launch_rows_of(const LinearArgs &a, cudaStream_t s)
@@ -584,6 +757,7 @@ int spdy_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, int dtyp
     a.dtype = dtype, a.bias_type = bias_dtype, a.out_type = out_dtype, a.activation = activation;
     a.wide_out = aligned(y, 16) && ldy * static_cast<int64_t>(type_size(out_dtype)) % 16 == 0;
     a.wide_res = residual && aligned(residual, 16) && ldres % 8 == 0;
+    a.wide_bias = aligned(bias, 16);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     return dtype == SPDY_BF16 ? launch_type<__nv_bfloat16>(a, workspace, s) : launch_type<__half>(a, workspace, s);
 }
