@@ -19,7 +19,7 @@ namespace cg = cooperative_groups;
 constexpr int BM = 128, BK = 64;           // rows of a tile; depth of a stage: 64 16-bit elements = one 128-byte swizzle row
 constexpr int kEpilogueWarps = 8;
 constexpr int kThreads = 32 * (2 + kEpilogueWarps);
-constexpr int64_t kFewRows = 8;            // at most this many rows take the multiply-add kernel
+constexpr int64_t kFewRows = 4;            // at most this many rows take the multiply-add kernel
 
 struct LinearArgs {
     const void *x, *w, *bias, *residual;
@@ -28,6 +28,7 @@ struct LinearArgs {
     int dtype, bias_type, out_type, activation;
     int tiles_m, tiles_n, k_blocks;
     int wide_out, wide_res, wide_bias;     // 16-byte accesses are possible on every row of y, of residual, on bias
+    int sectors;                           // every row of y and of the residual starts on 32 bytes
 };
 
 __device__ int g_timeouts;                 // waits that ran out of time (none in a working run); spdy_linear_check_status
@@ -214,16 +215,9 @@ template <class T> __device__ __forceinline__ uint4 residual8(const LinearArgs &
     return Elem<T>::pack(f);
 }
 
-// Activation, residual and the store of elements n .. n+7 of row m, whose sums (bias included) are in f.
-template <class T, int ACT> __device__ __forceinline__ void finish8(const LinearArgs &a, int64_t m, int64_t n, float *f, uint4 residual)
+// Stores elements n .. n+7 of row m.
+template <class T> __device__ __forceinline__ void store8(const LinearArgs &a, int64_t m, int64_t n, const float *f)
 {
-    activate<ACT, 8>(f);
-    if (a.residual) {
-        float res[8];
-        Elem<T>::unpack(residual, res);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] += res[i];
-    }
     if (m >= a.M || n >= a.N) return;
     const bool whole = n + 8 <= a.N && a.wide_out;
     if (a.out_type == SPDY_F32) {
@@ -248,49 +242,96 @@ template <class T, int ACT> __device__ __forceinline__ void finish8(const Linear
     }
 }
 
-// One warp carries COLS columns of its 32 rows (from row m0) of an accumulator at `tmem` to y, 32 columns at a time.  A lane
-// reads a row of 32 columns out of TMEM; through shared memory (4 KB, swizzled) they are turned so that four lanes hold a
-// row of eight each, and y and residual are touched in whole sectors.  Bias and residual of the next 32 columns are
-// fetched before the present ones are worked on, those of the first before the accumulator is waited for (`ready`).
-// `release` is called once the last columns have left TMEM.
-template <class T, int ACT, int COLS, class Ready, class Release>
-__device__ __forceinline__ void carry(const LinearArgs &a, uint32_t tmem, int64_t m0, int64_t n0, float4 *mine, Ready ready, Release release)
+// Activation and residual of eight sums, bias included.
+template <class T, int ACT> __device__ __forceinline__ void finish8(const LinearArgs &a, float *f, uint4 residual)
 {
-    const int lane = threadIdx.x & 31, sub = (lane & 3) * 8;
-    float b[8];
+    activate<ACT, 8>(f);
+    if (a.residual) {
+        float res[8];
+        Elem<T>::unpack(residual, res);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] += res[i];
+    }
+}
+
+__device__ __forceinline__ void load32(const void *p, uint4 &lo, uint4 &hi)
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(lo.x), "=r"(lo.y), "=r"(lo.z), "=r"(lo.w), "=r"(hi.x), "=r"(hi.y), "=r"(hi.z), "=r"(hi.w)
+                 : "l"(p)
+                 : "memory");
+}
+__device__ __forceinline__ void store32(void *p, uint4 lo, uint4 hi)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(lo.x), "r"(lo.y), "r"(lo.z), "r"(lo.w), "r"(hi.x), "r"(hi.y), "r"(hi.z), "r"(hi.w)
+                 : "memory");
+}
+
+// One warp carries COLS columns of its 32 rows (from row m0) of an accumulator at `tmem` to y, 32 columns at a time: a lane holds
+// a row, 32 columns of it, and touches y and residual in whole 32-byte sectors.  (Turning the rows through shared memory for
+// longer runs cost more than it gave: the tensor core's own reads take three quarters of the shared-memory bandwidth, and a
+// tile's epilogue took 8000 cycles, longer than its products at K = 768.)  `bias` is the warp's own COLS floats of shared memory.
+// The next 32 columns' residual is fetched before the present ones are worked on, the first before the accumulator is
+// waited for (`ready`); `release` is called once the last columns have left TMEM.
+template <class T, int ACT, int COLS, class Ready, class Release>
+__device__ __forceinline__ void carry(const LinearArgs &a, uint32_t tmem, int64_t m0, int64_t n0, float *bias, Ready ready, Release release)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t m = m0 + lane;
+    const T *res_row = a.residual ? static_cast<const T *>(a.residual) + m * a.ldres + n0 : nullptr;
+    // the fast way: all columns inside, every row 32-byte aligned
+    const bool fast = a.sectors && n0 + COLS <= a.N;
     uint4 res[4];
     const auto fetch = [&](int c) {
-        bias8<T>(a, n0 + c + sub, b);
-        if (a.residual)
+        if (!a.residual) return;
+        if (fast) {
+            if (m < a.M) load32(res_row + c, res[0], res[1]), load32(res_row + c + 16, res[2], res[3]);
+        } else {
 #pragma unroll
-            for (int it = 0; it < 4; ++it) res[it] = residual8<T>(a, m0 + it * 8 + (lane >> 2), n0 + c + sub);
+            for (int j = 0; j < 4; ++j) res[j] = residual8<T>(a, m, n0 + c + 8 * j);
+        }
     };
+    __syncwarp();
+    for (int i = lane; i < COLS; i += 32) bias[i] = a.bias && n0 + i < a.N ? bias_at(a, n0 + i) : 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) res[j] = make_uint4(0, 0, 0, 0);
     fetch(0);
+    __syncwarp();
     if (!ready()) return;
 #pragma unroll 1
     for (int c = 0; c < COLS; c += 32) {
         uint32_t v[32];
         tmem_load32(tmem + c, v);
         if (c + 32 == COLS) release();
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            mine[lane * 8 + (i ^ (lane & 7))] =
-                make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
-        __syncwarp();
-        float bias[8];
         uint4 residual[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bias[i] = b[i];
-#pragma unroll
-        for (int it = 0; it < 4; ++it) residual[it] = res[it];
+        for (int j = 0; j < 4; ++j) residual[j] = res[j];
         if (c + 32 < COLS) fetch(c + 32);
 #pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            const int row = it * 8 + (lane >> 2);
-            const float4 lo = mine[row * 8 + ((2 * (lane & 3)) ^ (row & 7))], hi = mine[row * 8 + ((2 * (lane & 3) + 1) ^ (row & 7))];
-            float f[8] = {lo.x + bias[0], lo.y + bias[1], lo.z + bias[2], lo.w + bias[3], hi.x + bias[4], hi.y + bias[5], hi.z + bias[6], hi.w + bias[7]};
-            finish8<T, ACT>(a, m0 + row, n0 + c + sub, f, residual[it]);
+        for (int j = 0; j < 4; j += 2) {
+            float f[16];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 b = reinterpret_cast<const float4 *>(bias + c)[2 * j + i];
+                f[4 * i] = __uint_as_float(v[8 * j + 4 * i]) + b.x, f[4 * i + 1] = __uint_as_float(v[8 * j + 4 * i + 1]) + b.y;
+                f[4 * i + 2] = __uint_as_float(v[8 * j + 4 * i + 2]) + b.z, f[4 * i + 3] = __uint_as_float(v[8 * j + 4 * i + 3]) + b.w;
+            }
+            finish8<T, ACT>(a, f, residual[j]);
+            finish8<T, ACT>(a, f + 8, residual[j + 1]);
+            const int64_t n = n0 + c + 8 * j;
+            if (fast) {
+                if (m >= a.M) continue;
+                if (a.out_type == SPDY_F32) {
+                    float *q = static_cast<float *>(a.y) + m * a.ldy + n;
+                    store32(q, Elem<float>::pack(f), Elem<float>::pack(f + 4));
+                    store32(q + 8, Elem<float>::pack(f + 8), Elem<float>::pack(f + 12));
+                } else {
+                    store32(static_cast<T *>(a.y) + m * a.ldy + n, Elem<T>::pack(f), Elem<T>::pack(f + 8));
+                }
+            } else {
+                store8<T>(a, m, n, f);
+                store8<T>(a, m, n + 8, f + 8);
+            }
         }
     }
 }
@@ -303,7 +344,9 @@ template <int BN, int MODE> struct Shape {
     static constexpr int kStageBytes = (BM + kRowsB) * BK * 2;
     static constexpr int kStages = kStageBytes >= 32768 ? 6 : 8;
     static constexpr int kTmemColumns = 2 * BN;
-    static constexpr int kSmem = 1024 + kStages * kStageBytes + kEpilogueWarps * 4096 + 256;
+    // behind the stages: the parts of a tile (kSplit), or the epilogue warps' bias
+    static constexpr int kExtra = MODE == kSplit ? BM * BN * 4 : kEpilogueWarps * (BN / 2) * 4;
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + kExtra;
 };
 
 struct Control {
@@ -323,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
     using S = Shape<BN, MODE>;
     extern __shared__ unsigned char raw_smem[];
     unsigned char *stages = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~static_cast<uintptr_t>(1023));
-    unsigned char *staging = stages + S::kStages * S::kStageBytes;
+    unsigned char *extra = stages + S::kStages * S::kStageBytes;
     __shared__ Control ctl;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     cg::cluster_group cluster = cg::this_cluster();
@@ -344,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
     __syncwarp();
     if (warp == 1) tmem_alloc<MODE == kPair>(&ctl.tmem, S::kTmemColumns);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    if (MODE == kPair) cluster.sync();  // the peer signals this block's barriers
+    if (MODE != kAlone) cluster.sync();  // other blocks signal this one's barriers or write its shared memory
     else __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = ctl.tmem;
@@ -411,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
         }
     } else if (MODE != kSplit) {
         const int quarter = warp & 3, half = (warp - 2) >> 2;
-        float4 *mine = reinterpret_cast<float4 *>(staging + (warp - 2) * 4096);
+        float *bias = reinterpret_cast<float *>(extra) + (warp - 2) * (BN / 2);
         int acc = 0;
         uint32_t acc_parity = 0;
         bool ok = true;
@@ -432,7 +475,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                     else barrier_arrive(&ctl.acc_empty[acc]);
                 }
             };
-            carry<T, ACT, BN / 2>(a, tmem + acc * BN + half * (BN / 2) + (static_cast<uint32_t>(quarter * 32) << 16), m0, n0, mine, ready, release);
+            carry<T, ACT, BN / 2>(a, tmem + acc * BN + half * (BN / 2) + (static_cast<uint32_t>(quarter * 32) << 16), m0, n0, bias, ready, release);
             if (++acc == 2) acc = 0, acc_parity ^= 1;
         }
     }
@@ -442,7 +485,6 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
         bool ok = true;
         if (warp >= 2) ok = barrier_wait(&ctl.acc_full[0], 0);
         __syncwarp();
-        cluster.sync();  // every block's products are done: the stages may be overwritten
         if (warp >= 2 && __all_sync(0xffffffffu, ok)) {
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const int quarter = warp & 3, half = (warp - 2) >> 2;
@@ -454,14 +496,14 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                 for (int i = 0; i < 8; ++i) {
                     const int col = c + 4 * i, owner = col / slice;
                     // [part][column group of 4][row] float4: consecutive lanes write consecutive 16 bytes
-                    float4 *to = cluster.map_shared_rank(reinterpret_cast<float4 *>(stages), owner) + (part * (slice / 4) + col % slice / 4) * BM + quarter * 32 + lane;
+                    float4 *to = cluster.map_shared_rank(reinterpret_cast<float4 *>(extra), owner) + (part * (slice / 4) + col % slice / 4) * BM + quarter * 32 + lane;
                     *to = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         }
         const int64_t m0 = static_cast<int64_t>(first % a.tiles_m) * BM, n0 = static_cast<int64_t>(first / a.tiles_m) * BN + part * slice;
-        const float4 *sums = reinterpret_cast<const float4 *>(stages);
+        const float4 *sums = reinterpret_cast<const float4 *>(extra);
         const int items = static_cast<int>(min(static_cast<int64_t>(BM), a.M - m0)) * (slice / 8);
         // the first round's bias and residual come while the parts are exchanged
         float b[8];
@@ -484,7 +526,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) f[j] += b[j];
-            finish8<T, ACT>(a, m, n, f, res);
+            finish8<T, ACT>(a, f, res);
+            store8<T>(a, m, n, f);
         }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -497,12 +540,13 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------------- few rows
-// One warp per COLS columns of y (rows of w) and ROWS rows of x: w is read once, x comes from L1.
+// A block of four warps per COLS columns of y (rows of w) and ROWS rows of x: w is read once, each warp a quarter of its K at a time,
+// x comes from L1; the warps' sums are added in their order.
 template <class T, int ROWS, int COLS, int ACT, bool WIDE> __global__ void __launch_bounds__(128) linear_rows_kernel(const LinearArgs a)
 {
-    const int lane = threadIdx.x & 31;
-    const int64_t n0 = (static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5)) * COLS, m0 = static_cast<int64_t>(blockIdx.y) * ROWS;
-    if (n0 >= a.N) return;
+    __shared__ float part[4][ROWS * COLS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * COLS, m0 = static_cast<int64_t>(blockIdx.y) * ROWS;
     float acc[ROWS][COLS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
@@ -511,30 +555,32 @@ template <class T, int ROWS, int COLS, int ACT, bool WIDE> __global__ void __lau
     const T *x = static_cast<const T *>(a.x) + m0 * a.ldx, *w = static_cast<const T *>(a.w) + n0 * a.ldw;
     if (WIDE) {
 #pragma unroll 2
-        for (int64_t k = lane * 8; k < a.K; k += 256) {
-            float wf[COLS][8];
+        for (int64_t k = threadIdx.x * 8; k < a.K; k += 1024) {
+            uint4 wr[COLS];
 #pragma unroll
-            for (int c = 0; c < COLS; ++c) Elem<T>::unpack(n0 + c < a.N ? load_stream(w + c * a.ldw + k) : make_uint4(0, 0, 0, 0), wf[c]);
+            for (int c = 0; c < COLS; ++c) wr[c] = n0 + c < a.N ? load_stream(w + c * a.ldw + k) : make_uint4(0, 0, 0, 0);
+            float xf[ROWS][8];
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                if (m0 + r >= a.M) break;
-                float xf[8];
-                Elem<T>::unpack(*reinterpret_cast<const uint4 *>(x + r * a.ldx + k), xf);
+            for (int r = 0; r < ROWS; ++r) Elem<T>::unpack(m0 + r < a.M ? *reinterpret_cast<const uint4 *>(x + r * a.ldx + k) : make_uint4(0, 0, 0, 0), xf[r]);
 #pragma unroll
-                for (int c = 0; c < COLS; ++c)
+            for (int c = 0; c < COLS; ++c) {
+                float wf[8];
+                Elem<T>::unpack(wr[c], wf);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[r][c] = fmaf(xf[i], wf[c][i], acc[r][c]);
+                for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[r][c] = fmaf(xf[r][i], wf[i], acc[r][c]);
             }
         }
     } else {
-        for (int64_t k = lane; k < a.K; k += 32) {
+#pragma unroll 4
+        for (int64_t k = threadIdx.x; k < a.K; k += 128) {
             float wf[COLS];
 #pragma unroll
             for (int c = 0; c < COLS; ++c) wf[c] = n0 + c < a.N ? Elem<T>::to_float(w[c * a.ldw + k]) : 0.f;
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
-                if (m0 + r >= a.M) break;
-                const float xf = Elem<T>::to_float(x[r * a.ldx + k]);
+                const float xf = m0 + r < a.M ? Elem<T>::to_float(x[r * a.ldx + k]) : 0.f;
 #pragma unroll
                 for (int c = 0; c < COLS; ++c) acc[r][c] = fmaf(xf, wf[c], acc[r][c]);
             }
@@ -543,18 +589,16 @@ template <class T, int ROWS, int COLS, int ACT, bool WIDE> __global__ void __lau
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-        for (int c = 0; c < COLS; ++c)
+        for (int c = 0; c < COLS; ++c) {
 #pragma unroll
             for (int d = 16; d; d >>= 1) acc[r][c] += __shfl_xor_sync(0xffffffffu, acc[r][c], d);
-    // lane r * COLS + c finishes element (r, c)
-    float z = 0.f;
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-        for (int c = 0; c < COLS; ++c)
-            if (lane == r * COLS + c) z = acc[r][c];
-    const int64_t m = m0 + lane / COLS, n = n0 + lane % COLS;
-    if (lane >= ROWS * COLS || m >= a.M || n >= a.N) return;
+            if (lane == 0) part[warp][r * COLS + c] = acc[r][c];
+        }
+    __syncthreads();
+    const int i = threadIdx.x;
+    const int64_t m = m0 + i / COLS, n = n0 + i % COLS;
+    if (i >= ROWS * COLS || m >= a.M || n >= a.N) return;
+    float z = (part[0][i] + part[1][i]) + (part[2][i] + part[3][i]);
     if (a.bias) z += bias_at(a, n);
     activate<ACT, 1>(&z);
     if (a.residual) z += Elem<T>::to_float(static_cast<const T *>(a.residual)[m * a.ldres + n]);
@@ -568,14 +612,19 @@ struct Repack {
     uint16_t *to[2];
     int64_t ld[2], rows[2], K, ldto;
 };
+// A thread copies eight elements of a row; those behind K are whatever (TMA never reads them).
 __global__ void __launch_bounds__(256) repack_kernel(const Repack p)
 {
     const int which = blockIdx.y;
     if (!p.to[which]) return;
-    for (int64_t r = blockIdx.x; r < p.rows[which]; r += gridDim.x) {
-        const uint16_t *from = p.from[which] + r * p.ld[which];
-        uint16_t *to = p.to[which] + r * p.ldto;
-        for (int64_t k = threadIdx.x; k < p.K; k += 256) to[k] = from[k];
+    const int64_t per_row = p.ldto / 8, total = p.rows[which] * per_row;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t r = i / per_row, k = (i - r * per_row) * 8;
+        const uint16_t *from = p.from[which] + r * p.ld[which] + k;
+        uint32_t e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = k + j < p.K ? from[j] : 0;
+        *reinterpret_cast<uint4 *>(p.to[which] + r * p.ldto + k) = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
     }
 }
 
@@ -631,13 +680,44 @@ template <class T, int BN, int ACT, int MODE> int launch_tiles(const CUtensorMap
     return SPDY_OK;
 }
 
+// How many clusters of `parts` blocks of the split kernel the device holds at once (a block takes a whole multiprocessor, and a
+// cluster lies within one group of them, so that fewer fit than the division says).  Asked once per device and size.
+template <class T, int ACT> int split_clusters(int parts)
+{
+    static int held[64][4];
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return 0;
+    const int at = parts == 2 ? 1 : parts == 4 ? 2 : 3;
+    int n = __atomic_load_n(&held[device][at], __ATOMIC_RELAXED);
+    if (n == 0) {
+        constexpr int smem = Shape<64, kSplit>::kSmem;
+        auto *kernel = linear_kernel<T, 64, ACT, kSplit>;
+        cudaLaunchConfig_t config = {};
+        config.gridDim = dim3(static_cast<unsigned>(parts * sm_count()));
+        config.blockDim = dim3(kThreads);
+        config.dynamicSmemBytes = smem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = static_cast<unsigned>(parts);
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        config.attrs = attr;
+        config.numAttrs = 1;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, kernel, &config) != cudaSuccess || n < 1) {
+            (void)cudaGetLastError();
+            n = 1;
+        }
+        __atomic_store_n(&held[device][at], n, __ATOMIC_RELAXED);
+    }
+    return n;
+}
+
 // Which tiles carry a product: the shape with the least estimated time, in cycles per multiprocessor.  A round of tiles costs its
 // slices of K (4096 multiply-adds a cycle; narrower tiles wait for L2: measured factors) and an epilogue that no product hides
 // (the last round's).
 struct TilePlan {
     int mode, width, parts;
 };
-TilePlan choose_tiles(int64_t M, int64_t N, int64_t k_blocks, int sms)
+template <class T, int ACT> TilePlan choose_tiles(int64_t M, int64_t N, int64_t k_blocks, int sms)
 {
     const auto div = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
     struct Option {
@@ -654,7 +734,7 @@ TilePlan choose_tiles(int64_t M, int64_t N, int64_t k_blocks, int sms)
     // Tiles that leave most multiprocessors idle share their K among up to 8 of them.
     const int64_t tiles = div(M, 128) * div(N, 64);
     int parts = 1;
-    while (parts < 8 && tiles * parts * 2 <= sms && k_blocks >= parts * 4) parts *= 2;
+    while (parts < 8 && tiles * parts * 2 <= sms && k_blocks >= parts * 4 && tiles <= split_clusters<T, ACT>(parts * 2)) parts *= 2;
     if (parts > 1) best = {kSplit, 64, parts};
     return best;
 }
@@ -673,13 +753,13 @@ template <class T, int ACT> int launch_product(LinearArgs a, void *workspace, cu
         a.w = ws, a.ldw = p.ldto;
     }
     if (p.to[0] || p.to[1]) {
-        const int64_t rows = p.rows[0] > p.rows[1] ? p.rows[0] : p.rows[1];
-        repack_kernel<<<dim3(static_cast<unsigned>(rows < 1184 ? rows : 1184), 2), 256, 0, s>>>(p);
+        const int64_t rows = p.rows[0] > p.rows[1] ? p.rows[0] : p.rows[1], blocks = (rows * (p.ldto / 8) + 255) / 256;
+        repack_kernel<<<dim3(static_cast<unsigned>(blocks < 2368 ? blocks : 2368), 2), 256, 0, s>>>(p);
         const int rc = finish_launch();
         if (rc != SPDY_OK) return rc;
     }
     a.k_blocks = static_cast<int>((a.K + BK - 1) / BK);
-    const TilePlan plan = choose_tiles(a.M, a.N, a.k_blocks, sm_count());
+    const TilePlan plan = choose_tiles<T, ACT>(a.M, a.N, a.k_blocks, sm_count());
     const int64_t rows = plan.mode == kPair ? 2 * BM : BM, tm = (a.M + rows - 1) / rows, tn = (a.N + plan.width - 1) / plan.width;
     if (tm * tn > 0x7fffffff / 8) return SPDY_ERR_UNSUPPORTED;
     a.tiles_m = static_cast<int>(tm), a.tiles_n = static_cast<int>(tn);
@@ -694,8 +774,8 @@ template <class T, int ACT> int launch_product(LinearArgs a, void *workspace, cu
 
 template <class T, int ROWS, int ACT> int launch_rows_of(const LinearArgs &a, cudaStream_t s)
 {
-    constexpr int COLS = ROWS == 1 ? 2 : 4;
-    const dim3 grid(static_cast<unsigned>((a.N + 4 * COLS - 1) / (4 * COLS)), static_cast<unsigned>((a.M + ROWS - 1) / ROWS));
+    constexpr int COLS = 4;
+    const dim3 grid(static_cast<unsigned>((a.N + COLS - 1) / COLS), static_cast<unsigned>((a.M + ROWS - 1) / ROWS));
     if (tma_ok(a.x, a.ldx) && tma_ok(a.w, a.ldw) && a.K % 8 == 0) linear_rows_kernel<T, ROWS, COLS, ACT, true><<<grid, 128, 0, s>>>(a);
     else linear_rows_kernel<T, ROWS, COLS, ACT, false><<<grid, 128, 0, s>>>(a);
     return finish_launch();
@@ -705,8 +785,8 @@ template <class T, int ACT> int launch_rows(const LinearArgs &a, cudaStream_t s)
 {
     if (a.M > 65535 * kFewRows) return SPDY_ERR_UNSUPPORTED;  // K = 0 only
     if (a.M == 1) return launch_rows_of<T, 1, ACT>(a, s);
-    if (a.M <= 4) return launch_rows_of<T, 4, ACT>(a, s);
-    return launch_rows_of<T, 8, ACT>(a, s);
+    if (a.M == 2) return launch_rows_of<T, 2, ACT>(a, s);
+    return launch_rows_of<T, 4, ACT>(a, s);
 }
 
 template <class T, int ACT> int launch(const LinearArgs &a, void *workspace, cudaStream_t s)
@@ -758,6 +838,7 @@ int spdy_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, int dtyp
     a.wide_out = aligned(y, 16) && ldy * static_cast<int64_t>(type_size(out_dtype)) % 16 == 0;
     a.wide_res = residual && aligned(residual, 16) && ldres % 8 == 0;
     a.wide_bias = aligned(bias, 16);
+    a.sectors = aligned(y, 32) && ldy * static_cast<int64_t>(type_size(out_dtype)) % 32 == 0 && (!residual || (aligned(residual, 32) && ldres % 16 == 0));
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     return dtype == SPDY_BF16 ? launch_type<__nv_bfloat16>(a, workspace, s) : launch_type<__half>(a, workspace, s);
 }

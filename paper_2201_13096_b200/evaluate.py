@@ -211,7 +211,7 @@ def linear(x, weight, bias=None, residual=None, activation: str = "none", out=No
             raise ValueError("the result must have x's type or be float32")
         px, pw = x.data_ptr(), weight.data_ptr()
         pws, need = None, 0
-        if (px | pw | ldx * 2 | ldw * 2) & 15 or M > 8:
+        if (px | pw | ldx * 2 | ldw * 2) & 15:
             need = lib.spdy_linear_workspace_bytes(px, ldx, pw, ldw, code, M, N, K)
             if need:
                 ws = x.new_empty(need, dtype=torch.uint8)
