@@ -1,7 +1,7 @@
 // y = act(x w^T + bias) + residual: kernels and C entry (spdy_eval.h).
 //
 // The product runs on the tensor cores (tcgen05, 16-bit operands, fp32 accumulators in TMEM); one thread feeds it with TMA
-// copies of 64-wide slices of x and w, one issues the matrix instructions, eight warps carry the finished tiles through the
+// copies of 64-wide slices of x and w, one issues the matrix instructions, sixteen warps carry the finished tiles through the
 // epilogue while the next tile is multiplied.  Large products pair two multiprocessors on a tile of 256 rows (cta_group::2), so
 // that each reads half of the tile's slice of w: with one multiprocessor per 128 x 256 tile the slices took about 15 TB/s out of
 // L2, which was the limit (8192^3: 1.29 PFLOP/s).  Few rows (single tokens) are a matter of reading w once: a kernel of plain
@@ -16,8 +16,9 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int BM = 128, BK = 64;           // rows of a tile; depth of a stage: 64 16-bit elements = one 128-byte swizzle row
-constexpr int kEpilogueWarps = 8;
+constexpr int BM = 128, BK = 64;           // rows of a block's tile; a slice of K: 64 16-bit elements = one 128-byte swizzle row
+constexpr int kSlices = 2;                 // slices of a stage: a round of barriers costs about 400 cycles, the products of one slice 128 to 512
+constexpr int kEpilogueWarps = 16;         // four to a scheduler: with two, a tile's epilogue took longer than its products at K = 768
 constexpr int kThreads = 32 * (2 + kEpilogueWarps);
 constexpr int64_t kFewRows = 4;            // at most this many rows take the multiply-add kernel
 
@@ -72,6 +73,15 @@ __device__ __forceinline__ void tma_load(void *to, const CUtensorMap *map, int x
 // Descriptor of a K-major operand whose rows are 128 bytes under the 128-byte swizzle: groups of 8 rows lie 1024 bytes apart.
 __device__ __forceinline__ uint64_t operand(uint32_t addr) { return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | 1ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61; }
 
+// One thread of a converged warp.  The loops below run on whole warps and elect the issuing thread around each TMA or tcgen05
+// instruction: these take their operands from uniform registers, and inside a branch on the lane number each operand cost a
+// trip there (690 cycles for four products of any size; 2.2 times less this way).
+__device__ __forceinline__ bool elect()
+{
+    uint32_t chosen;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(chosen));
+    return chosen != 0;
+}
 // The address of a shared variable in the first block of the cluster.
 __device__ __forceinline__ uint32_t first_blocks(uint32_t addr)
 {
@@ -121,17 +131,19 @@ template <bool PAIR> __device__ __forceinline__ void mma_commit(uint64_t *b)
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(b)), "h"(static_cast<uint16_t>(3)) : "memory");
     else asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(b)) : "memory");
 }
-__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t *v)
+// 16 columns of a warp's 32 rows, a row to a lane.
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float *v)
 {
+    uint32_t r[16];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, "
-        "%23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
         "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
-          "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]),
-          "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+          "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr)
         : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
 // ---------------------------------------------------------------------------------------------- epilogue
@@ -267,70 +279,63 @@ __device__ __forceinline__ void store32(void *p, uint4 lo, uint4 hi)
                  : "memory");
 }
 
-// One warp carries COLS columns of its 32 rows (from row m0) of an accumulator at `tmem` to y, 32 columns at a time: a lane holds
-// a row, 32 columns of it, and touches y and residual in whole 32-byte sectors.  (Turning the rows through shared memory for
-// longer runs cost more than it gave: the tensor core's own reads take three quarters of the shared-memory bandwidth, and a
-// tile's epilogue took 8000 cycles, longer than its products at K = 768.)  `bias` is the warp's own COLS floats of shared memory.
-// The next 32 columns' residual is fetched before the present ones are worked on, the first before the accumulator is
-// waited for (`ready`); `release` is called once the last columns have left TMEM.
-template <class T, int ACT, int COLS, class Ready, class Release>
+// One warp carries COLS columns of its 32 rows (from row m0) of an accumulator at `tmem` to y, 16 columns at a time: a lane holds
+// a row, 16 columns of it, and touches y and residual in whole 32-byte sectors.  (Turning the rows through shared memory for
+// longer runs cost more than it gave: the tensor core's operands and the copies that bring them take the shared memory's
+// bandwidth.)  `bias` is the warp's own COLS floats of shared memory.  The next 16 columns' residual is fetched before the
+// present ones are worked on, the first before the accumulator is waited for (`ready`); `release` is called once the last
+// columns have left TMEM.
+template <class T, int ACT, int COLS, bool RES, class Ready, class Release>
 __device__ __forceinline__ void carry(const LinearArgs &a, uint32_t tmem, int64_t m0, int64_t n0, float *bias, Ready ready, Release release)
 {
     const int lane = threadIdx.x & 31;
     const int64_t m = m0 + lane;
-    const T *res_row = a.residual ? static_cast<const T *>(a.residual) + m * a.ldres + n0 : nullptr;
     // the fast way: all columns inside, every row 32-byte aligned
-    const bool fast = a.sectors && n0 + COLS <= a.N;
-    uint4 res[4];
+    const bool inside = m < a.M, fast = a.sectors && n0 + COLS <= a.N;
+    const T *from = RES ? static_cast<const T *>(a.residual) + m * a.ldres + n0 : nullptr;
+    char *to = static_cast<char *>(a.y) + (m * a.ldy + n0) * (a.out_type == SPDY_F32 ? 4 : 2);
+    uint4 next[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
     const auto fetch = [&](int c) {
-        if (!a.residual) return;
+        if (!RES) return;
         if (fast) {
-            if (m < a.M) load32(res_row + c, res[0], res[1]), load32(res_row + c + 16, res[2], res[3]);
+            if (inside) load32(from + c, next[0], next[1]);
         } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) res[j] = residual8<T>(a, m, n0 + c + 8 * j);
+            next[0] = residual8<T>(a, m, n0 + c), next[1] = residual8<T>(a, m, n0 + c + 8);
         }
     };
     __syncwarp();
     for (int i = lane; i < COLS; i += 32) bias[i] = a.bias && n0 + i < a.N ? bias_at(a, n0 + i) : 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) res[j] = make_uint4(0, 0, 0, 0);
     fetch(0);
     __syncwarp();
     if (!ready()) return;
 #pragma unroll 1
-    for (int c = 0; c < COLS; c += 32) {
-        uint32_t v[32];
-        tmem_load32(tmem + c, v);
-        if (c + 32 == COLS) release();
-        uint4 residual[4];
+    for (int c = 0; c < COLS; c += 16) {
+        float f[16];
+        tmem_load16(tmem + c, f);
+        if (c + 16 == COLS) release();
+        const uint4 res[2] = {next[0], next[1]};
+        if (c + 16 < COLS) fetch(c + 16);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) residual[j] = res[j];
-        if (c + 32 < COLS) fetch(c + 32);
+        for (int i = 0; i < 4; ++i) {
+            const float4 b = reinterpret_cast<const float4 *>(bias + c)[i];
+            f[4 * i] += b.x, f[4 * i + 1] += b.y, f[4 * i + 2] += b.z, f[4 * i + 3] += b.w;
+        }
+        activate<ACT, 16>(f);
+        if (RES) {
+            float r[16];
+            Elem<T>::unpack(res[0], r), Elem<T>::unpack(res[1], r + 8);
 #pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-            float f[16];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float4 b = reinterpret_cast<const float4 *>(bias + c)[2 * j + i];
-                f[4 * i] = __uint_as_float(v[8 * j + 4 * i]) + b.x, f[4 * i + 1] = __uint_as_float(v[8 * j + 4 * i + 1]) + b.y;
-                f[4 * i + 2] = __uint_as_float(v[8 * j + 4 * i + 2]) + b.z, f[4 * i + 3] = __uint_as_float(v[8 * j + 4 * i + 3]) + b.w;
-            }
-            finish8<T, ACT>(a, f, residual[j]);
-            finish8<T, ACT>(a, f + 8, residual[j + 1]);
-            const int64_t n = n0 + c + 8 * j;
-            if (fast) {
-                if (m >= a.M) continue;
-                if (a.out_type == SPDY_F32) {
-                    float *q = static_cast<float *>(a.y) + m * a.ldy + n;
-                    store32(q, Elem<float>::pack(f), Elem<float>::pack(f + 4));
-                    store32(q + 8, Elem<float>::pack(f + 8), Elem<float>::pack(f + 12));
-                } else {
-                    store32(static_cast<T *>(a.y) + m * a.ldy + n, Elem<T>::pack(f), Elem<T>::pack(f + 8));
-                }
+            for (int i = 0; i < 16; ++i) f[i] += r[i];
+        }
+        if (!fast) {
+            store8<T>(a, m, n0 + c, f);
+            store8<T>(a, m, n0 + c + 8, f + 8);
+        } else if (inside) {
+            if (a.out_type == SPDY_F32) {
+                store32(to + 4 * c, Elem<float>::pack(f), Elem<float>::pack(f + 4));
+                store32(to + 4 * c + 32, Elem<float>::pack(f + 8), Elem<float>::pack(f + 12));
             } else {
-                store8<T>(a, m, n, f);
-                store8<T>(a, m, n + 8, f + 8);
+                store32(to + 2 * c, Elem<T>::pack(f), Elem<T>::pack(f + 8));
             }
         }
     }
@@ -341,11 +346,14 @@ enum { kAlone = 0, kSplit = 1, kPair = 2 };
 
 template <int BN, int MODE> struct Shape {
     static constexpr int kRowsB = MODE == kPair ? BN / 2 : BN;  // rows of w a block holds
-    static constexpr int kStageBytes = (BM + kRowsB) * BK * 2;
-    static constexpr int kStages = kStageBytes >= 32768 ? 6 : 8;
+    static constexpr int kSliceBytes = (BM + kRowsB) * BK * 2;  // x's rows, then w's
+    static constexpr int kStageBytes = kSlices * kSliceBytes;
+    static constexpr int kStages = 196608 / kStageBytes;
     static constexpr int kTmemColumns = 2 * BN;
     // behind the stages: the parts of a tile (kSplit), or the epilogue warps' bias
-    static constexpr int kExtra = MODE == kSplit ? BM * BN * 4 : kEpilogueWarps * (BN / 2) * 4;
+    static constexpr int kWarpColumns = BN / 4 < 32 ? 32 : BN / 4;  // of an epilogue warp; the warps beyond BN have none
+    static constexpr int kWorkers = 4 * (BN / kWarpColumns);
+    static constexpr int kExtra = MODE == kSplit ? BM * BN * 4 : kWorkers * kWarpColumns * 4;
     static constexpr int kSmem = 1024 + kStages * kStageBytes + kExtra;
 };
 
@@ -379,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kStages; ++i) barrier_init(&ctl.full[i], 1), barrier_init(&ctl.empty[i], 1);
-        for (int i = 0; i < 2; ++i) barrier_init(&ctl.acc_full[i], 1), barrier_init(&ctl.acc_empty[i], (MODE == kPair ? 2 : 1) * kEpilogueWarps);
+        for (int i = 0; i < 2; ++i) barrier_init(&ctl.acc_full[i], 1), barrier_init(&ctl.acc_empty[i], (MODE == kPair ? 2 : 1) * S::kWorkers);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_x)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_w)) : "memory");
@@ -393,77 +401,89 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
     const uint32_t tmem = ctl.tmem;
 
     if (warp == 0) {
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t parity = 0;
-            bool ok = true;
-            int issued = 0;
-            for (int tile = first; tile < tiles && ok; tile += step) {
-                const int m0 = tile % a.tiles_m * TILE_M + (MODE == kPair ? part * BM : 0), n0 = tile / a.tiles_m * BN + (MODE == kPair ? part * S::kRowsB : 0);
-                for (int kb = kb0; kb < kb1; ++kb) {
-                    ok = barrier_wait(&ctl.empty[stage], parity ^ 1);
-                    if (!ok) break;
-                    unsigned char *to = stages + stage * S::kStageBytes;
+        int stage = 0;
+        uint32_t parity = 0;
+        bool ok = true;
+        int issued = 0;
+        for (int tile = first; tile < tiles && ok; tile += step) {
+            const int m0 = tile % a.tiles_m * TILE_M + (MODE == kPair ? part * BM : 0), n0 = tile / a.tiles_m * BN + (MODE == kPair ? part * S::kRowsB : 0);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                ok = __all_sync(0xffffffffu, barrier_wait(&ctl.empty[stage], parity ^ 1));
+                if (!ok) break;
+                unsigned char *to = stages + stage * S::kStageBytes;
+                if (elect()) {
                     if (MODE == kPair) {  // both blocks' copies count on the first block's barrier
                         const uint32_t full = first_blocks(smem_addr(&ctl.full[stage]));
                         if (part == 0) barrier_expect(&ctl.full[stage], 2 * S::kStageBytes);
-                        tma_load_pair(to, &map_x, kb * BK, m0, full);
-                        tma_load_pair(to + BM * BK * 2, &map_w, kb * BK, n0, full);
+#pragma unroll
+                        for (int q = 0; q < kSlices; ++q) {
+                            tma_load_pair(to + q * S::kSliceBytes, &map_x, (kb * kSlices + q) * BK, m0, full);
+                            tma_load_pair(to + q * S::kSliceBytes + BM * BK * 2, &map_w, (kb * kSlices + q) * BK, n0, full);
+                        }
                     } else {
                         barrier_expect(&ctl.full[stage], S::kStageBytes);
-                        tma_load(to, &map_x, kb * BK, m0, &ctl.full[stage]);
-                        tma_load(to + BM * BK * 2, &map_w, kb * BK, n0, &ctl.full[stage]);
+#pragma unroll
+                        for (int q = 0; q < kSlices; ++q) {
+                            tma_load(to + q * S::kSliceBytes, &map_x, (kb * kSlices + q) * BK, m0, &ctl.full[stage]);
+                            tma_load(to + q * S::kSliceBytes + BM * BK * 2, &map_w, (kb * kSlices + q) * BK, n0, &ctl.full[stage]);
+                        }
                     }
-                    ++issued;
-                    if (++stage == S::kStages) stage = 0, parity ^= 1;
                 }
+                __syncwarp();
+                ++issued;
+                if (++stage == S::kStages) stage = 0, parity ^= 1;
             }
-            if (!ok && part == 0)  // copies in flight may not outlive the block (a peer's are counted on the same barriers)
-                for (int i = 0; i < S::kStages && i < issued; ++i) {
-                    const int n = issued - 1 - i;
-                    barrier_wait(&ctl.full[n % S::kStages], n / S::kStages & 1);
-                }
         }
+        if (!ok && part == 0)  // copies in flight may not outlive the block (a peer's are counted on the same barriers)
+            for (int i = 0; i < S::kStages && i < issued; ++i) {
+                const int n = issued - 1 - i;
+                barrier_wait(&ctl.full[n % S::kStages], n / S::kStages & 1);
+            }
     } else if (warp == 1) {
-        if (lane == 0 && (MODE != kPair || part == 0)) {
+        if (MODE != kPair || part == 0) {
             constexpr uint32_t format = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
             constexpr uint32_t idesc = 1u << 4 | format << 7 | format << 10 | static_cast<uint32_t>(BN / 8) << 17 | static_cast<uint32_t>(TILE_M / 16) << 24;
             int stage = 0, acc = 0;
             uint32_t parity = 0, acc_parity = 0;
             bool ok = true;
             for (int tile = first; tile < tiles && ok; tile += step) {
-                ok = barrier_wait(&ctl.acc_empty[acc], acc_parity ^ 1);
+                ok = __all_sync(0xffffffffu, barrier_wait(&ctl.acc_empty[acc], acc_parity ^ 1));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const uint32_t d = tmem + acc * BN;
                 for (int kb = kb0; kb < kb1; ++kb) {
-                    ok = barrier_wait(&ctl.full[stage], parity);
+                    ok = __all_sync(0xffffffffu, barrier_wait(&ctl.full[stage], parity));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t at = smem_addr(stages + stage * S::kStageBytes);
-                    const uint64_t da = operand(at), db = operand(at + BM * BK * 2);
+                    if (elect()) {
 #pragma unroll
-                    for (int k = 0; k < BK / 16; ++k) mma<MODE == kPair>(d, da + 2 * k, db + 2 * k, idesc, kb > kb0 || k > 0);
-                    mma_commit<MODE == kPair>(&ctl.empty[stage]);
+                        for (int q = 0; q < kSlices; ++q) {
+                            const uint64_t da = operand(at + q * S::kSliceBytes), db = operand(at + q * S::kSliceBytes + BM * BK * 2);
+#pragma unroll
+                            for (int k = 0; k < BK / 16; ++k) mma<MODE == kPair>(d, da + 2 * k, db + 2 * k, idesc, kb > kb0 || q > 0 || k > 0);
+                        }
+                        mma_commit<MODE == kPair>(&ctl.empty[stage]);
+                        if (kb + 1 == kb1) mma_commit<MODE == kPair>(&ctl.acc_full[acc]);
+                    }
+                    __syncwarp();
                     if (++stage == S::kStages) stage = 0, parity ^= 1;
                 }
-                if (!ok) break;
-                mma_commit<MODE == kPair>(&ctl.acc_full[acc]);
                 if (++acc == 2) acc = 0, acc_parity ^= 1;
             }
         }
     } else if (MODE != kSplit) {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
-        float *bias = reinterpret_cast<float *>(extra) + (warp - 2) * (BN / 2);
+        // warps 4 to 19: a warp reaches the quarter of TMEM's rows that its number names modulo four
+        const int quarter = warp & 3, group = (warp - 2) >> 2;
+        float *bias = reinterpret_cast<float *>(extra) + (warp - 2) * S::kWarpColumns;
         int acc = 0;
         uint32_t acc_parity = 0;
-        bool ok = true;
+        bool ok = group * S::kWarpColumns < BN;
         for (int tile = first; tile < tiles && ok; tile += step) {
             const int64_t m0 = static_cast<int64_t>(tile % a.tiles_m) * TILE_M + (MODE == kPair ? part * BM : 0) + quarter * 32;
-            const int64_t n0 = static_cast<int64_t>(tile / a.tiles_m) * BN + half * (BN / 2);
+            const int64_t n0 = static_cast<int64_t>(tile / a.tiles_m) * BN + group * S::kWarpColumns;
             const auto ready = [&] {
-                ok = barrier_wait(&ctl.acc_full[acc], acc_parity);
-                ok = __all_sync(0xffffffffu, ok);
+                ok = __all_sync(0xffffffffu, barrier_wait(&ctl.acc_full[acc], acc_parity));
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 return ok;
             };
@@ -475,33 +495,32 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                     else barrier_arrive(&ctl.acc_empty[acc]);
                 }
             };
-            carry<T, ACT, BN / 2>(a, tmem + acc * BN + half * (BN / 2) + (static_cast<uint32_t>(quarter * 32) << 16), m0, n0, bias, ready, release);
+            const uint32_t at = tmem + acc * BN + group * S::kWarpColumns + (static_cast<uint32_t>(quarter * 32) << 16);
+            if (a.residual) carry<T, ACT, S::kWarpColumns, true>(a, at, m0, n0, bias, ready, release);
+            else carry<T, ACT, S::kWarpColumns, false>(a, at, m0, n0, bias, ready, release);
             if (++acc == 2) acc = 0, acc_parity ^= 1;
         }
     }
     __syncwarp();
     if (MODE == kSplit) {
         const int slice = BN / parts;  // columns this block finishes
-        bool ok = true;
-        if (warp >= 2) ok = barrier_wait(&ctl.acc_full[0], 0);
-        __syncwarp();
-        if (warp >= 2 && __all_sync(0xffffffffu, ok)) {
+        const int quarter = warp & 3, group = (warp - 2) >> 2;
+        if (warp >= 2 && group * 16 < BN && __all_sync(0xffffffffu, barrier_wait(&ctl.acc_full[0], 0))) {
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const int quarter = warp & 3, half = (warp - 2) >> 2;
-#pragma unroll 1
-            for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += 32) {
-                uint32_t v[32];
-                tmem_load32(tmem + c + (static_cast<uint32_t>(quarter * 32) << 16), v);
+            for (int c = group * 16; c < BN; c += kEpilogueWarps / 4 * 16) {
+                float v[16];
+                tmem_load16(tmem + c + (static_cast<uint32_t>(quarter * 32) << 16), v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < 4; ++i) {
                     const int col = c + 4 * i, owner = col / slice;
                     // [part][column group of 4][row] float4: consecutive lanes write consecutive 16 bytes
                     float4 *to = cluster.map_shared_rank(reinterpret_cast<float4 *>(extra), owner) + (part * (slice / 4) + col % slice / 4) * BM + quarter * 32 + lane;
-                    *to = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+                    *to = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                 }
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         }
+        __syncwarp();
         const int64_t m0 = static_cast<int64_t>(first % a.tiles_m) * BM, n0 = static_cast<int64_t>(first / a.tiles_m) * BN + part * slice;
         const float4 *sums = reinterpret_cast<const float4 *>(extra);
         const int items = static_cast<int>(min(static_cast<int64_t>(BM), a.M - m0)) * (slice / 8);
@@ -712,7 +731,7 @@ template <class T, int ACT> int split_clusters(int parts)
 }
 
 // Which tiles carry a product: the shape with the least estimated time, in cycles per multiprocessor.  A round of tiles costs its
-// slices of K (4096 multiply-adds a cycle; narrower tiles wait for L2: measured factors) and an epilogue that no product hides
+// stages (4096 multiply-adds a cycle at best; a stage's barriers and copies have a floor near 500: measured) and an epilogue that no product hides
 // (the last round's).
 struct TilePlan {
     int mode, width, parts;
@@ -724,7 +743,7 @@ template <class T, int ACT> TilePlan choose_tiles(int64_t M, int64_t N, int64_t 
         int mode, width, rows, units;
         double per_slice, fixed;
     };
-    const Option options[4] = {{kPair, 256, 256, sms / 2, 512, 4000}, {kPair, 128, 256, sms / 2, 290, 2800}, {kAlone, 128, 128, sms, 300, 2500}, {kAlone, 64, 128, sms, 200, 2000}};
+    const Option options[4] = {{kPair, 256, 256, sms / 2, 1040, 4000}, {kPair, 128, 256, sms / 2, 600, 2800}, {kAlone, 128, 128, sms, 620, 2500}, {kAlone, 64, 128, sms, 540, 2000}};
     TilePlan best = {kAlone, 64, 1};
     double least = 1e300;
     for (const Option &o : options) {
@@ -734,7 +753,7 @@ template <class T, int ACT> TilePlan choose_tiles(int64_t M, int64_t N, int64_t 
     // Tiles that leave most multiprocessors idle share their K among up to 8 of them.
     const int64_t tiles = div(M, 128) * div(N, 64);
     int parts = 1;
-    while (parts < 8 && tiles * parts * 2 <= sms && k_blocks >= parts * 4 && tiles <= split_clusters<T, ACT>(parts * 2)) parts *= 2;
+    while (parts < 8 && tiles * parts * 2 <= sms && k_blocks >= parts * 2 && tiles <= split_clusters<T, ACT>(parts * 2)) parts *= 2;
     if (parts > 1) best = {kSplit, 64, parts};
     return best;
 }
@@ -758,7 +777,7 @@ template <class T, int ACT> int launch_product(LinearArgs a, void *workspace, cu
         const int rc = finish_launch();
         if (rc != SPDY_OK) return rc;
     }
-    a.k_blocks = static_cast<int>((a.K + BK - 1) / BK);
+    a.k_blocks = static_cast<int>((a.K + BK * kSlices - 1) / (BK * kSlices));
     const TilePlan plan = choose_tiles<T, ACT>(a.M, a.N, a.k_blocks, sm_count());
     const int64_t rows = plan.mode == kPair ? 2 * BM : BM, tm = (a.M + rows - 1) / rows, tn = (a.N + plan.width - 1) / plan.width;
     if (tm * tn > 0x7fffffff / 8) return SPDY_ERR_UNSUPPORTED;
