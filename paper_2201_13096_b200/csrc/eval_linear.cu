@@ -29,7 +29,7 @@ struct LinearArgs {
     int dtype, bias_type, out_type, activation;
     int tiles_m, tiles_n, k_blocks;
     int wide_out, wide_res, wide_bias;     // 16-byte accesses are possible on every row of y, of residual, on bias
-    int sectors;                           // every row of y and of the residual starts on 32 bytes
+    int sectors, words;                    // every row of y and of the residual starts on 32 bytes; 16-bit rows of y start on 4
 };
 
 __device__ int g_timeouts;                 // waits that ran out of time (none in a working run); spdy_linear_check_status
@@ -279,25 +279,70 @@ __device__ __forceinline__ void store32(void *p, uint4 lo, uint4 hi)
                  : "memory");
 }
 
+// 16 columns (from n) of 32 rows (from m), a row to a lane, stored by runs of columns; 1 KB of shared memory of the warp's own.
+// The values come by value: an address would put them into local memory on the fast way too.
+__device__ __noinline__ void turn_wide(const LinearArgs &a, int64_t m, int64_t n, uint4 v0, uint4 v1, uint4 v2, uint4 v3, unsigned char *turn)
+{
+    const int lane = threadIdx.x & 31;
+    uint4 *mine = reinterpret_cast<uint4 *>(turn);
+    for (int half = 0; half < 2; ++half) {
+        __syncwarp();
+        mine[2 * lane] = half ? v2 : v0;
+        mine[2 * lane + 1] = half ? v3 : v1;
+        __syncwarp();
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const int64_t row = m + it * 4 + lane / 8, col = n + half * 8 + lane % 8;
+            if (row < a.M && col < a.N) static_cast<float *>(a.y)[row * a.ldy + col] = reinterpret_cast<const float *>(turn)[it * 32 + lane];
+        }
+    }
+}
+__device__ __noinline__ void turn_narrow(const LinearArgs &a, int64_t m, int64_t n, uint4 v0, uint4 v1, unsigned char *turn)
+{
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+    reinterpret_cast<uint4 *>(turn)[2 * lane] = v0;
+    reinterpret_cast<uint4 *>(turn)[2 * lane + 1] = v1;
+    __syncwarp();
+    uint16_t *y = static_cast<uint16_t *>(a.y);
+    if (a.words && n + 16 <= a.N) {  // two columns to a lane
+        uint32_t v[8];
+#pragma unroll
+        for (int it = 0; it < 8; ++it) v[it] = reinterpret_cast<const uint32_t *>(turn)[it * 32 + lane];
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+            const int64_t row = m + it * 4 + lane / 8;
+            if (row < a.M) *reinterpret_cast<uint32_t *>(y + row * a.ldy + n + lane % 8 * 2) = v[it];
+        }
+        return;
+    }
+#pragma unroll
+    for (int it = 0; it < 16; ++it) {
+        const int64_t row = m + it * 2 + lane / 16, col = n + lane % 16;
+        if (row < a.M && col < a.N) y[row * a.ldy + col] = reinterpret_cast<const uint16_t *>(turn)[it * 32 + lane];
+    }
+}
+
 // One warp carries COLS columns of its 32 rows (from row m0) of an accumulator at `tmem` to y, 16 columns at a time: a lane holds
 // a row, 16 columns of it, and touches y and residual in whole 32-byte sectors.  (Turning the rows through shared memory for
 // longer runs cost more than it gave: the tensor core's operands and the copies that bring them take the shared memory's
 // bandwidth.)  `bias` is the warp's own COLS floats of shared memory.  The next 16 columns' residual is fetched before the
 // present ones are worked on, the first before the accumulator is waited for (`ready`); `release` is called once the last
-// columns have left TMEM.
-template <class T, int ACT, int COLS, bool RES, class Ready, class Release>
-__device__ __forceinline__ void carry(const LinearArgs &a, uint32_t tmem, int64_t m0, int64_t n0, float *bias, Ready ready, Release release)
+// columns have left TMEM.  Rows that start anywhere go through 1 KB of shared memory (`turn`), so that a store covers runs of
+// columns rather than single elements of 32 rows.
+// FAST: all columns lie inside and every row starts on 32 bytes.
+template <class T, int ACT, int COLS, bool RES, bool FAST, class Ready, class Release>
+__device__ __forceinline__ void carry(const LinearArgs &a, uint32_t tmem, int64_t m0, int64_t n0, float *bias, unsigned char *turn, Ready ready, Release release)
 {
     const int lane = threadIdx.x & 31;
     const int64_t m = m0 + lane;
-    // the fast way: all columns inside, every row 32-byte aligned
-    const bool inside = m < a.M, fast = a.sectors && n0 + COLS <= a.N;
+    const bool inside = m < a.M;
     const T *from = RES ? static_cast<const T *>(a.residual) + m * a.ldres + n0 : nullptr;
     char *to = static_cast<char *>(a.y) + (m * a.ldy + n0) * (a.out_type == SPDY_F32 ? 4 : 2);
     uint4 next[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
     const auto fetch = [&](int c) {
         if (!RES) return;
-        if (fast) {
+        if (FAST) {
             if (inside) load32(from + c, next[0], next[1]);
         } else {
             next[0] = residual8<T>(a, m, n0 + c), next[1] = residual8<T>(a, m, n0 + c + 8);
@@ -327,9 +372,9 @@ __device__ __forceinline__ void carry(const LinearArgs &a, uint32_t tmem, int64_
 #pragma unroll
             for (int i = 0; i < 16; ++i) f[i] += r[i];
         }
-        if (!fast) {
-            store8<T>(a, m, n0 + c, f);
-            store8<T>(a, m, n0 + c + 8, f + 8);
+        if (!FAST) {
+            if (a.out_type == SPDY_F32) turn_wide(a, m0, n0 + c, Elem<float>::pack(f), Elem<float>::pack(f + 4), Elem<float>::pack(f + 8), Elem<float>::pack(f + 12), turn);
+            else turn_narrow(a, m0, n0 + c, Elem<T>::pack(f), Elem<T>::pack(f + 8), turn);
         } else if (inside) {
             if (a.out_type == SPDY_F32) {
                 store32(to + 4 * c, Elem<float>::pack(f), Elem<float>::pack(f + 4));
@@ -350,10 +395,10 @@ template <int BN, int MODE> struct Shape {
     static constexpr int kStageBytes = kSlices * kSliceBytes;
     static constexpr int kStages = 196608 / kStageBytes;
     static constexpr int kTmemColumns = 2 * BN;
-    // behind the stages: the parts of a tile (kSplit), or the epilogue warps' bias
+    // behind the stages: the parts of a tile (kSplit), or the epilogue warps' bias and room to turn rows
     static constexpr int kWarpColumns = BN / 4 < 32 ? 32 : BN / 4;  // of an epilogue warp; the warps beyond BN have none
     static constexpr int kWorkers = 4 * (BN / kWarpColumns);
-    static constexpr int kExtra = MODE == kSplit ? BM * BN * 4 : kWorkers * kWarpColumns * 4;
+    static constexpr int kExtra = MODE == kSplit ? BM * BN * 4 : kWorkers * (kWarpColumns * 4 + 1024);
     static constexpr int kSmem = 1024 + kStages * kStageBytes + kExtra;
 };
 
@@ -475,7 +520,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
     } else if (MODE != kSplit) {
         // warps 4 to 19: a warp reaches the quarter of TMEM's rows that its number names modulo four
         const int quarter = warp & 3, group = (warp - 2) >> 2;
-        float *bias = reinterpret_cast<float *>(extra) + (warp - 2) * S::kWarpColumns;
+        unsigned char *turn = extra + (warp - 2) * 1024;
+        float *bias = reinterpret_cast<float *>(extra + S::kWorkers * 1024) + (warp - 2) * S::kWarpColumns;
         int acc = 0;
         uint32_t acc_parity = 0;
         bool ok = group * S::kWarpColumns < BN;
@@ -496,8 +542,13 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                 }
             };
             const uint32_t at = tmem + acc * BN + group * S::kWarpColumns + (static_cast<uint32_t>(quarter * 32) << 16);
-            if (a.residual) carry<T, ACT, S::kWarpColumns, true>(a, at, m0, n0, bias, ready, release);
-            else carry<T, ACT, S::kWarpColumns, false>(a, at, m0, n0, bias, ready, release);
+            if (a.sectors && n0 + S::kWarpColumns <= a.N) {
+                if (a.residual) carry<T, ACT, S::kWarpColumns, true, true>(a, at, m0, n0, bias, turn, ready, release);
+                else carry<T, ACT, S::kWarpColumns, false, true>(a, at, m0, n0, bias, turn, ready, release);
+            } else {
+                if (a.residual) carry<T, ACT, S::kWarpColumns, true, false>(a, at, m0, n0, bias, turn, ready, release);
+                else carry<T, ACT, S::kWarpColumns, false, false>(a, at, m0, n0, bias, turn, ready, release);
+            }
             if (++acc == 2) acc = 0, acc_parity ^= 1;
         }
     }
@@ -743,7 +794,7 @@ template <class T, int ACT> TilePlan choose_tiles(int64_t M, int64_t N, int64_t 
         int mode, width, rows, units;
         double per_slice, fixed;
     };
-    const Option options[4] = {{kPair, 256, 256, sms / 2, 1040, 4000}, {kPair, 128, 256, sms / 2, 600, 2800}, {kAlone, 128, 128, sms, 620, 2500}, {kAlone, 64, 128, sms, 540, 2000}};
+    const Option options[3] = {{kPair, 256, 256, sms / 2, 1040, 4000}, {kAlone, 128, 128, sms, 620, 2500}, {kAlone, 64, 128, sms, 540, 2000}};
     TilePlan best = {kAlone, 64, 1};
     double least = 1e300;
     for (const Option &o : options) {
@@ -787,7 +838,7 @@ template <class T, int ACT> int launch_product(LinearArgs a, void *workspace, cu
     if (rc == SPDY_OK) rc = make_map(&mw, a.w, a.ldw, a.N, a.K, a.dtype, plan.mode == kPair ? plan.width / 2 : plan.width);
     if (rc != SPDY_OK) return rc;
     if (plan.mode == kSplit) return launch_tiles<T, 64, ACT, kSplit>(mx, mw, a, plan.parts, s);
-    if (plan.mode == kPair) return plan.width == 256 ? launch_tiles<T, 256, ACT, kPair>(mx, mw, a, 2, s) : launch_tiles<T, 128, ACT, kPair>(mx, mw, a, 2, s);
+    if (plan.mode == kPair) return launch_tiles<T, 256, ACT, kPair>(mx, mw, a, 2, s);
     return plan.width == 128 ? launch_tiles<T, 128, ACT, kAlone>(mx, mw, a, 1, s) : launch_tiles<T, 64, ACT, kAlone>(mx, mw, a, 1, s);
 }
 
@@ -857,6 +908,7 @@ int spdy_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, int dtyp
     a.wide_out = aligned(y, 16) && ldy * static_cast<int64_t>(type_size(out_dtype)) % 16 == 0;
     a.wide_res = residual && aligned(residual, 16) && ldres % 8 == 0;
     a.wide_bias = aligned(bias, 16);
+    a.words = aligned(y, 4) && ldy % 2 == 0;
     a.sectors = aligned(y, 32) && ldy * static_cast<int64_t>(type_size(out_dtype)) % 32 == 0 && (!residual || (aligned(residual, 32) && ldres % 16 == 0));
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     return dtype == SPDY_BF16 ? launch_type<__nv_bfloat16>(a, workspace, s) : launch_type<__half>(a, workspace, s);

@@ -4,7 +4,8 @@
 // Mathematics.  Everything is kept in base 2: with c = log2(e) / T and the running maximum m of the logits, d_v = (x_v - m) c
 // and s = sum 2^d, a probability is 2^d_v / s.  The entropy needs t = sum 2^d d beside s: H = ln 2 (log2 s - t / s).  When the
 // maximum rises by delta / c, s becomes s 2^-delta and t becomes (t - s delta) 2^-delta.
-// m need not be the maximum: any logit that is at most 2^64 below it does (see raise), so that the sums are rescaled rarely.
+// m need not be the maximum: any logit within a factor of 4 of it does (see raise), so that the sums are rescaled
+// rarely and nothing large cancels in the end.
 // An element costs one fused multiply-add x c - b with b = m c rounded; the rounding r = m c - b is the same for all elements and
 // is taken back once per thread (2^-r s, and t - r s for t).  Where m c is so large that x c could overflow (rows of the type's
 // lowest value) m is subtracted first instead.  Beside that one instruction to unpack, one for the special-function unit
@@ -118,7 +119,7 @@ struct Reference {
     }
 };
 
-// What a thread has added up, relative to Reference(m, c): m is some logit, no other is more than 64 / c above it.
+// What a thread has added up, relative to Reference(m, c): m is some logit, no other is more than 2 / c above it.
 struct Running {
     float m, s, t;
 };
@@ -126,7 +127,7 @@ struct Running {
 // Makes `top` the logit the sums are relative to, if it is far above the present one (or the first).
 template <bool ENT> __device__ __forceinline__ void raise(Running &st, float top, float c)
 {
-    if (top > st.m && (top - st.m) * c > 64.f) {
+    if (top > st.m && (top - st.m) * c > 2.f) {
         if (st.s != 0.f) {
             const Reference old(st.m, c), now(top, c);
             const float d = max_nan(old.far || now.far ? (st.m - top) * c : old.base - now.base, -1000.f), f = ex2(d);

@@ -87,18 +87,33 @@ def library():
 # PyTorch, imported with the library (the package itself imports without it).
 torch = None
 _TYPES = {}
-_current_stream = _current_device = None
+_current_stream = _current_device = _empty_strided = None
 
 
 def _import_torch():
-    global torch, _current_stream, _current_device
+    global torch, _current_stream, _current_device, _empty_strided
     import torch as t
 
     _TYPES.update({t.float32: 0, t.bfloat16: 1, t.float16: 2})
     # the handle of the current stream as a number, without an object around it (small calls are bound by the host)
     _current_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda i: t.cuda.current_stream(i).cuda_stream)
     _current_device = getattr(t._C, "_cuda_getDevice", None) or t.cuda.current_device
+    # uninitialised memory on the current device by (shape, strides, type), again without the general call's argument parsing
+    try:
+        _empty_strided = t._C._dynamo.guards._empty_strided_cuda
+    except AttributeError:
+        _empty_strided = lambda shape, strides, dtype: t.empty_strided(shape, strides, dtype=dtype, device="cuda")  # noqa: E731
     torch = t
+
+
+def _matrix(rows: int, cols: int, dtype):
+    return _empty_strided((rows, cols), (cols, 1), dtype)
+
+
+def _vectors(count: int, n: int):
+    """``count`` float32 vectors of ``n``."""
+    f32 = torch.float32
+    return [_empty_strided((n,), (1,), f32) for _ in range(count)]
 
 
 def _dtype(t, what: str) -> int:
@@ -200,7 +215,7 @@ def linear(x, weight, bias=None, residual=None, activation: str = "none", out=No
         pr, ldres = residual.data_ptr(), _like(residual, "residual", M, N, dtype, dev)
     with _Scope(dev, stream) as handle:
         if out is None:
-            out = x.new_empty((M, N)) if out_dtype is None else x.new_empty((M, N), dtype=out_dtype)
+            out = _matrix(M, N, dtype if out_dtype is None else out_dtype)
             ldy = N
         else:
             if out_dtype is not None and out.dtype != out_dtype:
@@ -214,7 +229,7 @@ def linear(x, weight, bias=None, residual=None, activation: str = "none", out=No
         if (px | pw | ldx * 2 | ldw * 2) & 15:
             need = lib.spdy_linear_workspace_bytes(px, ldx, pw, ldw, code, M, N, K)
             if need:
-                ws = x.new_empty(need, dtype=torch.uint8)
+                ws = _empty_strided((need,), (1,), torch.uint8)
                 pws = ws.data_ptr()
         rc = lib.spdy_linear(px, ldx, pw, ldw, code, pb, bcode, pr, ldres, act, M, N, K, out.data_ptr(), ldy, ocode, pws, need, handle)
     if rc:
@@ -249,16 +264,15 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=No
     kind = _norm_params(x, weight, bias, D, dev, code)
     with _Scope(dev, stream) as handle:
         if out is None:
-            out, ldy = x.new_empty((R, D)), D
+            out, ldy = _matrix(R, D, x.dtype), D
         else:
             ldy = _like(out, "out", R, D, x.dtype, dev)
-        stats = x.new_empty((2, R), dtype=torch.float32)
-        p = stats.data_ptr()
-        rc = lib.spdy_layer_norm(x.data_ptr(), ldx, code, _ptr(weight), _ptr(bias), kind, R, D, eps, out.data_ptr(), ldy, p, p + 4 * R,
-                                 handle)
+        mean, rstd = _vectors(2, R)
+        rc = lib.spdy_layer_norm(x.data_ptr(), ldx, code, _ptr(weight), _ptr(bias), kind, R, D, eps, out.data_ptr(), ldy,
+                                 mean.data_ptr(), rstd.data_ptr(), handle)
     if rc:
         binding._check(rc, "spdy_layer_norm")
-    return (out, *stats.unbind(0))
+    return out, mean, rstd
 
 
 def layer_norm_backward(dy, x, weight, mean, rstd, out=None, params: bool = True, stream=None):
@@ -273,19 +287,17 @@ def layer_norm_backward(dy, x, weight, mean, rstd, out=None, params: bool = True
     pm, pr = _vector(mean, "mean", R, dev, torch.float32), _vector(rstd, "rstd", R, dev, torch.float32)
     with _Scope(dev, stream) as handle:
         if out is None:
-            out, lddx = x.new_empty((R, D)), D
+            out, lddx = _matrix(R, D, x.dtype), D
         else:
             lddx = _like(out, "out", R, D, x.dtype, dev)
         dw = db = pw = pb = pws = None
         need = 0
         if params:
-            grads = x.new_empty((2, D), dtype=torch.float32)
-            dw, db = grads.unbind(0)
-            pw = grads.data_ptr()
-            pb = pw + 4 * D
+            dw, db = _vectors(2, D)
+            pw, pb = dw.data_ptr(), db.data_ptr()
             need = lib.spdy_layer_norm_backward_workspace_bytes(R, D, code)
             if need:
-                ws = x.new_empty(need, dtype=torch.uint8)
+                ws = _empty_strided((need,), (1,), torch.uint8)
                 pws = ws.data_ptr()
         rc = lib.spdy_layer_norm_backward(dy.data_ptr(), lddy, x.data_ptr(), ldx, code, _ptr(weight), kind, pm, pr, R, D, out.data_ptr(),
                                           lddx, pw, pb, pws, need, handle)
@@ -302,7 +314,7 @@ def _logits(logits):
 
 def _grads_out(out, logits, R, V, dev):
     if out is None:
-        return logits.new_empty((R, V)), V
+        return _matrix(R, V, logits.dtype), V
     return out, _like(out, "out", R, V, logits.dtype, dev)
 
 
@@ -319,17 +331,16 @@ def token_logprobs(logits, tokens, top_k: int = 0, temperature: float = 1.0, str
     bits = _ids(tokens, "tokens", (R,), dev)
     top_k = int(top_k)
     with _Scope(dev, stream) as handle:
-        stats = logits.new_empty((3, R), dtype=torch.float32)
-        p = stats.data_ptr()
+        logprob, entropy, lse = _vectors(3, R)
         ids = lps = pi = pl = None
         if top_k > 0:
-            ids = logits.new_empty((R, top_k), dtype=torch.int32)
-            lps = logits.new_empty((R, top_k), dtype=torch.float32)
+            ids, lps = _matrix(R, top_k, torch.int32), _matrix(R, top_k, torch.float32)
             pi, pl = ids.data_ptr(), lps.data_ptr()
-        rc = lib.spdy_token_logprobs(*head, tokens.data_ptr(), bits, R, V, temperature, top_k, p, p + 4 * R, p + 8 * R, pi, pl, handle)
+        rc = lib.spdy_token_logprobs(*head, tokens.data_ptr(), bits, R, V, temperature, top_k, logprob.data_ptr(), entropy.data_ptr(),
+                                     lse.data_ptr(), pi, pl, handle)
     if rc:
         binding._check(rc, "spdy_token_logprobs")
-    return TokenLogprobs(*stats.unbind(0), ids, lps)
+    return TokenLogprobs(logprob, entropy, lse, ids, lps)
 
 
 def token_logprobs_backward(logits, tokens, lse, entropy=None, grad_logprob=None, grad_entropy=None, temperature: float = 1.0,
@@ -358,13 +369,12 @@ def token_logprobs_with_grad(logits, tokens, grad_logprob=None, grad_entropy=Non
     vectors = _optional(R, dev, grad_logprob=grad_logprob, grad_entropy=grad_entropy)
     with _Scope(dev, stream) as handle:
         out, ldo = _grads_out(out, logits, R, V, dev)
-        stats = logits.new_empty((3, R), dtype=torch.float32)
-        p = stats.data_ptr()
-        rc = lib.spdy_token_logprobs_with_grad(*head, tokens.data_ptr(), bits, R, V, temperature, *vectors, p, p + 4 * R, p + 8 * R,
-                                               out.data_ptr(), ldo, handle)
+        logprob, entropy, lse = _vectors(3, R)
+        rc = lib.spdy_token_logprobs_with_grad(*head, tokens.data_ptr(), bits, R, V, temperature, *vectors, logprob.data_ptr(),
+                                               entropy.data_ptr(), lse.data_ptr(), out.data_ptr(), ldo, handle)
     if rc:
         binding._check(rc, "spdy_token_logprobs_with_grad")
-    return TokenLogprobs(*stats.unbind(0)), out
+    return TokenLogprobs(logprob, entropy, lse), out
 
 
 def _teacher(top_ids, top_logprobs, R, dev):
@@ -388,12 +398,12 @@ def distill_loss(logits, top_ids, top_logprobs, temperature: float = 1.0, tail: 
     head, R, V, dev = _logits(logits)
     teacher, K = _teacher(top_ids, top_logprobs, R, dev)
     with _Scope(dev, stream) as handle:
-        stats = logits.new_empty((3, R) if tail else (2, R), dtype=torch.float32)
-        p = stats.data_ptr()
-        rc = lib.spdy_distill_loss(*head, *teacher, R, V, K, temperature, bool(tail), p, p + 4 * R, p + 8 * R if tail else None, handle)
+        out = _vectors(3 if tail else 2, R)
+        rc = lib.spdy_distill_loss(*head, *teacher, R, V, K, temperature, bool(tail), out[0].data_ptr(), out[1].data_ptr(),
+                                   out[2].data_ptr() if tail else None, handle)
     if rc:
         binding._check(rc, "spdy_distill_loss")
-    return DistillLoss(*stats.unbind(0))
+    return DistillLoss(*out)
 
 
 def distill_loss_backward(logits, top_ids, top_logprobs, lse, rest, grad_loss, temperature: float = 1.0, tail: bool = True,
@@ -424,10 +434,9 @@ def distill_loss_with_grad(logits, top_ids, top_logprobs, grad_loss, temperature
     pg = _vector(grad_loss, "grad_loss", R, dev, torch.float32)
     with _Scope(dev, stream) as handle:
         out, ldo = _grads_out(out, logits, R, V, dev)
-        stats = logits.new_empty((3, R) if tail else (2, R), dtype=torch.float32)
-        p = stats.data_ptr()
-        rc = lib.spdy_distill_loss_with_grad(*head, *teacher, R, V, K, temperature, bool(tail), pg, p, p + 4 * R,
-                                             p + 8 * R if tail else None, out.data_ptr(), ldo, handle)
+        sums = _vectors(3 if tail else 2, R)
+        rc = lib.spdy_distill_loss_with_grad(*head, *teacher, R, V, K, temperature, bool(tail), pg, sums[0].data_ptr(), sums[1].data_ptr(),
+                                             sums[2].data_ptr() if tail else None, out.data_ptr(), ldo, handle)
     if rc:
         binding._check(rc, "spdy_distill_loss_with_grad")
-    return DistillLoss(*stats.unbind(0)), out
+    return DistillLoss(*sums), out
