@@ -359,18 +359,46 @@ __device__ __forceinline__ void find_top(TopShared &sh, const uint32_t *groups, 
         }
     __syncthreads();
     int listed = static_cast<int>(sh.count);
-    uint32_t v = 0;  // stays 0 with fewer groups than `want`: every element is looked at
-    if (listed <= kListed) {
+    const int each = U << shift;
+    if (listed <= kListed && listed >= want) {
+        // the common case: every group that can hold one of the best is listed, those equal to v among them
         for (int i = tid; i < listed; i += NT) {
             const uint64_t k = sh.list[i];
             int rank = 0;
 #pragma unroll 8
             for (int j = 0; j < listed; ++j) rank += sh.list[j] > k;
-            if (rank == want - 1) sh.want = static_cast<uint32_t>(k >> 32);
+            if (rank == want - 1) sh.want = static_cast<uint32_t>(k >> 32), sh.count = 0;
         }
         __syncthreads();
-        v = sh.want;
-    } else {
+        const uint32_t least = sh.want;
+        for (int i = tid; i < listed * each; i += NT) {
+            const uint64_t k = sh.list[i / each];
+            if (static_cast<uint32_t>(k >> 32) < least) continue;
+            const int slot = static_cast<int>(~static_cast<uint32_t>(k));
+            const int g = g0 + (slot / NT << shift) * STEP + slot % NT + i % each * NT;
+            if (g >= g1) continue;
+            const int e = row.first(g);
+            float f[VEC];
+            Elem<T>::unpack(row.load(g), f);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                if (ordered(f[j]) < least || e + j < 0 || e + j >= row.n) continue;
+                const uint32_t at = atomicAdd(&sh.count, 1u);
+                if (at < kCandidates) sh.cand[at] = rank_key(f[j], static_cast<uint32_t>(e + j));
+            }
+        }
+        __syncthreads();
+        int have = static_cast<int>(sh.count);
+        if (have > kCandidates || have < want) {
+            __syncthreads();
+            radix_top<T, NT>(sh, row, g0, g1, want);
+            have = want;
+        }
+        select_top<NT>(sh, have, want);
+        return;
+    }
+    uint32_t v = 0;  // stays 0 with fewer groups than `want`: every element is looked at
+    if (listed > kListed) {
         for (int b = 31; b >= 0; --b) {
             const uint32_t trial = v | 1u << b;
             int count = 0;
@@ -391,7 +419,6 @@ __device__ __forceinline__ void find_top(TopShared &sh, const uint32_t *groups, 
         if (groups[i] >= least) sh.list[atomicAdd(&sh.count2, 1u)] = i;
     __syncthreads();
     listed = static_cast<int>(sh.count2);
-    const int each = U << shift;
     for (int i = tid; i < listed * each; i += NT) {
         const int slot = static_cast<int>(sh.list[i / each]);
         const int g = g0 + (slot / NT << shift) * STEP + slot % NT + i % each * NT;
@@ -461,23 +488,82 @@ struct TeacherShared {
     float x[SPDY_DISTILL_MAX];     // the student's logit at id
     float left, mass;              // mass: sum of q
     int bad;                       // an id >= V
+    int twice;                     // an id may come twice
 };
 
-// The entries of a row, by `n` threads; the student's logits only for ids in [e0, e1) (another block may be overwriting the
-// rest in place).  `bad` is zero before.
-template <class T> __device__ __forceinline__ void teacher_read(TeacherShared &sh, const LossArgs &a, int64_t row, int e0, int e1, int t, int n)
-{
-    for (int j = t; j < a.K; j += n) {
-        const int64_t id = index_at(a.ids, a.index_bits, row * a.K + j);
-        if (id >= a.V) sh.bad = 1;
-        const bool here = id >= 0 && id < a.V;
-        sh.id[j] = here ? static_cast<int32_t>(id) : -1;
-        sh.logq[j] = here ? a.top_lp[row * a.K + j] : neg_inf();
-        sh.x[j] = here && id >= e0 && id < e1 ? Elem<T>::to_float(static_cast<const T *>(a.logits)[row * a.ld + id]) : neg_inf();
-    }
-}
+// What a thread of n holds of a row's entries: those t, t + n, ...  Ids and log probabilities are on their way from the
+// constructor on; the student's logits follow from `place` and are put down by `settle`, so that a row need not wait for them
+// before it is streamed.
+template <class T, int N> struct Entries {
+    static constexpr int kEach = (SPDY_DISTILL_MAX + N - 1) / N;
+    int64_t id[kEach];
+    float logq[kEach], x[kEach];
 
-// q, log q, left and mass from the entries; one warp, after a barrier behind teacher_read.
+    __device__ __forceinline__ Entries(const LossArgs &a, int64_t row, int t)
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = i * N + t;
+            id[i] = j < a.K ? index_at(a.ids, a.index_bits, row * a.K + j) : -1;
+            logq[i] = j < a.K ? a.top_lp[row * a.K + j] : 0.f;
+        }
+    }
+    // The student's logits only for ids in [e0, e1) (another block may be overwriting the rest in place).
+    __device__ __forceinline__ void place(TeacherShared &sh, const LossArgs &a, int64_t row, int e0, int e1, int t)
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = i * N + t;
+            if (j >= a.K) break;
+            const bool here = id[i] >= 0 && id[i] < a.V;
+            if (id[i] >= a.V) sh.bad = 1;
+            sh.id[j] = here ? static_cast<int32_t>(id[i]) : -1;
+            sh.logq[j] = here ? logq[i] : neg_inf();
+            x[i] = here && id[i] >= e0 && id[i] < e1 ? Elem<T>::to_float(static_cast<const T *>(a.logits)[row * a.ld + id[i]]) : neg_inf();
+        }
+    }
+    __device__ __forceinline__ void settle(TeacherShared &sh, int K, int t) const
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (i * N + t < K) sh.x[i * N + t] = x[i];
+    }
+    // Marks the ids among elements first .. first + count - 1 in a bitmap; bit i of the result: entry i was the first to mark its id.
+    __device__ __forceinline__ uint32_t mark(TeacherShared &sh, int K, uint32_t *bitmap, int first, int count, int t) const
+    {
+        uint32_t marked = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = i * N + t;
+            if (j >= K) break;
+            const int pos = sh.id[j] - first;
+            if (sh.id[j] < 0 || pos < 0 || pos >= count) continue;
+            const uint32_t bit = 1u << (pos & 31);
+            if (atomicOr(&bitmap[pos >> 5], bit) & bit) sh.twice = 1;
+            else marked |= 1u << i;
+        }
+        return marked;
+    }
+    __device__ __forceinline__ void unmark(const TeacherShared &sh, int K, uint32_t *bitmap, int first, int count, int t) const
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = i * N + t;
+            if (j >= K) break;
+            const int pos = sh.id[j] - first;
+            if (sh.id[j] >= 0 && pos >= 0 && pos < count) bitmap[pos >> 5] = 0;
+        }
+    }
+    // Adds the logits of the entries that marked their ids to the sums over the set.
+    __device__ __forceinline__ void add_marked(uint32_t marked, float c, float &mi, float &si) const
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (marked >> i & 1) add_logit(mi, si, x[i], c);
+    }
+};
+
+// q, log q, left and mass from the entries; one warp, after a barrier behind Entries::place.
 template <bool TAIL> __device__ __forceinline__ void teacher_weights(TeacherShared &sh, int K)
 {
     const int lane = threadIdx.x & 31;
@@ -568,6 +654,10 @@ template <bool ENT, bool TAIL> __device__ __forceinline__ Stats warp_stats(Runni
     }
     return st;
 }
+
+struct NoEntries {
+    __device__ __forceinline__ NoEntries(const LossArgs &, int64_t, int) {}
+};
 
 // One thread writes a row's sums; `token_x` is the given token's logit.
 template <bool ENT, bool TAIL> __device__ __forceinline__ void write_sums(const LossArgs &a, int64_t r, const Stats &st, const RowEnd &e, int token, float token_x)
@@ -751,35 +841,18 @@ template <class T> __device__ __forceinline__ void write_set_gradient(const Teac
     for (int j = t; j < K; j += n) {
         const int32_t id = sh.id[j];
         if (id < 0 || id < e0 || id >= e1) continue;
-        float q = 0.f;
+        float q = sh.q[j];
         bool first = true;
+        if (sh.twice) {
+            q = 0.f;
 #pragma unroll 8
-        for (int i = 0; i < K; ++i)
-            if (sh.id[i] == id) {
-                first = first && i >= j;
-                q += sh.q[i];
-            }
+            for (int i = 0; i < K; ++i)
+                if (sh.id[i] == id) {
+                    first = first && i >= j;
+                    q += sh.q[i];
+                }
+        }
         if (first) out[id] = Elem<T>::from_float(ex2((sh.x[j] - k.p_m) * c) * k.p_scale - q * k.q_scale);
-    }
-}
-
-// Marks the teacher's ids among elements first .. first + count - 1 in a bitmap; the thread that marks one adds it to the sums
-// over the set.
-__device__ __forceinline__ void mark_set(const TeacherShared &sh, int K, uint32_t *bitmap, int first, int count, float c, float &mi, float &si, int t, int n)
-{
-    for (int j = t; j < K; j += n) {
-        const int pos = sh.id[j] - first;
-        if (sh.id[j] < 0 || pos < 0 || pos >= count) continue;
-        const uint32_t bit = 1u << (pos & 31);
-        if (!(atomicOr(&bitmap[pos >> 5], bit) & bit)) add_logit(mi, si, sh.x[j], c);
-    }
-}
-
-__device__ __forceinline__ void unmark_set(const TeacherShared &sh, int K, uint32_t *bitmap, int first, int count, int t, int n)
-{
-    for (int j = t; j < K; j += n) {
-        const int pos = sh.id[j] - first;
-        if (sh.id[j] >= 0 && pos >= 0 && pos < count) bitmap[pos >> 5] = 0;
     }
 }
 
@@ -797,13 +870,13 @@ constexpr int kWarpCandidates = 256;
 
 template <class T, int U, int MODE> struct WarpShared {
     TeacherShared teacher[MODE >= kDistill ? kWarpRows : 1];
-    uint32_t bitmap[MODE == kDistillTail ? kWarpRows : 1][U * Elem<T>::kVec];
+    uint32_t bitmap[MODE >= kDistill ? kWarpRows : 1][U * Elem<T>::kVec];
     uint64_t cand[MODE == kLogprobsTop ? kWarpRows : 1][kWarpCandidates];
     uint32_t count[kWarpRows];
 };
 
 // The `want` best of a warp's granules, as keys in cand[0..n), n <= kWarpCandidates; returns n.  The want-th largest granule's
-// largest element bounds the want-th largest element from below.
+// largest element (or lane's) bounds the want-th largest element from below.
 template <class T, int U> __device__ __forceinline__ int warp_top(uint4 *raw, const Row<T> &row, int G, int want, uint64_t *cand, uint32_t *count)
 {
     constexpr int VEC = Elem<T>::kVec;
@@ -812,12 +885,25 @@ template <class T, int U> __device__ __forceinline__ int warp_top(uint4 *raw, co
 #pragma unroll
     for (int u = 0; u < U; ++u) keys[u] = u * 32 + lane < G ? ordered(Elem<T>::max_of(raw[u])) : 0u;
     uint32_t v = 0;
-    for (int b = 31; b >= (VEC == 8 ? 12 : 0); --b) {  // 16-bit types: the low bits of the order are all alike
-        const uint32_t trial = v | 1u << b;
-        int n = 0;
+    if (want <= 32) {  // the want-th largest of the lanes' largest will do, a little lower
+        uint32_t mine = keys[0];
 #pragma unroll
-        for (int u = 0; u < U; ++u) n += keys[u] >= trial;
-        if (static_cast<int>(__reduce_add_sync(0xffffffffu, n)) >= want) v = trial;
+        for (int u = 1; u < U; ++u) mine = max(mine, keys[u]);
+        int rank = 0;
+#pragma unroll
+        for (int l = 0; l < 32; ++l) {
+            const uint32_t other = __shfl_sync(0xffffffffu, mine, l);
+            rank += other > mine || (other == mine && l < lane);
+        }
+        v = __reduce_max_sync(0xffffffffu, rank == want - 1 ? mine : 0u);
+    } else {
+        for (int b = 31; b >= (VEC == 8 ? 12 : 0); --b) {  // 16-bit types: the low bits of the order are all alike
+            const uint32_t trial = v | 1u << b;
+            int n = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) n += keys[u] >= trial;
+            if (static_cast<int>(__reduce_add_sync(0xffffffffu, n)) >= want) v = trial;
+        }
     }
     if (lane == 0) *count = 0;
     __syncwarp();
@@ -906,17 +992,19 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
     step.load(raw);
     int token = -1;
     float token_x = 0.f, mi = neg_inf(), si = 0.f;
-    if (TEACHER) {
-        if (lane == 0) teacher.bad = 0;
+    if constexpr (TEACHER) {
+        Entries<T, 32> entries(a, r, lane);
+        for (int i = lane; i < U * Elem<T>::kVec; i += 32) sh.bitmap[warp][i] = 0;
+        if (lane == 0) teacher.bad = teacher.twice = 0;
         __syncwarp();
-        teacher_read<T>(teacher, a, r, 0, static_cast<int>(a.V), lane, 32);
-        if (TAIL && GRAD != kGradSaved)
-            for (int i = lane; i < U * Elem<T>::kVec; i += 32) sh.bitmap[warp][i] = 0;
+        entries.place(teacher, a, r, 0, row.n, lane);
         __syncwarp();
         teacher_weights<TAIL>(teacher, a.K);
+        const uint32_t marked = entries.mark(teacher, a.K, sh.bitmap[warp], row.first(0), G * Elem<T>::kVec, lane);
+        entries.settle(teacher, a.K, lane);
+        if (TAIL && GRAD != kGradSaved) entries.add_marked(marked, a.c, mi, si);
+        __syncwarp();
         if (TAIL && GRAD != kGradSaved) {
-            mark_set(teacher, a.K, sh.bitmap[warp], row.first(0), G * Elem<T>::kVec, a.c, mi, si, lane, 32);
-            __syncwarp();
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const uint32_t bits = u * 32 + lane < G ? bits_of<T>(sh.bitmap[warp], u * 32 + lane) : 0u;
@@ -1037,10 +1125,12 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
         float mi = neg_inf(), si = 0.f;
         int token = -1;
         float token_x = 0.f;
-        if (TEACHER) {
-            if (tid == 0) teacher.bad = 0;
+        uint32_t marked = 0;
+        typename std::conditional<TEACHER, Entries<T, NT>, NoEntries>::type entries(a, r, tid);
+        if constexpr (TEACHER) {
+            if (tid == 0) teacher.bad = 0, teacher.twice = !TAIL;
             __syncthreads();
-            teacher_read<T>(teacher, a, r, rank == 0 ? 0 : row.first(g0), rank == 0 ? row.n : row.first(g1), tid, NT);
+            entries.place(teacher, a, r, rank == 0 ? 0 : row.first(g0), rank == 0 ? row.n : row.first(g1), tid);
             __syncthreads();
             if (warp == 0 && (rank == 0 || GRAD)) teacher_weights<TAIL>(teacher, a.K);
         } else if (a.ids) {
@@ -1058,8 +1148,9 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
 
         for (int seg = g0; seg < g1; seg = TAIL ? seg + kSegment : g1) {
             const int seg_end = TAIL ? min(g1, seg + kSegment) : g1;
-            if (TAIL) {
-                mark_set(teacher, a.K, bitmap, row.first(seg), (seg_end - seg) * Elem<T>::kVec, a.c, mi, si, tid, NT);
+            if constexpr (TAIL) {
+                const uint32_t now = entries.mark(teacher, a.K, bitmap, row.first(seg), (seg_end - seg) * Elem<T>::kVec, tid);
+                marked |= now;
                 __syncthreads();
             }
             for (int base = seg; base < seg_end; base += STEP, ++step) {
@@ -1089,13 +1180,17 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
                 raise<ENT>(run, all, a.c);
                 accumulate<T, U, ENT>(cur, a.c, run);
             }
-            if (TAIL) {
+            if constexpr (TAIL) {
                 __syncthreads();
-                unmark_set(teacher, a.K, bitmap, row.first(seg), (seg_end - seg) * Elem<T>::kVec, tid, NT);
+                entries.unmark(teacher, a.K, bitmap, row.first(seg), (seg_end - seg) * Elem<T>::kVec, tid);
                 if (seg_end < g1) __syncthreads();
             }
         }
 
+        if constexpr (TEACHER) {
+            if constexpr (TAIL) entries.add_marked(marked, a.c, mi, si);
+            entries.settle(teacher, a.K, tid);
+        }
         Stats st = warp_stats<ENT, TAIL>(run, mi, si, a.c);
         if (lane == 0) sh.part[warp] = st;
         __syncthreads();
@@ -1198,11 +1293,12 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
     int token = -1;
     float token_x = 0.f;
     uint4 next[U];
+    typename std::conditional<TEACHER, Entries<T, NT>, NoEntries>::type entries(a, r, threadIdx.x);
     Step<T, NT, U>(row, g0, threadIdx.x, g1).load_again(next);
     if constexpr (TEACHER) {
-        if (threadIdx.x == 0) shared.bad = 0;
+        if (threadIdx.x == 0) shared.bad = 0, shared.twice = 1;
         __syncthreads();
-        teacher_read<T>(shared, a, r, row.first(g0), row.first(g1), threadIdx.x, NT);
+        entries.place(shared, a, r, row.first(g0), row.first(g1), threadIdx.x);
         __syncthreads();
         if (threadIdx.x < 32) teacher_weights<TAIL>(shared, a.K);
         __syncthreads();
@@ -1222,6 +1318,7 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
         if (base + NT * U < g1) Step<T, NT, U>(row, base + NT * U, threadIdx.x, g1).load_again(next);
         writer.write(Step<T, NT, U>(row, base, threadIdx.x, g1), cur, a.c);
     }
+    if constexpr (TEACHER) entries.settle(shared, a.K, threadIdx.x);
     __syncthreads();
     if constexpr (TEACHER) write_set_gradient<T>(shared, a.K, out, row.first(g0), row.first(g1), a.c, k, threadIdx.x, NT);
     else if (threadIdx.x == 0 && token >= 0) write_token_gradient<T>(out, token, token_x, a.c, k);
