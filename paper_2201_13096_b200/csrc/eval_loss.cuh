@@ -138,24 +138,28 @@ template <bool ENT> __device__ __forceinline__ void raise(Running &st, float top
     }
 }
 
+// Adds a granule's elements with any reference: out of line, it is rare.
+template <class T> __device__ __noinline__ Running accumulate_far(uint4 raw, float c, Running st)
+{
+    const Reference ref(st.m, c);
+    float f[Elem<T>::kVec];
+    Elem<T>::unpack(raw, f);
+#pragma unroll
+    for (int i = 0; i < Elem<T>::kVec; ++i) {
+        const float d = max_nan(ref.far ? (f[i] - ref.sub) * c : fmaf(f[i], c, -ref.base), -1000.f), e = ex2(d);
+        st.s += e;
+        st.t = fmaf(e, d, st.t);
+    }
+    return st;
+}
+
 // Adds U granules of each thread of a warp, after raise.
 template <class T, int U, bool ENT> __device__ __forceinline__ void accumulate(const uint4 *raw, float c, Running &st)
 {
     const Reference ref(st.m, c);
     if (__any_sync(0xffffffffu, ref.far)) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float f[Elem<T>::kVec];
-            Elem<T>::unpack(raw[u], f);
-#pragma unroll 1
-            for (int i = 0; i < Elem<T>::kVec; ++i) {
-                const float d = max_nan(ref.far ? (f[0] - ref.sub) * c : fmaf(f[0], c, -ref.base), -1000.f), e = ex2(d);
-                st.s += e;
-                st.t = fmaf(e, d, st.t);
-#pragma unroll
-                for (int j = 0; j + 1 < Elem<T>::kVec; ++j) f[j] = f[j + 1];
-            }
-        }
+        for (int u = 0; u < U; ++u) st = accumulate_far<T>(raw[u], c, st);
         return;
     }
 #pragma unroll
@@ -186,12 +190,13 @@ template <bool ENT> __device__ __forceinline__ void settle(Running &st, float c)
 // -inf in place of the elements whose bit is set
 template <class T> __device__ __forceinline__ uint4 without(uint4 raw, uint32_t bits)
 {
-    float f[Elem<T>::kVec];
-    Elem<T>::unpack(raw, f);
-#pragma unroll
-    for (int i = 0; i < Elem<T>::kVec; ++i)
-        if (bits >> i & 1) f[i] = neg_inf();
-    return Elem<T>::pack(f);
+    constexpr uint32_t NI = Elem<T>::kNegInfWord;
+    if (sizeof(T) == 4) return make_uint4(bits & 1 ? NI : raw.x, bits & 2 ? NI : raw.y, bits & 4 ? NI : raw.z, bits & 8 ? NI : raw.w);
+    const auto word = [](uint32_t w, uint32_t two) {
+        const uint32_t mask = (two & 1 ? 0xffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
+        return (w & ~mask) | (NI & mask);
+    };
+    return make_uint4(word(raw.x, bits), word(raw.y, bits >> 2), word(raw.z, bits >> 4), word(raw.w, bits >> 6));
 }
 
 // The bits of granule g (counted from the first one the bitmap covers).
@@ -234,8 +239,8 @@ __device__ __forceinline__ uint64_t warp_nth_key(uint32_t value, uint32_t index,
 constexpr int kCandidates = 1536, kListed = 512;
 
 struct TopShared {
-    uint64_t cand[kCandidates];
-    uint64_t list[kListed];
+    uint64_t cand[kCandidates + 1];  // the last of each takes what is too many
+    uint64_t list[kListed + 1];
     uint64_t best[SPDY_TOP_MAX];  // the result, descending
     uint64_t tau[32];
     uint32_t count, count2;
@@ -272,7 +277,7 @@ template <int NT> __device__ __noinline__ void select_top(TopShared &sh, int n, 
         const uint64_t k = sh.cand[i];
         if (k < least) continue;
         int rank = 0;
-#pragma unroll 8
+#pragma unroll 4
         for (int j = 0; j < n; ++j) rank += sh.cand[j] > k;
         if (rank < want) sh.best[rank] = k;
     }
@@ -332,19 +337,33 @@ template <class T, int NT> __device__ __noinline__ void radix_top(TopShared &sh,
     __syncthreads();
 }
 
+// Appends granule g's elements of at least `least` to the candidates.
+template <class T> __device__ __noinline__ void append_candidates(TopShared &sh, const T *p, int n, int lead, int g, uint32_t least)
+{
+    const int e = g * Elem<T>::kVec - lead;
+    float f[Elem<T>::kVec];
+    Elem<T>::unpack(e >= 0 && e <= n - Elem<T>::kVec ? load_stream(p + e) : load_part(p, n, e), f);
+#pragma unroll
+    for (int j = 0; j < Elem<T>::kVec; ++j) {
+        if (ordered(f[j]) < least || e + j < 0 || e + j >= n) continue;
+        sh.cand[min(atomicAdd(&sh.count, 1u), static_cast<uint32_t>(kCandidates))] = rank_key(f[j], static_cast<uint32_t>(e + j));
+    }
+}
+
 // While a block streams its part of a row, each thread notes the largest element of each of its groups (the U granules of
-// one step, or of 2^shift steps in a row too long for `groups`) as an ordered 32-bit value, 0 for a group without elements.
+// one step, or of 2^shift steps in a row too long for the list), NaN for a group without elements.
 // Then the K-th largest group value v bounds the K-th largest element from below: elements above v lie in fewer than K
 // groups, which are read again; what may still be missing are elements equal to v, those with the lowest ids.
 // Result in sh.best[0..want).
 template <class T, int NT, int U>
-__device__ __forceinline__ void find_top(TopShared &sh, const uint32_t *groups, int n_groups, int shift, const Row<T> row, int g0, int g1, int want)
+__device__ __forceinline__ void find_top(TopShared &sh, const float *largest, int n_groups, int shift, const Row<T> row, int g0, int g1, int want)
 {
     constexpr int NW = NT / 32, STEP = NT * U, VEC = Elem<T>::kVec;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const auto group = [&](int i) { return ordered(largest[i]); };
     // a cheap bound first: the r-th largest lane of every warp, r such that the warps together have `want` lanes above it
     uint32_t lane_best = 0;
-    for (int i = 0; i < n_groups; ++i) lane_best = max(lane_best, groups[i * NT + tid]);
+    for (int i = 0; i < n_groups; ++i) lane_best = max(lane_best, group(i * NT + tid));
     const uint64_t mine = warp_nth_key(lane_best, static_cast<uint32_t>(lane), (want + NW - 1) / NW);
     if (lane == 0) sh.tau[warp] = mine >> 32;
     if (tid == 0) sh.count = 0, sh.want = 0;
@@ -353,9 +372,8 @@ __device__ __forceinline__ void find_top(TopShared &sh, const uint32_t *groups, 
     const int total = n_groups * NT;
 #pragma unroll 4
     for (int i = tid; i < total; i += NT)
-        if (groups[i] >= tau) {
-            const uint32_t at = atomicAdd(&sh.count, 1u);
-            if (at < kListed) sh.list[at] = static_cast<uint64_t>(groups[i]) << 32 | static_cast<uint32_t>(~i);
+        if (group(i) >= tau) {
+            sh.list[min(atomicAdd(&sh.count, 1u), static_cast<uint32_t>(kListed))] = static_cast<uint64_t>(group(i)) << 32 | static_cast<uint32_t>(~i);
         }
     __syncthreads();
     int listed = static_cast<int>(sh.count);
@@ -365,7 +383,7 @@ __device__ __forceinline__ void find_top(TopShared &sh, const uint32_t *groups, 
         for (int i = tid; i < listed; i += NT) {
             const uint64_t k = sh.list[i];
             int rank = 0;
-#pragma unroll 8
+#pragma unroll 4
             for (int j = 0; j < listed; ++j) rank += sh.list[j] > k;
             if (rank == want - 1) sh.want = static_cast<uint32_t>(k >> 32), sh.count = 0;
         }
@@ -377,15 +395,7 @@ __device__ __forceinline__ void find_top(TopShared &sh, const uint32_t *groups, 
             const int slot = static_cast<int>(~static_cast<uint32_t>(k));
             const int g = g0 + (slot / NT << shift) * STEP + slot % NT + i % each * NT;
             if (g >= g1) continue;
-            const int e = row.first(g);
-            float f[VEC];
-            Elem<T>::unpack(row.load(g), f);
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) {
-                if (ordered(f[j]) < least || e + j < 0 || e + j >= row.n) continue;
-                const uint32_t at = atomicAdd(&sh.count, 1u);
-                if (at < kCandidates) sh.cand[at] = rank_key(f[j], static_cast<uint32_t>(e + j));
-            }
+            append_candidates<T>(sh, row.p, row.n, row.lead, g, least);
         }
         __syncthreads();
         int have = static_cast<int>(sh.count);
@@ -402,13 +412,13 @@ __device__ __forceinline__ void find_top(TopShared &sh, const uint32_t *groups, 
         for (int b = 31; b >= 0; --b) {
             const uint32_t trial = v | 1u << b;
             int count = 0;
-            for (int i = tid; i < total; i += NT) count += groups[i] >= trial;
+            for (int i = tid; i < total; i += NT) count += group(i) >= trial;
             if (block_count<NT>(sh, count) >= want) v = trial;
         }
     }
     // the groups that can hold one of the best: those above v, and those equal to v unless they are many
     int ties = 0, above = 0;
-    for (int i = tid; i < total; i += NT) ties += groups[i] == v, above += groups[i] > v;
+    for (int i = tid; i < total; i += NT) ties += group(i) == v, above += group(i) > v;
     ties = block_count<NT>(sh, ties);
     above = block_count<NT>(sh, above);
     const bool few = ties + above <= kListed && ties <= 64 + want;
@@ -416,22 +426,14 @@ __device__ __forceinline__ void find_top(TopShared &sh, const uint32_t *groups, 
     if (tid == 0) sh.count = sh.count2 = 0;
     __syncthreads();
     for (int i = tid; i < total; i += NT)
-        if (groups[i] >= least) sh.list[atomicAdd(&sh.count2, 1u)] = i;
+        if (group(i) >= least) sh.list[atomicAdd(&sh.count2, 1u)] = i;
     __syncthreads();
     listed = static_cast<int>(sh.count2);
     for (int i = tid; i < listed * each; i += NT) {
         const int slot = static_cast<int>(sh.list[i / each]);
         const int g = g0 + (slot / NT << shift) * STEP + slot % NT + i % each * NT;
         if (g >= g1) continue;
-        const int e = row.first(g);
-        float f[VEC];
-        Elem<T>::unpack(row.load(g), f);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            if (ordered(f[j]) < least || e + j < 0 || e + j >= row.n) continue;
-            const uint32_t at = atomicAdd(&sh.count, 1u);
-            if (at < kCandidates) sh.cand[at] = rank_key(f[j], static_cast<uint32_t>(e + j));
-        }
+        append_candidates<T>(sh, row.p, row.n, row.lead, g, least);
     }
     __syncthreads();
     int have = static_cast<int>(sh.count);
@@ -520,6 +522,29 @@ template <class T, int N> struct Entries {
             sh.id[j] = here ? static_cast<int32_t>(id[i]) : -1;
             sh.logq[j] = here ? logq[i] : neg_inf();
             x[i] = here && id[i] >= e0 && id[i] < e1 ? Elem<T>::to_float(static_cast<const T *>(a.logits)[row * a.ld + id[i]]) : neg_inf();
+        }
+    }
+    // place without the student's logits, which `gather` fetches later (they cost registers meanwhile).
+    __device__ __forceinline__ void place_ids(TeacherShared &sh, const LossArgs &a, int t) const
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = i * N + t;
+            if (j >= a.K) break;
+            const bool here = id[i] >= 0 && id[i] < a.V;
+            if (id[i] >= a.V) sh.bad = 1;
+            sh.id[j] = here ? static_cast<int32_t>(id[i]) : -1;
+            sh.logq[j] = here ? logq[i] : neg_inf();
+        }
+    }
+    __device__ __forceinline__ void gather(const TeacherShared &sh, int K, const T *row, int e0, int e1, int t)
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int j = i * N + t;
+            if (j >= K) break;
+            const int at = sh.id[j];
+            x[i] = at >= 0 && at >= e0 && at < e1 ? Elem<T>::to_float(row[at]) : neg_inf();
         }
     }
     __device__ __forceinline__ void settle(TeacherShared &sh, int K, int t) const
@@ -774,10 +799,10 @@ struct Factors {
 template <class T, bool ENT> struct GradientWriter {
     T *out;
     bool same, entropy;
-    Reference ref;
-    float k0, k1;
+    float base, k0, k1;
+    const Factors &all;  // for the rare rest
     __device__ __forceinline__ GradientWriter(const Row<T> &row, T *to, const Factors &f)
-        : out(to), same(row.same_lead(to)), entropy(ENT && f.k1 != 0.f), ref(f.ref), k0(f.k0), k1(f.k1)
+        : out(to), same(row.same_lead(to)), entropy(ENT && f.k1 != 0.f), base(f.ref.base), k0(f.k0), k1(f.k1), all(f)
     {
     }
     template <bool ENTROPY> __device__ __forceinline__ uint4 gradient(uint4 raw, float c) const
@@ -786,7 +811,7 @@ template <class T, bool ENT> struct GradientWriter {
         Elem<T>::unpack(raw, f);
 #pragma unroll
         for (int i = 0; i < Elem<T>::kVec; ++i) {
-            float d = fmaf(f[i], c, -ref.base);
+            float d = fmaf(f[i], c, -base);
             if (ENTROPY) {
                 d = max_nan(d, -1000.f);
                 f[i] = ex2(d) * fmaf(k1, d, k0);
@@ -810,11 +835,11 @@ template <class T, bool ENT> struct GradientWriter {
     }
     template <int NT, int U> __device__ __forceinline__ void write(const Step<T, NT, U> &step, const uint4 *raw, float c) const
     {
-        if (!step.plain || !same || ref.far) {
+        if (!step.plain || !same || all.ref.far) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (step.g + u * NT < step.limit)
-                    step.store_part_of(out, same, u, ref.far ? far_gradient(raw[u], c, ref.sub, k0, k1) : ENT && entropy ? gradient<true>(raw[u], c) : gradient<false>(raw[u], c));
+                    step.store_part_of(out, same, u, all.ref.far ? far_gradient(raw[u], c, all.ref.sub, k0, k1) : ENT && entropy ? gradient<true>(raw[u], c) : gradient<false>(raw[u], c));
             return;
         }
         T *to = out + step.row.first(step.g);
@@ -845,7 +870,7 @@ template <class T> __device__ __forceinline__ void write_set_gradient(const Teac
         bool first = true;
         if (sh.twice) {
             q = 0.f;
-#pragma unroll 8
+#pragma unroll 4
             for (int i = 0; i < K; ++i)
                 if (sh.id[i] == id) {
                     first = first && i >= j;
@@ -871,7 +896,7 @@ constexpr int kWarpCandidates = 256;
 template <class T, int U, int MODE> struct WarpShared {
     TeacherShared teacher[MODE >= kDistill ? kWarpRows : 1];
     uint32_t bitmap[MODE >= kDistill ? kWarpRows : 1][U * Elem<T>::kVec];
-    uint64_t cand[MODE == kLogprobsTop ? kWarpRows : 1][kWarpCandidates];
+    uint64_t cand[MODE == kLogprobsTop ? kWarpRows : 1][kWarpCandidates + 1];  // the last takes what is too many
     uint32_t count[kWarpRows];
 };
 
@@ -890,7 +915,7 @@ template <class T, int U> __device__ __forceinline__ int warp_top(uint4 *raw, co
 #pragma unroll
         for (int u = 1; u < U; ++u) mine = max(mine, keys[u]);
         int rank = 0;
-#pragma unroll
+#pragma unroll 8
         for (int l = 0; l < 32; ++l) {
             const uint32_t other = __shfl_sync(0xffffffffu, mine, l);
             rank += other > mine || (other == mine && l < lane);
@@ -916,8 +941,7 @@ template <class T, int U> __device__ __forceinline__ int warp_top(uint4 *raw, co
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             if (ordered(f[i]) < v || e + i < 0 || e + i >= row.n) continue;
-            const uint32_t at = atomicAdd(count, 1u);
-            if (at < kWarpCandidates) cand[at] = rank_key(f[i], static_cast<uint32_t>(e + i));
+            cand[min(atomicAdd(count, 1u), static_cast<uint32_t>(kWarpCandidates))] = rank_key(f[i], static_cast<uint32_t>(e + i));
         }
     }
     __syncwarp();
@@ -984,7 +1008,7 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
     const int64_t r = static_cast<int64_t>(blockIdx.x) * kWarpRows + warp;
     if (r >= a.R) return;
     const Row<T> row(static_cast<const T *>(a.logits) + r * a.ld, a.V);
-    T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
+    T *out = static_cast<T *>(a.dlogits) + static_cast<int64_t>(r) * a.lddl;
     const int G = row.granules();
     TeacherShared &teacher = sh.teacher[TEACHER ? warp : 0];
     uint4 raw[U];
@@ -1036,7 +1060,7 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
             for (int i = lane; i < n; i += 32) {
                 const uint64_t key = cand[i];
                 int rank = 0;
-#pragma unroll 8
+#pragma unroll 4
                 for (int j = 0; j < n; ++j) rank += cand[j] > key;
                 if (rank >= a.K) continue;
                 a.top_ids[r * a.K + rank] = static_cast<int32_t>(~static_cast<uint32_t>(key));
@@ -1051,7 +1075,8 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
     // the elements are unpacked again rather than kept unpacked in twice the registers
 #pragma unroll
     for (int u = 0; u < U; ++u) asm volatile("" : "+r"(raw[u].x), "+r"(raw[u].y), "+r"(raw[u].z), "+r"(raw[u].w));
-    GradientWriter<T, ENT>(row, out, Factors(k, a.c)).write(step, raw, a.c);
+    const Factors factors(k, a.c);
+    GradientWriter<T, ENT>(row, out, factors).write(step, raw, a.c);
     __syncwarp();
     if (TEACHER) write_set_gradient<T>(teacher, a.K, out, 0, row.n, a.c, k, lane, 32);
     else if (lane == 0 && token >= 0 && token < a.V) write_token_gradient<T>(out, token, token_x, a.c, k);
@@ -1060,7 +1085,9 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
 // ------------------------------------------------------------------------------------------ long rows: a block or cluster each
 constexpr int kBitmapWords = 4096;  // ids of one segment of a row: 2^17 bits
 constexpr int kGroupSteps = 32;     // groups a thread notes at most
-constexpr int kRowThreads = 768;    // threads a multiprocessor holds of the long rows' kernels
+// Threads a multiprocessor holds of the long rows' kernels (by their registers: 80, or 96 where alternatives are looked for, with
+// blocks of 128 there: 2048 x 131072 with the best 20 took 133 us with 256 threads, 125 with 128).
+constexpr int row_threads(int mode) { return mode == 1 ? 640 : 768; }
 
 template <int NT> struct RowShared {
     Stats part[NT / 32];
@@ -1087,7 +1114,7 @@ template <class T> struct Share {
 // while this row is finished.  With GRAD the row is then read again, backwards, and its gradient written: rows in flight stay
 // in L2 (see row_cluster), so that memory is read once.
 template <class T, int NT, int U, int MODE, int GRAD>
-__global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const LossArgs a)
+__global__ void __launch_bounds__(NT, row_threads(MODE) / NT) loss_row_kernel(const LossArgs a)
 {
     constexpr bool ENT = MODE == kLogprobs || MODE == kLogprobsTop, TOP = MODE == kLogprobsTop;
     constexpr bool TEACHER = MODE >= kDistill, TAIL = MODE == kDistillTail;
@@ -1096,15 +1123,15 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
     __shared__ __align__(16) unsigned char shared_bytes[sizeof(RowShared<NT>)];
     RowShared<NT> &sh = *reinterpret_cast<RowShared<NT> *>(shared_bytes);
     TopShared &top = *reinterpret_cast<TopShared *>(dynamic);                               // TOP
-    uint32_t *groups = reinterpret_cast<uint32_t *>(dynamic + sizeof(TopShared));           // TOP
+    float *groups = reinterpret_cast<float *>(dynamic + sizeof(TopShared));                 // TOP
     TeacherShared &teacher = *reinterpret_cast<TeacherShared *>(dynamic);                   // TEACHER
     uint32_t *bitmap = reinterpret_cast<uint32_t *>(dynamic + sizeof(TeacherShared));       // TAIL
 
     cg::cluster_group cluster = cg::this_cluster();
     const int C = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int64_t stride = gridDim.x / C;
-    int64_t r = blockIdx.x / C;
+    const int stride = static_cast<int>(gridDim.x) / C;
+    int r = static_cast<int>(blockIdx.x) / C;
     uint4 next[U];
     const auto begin_row = [&](int64_t at) {  // a row's first granules; nothing beyond the last row
         if (at >= a.R) return;
@@ -1117,7 +1144,7 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
         __syncthreads();
     }
 
-    for (; r < a.R; r += stride) {
+    for (; r < a.R; r = static_cast<int>(min(static_cast<int64_t>(r) + stride, a.R))) {
         const Share<T> share(a, r, C, rank);
         const Row<T> &row = share.row;
         const int g0 = share.g0, g1 = share.g1;
@@ -1130,7 +1157,7 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
         if constexpr (TEACHER) {
             if (tid == 0) teacher.bad = 0, teacher.twice = !TAIL;
             __syncthreads();
-            entries.place(teacher, a, r, rank == 0 ? 0 : row.first(g0), rank == 0 ? row.n : row.first(g1), tid);
+            entries.place_ids(teacher, a, tid);
             __syncthreads();
             if (warp == 0 && (rank == 0 || GRAD)) teacher_weights<TAIL>(teacher, a.K);
         } else if (a.ids) {
@@ -1159,7 +1186,7 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
                 for (int u = 0; u < U; ++u) cur[u] = next[u];
                 // with a gradient the second reading begins where this one ends: `next` stays
                 if (base + STEP < g1) Step<T, NT, U>(row, base + STEP, tid, g1).load(next);
-                else if (!GRAD && !TOP) begin_row(r + stride);
+                else if (!GRAD && !TOP) begin_row(static_cast<int64_t>(r) + stride);
                 if (TAIL) {
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
@@ -1172,10 +1199,9 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
 #pragma unroll
                 for (int u = 1; u < U; ++u) all = fmaxf(all, Elem<T>::max_of(cur[u]));
                 if (TOP) {
-                    uint32_t key = base + tid < g1 ? ordered(all) : 0u;
-                    uint32_t *slot = groups + (step >> shift) * NT + tid;
-                    if (step & ((1 << shift) - 1)) key = max(key, *slot);
-                    *slot = key;
+                    float *slot = groups + (step >> shift) * NT + tid;
+                    const float largest = base + tid < g1 ? all : quiet_nan();
+                    *slot = step & ((1 << shift) - 1) ? fmaxf(largest, *slot) : largest;
                 }
                 raise<ENT>(run, all, a.c);
                 accumulate<T, U, ENT>(cur, a.c, run);
@@ -1188,6 +1214,7 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
         }
 
         if constexpr (TEACHER) {
+            entries.gather(teacher, a.K, row.p, rank == 0 ? 0 : row.first(g0), rank == 0 ? row.n : row.first(g1), tid);
             if constexpr (TAIL) entries.add_marked(marked, a.c, mi, si);
             entries.settle(teacher, a.K, tid);
         }
@@ -1250,28 +1277,27 @@ __global__ void __launch_bounds__(NT, kRowThreads / NT) loss_row_kernel(const Lo
             if (TOP) {
                 for (int i = tid; i < a.K; i += NT) {
                     const uint64_t key = top.best[i];
-                    a.top_ids[r * a.K + i] = static_cast<int32_t>(~static_cast<uint32_t>(key));
-                    a.top_logprobs[r * a.K + i] = log_prob(unordered(static_cast<uint32_t>(key >> 32)), sh.end, a.inv_t);
+                    a.top_ids[static_cast<int64_t>(r) * a.K + i] = static_cast<int32_t>(~static_cast<uint32_t>(key));
+                    a.top_logprobs[static_cast<int64_t>(r) * a.K + i] = log_prob(unordered(static_cast<uint32_t>(key >> 32)), sh.end, a.inv_t);
                 }
             }
         }
         if (GRAD) {
-            T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
+            T *out = static_cast<T *>(a.dlogits) + static_cast<int64_t>(r) * a.lddl;
             const GradientWriter<T, ENT> writer(row, out, sh.factors);
             for (int base = g0 + (steps - 1) * STEP; base >= g0; base -= STEP) {
                 uint4 cur[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) cur[u] = next[u];
                 if (base > g0) Step<T, NT, U>(row, base - STEP, tid, g1).load_again(next);
-                else begin_row(r + stride);
                 writer.write(Step<T, NT, U>(row, base, tid, g1), cur, a.c);
             }
-            if (g0 == g1) begin_row(r + stride);
+            begin_row(static_cast<int64_t>(r) + stride);
             __syncthreads();
             if (TEACHER) write_set_gradient<T>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, sh.grad, tid, NT);
             else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, sh.grad);
         } else if (TOP || g0 == g1) {  // the search for the alternatives needs the registers
-            begin_row(r + stride);
+            begin_row(static_cast<int64_t>(r) + stride);
         }
         __syncthreads();  // the next row overwrites shared memory
         if (C > 1) cluster.barrier_wait();
@@ -1286,7 +1312,7 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
     const int64_t r = blockIdx.x / a.segments;
     const int part = static_cast<int>(blockIdx.x % a.segments);
     const Row<T> row(static_cast<const T *>(a.logits) + r * a.ld, a.V);
-    T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
+    T *out = static_cast<T *>(a.dlogits) + static_cast<int64_t>(r) * a.lddl;
     const int G = row.granules(), per = (G + a.segments - 1) / a.segments;
     const int g0 = min(G, part * per), g1 = min(G, g0 + per);
     RowGrad k;
@@ -1310,7 +1336,8 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
         if (threadIdx.x == 0 && token >= 0) token_x = Elem<T>::to_float(row.p[token]);
         __syncthreads();  // read before it is overwritten in place
     }
-    const GradientWriter<T, !TEACHER> writer(row, out, Factors(k, a.c));
+    const Factors factors(k, a.c);
+    const GradientWriter<T, !TEACHER> writer(row, out, factors);
     for (int base = g0; base < g1; base += NT * U) {
         uint4 cur[U];
 #pragma unroll
@@ -1336,6 +1363,7 @@ constexpr int kSteps = 4;  // granules per thread and step of the long rows' ker
 
 template <class T, int NT, int MODE, int GRAD> inline int launch_row(const LossArgs &a, int cluster, cudaStream_t stream)
 {
+    if (a.R > kMostBlocks) return SPDY_ERR_UNSUPPORTED;  // rows are counted in 32 bits
     auto *kernel = loss_row_kernel<T, NT, kSteps, MODE, GRAD>;
     size_t smem = 0;
     if (MODE == kDistill) smem = sizeof(TeacherShared);
@@ -1350,7 +1378,7 @@ template <class T, int NT, int MODE, int GRAD> inline int launch_row(const LossA
     // Rows of few steps: blocks that stay, since the next row's first granules hide the start of each (16384 x 8192: 122 ->
     // 86 us).  Longer ones: a block per row, which the hardware deals out more evenly (4096 x 65536: 122 -> 111 us).
     const bool stay = most_granules<T>(a) <= 4096;
-    const int64_t held = stay ? std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * (kRowThreads / NT) / cluster) : kMostBlocks / cluster;
+    const int64_t held = stay ? std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * (row_threads(MODE) / NT) / cluster) : kMostBlocks / cluster;
     config.gridDim = dim3(static_cast<unsigned>(std::min(a.R, held) * cluster));
     config.blockDim = dim3(NT);
     config.dynamicSmemBytes = smem;
@@ -1369,7 +1397,7 @@ template <class T, int NT, int MODE, int GRAD> inline int launch_row(const LossA
 // work; with a gradient also as many as keep the rows in flight within 64 MB of L2.
 template <class T> inline int row_cluster(const LossArgs &a, int64_t G, int threads, bool grad)
 {
-    const int64_t slots = static_cast<int64_t>(sm_count()) * (kRowThreads / threads);
+    const int64_t slots = static_cast<int64_t>(sm_count()) * (row_threads(kDistill) / threads);
     int cluster = 1;
     if (grad)
         while (cluster < 8 && slots / cluster * G * 16 > (64ll << 20)) cluster *= 2;
@@ -1391,9 +1419,9 @@ template <class T, int MODE, int GRAD> int rows(const LossArgs &a, cudaStream_t 
     const int64_t G = most_granules<T>(a);
     if (G <= 128) return launch_warp<T, 4, MODE, GRAD>(a, stream);
     if (G <= 256) return launch_warp<T, 8, MODE, GRAD>(a, stream);
-    const int threads = G <= 1024 ? 128 : 256;
-    const int cluster = row_cluster<T>(a, G, threads, GRAD);
-    return threads == 128 ? launch_row<T, 128, MODE, GRAD>(a, cluster, stream) : launch_row<T, 256, MODE, GRAD>(a, cluster, stream);
+    if constexpr (MODE == kLogprobsTop) return launch_row<T, 128, MODE, GRAD>(a, row_cluster<T>(a, G, 128, GRAD), stream);
+    else if (G <= 1024) return launch_row<T, 128, MODE, GRAD>(a, row_cluster<T>(a, G, 128, GRAD), stream);
+    else return launch_row<T, 256, MODE, GRAD>(a, row_cluster<T>(a, G, 256, GRAD), stream);
 }
 
 template <class T, int MODE> int backward(LossArgs a, cudaStream_t stream)
