@@ -9,6 +9,9 @@ using namespace spdy_eval;
 
 namespace {
 
+constexpr int64_t kShortBytes = 256;    // rows up to here share a warp
+constexpr int64_t kRingMost = 32768;    // bytes of the longest rows that a ring holds
+
 struct NormArgs {
     const void *x, *dy, *weight, *bias;
     int64_t ldx, lddy, ldy, lddx, R, D;
@@ -49,6 +52,13 @@ template <class P, int N> __device__ __forceinline__ void params(const void *p, 
     for (int i = 0; i < N; ++i) f[i] = e + i >= 0 && e + i < D ? Elem<P>::to_float(at[i]) : fallback;
 }
 
+// The threads of a group of TPR, group `group` of the block, meet.
+template <int TPR> __device__ __forceinline__ void meet(int group)
+{
+    if (TPR <= 32) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
+}
+
 // Sums of TPR consecutive threads' values, in all of them.  `slot` alternates between calls, so that one barrier is enough.
 template <int TPR, int COUNT> __device__ __forceinline__ void row_sums(float *v, float (*shared)[32], int slot)
 {
@@ -58,16 +68,17 @@ template <int TPR, int COUNT> __device__ __forceinline__ void row_sums(float *v,
         for (int i = 0; i < COUNT; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
     if (TPR > 32) {
         constexpr int W = TPR / 32;
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = threadIdx.x / TPR;
         if (lane == 0)
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) shared[slot * COUNT + i][warp] = v[i];
-        __syncthreads();
+        meet<TPR>(group);
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) {
-            v[i] = lane < W ? shared[slot * COUNT + i][lane] : 0.f;
+            v[i] = lane < W ? shared[slot * COUNT + i][group * W + lane] : 0.f;
 #pragma unroll
-            for (int d = 16; d; d >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
+            for (int d = W / 2; d; d >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
+            v[i] = __shfl_sync(0xffffffffu, v[i], 0);
         }
     }
 }
@@ -166,6 +177,330 @@ template <class T, int NT> __global__ void __launch_bounds__(NT) norm_forward_lo
     }
 }
 
+// ---------------------------------------------------------------------------------------------- many rows
+// A block that stays on its multiprocessor walks over rows.  Each group of TPR threads owns a ring of S rows in shared memory,
+// which asynchronous copies fill S - 1 rows ahead of the sums: with rows fetched into registers instead, the reads paused
+// while a row was being summed.  Thread t works on the columns of granules t, TPR + t, ... counted from the row's start.
+// WHOLE: rows are aligned granules, a thread copies, reads and stores its own.  Else the copies bring the aligned granules that lie wholly
+// inside the row, single elements its ends, and everything is shifted on the way out of shared memory.
+__device__ __forceinline__ void copy16(void *to, const void *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to))), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// 16 bytes from byte `shift` of granule g on.
+__device__ __forceinline__ uint4 shifted(const uint4 *row, int g, int shift)
+{
+    const uint4 a = row[g];
+    if (shift == 0) return a;
+    const uint4 b = row[g + 1];
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int j = 0; j < 6; ++j) w[j] = shift & 8 ? w[j + 2] : w[j];
+#pragma unroll
+    for (int j = 0; j < 5; ++j) w[j] = shift & 4 ? w[j + 1] : w[j];
+    const int bits = (shift & 3) * 8;
+    return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+}
+
+// The ends of a row that starts anywhere, one element to each of the first 2 kVec threads: element `at` of the row, if `mine`.
+template <class T> struct Ends {
+    bool mine;
+    int at;
+    __device__ __forceinline__ Ends(const Row<T> &row, int t)
+    {
+        constexpr int VEC = Elem<T>::kVec;
+        const int inside = (row.n + row.lead) / VEC * VEC - row.lead;  // where the last granule begins, if it is not whole
+        at = t < VEC ? t : inside + t - VEC;
+        mine = t < VEC ? row.lead > 0 && t < VEC - row.lead : t < 2 * VEC && at < row.n;
+    }
+};
+
+template <class T, int TPR, int VPT, bool WHOLE> struct RowSlot {
+    static constexpr int VEC = Elem<T>::kVec;
+    static constexpr int kGranules = TPR * VPT + (WHOLE ? 0 : 2);
+    static __device__ __forceinline__ void fetch(uint4 *slot, const T *p, int n, int t)
+    {
+        if (WHOLE) {
+#pragma unroll
+            for (int v = 0; v < VPT; ++v)
+                if ((v * TPR + t) * VEC < n) copy16(slot + v * TPR + t, p + (v * TPR + t) * VEC);
+        } else {
+            const Row<T> row(p, n);
+#pragma unroll
+            for (int v = 0; v <= VPT; ++v)
+                if (v * TPR + t < kGranules && row.whole(v * TPR + t)) copy16(slot + v * TPR + t, p + row.first(v * TPR + t));
+        }
+    }
+    // columns of granule v * TPR + t (0 beyond n); `lead`: elements of the slot before the row
+    static __device__ __forceinline__ uint4 get(const uint4 *slot, int v, int t, int lead, int n)
+    {
+        if (WHOLE) return slot[v * TPR + t];
+        uint4 raw = shifted(slot, v * TPR + t, lead * static_cast<int>(sizeof(T)));
+        const int e = (v * TPR + t) * VEC;
+        if (e + VEC > n) {
+            float f[VEC];
+            Elem<T>::unpack(raw, f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) f[i] = e + i < n ? f[i] : 0.f;
+            raw = Elem<T>::pack(f);
+        }
+        return raw;
+    }
+    // The results of a row that starts anywhere, which lie in `slot` from its first granule on, to `out`.
+    static __device__ __forceinline__ void put(const uint4 *slot, T *out, int n, int t)
+    {
+        const Row<T> row(out, n);
+        const int shift = (VEC - row.lead) % VEC * static_cast<int>(sizeof(T));
+#pragma unroll
+        for (int v = 0; v <= VPT; ++v) {
+            const int g = v * TPR + t;
+            if (row.whole(g)) store_stream(out + row.first(g), shifted(slot, g - (row.lead > 0), shift));
+        }
+        const Ends<T> ends(row, t);
+        if (ends.mine) out[ends.at] = reinterpret_cast<const T *>(slot)[ends.at];
+    }
+};
+
+// A weight or bias in shared memory, as the group of threads uses it: its granules of columns, `fallback` for a NULL vector.
+template <class T, class P, int TPR, int VPT> struct ParamRow {
+    static constexpr int VEC = Elem<T>::kVec, PV = Elem<P>::kVec, kGranules = TPR * VPT * VEC / PV;
+    static __device__ __forceinline__ void fill(uint4 *to, const void *p, int D, float fallback)
+    {
+        P *at = reinterpret_cast<P *>(to);
+        for (int e = threadIdx.x; e < TPR * VPT * VEC; e += blockDim.x) at[e] = p && e < D ? static_cast<const P *>(p)[e] : Elem<P>::from_float(fallback);
+    }
+    static __device__ __forceinline__ void get(const uint4 *from, int v, int t, float *f)
+    {
+#pragma unroll
+        for (int i = 0; i < VEC / PV; ++i) Elem<P>::unpack(from[(v * TPR + t) * (VEC / PV) + i], f + i * PV);
+    }
+};
+
+template <class T, class P, int TPR, int VPT, bool WHOLE, int NT, int S, int PER_SM>
+__global__ void __launch_bounds__(NT, PER_SM) norm_forward_ring_kernel(const NormArgs a)
+{
+    using Slot = RowSlot<T, TPR, VPT, WHOLE>;
+    using Params = ParamRow<T, P, TPR, VPT>;
+    constexpr int GROUPS = NT / TPR, VEC = Elem<T>::kVec;
+    extern __shared__ uint4 memory[];
+    __shared__ float shared[2][32];
+    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR, D = static_cast<int>(a.D);
+    uint4 *weight = memory, *bias = memory + Params::kGranules, *ring = memory + 2 * Params::kGranules + group * (S * Slot::kGranules);
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * GROUPS;
+    int64_t r = static_cast<int64_t>(blockIdx.x) * GROUPS + group;
+    const auto at = [&](int64_t row) { return static_cast<const T *>(a.x) + row * a.ldx; };
+    const auto fetch = [&](int64_t row, int slot) {
+        if (row < a.R) Slot::fetch(ring + slot * Slot::kGranules, at(row), D, t);
+        copies_commit();
+    };
+    T end = Elem<T>::from_float(0.f);
+    const auto fetch_end = [&](int64_t row) {
+        if (WHOLE || row >= a.R) return;
+        const Ends<T> e(Row<T>(at(row), D), t);
+        if (e.mine) end = at(row)[e.at];
+    };
+#pragma unroll
+    for (int i = 0; i < S; ++i) fetch(r + i * stride, i);
+    fetch_end(r);
+    Params::fill(weight, a.weight, D, 1.f);
+    Params::fill(bias, a.bias, D, 0.f);
+    __syncthreads();
+    const float n = static_cast<float>(D);
+    for (int slot = 0; r < a.R; r += stride, slot = slot + 1 == S ? 0 : slot + 1) {
+        uint4 *mine = ring + slot * Slot::kGranules;
+        int lead = 0;
+        copies_wait<S - 1>();
+        if (!WHOLE) {
+            const Row<T> row(at(r), D);
+            const Ends<T> e(row, t);
+            lead = row.lead;
+            if (e.mine) reinterpret_cast<T *>(mine)[e.at + lead] = end;
+            meet<TPR>(group);
+            fetch_end(r + stride);
+        }
+        uint4 raw[VPT];
+#pragma unroll
+        for (int v = 0; v < VPT; ++v)
+            if ((v * TPR + t) * VEC < D) raw[v] = Slot::get(mine, v, t, lead, D);
+        float sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+            if ((v * TPR + t) * VEC >= D) continue;
+            float f[VEC];
+            Elem<T>::unpack(raw[v], f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sum += f[i];
+        }
+        row_sums<TPR, 1>(&sum, shared, 0);
+        if (WHOLE) fetch(r + S * stride, slot);
+        const float mean = sum / n;
+        float sq = 0.f;
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+            const int e = (v * TPR + t) * VEC;
+            if (e >= D) continue;
+            float f[VEC];
+            Elem<T>::unpack(raw[v], f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (WHOLE || e + i < D) sq = fmaf(f[i] - mean, f[i] - mean, sq);
+        }
+        row_sums<TPR, 1>(&sq, shared, 1);
+        const float rstd = 1.f / sqrtf(sq / n + a.eps);
+        if (t == 0) {
+            if (a.mean) a.mean[r] = mean;
+            if (a.rstd) a.rstd[r] = rstd;
+        }
+        T *out = static_cast<T *>(a.y) + r * a.ldy;
+        if (!WHOLE && TPR == 32) __syncwarp();  // all have read the slot (longer groups met in the sums)
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+            const int e = (v * TPR + t) * VEC;
+            if (e >= D) continue;
+            float f[VEC], w[VEC], b[VEC];
+            Elem<T>::unpack(raw[v], f);
+            Params::get(weight, v, t, w);
+            Params::get(bias, v, t, b);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) f[i] = fmaf((f[i] - mean) * rstd, w[i], b[i]);
+            if (WHOLE) store_stream(out + e, Elem<T>::pack(f));
+            else mine[v * TPR + t] = Elem<T>::pack(f);
+        }
+        if (!WHOLE) {
+            meet<TPR>(group);
+            Slot::put(mine, out, D, t);
+            meet<TPR>(group);
+            fetch(r + S * stride, slot);
+        }
+    }
+}
+
+// dx row by row, and the sums of its columns for dweight and dbias in the thread's registers; the groups' sums are joined through
+// shared memory in a fixed order, the blocks' by norm_columns_kernel.
+template <class T, class P, int TPR, int VPT, bool WHOLE, int NT, int S> __global__ void __launch_bounds__(NT, 1) norm_backward_ring_kernel(const NormArgs a)
+{
+    using Slot = RowSlot<T, TPR, VPT, WHOLE>;
+    using Params = ParamRow<T, P, TPR, VPT>;
+    constexpr int GROUPS = NT / TPR, VEC = Elem<T>::kVec;
+    extern __shared__ uint4 memory[];
+    __shared__ float shared[4][32];
+    const int group = threadIdx.x / TPR, t = threadIdx.x % TPR, D = static_cast<int>(a.D);
+    uint4 *weight = memory, *rings = memory + Params::kGranules, *ring = rings + group * (2 * S * Slot::kGranules);
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * GROUPS;
+    int64_t r = static_cast<int64_t>(blockIdx.x) * GROUPS + group;
+    const auto x_at = [&](int64_t row) { return static_cast<const T *>(a.x) + row * a.ldx; };
+    const auto dy_at = [&](int64_t row) { return static_cast<const T *>(a.dy) + row * a.lddy; };
+    const auto fetch = [&](int64_t row, int slot) {
+        if (row < a.R) {
+            Slot::fetch(ring + 2 * slot * Slot::kGranules, x_at(row), D, t);
+            Slot::fetch(ring + (2 * slot + 1) * Slot::kGranules, dy_at(row), D, t);
+        }
+        copies_commit();
+    };
+    T end_x = Elem<T>::from_float(0.f), end_dy = end_x;
+    float next_mean = 0.f, next_rstd = 0.f;
+    const auto fetch_ends = [&](int64_t row) {
+        if (row >= a.R) return;
+        next_mean = a.in_mean[row], next_rstd = a.in_rstd[row];
+        if (WHOLE) return;
+        const Ends<T> ex(Row<T>(x_at(row), D), t), ey(Row<T>(dy_at(row), D), t);
+        if (ex.mine) end_x = x_at(row)[ex.at];
+        if (ey.mine) end_dy = dy_at(row)[ey.at];
+    };
+#pragma unroll
+    for (int i = 0; i < S; ++i) fetch(r + i * stride, i);
+    fetch_ends(r);
+    Params::fill(weight, a.weight, D, 1.f);
+    __syncthreads();
+    float dw[VPT * VEC], db[VPT * VEC];
+#pragma unroll
+    for (int i = 0; i < VPT * VEC; ++i) dw[i] = db[i] = 0.f;
+    const float inv_n = 1.f / static_cast<float>(D);
+    int parity = 0;
+    for (int slot = 0; r < a.R; r += stride, slot = slot + 1 == S ? 0 : slot + 1, parity ^= 1) {
+        uint4 *x = ring + 2 * slot * Slot::kGranules, *dy = x + Slot::kGranules;
+        const float mean = next_mean, rstd = next_rstd;
+        int lead_x = 0, lead_dy = 0;
+        copies_wait<S - 1>();
+        if (!WHOLE) {
+            const Row<T> rx(x_at(r), D), ry(dy_at(r), D);
+            const Ends<T> ex(rx, t), ey(ry, t);
+            lead_x = rx.lead, lead_dy = ry.lead;
+            if (ex.mine) reinterpret_cast<T *>(x)[ex.at + lead_x] = end_x;
+            if (ey.mine) reinterpret_cast<T *>(dy)[ey.at + lead_dy] = end_dy;
+            meet<TPR>(group);
+        }
+        fetch_ends(r + stride);
+        float sums[2] = {0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+            if ((v * TPR + t) * VEC >= D) continue;
+            float w[VEC], h[VEC], u[VEC];
+            Params::get(weight, v, t, w);
+            Elem<T>::unpack(Slot::get(x, v, t, lead_x, D), h);
+            Elem<T>::unpack(Slot::get(dy, v, t, lead_dy, D), u);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const int k = v * VEC + i;
+                const float hat = (h[i] - mean) * rstd;  // beyond the row dy is 0, and so is all that follows
+                dw[k] = fmaf(u[i], hat, dw[k]);
+                db[k] += u[i];
+                u[i] *= w[i];
+                sums[0] += u[i];
+                sums[1] = fmaf(u[i], hat, sums[1]);
+            }
+        }
+        row_sums<TPR, 2>(sums, shared, parity);
+        const float mu = sums[0] * inv_n, mh = sums[1] * inv_n;
+        T *out = static_cast<T *>(a.dx) + r * a.lddx;
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+            const int e = (v * TPR + t) * VEC;
+            uint4 result = make_uint4(0, 0, 0, 0);
+            if (e < D) {
+                float w[VEC], h[VEC], f[VEC];
+                Params::get(weight, v, t, w);
+                Elem<T>::unpack(Slot::get(x, v, t, lead_x, D), h);
+                Elem<T>::unpack(Slot::get(dy, v, t, lead_dy, D), f);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) f[i] = rstd * (f[i] * w[i] - fmaf((h[i] - mean) * rstd, mh, mu));
+                result = Elem<T>::pack(f);
+                if (WHOLE) store_stream(out + e, result);
+            }
+            if (!WHOLE) {
+                meet<TPR>(group);  // granules v * TPR .. (v + 1) * TPR have been read; the last of them is not written yet
+                if (e < D) x[v * TPR + t] = result;
+            }
+        }
+        if (!WHOLE) {
+            meet<TPR>(group);
+            Slot::put(x, out, D, t);
+            meet<TPR>(group);
+        }
+        fetch(r + S * stride, slot);
+    }
+    if (!a.want_params) return;
+    copies_wait<0>();
+    __syncthreads();
+    float *columns = reinterpret_cast<float *>(rings) + static_cast<int64_t>(group) * 2 * D;  // [GROUPS][2][D]
+#pragma unroll
+    for (int k = 0; k < VPT * VEC; ++k) {
+        const int e = ((k / VEC) * TPR + t) * VEC + k % VEC;
+        if (e < D) columns[e] = dw[k], columns[D + e] = db[k];
+    }
+    __syncthreads();
+    float *to = a.partial + static_cast<int64_t>(blockIdx.x) * 2 * D;
+    for (int c = threadIdx.x; c < 2 * D; c += NT) {
+        float sum = 0.f;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) sum += reinterpret_cast<const float *>(rings)[g * 2 * D + c];
+        to[c] = sum;
+    }
+}
+
 // What a thread of the backward kernel holds of a row: VPT times 16 bytes (WIDE: rows start on 16 bytes; the last ones may be
 // partly outside and read as 0 there), or VPT single elements.
 template <class T, int VPT, bool WIDE> struct Held;
@@ -220,7 +555,7 @@ template <class T, int VPT> struct Held<T, VPT, false> {
 // Each group of TPR threads walks over rows, the next row's elements on their way while this one's are used, and keeps the sums of
 // its columns for dweight and dbias in registers; the groups of a block are joined through shared memory in a fixed order,
 // the blocks by norm_columns_kernel.
-template <class T, class P, int TPR, int VPT, bool WIDE, bool AHEAD, int NT> __global__ void __launch_bounds__(NT) norm_backward_kernel(const NormArgs a)
+template <class T, class P, int TPR, int VPT, bool WIDE, int NT> __global__ void __launch_bounds__(NT) norm_backward_kernel(const NormArgs a)
 {
     constexpr int GROUPS = NT / TPR, VEC = Held<T, VPT, WIDE>::kVec;
     __shared__ float shared[4][32];
@@ -240,13 +575,13 @@ template <class T, class P, int TPR, int VPT, bool WIDE, bool AHEAD, int NT> __g
         to_dy.load(static_cast<const T *>(a.dy) + at * a.lddy, n, t, TPR);
         to_mean = a.in_mean[at], to_rstd = a.in_rstd[at];
     };
-    if (AHEAD) fetch(static_cast<int64_t>(blockIdx.x) * GROUPS + group, next_x, next_dy, next_mean, next_rstd);
+    if (WIDE) fetch(static_cast<int64_t>(blockIdx.x) * GROUPS + group, next_x, next_dy, next_mean, next_rstd);
     int slot = 0;
     // the same number of rounds for all groups of a block: their threads meet in the sums
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * GROUPS; base < a.R; base += stride, slot ^= 1) {
         const int64_t r = base + group;
         const bool here = r < a.R;
-        if (AHEAD) {
+        if (WIDE) {
             x = next_x, dy = next_dy, mean = next_mean, rstd = next_rstd;
             if (base + stride < a.R) fetch(r + stride, next_x, next_dy, next_mean, next_rstd);
         } else {
@@ -359,6 +694,7 @@ __global__ void __launch_bounds__(1024) norm_columns_kernel(const float *partial
     const int64_t padded = (D + 31) / 32 * 32;
     const bool second = static_cast<int64_t>(blockIdx.x) * 32 >= padded;
     const int64_t col = second ? e - padded : e;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     float sum = 0.f;
     if (col < D) {
         const float *p = partial + (second ? D : 0) + col;
@@ -389,6 +725,29 @@ template <class T, int TPR, int VPT, int NT> int forward_with(const NormArgs &a,
     return finish_launch();
 }
 
+constexpr int64_t kRingBytes = 16 << 20;  // of x, from which on the forward's ring pays
+constexpr int kRingThreads = 512;
+constexpr int kMostShared = 226 * 1024;
+
+template <class T, class P, int TPR, int VPT, bool WHOLE> int forward_ring_with(const NormArgs &a, cudaStream_t s)
+{
+    constexpr int GROUPS = kRingThreads / TPR, S = VPT == 4 ? 3 : 4;
+    constexpr int smem = 16 * (2 * ParamRow<T, P, TPR, VPT>::kGranules + GROUPS * S * RowSlot<T, TPR, VPT, WHOLE>::kGranules);
+    constexpr int PER_SM = 2 * (smem + 1024) <= kMostShared ? 2 : 1;
+    static_assert(smem <= kMostShared, "");
+    auto *kernel = norm_forward_ring_kernel<T, P, TPR, VPT, WHOLE, kRingThreads, S, PER_SM>;
+    SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    const int64_t blocks = (a.R + GROUPS - 1) / GROUPS, most = PER_SM * sm_count();
+    kernel<<<static_cast<unsigned>(blocks < most ? blocks : most), kRingThreads, smem, s>>>(a);
+    return finish_launch();
+}
+template <class T, int TPR, int BYTES> int forward_ring(const NormArgs &a, bool whole, cudaStream_t s)
+{
+    constexpr int VPT = BYTES / 16;
+    if (a.param_type == SPDY_F32) return whole ? forward_ring_with<T, float, TPR, VPT, true>(a, s) : forward_ring_with<T, float, TPR, VPT, false>(a, s);
+    return whole ? forward_ring_with<T, T, TPR, VPT, true>(a, s) : forward_ring_with<T, T, TPR, VPT, false>(a, s);
+}
+
 template <class T> int forward(const NormArgs &a, cudaStream_t s)
 {
     constexpr int VEC = Elem<T>::kVec;
@@ -396,6 +755,17 @@ template <class T> int forward(const NormArgs &a, cudaStream_t s)
     const bool in_line = a.ldx % VEC == 0 && aligned(a.x, 16);
     const bool whole = in_line && a.ldy % VEC == 0 && aligned(a.y, 16) && a.D % VEC == 0;
     const int64_t G = (a.D + VEC - 1) / VEC + (in_line ? 0 : 1);
+    const int64_t bytes = a.D * static_cast<int64_t>(sizeof(T));
+    if (bytes > kShortBytes && bytes <= kRingMost && a.R * bytes >= kRingBytes) {
+        if (bytes <= 512) return forward_ring<T, 32, 16>(a, whole, s);
+        if (bytes <= 1024) return forward_ring<T, 32, 32>(a, whole, s);
+        if (bytes <= 1536) return forward_ring<T, 32, 48>(a, whole, s);
+        if (bytes <= 2048) return forward_ring<T, 32, 64>(a, whole, s);
+        if (bytes <= 4096) return forward_ring<T, 128, 32>(a, whole, s);
+        if (bytes <= 8192) return forward_ring<T, 128, 64>(a, whole, s);
+        if (bytes <= 16384) return forward_ring<T, 256, 64>(a, whole, s);
+        return forward_ring<T, 512, 64>(a, whole, s);
+    }
     // Short rows share a warp; a row stays with one warp (no barrier) up to 8 granules a thread.
     if (G <= 4) return forward_with<T, 4, 1, 128>(a, whole, s);
     if (G <= 8) return forward_with<T, 8, 1, 128>(a, whole, s);
@@ -413,54 +783,54 @@ template <class T> int forward(const NormArgs &a, cudaStream_t s)
     return finish_launch();
 }
 
-// How the backward kernel holds rows of D columns: threads per row, columns per thread.  Wide rows: up to 32 columns a thread
-// (64 sums in registers), single elements: up to 16.
-struct BackwardShape {
-    int threads, columns, block;
-};
-BackwardShape backward_shape(int64_t D, bool wide, int vec)
-{
-    if (wide) {
-        for (int t = 4; t <= 16; t *= 2)
-            if (D <= t * vec) return {t, vec, 128};
-        for (int c = vec; c <= 32; c += vec)
-            if (D <= 32 * c) return {32, c, 128};
-        return {D <= 4096 ? 128 : 256, 32, D <= 4096 ? 128 : 256};
-    }
-    for (int t = 8; t <= 32; t *= 2)
-        if (D <= 4 * t) return {t, 4, 128};
-    if (D <= 512) return {32, 16, 128};
-    return D <= 2048 ? BackwardShape{128, 16, 128} : BackwardShape{512, 16, 512};
-}
-
-constexpr int64_t kMostColumns = 8192;  // of rows held in registers
-
 bool backward_wide(const NormArgs &a, int64_t size) { return a.ldx * size % 16 == 0 && a.lddy * size % 16 == 0 && aligned(a.x, 16) && aligned(a.dy, 16); }
 
 // Blocks whose sums meet in the workspace; the same for every alignment, so that the workspace does not depend on it.
-int backward_blocks(int64_t R, int64_t D)
+int backward_blocks(int64_t R, int64_t D, int64_t size)
 {
-    if (D > kMostColumns) {
+    if (D * size > kRingMost) {
         const int64_t chunks = (R + 63) / 64;
         return static_cast<int>(chunks < 64 ? chunks : 64);
     }
-    const int64_t rows = D <= 32 ? 16 : D <= 1024 ? 4 : 1;  // a block's rows, at least
-    const int64_t blocks = (R + rows - 1) / rows, most = D <= 4096 ? 444 : 222;
+    const bool is_short = D * size <= kShortBytes;
+    const int64_t rows = is_short ? 16 : 4;  // a block's rows, at least
+    const int64_t blocks = (R + rows - 1) / rows, most = is_short ? 444 : sm_count();
     return static_cast<int>(blocks < most ? blocks : most);
 }
 
-template <class T, int TPR, int VPT, bool WIDE, int NT> int backward_with(const NormArgs &a, int blocks, cudaStream_t s)
+template <class T, class P, int TPR, int VPT, bool WHOLE> int backward_ring_with(const NormArgs &a, int blocks, cudaStream_t s)
 {
-    auto *kernel = a.param_type == SPDY_F32 ? norm_backward_kernel<T, float, TPR, VPT, WIDE, WIDE, NT> : norm_backward_kernel<T, T, TPR, VPT, WIDE, WIDE, NT>;
+    constexpr int GROUPS = kRingThreads / TPR, fixed = 16 * ParamRow<T, P, TPR, VPT>::kGranules, row = 32 * GROUPS * RowSlot<T, TPR, VPT, WHOLE>::kGranules;
+    constexpr int fit = (kMostShared - fixed) / row, S = fit < 4 ? fit : 4, smem = fixed + S * row;
+    static_assert(S >= 2, "");
+    static_assert(S * row >= GROUPS * 2 * TPR * VPT * Elem<T>::kVec * 4, "the columns' sums lie where the ring was");
+    auto *kernel = norm_backward_ring_kernel<T, P, TPR, VPT, WHOLE, kRingThreads, S>;
+    SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    kernel<<<blocks, kRingThreads, smem, s>>>(a);
+    return finish_launch();
+}
+template <class T, int TPR, int BYTES> int backward_ring(const NormArgs &a, bool whole, int blocks, cudaStream_t s)
+{
+    constexpr int VPT = BYTES / 16;
+    if (a.param_type == SPDY_F32) return whole ? backward_ring_with<T, float, TPR, VPT, true>(a, blocks, s) : backward_ring_with<T, float, TPR, VPT, false>(a, blocks, s);
+    return whole ? backward_ring_with<T, T, TPR, VPT, true>(a, blocks, s) : backward_ring_with<T, T, TPR, VPT, false>(a, blocks, s);
+}
+
+template <class T, int TPR, int VPT, bool WIDE> int backward_short(const NormArgs &a, int blocks, cudaStream_t s)
+{
+    constexpr int NT = 128;
+    auto *kernel = a.param_type == SPDY_F32 ? norm_backward_kernel<T, float, TPR, VPT, WIDE, NT> : norm_backward_kernel<T, T, TPR, VPT, WIDE, NT>;
     const size_t smem = a.want_params ? static_cast<size_t>(NT / TPR - 1) * 2 * static_cast<size_t>(a.D) * sizeof(float) : 0;
-    if (smem > 32 * 1024) SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
     kernel<<<blocks, NT, smem, s>>>(a);
     return finish_launch();
 }
 
 template <class T> int backward(const NormArgs &a, int blocks, cudaStream_t s)
 {
-    if (a.D > kMostColumns) {
+    constexpr int VEC = Elem<T>::kVec;
+    const int64_t bytes = a.D * static_cast<int64_t>(sizeof(T));
+    const bool wide = backward_wide(a, sizeof(T));
+    if (bytes > kRingMost) {
         if (a.R > 0x7fffffff) return SPDY_ERR_UNSUPPORTED;
         // the columns first: dx may overwrite dy or x
         if (a.want_params) {
@@ -471,26 +841,25 @@ template <class T> int backward(const NormArgs &a, int blocks, cudaStream_t s)
         norm_backward_long_kernel<T, 512><<<static_cast<unsigned>(a.R), 512, 0, s>>>(a);
         return finish_launch();
     }
-    constexpr int VEC = Elem<T>::kVec;
-    const bool wide = backward_wide(a, sizeof(T));
-    const BackwardShape p = backward_shape(a.D, wide, VEC);
-    if (wide) {
-        if (p.threads == 4) return backward_with<T, 4, 1, true, 128>(a, blocks, s);
-        if (p.threads == 8) return backward_with<T, 8, 1, true, 128>(a, blocks, s);
-        if (p.threads == 16) return backward_with<T, 16, 1, true, 128>(a, blocks, s);
-        if (p.threads == 128) return backward_with<T, 128, 32 / VEC, true, 128>(a, blocks, s);
-        if (p.threads == 256) return backward_with<T, 256, 32 / VEC, true, 256>(a, blocks, s);
-        if (p.columns <= 8) return backward_with<T, 32, 8 / VEC, true, 128>(a, blocks, s);
-        if (p.columns <= 16) return backward_with<T, 32, 16 / VEC, true, 128>(a, blocks, s);
-        if (p.columns <= 24) return backward_with<T, 32, 24 / VEC, true, 128>(a, blocks, s);
-        return backward_with<T, 32, 32 / VEC, true, 128>(a, blocks, s);
+    if (bytes > kShortBytes) {
+        const bool whole = wide && a.lddx % VEC == 0 && aligned(a.dx, 16) && a.D % VEC == 0;
+        if (bytes <= 512) return backward_ring<T, 32, 16>(a, whole, blocks, s);
+        if (bytes <= 1024) return backward_ring<T, 32, 32>(a, whole, blocks, s);
+        if (bytes <= 1536) return backward_ring<T, 32, 48>(a, whole, blocks, s);
+        if (bytes <= 2048) return backward_ring<T, 32, 64>(a, whole, blocks, s);
+        if (bytes <= 4096) return backward_ring<T, 128, 32>(a, whole, blocks, s);
+        if (bytes <= 8192) return backward_ring<T, 128, 64>(a, whole, blocks, s);
+        if (bytes <= 16384) return backward_ring<T, 256, 64>(a, whole, blocks, s);
+        return backward_ring<T, 512, 64>(a, whole, blocks, s);
     }
-    if (p.threads == 8) return backward_with<T, 8, 4, false, 128>(a, blocks, s);
-    if (p.threads == 16) return backward_with<T, 16, 4, false, 128>(a, blocks, s);
-    if (p.threads == 128) return backward_with<T, 128, 16, false, 128>(a, blocks, s);
-    if (p.threads == 512) return backward_with<T, 512, 16, false, 512>(a, blocks, s);
-    if (p.columns <= 4) return backward_with<T, 32, 4, false, 128>(a, blocks, s);
-    return backward_with<T, 32, 16, false, 128>(a, blocks, s);
+    if (wide) {
+        if (a.D <= 4 * VEC) return backward_short<T, 4, 1, true>(a, blocks, s);
+        if (a.D <= 8 * VEC) return backward_short<T, 8, 1, true>(a, blocks, s);
+        return backward_short<T, 16, 1, true>(a, blocks, s);
+    }
+    if (a.D <= 32) return backward_short<T, 8, 4, false>(a, blocks, s);
+    if (a.D <= 64) return backward_short<T, 16, 4, false>(a, blocks, s);
+    return backward_short<T, 32, 4, false>(a, blocks, s);
 }
 
 constexpr int64_t kMostWidth = 0x7fffffff - 64;
@@ -520,7 +889,7 @@ int spdy_layer_norm(const void *x, int64_t ldx, int dtype, const void *weight, c
 size_t spdy_layer_norm_backward_workspace_bytes(int64_t R, int64_t D, int dtype)
 {
     if (R <= 0 || D <= 0 || D > kMostWidth || !known_type(dtype)) return 0;
-    return static_cast<size_t>(backward_blocks(R, D)) * 2 * static_cast<size_t>(D) * sizeof(float);
+    return static_cast<size_t>(backward_blocks(R, D, static_cast<int64_t>(type_size(dtype)))) * 2 * static_cast<size_t>(D) * sizeof(float);
 }
 
 int spdy_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, int dtype, const void *weight, int param_dtype, const float *mean,
@@ -546,11 +915,18 @@ int spdy_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_
         if (workspace_bytes < spdy_layer_norm_backward_workspace_bytes(R, D, dtype)) return SPDY_ERR_WORKSPACE_TOO_SMALL;
         a.partial = static_cast<float *>(workspace);
     }
-    const int blocks = backward_blocks(R, D);
+    const int blocks = backward_blocks(R, D, static_cast<int64_t>(type_size(dtype)));
     const int rc = dtype == SPDY_F32 ? backward<float>(a, blocks, s) : dtype == SPDY_BF16 ? backward<__nv_bfloat16>(a, blocks, s) : backward<__half>(a, blocks, s);
     if (rc != SPDY_OK || !a.want_params) return rc;
-    norm_columns_kernel<<<static_cast<unsigned>((D + 31) / 32 * 2), 1024, 0, s>>>(a.partial, blocks, D, dweight, dbias);
-    return finish_launch();
+    // launched while the blocks before it still run; it waits for them itself
+    cudaLaunchAttribute early = {};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(static_cast<unsigned>((D + 31) / 32 * 2)), config.blockDim = dim3(1024), config.stream = s;
+    config.attrs = &early, config.numAttrs = 1;
+    SPDY_EVAL_TRY(cudaLaunchKernelEx(&config, norm_columns_kernel, static_cast<const float *>(a.partial), blocks, D, dweight, dbias));
+    return SPDY_OK;
 }
 
 }  // extern "C"
