@@ -725,7 +725,7 @@ template <class T, int TPR, int VPT, int NT> int forward_with(const NormArgs &a,
     return finish_launch();
 }
 
-constexpr int64_t kRingBytes = 16 << 20;  // of x, from which on the forward's ring pays
+constexpr int64_t kRingBytes = 24 << 20;  // of x, from which on the forward's ring pays (direct and ring, us: 1024 bf16 columns 16 MB 11.9, 10.6, 64 MB 33.3, 29.0; 4096 columns 64 MB 49.6, 31.0; 8192 columns 16 MB 10.6, 12.6, 64 MB 35.8, 33.2; 1024 f32 columns 16 MB 8.7, 10.5)
 constexpr int kRingThreads = 512;
 constexpr int kMostShared = 226 * 1024;
 
