@@ -63,6 +63,15 @@ __device__ __forceinline__ void store_stream(void *p, uint4 v)
     asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+// 16 bytes to shared memory, both ends aligned; counted by commit and waited for by the issuing thread.
+__device__ __forceinline__ void copy16(void *to, const void *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to))), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Until at most N of the thread's groups of copies are on their way.
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Element types: how many fit 16 bytes, conversion, and the bit pattern of -inf repeated over a word.
 template <class T> struct Elem;
 template <> struct Elem<float> {
@@ -223,6 +232,24 @@ template <class T, int NT, int U> struct Step {
         } else {
 #pragma unroll
             for (int u = 0; u < U; ++u) v[u] = load_part_of(u);
+        }
+    }
+    // to shared memory, granule u to to[u * NT]; asynchronous but for the row's ends
+    __device__ __forceinline__ void copy(uint4 *to) const
+    {
+        constexpr uint32_t NI = Elem<T>::kNegInfWord;
+        if (plain) {
+            const T *p = row.p + row.first(g);
+#pragma unroll
+            for (int u = 0; u < U; ++u) copy16(to + u * NT, p + u * NT * Elem<T>::kVec);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int at = g + u * NT;
+                if (at >= limit) to[u * NT] = make_uint4(NI, NI, NI, NI);
+                else if (row.whole(at)) copy16(to + u * NT, row.p + row.first(at));
+                else to[u * NT] = load_part(row.p, row.n, row.first(at));
+            }
         }
     }
     __device__ __forceinline__ void load_again(uint4 *v) const  // not to be read after this

@@ -183,13 +183,6 @@ template <class T, int NT> __global__ void __launch_bounds__(NT) norm_forward_lo
 // while a row was being summed.  Thread t works on the columns of granules t, TPR + t, ... counted from the row's start.
 // WHOLE: rows are aligned granules, a thread copies, reads and stores its own.  Else the copies bring the aligned granules that lie wholly
 // inside the row, single elements its ends, and everything is shifted on the way out of shared memory.
-__device__ __forceinline__ void copy16(void *to, const void *from)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(__cvta_generic_to_shared(to))), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // 16 bytes from byte `shift` of granule g on.
 __device__ __forceinline__ uint4 shifted(const uint4 *row, int g, int shift)
 {

@@ -39,6 +39,7 @@ struct LossArgs {
     void *dlogits;
     int64_t lddl;
     int segments;            // blocks per row of the backward kernel
+    int steps;               // steps of a block's part of a row (the longest)
 };
 
 __device__ __forceinline__ int64_t index_at(const void *ids, int bits, int64_t i)
@@ -1083,11 +1084,21 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
 }
 
 // ------------------------------------------------------------------------------------------ long rows: a block or cluster each
-constexpr int kBitmapWords = 4096;  // ids of one segment of a row: 2^17 bits
+__host__ __device__ constexpr int bitmap_words(int threads) { return threads == 128 ? 512 : 4096; }  // ids of one segment of a row, a bit each: all of a row for 128 threads, 2^17 for 256
 constexpr int kGroupSteps = 32;     // groups a thread notes at most
 // Threads a multiprocessor holds of the long rows' kernels (by their registers: 80, or 96 where alternatives are looked for, with
 // blocks of 128 there: 2048 x 131072 with the best 20 took 133 us with 256 threads, 125 with 128).
-constexpr int row_threads(int mode) { return mode == 1 ? 640 : 768; }
+__host__ __device__ constexpr bool in_ring(int mode, int grad) { return mode >= kDistill || grad; }
+__host__ __device__ constexpr int row_threads(int mode, int grad) { return mode == kLogprobsTop ? 640 : in_ring(mode, grad) ? 1024 : 768; }
+
+// Shared memory of a block beside the ring, and the steps of U granules a thread that its ring holds: what fits the multiprocessor's share, at most 4.
+__host__ __device__ constexpr int fixed_shared(int mode, int threads) { return mode < kDistill ? 0 : static_cast<int>(sizeof(TeacherShared)) + (mode == kDistillTail ? 4 * bitmap_words(threads) : 0); }
+__host__ __device__ constexpr int ring_steps(int mode, int grad, int threads, int u)
+{
+    return (227 * 1024 / (row_threads(mode, grad) / threads) - 2048 - fixed_shared(mode, threads)) / (16 * threads * u) < 4
+               ? (227 * 1024 / (row_threads(mode, grad) / threads) - 2048 - fixed_shared(mode, threads)) / (16 * threads * u)
+               : 4;
+}
 
 template <int NT> struct RowShared {
     Stats part[NT / 32];
@@ -1109,16 +1120,19 @@ template <class T> struct Share {
     }
 };
 
-// Blocks stay and walk over rows; a row belongs to one block, or to a cluster whose blocks divide its granules.  The row is
-// streamed, the next U granules of a thread in flight while the present ones are added up, and the next row's first ones
-// while this row is finished.  With GRAD the row is then read again, backwards, and its gradient written: rows in flight stay
-// in L2 (see row_cluster), so that memory is read once.
+// A block's part of a row goes through a ring of H steps in shared memory, each thread's granules copied by itself (so that no
+// barrier is needed) H - 1 steps ahead.  With GRAD the row is then read again, backwards: its last H steps are still in the
+// ring, and the earlier ones in L2 as long as the rows in flight fit (see row_cluster).  As slots fall free the next row's
+// first steps are fetched into them, so that nothing pauses between rows; since they fall free in reverse, the ring's
+// direction turns with every row.  (With a step ahead in registers instead: 4096 x 65536 with gradient 246 us.)
 template <class T, int NT, int U, int MODE, int GRAD>
-__global__ void __launch_bounds__(NT, row_threads(MODE) / NT) loss_row_kernel(const LossArgs a)
+__global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_kernel(const LossArgs a)
 {
     constexpr bool ENT = MODE == kLogprobs || MODE == kLogprobsTop, TOP = MODE == kLogprobsTop;
     constexpr bool TEACHER = MODE >= kDistill, TAIL = MODE == kDistillTail;
     constexpr int NW = NT / 32, STEP = NT * U;
+    constexpr bool RING = in_ring(MODE, GRAD);
+    constexpr int H = !RING ? 1 : ring_steps(MODE, GRAD, NT, U);
     extern __shared__ __align__(16) unsigned char dynamic[];
     __shared__ __align__(16) unsigned char shared_bytes[sizeof(RowShared<NT>)];
     RowShared<NT> &sh = *reinterpret_cast<RowShared<NT> *>(shared_bytes);
@@ -1132,15 +1146,46 @@ __global__ void __launch_bounds__(NT, row_threads(MODE) / NT) loss_row_kernel(co
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int stride = static_cast<int>(gridDim.x) / C;
     int r = static_cast<int>(blockIdx.x) / C;
+    // without the ring: a step ahead in registers
     uint4 next[U];
     const auto begin_row = [&](int64_t at) {  // a row's first granules; nothing beyond the last row
         if (at >= a.R) return;
         const Share<T> s(a, at, C, rank);
         Step<T, NT, U>(s.row, s.g0, tid, s.g1).load(next);
     };
-    begin_row(r);
+    // else the ring: `slots` of it in use, `slot` the present one, `turn` the direction
+    uint4 *const ring = reinterpret_cast<uint4 *>(dynamic + fixed_shared(MODE, NT)) + tid;
+    const int slots = min(H, a.steps);
+    int slot = 0, turn = 1;
+    const auto advance = [&](int by) {
+        slot += by;
+        slot = slot < 0 ? slots - 1 : slot >= slots ? 0 : slot;
+    };
+    const auto fetch = [&](const Row<T> &row, int g0, int g1, int step, int to) { Step<T, NT, U>(row, g0 + step * STEP, tid, g1).copy(ring + to * STEP); };
+    const auto fetch_of = [&](int64_t at, int step, int to) {  // nothing beyond the last row
+        if (at >= a.R) return;
+        const Share<T> s(a, at, C, rank);
+        fetch(s.row, s.g0, s.g1, step, to);
+    };
+    // the present step's granules; the slots - 1 groups committed since are left on their way
+    const auto take = [&](uint4 *to) {
+        if (slots == 1) copies_wait<0>();
+        else if (slots == 2) copies_wait<1>();
+        else if (slots == 3) copies_wait<2>();
+        else copies_wait<3>();
+#pragma unroll
+        for (int u = 0; u < U; ++u) to[u] = ring[slot * STEP + u * NT];
+    };
+    if (!RING) {
+        begin_row(r);
+    } else {
+        for (int i = 0; i < slots; ++i) {
+            fetch_of(r, i, i);
+            copies_commit();
+        }
+    }
     if (TAIL) {
-        for (int i = tid; i < kBitmapWords; i += NT) bitmap[i] = 0;
+        for (int i = tid; i < bitmap_words(NT); i += NT) bitmap[i] = 0;
         __syncthreads();
     }
 
@@ -1165,33 +1210,36 @@ __global__ void __launch_bounds__(NT, row_threads(MODE) / NT) loss_row_kernel(co
             if (token >= 0 && token < a.V && tid == 0) token_x = Elem<T>::to_float(row.p[token]);
         }
 
-        constexpr int kSegment = kBitmapWords * 32 / Elem<T>::kVec;  // granules
+        constexpr int kSegment = bitmap_words(NT) * 32 / Elem<T>::kVec;  // granules
         static_assert(kSegment % STEP == 0, "a segment is whole steps");
-        const int steps = (g1 - g0 + STEP - 1) / STEP;
+        const int steps = !RING ? (g1 - g0 + STEP - 1) / STEP : a.steps;  // in the ring all rows take as many
         int shift = 0;
         if (TOP)
             while (steps >> shift >= kGroupSteps) ++shift;
         int step = 0;
 
-        for (int seg = g0; seg < g1; seg = TAIL ? seg + kSegment : g1) {
-            const int seg_end = TAIL ? min(g1, seg + kSegment) : g1;
+        const int end = g0 + steps * STEP;
+        for (int seg = g0; seg < end; seg = TAIL ? seg + kSegment : end) {
+            const int seg_end = TAIL ? min(end, seg + kSegment) : end;
             if constexpr (TAIL) {
-                const uint32_t now = entries.mark(teacher, a.K, bitmap, row.first(seg), (seg_end - seg) * Elem<T>::kVec, tid);
+                const uint32_t now = entries.mark(teacher, a.K, bitmap, row.first(seg), (min(seg_end, g1) - seg) * Elem<T>::kVec, tid);
                 marked |= now;
                 __syncthreads();
             }
             for (int base = seg; base < seg_end; base += STEP, ++step) {
                 uint4 cur[U];
+                if (!RING) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) cur[u] = next[u];
-                // with a gradient the second reading begins where this one ends: `next` stays
-                if (base + STEP < g1) Step<T, NT, U>(row, base + STEP, tid, g1).load(next);
-                else if (!GRAD && !TOP) begin_row(static_cast<int64_t>(r) + stride);
+                    for (int u = 0; u < U; ++u) cur[u] = next[u];
+                    if (base + STEP < g1) Step<T, NT, U>(row, base + STEP, tid, g1).load(next);
+                    else if (!TOP) begin_row(static_cast<int64_t>(r) + stride);
+                } else {
+                    take(cur);
+                }
                 if (TAIL) {
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
-                        const int g = base + u * NT + tid;
-                        const uint32_t bits = g < seg_end ? bits_of<T>(bitmap, g - seg) : 0u;
+                        const uint32_t bits = bits_of<T>(bitmap, base + u * NT + tid - seg);
                         if (bits) cur[u] = without<T>(cur[u], bits);
                     }
                 }
@@ -1205,11 +1253,17 @@ __global__ void __launch_bounds__(NT, row_threads(MODE) / NT) loss_row_kernel(co
                 }
                 raise<ENT>(run, all, a.c);
                 accumulate<T, U, ENT>(cur, a.c, run);
+                if (RING) {
+                    if (step + slots < steps) fetch(row, g0, g1, step + slots, slot);
+                    else if (!GRAD) fetch_of(static_cast<int64_t>(r) + stride, step + slots - steps, slot);
+                    copies_commit();
+                    advance(turn);
+                }
             }
             if constexpr (TAIL) {
                 __syncthreads();
-                entries.unmark(teacher, a.K, bitmap, row.first(seg), (seg_end - seg) * Elem<T>::kVec, tid);
-                if (seg_end < g1) __syncthreads();
+                entries.unmark(teacher, a.K, bitmap, row.first(seg), (min(seg_end, g1) - seg) * Elem<T>::kVec, tid);
+                if (seg_end < end) __syncthreads();
             }
         }
 
@@ -1285,18 +1339,21 @@ __global__ void __launch_bounds__(NT, row_threads(MODE) / NT) loss_row_kernel(co
         if (GRAD) {
             T *out = static_cast<T *>(a.dlogits) + static_cast<int64_t>(r) * a.lddl;
             const GradientWriter<T, ENT> writer(row, out, sh.factors);
-            for (int base = g0 + (steps - 1) * STEP; base >= g0; base -= STEP) {
+            for (step = steps - 1; step >= 0; --step) {
                 uint4 cur[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) cur[u] = next[u];
-                if (base > g0) Step<T, NT, U>(row, base - STEP, tid, g1).load_again(next);
-                writer.write(Step<T, NT, U>(row, base, tid, g1), cur, a.c);
+                advance(-turn);
+                take(cur);
+                writer.write(Step<T, NT, U>(row, g0 + step * STEP, tid, g1), cur, a.c);
+                if (step >= slots) fetch(row, g0, g1, step - slots, slot);
+                else fetch_of(static_cast<int64_t>(r) + stride, slots - 1 - step, slot);
+                copies_commit();
             }
-            begin_row(static_cast<int64_t>(r) + stride);
+            advance(-turn);  // to where the next row's first step went
+            turn = -turn;
             __syncthreads();
             if (TEACHER) write_set_gradient<T>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, sh.grad, tid, NT);
             else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, sh.grad);
-        } else if (TOP || g0 == g1) {  // the search for the alternatives needs the registers
+        } else if (TOP || (!RING && g0 == g1)) {  // the search for the alternatives needs the registers
             begin_row(static_cast<int64_t>(r) + stride);
         }
         __syncthreads();  // the next row overwrites shared memory
@@ -1359,16 +1416,22 @@ template <class T> inline int64_t most_granules(const LossArgs &a)
 }
 
 constexpr int64_t kMostBlocks = 0x7fffffff;
+constexpr int64_t kL2 = 64;  // MB
 constexpr int kSteps = 4;  // granules per thread and step of the long rows' kernels
 
-template <class T, int NT, int MODE, int GRAD> inline int launch_row(const LossArgs &a, int cluster, cudaStream_t stream)
+template <class T, int NT, int MODE, int GRAD> inline int launch_row(LossArgs a, int cluster, cudaStream_t stream)
 {
     if (a.R > kMostBlocks) return SPDY_ERR_UNSUPPORTED;  // rows are counted in 32 bits
     auto *kernel = loss_row_kernel<T, NT, kSteps, MODE, GRAD>;
+    constexpr int kStep = NT * kSteps;
+    a.steps = static_cast<int>(((most_granules<T>(a) + cluster - 1) / cluster + kStep - 1) / kStep);
     size_t smem = 0;
-    if (MODE == kDistill) smem = sizeof(TeacherShared);
-    if (MODE == kDistillTail) smem = sizeof(TeacherShared) + 4 * kBitmapWords;
-    if (MODE == kLogprobsTop) {
+    if (in_ring(MODE, GRAD)) {
+        constexpr int H = ring_steps(MODE, GRAD, NT, kSteps);
+        static_assert(!in_ring(MODE, GRAD) || H >= 2, "");
+        smem = fixed_shared(MODE, NT) + 16 * kStep * static_cast<size_t>(std::min(H, a.steps));
+        if (smem > 40 * 1024) SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    } else if (MODE == kLogprobsTop) {
         const int64_t steps = (most_granules<T>(a) / cluster + NT * kSteps) / (NT * kSteps);
         smem = sizeof(TopShared) + sizeof(uint32_t) * NT * static_cast<size_t>(steps < kGroupSteps ? steps + 1 : kGroupSteps + 1);
         SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -1378,7 +1441,7 @@ template <class T, int NT, int MODE, int GRAD> inline int launch_row(const LossA
     // Rows of few steps: blocks that stay, since the next row's first granules hide the start of each (16384 x 8192: 122 ->
     // 86 us).  Longer ones: a block per row, which the hardware deals out more evenly (4096 x 65536: 122 -> 111 us).
     const bool stay = most_granules<T>(a) <= 4096;
-    const int64_t held = stay ? std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * (row_threads(MODE) / NT) / cluster) : kMostBlocks / cluster;
+    const int64_t held = stay ? std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * (row_threads(MODE, GRAD) / NT) / cluster) : kMostBlocks / cluster;
     config.gridDim = dim3(static_cast<unsigned>(std::min(a.R, held) * cluster));
     config.blockDim = dim3(NT);
     config.dynamicSmemBytes = smem;
@@ -1394,14 +1457,14 @@ template <class T, int NT, int MODE, int GRAD> inline int launch_row(const LossA
 }
 
 // Blocks that share a row: more when the rows alone would not fill the device twice and every block still has a step of
-// work; with a gradient also as many as keep the rows in flight within 64 MB of L2.
-template <class T> inline int row_cluster(const LossArgs &a, int64_t G, int threads, bool grad)
+// work; with a gradient also as many as keep what the ring does not hold of the rows in flight within 64 MB of L2.
+template <class T, int NT, int MODE, int GRAD> inline int row_cluster(const LossArgs &a)
 {
-    const int64_t slots = static_cast<int64_t>(sm_count()) * (row_threads(kDistill) / threads);
+    const int64_t G = most_granules<T>(a), slots = static_cast<int64_t>(sm_count()) * (row_threads(MODE, GRAD) / NT);
     int cluster = 1;
-    if (grad)
-        while (cluster < 8 && slots / cluster * G * 16 > (64ll << 20)) cluster *= 2;
-    while (cluster < 8 && a.R * cluster < 2 * sm_count() && G > static_cast<int64_t>(cluster) * threads * kSteps) cluster *= 2;
+    if (GRAD)
+        while (cluster < 8 && slots * 16 * (G / cluster - ring_steps(MODE, GRAD, NT, kSteps) * NT * kSteps) > (kL2 << 20)) cluster *= 2;
+    while (cluster < 8 && a.R * cluster < 2 * sm_count() && G > static_cast<int64_t>(cluster) * NT * kSteps) cluster *= 2;
     return cluster;
 }
 
@@ -1419,9 +1482,9 @@ template <class T, int MODE, int GRAD> int rows(const LossArgs &a, cudaStream_t 
     const int64_t G = most_granules<T>(a);
     if (G <= 128) return launch_warp<T, 4, MODE, GRAD>(a, stream);
     if (G <= 256) return launch_warp<T, 8, MODE, GRAD>(a, stream);
-    if constexpr (MODE == kLogprobsTop) return launch_row<T, 128, MODE, GRAD>(a, row_cluster<T>(a, G, 128, GRAD), stream);
-    else if (G <= 1024) return launch_row<T, 128, MODE, GRAD>(a, row_cluster<T>(a, G, 128, GRAD), stream);
-    else return launch_row<T, 256, MODE, GRAD>(a, row_cluster<T>(a, G, 256, GRAD), stream);
+    if constexpr (MODE == kLogprobsTop) return launch_row<T, 128, MODE, GRAD>(a, row_cluster<T, 128, MODE, GRAD>(a), stream);
+    else if (G <= 1024) return launch_row<T, 128, MODE, GRAD>(a, row_cluster<T, 128, MODE, GRAD>(a), stream);
+    else return launch_row<T, 256, MODE, GRAD>(a, row_cluster<T, 256, MODE, GRAD>(a), stream);
 }
 
 template <class T, int MODE> int backward(LossArgs a, cudaStream_t stream)
