@@ -39,7 +39,8 @@ struct LossArgs {
     void *dlogits;
     int64_t lddl;
     int segments;            // blocks per row of the backward kernel
-    int steps;               // steps of a block's part of a row (the longest)
+    int stride;              // rows in flight of the long rows' kernel
+    int per_block, steps;    // granules of a row that one of a cluster's blocks takes, and their steps (of the longest row)
 };
 
 __device__ __forceinline__ int64_t index_at(const void *ids, int bits, int64_t i)
@@ -672,11 +673,9 @@ template <bool ENT, bool TAIL> __device__ __forceinline__ Stats warp_stats(Runni
     st.s = warp_sum(st.s);
     if (ENT) st.t = warp_sum(st.t);
     if (TAIL) {
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            const float om = __shfl_xor_sync(0xffffffffu, st.mi, d), os = __shfl_xor_sync(0xffffffffu, st.si, d);
-            join_sums(st.mi, st.si, om, os, c);
-        }
+        st.mi = warp_max(mi);
+        if (si != 0.f) st.si = si * ex2((mi - st.mi) * c);
+        st.si = warp_sum(st.si);
     }
     return st;
 }
@@ -883,10 +882,9 @@ template <class T> __device__ __forceinline__ void write_set_gradient(const Teac
 }
 
 // Entries that block `b` of a row's cluster contributes to its alternatives.
-template <class T> __device__ __forceinline__ int share_count(const Row<T> &row, int blocks, int b, int K)
+template <class T> __device__ __forceinline__ int share_count(const Row<T> &row, int per, int b, int K)
 {
-    const int G = row.granules(), per = (G + blocks - 1) / blocks;
-    const int g0 = min(G, b * per), g1 = min(G, g0 + per);
+    const int G = row.granules(), g0 = min(G, b * per), g1 = min(G, g0 + per);
     return max(0, min(K, min(row.n, row.first(g1)) - max(0, row.first(g0))));
 }
 
@@ -894,17 +892,25 @@ template <class T> __device__ __forceinline__ int share_count(const Row<T> &row,
 constexpr int kWarpRows = 4;         // rows, and warps, of a block
 constexpr int kWarpCandidates = 256;
 
+constexpr int kWarpListed = 160;     // granules: the best 128 and some equal ones
+
+struct WarpTop {
+    uint4 granule[kWarpListed];
+    uint64_t cand[kWarpCandidates + 1];  // the last takes what is too many
+    uint16_t index[kWarpListed];
+};
+
 template <class T, int U, int MODE> struct WarpShared {
     TeacherShared teacher[MODE >= kDistill ? kWarpRows : 1];
     uint32_t bitmap[MODE >= kDistill ? kWarpRows : 1][U * Elem<T>::kVec];
-    uint64_t cand[MODE == kLogprobsTop ? kWarpRows : 1][kWarpCandidates + 1];  // the last takes what is too many
-    uint32_t count[kWarpRows];
+    WarpTop top[MODE == kLogprobsTop ? kWarpRows : 1];
 };
 
-// The `want` best of a warp's granules, as keys in cand[0..n), n <= kWarpCandidates; returns n.  The want-th largest granule's
+// The `want` best of a warp's granules, as keys in sh.cand[0..n), n <= kWarpCandidates; returns n.  The want-th largest granule's
 // largest element (or lane's) bounds the want-th largest element from below.
-template <class T, int U> __device__ __forceinline__ int warp_top(uint4 *raw, const Row<T> &row, int G, int want, uint64_t *cand, uint32_t *count)
+template <class T, int U> __device__ __forceinline__ int warp_top(uint4 *raw, const Row<T> &row, int G, int want, WarpTop &sh)
 {
+    uint64_t *const cand = sh.cand;
     constexpr int VEC = Elem<T>::kVec;
     const int lane = threadIdx.x & 31;
     uint32_t keys[U];
@@ -931,22 +937,34 @@ template <class T, int U> __device__ __forceinline__ int warp_top(uint4 *raw, co
             if (static_cast<int>(__reduce_add_sync(0xffffffffu, n)) >= want) v = trial;
         }
     }
-    if (lane == 0) *count = 0;
-    __syncwarp();
+    // the granules that can hold one of the best are put side by side, so that the lanes share their elements
+    const uint32_t below = (1u << lane) - 1u;
+    int listed = 0, n = 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (v != 0 && keys[u] < v) continue;
-        const int e = row.first(u * 32 + lane);
-        float f[VEC];
-        Elem<T>::unpack(raw[u], f);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            if (ordered(f[i]) < v || e + i < 0 || e + i >= row.n) continue;
-            cand[min(atomicAdd(count, 1u), static_cast<uint32_t>(kWarpCandidates))] = rank_key(f[i], static_cast<uint32_t>(e + i));
-        }
+        const bool takes = u * 32 + lane < G && (v == 0 || keys[u] >= v);
+        const uint32_t mask = __ballot_sync(0xffffffffu, takes);
+        const int at = listed + __popc(mask & below);
+        if (takes && at < kWarpListed) sh.granule[at] = raw[u], sh.index[at] = static_cast<uint16_t>(u * 32 + lane);
+        listed += __popc(mask);
     }
     __syncwarp();
-    const int n = static_cast<int>(*count);
+    if (listed <= kWarpListed) {
+        for (int i = lane; i - lane < listed * VEC; i += 32) {
+            bool takes = false;
+            uint64_t key = 0;
+            if (i < listed * VEC) {
+                const float f = Elem<T>::to_float(reinterpret_cast<const T *>(sh.granule)[i]);
+                const int e = row.first(sh.index[i / VEC]) + i % VEC;
+                takes = ordered(f) >= v && e >= 0 && e < row.n;
+                key = rank_key(f, static_cast<uint32_t>(e));
+            }
+            const uint32_t mask = __ballot_sync(0xffffffffu, takes);
+            if (takes) cand[min(n + __popc(mask & below), kWarpCandidates)] = key;
+            n += __popc(mask);
+        }
+        __syncwarp();
+    }
     if (n <= kWarpCandidates && n >= want) return n;
     // many equal or many in few granules (or a bound from beyond the row's end, beside NaN alone): the want-th largest element itself, bit by bit, then those above it and the first
     // ones equal to it
@@ -1056,8 +1074,8 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
             if (lane == 0) a.loss[r] = loss;
         }
         if (MODE == kLogprobsTop) {
-            uint64_t *cand = sh.cand[warp];
-            const int n = warp_top<T, U>(raw, row, G, a.K, cand, &sh.count[warp]);
+            const uint64_t *cand = sh.top[warp].cand;
+            const int n = warp_top<T, U>(raw, row, G, a.K, sh.top[warp]);
             for (int i = lane; i < n; i += 32) {
                 const uint64_t key = cand[i];
                 int rank = 0;
@@ -1113,10 +1131,10 @@ template <int NT> struct RowShared {
 template <class T> struct Share {
     Row<T> row;
     int g0, g1;
-    __device__ __forceinline__ Share(const LossArgs &a, int64_t r, int blocks, int rank) : row(static_cast<const T *>(a.logits) + r * a.ld, a.V)
+    __device__ __forceinline__ Share(const LossArgs &a, int64_t r, int rank) : row(static_cast<const T *>(a.logits) + r * a.ld, a.V)
     {
-        const int G = row.granules(), per = (G + blocks - 1) / blocks;
-        g0 = min(G, rank * per), g1 = min(G, g0 + per);
+        const int G = row.granules();
+        g0 = min(G, rank * a.per_block), g1 = min(G, g0 + a.per_block);
     }
 };
 
@@ -1144,13 +1162,13 @@ __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_ker
     cg::cluster_group cluster = cg::this_cluster();
     const int C = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int stride = static_cast<int>(gridDim.x) / C;
+    const int stride = a.stride;
     int r = static_cast<int>(blockIdx.x) / C;
     // without the ring: a step ahead in registers
     uint4 next[U];
     const auto begin_row = [&](int64_t at) {  // a row's first granules; nothing beyond the last row
         if (at >= a.R) return;
-        const Share<T> s(a, at, C, rank);
+        const Share<T> s(a, at, rank);
         Step<T, NT, U>(s.row, s.g0, tid, s.g1).load(next);
     };
     // else the ring: `slots` of it in use, `slot` the present one, `turn` the direction
@@ -1164,7 +1182,7 @@ __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_ker
     const auto fetch = [&](const Row<T> &row, int g0, int g1, int step, int to) { Step<T, NT, U>(row, g0 + step * STEP, tid, g1).copy(ring + to * STEP); };
     const auto fetch_of = [&](int64_t at, int step, int to) {  // nothing beyond the last row
         if (at >= a.R) return;
-        const Share<T> s(a, at, C, rank);
+        const Share<T> s(a, at, rank);
         fetch(s.row, s.g0, s.g1, step, to);
     };
     // the present step's granules; the slots - 1 groups committed since are left on their way
@@ -1190,7 +1208,7 @@ __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_ker
     }
 
     for (; r < a.R; r = static_cast<int>(min(static_cast<int64_t>(r) + stride, a.R))) {
-        const Share<T> share(a, r, C, rank);
+        const Share<T> share(a, r, rank);
         const Row<T> &row = share.row;
         const int g0 = share.g0, g1 = share.g1;
         Running run = {neg_inf(), 0.f, 0.f};
@@ -1212,7 +1230,7 @@ __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_ker
 
         constexpr int kSegment = bitmap_words(NT) * 32 / Elem<T>::kVec;  // granules
         static_assert(kSegment % STEP == 0, "a segment is whole steps");
-        const int steps = !RING ? (g1 - g0 + STEP - 1) / STEP : a.steps;  // in the ring all rows take as many
+        const int steps = a.steps;
         int shift = 0;
         if (TOP)
             while (steps >> shift >= kGroupSteps) ++shift;
@@ -1231,7 +1249,7 @@ __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_ker
                 if (!RING) {
 #pragma unroll
                     for (int u = 0; u < U; ++u) cur[u] = next[u];
-                    if (base + STEP < g1) Step<T, NT, U>(row, base + STEP, tid, g1).load(next);
+                    if (step + 1 < steps) Step<T, NT, U>(row, base + STEP, tid, g1).load(next);
                     else if (!TOP) begin_row(static_cast<int64_t>(r) + stride);
                 } else {
                     take(cur);
@@ -1308,7 +1326,7 @@ __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_ker
             if (TOP && rank == 0) {
                 __syncthreads();
                 int n = 0;
-                for (int b = 0; b < C; ++b) n += share_count<T>(row, C, b, a.K);
+                for (int b = 0; b < C; ++b) n += share_count<T>(row, a.per_block, b, a.K);
                 select_top<NT>(top, n, a.K);
             }
         }
@@ -1353,7 +1371,7 @@ __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_ker
             __syncthreads();
             if (TEACHER) write_set_gradient<T>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, sh.grad, tid, NT);
             else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, sh.grad);
-        } else if (TOP || (!RING && g0 == g1)) {  // the search for the alternatives needs the registers
+        } else if (TOP) {  // the search for the alternatives needs the registers
             begin_row(static_cast<int64_t>(r) + stride);
         }
         __syncthreads();  // the next row overwrites shared memory
@@ -1424,7 +1442,8 @@ template <class T, int NT, int MODE, int GRAD> inline int launch_row(LossArgs a,
     if (a.R > kMostBlocks) return SPDY_ERR_UNSUPPORTED;  // rows are counted in 32 bits
     auto *kernel = loss_row_kernel<T, NT, kSteps, MODE, GRAD>;
     constexpr int kStep = NT * kSteps;
-    a.steps = static_cast<int>(((most_granules<T>(a) + cluster - 1) / cluster + kStep - 1) / kStep);
+    a.per_block = static_cast<int>((most_granules<T>(a) + cluster - 1) / cluster);
+    a.steps = (a.per_block - 1) / kStep + 1;
     size_t smem = 0;
     if (in_ring(MODE, GRAD)) {
         constexpr int H = ring_steps(MODE, GRAD, NT, kSteps);
@@ -1432,17 +1451,17 @@ template <class T, int NT, int MODE, int GRAD> inline int launch_row(LossArgs a,
         smem = fixed_shared(MODE, NT) + 16 * kStep * static_cast<size_t>(std::min(H, a.steps));
         if (smem > 40 * 1024) SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
     } else if (MODE == kLogprobsTop) {
-        const int64_t steps = (most_granules<T>(a) / cluster + NT * kSteps) / (NT * kSteps);
-        smem = sizeof(TopShared) + sizeof(uint32_t) * NT * static_cast<size_t>(steps < kGroupSteps ? steps + 1 : kGroupSteps + 1);
+        smem = sizeof(TopShared) + sizeof(uint32_t) * NT * static_cast<size_t>(std::min(a.steps, kGroupSteps));
         SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                           static_cast<int>(sizeof(TopShared) + sizeof(uint32_t) * NT * (kGroupSteps + 1))));
+                                           static_cast<int>(sizeof(TopShared) + sizeof(uint32_t) * NT * kGroupSteps)));
     }
     cudaLaunchConfig_t config = {};
     // Rows of few steps: blocks that stay, since the next row's first granules hide the start of each (16384 x 8192: 122 ->
     // 86 us).  Longer ones: a block per row, which the hardware deals out more evenly (4096 x 65536: 122 -> 111 us).
     const bool stay = most_granules<T>(a) <= 4096;
     const int64_t held = stay ? std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * (row_threads(MODE, GRAD) / NT) / cluster) : kMostBlocks / cluster;
-    config.gridDim = dim3(static_cast<unsigned>(std::min(a.R, held) * cluster));
+    a.stride = static_cast<int>(std::min(a.R, held));
+    config.gridDim = dim3(static_cast<unsigned>(a.stride * cluster));
     config.blockDim = dim3(NT);
     config.dynamicSmemBytes = smem;
     config.stream = stream;
