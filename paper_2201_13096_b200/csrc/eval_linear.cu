@@ -20,7 +20,7 @@ constexpr int BM = 128, BK = 64;           // rows of a block's tile; a slice of
 constexpr int kSlices = 2;                 // slices of a stage: a round of barriers costs about 400 cycles, the products of one slice 128 to 512
 constexpr int kEpilogueWarps = 16;         // four to a scheduler: with two, a tile's epilogue took longer than its products at K = 768
 constexpr int kThreads = 32 * (2 + kEpilogueWarps);
-constexpr int64_t kFewRows = 4;            // at most this many rows take the multiply-add kernel
+constexpr int64_t kFewRows = 8;            // at most this many rows take the multiply-add kernel (it and the tensor cores, us, K = N = 4096: 1 row 6.3, 18.5; 8 rows 16.5, 18.5; 16 rows 28.7, 14.4)
 
 struct LinearArgs {
     const void *x, *w, *bias, *residual;

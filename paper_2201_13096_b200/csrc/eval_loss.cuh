@@ -39,7 +39,6 @@ struct LossArgs {
     void *dlogits;
     int64_t lddl;
     int segments;            // blocks per row of the backward kernel
-    int stride;              // rows in flight of the long rows' kernel
     int per_block, steps;    // granules of a row that one of a cluster's blocks takes, and their steps (of the longest row)
 };
 
@@ -1027,7 +1026,7 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
     const int64_t r = static_cast<int64_t>(blockIdx.x) * kWarpRows + warp;
     if (r >= a.R) return;
     const Row<T> row(static_cast<const T *>(a.logits) + r * a.ld, a.V);
-    T *out = static_cast<T *>(a.dlogits) + static_cast<int64_t>(r) * a.lddl;
+    T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
     const int G = row.granules();
     TeacherShared &teacher = sh.teacher[TEACHER ? warp : 0];
     uint4 raw[U];
@@ -1127,22 +1126,13 @@ template <int NT> struct RowShared {
     uint32_t found;  // entries of top.best
 };
 
-// The granules of a row that a block of a cluster works on.
-template <class T> struct Share {
-    Row<T> row;
-    int g0, g1;
-    __device__ __forceinline__ Share(const LossArgs &a, int64_t r, int rank) : row(static_cast<const T *>(a.logits) + r * a.ld, a.V)
-    {
-        const int G = row.granules();
-        g0 = min(G, rank * a.per_block), g1 = min(G, g0 + a.per_block);
-    }
-};
-
-// A block's part of a row goes through a ring of H steps in shared memory, each thread's granules copied by itself (so that no
-// barrier is needed) H - 1 steps ahead.  With GRAD the row is then read again, backwards: its last H steps are still in the
-// ring, and the earlier ones in L2 as long as the rows in flight fit (see row_cluster).  As slots fall free the next row's
-// first steps are fetched into them, so that nothing pauses between rows; since they fall free in reverse, the ring's
-// direction turns with every row.  (With a step ahead in registers instead: 4096 x 65536 with gradient 246 us.)
+// A row belongs to one block, or to a cluster whose blocks divide its granules.  A block's part goes through a ring of H steps in shared
+// memory, each thread's granules copied by itself (so that no barrier is needed) up to H steps ahead.  With GRAD the row is then
+// read again, backwards: its last H steps are still in the ring, the earlier ones in L2 as long as the rows in flight fit (see
+// row_cluster).  A step ahead in registers instead took 246 us for 4096 x 65536 bf16 with gradient (now 214), and 136 for the
+// distillation's loss alone (now 111); but the plain log probabilities, with the fewest instructions, lose to the way through shared memory
+// (2048 x 131072: 99 us in registers, 105 through the ring), and where alternatives are looked for, these need the space.
+// One row per block: with blocks that stay and walk over rows 8192 x 30000 with gradient took 236 us, now 211.
 template <class T, int NT, int U, int MODE, int GRAD>
 __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_kernel(const LossArgs a)
 {
@@ -1162,29 +1152,17 @@ __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_ker
     cg::cluster_group cluster = cg::this_cluster();
     const int C = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int stride = a.stride;
-    int r = static_cast<int>(blockIdx.x) / C;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) / C;
+    const int steps = a.steps;  // all rows take as many, some of the last granules may lie behind the row
+    const Row<T> row(static_cast<const T *>(a.logits) + r * a.ld, a.V);
+    const int g0 = min(row.granules(), rank * a.per_block), g1 = min(row.granules(), g0 + a.per_block);
     // without the ring: a step ahead in registers
     uint4 next[U];
-    const auto begin_row = [&](int64_t at) {  // a row's first granules; nothing beyond the last row
-        if (at >= a.R) return;
-        const Share<T> s(a, at, rank);
-        Step<T, NT, U>(s.row, s.g0, tid, s.g1).load(next);
-    };
-    // else the ring: `slots` of it in use, `slot` the present one, `turn` the direction
+    // with it: `slots` of the ring in use, `slot` the present one
     uint4 *const ring = reinterpret_cast<uint4 *>(dynamic + fixed_shared(MODE, NT)) + tid;
-    const int slots = min(H, a.steps);
-    int slot = 0, turn = 1;
-    const auto advance = [&](int by) {
-        slot += by;
-        slot = slot < 0 ? slots - 1 : slot >= slots ? 0 : slot;
-    };
-    const auto fetch = [&](const Row<T> &row, int g0, int g1, int step, int to) { Step<T, NT, U>(row, g0 + step * STEP, tid, g1).copy(ring + to * STEP); };
-    const auto fetch_of = [&](int64_t at, int step, int to) {  // nothing beyond the last row
-        if (at >= a.R) return;
-        const Share<T> s(a, at, rank);
-        fetch(s.row, s.g0, s.g1, step, to);
-    };
+    const int slots = min(H, steps);
+    int slot = 0;
+    const auto fetch = [&](int step, int to) { Step<T, NT, U>(row, g0 + step * STEP, tid, g1).copy(ring + to * STEP); };
     // the present step's granules; the slots - 1 groups committed since are left on their way
     const auto take = [&](uint4 *to) {
         if (slots == 1) copies_wait<0>();
@@ -1195,188 +1173,174 @@ __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_ker
         for (int u = 0; u < U; ++u) to[u] = ring[slot * STEP + u * NT];
     };
     if (!RING) {
-        begin_row(r);
+        Step<T, NT, U>(row, g0, tid, g1).load(next);
     } else {
         for (int i = 0; i < slots; ++i) {
-            fetch_of(r, i, i);
+            fetch(i, i);
             copies_commit();
         }
     }
     if (TAIL) {
-        for (int i = tid; i < bitmap_words(NT); i += NT) bitmap[i] = 0;
+        const int words = min(bitmap_words(NT), (steps * STEP * Elem<T>::kVec + 31) / 32);
+        for (int i = tid; i < words; i += NT) bitmap[i] = 0;
+    }
+    Running run = {neg_inf(), 0.f, 0.f};
+    float mi = neg_inf(), si = 0.f;
+    int token = -1;
+    float token_x = 0.f;
+    uint32_t marked = 0;
+    typename std::conditional<TEACHER, Entries<T, NT>, NoEntries>::type entries(a, r, tid);
+    if constexpr (TEACHER) {
+        if (tid == 0) teacher.bad = 0, teacher.twice = !TAIL;
         __syncthreads();
+        entries.place_ids(teacher, a, tid);
+        __syncthreads();
+        if (warp == 0 && (rank == 0 || GRAD)) teacher_weights<TAIL>(teacher, a.K);
+    } else if (a.ids) {
+        token = token_at(a, r);
+        if (token >= 0 && token < a.V && tid == 0) token_x = Elem<T>::to_float(row.p[token]);
     }
 
-    for (; r < a.R; r = static_cast<int>(min(static_cast<int64_t>(r) + stride, a.R))) {
-        const Share<T> share(a, r, rank);
-        const Row<T> &row = share.row;
-        const int g0 = share.g0, g1 = share.g1;
-        Running run = {neg_inf(), 0.f, 0.f};
-        float mi = neg_inf(), si = 0.f;
-        int token = -1;
-        float token_x = 0.f;
-        uint32_t marked = 0;
-        typename std::conditional<TEACHER, Entries<T, NT>, NoEntries>::type entries(a, r, tid);
-        if constexpr (TEACHER) {
-            if (tid == 0) teacher.bad = 0, teacher.twice = !TAIL;
+    constexpr int kSegment = bitmap_words(NT) * 32 / Elem<T>::kVec;  // granules
+    static_assert(kSegment % STEP == 0, "a segment is whole steps");
+    int shift = 0;
+    if (TOP)
+        while (steps >> shift >= kGroupSteps) ++shift;
+    int step = 0;
+
+    const int end = g0 + steps * STEP;
+    for (int seg = g0; seg < end; seg = TAIL ? seg + kSegment : end) {
+        const int seg_end = TAIL ? min(end, seg + kSegment) : end;
+        if constexpr (TAIL) {
+            const uint32_t now = entries.mark(teacher, a.K, bitmap, row.first(seg), (min(seg_end, g1) - seg) * Elem<T>::kVec, tid);
+            marked |= now;
             __syncthreads();
-            entries.place_ids(teacher, a, tid);
+        }
+        for (int base = seg; base < seg_end; base += STEP, ++step) {
+            uint4 cur[U];
+            if (!RING) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) cur[u] = next[u];
+                if (step + 1 < steps) Step<T, NT, U>(row, base + STEP, tid, g1).load(next);
+            } else {
+                take(cur);
+            }
+            if (TAIL) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const uint32_t bits = bits_of<T>(bitmap, base + u * NT + tid - seg);
+                    if (bits) cur[u] = without<T>(cur[u], bits);
+                }
+            }
+            float all = Elem<T>::max_of(cur[0]);
+#pragma unroll
+            for (int u = 1; u < U; ++u) all = fmaxf(all, Elem<T>::max_of(cur[u]));
+            if (TOP) {
+                float *slot = groups + (step >> shift) * NT + tid;
+                const float largest = base + tid < g1 ? all : quiet_nan();
+                *slot = step & ((1 << shift) - 1) ? fmaxf(largest, *slot) : largest;
+            }
+            raise<ENT>(run, all, a.c);
+            accumulate<T, U, ENT>(cur, a.c, run);
+            if (RING) {
+                if (step + slots < steps) fetch(step + slots, slot);
+                copies_commit();
+                slot = slot + 1 == slots ? 0 : slot + 1;
+            }
+        }
+        if constexpr (TAIL) {
+            if (seg_end == end) break;
             __syncthreads();
-            if (warp == 0 && (rank == 0 || GRAD)) teacher_weights<TAIL>(teacher, a.K);
-        } else if (a.ids) {
-            token = token_at(a, r);
-            if (token >= 0 && token < a.V && tid == 0) token_x = Elem<T>::to_float(row.p[token]);
+            entries.unmark(teacher, a.K, bitmap, row.first(seg), (min(seg_end, g1) - seg) * Elem<T>::kVec, tid);
+            __syncthreads();
         }
+    }
 
-        constexpr int kSegment = bitmap_words(NT) * 32 / Elem<T>::kVec;  // granules
-        static_assert(kSegment % STEP == 0, "a segment is whole steps");
-        const int steps = a.steps;
-        int shift = 0;
-        if (TOP)
-            while (steps >> shift >= kGroupSteps) ++shift;
-        int step = 0;
-
-        const int end = g0 + steps * STEP;
-        for (int seg = g0; seg < end; seg = TAIL ? seg + kSegment : end) {
-            const int seg_end = TAIL ? min(end, seg + kSegment) : end;
-            if constexpr (TAIL) {
-                const uint32_t now = entries.mark(teacher, a.K, bitmap, row.first(seg), (min(seg_end, g1) - seg) * Elem<T>::kVec, tid);
-                marked |= now;
-                __syncthreads();
-            }
-            for (int base = seg; base < seg_end; base += STEP, ++step) {
-                uint4 cur[U];
-                if (!RING) {
+    if constexpr (TEACHER) {
+        entries.gather(teacher, a.K, row.p, rank == 0 ? 0 : row.first(g0), rank == 0 ? row.n : row.first(g1), tid);
+        if constexpr (TAIL) entries.add_marked(marked, a.c, mi, si);
+        entries.settle(teacher, a.K, tid);
+    }
+    Stats st = warp_stats<ENT, TAIL>(run, mi, si, a.c);
+    if (lane == 0) sh.part[warp] = st;
+    __syncthreads();
+    // The first warp alone joins the sums and works out what the row needs; a row's other threads only read the factors.
+    if (warp == 0) {
+        st = lane < NW ? sh.part[lane] : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
 #pragma unroll
-                    for (int u = 0; u < U; ++u) cur[u] = next[u];
-                    if (step + 1 < steps) Step<T, NT, U>(row, base + STEP, tid, g1).load(next);
-                    else if (!TOP) begin_row(static_cast<int64_t>(r) + stride);
-                } else {
-                    take(cur);
-                }
-                if (TAIL) {
+        for (int d = NW / 2; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
+        if (C > 1 && lane == 0) sh.pub = st;
+    }
+    if (TOP) {
+        const int e0 = max(0, row.first(g0)), e1 = min(row.n, row.first(g1));
+        const int want = max(0, min(a.K, e1 - e0));
+        if (want > 0) find_top<T, NT, U>(top, groups, (steps + (1 << shift) - 1) >> shift, shift, row, g0, g1, want);
+        if (tid == 0) sh.found = static_cast<uint32_t>(want);
+    }
+    if (C > 1) {
+        cluster.sync();
+        if (warp == 0 && (rank == 0 || GRAD)) {
+            st = lane < C ? *cluster.map_shared_rank(&sh.pub, lane) : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const uint32_t bits = bits_of<T>(bitmap, base + u * NT + tid - seg);
-                        if (bits) cur[u] = without<T>(cur[u], bits);
-                    }
-                }
-                float all = Elem<T>::max_of(cur[0]);
-#pragma unroll
-                for (int u = 1; u < U; ++u) all = fmaxf(all, Elem<T>::max_of(cur[u]));
-                if (TOP) {
-                    float *slot = groups + (step >> shift) * NT + tid;
-                    const float largest = base + tid < g1 ? all : quiet_nan();
-                    *slot = step & ((1 << shift) - 1) ? fmaxf(largest, *slot) : largest;
-                }
-                raise<ENT>(run, all, a.c);
-                accumulate<T, U, ENT>(cur, a.c, run);
-                if (RING) {
-                    if (step + slots < steps) fetch(row, g0, g1, step + slots, slot);
-                    else if (!GRAD) fetch_of(static_cast<int64_t>(r) + stride, step + slots - steps, slot);
-                    copies_commit();
-                    advance(turn);
-                }
-            }
-            if constexpr (TAIL) {
-                __syncthreads();
-                entries.unmark(teacher, a.K, bitmap, row.first(seg), (min(seg_end, g1) - seg) * Elem<T>::kVec, tid);
-                if (seg_end < end) __syncthreads();
+            for (int d = 4; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
+        }
+        if (TOP && rank == 0) {
+            int n = 0;  // the blocks' lists side by side
+            for (int b = 0; b < C; ++b) {
+                const int m = static_cast<int>(*cluster.map_shared_rank(&sh.found, b));
+                const TopShared *other = cluster.map_shared_rank(&top, b);
+                for (int i = tid; i < m; i += NT) top.cand[n + i] = other->best[i];
+                n += m;
             }
         }
-
-        if constexpr (TEACHER) {
-            entries.gather(teacher, a.K, row.p, rank == 0 ? 0 : row.first(g0), rank == 0 ? row.n : row.first(g1), tid);
-            if constexpr (TAIL) entries.add_marked(marked, a.c, mi, si);
-            entries.settle(teacher, a.K, tid);
+        cluster.barrier_arrive();  // its other half stands at the row's end: shared memory may be read until then
+        if (TOP && rank == 0) {
+            __syncthreads();
+            int n = 0;
+            for (int b = 0; b < C; ++b) n += share_count<T>(row, a.per_block, b, a.K);
+            select_top<NT>(top, n, a.K);
         }
-        Stats st = warp_stats<ENT, TAIL>(run, mi, si, a.c);
-        if (lane == 0) sh.part[warp] = st;
-        __syncthreads();
-        // The first warp alone joins the sums and works out what the row needs; a row's other threads only read the factors.
-        if (warp == 0) {
-            st = lane < NW ? sh.part[lane] : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
-#pragma unroll
-            for (int d = NW / 2; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-            if (C > 1 && lane == 0) sh.pub = st;
+    }
+    if (warp == 0 && (rank == 0 || GRAD)) {
+        const RowEnd e = row_end<TAIL>(st, a.c);
+        if (GRAD) {
+            const RowGrad k = TEACHER ? teacher_gradient<TAIL>(a, r, e, teacher) : token_gradient(a, r, st, e, token);
+            const Factors f(k, a.c);
+            if (lane == 0) sh.grad = k, sh.factors = f;
+        }
+        if (lane == 0) sh.end = e;
+        if (lane == 0 && rank == 0) write_sums<ENT, TAIL>(a, r, st, e, token, token_x);
+    }
+    if (GRAD || TEACHER || TOP) __syncthreads();
+    if (rank == 0) {
+        if (TEACHER && warp == NW - 1 && a.loss) {
+            const float loss = teacher_loss<TAIL>(teacher, sh.end, a.inv_t, a.K);
+            if (lane == 0) a.loss[r] = loss;
         }
         if (TOP) {
-            const int e0 = max(0, row.first(g0)), e1 = min(row.n, row.first(g1));
-            const int want = max(0, min(a.K, e1 - e0));
-            if (want > 0) find_top<T, NT, U>(top, groups, (steps + (1 << shift) - 1) >> shift, shift, row, g0, g1, want);
-            if (tid == 0) sh.found = static_cast<uint32_t>(want);
-        }
-        if (C > 1) {
-            cluster.sync();
-            if (warp == 0 && (rank == 0 || GRAD)) {
-                st = lane < C ? *cluster.map_shared_rank(&sh.pub, lane) : Stats{neg_inf(), 0.f, 0.f, neg_inf(), 0.f};
-#pragma unroll
-                for (int d = 4; d; d >>= 1) join_stats<ENT, TAIL>(st, shuffle_xor<ENT, TAIL>(st, d), a.c);
-            }
-            if (TOP && rank == 0) {
-                int n = 0;  // the blocks' lists side by side
-                for (int b = 0; b < C; ++b) {
-                    const int m = static_cast<int>(*cluster.map_shared_rank(&sh.found, b));
-                    const TopShared *other = cluster.map_shared_rank(&top, b);
-                    for (int i = tid; i < m; i += NT) top.cand[n + i] = other->best[i];
-                    n += m;
-                }
-            }
-            cluster.barrier_arrive();  // its other half stands at the row's end: shared memory may be read until then
-            if (TOP && rank == 0) {
-                __syncthreads();
-                int n = 0;
-                for (int b = 0; b < C; ++b) n += share_count<T>(row, a.per_block, b, a.K);
-                select_top<NT>(top, n, a.K);
+            for (int i = tid; i < a.K; i += NT) {
+                const uint64_t key = top.best[i];
+                a.top_ids[r * a.K + i] = static_cast<int32_t>(~static_cast<uint32_t>(key));
+                a.top_logprobs[r * a.K + i] = log_prob(unordered(static_cast<uint32_t>(key >> 32)), sh.end, a.inv_t);
             }
         }
-        if (warp == 0 && (rank == 0 || GRAD)) {
-            const RowEnd e = row_end<TAIL>(st, a.c);
-            if (GRAD) {
-                const RowGrad k = TEACHER ? teacher_gradient<TAIL>(a, r, e, teacher) : token_gradient(a, r, st, e, token);
-                const Factors f(k, a.c);
-                if (lane == 0) sh.grad = k, sh.factors = f;
-            }
-            if (lane == 0) sh.end = e;
-            if (lane == 0 && rank == 0) write_sums<ENT, TAIL>(a, r, st, e, token, token_x);
-        }
-        if (GRAD || TEACHER || TOP) __syncthreads();
-        if (rank == 0) {
-            if (TEACHER && warp == NW - 1 && a.loss) {
-                const float loss = teacher_loss<TAIL>(teacher, sh.end, a.inv_t, a.K);
-                if (lane == 0) a.loss[r] = loss;
-            }
-            if (TOP) {
-                for (int i = tid; i < a.K; i += NT) {
-                    const uint64_t key = top.best[i];
-                    a.top_ids[static_cast<int64_t>(r) * a.K + i] = static_cast<int32_t>(~static_cast<uint32_t>(key));
-                    a.top_logprobs[static_cast<int64_t>(r) * a.K + i] = log_prob(unordered(static_cast<uint32_t>(key >> 32)), sh.end, a.inv_t);
-                }
-            }
-        }
-        if (GRAD) {
-            T *out = static_cast<T *>(a.dlogits) + static_cast<int64_t>(r) * a.lddl;
-            const GradientWriter<T, ENT> writer(row, out, sh.factors);
-            for (step = steps - 1; step >= 0; --step) {
-                uint4 cur[U];
-                advance(-turn);
-                take(cur);
-                writer.write(Step<T, NT, U>(row, g0 + step * STEP, tid, g1), cur, a.c);
-                if (step >= slots) fetch(row, g0, g1, step - slots, slot);
-                else fetch_of(static_cast<int64_t>(r) + stride, slots - 1 - step, slot);
-                copies_commit();
-            }
-            advance(-turn);  // to where the next row's first step went
-            turn = -turn;
-            __syncthreads();
-            if (TEACHER) write_set_gradient<T>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, sh.grad, tid, NT);
-            else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, sh.grad);
-        } else if (TOP) {  // the search for the alternatives needs the registers
-            begin_row(static_cast<int64_t>(r) + stride);
-        }
-        __syncthreads();  // the next row overwrites shared memory
-        if (C > 1) cluster.barrier_wait();
     }
+    if (GRAD) {
+        T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
+        const GradientWriter<T, ENT> writer(row, out, sh.factors);
+        for (step = steps - 1; step >= 0; --step) {
+            uint4 cur[U];
+            slot = slot == 0 ? slots - 1 : slot - 1;
+            take(cur);
+            writer.write(Step<T, NT, U>(row, g0 + step * STEP, tid, g1), cur, a.c);
+            if (step >= slots) fetch(step - slots, slot);
+            copies_commit();
+        }
+        __syncthreads();
+        if (TEACHER) write_set_gradient<T>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, sh.grad, tid, NT);
+        else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, sh.grad);
+    }
+    if (C > 1) cluster.barrier_wait();
 }
 
 // Gradients from saved sums: one read and one write of the row, a.segments blocks per row.
@@ -1387,7 +1351,7 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
     const int64_t r = blockIdx.x / a.segments;
     const int part = static_cast<int>(blockIdx.x % a.segments);
     const Row<T> row(static_cast<const T *>(a.logits) + r * a.ld, a.V);
-    T *out = static_cast<T *>(a.dlogits) + static_cast<int64_t>(r) * a.lddl;
+    T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
     const int G = row.granules(), per = (G + a.segments - 1) / a.segments;
     const int g0 = min(G, part * per), g1 = min(G, g0 + per);
     RowGrad k;
@@ -1439,7 +1403,7 @@ constexpr int kSteps = 4;  // granules per thread and step of the long rows' ker
 
 template <class T, int NT, int MODE, int GRAD> inline int launch_row(LossArgs a, int cluster, cudaStream_t stream)
 {
-    if (a.R > kMostBlocks) return SPDY_ERR_UNSUPPORTED;  // rows are counted in 32 bits
+    if (a.R > kMostBlocks / cluster) return SPDY_ERR_UNSUPPORTED;
     auto *kernel = loss_row_kernel<T, NT, kSteps, MODE, GRAD>;
     constexpr int kStep = NT * kSteps;
     a.per_block = static_cast<int>((most_granules<T>(a) + cluster - 1) / cluster);
@@ -1456,12 +1420,7 @@ template <class T, int NT, int MODE, int GRAD> inline int launch_row(LossArgs a,
                                            static_cast<int>(sizeof(TopShared) + sizeof(uint32_t) * NT * kGroupSteps)));
     }
     cudaLaunchConfig_t config = {};
-    // Rows of few steps: blocks that stay, since the next row's first granules hide the start of each (16384 x 8192: 122 ->
-    // 86 us).  Longer ones: a block per row, which the hardware deals out more evenly (4096 x 65536: 122 -> 111 us).
-    const bool stay = most_granules<T>(a) <= 4096;
-    const int64_t held = stay ? std::max<int64_t>(1, static_cast<int64_t>(sm_count()) * (row_threads(MODE, GRAD) / NT) / cluster) : kMostBlocks / cluster;
-    a.stride = static_cast<int>(std::min(a.R, held));
-    config.gridDim = dim3(static_cast<unsigned>(a.stride * cluster));
+    config.gridDim = dim3(static_cast<unsigned>(a.R * cluster));
     config.blockDim = dim3(NT);
     config.dynamicSmemBytes = smem;
     config.stream = stream;
