@@ -1103,10 +1103,11 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
 // ------------------------------------------------------------------------------------------ long rows: a block or cluster each
 __host__ __device__ constexpr int bitmap_words(int threads) { return threads == 128 ? 512 : 4096; }  // ids of one segment of a row, a bit each: all of a row for 128 threads, 2^17 for 256
 constexpr int kGroupSteps = 32;     // groups a thread notes at most
-// Threads a multiprocessor holds of the long rows' kernels (by their registers: 80, or 96 where alternatives are looked for, with
-// blocks of 128 there: 2048 x 131072 with the best 20 took 133 us with 256 threads, 125 with 128).
+// Threads a multiprocessor holds of the long rows' kernels.  With the ring 64 registers a thread are enough (16384 x 8192 bf16,
+// distillation with gradient: 203 us with 768 threads, 186 with 1024); a step ahead in registers takes up to 80.  Blocks of 128
+// where alternatives are looked for: 2048 x 131072 with the best 20 took 133 us with 256 threads, 125 with 128.
 __host__ __device__ constexpr bool in_ring(int mode, int grad) { return mode >= kDistill || grad; }
-__host__ __device__ constexpr int row_threads(int mode, int grad) { return mode == kLogprobsTop ? 640 : in_ring(mode, grad) ? 1024 : 768; }
+__host__ __device__ constexpr int row_threads(int mode, int grad) { return in_ring(mode, grad) ? 1024 : 768; }
 
 // Shared memory of a block beside the ring, and the steps of U granules a thread that its ring holds: what fits the multiprocessor's share, at most 4.
 __host__ __device__ constexpr int fixed_shared(int mode, int threads) { return mode < kDistill ? 0 : static_cast<int>(sizeof(TeacherShared)) + (mode == kDistillTail ? 4 * bitmap_words(threads) : 0); }
