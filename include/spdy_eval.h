@@ -18,6 +18,7 @@
  *   - Sums, statistics and gradients of parameters are held in fp32; 16-bit outputs are rounded once.  No atomics on
  *     floating-point data: the same call on the same data gives the same bits.
  *   - Rows or columns may be zero in number: the call is a no-op (parameter gradients of no rows are written as 0).
+ *   - At most 2^31 - 1 blocks per launch: rows beyond that number (times up to 8 for long rows) are SPDY_ERR_UNSUPPORTED.
  * Errors: SPDY_ERR_INVALID_ARG (null pointer, size or stride out of range, unknown type, bad alignment),
  * SPDY_ERR_WORKSPACE_TOO_SMALL, SPDY_ERR_UNSUPPORTED (a size beyond a stated limit), SPDY_ERR_CUDA.
  */
@@ -45,7 +46,7 @@ typedef enum spdy_activation {
  *   fp32.  bias [N] of `bias_dtype` (`dtype` or SPDY_F32) and residual may be NULL.  y [M][N] is `out_dtype`: `dtype` or
  *   SPDY_F32.  y may be the residual itself (same pointer, stride and type).
  *   workspace: spdy_linear_workspace_bytes(...) bytes, 256-byte aligned, contents undefined afterwards; 0 bytes (and NULL)
- *   when the query says 0.  It holds copies of operands whose rows do not start on 16-byte boundaries, and partial sums.
+ *   when the query says 0.  It holds copies of operands whose rows do not start on 16-byte boundaries.
  *   K = 0 gives act(bias) + residual.
  */
 size_t spdy_linear_workspace_bytes(const void *x, int64_t ldx, const void *w, int64_t ldw, int dtype, int64_t M, int64_t N,
@@ -104,7 +105,9 @@ int spdy_token_logprobs(const void *logits, int64_t ld, int dtype, const void *t
  *   dlogits_v = (grad_logprob ([v = token] - p_v) - grad_entropy p_v (log p_v + entropy)) / T
  *   lse, entropy [R]: what the forward call gave (entropy may be NULL when grad_entropy is); grad_logprob, grad_entropy [R]
  *   fp32, either may be NULL (0).  dlogits [R][V] of `dtype`, may be the logits themselves.
- * spdy_token_logprobs_with_grad does the forward and this in one call (the row is read once where it fits on chip).
+ * spdy_token_logprobs_with_grad does the forward and this in one call: memory is read once as far as the rows in flight fit
+ * on chip.  It keeps the sums it works from, whereas an lse in fp32 cannot resolve rows whose logits are of the order of the
+ * type's lowest value (lse has their size, and an ulp of it is larger than any logit's difference): use it for such rows.
  */
 int spdy_token_logprobs_backward(const void *logits, int64_t ld, int dtype, const void *tokens, int index_bits, int64_t R,
                                  int64_t V, float temperature, const float *lse, const float *entropy,

@@ -198,12 +198,6 @@ template <class T> struct Row {
     // granules g0 .. g1 - 1 are all whole
     __device__ __forceinline__ bool inner(int g0, int g1) const { return first(g0) >= 0 && first(g1) <= n; }
     __device__ __forceinline__ bool same_lead(const T *q) const { return (reinterpret_cast<uintptr_t>(q) & 15) == (reinterpret_cast<uintptr_t>(p) & 15); }
-    // v, converted already, to granule g's elements of `q`, a row of as many elements that may start elsewhere; `same`: same_lead(q)
-    __device__ __forceinline__ void store(T *q, bool same, int g, uint4 v) const
-    {
-        if (same && whole(g)) store_stream(q + first(g), v);
-        else store_part(q, n, first(g), v);
-    }
 };
 
 // The granules base + t, base + t + NT, ... (U of them) of a row, for a block or warp of NT threads: where all are whole and

@@ -3,9 +3,15 @@
 // The product runs on the tensor cores (tcgen05, 16-bit operands, fp32 accumulators in TMEM); one thread feeds it with TMA
 // copies of 64-wide slices of x and w, one issues the matrix instructions, sixteen warps carry the finished tiles through the
 // epilogue while the next tile is multiplied.  Large products pair two multiprocessors on a tile of 256 rows (cta_group::2), so
-// that each reads half of the tile's slice of w: with one multiprocessor per 128 x 256 tile the slices took about 15 TB/s out of
-// L2, which was the limit (8192^3: 1.29 PFLOP/s).  Few rows (single tokens) are a matter of reading w once: a kernel of plain
-// multiply-adds streams it.
+// that each brings half of the tile's rows of w: per product the pair moves 2/3 of what two single 128 x 256 tiles would
+// (8192^3 with those: 1.29 PFLOP/s, with pairs 1.41 to 1.46, of 1.63 to 1.68 that the card's library product reaches).  Few rows (single tokens)
+// are a matter of reading w once: a kernel of plain multiply-adds streams it.
+//
+// Measured, bf16, us in a graph (and the floor: the larger of bytes at 6.56 TB/s and operations at 1.68 PFLOP/s):
+// 4096 x 768 x 3072 (rows, K, columns) with bias and gelu 28.5 (11.5), 16384 x 1024 x 4096 with gelu 111 (82),
+// 8192 x 4096 x 1024 with residual 60 (41), 8192^3 751 to 782 (656), 512 x 1024 x 4096 12.7, 128 x 768 x 3072 9.4, 16 x 4096 x 1024 10.6.
+// Bound: large products by the feed of the tensor cores (a stage's barriers and copies beside its products), the middle ones by whole rounds of tiles
+// and the last one's epilogue, the small ones by the fixed way through barriers, TMEM and the exchange of parts (about 8 us).
 #include <cuda.h>
 
 #include "eval_common.cuh"
@@ -75,7 +81,7 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr) { return static_cast<
 
 // One thread of a converged warp.  The loops below run on whole warps and elect the issuing thread around each TMA or tcgen05
 // instruction: these take their operands from uniform registers, and inside a branch on the lane number each operand cost a
-// trip there (690 cycles for four products of any size; 2.2 times less this way).
+// trip there (a pair's 64-wide slice of K: 731 cycles with the branch, 521 this way).
 __device__ __forceinline__ bool elect()
 {
     uint32_t chosen;
@@ -161,7 +167,7 @@ __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 // z Phi(z), Phi the normal distribution function.  Phi(z) - 1/2 = z Q(z^2) with Q a polynomial of degree 13 on |z| <= 5 (least
 // maximum of |z Q - (Phi - 1/2)| by reweighted Chebyshev fits, 3e-8; 1.1e-7 with fp32 arithmetic), in the variable
 // 2 z^2 / 25 - 1, where its coefficients' magnitudes sum to 0.4.  Beyond -5 (Phi below 2.9e-7) the result is -0, beyond 5 z.
-// The library's erff costs about 38 instructions here, this 12 in pairs.
+// No branch, and 15 of its operations go in pairs, where erff takes both sides of a branch.
 template <int N> __device__ __forceinline__ void gelu(float *f)
 {
     constexpr float kQ[14] = {-0.000253382081f, 0.000710501277f, -0.000840798195f, 0.00144300074f, -0.00358738378f, 0.00669657066f, -0.0106615145f, 0.0162687358f, -0.0234041531f, 0.0314699598f, -0.0404270627f, 0.0515184402f, -0.0702967867f, 0.141363814f};
@@ -610,8 +616,9 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
 }
 
 // ---------------------------------------------------------------------------------------------- few rows
-// A block of four warps per COLS columns of y (rows of w) and ROWS rows of x: w is read once, each warp a quarter of its K at a time,
-// x comes from L1; the warps' sums are added in their order.
+// A block of four warps per COLS columns of y (rows of w) and ROWS rows of x: w is read once per ROWS rows, each warp a quarter of its
+// K at a time, x comes from L1; the warps' sums are added in their order.  Bound by w's bytes and the launch: 1 x 768 x 3072 4.1 us,
+// 1 x 4096 x 4096 6.3 us (33.6 MB, 5.3 TB/s; w stays in L2 between such calls).
 template <class T, int ROWS, int COLS, int ACT, bool WIDE> __global__ void __launch_bounds__(128) linear_rows_kernel(const LinearArgs a)
 {
     __shared__ float part[4][ROWS * COLS];
@@ -676,7 +683,8 @@ template <class T, int ROWS, int COLS, int ACT, bool WIDE> __global__ void __lau
     else static_cast<T *>(a.y)[m * a.ldy + n] = Elem<T>::from_float(z);
 }
 
-// Copies of operands whose rows TMA cannot read (a row has to start on 16 bytes), with rows of ldto elements.
+// Copies of operands whose rows TMA cannot read (a row has to start on 16 bytes), with rows of ldto elements.  They cost one more
+// read and write of such an operand and a launch (333 x 1001 x 517, both unaligned: 14.8 us).
 struct Repack {
     const uint16_t *from[2];
     uint16_t *to[2];
