@@ -1446,7 +1446,8 @@ template <class T, int NT, int MODE, int GRAD> inline int launch_row(LossArgs a,
 
 // Blocks that share a row (a cluster, its sums exchanged through the blocks' shared memory): more when the rows alone would not
 // fill the device twice and every block still has a step of work; with a gradient also as many as keep what the ring does not hold
-// of the rows in flight within 64 MB of L2 (2048 x 131072 bf16, distillation with gradient: one block to a row 235 us, two 222,
+// of the rows in flight within 64 MB of L2.  No more than that to fill the last round of rows (two blocks to a row: 640 x 32768
+// f16, distillation with gradient 24.7 to 28.8 us).  (2048 x 131072 bf16, distillation with gradient: one block to a row 235 us, two 222,
 // four 248).
 template <class T, int NT, int MODE, int GRAD> inline int row_cluster(const LossArgs &a)
 {
