@@ -1479,18 +1479,22 @@ template <class T, int MODE, int GRAD> int rows(const LossArgs &a, cudaStream_t 
     else return launch_row<T, 256, MODE, GRAD>(a, row_cluster<T, 256, MODE, GRAD>(a), stream);
 }
 
-template <class T, int MODE> int backward(LossArgs a, cudaStream_t stream)
+template <class T, int MODE, int NT> int backward_rows(LossArgs a, int64_t G, cudaStream_t stream)
 {
-    constexpr int NT = 256, U = kSteps;
-    constexpr bool TEACHER = MODE >= kDistill, TAIL = MODE == kDistillTail;
-    const int64_t G = most_granules<T>(a);
-    if (G <= 128) return launch_warp<T, 4, MODE, kGradSaved>(a, stream);
-    if (G <= 256) return launch_warp<T, 8, MODE, kGradSaved>(a, stream);
+    constexpr int U = kSteps;
     a.segments = static_cast<int>((G + 2 * NT * U - 1) / (2 * NT * U));
     if (a.R * a.segments < 4 * sm_count()) a.segments = static_cast<int>((G + NT - 1) / NT);
     if (a.R * a.segments > kMostBlocks) return SPDY_ERR_UNSUPPORTED;
-    loss_backward_kernel<T, NT, U, TEACHER, TAIL><<<static_cast<unsigned>(a.R * a.segments), NT, 0, stream>>>(a);
+    loss_backward_kernel<T, NT, U, MODE >= kDistill, MODE == kDistillTail><<<static_cast<unsigned>(a.R * a.segments), NT, 0, stream>>>(a);
     return finish_launch();
+}
+template <class T, int MODE> int backward(const LossArgs &a, cudaStream_t stream)
+{
+    const int64_t G = most_granules<T>(a);
+    if (G <= 128) return launch_warp<T, 4, MODE, kGradSaved>(a, stream);
+    if (G <= 256) return launch_warp<T, 8, MODE, kGradSaved>(a, stream);
+    // as for the forward pass; 16384 x 2300 bf16: 48 us, with 256 threads 85
+    return G <= 1024 ? backward_rows<T, MODE, 128>(a, G, stream) : backward_rows<T, MODE, 256>(a, G, stream);
 }
 
 #define SPDY_EVAL_BY_TYPE(dtype, call)                                                          \
