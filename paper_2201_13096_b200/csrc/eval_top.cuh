@@ -42,7 +42,7 @@ struct TopShared {
     uint64_t list[kListed + 1];
     uint64_t best[SPDY_TOP_MAX];  // the result, descending
     uint64_t tau[32];
-    uint32_t count, count2;
+    uint32_t count, count2, entries;  // candidates, block_count's, the list's
     uint32_t hist[256];
     uint64_t prefix;
     uint32_t want;
@@ -165,17 +165,17 @@ __device__ __forceinline__ void find_top(TopShared &sh, const float *largest, in
     for (int i = 0; i < n_groups; ++i) lane_best = max(lane_best, group(i * NT + tid));
     const uint64_t mine = warp_nth_key(lane_best, static_cast<uint32_t>(lane), (want + NW - 1) / NW);
     if (lane == 0) sh.tau[warp] = mine >> 32;
-    if (tid == 0) sh.count = 0, sh.want = 0;
+    if (tid == 0) sh.count = sh.entries = sh.want = 0;
     __syncthreads();
     const uint32_t tau = max(1u, __reduce_min_sync(0xffffffffu, lane < NW ? static_cast<uint32_t>(sh.tau[lane]) : 0xffffffffu));
     const int total = n_groups * NT;
 #pragma unroll 4
     for (int i = tid; i < total; i += NT)
         if (group(i) >= tau) {
-            sh.list[min(atomicAdd(&sh.count, 1u), static_cast<uint32_t>(kListed))] = static_cast<uint64_t>(group(i)) << 32 | static_cast<uint32_t>(~i);
+            sh.list[min(atomicAdd(&sh.entries, 1u), static_cast<uint32_t>(kListed))] = static_cast<uint64_t>(group(i)) << 32 | static_cast<uint32_t>(~i);
         }
     __syncthreads();
-    int listed = static_cast<int>(sh.count);
+    int listed = static_cast<int>(sh.entries);  // decides which way all threads take: never written again
     const int each = U << shift;
     if (listed <= kListed && listed >= want) {
         // the common case: every group that can hold one of the best is listed, those equal to v among them
@@ -184,7 +184,7 @@ __device__ __forceinline__ void find_top(TopShared &sh, const float *largest, in
             int rank = 0;
 #pragma unroll 4
             for (int j = 0; j < listed; ++j) rank += sh.list[j] > k;
-            if (rank == want - 1) sh.want = static_cast<uint32_t>(k >> 32), sh.count = 0;
+            if (rank == want - 1) sh.want = static_cast<uint32_t>(k >> 32);
         }
         __syncthreads();
         const uint32_t least = sh.want;
