@@ -10,6 +10,7 @@
 #include <stdint.h>
 
 #include "../../include/spdy_eval.h"
+#include "eval_ranges.h"
 
 namespace spdy {
 void note_cuda_error(int err);  // spdy_api.cu: what spdy_last_cuda_error() reports

@@ -49,7 +49,7 @@ template <class P, int N> __device__ __forceinline__ void params(const void *p, 
     }
     const P *at = static_cast<const P *>(p) + e;
     constexpr int PV = Elem<P>::kVec;
-    if (N % PV == 0 && wide && e % PV == 0 && e + N <= D) {
+    if (in_granules(wide, e, N, D, PV)) {
 #pragma unroll
         for (int i = 0; i + PV <= N; i += PV) Elem<P>::unpack(*reinterpret_cast<const uint4 *>(at + i), f + i);
         return;

@@ -1,4 +1,5 @@
-"""Device code that the host compiler runs thread by thread (tests/native), in orders that a GPU seldom takes."""
+"""Device code that the host compiler runs (tests/native): index arithmetic, and a block thread by thread in orders that a GPU
+seldom takes."""
 import os
 import subprocess
 
@@ -16,3 +17,7 @@ def run_native(name, tmp_path, *flags):
 
 def test_search_for_the_largest_elements_in_any_order_of_warps(tmp_path):
     run_native("top_search", tmp_path)
+
+
+def test_granules_that_are_read_lie_inside(tmp_path):
+    run_native("ranges", tmp_path)
