@@ -105,9 +105,11 @@ int spdy_token_logprobs(const void *logits, int64_t ld, int dtype, const void *t
  *   dlogits_v = (grad_logprob ([v = token] - p_v) - grad_entropy p_v (log p_v + entropy)) / T
  *   lse, entropy [R]: what the forward call gave (entropy may be NULL when grad_entropy is); grad_logprob, grad_entropy [R]
  *   fp32, either may be NULL (0).  dlogits [R][V] of `dtype`, may be the logits themselves.
- * spdy_token_logprobs_with_grad does the forward and this in one call: memory is read once as far as the rows in flight fit
- * on chip.  It keeps the sums it works from, whereas an lse in fp32 cannot resolve rows whose logits are of the order of the
- * type's lowest value (lse has their size, and an ulp of it is larger than any logit's difference): use it for such rows.
+ * An lse in fp32 is off by up to 2^-24 of itself, and p by that much relative to p; in rows whose largest logit over T is
+ * beyond 1e7 (an all-masked row under a finite mask of -1e9) it no longer tells how many ids share the mass: p is then at most 1
+ * each.  spdy_token_logprobs_with_grad does the forward and this in one call: memory is read once as far as the rows in flight
+ * fit on chip, and the gradient comes from the sums themselves, whatever their size.  lse (and entropy with grad_entropy) are
+ * required there too.
  */
 int spdy_token_logprobs_backward(const void *logits, int64_t ld, int dtype, const void *tokens, int index_bits, int64_t R,
                                  int64_t V, float temperature, const float *lse, const float *entropy,

@@ -7,8 +7,8 @@
 // m need not be the maximum: any logit within a factor of 4 of it does (see raise), so that the sums are rescaled
 // rarely and nothing large cancels in the end.
 // An element costs one fused multiply-add x c - b with b = m c rounded; the rounding r = m c - b is the same for all elements and
-// is taken back once per thread (2^-r s, and t - r s for t).  Where m c is so large that x c could overflow (rows of the type's
-// lowest value) m is subtracted first instead.  Beside that one instruction to unpack, one for the special-function unit
+// is taken back once per thread (2^-r s, and t - r s for t).  From |m c| = 2^24 on, where r could reach 1 and soon what 2^r
+// overflows at (masks of -1e9, tiny temperatures), m is subtracted first instead.  Beside that one instruction to unpack, one for the special-function unit
 // (16 results a cycle and multiprocessor) and one or two to add up.
 //
 // Bound.  Rows are read once, and with a gradient written once.  At 4 to 6 bytes moved and 8 to 20 instructions issued per element the
@@ -115,15 +115,17 @@ template <bool ENT, bool TAIL> __device__ __forceinline__ Stats shuffle_xor(cons
     return b;
 }
 
-// What 2^(x c - base) is relative to: base = m c rounded, or 0 after subtracting sub = m where m c is too large for that.
+// What 2^(x c - base) is relative to: base = m c rounded (off by at most 1/2), or, far from 0, m c itself after subtracting
+// sub = m.  With m = -inf there is nothing yet: base is 0, and ids that are not allowed give 2^-inf.
+constexpr float kFar = 16777216.f;
 struct Reference {
     float base, sub;
     bool far;
     __device__ __forceinline__ Reference(float m, float c)
     {
-        base = m * c;
-        far = !(fabsf(base) < 1e35f);  // also m = -inf, +inf
-        sub = far && m != neg_inf() ? m : 0.f;
+        base = m == neg_inf() ? 0.f : m * c;
+        far = !(fabsf(base) < kFar);  // also m = +inf and NaN
+        sub = far ? m : 0.f;
         if (far) base = 0.f;
     }
 };
@@ -139,7 +141,8 @@ template <bool ENT> __device__ __forceinline__ void raise(Running &st, float top
     if (top > st.m && (top - st.m) * c > 2.f) {
         if (st.s != 0.f) {
             const Reference old(st.m, c), now(top, c);
-            const float d = max_nan(old.far || now.far ? (st.m - top) * c : old.base - now.base, -1000.f), f = ex2(d);
+            const float rise = old.far ? (now.far ? (st.m - top) * c : fmaf(st.m, c, -now.base)) : now.far ? -fmaf(top, c, -old.base) : old.base - now.base;
+            const float d = max_nan(rise, -1000.f), f = ex2(d);
             if (ENT) st.t = f * fmaf(st.s, d, st.t);
             st.s *= f;
         }
@@ -368,7 +371,12 @@ template <bool TAIL> __device__ __forceinline__ RowEnd row_end(const Stats &st, 
     e.m = m, e.s = s, e.ls = log2f(s), e.empty = s == 0.f;
     return e;
 }
-__device__ __forceinline__ float lse_of(float m, float ls, bool empty, float inv_t) { return empty ? neg_inf() : fmaf(m, inv_t, kLn2 * ls); }
+// Far from 0 the maximum over T is rounded by itself, as saved_exponent has it.
+__device__ __forceinline__ float lse_of(float m, float ls, bool empty, const LossArgs &a)
+{
+    if (empty) return neg_inf();
+    return fabsf(m * a.c) < kFar ? fmaf(m, a.inv_t, kLn2 * ls) : m / a.temperature + kLn2 * ls;
+}
 __device__ __forceinline__ float log_prob(float x, const RowEnd &e, float inv_t) { return e.empty ? neg_inf() : fmaf(x - e.m, inv_t, -kLn2 * e.ls); }
 
 // One warp: the loss of a row, in all lanes.
@@ -417,20 +425,36 @@ struct NoEntries {
 // One thread writes a row's sums; `token_x` is the given token's logit.
 template <bool ENT, bool TAIL> __device__ __forceinline__ void write_sums(const LossArgs &a, int64_t r, const Stats &st, const RowEnd &e, int token, float token_x)
 {
-    if (a.lse) a.lse[r] = lse_of(e.m, e.ls, e.empty, a.inv_t);
+    if (a.lse) a.lse[r] = lse_of(e.m, e.ls, e.empty, a);
     if (ENT) {
         if (a.entropy) a.entropy[r] = e.empty ? 0.f : kLn2 * (e.ls - st.t / st.s);
         if (a.logprob) a.logprob[r] = token < 0 ? 0.f : token >= a.V ? quiet_nan() : log_prob(token_x, e, a.inv_t);
     }
-    if (TAIL && a.rest) a.rest[r] = lse_of(e.mr, e.lsr, e.rest_empty, a.inv_t);
+    if (TAIL && a.rest) a.rest[r] = lse_of(e.mr, e.lsr, e.rest_empty, a);
 }
 
 // A row's gradient: 2^d (k0 + k1 d) with d = (x - m) c for every element, `hit` more for the given token, and for the
-// teacher's ids 2^((x - p_m) c) p_scale - q q_scale instead.
+// teacher's ids 2^((x - p_m) c) p_scale - q q_scale instead.  Where t (p_t) is not 0, m (p_m) is a saved lse far from 0 and t the
+// temperature.
 struct RowGrad {
-    float m, k0, k1, hit;
-    float p_m, p_scale, q_scale;
+    float m, t, k0, k1, hit;
+    float p_m, p_t, p_scale, q_scale;
 };
+
+// log2 p from a saved lse far from 0, whose last place may be worth more than the row's sum: the division rounds the largest
+// logit as lse_of rounded it, and p is at most 1.
+__device__ __forceinline__ float saved_exponent(float x, float lse, float temperature)
+{
+    const float d = (x / temperature - lse) * kLog2e;
+    return d > 0.f ? 0.f : d;
+}
+__device__ __forceinline__ float exponent(float x, float m, float t, float c) { return t != 0.f ? saved_exponent(x, m, t) : (x - m) * c; }
+__device__ __forceinline__ void saved_reference(float lse, float temperature, float &m, float &t)
+{
+    const bool near = fabsf(lse) < kFar * kLn2;
+    m = near ? lse * temperature : lse;
+    t = near ? 0.f : temperature;
+}
 
 template <bool TAIL> __device__ __forceinline__ RowGrad teacher_gradient(const LossArgs &a, int64_t r, const RowEnd &e, const TeacherShared &teacher)
 {
@@ -457,16 +481,17 @@ template <bool TAIL> __device__ __forceinline__ RowGrad teacher_gradient_saved(c
     RowGrad k = {};
     const float lse = a.in_lse[r], g = teacher.bad ? quiet_nan() : a.grad[r] * a.inv_t;
     const bool empty = lse == neg_inf();
-    k.p_m = empty ? 0.f : lse * a.temperature;
+    if (!empty) saved_reference(lse, a.temperature, k.p_m, k.p_t);
     if (TAIL) {
         const float rest = a.in_rest[r];
         const bool none = rest == neg_inf();
         const float mass = teacher.mass + (none ? 0.f : teacher.left);
-        k.m = none ? 0.f : rest * a.temperature;
-        k.k0 = none ? 0.f : g * fmaf(mass, expf(rest - lse), -teacher.left);
+        if (!none) saved_reference(rest, a.temperature, k.m, k.t);
+        const float over = rest - lse;  // at most 0 but for the two roundings
+        k.k0 = none ? 0.f : g * fmaf(mass, over > 0.f ? 1.f : expf(over), -teacher.left);
         k.p_scale = g * mass;
     } else {
-        k.m = k.p_m;
+        k.m = k.p_m, k.t = k.p_t;
         k.k0 = k.p_scale = g * teacher.mass;
     }
     k.q_scale = g;
@@ -506,19 +531,20 @@ __device__ __forceinline__ RowGrad token_gradient_saved(const LossArgs &a, int64
     if (lse == neg_inf()) {
         k.k0 = k.hit = gl != gl ? gl : 0.f;
     } else {
-        k.m = lse * a.temperature;
+        saved_reference(lse, a.temperature, k.m, k.t);
         k.k0 = -(a.grad_entropy ? fmaf(gh, a.in_entropy[r], gl) : gl);
         k.k1 = -gh * kLn2;
     }
     return k;
 }
 
-// A row's factors relative to Reference(m, c) (compare settle).
+// A row's factors relative to Reference(m, c) (compare settle), or to a saved lse.
 struct Factors {
     Reference ref;
-    float k0, k1;
-    __device__ __forceinline__ Factors(const RowGrad &k, float c) : ref(k.m, c)
+    float k0, k1, t;
+    __device__ __forceinline__ Factors(const RowGrad &k, float c) : ref(k.m, c), t(k.t)
     {
+        if (t != 0.f) ref.far = true, ref.base = 0.f, ref.sub = k.m;
         const float r = ref.far ? 0.f : fmaf(k.m, c, -ref.base), f = ex2(-r);
         k0 = f * fmaf(-r, k.k1, k.k0);
         k1 = f * k.k1;
@@ -552,13 +578,13 @@ template <class T, bool ENT> struct GradientWriter {
         return Elem<T>::pack(f);
     }
     // A granule's elements one by one, with a far reference.
-    static __device__ __noinline__ uint4 far_gradient(uint4 raw, float c, float sub, float k0, float k1)
+    static __device__ __noinline__ uint4 far_gradient(uint4 raw, float c, float sub, float t, float k0, float k1)
     {
         float f[Elem<T>::kVec];
         Elem<T>::unpack(raw, f);
 #pragma unroll
         for (int i = 0; i < Elem<T>::kVec; ++i) {
-            const float d = max_nan((f[i] - sub) * c, -1000.f);
+            const float d = max_nan(exponent(f[i], sub, t, c), -1000.f);
             f[i] = ex2(d) * fmaf(k1, d, k0);
         }
         return Elem<T>::pack(f);
@@ -569,7 +595,7 @@ template <class T, bool ENT> struct GradientWriter {
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (step.g + u * NT < step.limit)
-                    step.store_part_of(out, same, u, all.ref.far ? far_gradient(raw[u], c, all.ref.sub, k0, k1) : ENT && entropy ? gradient<true>(raw[u], c) : gradient<false>(raw[u], c));
+                    step.store_part_of(out, same, u, all.ref.far ? far_gradient(raw[u], c, all.ref.sub, all.t, k0, k1) : ENT && entropy ? gradient<true>(raw[u], c) : gradient<false>(raw[u], c));
             return;
         }
         T *to = out + step.row.first(step.g);
@@ -586,7 +612,7 @@ template <class T, bool ENT> struct GradientWriter {
 // The given token's element, written again by one thread behind a barrier.
 template <class T> __device__ __forceinline__ void write_token_gradient(T *out, int token, float x, float c, const RowGrad &k)
 {
-    const float d = max_nan((x - k.m) * c, -1000.f);
+    const float d = max_nan(exponent(x, k.m, k.t, c), -1000.f);
     out[token] = Elem<T>::from_float(fmaf(ex2(d), fmaf(k.k1, d, k.k0), k.hit));
 }
 
@@ -607,7 +633,7 @@ template <class T> __device__ __forceinline__ void write_set_gradient(const Teac
                     q += sh.q[i];
                 }
         }
-        if (first) out[id] = Elem<T>::from_float(ex2((sh.x[j] - k.p_m) * c) * k.p_scale - q * k.q_scale);
+        if (first) out[id] = Elem<T>::from_float(ex2(exponent(sh.x[j], k.p_m, k.p_t, c)) * k.p_scale - q * k.q_scale);
     }
 }
 

@@ -31,3 +31,163 @@ def test_layer_norm_of_rows_that_start_anywhere_with_fp32_parameters(dtype, R, D
     want, mean64, rstd64 = ref.layer_norm(x, w, b, 1e-5)
     y, mean, rstd = evaluate.layer_norm(x, w, b)
     ref.close(y, want, norm_bounds(x, w, b, want, rstd64), "y")
+
+
+# ------------------------------------------------------------------------------------------------ large finite logits
+
+def lowered(x):
+    """(64-bit logits less each row's largest, that largest): beside -1e30 not even 64 bits resolve the log of a count."""
+    top = ref.d64(x).amax(1, keepdim=True)
+    return ref.d64(x) - top, top[:, 0]
+
+
+def distill_lowered(x, ids, lps, temperature, tail, weight):
+    """``ref.distill`` for rows of distinct ids, some logits allowed outside them, every sum relative to its own largest term: (loss,
+    lse, rest, gradient, log p, p, the softmax outside the ids and its log)."""
+    low, top = lowered(x)
+    t, teacher, ids = low / temperature, ref.d64(lps), ids.cpu()
+    if not tail:
+        teacher = torch.log_softmax(teacher, 1)
+    q = teacher.exp()
+    inside = torch.zeros(t.shape, dtype=torch.bool).scatter(1, ids, True)
+    left = (1.0 - q.sum(1)).clamp(min=0.0) if tail else torch.zeros(len(t), dtype=torch.float64)
+    logp = torch.log_softmax(t, 1)
+    best_out = t.masked_fill(inside, -INF).amax(1, keepdim=True)
+    out_log = torch.log_softmax((t - best_out).masked_fill(inside, -INF), 1)
+    log_rest = torch.logsumexp((t - best_out).masked_fill(inside, -INF), 1) + best_out[:, 0] - torch.logsumexp(t, 1)  # of p outside
+    loss = (q * (teacher - logp.gather(1, ids))).sum(1) + torch.where(left > 0, left * (left.log() - log_rest), torch.zeros_like(left))
+    grad = (q.sum(1) + left)[:, None] * logp.exp() - left[:, None] * out_log.exp()
+    grad = grad.scatter_add(1, ids, -q) * ref.d64(weight)[:, None] / temperature
+    lse = torch.logsumexp(t, 1) + top / temperature
+    return loss, lse, lse + log_rest, grad, logp, logp.exp(), out_log.exp(), out_log
+
+
+def magnitudes(x, temperature):
+    """The magnitude of each row's largest logit over T, which lse is rounded relative to."""
+    return (ref.d64(x).amax(1) / temperature).abs()
+
+
+def masked_rows(V, dtype, value, seed):
+    """Seven rows of ordinary logits in which ``value`` marks ids that are not allowed: all of them, all but one, the first half, the
+    second half, 95 in 100, every second, none."""
+    x = rand(7, V, seed=seed, dtype=dtype, scale=3.0)
+    few = (torch.rand(V, generator=torch.Generator().manual_seed(seed)) < 0.95).cuda()
+    few[:2] = False  # some stay
+    x[0] = value
+    x[1, torch.arange(V, device="cuda") != V // 3] = value
+    x[2, :V // 2] = value
+    x[3, V // 2:] = value
+    x[4, few] = value
+    x[5, ::2] = value
+    return x
+
+
+def gradient_bound(p, logp, size):
+    """p is off by its exponent's rounding, which is relative to |log p| (and 2^-20 for the sum it is divided by); below 2^-126 it is 0."""
+    rel = 2.0 ** -20 * (14 + torch.where(p > 0, logp.abs(), torch.zeros_like(p)))
+    return (rel * p + 2.0 ** -126) * size
+
+
+LARGE = [(F32, -1e9), (F32, -5e9), (F32, -1e10), (F32, -3e10), (F32, -1e20), (F32, -1e30), (BF16, -1e9), (BF16, -1e10), (BF16, -3e10), (BF16, -1e30), (F16, -6e4)]
+
+
+@gpu
+@pytest.mark.parametrize("V", [40, 1500, 3000, 30000])
+@pytest.mark.parametrize("dtype,value", LARGE)
+def test_token_logprobs_where_large_finite_numbers_mask(dtype, value, V):
+    x = masked_rows(V, dtype, value, V)
+    tokens = torch.tensor([1, V // 3, V - 1, 0, 2, 1, -1], device="cuda")
+    gl, gh = rand(7, seed=5), rand(7, seed=6)
+    for temperature in (1.0, 0.7, 0.1):
+        low, top = lowered(x)
+        lp, h, lse = ref.token_logprobs(low, tokens, temperature)
+        lse = lse + top / temperature
+        err = 2.0 ** -21 * (magnitudes(x, temperature) + 14)
+        # beside the largest logit nothing of a row's size comes in: its sums are relative to it
+        flat = 2.0 ** -19 * 14 * torch.ones(7, dtype=torch.float64)
+        logp, p, _ = ref.softmax_row(low, temperature)
+        want = ref.token_logprobs_grad(low, tokens, gl, gh, temperature)
+        size = ref.d64(gl).abs()[:, None] + ref.d64(gh).abs()[:, None] * (2 * torch.where(p > 0, logp.abs(), torch.zeros_like(p)) + 14)
+        got = evaluate.token_logprobs(x, tokens, top_k=min(20, V), temperature=temperature)
+        both, grad = evaluate.token_logprobs_with_grad(x, tokens, gl, gh, temperature=temperature)
+        for values in (got, both):
+            ref.close(values.lse, lse, err, "lse")
+            ref.close(values.logprob, lp, flat + 2.0 ** -21 * lp.abs(), "logprob")
+            ref.close(values.entropy, h, flat, "entropy")
+        assert torch.equal(got.top_ids.cpu().long(), ref.top(x, min(20, V)))
+        ref.close(got.top_logprobs, logp.gather(1, got.top_ids.cpu().long()), 2.0 ** -19 * 14 + 2.0 ** -21 * logp.gather(1, got.top_ids.cpu().long()).abs(), "alternatives")
+        ref.close(grad, want, 2 * gradient_bound(p, logp, size) / temperature + 2.0 ** -21 * want.abs(), "with_grad")
+        back = evaluate.token_logprobs_backward(x, tokens, got.lse, got.entropy, gl, gh, temperature=temperature)
+        small = magnitudes(x, temperature) < 1e4
+        assert torch.equal(small, torch.arange(7) > 0)
+        e = 2 * (err[:, None] * p * size + gradient_bound(p, logp, size)) / temperature + 2.0 ** -21 * want.abs()
+        ref.close(back[1:], want[1:], e[1:], "backward")
+        # an lse of that size names no row's sum: p is between 0 and 1 all the same
+        most = (ref.d64(gl).abs() + ref.d64(gh).abs() * (14 + 1))[0] / temperature
+        assert bool(torch.isfinite(back[0]).all()) and float(back[0].float().abs().max()) <= float(most) * 1.01
+
+
+@gpu
+@pytest.mark.parametrize("tail", [True, False])
+@pytest.mark.parametrize("V", [40, 1500, 3000, 30000])
+@pytest.mark.parametrize("dtype,value", LARGE)
+def test_distillation_where_large_finite_numbers_mask(dtype, value, V, tail):
+    K = 6
+    x = masked_rows(V, dtype, value, V + 1)
+    g = torch.Generator().manual_seed(V)
+    scores = torch.where(ref.d64(x) < -1e4, torch.full((7, V), -20.0, dtype=torch.float64), ref.d64(x)) + torch.randn(7, V, generator=g, dtype=torch.float64)
+    best = torch.log_softmax(scores, 1).topk(K, dim=1)
+    ids, lps = best.indices.cuda(), best.values.float().cuda()
+    weight = rand(7, seed=8)
+    for temperature in (1.0, 0.7, 0.1):
+        loss, lse, rest, grad, logp, p, outside, out_log = distill_lowered(x, ids, lps, temperature, tail, weight)
+        err = 2.0 ** -21 * (magnitudes(x, temperature) + 14)
+        # log p within 2^-21 of itself and 2^-19 * 14, q and 1 - sum q within 2^-20, the latter times the tail's logarithm
+        bound = 2.0 ** -19 * 44 + 2.0 ** -20 * loss.abs() + 2.0 ** -20 * (torch.exp(ref.d64(lps)) * logp.gather(1, ids.cpu()).abs()).sum(1)
+        if tail:
+            bound = bound + 2.0 ** -20 * (rest - lse).abs()
+        got = evaluate.distill_loss(x, ids, lps, temperature=temperature, tail=tail)
+        both, once = evaluate.distill_loss_with_grad(x, ids, lps, weight, temperature=temperature, tail=tail)
+        inside = torch.zeros(7, V, dtype=torch.float64).scatter(1, ids.cpu(), 1.0)
+        e = gradient_bound(p, logp, 4.0) + 2.0 ** -20 * inside
+        if tail:
+            e = e + gradient_bound(outside, out_log, 4.0)
+        e = e * ref.d64(weight).abs()[:, None] / temperature + 2.0 ** -20 * grad.abs()
+        for values in (got, both):
+            ref.close(values.lse, lse, err, "lse")
+            ref.close(values.loss, loss, bound, "loss")
+            if tail:
+                ref.close(values.rest, rest, 2.0 ** -21 * (rest.abs() + 14), "rest")
+        ref.close(once, grad, e, "with_grad")
+        back = evaluate.distill_loss_backward(x, ids, lps, got.lse, got.rest, weight, temperature=temperature, tail=tail)
+        rows = [r for r in range(7) if lse[r].abs() < 1e4 and (not tail or rest[r].abs() < 1e4)]
+        assert len(rows) >= 4  # with few ids all of those allowed may be the teacher's
+        extra = 4 * (err[:, None] * (p + inside) + (2.0 ** -21 * (rest.abs() + 14))[:, None] * outside * float(tail)) * ref.d64(weight).abs()[:, None] / temperature
+        ref.close(back[rows], grad[rows], (e + extra)[rows], "backward")
+        assert bool(torch.isfinite(back).all()) and bool((back.float().abs().cpu() <= 3.01 * weight.abs().cpu()[:, None] / temperature).all())
+
+
+@gpu
+@pytest.mark.parametrize("V", [40, 1500, 3000, 30000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("temperature", [1e-9, 1e-6, 1e6])
+def test_token_logprobs_at_extreme_temperatures(dtype, V, temperature):
+    x = rand(5, V, seed=V, dtype=dtype, scale=3.0)
+    x[0] = 13.7
+    x[1, V // 2:] = 20.3
+    tokens = x.argmax(1)
+    gl, gh = rand(5, seed=5), rand(5, seed=6)
+    low, top = lowered(x)
+    lp, h, lse = ref.token_logprobs(low, tokens, temperature)
+    lse = lse + top / temperature
+    logp, p, _ = ref.softmax_row(low, temperature)
+    flat = 2.0 ** -19 * 14 * torch.ones(5, dtype=torch.float64)
+    got = evaluate.token_logprobs(x, tokens, temperature=temperature)
+    both, grad = evaluate.token_logprobs_with_grad(x, tokens, gl, gh, temperature=temperature)
+    for values in (got, both):
+        ref.close(values.lse, lse, 2.0 ** -21 * (magnitudes(x, temperature) + 14), "lse")
+        ref.close(values.logprob, lp, flat + 2.0 ** -21 * lp.abs(), "logprob")
+        ref.close(values.entropy, h, flat, "entropy")
+    want = ref.token_logprobs_grad(low, tokens, gl, gh, temperature)
+    size = ref.d64(gl).abs()[:, None] + ref.d64(gh).abs()[:, None] * (2 * torch.where(p > 0, logp.abs(), torch.zeros_like(p)) + 14)
+    ref.close(grad, want, 2 * gradient_bound(p, logp, size) / temperature + 2.0 ** -21 * want.abs(), "with_grad")
