@@ -29,11 +29,18 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// max(a, b) that keeps NaN (fmaxf drops it).
+// max(a, b) and min(a, b) that keep NaN (fmaxf and fminf drop it).
 __device__ __forceinline__ float max_nan(float a, float b)
 {
     float y;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
+__device__ __forceinline__ float min_nan(float a, float b)
+{
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
     return y;
 }
 

@@ -14,7 +14,7 @@ LossArgs base_args(const void *logits, int64_t ld, const void *ids, int bits, co
 {
     LossArgs a = {};
     a.logits = logits, a.ld = ld, a.R = R, a.V = V, a.K = K;
-    a.c = kLog2e / temperature, a.inv_t = 1.f / temperature, a.temperature = temperature;
+    a.c = kLog2e / temperature, a.inv_t = 1.f / temperature, a.temperature = temperature, a.lower = temperature == 1.f ? 0.f : 1.8e-7f;
     a.ids = ids, a.index_bits = bits, a.top_lp = top_lp;
     return a;
 }

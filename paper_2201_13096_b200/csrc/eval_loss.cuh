@@ -34,6 +34,7 @@ struct LossArgs {
     const void *logits;
     int64_t ld, R, V;
     float c, inv_t, temperature;  // c = log2(e) / T
+    float lower;             // saved_reference
     const void *ids;         // tokens [R] or the teacher's ids [R][K]
     int index_bits;
     int32_t K;               // top_k or the teacher's entries
@@ -371,12 +372,7 @@ template <bool TAIL> __device__ __forceinline__ RowEnd row_end(const Stats &st, 
     e.m = m, e.s = s, e.ls = log2f(s), e.empty = s == 0.f;
     return e;
 }
-// Far from 0 the maximum over T is rounded by itself, as saved_exponent has it.
-__device__ __forceinline__ float lse_of(float m, float ls, bool empty, const LossArgs &a)
-{
-    if (empty) return neg_inf();
-    return fabsf(m * a.c) < kFar ? fmaf(m, a.inv_t, kLn2 * ls) : m / a.temperature + kLn2 * ls;
-}
+__device__ __forceinline__ float lse_of(float m, float ls, bool empty, float inv_t) { return empty ? neg_inf() : fmaf(m, inv_t, kLn2 * ls); }
 __device__ __forceinline__ float log_prob(float x, const RowEnd &e, float inv_t) { return e.empty ? neg_inf() : fmaf(x - e.m, inv_t, -kLn2 * e.ls); }
 
 // One warp: the loss of a row, in all lanes.
@@ -425,36 +421,20 @@ struct NoEntries {
 // One thread writes a row's sums; `token_x` is the given token's logit.
 template <bool ENT, bool TAIL> __device__ __forceinline__ void write_sums(const LossArgs &a, int64_t r, const Stats &st, const RowEnd &e, int token, float token_x)
 {
-    if (a.lse) a.lse[r] = lse_of(e.m, e.ls, e.empty, a);
+    if (a.lse) a.lse[r] = lse_of(e.m, e.ls, e.empty, a.inv_t);
     if (ENT) {
         if (a.entropy) a.entropy[r] = e.empty ? 0.f : kLn2 * (e.ls - st.t / st.s);
         if (a.logprob) a.logprob[r] = token < 0 ? 0.f : token >= a.V ? quiet_nan() : log_prob(token_x, e, a.inv_t);
     }
-    if (TAIL && a.rest) a.rest[r] = lse_of(e.mr, e.lsr, e.rest_empty, a);
+    if (TAIL && a.rest) a.rest[r] = lse_of(e.mr, e.lsr, e.rest_empty, a.inv_t);
 }
 
 // A row's gradient: 2^d (k0 + k1 d) with d = (x - m) c for every element, `hit` more for the given token, and for the
-// teacher's ids 2^((x - p_m) c) p_scale - q q_scale instead.  Where t (p_t) is not 0, m (p_m) is a saved lse far from 0 and t the
-// temperature.
+// teacher's ids 2^((x - p_m) c) p_scale - q q_scale instead.
 struct RowGrad {
-    float m, t, k0, k1, hit;
-    float p_m, p_t, p_scale, q_scale;
+    float m, k0, k1, hit;
+    float p_m, p_scale, q_scale;
 };
-
-// log2 p from a saved lse far from 0, whose last place may be worth more than the row's sum: the division rounds the largest
-// logit as lse_of rounded it, and p is at most 1.
-__device__ __forceinline__ float saved_exponent(float x, float lse, float temperature)
-{
-    const float d = (x / temperature - lse) * kLog2e;
-    return d > 0.f ? 0.f : d;
-}
-__device__ __forceinline__ float exponent(float x, float m, float t, float c) { return t != 0.f ? saved_exponent(x, m, t) : (x - m) * c; }
-__device__ __forceinline__ void saved_reference(float lse, float temperature, float &m, float &t)
-{
-    const bool near = fabsf(lse) < kFar * kLn2;
-    m = near ? lse * temperature : lse;
-    t = near ? 0.f : temperature;
-}
 
 template <bool TAIL> __device__ __forceinline__ RowGrad teacher_gradient(const LossArgs &a, int64_t r, const RowEnd &e, const TeacherShared &teacher)
 {
@@ -476,22 +456,35 @@ template <bool TAIL> __device__ __forceinline__ RowGrad teacher_gradient(const L
     return k;
 }
 
+// The logit that a saved lse stands for.  Far from 0 the last place of lse may be worth more than the row's whole sum: there it is
+// lowered by the roundings on the way (the quotient's, the sum's, the product's), so that the row's largest logits are not below
+// it, and p is counted at most 1 (exponent).
+__device__ __forceinline__ float saved_reference(const LossArgs &a, float lse)
+{
+    const float m = lse * a.temperature;
+    return max_nan(fmaf(-fabsf(m), fabsf(m * a.c) < kFar ? 0.f : a.lower, m), -3.4028235e38f);
+}
+template <bool SAVED> __device__ __forceinline__ float exponent(float x, float m, float c)
+{
+    return SAVED ? min_nan((x - m) * c, 0.f) : (x - m) * c;
+}
+
 template <bool TAIL> __device__ __forceinline__ RowGrad teacher_gradient_saved(const LossArgs &a, int64_t r, const TeacherShared &teacher)
 {
     RowGrad k = {};
     const float lse = a.in_lse[r], g = teacher.bad ? quiet_nan() : a.grad[r] * a.inv_t;
     const bool empty = lse == neg_inf();
-    if (!empty) saved_reference(lse, a.temperature, k.p_m, k.p_t);
+    k.p_m = empty ? 0.f : saved_reference(a, lse);
     if (TAIL) {
         const float rest = a.in_rest[r];
         const bool none = rest == neg_inf();
         const float mass = teacher.mass + (none ? 0.f : teacher.left);
-        if (!none) saved_reference(rest, a.temperature, k.m, k.t);
-        const float over = rest - lse;  // at most 0 but for the two roundings
+        k.m = none ? 0.f : saved_reference(a, rest);
+        const float over = rest - lse;  // above 0 by its roundings alone
         k.k0 = none ? 0.f : g * fmaf(mass, over > 0.f ? 1.f : expf(over), -teacher.left);
         k.p_scale = g * mass;
     } else {
-        k.m = k.p_m, k.t = k.p_t;
+        k.m = k.p_m;
         k.k0 = k.p_scale = g * teacher.mass;
     }
     k.q_scale = g;
@@ -531,20 +524,19 @@ __device__ __forceinline__ RowGrad token_gradient_saved(const LossArgs &a, int64
     if (lse == neg_inf()) {
         k.k0 = k.hit = gl != gl ? gl : 0.f;
     } else {
-        saved_reference(lse, a.temperature, k.m, k.t);
+        k.m = saved_reference(a, lse);
         k.k0 = -(a.grad_entropy ? fmaf(gh, a.in_entropy[r], gl) : gl);
         k.k1 = -gh * kLn2;
     }
     return k;
 }
 
-// A row's factors relative to Reference(m, c) (compare settle), or to a saved lse.
+// A row's factors relative to Reference(m, c) (compare settle).
 struct Factors {
     Reference ref;
-    float k0, k1, t;
-    __device__ __forceinline__ Factors(const RowGrad &k, float c) : ref(k.m, c), t(k.t)
+    float k0, k1;
+    __device__ __forceinline__ Factors(const RowGrad &k, float c) : ref(k.m, c)
     {
-        if (t != 0.f) ref.far = true, ref.base = 0.f, ref.sub = k.m;
         const float r = ref.far ? 0.f : fmaf(k.m, c, -ref.base), f = ex2(-r);
         k0 = f * fmaf(-r, k.k1, k.k0);
         k1 = f * k.k1;
@@ -552,7 +544,7 @@ struct Factors {
 };
 
 // How a row's elements are turned into their gradients and written.
-template <class T, bool ENT> struct GradientWriter {
+template <class T, bool ENT, bool SAVED> struct GradientWriter {
     T *out;
     bool same, entropy;
     float base, k0, k1;
@@ -578,13 +570,13 @@ template <class T, bool ENT> struct GradientWriter {
         return Elem<T>::pack(f);
     }
     // A granule's elements one by one, with a far reference.
-    static __device__ __noinline__ uint4 far_gradient(uint4 raw, float c, float sub, float t, float k0, float k1)
+    static __device__ __noinline__ uint4 far_gradient(uint4 raw, float c, float sub, float k0, float k1)
     {
         float f[Elem<T>::kVec];
         Elem<T>::unpack(raw, f);
 #pragma unroll
         for (int i = 0; i < Elem<T>::kVec; ++i) {
-            const float d = max_nan(exponent(f[i], sub, t, c), -1000.f);
+            const float d = max_nan(exponent<SAVED>(f[i], sub, c), -1000.f);
             f[i] = ex2(d) * fmaf(k1, d, k0);
         }
         return Elem<T>::pack(f);
@@ -595,7 +587,7 @@ template <class T, bool ENT> struct GradientWriter {
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (step.g + u * NT < step.limit)
-                    step.store_part_of(out, same, u, all.ref.far ? far_gradient(raw[u], c, all.ref.sub, all.t, k0, k1) : ENT && entropy ? gradient<true>(raw[u], c) : gradient<false>(raw[u], c));
+                    step.store_part_of(out, same, u, all.ref.far ? far_gradient(raw[u], c, all.ref.sub, k0, k1) : ENT && entropy ? gradient<true>(raw[u], c) : gradient<false>(raw[u], c));
             return;
         }
         T *to = out + step.row.first(step.g);
@@ -610,14 +602,14 @@ template <class T, bool ENT> struct GradientWriter {
 };
 
 // The given token's element, written again by one thread behind a barrier.
-template <class T> __device__ __forceinline__ void write_token_gradient(T *out, int token, float x, float c, const RowGrad &k)
+template <class T, bool SAVED> __device__ __forceinline__ void write_token_gradient(T *out, int token, float x, float c, const RowGrad &k)
 {
-    const float d = max_nan(exponent(x, k.m, k.t, c), -1000.f);
+    const float d = max_nan(exponent<SAVED>(x, k.m, c), -1000.f);
     out[token] = Elem<T>::from_float(fmaf(ex2(d), fmaf(k.k1, d, k.k0), k.hit));
 }
 
 // The teacher's ids that lie in [e0, e1), written again behind a barrier by the thread of the id's first entry, by `n` threads.
-template <class T> __device__ __forceinline__ void write_set_gradient(const TeacherShared &sh, int K, T *out, int e0, int e1, float c, const RowGrad &k, int t, int n)
+template <class T, bool SAVED> __device__ __forceinline__ void write_set_gradient(const TeacherShared &sh, int K, T *out, int e0, int e1, float c, const RowGrad &k, int t, int n)
 {
     for (int j = t; j < K; j += n) {
         const int32_t id = sh.id[j];
@@ -633,7 +625,7 @@ template <class T> __device__ __forceinline__ void write_set_gradient(const Teac
                     q += sh.q[i];
                 }
         }
-        if (first) out[id] = Elem<T>::from_float(ex2(exponent(sh.x[j], k.p_m, k.p_t, c)) * k.p_scale - q * k.q_scale);
+        if (first) out[id] = Elem<T>::from_float(ex2(exponent<SAVED>(sh.x[j], k.p_m, c)) * k.p_scale - q * k.q_scale);
     }
 }
 
@@ -852,10 +844,11 @@ template <class T, int U, int MODE, int GRAD> __global__ void __launch_bounds__(
 #pragma unroll
     for (int u = 0; u < U; ++u) asm volatile("" : "+r"(raw[u].x), "+r"(raw[u].y), "+r"(raw[u].z), "+r"(raw[u].w));
     const Factors factors(k, a.c);
-    GradientWriter<T, ENT>(row, out, factors).write(step, raw, a.c);
+    constexpr bool SAVED = GRAD == kGradSaved;
+    GradientWriter<T, ENT, SAVED>(row, out, factors).write(step, raw, a.c);
     __syncwarp();
-    if (TEACHER) write_set_gradient<T>(teacher, a.K, out, 0, row.n, a.c, k, lane, 32);
-    else if (lane == 0 && token >= 0 && token < a.V) write_token_gradient<T>(out, token, token_x, a.c, k);
+    if (TEACHER) write_set_gradient<T, SAVED>(teacher, a.K, out, 0, row.n, a.c, k, lane, 32);
+    else if (lane == 0 && token >= 0 && token < a.V) write_token_gradient<T, SAVED>(out, token, token_x, a.c, k);
 }
 
 // ------------------------------------------------------------------------------------------ long rows: a block or cluster each
@@ -1086,7 +1079,7 @@ __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_ker
     }
     if (GRAD) {
         T *out = static_cast<T *>(a.dlogits) + r * a.lddl;
-        const GradientWriter<T, ENT> writer(row, out, sh.factors);
+        const GradientWriter<T, ENT, false> writer(row, out, sh.factors);
         for (step = steps - 1; step >= 0; --step) {
             uint4 cur[U];
             slot = slot == 0 ? slots - 1 : slot - 1;
@@ -1096,8 +1089,8 @@ __global__ void __launch_bounds__(NT, row_threads(MODE, GRAD) / NT) loss_row_ker
             copies_commit();
         }
         __syncthreads();
-        if (TEACHER) write_set_gradient<T>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, sh.grad, tid, NT);
-        else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T>(out, token, token_x, a.c, sh.grad);
+        if (TEACHER) write_set_gradient<T, false>(teacher, a.K, out, row.first(g0), row.first(g1), a.c, sh.grad, tid, NT);
+        else if (tid == 0 && token >= 0 && token < a.V && token >= row.first(g0) && token < row.first(g1)) write_token_gradient<T, false>(out, token, token_x, a.c, sh.grad);
     }
     if (C > 1) cluster.barrier_wait();
 }
@@ -1136,7 +1129,7 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
         __syncthreads();  // read before it is overwritten in place
     }
     const Factors factors(k, a.c);
-    const GradientWriter<T, !TEACHER> writer(row, out, factors);
+    const GradientWriter<T, !TEACHER, true> writer(row, out, factors);
     for (int base = g0; base < g1; base += NT * U) {
         uint4 cur[U];
 #pragma unroll
@@ -1146,8 +1139,8 @@ __global__ void __launch_bounds__(NT) loss_backward_kernel(const LossArgs a)
     }
     if constexpr (TEACHER) entries.settle(shared, a.K, threadIdx.x);
     __syncthreads();
-    if constexpr (TEACHER) write_set_gradient<T>(shared, a.K, out, row.first(g0), row.first(g1), a.c, k, threadIdx.x, NT);
-    else if (threadIdx.x == 0 && token >= 0) write_token_gradient<T>(out, token, token_x, a.c, k);
+    if constexpr (TEACHER) write_set_gradient<T, true>(shared, a.K, out, row.first(g0), row.first(g1), a.c, k, threadIdx.x, NT);
+    else if (threadIdx.x == 0 && token >= 0) write_token_gradient<T, true>(out, token, token_x, a.c, k);
 }
 
 // ------------------------------------------------------------------------------------------ launches

@@ -28,7 +28,7 @@ LossArgs base_args(const void *logits, int64_t ld, const void *tokens, int bits,
 {
     LossArgs a = {};
     a.logits = logits, a.ld = ld, a.R = R, a.V = V;
-    a.c = kLog2e / temperature, a.inv_t = 1.f / temperature, a.temperature = temperature;
+    a.c = kLog2e / temperature, a.inv_t = 1.f / temperature, a.temperature = temperature, a.lower = temperature == 1.f ? 0.f : 1.8e-7f;
     a.ids = tokens, a.index_bits = bits;
     return a;
 }
