@@ -36,8 +36,8 @@ typedef enum spdy_dtype { SPDY_F32 = 0, SPDY_BF16 = 1, SPDY_F16 = 2 } spdy_dtype
 typedef enum spdy_activation {
     SPDY_ACT_NONE = 0,
     SPDY_ACT_RELU = 1, /* max(z, 0); NaN stays NaN */
-    SPDY_ACT_GELU = 2, /* z (1 + erf(z / sqrt 2)) / 2 */
-    SPDY_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+    SPDY_ACT_GELU = 2, /* z (1 + erf(z / sqrt 2)) / 2, within 2^-20 (1 + z^2 / 16) of itself, the negative tail too; 0 at -inf */
+    SPDY_ACT_SILU = 3  /* z / (1 + exp(-z)), within 2^-20 (1 + |z| / 8) of itself; 0 at -inf */
 } spdy_activation;
 
 /*

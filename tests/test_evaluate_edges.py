@@ -191,3 +191,24 @@ def test_token_logprobs_at_extreme_temperatures(dtype, V, temperature):
     want = ref.token_logprobs_grad(low, tokens, gl, gh, temperature)
     size = ref.d64(gl).abs()[:, None] + ref.d64(gh).abs()[:, None] * (2 * torch.where(p > 0, logp.abs(), torch.zeros_like(p)) + 14)
     ref.close(grad, want, 2 * gradient_bound(p, logp, size) / temperature + 2.0 ** -21 * want.abs(), "with_grad")
+
+
+# ------------------------------------------------------------------------------------------------ activations
+
+@gpu
+@pytest.mark.parametrize("M", [1, 16, 300])
+@pytest.mark.parametrize("kind", ["gelu", "silu"])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_activations_are_accurate_relative_to_themselves(dtype, kind, M):
+    """Down to where they underflow: a value formed from 1 + erf would lose the negative tail."""
+    z = torch.cat([torch.linspace(-13, 13, 4001), torch.linspace(-6, -2, 2001), rand(2000, seed=3).cpu(), torch.tensor([0.0, -0.0, 1e-6, -1e-6, 40.0, 1e4, -60.0, -1e3, INF])]).cuda()
+    x, w = torch.zeros(M, 16, dtype=dtype, device="cuda"), torch.zeros(z.numel(), 16, dtype=dtype, device="cuda")
+    zd = ref.d64(z)
+    want = 0.5 * zd * torch.special.erfc(-zd / math.sqrt(2.0)) if kind == "gelu" else zd * torch.sigmoid(zd)
+    # the exponential's argument, z^2 log2(e) / 2 or z log2(e), is rounded to 24 bits; some ten roundings beside it
+    err = 2.0 ** -20 * want.abs() * (1 + (zd ** 2 / 16 if kind == "gelu" else zd.abs() / 8).clamp(max=100.0))
+    err[zd == INF] = 0.0
+    got = evaluate.linear(x, w, bias=z, activation=kind, out_dtype=F32)
+    ref.close(got, want.expand(M, -1), err.expand(M, -1), "fp32")
+    ref.close(evaluate.linear(x, w, bias=z, activation=kind), want.expand(M, -1), err.expand(M, -1), "16 bits")
+    assert torch.isnan(evaluate.linear(x, w, bias=torch.full_like(z, math.nan), activation=kind)).all()
