@@ -879,10 +879,19 @@ template <class T, int ROWS, int ACT> int launch_rows_of(const LinearArgs &a, cu
 
 template <class T, int ACT> int launch_rows(const LinearArgs &a, cudaStream_t s)
 {
-    if (a.M > 65535 * kFewRows) return SPDY_ERR_UNSUPPORTED;  // K = 0 only
     if (a.M == 1) return launch_rows_of<T, 1, ACT>(a, s);
     if (a.M == 2) return launch_rows_of<T, 2, ACT>(a, s);
-    return launch_rows_of<T, 4, ACT>(a, s);
+    // A grid's second dimension ends at 65535: rows without products (K = 0) may be more.
+    constexpr int64_t most = 65535 * 4;
+    LinearArgs some = a;
+    for (int64_t m = 0; m < a.M; m += most) {
+        some.M = a.M - m < most ? a.M - m : most;
+        some.y = static_cast<char *>(a.y) + m * a.ldy * static_cast<int64_t>(type_size(a.out_type));
+        if (a.residual) some.residual = static_cast<const T *>(a.residual) + m * a.ldres;
+        const int rc = launch_rows_of<T, 4, ACT>(some, s);
+        if (rc != SPDY_OK) return rc;
+    }
+    return SPDY_OK;
 }
 
 template <class T, int ACT> int launch(const LinearArgs &a, void *workspace, cudaStream_t s)

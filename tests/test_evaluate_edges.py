@@ -212,3 +212,18 @@ def test_activations_are_accurate_relative_to_themselves(dtype, kind, M):
     ref.close(got, want.expand(M, -1), err.expand(M, -1), "fp32")
     ref.close(evaluate.linear(x, w, bias=z, activation=kind), want.expand(M, -1), err.expand(M, -1), "16 bits")
     assert torch.isnan(evaluate.linear(x, w, bias=torch.full_like(z, math.nan), activation=kind)).all()
+
+
+# ------------------------------------------------------------------------------------------------ linear
+
+@gpu
+@pytest.mark.parametrize("M", [262140, 262141, 600001])
+@pytest.mark.parametrize("out_dtype", [BF16, F32])
+def test_linear_without_products_has_as_many_rows_as_any(M, out_dtype):
+    N = 3
+    x, w = torch.empty(M, 0, dtype=BF16, device="cuda"), torch.empty(N, 0, dtype=BF16, device="cuda")
+    b, res = rand(N, seed=1), rand(M, N, seed=2, dtype=BF16, pad=2)
+    want, err = ref.linear(x, w, b, res, "silu")
+    ref.close(evaluate.linear(x, w, b, res, "silu", out_dtype=out_dtype), want, err)
+    want, err = ref.linear(x, w, b, None, "none")
+    ref.close(evaluate.linear(x, w, b, out_dtype=out_dtype), want, err)
