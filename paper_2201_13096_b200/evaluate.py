@@ -7,6 +7,8 @@ against the dense one afterwards.  ``linear`` and ``layer_norm`` carry a block o
 
 Every call runs in the CUDA library on ``stream`` (default: torch's current stream of the tensors' device); PyTorch supplies
 memory and streams.  Matrices are 2-D CUDA tensors with unit column stride and any row stride.  There is no CPU fallback.
+Nothing is recorded for autograd: with gradients enabled, tensors that require one are refused (detach them, and take the
+gradient from the ``..._backward`` and ``..._with_grad`` calls).
 """
 from __future__ import annotations
 
@@ -123,8 +125,15 @@ def _dtype(t, what: str) -> int:
     return code
 
 
+def _refuse_gradient(what: str):
+    if torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, which this call does not record: pass {what}.detach() or call under torch.no_grad()")
+
+
 def _rows(t, what: str):
     """(rows, columns, row stride in elements, device index) of a 2-D CUDA tensor with unit column stride."""
+    if t.requires_grad:
+        _refuse_gradient(what)
     if not t.is_cuda or t.ndim != 2:
         raise ValueError(f"{what} must be a 2-D CUDA tensor")
     (r, c), (s0, s1) = t.shape, t.stride()
@@ -146,6 +155,8 @@ def _like(t, what: str, rows: int, cols: int, dtype, device: int) -> int:
 
 
 def _vector(t, what: str, n: int, device: int, dtype=None):
+    if t.requires_grad:
+        _refuse_gradient(what)
     if t.ndim != 1 or t.shape[0] != n or t.get_device() != device or (n > 1 and not t.is_contiguous()):
         raise ValueError(f"{what} must be a contiguous [{n}] tensor on cuda:{device}")
     if dtype is not None and t.dtype != dtype:
@@ -382,6 +393,8 @@ def _teacher(top_ids, top_logprobs, R, dev):
     if top_ids.ndim != 2:
         raise ValueError("top_ids must be [R][K]")
     K = top_ids.shape[1]
+    if top_logprobs.requires_grad:
+        _refuse_gradient("top_logprobs")
     bits = _ids(top_ids, "top_ids", (R, K), dev)
     if (top_logprobs.shape != (R, K) or top_logprobs.dtype != torch.float32 or top_logprobs.get_device() != dev
             or not top_logprobs.is_contiguous()):

@@ -1,12 +1,11 @@
-"""The evaluation operators at the ends of their ranges: alignments, magnitudes, counts, threads and what they refuse."""
+"""The evaluation operators at the ends of their ranges: alignments, magnitudes, counts, and what they refuse."""
 import math
-import threading
 
 import pytest
 import torch
 
 import eval_reference as ref
-from paper_2201_13096_b200 import binding, build as build_mod, evaluate
+from paper_2201_13096_b200 import build as build_mod, evaluate
 from test_evaluate import BF16, F16, F32, norm_bounds, rand
 
 INF = math.inf
@@ -227,3 +226,39 @@ def test_linear_without_products_has_as_many_rows_as_any(M, out_dtype):
     ref.close(evaluate.linear(x, w, b, res, "silu", out_dtype=out_dtype), want, err)
     want, err = ref.linear(x, w, b, None, "none")
     ref.close(evaluate.linear(x, w, b, out_dtype=out_dtype), want, err)
+
+
+# ------------------------------------------------------------------------------------------------ gradients that autograd expects
+
+def test_tensors_that_require_a_gradient_are_refused():
+    x = torch.zeros(2, 8, requires_grad=True)
+    evaluate.library()
+    with pytest.raises(ValueError, match="gradient"):
+        evaluate.layer_norm(x)
+    with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):
+        evaluate.layer_norm(x)
+
+
+@gpu
+def test_every_tensor_that_requires_a_gradient_is_refused():
+    """Nothing is recorded, so that a result without history would lose it in silence."""
+    x, w, b = rand(4, 16, dtype=BF16), rand(16, 16, seed=1, dtype=BF16), rand(16, seed=2, dtype=BF16)
+    logits, tokens, v = rand(4, 16, seed=3), torch.zeros(4, dtype=torch.int64, device="cuda"), rand(4, seed=4)
+    ids, lps = torch.arange(2, device="cuda").expand(4, 2).contiguous(), torch.full((4, 2), -2.0, device="cuda")
+    calls = [
+        (evaluate.linear, (x, w, b, x)), (evaluate.layer_norm, (x, b, b)), (evaluate.layer_norm_backward, (x, x, b, v, v)),
+        (evaluate.token_logprobs, (logits, tokens)), (evaluate.token_logprobs_backward, (logits, tokens, v, v, v, v)),
+        (evaluate.token_logprobs_with_grad, (logits, tokens, v, v)), (evaluate.distill_loss, (logits, ids, lps)),
+        (evaluate.distill_loss_backward, (logits, ids, lps, v, v, v)), (evaluate.distill_loss_with_grad, (logits, ids, lps, v)),
+    ]
+    for call, args in calls:
+        call(*args)
+        for k, t in enumerate(args):
+            if not t.is_floating_point():
+                continue
+            tracked = [*args[:k], t.detach().clone().requires_grad_(), *args[k + 1:]]
+            with pytest.raises(ValueError, match="gradient"):
+                call(*tracked)
+            with torch.no_grad():
+                call(*tracked)
+    torch.cuda.synchronize()
