@@ -92,20 +92,35 @@ _TYPES = {}
 _current_stream = _current_device = _empty_strided = None
 
 
+def _checked(fast, plain, same):
+    """``fast`` if it is there and ``same(fast, plain)``, else ``plain``: an entry of torch without a promise is used only as far as
+    it answers like the public one."""
+    try:
+        return fast if fast is not None and same(fast, plain) else plain
+    except Exception:
+        return plain
+
+
+def _same_memory(fast, plain):
+    a, b = fast((2, 3), (4, 1), torch.float16), plain((2, 3), (4, 1), torch.float16)
+    return all(f(a) == f(b) for f in (type, lambda t: t.shape, lambda t: t.stride(), lambda t: t.dtype, lambda t: t.device, lambda t: t.requires_grad))
+
+
 def _import_torch():
     global torch, _current_stream, _current_device, _empty_strided
     import torch as t
 
-    _TYPES.update({t.float32: 0, t.bfloat16: 1, t.float16: 2})
-    # the handle of the current stream as a number, without an object around it (small calls are bound by the host)
-    _current_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda i: t.cuda.current_stream(i).cuda_stream)
-    _current_device = getattr(t._C, "_cuda_getDevice", None) or t.cuda.current_device
-    # uninitialised memory on the current device by (shape, strides, type), again without the general call's argument parsing
-    try:
-        _empty_strided = t._C._dynamo.guards._empty_strided_cuda
-    except AttributeError:
-        _empty_strided = lambda shape, strides, dtype: t.empty_strided(shape, strides, dtype=dtype, device="cuda")  # noqa: E731
     torch = t
+    _TYPES.update({t.float32: 0, t.bfloat16: 1, t.float16: 2})
+    # Small calls are bound by the host: the handle of the current stream as a number, without an object around it, and
+    # uninitialised memory on the current device by (shape, strides, type), without the general call's argument parsing.
+    _current_stream, _current_device = lambda i: t.cuda.current_stream(i).cuda_stream, t.cuda.current_device
+    _empty_strided = lambda shape, strides, dtype: t.empty_strided(shape, strides, dtype=dtype, device="cuda")  # noqa: E731
+    if t.cuda.is_available():
+        _current_device = _checked(getattr(t._C, "_cuda_getDevice", None), _current_device, lambda f, p: f() == p())
+        _current_stream = _checked(getattr(t._C, "_cuda_getCurrentRawStream", None), _current_stream, lambda f, p: f(_current_device()) == p(_current_device()))
+        guards = getattr(getattr(t._C, "_dynamo", None), "guards", None)
+        _empty_strided = _checked(getattr(guards, "_empty_strided_cuda", None), _empty_strided, _same_memory)
 
 
 def _matrix(rows: int, cols: int, dtype):

@@ -262,3 +262,24 @@ def test_every_tensor_that_requires_a_gradient_is_refused():
             with torch.no_grad():
                 call(*tracked)
     torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------------------------------------ what torch does not promise
+
+def test_an_entry_of_torch_that_answers_otherwise_is_not_used():
+    evaluate.library()
+    plain = lambda shape, strides, dtype: torch.empty_strided(shape, strides, dtype=dtype)  # noqa: E731
+    for fast in (None, lambda *a: 1 / 0, lambda shape, strides: plain(shape, strides, F16), lambda shape, strides, dtype: plain(shape, strides, F32),
+                 lambda shape, strides, dtype: torch.empty(shape, dtype=dtype), lambda *a: None):
+        assert evaluate._checked(fast, plain, evaluate._same_memory) is plain
+    good = lambda shape, strides, dtype: plain(shape, strides, dtype)  # noqa: E731
+    assert evaluate._checked(good, plain, evaluate._same_memory) is good
+
+
+@gpu
+def test_results_lie_in_memory_of_the_kind_asked_for():
+    evaluate.library()
+    t = evaluate._empty_strided((3, 5), (5, 1), BF16)
+    assert t.is_cuda and t.shape == (3, 5) and t.is_contiguous() and t.dtype == BF16
+    assert evaluate._current_device() == torch.cuda.current_device()
+    assert evaluate._current_stream(0) == torch.cuda.current_stream(0).cuda_stream
