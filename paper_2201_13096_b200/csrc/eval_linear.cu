@@ -49,11 +49,11 @@ __device__ __forceinline__ void barrier_expect(uint64_t *b, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes) : "memory");
 }
-// Waits until the phase of `parity` is over; gives up after about two seconds and counts that.
+// Waits until the phase of `parity` is over; gives up after about two seconds of polling and counts that.
 __device__ __forceinline__ bool barrier_wait(uint64_t *b, uint32_t parity)
 {
     const uint32_t addr = smem_addr(b);
-    long long start = 0;
+    Patience patience;
     for (;;) {
         uint32_t done;
         asm volatile(
@@ -62,9 +62,7 @@ __device__ __forceinline__ bool barrier_wait(uint64_t *b, uint32_t parity)
             : "r"(addr), "r"(parity)
             : "memory");
         if (done) return true;
-        const long long now = clock64();
-        if (start == 0) start = now;
-        if (now - start > 4000000000ll) {
+        if (patience.over(clock64())) {
             atomicAdd(&g_timeouts, 1);
             return false;
         }
