@@ -56,8 +56,8 @@ int spdy_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, int dtyp
                 int out_dtype, void *workspace, size_t workspace_bytes, void *cuda_stream);
 /*
  * The kernels of spdy_linear wait on barriers between their warps with a limit of about two seconds of polling (time in which
- * the kernel is preempted does not count); a wait that runs out is counted and the tile is left unfinished (never seen; it would
- * mean a broken device or library).  Reads and clears that
+ * the kernel is preempted does not count); a wait that runs out is counted and what was waited for is NaN in y (never seen; it
+ * would mean a broken device or library).  Reads and clears that
  * count on the current device, waiting for `cuda_stream`: SPDY_OK, or SPDY_ERR_INTERNAL if it was not zero.
  */
 int spdy_linear_check_status(void *cuda_stream);

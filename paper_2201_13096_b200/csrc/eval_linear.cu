@@ -345,6 +345,17 @@ __device__ __noinline__ void turn_narrow(const LinearArgs &a, int64_t m, int64_t
     }
 }
 
+// NaN in `cols` columns (from n) of a warp's 32 rows (from m): a tile whose products never came.
+__device__ __noinline__ void spoil(const LinearArgs &a, int64_t m, int64_t n, int cols)
+{
+    m += threadIdx.x & 31;
+    if (m >= a.M) return;
+    for (int c = 0; c < cols && n + c < a.N; ++c) {
+        if (a.out_type == SPDY_F32) static_cast<float *>(a.y)[m * a.ldy + n + c] = quiet_nan();
+        else static_cast<uint16_t *>(a.y)[m * a.ldy + n + c] = 0x7fffu;  // in bf16 and in f16
+    }
+}
+
 // One warp carries COLS columns of its 32 rows (from row m0) of an accumulator at `tmem` to y, 16 columns at a time: a lane holds
 // a row, 16 columns of it, and touches y and residual in whole 32-byte sectors.  (Turning the rows through shared memory for
 // longer runs cost more than it gave: the tensor core's operands and the copies that bring them take the shared memory's
@@ -374,7 +385,7 @@ __device__ __forceinline__ void carry(const LinearArgs &a, uint32_t tmem, int64_
     for (int i = lane; i < COLS; i += 32) bias[i] = a.bias && n0 + i < a.N ? bias_at(a, n0 + i) : 0.f;
     fetch(0);
     __syncwarp();
-    if (!ready()) return;
+    if (!ready()) return spoil(a, m0, n0, COLS);
 #pragma unroll 1
     for (int c = 0; c < COLS; c += 16) {
         float f[16];
@@ -501,7 +512,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                 if (++stage == S::kStages) stage = 0, parity ^= 1;
             }
         }
-        if (!ok && part == 0)  // copies in flight may not outlive the block (a peer's are counted on the same barriers)
+        // no copy outlives the block, whatever the other warps met (of a pair, both blocks' are counted on the first one's barriers)
+        if (MODE != kPair || part == 0)
             for (int i = 0; i < S::kStages && i < issued; ++i) {
                 const int n = issued - 1 - i;
                 barrier_wait(&ctl.full[n % S::kStages], n / S::kStages & 1);
@@ -510,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
         if (MODE != kPair || part == 0) {
             constexpr uint32_t format = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
             constexpr uint32_t idesc = 1u << 4 | format << 7 | format << 10 | static_cast<uint32_t>(BN / 8) << 17 | static_cast<uint32_t>(TILE_M / 16) << 24;
-            int stage = 0, acc = 0;
+            int stage = 0, acc = 0, issued = 0;
             uint32_t parity = 0, acc_parity = 0;
             bool ok = true;
             for (int tile = first; tile < tiles && ok; tile += step) {
@@ -534,10 +546,13 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                         if (kb + 1 == kb1) mma_commit<MODE == kPair>(&ctl.acc_full[acc]);
                     }
                     __syncwarp();
+                    ++issued;
                     if (++stage == S::kStages) stage = 0, parity ^= 1;
                 }
                 if (++acc == 2) acc = 0, acc_parity ^= 1;
             }
+            // nor does a product: TMEM is freed once the last one issued is done
+            if (issued > 0) barrier_wait(&ctl.empty[(issued - 1) % S::kStages], (issued - 1) / S::kStages & 1);
         }
     } else if (MODE != kSplit) {
         // warps 4 to 19: a warp reaches the quarter of TMEM's rows that its number names modulo four
@@ -546,10 +561,14 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
         float *bias = reinterpret_cast<float *>(extra + S::kWorkers * 1024) + (warp - 2) * S::kWarpColumns;
         int acc = 0;
         uint32_t acc_parity = 0;
-        bool ok = group * S::kWarpColumns < BN;
-        for (int tile = first; tile < tiles && ok; tile += step) {
+        bool ok = true;
+        for (int tile = group * S::kWarpColumns < BN ? first : tiles; tile < tiles; tile += step) {
             const int64_t m0 = static_cast<int64_t>(tile % a.tiles_m) * TILE_M + (MODE == kPair ? part * BM : 0) + quarter * 32;
             const int64_t n0 = static_cast<int64_t>(tile / a.tiles_m) * BN + group * S::kWarpColumns;
+            if (!ok) {
+                spoil(a, m0, n0, S::kWarpColumns);
+                continue;
+            }
             const auto ready = [&] {
                 ok = __all_sync(0xffffffffu, barrier_wait(&ctl.acc_full[acc], acc_parity));
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -578,11 +597,15 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
     if (MODE == kSplit) {
         const int slice = BN / parts;  // columns this block finishes
         const int quarter = warp & 3, group = (warp - 2) >> 2;
-        if (warp >= 2 && group * 16 < BN && __all_sync(0xffffffffu, barrier_wait(&ctl.acc_full[0], 0))) {
+        if (warp >= 2 && group * 16 < BN) {
+            const bool ok = __all_sync(0xffffffffu, barrier_wait(&ctl.acc_full[0], 0));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             for (int c = group * 16; c < BN; c += kEpilogueWarps / 4 * 16) {
                 float v[16];
                 tmem_load16(tmem + c + (static_cast<uint32_t>(quarter * 32) << 16), v);
+                if (!ok)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = quiet_nan();
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int col = c + 4 * i, owner = col / slice;
