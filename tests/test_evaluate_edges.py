@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import eval_reference as ref
+import test_evaluate
 from paper_2201_13096_b200 import build as build_mod, evaluate
 from test_evaluate import BF16, F16, F32, norm_bounds, rand
 
@@ -283,3 +284,32 @@ def test_results_lie_in_memory_of_the_kind_asked_for():
     assert t.is_cuda and t.shape == (3, 5) and t.is_contiguous() and t.dtype == BF16
     assert evaluate._current_device() == torch.cuda.current_device()
     assert evaluate._current_stream(0) == torch.cuda.current_stream(0).cuda_stream
+
+
+# ------------------------------------------------------------------------------------------------ linear: large products
+
+def tiles_of(M, N, K, sms=148):
+    """The tile shape with the least estimated time, as the library estimates it for products too large to share a tile's K."""
+    up, k = (lambda a, b: -(-a // b)), -(-K // 128)
+    assert up(M, 128) * up(N, 64) * 2 > sms
+    options = {"pair": (256, 256, sms // 2, 1040, 4000), "128": (128, 128, sms, 620, 2500), "64": (128, 64, sms, 540, 2000)}
+    time = {name: up(up(M, r) * up(N, w), units) * per * k + fixed for name, (r, w, units, per, fixed) in options.items()}
+    return min(time, key=time.get), up(up(M, 256) * up(N, 256), sms // 2)
+
+
+# M, K, N, dtype, activation, bias, residual, pad of x, pad of w, tiles, tiles of 256 x 256 that a pair of multiprocessors has at most
+PRODUCTS = [
+    (2304, 1536, 2048, BF16, "none", None, False, 0, 0, "pair", 1), (2290, 1001, 1793, BF16, "gelu", "same", True, 0, 0, "pair", 1),
+    (4097, 520, 2999, F16, "silu", "same", True, 8, 16, "pair", 3), (4100, 384, 3000, BF16, "relu", F32, True, 0, 0, "pair", 3),
+    (8191, 700, 2559, BF16, "gelu", "same", True, 5, 3, "pair", 5), (16390, 400, 765, F16, "none", "same", True, 0, 8, "pair", 3),
+    (2305, 1000, 2311, F16, "gelu", "same", True, 0, 0, "128", 2), (16390, 640, 60, BF16, "none", None, True, 8, 0, "64", 1),
+]
+
+
+@gpu
+@pytest.mark.parametrize("M,K,N,dtype,kind,bias,residual,padx,padw,tiles,rounds", PRODUCTS)
+def test_large_products_against_the_formula(M, K, N, dtype, kind, bias, residual, padx, padw, tiles, rounds):
+    """Pairs of multiprocessors on a tile: rings that wrap around, accumulators used again, ends of rows, columns and K, strided operands,
+    both result types, over the residual, into a wider buffer."""
+    assert tiles_of(M, N, K) == (tiles, rounds)
+    test_evaluate.test_linear_against_the_formula(M, K, N, dtype, kind, bias, residual, padx, padw)
