@@ -139,7 +139,7 @@ struct Running {
 // Makes `top` the logit the sums are relative to, if it is far above the present one (or the first).
 template <bool ENT> __device__ __forceinline__ void raise(Running &st, float top, float c)
 {
-    if (top > st.m && (top - st.m) * c > 2.f) {
+    if ((top - st.m) * c > 2.f) {  // not so where both are -inf, or one is NaN
         if (st.s != 0.f) {
             const Reference old(st.m, c), now(top, c);
             const float rise = old.far ? (now.far ? (st.m - top) * c : fmaf(st.m, c, -now.base)) : now.far ? -fmaf(top, c, -old.base) : old.base - now.base;
