@@ -26,7 +26,10 @@ constexpr int BM = 128, BK = 64;           // rows of a block's tile; a slice of
 constexpr int kSlices = 2;                 // slices of a stage: a round of barriers costs about 400 cycles, the products of one slice 128 to 512
 constexpr int kEpilogueWarps = 16;         // four to a scheduler: with two, a tile's epilogue took longer than its products at K = 768
 constexpr int kThreads = 32 * (2 + kEpilogueWarps);
-constexpr int64_t kFewRows = 8;            // at most this many rows take the multiply-add kernel (it and the tensor cores, us, K = N = 4096: 1 row 6.3, 18.5; 8 rows 16.5, 18.5; 16 rows 28.7, 14.4)
+// At most this many rows take the multiply-add kernel.  It and the tensor cores in one build, us, with a w that comes from memory:
+// 4096 x 4096 4 rows 11.2, 17.9, 8 rows 17.7, 18.0 to 22.5, 9 rows 23.7, 17.5; 1024 x 4096 8 rows 8.8, 8.8, 9 rows 11.9, 8.8; 768 x 768 8 rows
+// 2.9, 6.4, 9 rows 3.1, 6.4; 2048 x 8192 4 rows 12.7, 19.1, 8 rows 20.9, 18.7.
+constexpr int64_t kFewRows = 8;
 
 struct LinearArgs {
     const void *x, *w, *bias, *residual;
