@@ -17,7 +17,8 @@
  *     allow.  Outputs may not overlap inputs except where a function says so.
  *   - Sums, statistics and gradients of parameters are held in fp32; 16-bit outputs are rounded once.  No atomics on
  *     floating-point data: the same call on the same data gives the same bits.
- *   - Rows or columns may be zero in number: the call is a no-op (parameter gradients of no rows are written as 0).
+ *   - Rows may be zero in number, and spdy_linear's columns: the call is a no-op (parameter gradients of no rows are written as
+ *     0).  Rows of no columns (D = 0, V = 0) have no mean and no distribution: SPDY_ERR_INVALID_ARG.
  *   - At most 2^31 - 1 blocks per launch: rows beyond that number (times up to 8 for long rows) are SPDY_ERR_UNSUPPORTED.
  * Errors: SPDY_ERR_INVALID_ARG (null pointer, size or stride out of range, unknown type, bad alignment),
  * SPDY_ERR_WORKSPACE_TOO_SMALL, SPDY_ERR_UNSUPPORTED (a size beyond a stated limit), SPDY_ERR_CUDA.
@@ -139,6 +140,8 @@ int spdy_token_logprobs_with_grad(const void *logits, int64_t ld, int dtype, con
  *   dlogits_v = grad_loss / T (A p_v - sum of q_j with id_j = v)   in S
  *               grad_loss / T (A p_v - left p_v / p_rest)          outside
  *   (without the tail A p_v outside).  dlogits [R][V] of `dtype`, may be the logits themselves.
+ * From saved sums the gradient is as exact as an fp32 lse and rest let it be (see spdy_token_logprobs_backward), p and p / p_rest at
+ * most 1.  spdy_distill_loss_with_grad works from the sums themselves; lse, and rest with the tail, are required there too.
  */
 #define SPDY_DISTILL_MAX 256
 int spdy_distill_loss(const void *logits, int64_t ld, int dtype, const void *ids, int index_bits, const float *top_logprobs,

@@ -6,9 +6,9 @@
 // to 256 bytes (which share a warp): rows in registers.  Rows beyond 32 KB are read again per sum.
 //
 // Measured, bf16, us (and the bytes at 6.56 TB/s; a plain copy of the forward's bytes takes 24.0, an addition of the backward's
-// three matrices 32): 32768 x 1024 forward 28.8 (20.5), backward 47.9 (30.7); 8192 x 4096 31.4, 53.7; 32768 x 999 (rows that
-// start anywhere) 52.1, 86.4; 200000 x 128 34.9 (15.6), 49.9 (23.4); 128 x 768 4.5, 12.4.  With rows in registers, the next one's
-// on their way: 33.4, 60; 49.6, 87; 56, 179.
+// three matrices 32): 32768 x 1024 forward 27.0 (20.5), backward 47.3 (30.7); 8192 x 4096 29.4, 52.0; 32768 x 999 (rows that
+// start anywhere) 49.7, 84.2; 200000 x 128 32.9 (15.6), 49.4 (23.4); 128 x 768 4.3, 12.4.  With rows in registers, the next one's
+// on their way: 33.4, 60; 49.6, 87; 56, 179.  fp32: 16384 x 1024 22.0 (20.5), 41.4 (30.7); 32768 x 1024 48.6 (40.9), 73.5 (61.4).
 #include "eval_common.cuh"
 
 using namespace spdy_eval;
@@ -687,7 +687,7 @@ template <class T> __global__ void __launch_bounds__(256) norm_backward_columns_
 }
 
 // dweight and dbias from the blocks' sums, 32 columns per block, each of 32 warps adding every 32nd block's.  Bound by its
-// latency (about 5 us for 1024 columns of 148 blocks), so it is launched early.
+// latency (about 5 us for 1024 columns of 148 blocks).
 __global__ void __launch_bounds__(1024) norm_columns_kernel(const float *partial, int blocks, int64_t D, float *dweight, float *dbias)
 {
     __shared__ float part[32][32];
@@ -925,7 +925,7 @@ int spdy_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_
     const int blocks = backward_blocks(R, D, static_cast<int64_t>(type_size(dtype)));
     const int rc = dtype == SPDY_F32 ? backward<float>(a, blocks, s) : dtype == SPDY_BF16 ? backward<__nv_bfloat16>(a, blocks, s) : backward<__half>(a, blocks, s);
     if (rc != SPDY_OK || !a.want_params) return rc;
-    // launched while the blocks before it still run; it waits for them itself
+    // sent to the device before the blocks in front of it are done, which it waits for itself: no gap for the launch between them
     cudaLaunchAttribute early = {};
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;

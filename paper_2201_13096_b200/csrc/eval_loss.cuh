@@ -14,9 +14,11 @@
 // Bound.  Rows are read once, and with a gradient written once.  At 4 to 6 bytes moved and 8 to 20 instructions issued per element the
 // issue slots (65 to 75 % taken) and memory (50 to 65 %) are loaded alike; rows of a few thousand elements add their ends: some hundred
 // instructions per thread to join the sums and the teacher's entries.
-// Measured, bf16, us (and the bytes at 6.56 TB/s): 2048 x 131072 log probabilities 97 (82), with the best 20 127, with
-// gradient 222 (164), distillation 97, with gradient 220; 4096 x 65536 101 (82), 122, 214 (164), 106, 215; 1024 x 50001 (rows that start
-// anywhere) 31 (16), 33, 53 (31), 31, 57; 16384 x 8192 73 (41), 140, 113 (82), 97, 149; 65536 x 2000 64 (40), 177, 122 (80), 135, 216.
+// Measured, bf16, us (and the bytes at 6.56 TB/s): 2048 x 131072 log probabilities 94 (82), with the best 20 128, with
+// gradient 220 (164), distillation from 32 ids 94, with gradient 220; 4096 x 65536 104 (82), 124, 214 (164), 106, 215; 1024 x 50001 (rows
+// that start anywhere) 28 (16), 36, 55 (31), 31, 57; 16384 x 8192 72 (41), 139, 109 (82), 89, 144; 65536 x 2000 62 (40), 176, 115 (80),
+// 113, 192.  Backward passes from saved sums: 159, 159, 37, 84, 98 and 200, 204, 50, 102, 144.  Masks of -inf cost nothing: 95 % of
+// 8192 x 30000 118, of 65536 x 2000 62.
 #ifndef SPDY_EVAL_LOSS_CUH
 #define SPDY_EVAL_LOSS_CUH
 
@@ -882,7 +884,7 @@ template <int NT> struct RowShared {
 // memory, each thread's granules copied by itself (so that no barrier is needed) up to H steps ahead.  With GRAD the row is then
 // read again, backwards: its last H steps are still in the ring, the earlier ones in L2 as long as the rows in flight fit (see
 // row_cluster).  A step ahead in registers instead took 246 us for 4096 x 65536 bf16 with gradient (now 214), and 136 for the
-// distillation's loss alone (now 111); but the plain log probabilities, with the fewest instructions, lose to the way through shared memory
+// distillation's loss alone (now 106); but the plain log probabilities, with the fewest instructions, lose to the way through shared memory
 // (2048 x 131072: 99 us in registers, 105 through the ring), and where alternatives are looked for, these need the space.
 // One row per block: with blocks that stay and walk over rows 8192 x 30000 with gradient took 236 us, now 211.
 template <class T, int NT, int U, int MODE, int GRAD>
