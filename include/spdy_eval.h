@@ -6,7 +6,8 @@
  * for a profile (Section 3.4); the pruned model is then tuned against the dense one.  The operators here carry that
  * work on the device: linear layers with their epilogue, layer normalisation with its gradients, log probabilities
  * of given tokens with entropy and top alternatives, and the distillation loss against the dense model's top log
- * probabilities with its gradient.
+ * probabilities with its gradient.  spdy_linear has no backward call: its input's gradient is the product with the transposed
+ * weight, its weight's gradient is left to the caller.
  *
  * Common rules
  *   - All pointers are device pointers on the current device unless they say "host"; the work is enqueued on
