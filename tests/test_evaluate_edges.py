@@ -313,3 +313,51 @@ def test_large_products_against_the_formula(M, K, N, dtype, kind, bias, residual
     both result types, over the residual, into a wider buffer."""
     assert tiles_of(M, N, K) == (tiles, rounds)
     test_evaluate.test_linear_against_the_formula(M, K, N, dtype, kind, bias, residual, padx, padw)
+
+
+# ------------------------------------------------------------------------------------------------ offsets beyond 32 bits
+
+def filled(R, C, seed):
+    """bf16 values whose last rows lie beyond 2^31 elements."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.empty(R, C, dtype=BF16, device="cuda").normal_(generator=g)
+
+
+@gpu
+def test_rows_beyond_the_first_2_to_the_31_elements():
+    R, C = 66000, 33001
+    assert (R - 2) * C > 2 ** 31
+    x = filled(R, C, 1)
+    at = torch.tensor([0, 1, R - 2, R - 1])
+    xs = x[at.cuda()].clone()
+    tokens = torch.arange(R, device="cuda") % C
+    ids = (torch.arange(4, device="cuda")[None, :] * 7919 + torch.arange(R, device="cuda")[:, None]) % C
+    lps = torch.full((R, 4), -2.0, device="cuda")
+    g = torch.ones(R, device="cuda")
+    lp, h, lse = ref.token_logprobs(xs, tokens[at.cuda()], 1.0)
+    flat = 2.0 ** -19 * 14
+    got = evaluate.token_logprobs(x, tokens, top_k=5)
+    ref.close(got.logprob[at.cuda()], lp, flat)
+    assert torch.equal(got.top_ids[at.cuda()].cpu().long(), ref.top(xs, 5))
+    y, mean, rstd = evaluate.layer_norm(x)
+    want, mean64, rstd64 = ref.layer_norm(xs, None, None, 1e-5)
+    ref.close(y[at.cuda()], want, norm_bounds(xs, None, None, want, rstd64), "y")
+    dx, _, _ = evaluate.layer_norm_backward(y, x, None, mean, rstd, out=y, params=False)
+    dx64, _, _ = ref.layer_norm_backward(want.bfloat16(), xs, None, mean64, rstd64)
+    ref.close(dx[at.cuda()], dx64, 0.02 * (1 + want.abs()))  # y was rounded to 16 bits, the gradient of which is nearly all cancelled
+    del y, dx
+    loss, _, _, grad = ref.distill(xs, ids[at.cuda()], lps[at.cuda()], 1.0, True, g[at.cuda()].cpu())
+    out, dlogits = evaluate.distill_loss_with_grad(x, ids, lps, g, out=x)
+    ref.close(out.loss[at.cuda()], loss, 1e-4)
+    ref.close(dlogits[at.cuda()], grad, 1e-6)
+
+
+@gpu
+@pytest.mark.parametrize("K", [64, 61])
+def test_products_beyond_the_first_2_to_the_31_elements(K):
+    M, N = 1100000, 2000
+    assert (M - 2) * N > 2 ** 31
+    x, w, b = rand(300, K, seed=1, dtype=BF16).repeat(-(-M // 300), 1)[:M], rand(N, K, seed=2, dtype=BF16, scale=K ** -0.5), rand(N, seed=3)
+    at = torch.tensor([0, 1, M // 2, M - 2, M - 1])
+    want, err = ref.linear(x[at.cuda()], w, b, None, "gelu")
+    ref.close(evaluate.linear(x, w, b, activation="gelu")[at.cuda()], want, err)
