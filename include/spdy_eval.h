@@ -108,9 +108,9 @@ int spdy_token_logprobs(const void *logits, int64_t ld, int dtype, const void *t
  *   dlogits_v = (grad_logprob ([v = token] - p_v) - grad_entropy p_v (log p_v + entropy)) / T
  *   lse, entropy [R]: what the forward call gave (entropy may be NULL when grad_entropy is); grad_logprob, grad_entropy [R]
  *   fp32, either may be NULL (0).  dlogits [R][V] of `dtype`, may be the logits themselves.
- * An lse in fp32 is off by up to 2^-24 of itself, and p by that much relative to p; in rows whose largest logit over T is
- * beyond 1e7 (an all-masked row under a finite mask of -1e9) it no longer tells how many ids share the mass: p is then at most 1
- * each.  spdy_token_logprobs_with_grad does the forward and this in one call: memory is read once as far as the rows in flight
+ * An lse in fp32 is off by up to 2^-24 |lse|, and every p from it by that much relative to itself; in rows whose largest logit
+ * over T is beyond 1e7 (an all-masked row under a finite mask of -1e9) it no longer tells how many ids share the mass: p is then at
+ * most 1 each.  spdy_token_logprobs_with_grad does the forward and this in one call: memory is read once as far as the rows in flight
  * fit on chip, and the gradient comes from the sums themselves, whatever their size.  lse (and entropy with grad_entropy) are
  * required there too.
  */
