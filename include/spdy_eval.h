@@ -124,6 +124,44 @@ int spdy_token_logprobs_with_grad(const void *logits, int64_t ld, int dtype, con
                                   void *cuda_stream);
 
 /*
+ * The same values under softmax((hidden weight^T + bias) / temperature), straight from a head's input and weight: the logits
+ *   x_rv = sum_d hidden[r][d] weight[v][d] + bias[v]   (products summed in fp32)
+ * are never kept.
+ *   hidden [R][D], weight [V][D]: `dtype` (SPDY_BF16 or SPDY_F16), D >= 1; bias [V] of `bias_dtype` (`dtype` or SPDY_F32), may be NULL;
+ *   a bias of -inf marks ids that are not allowed.  R, V and D below 2^31 - 65536.
+ *   tokens, logprob, entropy, lse, rows with nothing left, NaN and infinities: as spdy_token_logprobs has them.  The tensor
+ *   core's sums are cut, not rounded: a logit is off by up to about 2^-24 D / 16 of itself.
+ * Gradients of sum_r grad_logprob[r] logprob[r] + grad_entropy[r] entropy[r], with g_rv the gradient by x_rv
+ * (spdy_token_logprobs_backward's dlogits):
+ *   dhidden[r][d] = sum_v g_rv weight[v][d],   dweight[v][d] = sum_r g_rv hidden[r][d],   dbias[v] = sum_r g_rv
+ *   dhidden [R][D] and dweight [V][D] of `dtype`, dbias [V] fp32 (from sums in fp32); each may be NULL.  They may not overlap the inputs.
+ *   g is computed in fp32 and rounded to 16 bits once, as the operand of the two products (in half precision times a power of two that
+ *   brings its largest row near 2^14).  A row of hidden that is not finite spoils dweight, with or without a token.
+ *   ..._backward takes lse (and entropy with grad_entropy) from the forward call, ..._with_grad computes all in one call.
+ *   workspace: ..._workspace_bytes(...) bytes, 256-byte aligned, contents undefined afterwards; `forward` and `gradients` say which
+ *   of the two the call computes.  With gradients it holds g for as many ids at a time as 256 MB hold (2048 at least).
+ * spdy_linear_check_status reports for these kernels too.
+ */
+size_t spdy_linear_token_logprobs_workspace_bytes(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int dtype,
+                                                  int64_t R, int64_t V, int64_t D, int forward, int gradients);
+int spdy_linear_token_logprobs(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int dtype, const void *bias,
+                               int bias_dtype, const void *tokens, int index_bits, int64_t R, int64_t V, int64_t D,
+                               float temperature, float *logprob, float *entropy, float *lse, void *workspace,
+                               size_t workspace_bytes, void *cuda_stream);
+int spdy_linear_token_logprobs_backward(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int dtype,
+                                        const void *bias, int bias_dtype, const void *tokens, int index_bits, int64_t R,
+                                        int64_t V, int64_t D, float temperature, const float *lse, const float *entropy,
+                                        const float *grad_logprob, const float *grad_entropy, void *dhidden, int64_t lddh,
+                                        void *dweight, int64_t lddw, float *dbias, void *workspace, size_t workspace_bytes,
+                                        void *cuda_stream);
+int spdy_linear_token_logprobs_with_grad(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int dtype,
+                                         const void *bias, int bias_dtype, const void *tokens, int index_bits, int64_t R,
+                                         int64_t V, int64_t D, float temperature, const float *grad_logprob,
+                                         const float *grad_entropy, float *logprob, float *entropy, float *lse, void *dhidden,
+                                         int64_t lddh, void *dweight, int64_t lddw, float *dbias, void *workspace,
+                                         size_t workspace_bytes, void *cuda_stream);
+
+/*
  * Distillation from a teacher's top log probabilities.  p = softmax(logits / temperature) is the student's row, S the ids a
  * row of `ids` names, and
  *   tail != 0: q_j = exp(top_logprobs_j), left = max(0, 1 - sum_j q_j), p_rest = the student's probability outside S,

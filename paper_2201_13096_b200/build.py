@@ -27,6 +27,7 @@ HEADERS = [os.path.join(os.path.dirname(PKG), "include", "spdy_dp.h"),
 EVAL_HEADERS = [os.path.join(os.path.dirname(PKG), "include", "spdy_dp.h"),
                 os.path.join(os.path.dirname(PKG), "include", "spdy_eval.h"),
                 os.path.join(CSRC, "eval_common.cuh"), os.path.join(CSRC, "eval_loss.cuh"),
+                os.path.join(CSRC, "eval_tensor.cuh"),
                 os.path.join(CSRC, "eval_top.cuh"), os.path.join(CSRC, "eval_ranges.h")]
 HOST_SOURCES = [os.path.join(CSRC, "spdy_plan.cpp"), os.path.join(CSRC, "spdy_search.cpp")]
 LIB = os.path.join(PKG, "libspdy_dp.so")

@@ -292,6 +292,7 @@ __device__ __forceinline__ void add_logit(float &m, float &s, float x, float c)
 
 inline bool known_type(int t) { return t == SPDY_F32 || t == SPDY_BF16 || t == SPDY_F16; }
 inline size_t type_size(int t) { return t == SPDY_F32 ? 4 : 2; }
+inline bool temperature_ok(float t) { return t > 0.f && t <= 3.4e38f && kLog2e / t <= 3.4e38f && kLog2e / t > 0.f; }
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 inline int finish_launch()

@@ -12,17 +12,18 @@
 // 8192 x 4096 x 1024 with residual 60 (41), 8192^3 751 to 782 (656), 512 x 1024 x 4096 12.7, 128 x 768 x 3072 9.4, 16 x 4096 x 1024 10.6.
 // Bound: large products by the feed of the tensor cores (a stage's barriers and copies beside its products), the middle ones by whole rounds of tiles
 // and the last one's epilogue, the small ones by the fixed way through barriers, TMEM and the exchange of parts (about 8 us).
-#include <cuda.h>
-
-#include "eval_common.cuh"
+#include "eval_tensor.cuh"
 
 using namespace spdy_eval;
+
+namespace spdy_eval {
+int linear_logprobs_timeouts(cudaStream_t s, int *count);  // eval_linear_logprobs.cu
+}
 
 namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int BM = 128, BK = 64;           // rows of a block's tile; a slice of K: 64 16-bit elements = one 128-byte swizzle row
 constexpr int kSlices = 2;                 // slices of a stage: a round of barriers costs about 400 cycles, the products of one slice 128 to 512
 constexpr int kEpilogueWarps = 16;         // four to a scheduler: with two, a tile's epilogue took longer than its products at K = 768
 constexpr int kThreads = 32 * (2 + kEpilogueWarps);
@@ -41,136 +42,7 @@ struct LinearArgs {
     int sectors, words;                    // every row of y and of the residual starts on 32 bytes; 16-bit rows of y start on 4
 };
 
-__device__ int g_timeouts;                 // waits that ran out of time (none in a working run); spdy_linear_check_status
-
-// ---------------------------------------------------------------------------------------------- mbarrier, TMA, tcgen05
-__device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-
-__device__ __forceinline__ void barrier_init(uint64_t *b, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(b)), "r"(count) : "memory"); }
-__device__ __forceinline__ void barrier_arrive(uint64_t *b) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(b)) : "memory"); }
-__device__ __forceinline__ void barrier_expect(uint64_t *b, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(b)), "r"(bytes) : "memory");
-}
-// Waits until the phase of `parity` is over; gives up after about two seconds of polling and counts that.
-__device__ __forceinline__ bool barrier_wait(uint64_t *b, uint32_t parity)
-{
-    const uint32_t addr = smem_addr(b);
-    Patience patience;
-    for (;;) {
-        uint32_t done;
-        asm volatile(
-            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-            : "=r"(done)
-            : "r"(addr), "r"(parity)
-            : "memory");
-        if (done) return true;
-        if (patience.over(clock64())) {
-            atomicAdd(&g_timeouts, 1);
-            return false;
-        }
-    }
-}
-__device__ __forceinline__ void tma_load(void *to, const CUtensorMap *map, int x, int y, uint64_t *b)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_addr(to)),
-                 "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_addr(b))
-                 : "memory");
-}
-// Descriptor of a K-major operand whose rows are 128 bytes under the 128-byte swizzle: groups of 8 rows lie 1024 bytes apart.
-__device__ __forceinline__ uint64_t operand(uint32_t addr) { return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | 1ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61; }
-
-// One thread of a converged warp.  The loops below run on whole warps and elect the issuing thread around each TMA or tcgen05
-// instruction: these take their operands from uniform registers, and inside a branch on the lane number each operand cost a
-// trip there (a pair's 64-wide slice of K: 731 cycles with the branch, 521 this way).
-__device__ __forceinline__ bool elect()
-{
-    uint32_t chosen;
-    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(chosen));
-    return chosen != 0;
-}
-// The address of a shared variable in the first block of the cluster.
-__device__ __forceinline__ uint32_t first_blocks(uint32_t addr)
-{
-    uint32_t r;
-    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
-    return r;
-}
-__device__ __forceinline__ void barrier_arrive_at(uint32_t addr) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory"); }
-// A copy to this block's shared memory that counts on a barrier of either block of the pair.
-__device__ __forceinline__ void tma_load_pair(void *to, const CUtensorMap *map, int x, int y, uint32_t barrier)
-{
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_addr(to)),
-                 "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(barrier)
-                 : "memory");
-}
-
-template <bool PAIR> __device__ __forceinline__ void tmem_alloc(uint32_t *to, int columns)
-{
-    if (PAIR) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    } else {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-}
-template <bool PAIR> __device__ __forceinline__ void tmem_free(uint32_t tmem, int columns)
-{
-    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
-    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
-}
-template <bool PAIR> __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
-{
-    if (PAIR)
-        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
-                     "r"(static_cast<uint32_t>(add))
-                     : "memory");
-    else
-        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
-                     "r"(static_cast<uint32_t>(add))
-                     : "memory");
-}
-// Signals the barrier (of both blocks of a pair) when the products issued so far are done.
-template <bool PAIR> __device__ __forceinline__ void mma_commit(uint64_t *b)
-{
-    if (PAIR)
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(b)), "h"(static_cast<uint16_t>(3)) : "memory");
-    else asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(b)) : "memory");
-}
-// 16 columns of a warp's 32 rows, a row to a lane.
-__device__ __forceinline__ void tmem_load16(uint32_t addr, float *v)
-{
-    uint32_t r[16];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
-          "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(addr)
-        : "memory");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-
 // ---------------------------------------------------------------------------------------------- epilogue
-// Two fp32 operations per instruction.
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    float2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;"
-        : "=l"(reinterpret_cast<unsigned long long &>(r))
-        : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)), "l"(reinterpret_cast<unsigned long long &>(c)));
-    return r;
-}
-__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
-
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    float2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long &>(r)) : "l"(reinterpret_cast<unsigned long long &>(a)), "l"(reinterpret_cast<unsigned long long &>(b)));
-    return r;
-}
 // 1 / x to about an ulp, on the special-function unit
 __device__ __forceinline__ float rcp(float x)
 {
@@ -289,19 +161,6 @@ template <class T, int ACT> __device__ __forceinline__ void finish8(const Linear
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] += res[i];
     }
-}
-
-__device__ __forceinline__ void load32(const void *p, uint4 &lo, uint4 &hi)
-{
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(lo.x), "=r"(lo.y), "=r"(lo.z), "=r"(lo.w), "=r"(hi.x), "=r"(hi.y), "=r"(hi.z), "=r"(hi.w)
-                 : "l"(p)
-                 : "memory");
-}
-__device__ __forceinline__ void store32(void *p, uint4 lo, uint4 hi)
-{
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(lo.x), "r"(lo.y), "r"(lo.z), "r"(lo.w), "r"(hi.x), "r"(hi.y), "r"(hi.z), "r"(hi.w)
-                 : "memory");
 }
 
 // 16 columns (from n) of 32 rows (from m), a row to a lane, stored by runs of columns; 1 KB of shared memory of the warp's own.
@@ -725,60 +584,8 @@ template <class T, int ROWS, int COLS, int ACT, bool WIDE> __global__ void __lau
     else static_cast<T *>(a.y)[m * a.ldy + n] = Elem<T>::from_float(z);
 }
 
-// Copies of operands whose rows TMA cannot read (a row has to start on 16 bytes), with rows of ldto elements.  They cost one more
-// read and write of such an operand and a launch (333 x 1001 x 517, both unaligned: 14.8 us).
-struct Repack {
-    const uint16_t *from[2];
-    uint16_t *to[2];
-    int64_t ld[2], rows[2], K, ldto;
-};
-// A thread copies eight elements of a row; those behind K are whatever (TMA never reads them).
-__global__ void __launch_bounds__(256) repack_kernel(const Repack p)
-{
-    const int which = blockIdx.y;
-    if (!p.to[which]) return;
-    const int64_t per_row = p.ldto / 8, total = p.rows[which] * per_row;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t r = i / per_row, k = (i - r * per_row) * 8;
-        const uint16_t *from = p.from[which] + r * p.ld[which] + k;
-        uint32_t e[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = k + j < p.K ? from[j] : 0;
-        *reinterpret_cast<uint4 *>(p.to[which] + r * p.ldto + k) = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
-    }
-}
-
 // ---------------------------------------------------------------------------------------------- launches
-using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled()
-{
-    static EncodeTiled fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) p = nullptr;
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
-    return fn;
-}
-
-int make_map(CUtensorMap *map, const void *p, int64_t ld, int64_t rows, int64_t K, int dtype, int box_rows)
-{
-    EncodeTiled encode = encode_tiled();
-    if (!encode) return SPDY_ERR_UNSUPPORTED;
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(K), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(ld) * 2};
-    const cuuint32_t box[2] = {BK, static_cast<cuuint32_t>(box_rows)}, steps[2] = {1, 1};
-    const CUresult rc = encode(map, dtype == SPDY_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(p), dims, strides, box,
-                               steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return rc == CUDA_SUCCESS ? SPDY_OK : SPDY_ERR_UNSUPPORTED;
-}
-
-bool tma_ok(const void *p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0 && ld * 2 < (1ll << 40); }
 bool on_tensor_cores(int64_t M, int64_t K) { return M > kFewRows && K > 0; }
-int64_t packed_ld(int64_t K) { return (K + 7) / 8 * 8; }
-size_t packed_bytes(int64_t rows, int64_t K) { return (static_cast<size_t>(rows) * static_cast<size_t>(packed_ld(K)) * 2 + 255) / 256 * 256; }
-
 template <class T, int BN, int ACT, int MODE> int launch_tiles(const CUtensorMap &mx, const CUtensorMap &mw, const LinearArgs &a, int parts, cudaStream_t s)
 {
     constexpr int smem = Shape<BN, MODE>::kSmem;
@@ -933,8 +740,6 @@ template <class T> int launch_type(const LinearArgs &a, void *workspace, cudaStr
     }
 }
 
-bool half_type(int t) { return t == SPDY_BF16 || t == SPDY_F16; }
-
 }  // namespace
 
 extern "C" {
@@ -976,14 +781,11 @@ int spdy_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, int dtyp
 int spdy_linear_check_status(void *cuda_stream)
 {
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    int count = 0;
-    const int zero = 0;
-    SPDY_EVAL_TRY(cudaMemcpyFromSymbolAsync(&count, g_timeouts, sizeof count, 0, cudaMemcpyDeviceToHost, s));
-    SPDY_EVAL_TRY(cudaStreamSynchronize(s));
-    if (count == 0) return SPDY_OK;
-    SPDY_EVAL_TRY(cudaMemcpyToSymbolAsync(g_timeouts, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, s));
-    SPDY_EVAL_TRY(cudaStreamSynchronize(s));
-    return SPDY_ERR_INTERNAL;
+    int count = 0, more = 0;
+    int rc = take_timeouts(s, &count);
+    if (rc == SPDY_OK) rc = linear_logprobs_timeouts(s, &more);
+    if (rc != SPDY_OK) return rc;
+    return count + more == 0 ? SPDY_OK : SPDY_ERR_INTERNAL;
 }
 
 }  // extern "C"

@@ -1,0 +1,921 @@
+// Log probabilities of given tokens under softmax((hidden weight^T + bias) / T), entropy and gradients, without a table of logits:
+// kernels and C entries (spdy_eval.h).
+//
+// Everything large is a product on the tensor cores, carried by one kernel: pairs of multiprocessors (cta_group::2) on tiles of
+// 256 x 256, operands brought by TMA, two fp32 accumulators in TMEM, sixteen warps that carry a finished tile on while the next
+// is multiplied.  What is done with a tile differs:
+//   kStats   logits of 256 rows and ids -> per row the largest, the sum of exponentials relative to it, and the sum that the
+//            entropy needs; the given token's logit.  A second kernel joins a row's tiles in their order.
+//   kGrad    the same logits again -> the gradient by the logits, rounded to 16 bits, of one piece of the vocabulary
+//   kHidden  (the piece's gradient) x (the piece's rows of weight): fp32 sums of dhidden, added up over the pieces
+//   kWeight  (the piece's gradient)^T x hidden: the piece's rows of dweight (kWeightParts: as fp32 sums, where few tiles share
+//            their summed index among more multiprocessors)
+// The gradient's piece is the only thing of size rows x ids, and pieces are as wide as a fixed budget allows.  In the last two products
+// one or both operands have the summed index as their rows ("MN-major"); TMA brings them as boxes of 64 columns, and the matrix
+// descriptors name that order, so nothing is transposed.
+#include "eval_tensor.cuh"
+
+using namespace spdy_eval;
+
+namespace spdy_eval {
+int linear_logprobs_timeouts(cudaStream_t s, int *count) { return take_timeouts(s, count); }
+}
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kSlices = 2;                               // 64-wide slices of the summed index to a stage
+constexpr int kTile = 256, kWarpColumns = 64;            // of a pair's tile; columns that an epilogue warp carries
+constexpr int kEpilogueWarps = 16, kThreads = 32 * (2 + kEpilogueWarps);
+constexpr int kSliceBytes = 2 * BM * BK * 2;             // 128 rows or columns of each operand
+constexpr int kStageBytes = kSlices * kSliceBytes, kStages = 196608 / kStageBytes;
+constexpr int kStageK = kSlices * BK;
+constexpr int kConsts = 8;                               // floats per row that the gradient needs
+
+enum Kind { kStats, kGrad, kHidden, kWeight, kWeightParts };
+
+// Which operands have the summed index as their rows.
+template <int KIND> struct Order {
+    static constexpr bool kA = KIND == kWeight || KIND == kWeightParts, kB = kA || KIND == kHidden;
+};
+
+struct ProductArgs {
+    int64_t M, N;                  // rows and columns of the result that exist
+    int tiles_m, tiles_n, splits, group, k_blocks;
+    int b_row0;                    // first row of the second operand
+    // kStats, kGrad
+    const void *bias, *tokens;
+    int bias_type, index_bits;
+    int64_t v0;                    // the first column's id
+    float c;                       // log2(e) / T
+    float *partial, *token_logit;  // [tiles_n][3][padded_rows], [M]
+    int64_t padded_rows;
+    const float *consts;           // [M][kConsts]
+    const uint32_t *scale_bits;    // NULL, or the largest gradient's bits (half precision)
+    float *column_sums;            // NULL, or [row groups of 32][N]
+    int64_t ld_sums;
+    void *out;                     // kGrad: the piece; kWeight: 16 bits; parts: fp32 [splits][M][ldo]
+    int64_t ldo;
+    int add, sectors;              // parts: to what is there already; kWeight: rows of out start on 32 bytes
+};
+
+// Half precision keeps the gradient by the logits times a power of two that brings the largest row's to 2^13 .. 2^14: the least normal number is then
+// 2^-28 of it.
+__device__ __forceinline__ int scale_power(const uint32_t *bits)
+{
+    if (!bits) return 0;
+    const int e = static_cast<int>(*bits >> 23);
+    return e == 0 || e >= 255 ? 0 : min(13 - (e - 127), 100);
+}
+__device__ __forceinline__ float power_of_two(int k) { return __int_as_float((k + 127) << 23); }
+
+__device__ __forceinline__ int64_t token_at(const void *tokens, int bits, int64_t r)
+{
+    return bits == 64 ? static_cast<const int64_t *>(tokens)[r] : static_cast<const int32_t *>(tokens)[r];
+}
+__device__ __forceinline__ float value_at(const void *p, int type, int64_t n)
+{
+    if (type == SPDY_F32) return static_cast<const float *>(p)[n];
+    if (type == SPDY_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[n]);
+    return __half2float(static_cast<const __half *>(p)[n]);
+}
+
+// Running sums of a row relative to its largest logit m: s = sum 2^((x - m) c), t = sum 2^((x - m) c) (x - m) c.
+struct Sums {
+    float m, s, t;
+};
+// Relative to `top` >= m instead.  A shift beyond -1e30 leaves nothing, and is cut there so that 0 times it stays 0.
+__device__ __forceinline__ void raise(Sums &a, float top, float c)
+{
+    if (a.s != 0.f) {
+        const float shift = max_nan((a.m - top) * c, -1e30f), f = ex2(shift);
+        a.t = f * fmaf(a.s, shift, a.t);
+        a.s *= f;
+    }
+    a.m = top;
+}
+__device__ __forceinline__ void join(Sums &a, Sums b, float c)
+{
+    const float top = fmaxf(a.m, b.m);
+    raise(a, top, c), raise(b, top, c);
+    a.s += b.s, a.t += b.t;
+}
+
+// Descriptor of an operand whose rows are the summed index: boxes of 64 columns (128 bytes, swizzled) and 64 rows, 8 KB apart;
+// groups of 8 rows lie 1024 bytes apart.
+__device__ __forceinline__ uint64_t operand_by_columns(uint32_t addr)
+{
+    return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | 512ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61;
+}
+
+// The tile of an item: groups of `group` tiles down, all tiles across before the next group.
+__device__ __forceinline__ void tile_of(const ProductArgs &a, int item, int &split, int &tm, int &tn)
+{
+    const int tiles = a.tiles_m * a.tiles_n;
+    split = item / tiles;
+    const int tile = item - split * tiles, per_group = a.group * a.tiles_n, g = tile / per_group, rest = tile - g * per_group;
+    const int rows = min(a.group, a.tiles_m - g * a.group);
+    tn = rest / rows;
+    tm = g * a.group + rest - tn * rows;
+}
+
+struct Control {
+    uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
+    uint32_t tmem;
+};
+
+// ---------------------------------------------------------------------------------------------- what is done with a tile
+// Each function carries 64 columns of a warp's 32 rows, a row to a lane.  `ready` waits for the accumulator and says whether it came
+// (if not, what is written is NaN); `release` is called once the last columns have left TMEM.
+
+// The ids' bias in the warp's shared memory.
+__device__ __forceinline__ void stage_bias(const ProductArgs &a, int64_t n0, float *bias)
+{
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+    for (int i = lane; i < kWarpColumns; i += 32) bias[i] = a.bias && n0 + i < a.N ? value_at(a.bias, a.bias_type, a.v0 + n0 + i) : 0.f;
+    __syncwarp();
+}
+// 16 logits of a row; ids beyond the vocabulary are -inf.
+__device__ __forceinline__ void load_logits(const ProductArgs &a, uint32_t tmem, int64_t n, const float *bias, float *f)
+{
+    tmem_load16(tmem, f);
+    if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 b = reinterpret_cast<const float4 *>(bias)[i];
+            f[4 * i] += b.x, f[4 * i + 1] += b.y, f[4 * i + 2] += b.z, f[4 * i + 3] += b.w;
+        }
+    }
+    if (n + 16 > a.N)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (n + i >= a.N) f[i] = neg_inf();
+}
+
+template <class Ready, class Release>
+__device__ __forceinline__ Sums carry_stats(const ProductArgs &a, uint32_t tmem, int64_t m, int64_t n0, float *bias, Ready ready, Release release)
+{
+    int64_t token = -1;
+    if (m < a.M && a.token_logit) token = token_at(a.tokens, a.index_bits, m);
+    stage_bias(a, n0, bias);
+    if (!ready()) {
+        if (token >= n0 && token < n0 + kWarpColumns && token < a.N) a.token_logit[m] = quiet_nan();
+        return {0.f, quiet_nan(), quiet_nan()};
+    }
+    Sums sums = {neg_inf(), 0.f, 0.f};
+#pragma unroll 1
+    for (int c = 0; c < kWarpColumns; c += 16) {
+        float f[16];
+        load_logits(a, tmem + c, n0 + c, bias + c, f);
+        if (c + 16 == kWarpColumns) release();
+        float top = sums.m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, f[i]);
+        raise(sums, top, a.c);
+        const float ref = top == neg_inf() ? 0.f : top;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float d = (f[i] - ref) * a.c, e = ex2(d);
+            sums.s += e;
+            sums.t = fmaf(e, max_nan(d, -200.f), sums.t);  // below -200 e is 0
+        }
+        const int64_t at = token - (n0 + c);
+        if (at >= 0 && at < 16 && token < a.N) {
+            float x = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x = at == i ? f[i] : x;
+            a.token_logit[m] = x;
+        }
+    }
+    return sums;
+}
+
+// Sums over the 32 rows of 16 columns, each lane's `f`: of column `lane / 2` in the lane, by halves of the columns that partners exchange.
+__device__ __forceinline__ float sum_columns(const float *f)
+{
+    const int lane = threadIdx.x & 31;
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const bool up = lane & 16;
+        v[i] = (up ? f[i + 8] : f[i]) + __shfl_xor_sync(0xffffffffu, up ? f[i] : f[i + 8], 16);
+    }
+#pragma unroll
+    for (int half = 4, bit = 8; half; half >>= 1, bit >>= 1) {
+        const bool up = lane & bit;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < half) v[i] = (up ? v[i + half] : v[i]) + __shfl_xor_sync(0xffffffffu, up ? v[i] : v[i + half], bit);
+    }
+    return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1);
+}
+
+// Gradient by 64 logits of a row: d = [v = token] a - p (ab + b2 y), y = log2 p = (x - ref) c - ls, rounded to 16 bits once.
+// ENT: with the entropy's gradient (b2 is not 0).
+template <class T, bool ENT, class Ready, class Release>
+__device__ __forceinline__ void carry_grad(const ProductArgs &a, uint32_t tmem, int64_t m0, int64_t n0, float *bias, Ready ready, Release release)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t m = m0 + lane;
+    const bool inside = m < a.M;
+    float4 k = make_float4(0.f, 0.f, 0.f, 0.f), more = make_float4(0.f, __int_as_float(-1), 0.f, 0.f);
+    if (inside) {
+        k = reinterpret_cast<const float4 *>(a.consts)[2 * m], more = reinterpret_cast<const float4 *>(a.consts)[2 * m + 1];
+        const float scale = power_of_two(scale_power(a.scale_bits));
+        k.z *= scale, k.w *= scale, more.x *= scale;
+    }
+    const int64_t token = __float_as_int(more.y);
+    stage_bias(a, n0, bias);
+    const bool ok = ready();
+    char *to = static_cast<char *>(a.out) + (m * a.ldo + n0) * 2;
+#pragma unroll 1
+    for (int c = 0; c < kWarpColumns; c += 16) {
+        float f[16];
+        load_logits(a, tmem + c, n0 + c, bias + c, f);
+        if (c + 16 == kWarpColumns) release();
+        if (n0 + c >= a.N) continue;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float y = min_nan(fmaf(f[i] - k.x, a.c, -k.y), 0.f);
+            f[i] = ENT ? -ex2(y) * fmaf(more.x, max_nan(y, -200.f), k.w) : -ex2(y) * k.w;
+            if (!ok) f[i] = quiet_nan();
+        }
+        const int64_t at = token - (a.v0 + n0 + c);
+        if (at >= 0 && at < 16)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (at == i) f[i] += k.z;
+        if (inside) store32(to + 2 * c, Elem<T>::pack(f), Elem<T>::pack(f + 8));
+        if (a.column_sums) {
+            if (!inside)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) f[i] = 0.f;
+            const float sum = sum_columns(f);
+            const int64_t n = n0 + c + (lane >> 1);
+            if (!(lane & 1) && n < a.N && m0 < a.M) a.column_sums[m0 / 32 * a.ld_sums + n] = sum;
+        }
+    }
+}
+
+template <class Ready, class Release>
+__device__ __forceinline__ void carry_parts(const ProductArgs &a, uint32_t tmem, int split, int64_t m0, int64_t n0, Ready ready, Release release)
+{
+    const int64_t m = m0 + (threadIdx.x & 31);
+    float *to = static_cast<float *>(a.out) + (split * a.M + m) * a.ldo + n0;
+    const bool ok = ready();
+#pragma unroll 1
+    for (int c = 0; c < kWarpColumns; c += 16) {
+        float f[16];
+        tmem_load16(tmem + c, f);
+        if (c + 16 == kWarpColumns) release();
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int h = 0; h < 16; h += 8) {
+            if (n0 + c + h >= a.N) break;  // ldo is a multiple of 8
+            uint4 lo, hi;
+            float old[8] = {};
+            if (a.add) load32(to + c + h, lo, hi), Elem<float>::unpack(lo, old), Elem<float>::unpack(hi, old + 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) old[i] = ok ? old[i] + f[h + i] : quiet_nan();
+            store32(to + c + h, Elem<float>::pack(old), Elem<float>::pack(old + 4));
+        }
+    }
+}
+
+// 16 columns (from n) of 32 rows (from m), a row to a lane, stored by runs of columns; 1 KB of shared memory of the warp's own.
+__device__ __noinline__ void store_turned(const ProductArgs &a, int64_t m, int64_t n, uint4 v0, uint4 v1, unsigned char *turn)
+{
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+    reinterpret_cast<uint4 *>(turn)[2 * lane] = v0;
+    reinterpret_cast<uint4 *>(turn)[2 * lane + 1] = v1;
+    __syncwarp();
+    uint16_t *y = static_cast<uint16_t *>(a.out);
+#pragma unroll
+    for (int it = 0; it < 16; ++it) {
+        const int64_t row = m + it * 2 + lane / 16, col = n + lane % 16;
+        if (row < a.M && col < a.N) y[row * a.ldo + col] = reinterpret_cast<const uint16_t *>(turn)[it * 32 + lane];
+    }
+}
+
+template <class T, class Ready, class Release>
+__device__ __forceinline__ void carry_store(const ProductArgs &a, uint32_t tmem, int64_t m0, int64_t n0, unsigned char *turn, Ready ready, Release release)
+{
+    const int64_t m = m0 + (threadIdx.x & 31);
+    char *to = static_cast<char *>(a.out) + (m * a.ldo + n0) * 2;
+    const float scale = power_of_two(-scale_power(a.scale_bits));
+    const bool ok = ready();
+#pragma unroll 1
+    for (int c = 0; c < kWarpColumns; c += 16) {
+        float f[16];
+        tmem_load16(tmem + c, f);
+        if (c + 16 == kWarpColumns) release();
+        if (n0 + c >= a.N) continue;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) f[i] = ok ? f[i] * scale : quiet_nan();
+        if (!a.sectors || n0 + c + 16 > a.N) store_turned(a, m0, n0 + c, Elem<T>::pack(f), Elem<T>::pack(f + 8), turn);
+        else if (m < a.M) store32(to + 2 * c, Elem<T>::pack(f), Elem<T>::pack(f + 8));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- the product
+constexpr int kBiasBytes = kEpilogueWarps * kWarpColumns * 4, kTurnBytes = kEpilogueWarps * 1024, kJoinBytes = 2 * 16 * 32 * 12;
+template <int KIND> constexpr int extra_bytes() { return KIND == kStats ? kBiasBytes + kJoinBytes : KIND == kGrad ? kBiasBytes : KIND == kWeight ? kTurnBytes : 0; }
+template <int KIND> constexpr int smem_bytes() { return 1024 + kStages * kStageBytes + extra_bytes<KIND>(); }
+
+template <class T, int KIND, bool ENT>
+__global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ ProductArgs a)
+{
+    extern __shared__ unsigned char raw_smem[];
+    unsigned char *stages = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw_smem) + 1023) & ~static_cast<uintptr_t>(1023));
+    unsigned char *extra = stages + kStages * kStageBytes;
+    __shared__ Control ctl;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int part = static_cast<int>(cluster.block_rank());
+    const int items = a.tiles_m * a.tiles_n * a.splits, first = static_cast<int>(blockIdx.x) / 2, step = static_cast<int>(gridDim.x) / 2;
+    constexpr bool kColumnsA = Order<KIND>::kA, kColumnsB = Order<KIND>::kB;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) barrier_init(&ctl.full[i], 1), barrier_init(&ctl.empty[i], 1);
+        for (int i = 0; i < 2; ++i) barrier_init(&ctl.acc_full[i], 1), barrier_init(&ctl.acc_empty[i], 2 * kEpilogueWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_a)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_b)) : "memory");
+    }
+    __syncwarp();
+    if (warp == 1) tmem_alloc<true>(&ctl.tmem, 512);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    cluster.sync();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = ctl.tmem;
+    const auto range = [&](int split, int &kb0, int &kb1) {
+        kb0 = static_cast<int>(static_cast<int64_t>(a.k_blocks) * split / a.splits), kb1 = static_cast<int>(static_cast<int64_t>(a.k_blocks) * (split + 1) / a.splits);
+    };
+
+    if (warp == 0) {
+        int stage = 0, issued = 0;
+        uint32_t parity = 0;
+        bool ok = true;
+        for (int item = first; item < items && ok; item += step) {
+            int split, tm, tn, kb0, kb1;
+            tile_of(a, item, split, tm, tn);
+            range(split, kb0, kb1);
+            const int m0 = tm * kTile + part * BM, n0 = tn * kTile + part * BM;
+            if (kb0 == kb1) continue;  // a share of the last, shorter piece may be empty: nothing to add
+            for (int kb = kb0; kb < kb1; ++kb) {
+                ok = __all_sync(0xffffffffu, barrier_wait(&ctl.empty[stage], parity ^ 1));
+                if (!ok) break;
+                unsigned char *to = stages + stage * kStageBytes;
+                if (elect()) {
+                    const uint32_t full = first_blocks(smem_addr(&ctl.full[stage]));  // both blocks' copies count on the first block's barrier
+                    if (part == 0) barrier_expect(&ctl.full[stage], 2 * kStageBytes);
+#pragma unroll
+                    for (int q = 0; q < kSlices; ++q) {
+                        const int k = (kb * kSlices + q) * BK;
+                        unsigned char *ta = to + q * kSliceBytes, *tb = ta + BM * BK * 2;
+                        if (kColumnsA) tma_load_pair(ta, &map_a, m0, k, full), tma_load_pair(ta + 8192, &map_a, m0 + 64, k, full);
+                        else tma_load_pair(ta, &map_a, k, m0, full);
+                        if (kColumnsB) tma_load_pair(tb, &map_b, n0, a.b_row0 + k, full), tma_load_pair(tb + 8192, &map_b, n0 + 64, a.b_row0 + k, full);
+                        else tma_load_pair(tb, &map_b, k, a.b_row0 + n0, full);
+                    }
+                }
+                __syncwarp();
+                ++issued;
+                if (++stage == kStages) stage = 0, parity ^= 1;
+            }
+        }
+        // no copy outlives the block, whatever the other warps met (both blocks' are counted on the first one's barriers)
+        if (part == 0)
+            for (int i = 0; i < kStages && i < issued; ++i) {
+                const int n = issued - 1 - i;
+                barrier_wait(&ctl.full[n % kStages], n / kStages & 1);
+            }
+    } else if (warp == 1) {
+        if (part == 0) {
+            constexpr uint32_t format = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+            constexpr uint32_t idesc = 1u << 4 | format << 7 | format << 10 | static_cast<uint32_t>(kColumnsA) << 15 | static_cast<uint32_t>(kColumnsB) << 16 |
+                                       static_cast<uint32_t>(kTile / 8) << 17 | static_cast<uint32_t>(kTile / 16) << 24;
+            int stage = 0, acc = 0, issued = 0;
+            uint32_t parity = 0, acc_parity = 0;
+            bool ok = true;
+            for (int item = first; item < items && ok; item += step) {
+                int split, tm, tn, kb0, kb1;
+                tile_of(a, item, split, tm, tn);
+                range(split, kb0, kb1);
+                if (kb0 == kb1) continue;
+                ok = __all_sync(0xffffffffu, barrier_wait(&ctl.acc_empty[acc], acc_parity ^ 1));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const uint32_t d = tmem + acc * kTile;
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    ok = __all_sync(0xffffffffu, barrier_wait(&ctl.full[stage], parity));
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t at = smem_addr(stages + stage * kStageBytes);
+                    if (elect()) {
+#pragma unroll
+                        for (int q = 0; q < kSlices; ++q) {
+                            const uint32_t pa = at + q * kSliceBytes, pb = pa + BM * BK * 2;
+                            const uint64_t da = kColumnsA ? operand_by_columns(pa) : operand(pa), db = kColumnsB ? operand_by_columns(pb) : operand(pb);
+                            // 16 of the summed index further: 32 bytes along a row, or 16 rows of 128 bytes
+#pragma unroll
+                            for (int k = 0; k < BK / 16; ++k) mma<true>(d, da + (kColumnsA ? 128 : 2) * k, db + (kColumnsB ? 128 : 2) * k, idesc, kb > kb0 || q > 0 || k > 0);
+                        }
+                        mma_commit<true>(&ctl.empty[stage]);
+                        if (kb + 1 == kb1) mma_commit<true>(&ctl.acc_full[acc]);
+                    }
+                    __syncwarp();
+                    ++issued;
+                    if (++stage == kStages) stage = 0, parity ^= 1;
+                }
+                if (++acc == 2) acc = 0, acc_parity ^= 1;
+            }
+            // nor does a product: TMEM is freed once the last one issued is done
+            if (issued > 0) barrier_wait(&ctl.empty[(issued - 1) % kStages], (issued - 1) / kStages & 1);
+        }
+    } else {
+        // warps 2 to 17: a warp reaches the quarter of TMEM's rows that its number names modulo four
+        const int quarter = warp & 3, group = (warp - 2) >> 2;
+        float *bias = reinterpret_cast<float *>(extra) + (warp - 2) * kWarpColumns;
+        int acc = 0;
+        uint32_t acc_parity = 0;
+        bool ok = true;
+        for (int item = first; item < items; item += step) {
+            int split, tm, tn, kb0, kb1;
+            tile_of(a, item, split, tm, tn);
+            range(split, kb0, kb1);
+            if (kb0 == kb1) continue;
+            const int64_t m0 = static_cast<int64_t>(tm) * kTile + part * BM + quarter * 32, n0 = static_cast<int64_t>(tn) * kTile + group * kWarpColumns;
+            const auto ready = [&] {  // once a wait has run out, nothing is waited for any more
+                ok = ok && __all_sync(0xffffffffu, barrier_wait(&ctl.acc_full[acc], acc_parity));
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                return ok;
+            };
+            const auto release = [&] {
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) barrier_arrive_at(first_blocks(smem_addr(&ctl.acc_empty[acc])));
+            };
+            const uint32_t at = tmem + acc * kTile + group * kWarpColumns + (static_cast<uint32_t>(quarter * 32) << 16);
+            if (KIND == kStats) {
+                const Sums mine = carry_stats(a, at, m0 + lane, n0, bias, ready, release);
+                // the four warps of these rows join their columns; two rooms, so that one barrier a tile is enough
+                float *room = reinterpret_cast<float *>(extra + kBiasBytes) + ((acc * 4 + quarter) * 4) * 96 + lane;
+                if (group > 0) room[group * 96] = mine.m, room[group * 96 + 32] = mine.s, room[group * 96 + 64] = mine.t;
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + quarter) : "memory");
+                if (group == 0) {
+                    Sums sums = mine;
+#pragma unroll
+                    for (int g = 1; g < 4; ++g) join(sums, {room[g * 96], room[g * 96 + 32], room[g * 96 + 64]}, a.c);
+                    if (m0 < a.padded_rows) {
+                        float *to = a.partial + static_cast<int64_t>(tn) * 3 * a.padded_rows + m0 + lane;
+                        to[0] = sums.m, to[a.padded_rows] = sums.s, to[2 * a.padded_rows] = sums.t;
+                    }
+                }
+            } else if (KIND == kGrad) {
+                carry_grad<T, ENT>(a, at, m0, n0, bias, ready, release);
+            } else if (KIND == kHidden || KIND == kWeightParts) {
+                carry_parts(a, at, split, m0, n0, ready, release);
+            } else {
+                carry_store<T>(a, at, m0, n0, extra + (warp - 2) * 1024, ready, release);
+            }
+            if (++acc == 2) acc = 0, acc_parity ^= 1;
+        }
+    }
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    cluster.sync();  // no block leaves while its barriers are signalled or its operands read
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        tmem_free<true>(tmem, 512);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- rows
+struct RowArgs {
+    int64_t R, V, padded_rows;
+    int tiles;
+    const float *partial, *token_logit;
+    const void *tokens;
+    int index_bits;
+    float c, temperature;
+    const float *in_lse, *in_entropy;          // a forward call's, when there is no partial
+    float *logprob, *entropy, *lse;            // each may be NULL
+    const float *grad_logprob, *grad_entropy;  // each may be NULL
+    float *consts;                             // NULL without a gradient
+    uint32_t *scale_bits;                      // NULL unless half precision
+};
+
+// What carry_grad needs of a row, from the reference and base-2 logarithm of the sum relative to it.
+__device__ __forceinline__ void write_consts(const RowArgs &a, int64_t r, int64_t token, float ref, float ls, float entropy, bool empty)
+{
+    float ga = a.grad_logprob && token >= 0 ? a.grad_logprob[r] / a.temperature : 0.f;
+    float gb = a.grad_entropy ? a.grad_entropy[r] / a.temperature : 0.f;
+    if (token >= a.V && a.grad_logprob) ga = quiet_nan();
+    if (empty) ref = ls = entropy = 0.f, ga = gb = 0.f;  // nothing allowed: no gradient
+    float4 *to = reinterpret_cast<float4 *>(a.consts) + 2 * r;
+    const float ab = ga + (a.grad_entropy ? gb * entropy : 0.f);
+    to[0] = make_float4(ref, ls, ga, ab);
+    to[1] = make_float4(gb * kLn2, __int_as_float(token < 0 || token >= a.V ? -1 : static_cast<int>(token)), 0.f, 0.f);
+    if (a.scale_bits) {  // |d| <= |ga| + |gb| (p |log p| + p H), and p |log p| < 0.37
+        const float most = fabsf(ga) + fabsf(gb) * (0.37f + entropy);
+        if (most > 0.f) atomicMax(a.scale_bits, __float_as_uint(most));  // of whole numbers: the order does not matter
+    }
+}
+
+// Joins the tiles of 32 rows, a row to a lane: each warp a part of the tiles, then the warps in their order.
+constexpr int kRowWarps = 16;
+__global__ void __launch_bounds__(32 * kRowWarps) rows_kernel(const RowArgs a)
+{
+    __shared__ float room[kRowWarps][3][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+    Sums sums = {neg_inf(), 0.f, 0.f};
+#pragma unroll 4
+    for (int tile = warp; tile < a.tiles; tile += kRowWarps) {
+        const float *from = a.partial + static_cast<int64_t>(tile) * 3 * a.padded_rows + r;
+        join(sums, {from[0], from[a.padded_rows], from[2 * a.padded_rows]}, a.c);
+    }
+    room[warp][0][lane] = sums.m, room[warp][1][lane] = sums.s, room[warp][2][lane] = sums.t;
+    __syncthreads();
+    if (warp > 0 || r >= a.R) return;
+    for (int w = 1; w < kRowWarps; ++w) join(sums, {room[w][0][lane], room[w][1][lane], room[w][2][lane]}, a.c);
+    const int64_t token = a.tokens ? token_at(a.tokens, a.index_bits, r) : -1;
+    const bool empty = sums.s == 0.f;
+    const float log_s = logf(sums.s), entropy = empty ? 0.f : log_s - kLn2 * (sums.t / sums.s);
+    if (a.lse) a.lse[r] = sums.m / a.temperature + log_s;
+    if (a.entropy) a.entropy[r] = entropy;
+    if (a.logprob) {
+        float lp = 0.f;
+        if (token >= a.V) lp = quiet_nan();
+        else if (token >= 0) lp = empty ? neg_inf() : (a.token_logit[r] - sums.m) / a.temperature - log_s;
+        a.logprob[r] = lp;
+    }
+    if (a.consts) write_consts(a, r, token, sums.m, log2f(sums.s), entropy, empty);
+}
+
+// The same from a forward call's lse and entropy.
+__global__ void __launch_bounds__(256) saved_rows_kernel(const RowArgs a)
+{
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (r >= a.R) return;
+    const float lse = a.in_lse[r];
+    write_consts(a, r, a.tokens ? token_at(a.tokens, a.index_bits, r) : -1, lse * a.temperature, 0.f, a.in_entropy ? a.in_entropy[r] : 0.f, lse == neg_inf());
+}
+
+// ---------------------------------------------------------------------------------------------- sums of parts
+// out[m][n] = sum over the splits of parts[split][m][n], in their order, times 2^-scale, rounded once.
+template <class T>
+__global__ void __launch_bounds__(256) finish_kernel(const float *parts, int splits, int64_t M, int64_t N, int64_t ldp, const uint32_t *scale_bits, T *out, int64_t ldo)
+{
+    const float scale = power_of_two(-scale_power(scale_bits));
+    const int64_t total = M * N;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t m = i / N, n = i - m * N;
+        float sum = 0.f;
+        for (int s = 0; s < splits; ++s) sum += parts[(s * M + m) * ldp + n];
+        out[m * ldo + n] = Elem<T>::from_float(sum * scale);
+    }
+}
+
+// dbias of a piece: the row groups' sums in their order, eight runs of them to a column.
+__global__ void __launch_bounds__(256) bias_kernel(const float *sums, int64_t groups, int64_t N, int64_t ld, const uint32_t *scale_bits, float *dbias)
+{
+    __shared__ float room[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+    float sum = 0.f;
+    if (n < N)
+        for (int64_t g = warp; g < groups; g += 8) sum += sums[g * ld + n];
+    room[warp][lane] = sum;
+    __syncthreads();
+    if (warp > 0 || n >= N) return;
+    for (int w = 1; w < 8; ++w) sum += room[w][lane];
+    dbias[n] = sum * power_of_two(-scale_power(scale_bits));
+}
+
+// ---------------------------------------------------------------------------------------------- launches
+int64_t div_up(int64_t x, int64_t y) { return (x + y - 1) / y; }
+size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// The gradient by the logits is kept for one piece of the vocabulary: as many ids as this much memory holds, 2048 at least.
+constexpr int64_t kPieceBytes = 256ll << 20, kLeastPiece = 2048;
+
+struct Layout {
+    size_t hidden, weight, partial, token_logit, consts, scale, piece, parts, sums, total;
+    int64_t padded_rows, width, ld_parts;  // width: ids of a piece
+    int hidden_splits, weight_splits;
+};
+
+// How many parts the sum of a product of few tiles is split into, so that it fills the pairs of multiprocessors: the least estimated time in stages,
+// a part costing its share and about five more for its way in and out.
+int choose_splits(int64_t tiles, int64_t k_blocks)
+{
+    const int64_t pairs = sm_count() / 2;
+    int best = 1;
+    double least = 1e300;
+    for (int s = 1; s <= 64 && s <= k_blocks; ++s) {
+        const double time = static_cast<double>(div_up(tiles * s, pairs)) * (static_cast<double>(div_up(k_blocks, s)) + 5.0) + 0.25 * s;
+        if (time < least) least = time, best = s;
+    }
+    return best;
+}
+
+Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int64_t R, int64_t V, int64_t D, bool stats, bool grads)
+{
+    Layout l = {};
+    size_t at = 0;
+    const auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += rounded(bytes);
+        return here;
+    };
+    l.padded_rows = div_up(R, 32) * 32;
+    l.hidden = take(tma_ok(hidden, ldh) ? 0 : packed_bytes(R, D));
+    l.weight = take(tma_ok(weight, ldw) ? 0 : packed_bytes(V, D));
+    if (stats) {
+        l.partial = take(static_cast<size_t>(div_up(V, kTile)) * 3 * l.padded_rows * 4);
+        l.token_logit = take(static_cast<size_t>(R) * 4);
+    }
+    if (grads) {
+        int64_t width = kPieceBytes / 2 / R / kTile * kTile;
+        if (width < kLeastPiece) width = kLeastPiece;
+        const int64_t pieces = div_up(V, width);
+        width = div_up(div_up(V, pieces), kTile) * kTile;  // pieces of one size
+        l.width = width < V ? width : div_up(V, 64) * 64;
+        l.ld_parts = div_up(D, 8) * 8;
+        const int64_t across = div_up(D, kTile);
+        l.hidden_splits = choose_splits(div_up(R, kTile) * across, div_up(l.width < V ? l.width : V, kStageK));
+        l.weight_splits = choose_splits(div_up(l.width < V ? l.width : V, kTile) * across, div_up(R, kStageK));
+        l.consts = take(static_cast<size_t>(R) * kConsts * 4);
+        l.scale = take(256);
+        l.piece = take(static_cast<size_t>(R) * l.width * 2);
+        size_t parts = static_cast<size_t>(l.hidden_splits) * R * l.ld_parts * 4;
+        at = rounded(at);
+        l.parts = take(parts + (l.weight_splits > 1 ? static_cast<size_t>(l.weight_splits) * l.width * l.ld_parts * 4 : 0));
+        l.sums = take(static_cast<size_t>(l.padded_rows / 32) * l.width * 4);
+    }
+    l.total = at;
+    return l;
+}
+
+struct HeadArgs {
+    const void *hidden, *weight, *bias, *tokens;
+    int64_t ldh, ldw, R, V, D;
+    int dtype, bias_type, index_bits;
+    float temperature;
+    const float *in_lse, *in_entropy, *grad_logprob, *grad_entropy;
+    float *logprob, *entropy, *lse;
+    void *dhidden, *dweight;
+    int64_t lddh, lddw;
+    float *dbias;
+    bool stats, grads;
+};
+
+// A map of a row-major matrix [rows][columns], boxes of 64 columns and `box_rows` rows.
+int map_of(CUtensorMap *map, const void *p, int64_t ld, int64_t rows, int64_t columns, int dtype, int box_rows) { return make_map(map, p, ld, rows, columns, dtype, box_rows); }
+
+template <class T, int KIND, bool ENT> int launch_product(const CUtensorMap &ma, const CUtensorMap &mb, ProductArgs a, int64_t K, int group, int splits, cudaStream_t s)
+{
+    const int64_t tm = div_up(a.M, kTile), tn = div_up(a.N, kTile);
+    if (tm * tn * splits > 0x3fffffff) return SPDY_ERR_UNSUPPORTED;
+    a.tiles_m = static_cast<int>(tm), a.tiles_n = static_cast<int>(tn), a.splits = splits;
+    a.group = group < a.tiles_m ? group : a.tiles_m;
+    a.k_blocks = static_cast<int>(div_up(K, kStageK));
+    if (static_cast<int64_t>(a.group) * a.tiles_n > 0x3fffffff) return SPDY_ERR_UNSUPPORTED;
+    const int items = a.tiles_m * a.tiles_n * splits, pairs = sm_count() / 2;
+    auto *kernel = product_kernel<T, KIND, ENT>;
+    SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<KIND>()));
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(static_cast<unsigned>((items < pairs ? items : pairs) * 2));
+    config.blockDim = dim3(kThreads);
+    config.dynamicSmemBytes = smem_bytes<KIND>();
+    config.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    config.attrs = attr, config.numAttrs = 1;
+    SPDY_EVAL_TRY(cudaLaunchKernelEx(&config, kernel, ma, mb, a));
+    return SPDY_OK;
+}
+
+// Tiles down that are worked on side by side: in a product over the width, as many as leave their rows of hidden (or of the piece) in L2.
+int group_of(int64_t K)
+{
+    const int64_t g = (48ll << 20) / (kTile * K * 2);
+    return static_cast<int>(g < 8 ? 8 : g > 4096 ? 4096 : g);
+}
+
+#define HEAD_TRY(expr)                     \
+    do {                                   \
+        const int rc__ = (expr);           \
+        if (rc__ != SPDY_OK) return rc__;  \
+    } while (0)
+
+template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
+{
+    const Layout l = lay_out(h.hidden, h.ldh, h.weight, h.ldw, h.R, h.V, h.D, h.stats, h.grads);
+    char *ws = static_cast<char *>(workspace);
+    const int64_t R = h.R, V = h.V, D = h.D;
+    Repack p = {};
+    p.K = D, p.ldto = packed_ld(D);
+    if (!tma_ok(h.hidden, h.ldh)) {
+        p.from[0] = static_cast<const uint16_t *>(h.hidden), p.ld[0] = h.ldh, p.rows[0] = R, p.to[0] = reinterpret_cast<uint16_t *>(ws + l.hidden);
+        h.hidden = ws + l.hidden, h.ldh = p.ldto;
+    }
+    if (!tma_ok(h.weight, h.ldw)) {
+        p.from[1] = static_cast<const uint16_t *>(h.weight), p.ld[1] = h.ldw, p.rows[1] = V, p.to[1] = reinterpret_cast<uint16_t *>(ws + l.weight);
+        h.weight = ws + l.weight, h.ldw = p.ldto;
+    }
+    if (p.to[0] || p.to[1]) {
+        const int64_t rows = p.rows[0] > p.rows[1] ? p.rows[0] : p.rows[1], blocks = div_up(rows * (p.ldto / 8), 256);
+        repack_kernel<<<dim3(static_cast<unsigned>(blocks < 2368 ? blocks : 2368), 2), 256, 0, s>>>(p);
+        HEAD_TRY(finish_launch());
+    }
+    CUtensorMap hidden, weight;
+    HEAD_TRY(map_of(&hidden, h.hidden, h.ldh, R, D, h.dtype, BM));
+    HEAD_TRY(map_of(&weight, h.weight, h.ldw, V, D, h.dtype, BM));
+
+    RowArgs rows = {};
+    rows.R = R, rows.V = V, rows.padded_rows = l.padded_rows;
+    rows.tokens = h.tokens, rows.index_bits = h.index_bits, rows.c = kLog2e / h.temperature, rows.temperature = h.temperature;
+    rows.in_lse = h.in_lse, rows.in_entropy = h.in_entropy, rows.logprob = h.logprob, rows.entropy = h.entropy, rows.lse = h.lse;
+    rows.grad_logprob = h.grad_logprob, rows.grad_entropy = h.grad_entropy;
+    ProductArgs base = {};
+    base.bias = h.bias, base.bias_type = h.bias_type, base.tokens = h.tokens, base.index_bits = h.index_bits;
+    base.c = rows.c, base.padded_rows = l.padded_rows;
+    if (h.grads) {
+        rows.consts = reinterpret_cast<float *>(ws + l.consts);
+        if (h.dtype == SPDY_F16) {
+            rows.scale_bits = reinterpret_cast<uint32_t *>(ws + l.scale);
+            SPDY_EVAL_TRY(cudaMemsetAsync(rows.scale_bits, 0, 4, s));
+        }
+        base.consts = rows.consts, base.scale_bits = rows.scale_bits;
+    }
+    if (h.stats) {
+        ProductArgs a = base;
+        a.M = R, a.N = V;
+        a.partial = reinterpret_cast<float *>(ws + l.partial);
+        a.token_logit = h.tokens ? reinterpret_cast<float *>(ws + l.token_logit) : nullptr;
+        HEAD_TRY((launch_product<T, kStats, true>(hidden, weight, a, D, group_of(D), 1, s)));
+        rows.partial = a.partial, rows.token_logit = a.token_logit, rows.tiles = static_cast<int>(div_up(V, kTile));
+        rows_kernel<<<static_cast<unsigned>(div_up(R, 32)), 32 * kRowWarps, 0, s>>>(rows);
+    } else {
+        saved_rows_kernel<<<static_cast<unsigned>(div_up(R, 256)), 256, 0, s>>>(rows);
+    }
+    HEAD_TRY(finish_launch());
+    if (!h.grads) return SPDY_OK;
+
+    CUtensorMap hidden_columns, weight_columns;
+    HEAD_TRY(map_of(&hidden_columns, h.hidden, h.ldh, R, D, h.dtype, BK));
+    HEAD_TRY(map_of(&weight_columns, h.weight, h.ldw, V, D, h.dtype, BK));
+    float *hidden_parts = reinterpret_cast<float *>(ws + l.parts), *weight_parts = hidden_parts + static_cast<size_t>(l.hidden_splits) * R * l.ld_parts;
+    const unsigned finish_blocks = static_cast<unsigned>(sm_count()) * 8;
+    for (int64_t v0 = 0; v0 < V; v0 += l.width) {
+        const int64_t n = V - v0 < l.width ? V - v0 : l.width;
+        ProductArgs a = base;
+        a.M = R, a.N = n, a.v0 = v0, a.b_row0 = static_cast<int>(v0);
+        a.out = ws + l.piece, a.ldo = l.width;
+        if (h.dbias) a.column_sums = reinterpret_cast<float *>(ws + l.sums), a.ld_sums = l.width;
+        if (h.grad_entropy) HEAD_TRY((launch_product<T, kGrad, true>(hidden, weight, a, D, group_of(D), 1, s)));
+        else HEAD_TRY((launch_product<T, kGrad, false>(hidden, weight, a, D, group_of(D), 1, s)));
+        if (h.dbias) {
+            bias_kernel<<<static_cast<unsigned>(div_up(n, 32)), 256, 0, s>>>(a.column_sums, div_up(R, 32), n, l.width, base.scale_bits, h.dbias + v0);
+            HEAD_TRY(finish_launch());
+        }
+        CUtensorMap piece, piece_columns;
+        if (h.dhidden) {
+            HEAD_TRY(map_of(&piece, ws + l.piece, l.width, R, n, h.dtype, BM));
+            ProductArgs b = {};
+            b.M = R, b.N = D, b.b_row0 = static_cast<int>(v0), b.out = hidden_parts, b.ldo = l.ld_parts, b.add = v0 > 0;
+            HEAD_TRY((launch_product<T, kHidden, false>(piece, weight_columns, b, n, 8, l.hidden_splits, s)));
+        }
+        if (h.dweight) {
+            HEAD_TRY(map_of(&piece_columns, ws + l.piece, l.width, R, n, h.dtype, BK));
+            ProductArgs b = {};
+            b.M = n, b.N = D;
+            T *out = static_cast<T *>(h.dweight) + v0 * h.lddw;
+            if (l.weight_splits == 1) {
+                b.out = out, b.ldo = h.lddw, b.scale_bits = base.scale_bits;
+                b.sectors = aligned(out, 32) && h.lddw % 16 == 0;
+                HEAD_TRY((launch_product<T, kWeight, false>(piece_columns, hidden_columns, b, R, 8, 1, s)));
+            } else {
+                b.out = weight_parts, b.ldo = l.ld_parts;
+                HEAD_TRY((launch_product<T, kWeightParts, false>(piece_columns, hidden_columns, b, R, 8, l.weight_splits, s)));
+                finish_kernel<T><<<finish_blocks, 256, 0, s>>>(weight_parts, l.weight_splits, n, D, l.ld_parts, base.scale_bits, out, h.lddw);
+                HEAD_TRY(finish_launch());
+            }
+        }
+    }
+    if (h.dhidden) {
+        finish_kernel<T><<<finish_blocks, 256, 0, s>>>(hidden_parts, l.hidden_splits, R, D, l.ld_parts, base.scale_bits, static_cast<T *>(h.dhidden), h.lddh);
+        HEAD_TRY(finish_launch());
+    }
+    return SPDY_OK;
+}
+
+constexpr int64_t kMost = 0x7fff0000;  // rows, ids, width: tile coordinates are 32-bit
+
+bool head_ok(const HeadArgs &h)
+{
+    if (!half_type(h.dtype) || h.R < 0 || h.V < 1 || h.D < 1 || h.R > kMost || h.V > kMost || h.D > kMost || h.ldw < h.D || !temperature_ok(h.temperature)) return false;
+    if (!h.weight || !aligned(h.weight, 2)) return false;
+    if (h.bias && ((h.bias_type != h.dtype && h.bias_type != SPDY_F32) || !aligned(h.bias, type_size(h.bias_type)))) return false;
+    if (h.tokens && ((h.index_bits != 32 && h.index_bits != 64) || !aligned(h.tokens, h.index_bits / 8))) return false;
+    return h.R == 0 || (h.hidden && aligned(h.hidden, 2) && h.ldh >= h.D);
+}
+
+// Whether two matrices of 16-bit elements share memory (rows of one buffer that lie side by side do not, and are not told apart here
+// unless their strides are the same).
+bool overlap(const void *p, int64_t ldp, int64_t rows_p, const void *q, int64_t ldq, int64_t rows_q, int64_t columns)
+{
+    if (!p || !q || rows_p <= 0 || rows_q <= 0) return false;
+    const uint64_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    const uint64_t a1 = a + static_cast<uint64_t>((rows_p - 1) * ldp + columns) * 2, b1 = b + static_cast<uint64_t>((rows_q - 1) * ldq + columns) * 2;
+    if (a1 <= b || b1 <= a) return false;
+    if (ldp != ldq) return true;
+    const uint64_t stride = static_cast<uint64_t>(ldp) * 2, between = (a > b ? a - b : b - a) % stride;
+    return between < static_cast<uint64_t>(columns) * 2 || between > stride - static_cast<uint64_t>(columns) * 2;
+}
+
+bool grads_ok(const HeadArgs &h)
+{
+    if (h.dhidden && h.R > 0 && (!aligned(h.dhidden, 2) || h.lddh < h.D)) return false;
+    if (h.dweight && (!aligned(h.dweight, 2) || h.lddw < h.D)) return false;
+    return !overlap(h.dhidden, h.lddh, h.R, h.hidden, h.ldh, h.R, h.D) && !overlap(h.dhidden, h.lddh, h.R, h.weight, h.ldw, h.V, h.D) &&
+           !overlap(h.dweight, h.lddw, h.V, h.hidden, h.ldh, h.R, h.D) && !overlap(h.dweight, h.lddw, h.V, h.weight, h.ldw, h.V, h.D) &&
+           !overlap(h.dweight, h.lddw, h.V, h.dhidden, h.lddh, h.R, h.D);
+}
+
+int run(const HeadArgs &h, void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    if (h.R == 0) {  // gradients of no rows are 0
+        if (h.grads && h.dweight) SPDY_EVAL_TRY(cudaMemset2DAsync(h.dweight, static_cast<size_t>(h.lddw) * 2, 0, static_cast<size_t>(h.D) * 2, static_cast<size_t>(h.V), s));
+        if (h.grads && h.dbias) SPDY_EVAL_TRY(cudaMemsetAsync(h.dbias, 0, static_cast<size_t>(h.V) * 4, s));
+        return SPDY_OK;
+    }
+    if (!workspace || !aligned(workspace, 256)) return SPDY_ERR_INVALID_ARG;
+    if (workspace_bytes < lay_out(h.hidden, h.ldh, h.weight, h.ldw, h.R, h.V, h.D, h.stats, h.grads).total) return SPDY_ERR_WORKSPACE_TOO_SMALL;
+    return h.dtype == SPDY_BF16 ? run_head<__nv_bfloat16>(h, workspace, s) : run_head<__half>(h, workspace, s);
+}
+
+HeadArgs head(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int dtype, const void *bias, int bias_dtype, const void *tokens, int index_bits, int64_t R,
+              int64_t V, int64_t D, float temperature)
+{
+    HeadArgs h = {};
+    h.hidden = hidden, h.ldh = ldh, h.weight = weight, h.ldw = ldw, h.dtype = dtype, h.bias = bias, h.bias_type = bias_dtype, h.tokens = tokens, h.index_bits = index_bits;
+    h.R = R, h.V = V, h.D = D, h.temperature = temperature;
+    return h;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t spdy_linear_token_logprobs_workspace_bytes(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int dtype, int64_t R, int64_t V, int64_t D, int forward,
+                                                  int gradients)
+{
+    if (!half_type(dtype) || R <= 0 || V <= 0 || D <= 0 || R > kMost || V > kMost || D > kMost) return 0;
+    return lay_out(hidden, ldh, weight, ldw, R, V, D, forward != 0, gradients != 0).total;
+}
+
+int spdy_linear_token_logprobs(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int dtype, const void *bias, int bias_dtype, const void *tokens, int index_bits,
+                               int64_t R, int64_t V, int64_t D, float temperature, float *logprob, float *entropy, float *lse, void *workspace, size_t workspace_bytes,
+                               void *cuda_stream)
+{
+    HeadArgs h = head(hidden, ldh, weight, ldw, dtype, bias, bias_dtype, tokens, index_bits, R, V, D, temperature);
+    h.logprob = logprob, h.entropy = entropy, h.lse = lse, h.stats = true;
+    if (!head_ok(h) || (R > 0 && logprob && !tokens)) return SPDY_ERR_INVALID_ARG;
+    return run(h, workspace, workspace_bytes, cuda_stream);
+}
+
+int spdy_linear_token_logprobs_backward(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int dtype, const void *bias, int bias_dtype, const void *tokens,
+                                        int index_bits, int64_t R, int64_t V, int64_t D, float temperature, const float *lse, const float *entropy,
+                                        const float *grad_logprob, const float *grad_entropy, void *dhidden, int64_t lddh, void *dweight, int64_t lddw, float *dbias,
+                                        void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    HeadArgs h = head(hidden, ldh, weight, ldw, dtype, bias, bias_dtype, tokens, index_bits, R, V, D, temperature);
+    h.in_lse = lse, h.in_entropy = entropy, h.grad_logprob = grad_logprob, h.grad_entropy = grad_entropy;
+    h.dhidden = dhidden, h.lddh = lddh, h.dweight = dweight, h.lddw = lddw, h.dbias = dbias, h.grads = true;
+    if (!head_ok(h) || !grads_ok(h)) return SPDY_ERR_INVALID_ARG;
+    if (R > 0 && (!lse || (grad_logprob && !tokens) || (grad_entropy && !entropy))) return SPDY_ERR_INVALID_ARG;
+    return run(h, workspace, workspace_bytes, cuda_stream);
+}
+
+int spdy_linear_token_logprobs_with_grad(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int dtype, const void *bias, int bias_dtype, const void *tokens,
+                                         int index_bits, int64_t R, int64_t V, int64_t D, float temperature, const float *grad_logprob, const float *grad_entropy,
+                                         float *logprob, float *entropy, float *lse, void *dhidden, int64_t lddh, void *dweight, int64_t lddw, float *dbias, void *workspace,
+                                         size_t workspace_bytes, void *cuda_stream)
+{
+    HeadArgs h = head(hidden, ldh, weight, ldw, dtype, bias, bias_dtype, tokens, index_bits, R, V, D, temperature);
+    h.grad_logprob = grad_logprob, h.grad_entropy = grad_entropy, h.logprob = logprob, h.entropy = entropy, h.lse = lse;
+    h.dhidden = dhidden, h.lddh = lddh, h.dweight = dweight, h.lddw = lddw, h.dbias = dbias, h.stats = h.grads = true;
+    if (!head_ok(h) || !grads_ok(h) || (R > 0 && (logprob || grad_logprob) && !tokens)) return SPDY_ERR_INVALID_ARG;
+    return run(h, workspace, workspace_bytes, cuda_stream);
+}
+
+}  // extern "C"

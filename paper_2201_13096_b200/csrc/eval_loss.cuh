@@ -1253,7 +1253,6 @@ inline bool rows_ok(const void *p, int64_t ld, int dtype, int64_t R, int64_t V)
 {
     return known_type(dtype) && R >= 0 && V >= 1 && V <= kMostColumns && ld >= V && (R == 0 || (p && aligned(p, type_size(dtype))));
 }
-inline bool temperature_ok(float t) { return t > 0.f && t <= 3.4e38f && kLog2e / t <= 3.4e38f && kLog2e / t > 0.f; }
 
 }  // namespace spdy_eval
 #endif

@@ -22,13 +22,15 @@ from . import binding
 EXPORTS = (
     "spdy_linear", "spdy_linear_workspace_bytes", "spdy_linear_check_status", "spdy_layer_norm", "spdy_layer_norm_backward",
     "spdy_layer_norm_backward_workspace_bytes", "spdy_token_logprobs", "spdy_token_logprobs_backward",
-    "spdy_token_logprobs_with_grad", "spdy_distill_loss", "spdy_distill_loss_backward", "spdy_distill_loss_with_grad",
+    "spdy_token_logprobs_with_grad", "spdy_linear_token_logprobs", "spdy_linear_token_logprobs_backward",
+    "spdy_linear_token_logprobs_with_grad", "spdy_linear_token_logprobs_workspace_bytes", "spdy_distill_loss", "spdy_distill_loss_backward", "spdy_distill_loss_with_grad",
 )
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 SPDY_TOP_MAX, SPDY_DISTILL_MAX = 128, 256
 
-__all__ = ["TokenLogprobs", "DistillLoss", "linear", "linear_check_status", "layer_norm", "layer_norm_backward", "token_logprobs",
-           "token_logprobs_backward", "token_logprobs_with_grad", "distill_loss", "distill_loss_backward",
+__all__ = ["TokenLogprobs", "LinearGrads", "DistillLoss", "linear", "linear_check_status", "layer_norm", "layer_norm_backward", "token_logprobs",
+           "token_logprobs_backward", "token_logprobs_with_grad", "linear_token_logprobs", "linear_token_logprobs_backward",
+           "linear_token_logprobs_with_grad", "distill_loss", "distill_loss_backward",
            "distill_loss_with_grad"]
 
 
@@ -40,6 +42,14 @@ class TokenLogprobs(NamedTuple):
     lse: object
     top_ids: Optional[object] = None
     top_logprobs: Optional[object] = None
+
+
+class LinearGrads(NamedTuple):
+    """Gradients by a linear layer's input, weight and bias; None where they were not asked for."""
+
+    dhidden: object
+    dweight: object
+    dbias: Optional[object] = None
 
 
 class DistillLoss(NamedTuple):
@@ -62,6 +72,7 @@ def _load():
         vp, i32, i64, f32, size, cint = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t,
                                          ctypes.c_int)
         rows = [vp, i64, cint, vp, cint]
+        head = [vp, i64, vp, i64, cint, vp, cint, vp, cint, i64, i64, i64, f32]
         for name, result, args in (
             ("spdy_linear_workspace_bytes", size, [vp, i64, vp, i64, cint, i64, i64, i64]),
             ("spdy_linear", cint, [vp, i64, vp, i64, cint, vp, cint, vp, i64, cint, i64, i64, i64, vp, i64, cint, vp, size, vp]),
@@ -72,6 +83,10 @@ def _load():
             ("spdy_token_logprobs", cint, rows + [i64, i64, f32, i32, vp, vp, vp, vp, vp, vp]),
             ("spdy_token_logprobs_backward", cint, rows + [i64, i64, f32, vp, vp, vp, vp, vp, i64, vp]),
             ("spdy_token_logprobs_with_grad", cint, rows + [i64, i64, f32, vp, vp, vp, vp, vp, vp, i64, vp]),
+            ("spdy_linear_token_logprobs_workspace_bytes", size, [vp, i64, vp, i64, cint, i64, i64, i64, cint, cint]),
+            ("spdy_linear_token_logprobs", cint, head + [vp, vp, vp, vp, size, vp]),
+            ("spdy_linear_token_logprobs_backward", cint, head + [vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, size, vp]),
+            ("spdy_linear_token_logprobs_with_grad", cint, head + [vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, size, vp]),
             ("spdy_distill_loss", cint, rows + [vp, i64, i64, i32, f32, cint, vp, vp, vp, vp]),
             ("spdy_distill_loss_backward", cint, rows + [vp, i64, i64, i32, f32, cint, vp, vp, vp, vp, i64, vp]),
             ("spdy_distill_loss_with_grad", cint, rows + [vp, i64, i64, i32, f32, cint, vp, vp, vp, vp, vp, i64, vp]),
@@ -402,6 +417,107 @@ def token_logprobs_with_grad(logits, tokens, grad_logprob=None, grad_entropy=Non
     if rc:
         binding._check(rc, "spdy_token_logprobs_with_grad")
     return TokenLogprobs(logprob, entropy, lse), out
+
+
+def _head(hidden, weight, tokens, bias, temperature):
+    """The C calls' common arguments, and what the outputs are made from: rows, ids, width, device and the workspace query's share."""
+    dtype = hidden.dtype
+    code = _TYPES.get(dtype, 0)
+    if not code:
+        raise ValueError("hidden must be bfloat16 or float16")
+    R, D, ldh, dev = _rows(hidden, "hidden")
+    V, d, ldw, wdev = _rows(weight, "weight")
+    if d != D or wdev != dev or weight.dtype != dtype:
+        raise ValueError(f"weight must be [V][{D}] of {dtype} on cuda:{dev}")
+    pb, bcode = None, 0
+    if bias is not None:
+        pb, bcode = _vector(bias, "bias", V, dev), _TYPES.get(bias.dtype, -1)
+        if bcode and bcode != code:
+            raise ValueError("bias must have hidden's type or be float32")
+    bits = _ids(tokens, "tokens", (R,), dev)
+    query = (hidden.data_ptr(), ldh, weight.data_ptr(), ldw, code)
+    return (*query, pb, bcode, tokens.data_ptr(), bits, R, V, D, temperature), R, V, D, dev, query
+
+
+def _head_workspace(lib, query, R, V, D, forward, gradients):
+    need = lib.spdy_linear_token_logprobs_workspace_bytes(*query, R, V, D, forward, gradients)
+    ws = _empty_strided((need,), (1,), torch.uint8) if need else None
+    return _ptr(ws), need, ws
+
+
+def _head_grads(hidden, weight, bias, R, V, D, dev, wanted, dhidden, dweight):
+    """``LinearGrads`` to write, and the C calls' arguments for them."""
+    unknown = set(wanted) - {"hidden", "weight", "bias"}
+    if unknown:
+        raise ValueError(f"wanted names hidden, weight and bias, not {sorted(unknown)}")
+    if (dhidden is not None and "hidden" not in wanted) or (dweight is not None and "weight" not in wanted):
+        raise ValueError("a gradient's tensor is given, and the gradient is not wanted")
+    ldh = ldw = D
+    if "hidden" in wanted:
+        if dhidden is None:
+            dhidden = _matrix(R, D, hidden.dtype)
+        else:
+            ldh = _like(dhidden, "dhidden", R, D, hidden.dtype, dev)
+    if "weight" in wanted:
+        if dweight is None:
+            dweight = _matrix(V, D, hidden.dtype)
+        else:
+            ldw = _like(dweight, "dweight", V, D, hidden.dtype, dev)
+    dbias = _vectors(1, V)[0] if "bias" in wanted and bias is not None else None
+    return LinearGrads(dhidden, dweight, dbias), (_ptr(dhidden), ldh, _ptr(dweight), ldw, _ptr(dbias))
+
+
+def linear_token_logprobs(hidden, weight, tokens, bias=None, temperature: float = 1.0, stream=None) -> TokenLogprobs:
+    """``spdy_linear_token_logprobs``: ``token_logprobs(hidden @ weight.T + bias, tokens)`` without the table of logits.
+
+    ``hidden`` [R][D] and ``weight`` [V][D] bfloat16 or float16 (the same), ``bias`` [V] of that type or float32 (-inf: id not
+    allowed), ``tokens`` [R] int32 or int64 (negative = none).  ``logprob``, ``entropy`` and ``lse`` [R] are float32."""
+    lib = _lib or _load()
+    head, R, V, D, dev, query = _head(hidden, weight, tokens, bias, temperature)
+    with _Scope(dev, stream) as handle:
+        logprob, entropy, lse = _vectors(3, R)
+        pws, need, ws = _head_workspace(lib, query, R, V, D, 1, 0)
+        rc = lib.spdy_linear_token_logprobs(*head, logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), pws, need, handle)
+    if rc:
+        binding._check(rc, "spdy_linear_token_logprobs")
+    return TokenLogprobs(logprob, entropy, lse)
+
+
+def linear_token_logprobs_backward(hidden, weight, tokens, lse, entropy=None, grad_logprob=None, grad_entropy=None, bias=None,
+                                   temperature: float = 1.0, wanted=("hidden", "weight", "bias"), dhidden=None, dweight=None,
+                                   stream=None) -> LinearGrads:
+    """``spdy_linear_token_logprobs_backward``: the gradients of ``sum(grad_logprob * logprob + grad_entropy * entropy)`` by
+    ``hidden``, ``weight`` (their type) and, where there is one, ``bias`` (float32), from the forward call's ``lse`` and (with
+    ``grad_entropy``) ``entropy``.  ``wanted`` names the ones to compute; ``dhidden`` and ``dweight`` may be given, with rows of
+    any stride, and are overwritten."""
+    lib = _lib or _load()
+    head, R, V, D, dev, query = _head(hidden, weight, tokens, bias, temperature)
+    vectors = _optional(R, dev, lse=lse, entropy=entropy, grad_logprob=grad_logprob, grad_entropy=grad_entropy)
+    with _Scope(dev, stream) as handle:
+        grads, outs = _head_grads(hidden, weight, bias, R, V, D, dev, wanted, dhidden, dweight)
+        pws, need, ws = _head_workspace(lib, query, R, V, D, 0, 1)
+        rc = lib.spdy_linear_token_logprobs_backward(*head, *vectors, *outs, pws, need, handle)
+    if rc:
+        binding._check(rc, "spdy_linear_token_logprobs_backward")
+    return grads
+
+
+def linear_token_logprobs_with_grad(hidden, weight, tokens, grad_logprob=None, grad_entropy=None, bias=None, temperature: float = 1.0,
+                                    wanted=("hidden", "weight", "bias"), dhidden=None, dweight=None, stream=None):
+    """``spdy_linear_token_logprobs_with_grad``: (``TokenLogprobs``, ``LinearGrads``) in one call, for a loss whose weights per row
+    are known beforehand."""
+    lib = _lib or _load()
+    head, R, V, D, dev, query = _head(hidden, weight, tokens, bias, temperature)
+    vectors = _optional(R, dev, grad_logprob=grad_logprob, grad_entropy=grad_entropy)
+    with _Scope(dev, stream) as handle:
+        logprob, entropy, lse = _vectors(3, R)
+        grads, outs = _head_grads(hidden, weight, bias, R, V, D, dev, wanted, dhidden, dweight)
+        pws, need, ws = _head_workspace(lib, query, R, V, D, 1, 1)
+        rc = lib.spdy_linear_token_logprobs_with_grad(*head, *vectors, logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), *outs, pws,
+                                                      need, handle)
+    if rc:
+        binding._check(rc, "spdy_linear_token_logprobs_with_grad")
+    return TokenLogprobs(logprob, entropy, lse), grads
 
 
 def _teacher(top_ids, top_logprobs, R, dev):
