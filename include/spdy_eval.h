@@ -195,6 +195,60 @@ int spdy_distill_loss_with_grad(const void *logits, int64_t ld, int dtype, const
                                 const float *grad_loss, float *loss, float *lse, float *rest, void *dlogits, int64_t lddl,
                                 void *cuda_stream);
 
+/*
+ * An AdamW step over many tensors at once.  For each element, with t = step:
+ *   g = grad grad_scale,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32, each operation rounded; the square root and the quotient within 2^-21 of themselves.  With a master copy it is the
+ * copy that is stepped, and param that is rounded from it.
+ *   tensors, options: host memory, read before the call returns.  A tensor is n contiguous elements; param, grad and master need
+ *   the alignment of their types, m and v 16 bytes.  grad NULL: the tensor is left alone.  Memory that is written may belong to one
+ *   tensor only.
+ *   state_bits 32: m, v fp32 [n].  state_bits 8: m, v bytes [n], m_exp, v_exp bytes [ceil(n / 32)]; all 0 to begin with.
+ *     32 consecutive elements share E, the fp32 exponent field (at least 1) of the largest magnitude among them; E = 255: the block
+ *     holds a value that is not finite, or one from 2^127 on, and all of it reads as NaN.  Relative to 2^(E - 127) an element is a
+ *     floating-point number with 3 bits of mantissa: m has a sign and 4 bits of exponent, field 14 being the binade of the largest
+ *     (so that m ends at 2^-16 to 2^-17 of the largest); v has 5 bits, field 30 (2^-31 to 2^-32).  Rounding is stochastic, by 20 random
+ *     bits; a positive v is never rounded to 0.  The update uses m and v as they are before this rounding.
+ *   keep_zeros: elements whose weight (master, where there is one) is 0 stay 0, and so do their m and v: pruned weights stay pruned.
+ *   rounding of 16-bit params without a master: 0 to nearest, 1 stochastic (a change of less than half a step is lost to nearest).
+ *   Random bits are a hash of (seed, t modulo 2^32, index in `tensors`, element): the same call gives the same bits.
+ *   step >= 1.  step_device, lr_device: device scalars used instead of step and lr, read when the kernel runs, for captured steps
+ *   (lr_device needs step_device; a step below 1 counts as 1).  grad_scale, skip: device scalars or NULL; with *skip != 0 nothing is
+ *   changed.  Infinities and NaN in grad are not looked for.
+ */
+typedef struct spdy_adamw_tensor {
+    void *param;
+    const void *grad;
+    float *master; /* NULL, or fp32 [n]: only with 16-bit params */
+    void *m, *v;
+    uint8_t *m_exp, *v_exp;
+    int64_t n;
+    float weight_decay;
+    int32_t param_dtype, grad_dtype; /* grad: param's type or SPDY_F32 */
+    int32_t state_bits, keep_zeros;
+    int32_t reserved; /* 0 */
+} spdy_adamw_tensor;
+
+typedef struct spdy_adamw_options {
+    double lr, beta1, beta2, eps; /* 0 <= beta < 1, eps >= 0 */
+    int64_t step;
+    uint32_t seed;
+    int32_t rounding;
+    const float *lr_device;
+    const int64_t *step_device;
+    const float *grad_scale, *skip;
+} spdy_adamw_options;
+
+int spdy_adamw_step(const spdy_adamw_tensor *tensors, int32_t count, const spdy_adamw_options *options, void *cuda_stream);
+
+/*
+ * The moments of tensors with state_bits 8 as numbers: m_out[i], v_out[i] (host arrays of device pointers) receive n elements of
+ * `out_dtype`, SPDY_F32 or SPDY_BF16 (both hold them exactly; below 2^-133 bf16 rounds).  param, grad and master are not looked at.
+ */
+int spdy_adamw_moments(const spdy_adamw_tensor *tensors, int32_t count, void *const *m_out, void *const *v_out, int out_dtype,
+                       void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

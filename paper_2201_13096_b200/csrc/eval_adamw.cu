@@ -1,0 +1,401 @@
+// AdamW steps over many tensors at once, with moments in 32 or in 8 bits: kernels and C entries (spdy_eval.h).
+//
+//   g = grad * grad_scale,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+//   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps)
+//
+// Moments in 8 bits: 32 consecutive elements share a byte E, the fp32 exponent field (at least 1) of the largest magnitude among
+// them; an element y is a small floating-point number relative to 2^(E - 127), and fp32's own layout does the conversion: times a
+// power of two that puts the block's largest into exponent field 14 (first moment: sign, 4 bits of exponent, 3 of mantissa) or 30
+// (second: 5 and 3), the upper bits of y's pattern ARE the code, its lower 20 bits the part cut off, fields of 0 included, since fp32
+// has them too.  20 random bits added before the cut round it up with the right probability: an average that moves by 1 - beta2 = 0.1 %
+// of itself a step would stand still under rounding to nearest, with steps of 6 to 12 %.  A positive second moment is never rounded to
+// 0: its floor, 2^-32 of the block's largest, is what keeps m / sqrt(v) of small elements bounded (m itself ends at 2^-17).
+// The random bits are a hash of (seed, step, tensor, element), so a step can be repeated bit for bit.
+#include "eval_common.cuh"
+
+using namespace spdy_eval;
+
+namespace {
+
+constexpr int kThreads = 256, kPer = 8, kChunk = kThreads * kPer;  // elements a thread and a block work on at a time
+constexpr int kBlock = 32;                                        // elements that share an exponent
+
+struct Entry {
+    void *param;
+    const void *grad;
+    float *master;
+    void *m, *v;
+    uint8_t *m_exp, *v_exp;
+    int64_t n;
+    uint32_t first;       // chunks of the tensors before it
+    float weight_decay;
+    uint32_t index;       // in the caller's list
+    uint32_t flags;       // kWide*, kKeepZeros
+};
+enum { kWideParam = 1, kWideGrad = 2, kWideMaster = 4, kKeepZeros = 8 };
+
+struct StepArgs {
+    float b1, b2, g1, g2, eps, rate, root;  // g1 = 1 - b1, rate = lr / (1 - b1^t), root = 1 / sqrt(1 - b2^t)
+    double lr, beta1, beta2;
+    uint32_t seed, key;                     // key: of seed and step
+    const float *lr_device, *grad_scale, *skip;
+    const int64_t *step_device;
+};
+
+// As many tensors as a launch's parameters (32764 bytes) hold; few of them for small calls, whose launch then copies less.
+template <int CAP> struct Table {
+    Entry e[CAP];
+    uint32_t count, chunks;
+};
+constexpr int kFew = 16, kMany = 360;
+
+// A hash of 32 bits: two odd multipliers, each of which carries bits up, and shifts that bring them down again.
+SPDY_EVAL_FN uint32_t mix(uint32_t x)
+{
+    x = (x ^ (x >> 16)) * 0x7feb352du;
+    x = (x ^ (x >> 15)) * 0x846ca68bu;
+    return x ^ (x >> 16);
+}
+
+__device__ __forceinline__ float exponent(int field) { return __int_as_float(field << 23); }  // 2^(field - 127), 1 <= field <= 254
+
+// 2^(E - 127) of a stored byte; 255 marks a block that is not finite, 0 comes with codes of 0 only (a fresh state)
+__device__ __forceinline__ float block_scale(uint32_t E) { return E == 255 ? quiet_nan() : E == 0 ? __int_as_float(1 << 22) : exponent(static_cast<int>(E)); }
+
+template <bool SIGNED> __device__ __forceinline__ float decode(uint32_t code, float scale)
+{
+    constexpr float up = SIGNED ? 0x1p113f : 0x1p97f;
+    if (!SIGNED) return __uint_as_float(code << 20) * up * scale;
+    return __uint_as_float((code & 0x80u) << 24 | (code & 0x7fu) << 20) * up * scale;
+}
+
+// Codes of a thread's eight elements (a quarter of a block: four neighbouring lanes), and the block's byte.
+template <bool SIGNED> __device__ __forceinline__ uint2 encode(const float *y, const uint32_t *random, uint32_t &E)
+{
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) most = max(most, __float_as_uint(y[i]) & 0x7fffffffu);
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    E = max(most >> 23, 1u);
+    const bool bad = E >= 254;
+    const float down = bad ? 0.f : exponent(254 - static_cast<int>(E));
+    if (bad) E = 255;
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const float scaled = fabsf(y[i]) * down * (SIGNED ? 0x1p-113f : 0x1p-97f);
+        uint32_t code = (__float_as_uint(scaled) + (SIGNED ? random[i] & 0xfffffu : random[i] >> 12)) >> 20;
+        if (SIGNED) code |= __float_as_uint(y[i]) >> 24 & 0x80u;
+        else if (y[i] > 0.f) code = max(code, 1u);
+        w[i / 4] |= (bad ? 0u : code) << 8 * (i % 4);
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+// Eight elements from e on of a vector of n; `wide`: they may be moved 16 bytes at a time.
+template <class T> __device__ __forceinline__ void load8(const T *p, int64_t e, int64_t n, bool wide, float *f)
+{
+    if (wide && e + kPer <= n) {
+        const uint4 *q = reinterpret_cast<const uint4 *>(p + e);
+        Elem<T>::unpack(load_stream(q), f);
+        if (sizeof(T) == 4) Elem<T>::unpack(load_stream(q + 1), f + 4);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) f[i] = e + i < n ? Elem<T>::to_float(p[e + i]) : 0.f;
+    }
+}
+template <class T> __device__ __forceinline__ void store8(T *p, int64_t e, int64_t n, bool wide, const float *f)
+{
+    if (wide && e + kPer <= n) {
+        uint4 *q = reinterpret_cast<uint4 *>(p + e);
+        store_stream(q, Elem<T>::pack(f));
+        if (sizeof(T) == 4) store_stream(q + 1, Elem<T>::pack(f + 4));
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (e + i < n) p[e + i] = Elem<T>::from_float(f[i]);
+    }
+}
+__device__ __forceinline__ uint2 load_codes(const uint8_t *p, int64_t e, int64_t n)
+{
+    if (e + kPer <= n) return *reinterpret_cast<const uint2 *>(p + e);
+    uint32_t w[2] = {0, 0};
+    for (int i = 0; i < kPer && e + i < n; ++i) w[i / 4] |= static_cast<uint32_t>(p[e + i]) << 8 * (i % 4);
+    return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void store_codes(uint8_t *p, int64_t e, int64_t n, uint2 v)
+{
+    if (e + kPer <= n) {
+        *reinterpret_cast<uint2 *>(p + e) = v;
+        return;
+    }
+    for (int i = 0; i < kPer && e + i < n; ++i) p[e + i] = static_cast<uint8_t>((i < 4 ? v.x : v.y) >> 8 * (i % 4));
+}
+
+// y to 16 bits, up with the probability of the part cut off: fp32's pattern again, brought to half precision's exponents by a power of two.
+template <class T> __device__ __forceinline__ float round_random(float y, uint32_t random)
+{
+    constexpr bool brain = std::is_same<T, __nv_bfloat16>::value;
+    constexpr int shift = brain ? 16 : 13;
+    uint32_t code = (__float_as_uint(fabsf(y) * (brain ? 1.f : 0x1p-112f)) + (random >> (32 - shift))) >> shift;
+    code = min(code, brain ? 0x7f80u : 0x7c00u) | (__float_as_uint(y) >> 16 & 0x8000u);
+    const unsigned short bits = static_cast<unsigned short>(code);
+    const float rounded = brain ? __uint_as_float(code << 16) : __half2float(__ushort_as_half(bits));
+    return fabsf(y) <= 3.4028235e38f ? rounded : y;
+}
+
+__device__ double power(double b, int64_t t)
+{
+    double r = 1.0;
+    for (; t > 0; t >>= 1, b *= b)
+        if (t & 1) r *= b;
+    return r;
+}
+
+__device__ __forceinline__ float root_of(float x)
+{
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <class P, class G, int BITS, bool MASTER, bool RANDOM, int CAP>
+__global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ StepArgs s)
+{
+    if (s.skip && *s.skip != 0.f) return;
+    __shared__ float derived[3];
+    float rate = s.rate, root = s.root;
+    double lr = s.lr;
+    uint32_t key = s.key;
+    if (s.step_device || s.lr_device) {  // a captured step reads its number and rate when it is replayed
+        const int64_t t = max(s.step_device ? *s.step_device : 1ll, 1ll);
+        if (s.lr_device) lr = *s.lr_device;
+        if (threadIdx.x == 0) derived[0] = static_cast<float>(lr / (1.0 - power(s.beta1, t)));
+        if (threadIdx.x == 32) derived[1] = static_cast<float>(1.0 / sqrt(1.0 - power(s.beta2, t)));
+        __syncthreads();
+        if (s.step_device) key = mix(mix(s.seed) + static_cast<uint32_t>(t));
+        rate = derived[0], root = derived[1];
+    }
+    const float scale = s.grad_scale ? *s.grad_scale : 1.f;
+    uint32_t at = 0;
+    for (uint32_t chunk = blockIdx.x; chunk < table.chunks; chunk += gridDim.x) {
+        while (at + 1 < table.count && chunk >= table.e[at + 1].first) ++at;
+        const Entry &t = table.e[at];
+        const int64_t n = t.n, e = static_cast<int64_t>(chunk - t.first) * kChunk + threadIdx.x * kPer;
+        float p[kPer], g[kPer], m[kPer], v[kPer];
+        if (MASTER) load8(t.master, e, n, t.flags & kWideMaster, p);
+        else load8(static_cast<const P *>(t.param), e, n, t.flags & kWideParam, p);
+        load8(static_cast<const G *>(t.grad), e, n, t.flags & kWideGrad, g);
+        if (BITS == 32) {
+            load8(static_cast<const float *>(t.m), e, n, true, m);
+            load8(static_cast<const float *>(t.v), e, n, true, v);
+        } else {
+            const uint2 cm = load_codes(static_cast<const uint8_t *>(t.m), e, n), cv = load_codes(static_cast<const uint8_t *>(t.v), e, n);
+            const float sm = e < n ? block_scale(t.m_exp[e / kBlock]) : 0.f, sv = e < n ? block_scale(t.v_exp[e / kBlock]) : 0.f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                m[i] = decode<true>((i < 4 ? cm.x : cm.y) >> 8 * (i % 4) & 0xffu, sm);
+                v[i] = decode<false>((i < 4 ? cv.x : cv.y) >> 8 * (i % 4) & 0xffu, sv);
+                if (e + i >= n) m[i] = v[i] = 0.f;  // a block that is not finite has nothing behind the tensor's end
+            }
+        }
+        const float decay = static_cast<float>(1.0 - lr * static_cast<double>(t.weight_decay));
+        uint32_t random[kPer];
+        if (BITS == 8 || RANDOM) {
+            const uint32_t start = mix(key + t.index) + static_cast<uint32_t>(e) + static_cast<uint32_t>(e >> 32) * 0x9e3779b9u;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) random[i] = mix(start + i);
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            // every product and sum rounded by itself: the 8-bit codes below are those of the plain formula, bit for bit
+            const float old = p[i], gs = g[i] * scale;
+            m[i] = m[i] * s.b1 + gs * s.g1;
+            v[i] = v[i] * s.b2 + gs * s.g2 * gs;
+            p[i] = old * decay - __fdividef(m[i] * rate, root_of(v[i]) * root + s.eps);
+            if ((t.flags & kKeepZeros) && old == 0.f) p[i] = m[i] = v[i] = 0.f;
+        }
+        if (BITS == 32) {
+            store8(static_cast<float *>(t.m), e, n, true, m);
+            store8(static_cast<float *>(t.v), e, n, true, v);
+        } else {
+            uint32_t em, ev;
+            const uint2 cm = encode<true>(m, random, em), cv = encode<false>(v, random, ev);
+            if (e < n) {
+                store_codes(static_cast<uint8_t *>(t.m), e, n, cm), store_codes(static_cast<uint8_t *>(t.v), e, n, cv);
+                if ((threadIdx.x & 3) == 0) t.m_exp[e / kBlock] = static_cast<uint8_t>(em), t.v_exp[e / kBlock] = static_cast<uint8_t>(ev);
+            }
+        }
+        if (MASTER) store8(t.master, e, n, t.flags & kWideMaster, p);
+        if (RANDOM)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) p[i] = round_random<P>(p[i], random[i] * 0x9e3779b1u);
+        store8(static_cast<P *>(t.param), e, n, t.flags & kWideParam, p);
+    }
+}
+
+// Moments in 8 bits as numbers.  param and master of the table: where the first and the second go.
+template <class T, int CAP> __global__ void __launch_bounds__(kThreads) moments_kernel(const __grid_constant__ Table<CAP> table)
+{
+    uint32_t at = 0;
+    for (uint32_t chunk = blockIdx.x; chunk < table.chunks; chunk += gridDim.x) {
+        while (at + 1 < table.count && chunk >= table.e[at + 1].first) ++at;
+        const Entry &t = table.e[at];
+        const int64_t n = t.n, e = static_cast<int64_t>(chunk - t.first) * kChunk + threadIdx.x * kPer;
+        if (e >= n) continue;
+        const uint2 cm = load_codes(static_cast<const uint8_t *>(t.m), e, n), cv = load_codes(static_cast<const uint8_t *>(t.v), e, n);
+        const float sm = block_scale(t.m_exp[e / kBlock]), sv = block_scale(t.v_exp[e / kBlock]);
+        float m[kPer], v[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            m[i] = decode<true>((i < 4 ? cm.x : cm.y) >> 8 * (i % 4) & 0xffu, sm);
+            v[i] = decode<false>((i < 4 ? cv.x : cv.y) >> 8 * (i % 4) & 0xffu, sv);
+        }
+        store8(static_cast<T *>(t.param), e, n, t.flags & kWideParam, m);
+        store8(reinterpret_cast<T *>(t.master), e, n, t.flags & kWideMaster, v);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- launches
+template <class K, int CAP, class... A> int launch(K kernel, const Table<CAP> &table, cudaStream_t stream, A... more)
+{
+    // enough blocks to fill the device eight times over a multiprocessor; the rest is walked over
+    const uint32_t most = static_cast<uint32_t>(sm_count()) * 8;
+    kernel<<<table.chunks < most ? table.chunks : most, kThreads, 0, stream>>>(table, more...);
+    return finish_launch();
+}
+
+// Calls `go` with the tensors that `wanted` names, as many at a time as a launch takes.
+template <int CAP, class Wanted, class Fill, class Go> int batches(int32_t count, const spdy_adamw_tensor *tensors, Wanted wanted, Fill fill, Go go)
+{
+    Table<CAP> table;
+    table.count = table.chunks = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        if (!wanted(tensors[i])) continue;
+        const int64_t chunks = (tensors[i].n + kChunk - 1) / kChunk;
+        if (table.count == CAP || (table.count && chunks + table.chunks > 0x7fffffff)) {
+            const int rc = go(table);
+            if (rc != SPDY_OK) return rc;
+            table.count = table.chunks = 0;
+        }
+        Entry &e = table.e[table.count++];
+        fill(e, i);
+        e.first = table.chunks, e.n = tensors[i].n, e.index = static_cast<uint32_t>(i);
+        table.chunks += static_cast<uint32_t>(chunks);
+    }
+    return table.count ? go(table) : SPDY_OK;
+}
+template <class Wanted, class Fill, class GoFew, class GoMany>
+int all_batches(int32_t count, const spdy_adamw_tensor *tensors, Wanted wanted, Fill fill, GoFew few, GoMany many)
+{
+    int n = 0;
+    for (int32_t i = 0; i < count; ++i) n += wanted(tensors[i]) ? 1 : 0;
+    if (n == 0) return SPDY_OK;
+    return n <= kFew ? batches<kFew>(count, tensors, wanted, fill, few) : batches<kMany>(count, tensors, wanted, fill, many);
+}
+
+template <class P, class G, int BITS, bool MASTER, bool RANDOM> int step_kind(int32_t count, const spdy_adamw_tensor *tensors, int ptype, int gtype, const StepArgs &s, cudaStream_t stream)
+{
+    const auto wanted = [&](const spdy_adamw_tensor &t) {
+        return t.grad && t.n > 0 && t.param_dtype == ptype && t.grad_dtype == gtype && t.state_bits == BITS && (t.master != nullptr) == MASTER;
+    };
+    const auto fill = [&](Entry &e, int32_t i) {
+        const spdy_adamw_tensor &t = tensors[i];
+        e.param = t.param, e.grad = t.grad, e.master = t.master, e.m = t.m, e.v = t.v, e.m_exp = t.m_exp, e.v_exp = t.v_exp;
+        e.weight_decay = t.weight_decay;
+        e.flags = (aligned(t.param, 16) ? kWideParam : 0) | (aligned(t.grad, 16) ? kWideGrad : 0) | (aligned(t.master, 16) ? kWideMaster : 0) | (t.keep_zeros ? kKeepZeros : 0);
+    };
+    const auto go = [&](const auto &table) {
+        constexpr int cap = static_cast<int>(sizeof(table.e) / sizeof(Entry));
+        return launch(step_kernel<P, G, BITS, MASTER, RANDOM, cap>, table, stream, s);
+    };
+    return all_batches(count, tensors, wanted, fill, go, go);
+}
+
+template <class P, class G, int BITS> int step_copies(int32_t count, const spdy_adamw_tensor *tensors, int ptype, int gtype, bool random, const StepArgs &s, cudaStream_t stream)
+{
+    if constexpr (sizeof(P) == 2) {
+        const int rc = step_kind<P, G, BITS, true, false>(count, tensors, ptype, gtype, s, stream);
+        if (rc != SPDY_OK) return rc;
+        if (random) return step_kind<P, G, BITS, false, true>(count, tensors, ptype, gtype, s, stream);
+    }
+    return step_kind<P, G, BITS, false, false>(count, tensors, ptype, gtype, s, stream);
+}
+template <class P, class G> int step_types(int32_t count, const spdy_adamw_tensor *tensors, int ptype, int gtype, bool random, const StepArgs &s, cudaStream_t stream)
+{
+    const int rc = step_copies<P, G, 32>(count, tensors, ptype, gtype, random, s, stream);
+    return rc != SPDY_OK ? rc : step_copies<P, G, 8>(count, tensors, ptype, gtype, random, s, stream);
+}
+
+bool states_ok(const spdy_adamw_tensor &t)
+{
+    if (t.state_bits != 32 && t.state_bits != 8) return false;
+    if (t.n == 0) return true;
+    return t.m && t.v && aligned(t.m, 16) && aligned(t.v, 16) && (t.state_bits == 32 || (t.m_exp && t.v_exp));
+}
+constexpr int64_t kMostElements = 1ll << 41;  // chunks of one tensor are counted in 32 bits
+
+bool tensor_ok(const spdy_adamw_tensor &t)
+{
+    if (t.n < 0 || t.n > kMostElements || !known_type(t.param_dtype) || !states_ok(t) || !(t.weight_decay >= 0.f && t.weight_decay <= 3.4e38f)) return false;
+    if (t.grad && t.grad_dtype != t.param_dtype && t.grad_dtype != SPDY_F32) return false;
+    if (t.master && t.param_dtype == SPDY_F32) return false;
+    return t.n == 0 || (t.param && aligned(t.param, type_size(t.param_dtype)) && aligned(t.master, 4) && (!t.grad || aligned(t.grad, type_size(t.grad_dtype))));
+}
+
+}  // namespace
+
+extern "C" {
+
+int spdy_adamw_step(const spdy_adamw_tensor *tensors, int32_t count, const spdy_adamw_options *o, void *cuda_stream)
+{
+    if (count < 0 || (count > 0 && !tensors) || !o) return SPDY_ERR_INVALID_ARG;
+    const auto part = [](double b) { return b >= 0.0 && b < 1.0; };
+    if (!part(o->beta1) || !part(o->beta2) || !(o->eps >= 0.0 && o->eps <= 1e30) || (o->rounding != 0 && o->rounding != 1)) return SPDY_ERR_INVALID_ARG;
+    if ((!o->lr_device && !(o->lr >= 0.0 && o->lr <= 1e30)) || (!o->step_device && o->step < 1)) return SPDY_ERR_INVALID_ARG;
+    if (!aligned(o->lr_device, 4) || !aligned(o->step_device, 8) || !aligned(o->grad_scale, 4) || !aligned(o->skip, 4)) return SPDY_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < count; ++i)
+        if (!tensor_ok(tensors[i])) return SPDY_ERR_INVALID_ARG;
+    StepArgs s = {};
+    s.b1 = static_cast<float>(o->beta1), s.b2 = static_cast<float>(o->beta2);
+    s.g1 = static_cast<float>(1.0 - o->beta1), s.g2 = static_cast<float>(1.0 - o->beta2), s.eps = static_cast<float>(o->eps);
+    s.lr = o->lr, s.beta1 = o->beta1, s.beta2 = o->beta2;
+    const double t = static_cast<double>(o->step);
+    s.rate = static_cast<float>(o->lr / (1.0 - pow(o->beta1, t))), s.root = static_cast<float>(1.0 / sqrt(1.0 - pow(o->beta2, t)));
+    s.seed = o->seed, s.key = mix(mix(o->seed) + static_cast<uint32_t>(o->step));
+    s.lr_device = o->lr_device, s.step_device = o->step_device, s.grad_scale = o->grad_scale, s.skip = o->skip;
+    if (s.lr_device && !s.step_device) return SPDY_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const bool random = o->rounding == 1;
+    int rc = step_types<float, float>(count, tensors, SPDY_F32, SPDY_F32, random, s, stream);
+    if (rc == SPDY_OK) rc = step_types<__nv_bfloat16, __nv_bfloat16>(count, tensors, SPDY_BF16, SPDY_BF16, random, s, stream);
+    if (rc == SPDY_OK) rc = step_types<__nv_bfloat16, float>(count, tensors, SPDY_BF16, SPDY_F32, random, s, stream);
+    if (rc == SPDY_OK) rc = step_types<__half, __half>(count, tensors, SPDY_F16, SPDY_F16, random, s, stream);
+    if (rc == SPDY_OK) rc = step_types<__half, float>(count, tensors, SPDY_F16, SPDY_F32, random, s, stream);
+    return rc;
+}
+
+int spdy_adamw_moments(const spdy_adamw_tensor *tensors, int32_t count, void *const *m_out, void *const *v_out, int out_dtype, void *cuda_stream)
+{
+    if (count < 0 || (count > 0 && (!tensors || !m_out || !v_out)) || (out_dtype != SPDY_F32 && out_dtype != SPDY_BF16)) return SPDY_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < count; ++i) {
+        if (tensors[i].n < 0 || tensors[i].n > kMostElements || !states_ok(tensors[i]) || tensors[i].state_bits != 8) return SPDY_ERR_INVALID_ARG;
+        if (tensors[i].n > 0 && (!m_out[i] || !v_out[i] || !aligned(m_out[i], type_size(out_dtype)) || !aligned(v_out[i], type_size(out_dtype)))) return SPDY_ERR_INVALID_ARG;
+    }
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const auto wanted = [](const spdy_adamw_tensor &t) { return t.n > 0; };
+    const auto fill = [&](Entry &e, int32_t i) {
+        const spdy_adamw_tensor &t = tensors[i];
+        e = {};
+        e.param = m_out[i], e.master = static_cast<float *>(v_out[i]), e.m = t.m, e.v = t.v, e.m_exp = t.m_exp, e.v_exp = t.v_exp;
+        e.flags = (aligned(m_out[i], 16) ? kWideParam : 0) | (aligned(v_out[i], 16) ? kWideMaster : 0);
+    };
+    const auto go = [&](const auto &table) {
+        constexpr int cap = static_cast<int>(sizeof(table.e) / sizeof(Entry));
+        return out_dtype == SPDY_F32 ? launch(moments_kernel<float, cap>, table, stream) : launch(moments_kernel<__nv_bfloat16, cap>, table, stream);
+    };
+    return all_batches(count, tensors, wanted, fill, go, go);
+}
+
+}  // extern "C"

@@ -17,6 +17,8 @@ import contextlib
 import ctypes
 from typing import NamedTuple, Optional
 
+import numpy as np
+
 from . import binding
 
 EXPORTS = (
@@ -24,6 +26,7 @@ EXPORTS = (
     "spdy_layer_norm_backward_workspace_bytes", "spdy_token_logprobs", "spdy_token_logprobs_backward",
     "spdy_token_logprobs_with_grad", "spdy_linear_token_logprobs", "spdy_linear_token_logprobs_backward",
     "spdy_linear_token_logprobs_with_grad", "spdy_linear_token_logprobs_workspace_bytes", "spdy_distill_loss", "spdy_distill_loss_backward", "spdy_distill_loss_with_grad",
+    "spdy_adamw_step", "spdy_adamw_moments",
 )
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 SPDY_TOP_MAX, SPDY_DISTILL_MAX = 128, 256
@@ -31,7 +34,7 @@ SPDY_TOP_MAX, SPDY_DISTILL_MAX = 128, 256
 __all__ = ["TokenLogprobs", "LinearGrads", "DistillLoss", "linear", "linear_check_status", "layer_norm", "layer_norm_backward", "token_logprobs",
            "token_logprobs_backward", "token_logprobs_with_grad", "linear_token_logprobs", "linear_token_logprobs_backward",
            "linear_token_logprobs_with_grad", "distill_loss", "distill_loss_backward",
-           "distill_loss_with_grad"]
+           "distill_loss_with_grad", "AdamW", "AdamWMoments", "adamw_step", "adamw_moments"]
 
 
 class TokenLogprobs(NamedTuple):
@@ -89,6 +92,8 @@ def _load():
             ("spdy_linear_token_logprobs_with_grad", cint, head + [vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, size, vp]),
             ("spdy_distill_loss", cint, rows + [vp, i64, i64, i32, f32, cint, vp, vp, vp, vp]),
             ("spdy_distill_loss_backward", cint, rows + [vp, i64, i64, i32, f32, cint, vp, vp, vp, vp, i64, vp]),
+            ("spdy_adamw_step", cint, [vp, i32, vp, vp]),
+            ("spdy_adamw_moments", cint, [vp, i32, vp, vp, cint, vp]),
             ("spdy_distill_loss_with_grad", cint, rows + [vp, i64, i64, i32, f32, cint, vp, vp, vp, vp, vp, i64, vp]),
         ):
             fn = getattr(lib, name)
@@ -585,3 +590,199 @@ def distill_loss_with_grad(logits, top_ids, top_logprobs, grad_loss, temperature
     if rc:
         binding._check(rc, "spdy_distill_loss_with_grad")
     return DistillLoss(*sums), out
+
+
+class AdamWMoments(NamedTuple):
+    """A tensor's moments: float32 [n], or bytes [n] with the bytes [ceil(n / 32)] that blocks of 32 elements share."""
+
+    m: object
+    v: object
+    m_exp: Optional[object] = None
+    v_exp: Optional[object] = None
+
+
+_TENSOR = np.dtype([("param", "u8"), ("grad", "u8"), ("master", "u8"), ("m", "u8"), ("v", "u8"), ("m_exp", "u8"), ("v_exp", "u8"), ("n", "i8"),
+                    ("weight_decay", "f4"), ("param_dtype", "i4"), ("grad_dtype", "i4"), ("state_bits", "i4"), ("keep_zeros", "i4"), ("reserved", "i4")])
+
+
+class _AdamWOptions(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("step", ctypes.c_int64),
+                ("seed", ctypes.c_uint32), ("rounding", ctypes.c_int32), ("lr_device", ctypes.c_void_p), ("step_device", ctypes.c_void_p),
+                ("grad_scale", ctypes.c_void_p), ("skip", ctypes.c_void_p)]
+
+
+def _per_tensor(value, count: int, what: str):
+    values = list(value) if isinstance(value, (list, tuple)) else [value] * count
+    if len(values) != count:
+        raise ValueError(f"{what} must be one value or one for each of the {count} parameters")
+    return values
+
+
+class AdamW:
+    """What ``adamw_step`` keeps of a list of parameters: their moments, master copies and settings (``spdy_adamw_tensor``).
+
+    ``params``: contiguous float32, bfloat16 or float16 CUDA tensors of one device, changed in place by the steps.  ``bits``: 32 or 8
+    bits for each moment.  ``masters``: None, True (float32 copies of the 16-bit parameters are made here), or a list of float32
+    tensors (None where there is no copy).  ``moments``: None (zeros), or a list of ``AdamWMoments`` to go on with, which the steps
+    change in place.  ``weight_decay`` and ``keep_zeros`` (elements whose weight is 0 stay 0): one value, or one for each parameter.
+    ``rounding`` of 16-bit parameters without a master: "nearest" or "stochastic"."""
+
+    def __init__(self, params, bits: int = 32, masters=None, moments=None, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, keep_zeros=False,
+                 rounding: str = "nearest"):
+        _load()
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("params must hold a tensor at least")
+        if bits not in (32, 8):
+            raise ValueError("bits must be 32 or 8")
+        if rounding not in ("nearest", "stochastic"):
+            raise ValueError("rounding must be nearest or stochastic")
+        self.bits, self.betas, self.eps, self.rounding = bits, (float(betas[0]), float(betas[1])), float(eps), rounding
+        if not (0.0 <= self.betas[0] < 1.0 and 0.0 <= self.betas[1] < 1.0 and 0.0 <= self.eps <= 1e30):
+            raise ValueError("betas must be in [0, 1), eps at least 0")
+        count = len(self.params)
+        self.device = self.params[0].get_device()
+        for i, p in enumerate(self.params):
+            if not p.is_cuda or p.get_device() != self.device or not p.is_contiguous():
+                raise ValueError(f"params[{i}] must be a contiguous CUDA tensor on cuda:{self.device}")
+            _dtype(p, f"params[{i}]")
+        decay, keep = _per_tensor(weight_decay, count, "weight_decay"), _per_tensor(keep_zeros, count, "keep_zeros")
+        if not all(0.0 <= float(d) <= 3.4e38 for d in decay):
+            raise ValueError("weight_decay must be finite and at least 0")
+        with torch.cuda.device(self.device), torch.no_grad():
+            if masters is True:
+                masters = [None if p.dtype == torch.float32 else p.detach().float() for p in self.params]
+            self.masters = _per_tensor(masters, count, "masters")
+            if moments is None:
+                moments = [self._fresh(p.numel()) for p in self.params]
+            self.moments = _per_tensor(list(moments), count, "moments")
+        self._table = np.zeros(count, dtype=_TENSOR)
+        for i, (p, master, mom) in enumerate(zip(self.params, self.masters, self.moments)):
+            n = p.numel()
+            if master is not None:
+                if p.dtype == torch.float32:
+                    raise ValueError(f"params[{i}] is float32 and needs no master")
+                self._flat(master, f"masters[{i}]", n, torch.float32)
+            if bits == 32:
+                parts = ((mom.m, "m", n, torch.float32), (mom.v, "v", n, torch.float32))
+            else:
+                blocks = (n + 31) // 32
+                parts = ((mom.m, "m", n, torch.uint8), (mom.v, "v", n, torch.uint8), (mom.m_exp, "m_exp", blocks, torch.uint8),
+                         (mom.v_exp, "v_exp", blocks, torch.uint8))
+            for t, name, size, dtype in parts:
+                self._flat(t, f"moments[{i}].{name}", size, dtype)
+            if n and (mom.m.data_ptr() | mom.v.data_ptr()) & 15:
+                raise ValueError(f"moments[{i}] must start on 16 bytes")
+            row = self._table[i]
+            row["param"], row["master"], row["n"] = p.data_ptr(), _ptr(master) or 0, n
+            row["m"], row["v"] = mom.m.data_ptr(), mom.v.data_ptr()
+            if bits == 8:
+                row["m_exp"], row["v_exp"] = mom.m_exp.data_ptr(), mom.v_exp.data_ptr()
+            row["weight_decay"], row["param_dtype"], row["grad_dtype"] = float(decay[i]), _TYPES[p.dtype], _TYPES[p.dtype]
+            row["state_bits"], row["keep_zeros"] = bits, bool(keep[i])
+        written = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self._written() if t.numel())
+        if any(a[1] > b[0] for a, b in zip(written, written[1:])):
+            raise ValueError("params, masters and moments must not share memory")
+        self._grad_dtypes = self._table["grad_dtype"].tolist()
+        self._shapes = [p.shape for p in self.params]
+        self._dtypes = [p.dtype for p in self.params]
+        self._leaves = [p for p in self.params if p.requires_grad]
+
+    def _fresh(self, n: int) -> AdamWMoments:
+        if self.bits == 32:
+            return AdamWMoments(*(torch.zeros(n, device="cuda") for _ in range(2)))
+        return AdamWMoments(*(torch.zeros(size, dtype=torch.uint8, device="cuda") for size in (n, n, (n + 31) // 32, (n + 31) // 32)))
+
+    def _flat(self, t, what: str, n: int, dtype):
+        if t is None or not t.is_cuda or t.get_device() != self.device or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{what} must be a contiguous tensor of {n} {dtype} on cuda:{self.device}")
+        if t.requires_grad:
+            raise ValueError(f"{what} must not require a gradient")
+
+    def _written(self):
+        for p, master, mom in zip(self.params, self.masters, self.moments):
+            yield p
+            yield from (t for t in (master, *mom) if t is not None)
+
+
+def _scalar(t, what: str, dtype, device: int) -> int:
+    if not t.is_cuda or t.get_device() != device or t.dtype != dtype or t.numel() != 1:
+        raise ValueError(f"{what} must be one {dtype} on cuda:{device}")
+    if t.requires_grad:
+        _refuse_gradient(what)
+    return t.data_ptr()
+
+
+def adamw_step(plan: AdamW, grads, lr, step, seed: int = 0, grad_scale=None, skip=None, stream=None) -> None:
+    """``spdy_adamw_step``: one step on all of ``plan``'s parameters, in place.
+
+    ``grads``: one contiguous tensor of its parameter's shape for each, of its type or float32 (None: the parameter is left alone).
+    ``step`` counts from 1.  ``lr`` and ``step`` are numbers, or (for captured steps, which read them when they are replayed) a
+    float32 and an int64 CUDA tensor of one element; with ``lr`` a tensor ``step`` has to be one.  ``seed`` (32 bits) drives
+    stochastic rounding.  ``grad_scale``: a float32 CUDA tensor of one element that the gradients are multiplied by; ``skip``: one
+    that leaves everything unchanged if it is not 0."""
+    lib = _lib or _load()
+    if len(grads) != len(plan.params):
+        raise ValueError(f"grads must hold one entry for each of the {len(plan.params)} parameters")
+    dev, f32 = plan.device, torch.float32
+    pointers, kinds = [], plan._grad_dtypes
+    for i, (g, shape, dtype) in enumerate(zip(grads, plan._shapes, plan._dtypes)):
+        if g is None:
+            pointers.append(0)
+            continue
+        if g.requires_grad:
+            _refuse_gradient(f"grads[{i}]")
+        if g.shape != shape or g.get_device() != dev or not g.is_contiguous():
+            raise ValueError(f"grads[{i}] must be a contiguous {list(shape)} tensor on cuda:{dev}")
+        if g.dtype is not dtype:
+            if g.dtype is not f32:
+                raise ValueError(f"grads[{i}] must be {dtype} or float32")
+            if kinds is plan._grad_dtypes:
+                kinds = list(kinds)
+            kinds[i] = 0
+        pointers.append(g.data_ptr())
+    table = plan._table.copy()  # the plan's own stays as it is: calls of several threads do not meet
+    table["grad"] = pointers
+    if kinds is not plan._grad_dtypes:
+        table["grad_dtype"] = kinds
+    o = _AdamWOptions(0.0, *plan.betas, plan.eps, 1, seed & 0xFFFFFFFF, plan.rounding == "stochastic")
+    if isinstance(lr, torch.Tensor):
+        o.lr_device = _scalar(lr, "lr", f32, dev)
+        if not isinstance(step, torch.Tensor):
+            raise ValueError("step must be a tensor where lr is one")
+    else:
+        o.lr = lr
+    if isinstance(step, torch.Tensor):
+        o.step_device = _scalar(step, "step", torch.int64, dev)
+    else:
+        o.step = step
+    if grad_scale is not None:
+        o.grad_scale = _scalar(grad_scale, "grad_scale", f32, dev)
+    if skip is not None:
+        o.skip = _scalar(skip, "skip", f32, dev)
+    with _Scope(dev, stream) as handle:
+        rc = lib.spdy_adamw_step(table.ctypes.data, len(pointers), ctypes.byref(o), handle)
+    if rc:
+        binding._check(rc, "spdy_adamw_step")
+    if plan._leaves:  # a graph that was recorded before must notice
+        torch.autograd.graph.increment_version(plan._leaves)
+
+
+def adamw_moments(plan: AdamW, dtype=None, stream=None):
+    """The moments of all parameters as numbers: a list of (m, v), in the parameters' shapes.  With 32 bits they are the plan's own
+    tensors; with 8 bits ``spdy_adamw_moments`` writes new ones of ``dtype``, float32 (the default) or bfloat16 (as exact)."""
+    lib = _lib or _load()
+    if plan.bits == 32:
+        if dtype not in (None, torch.float32):
+            raise ValueError("moments of 32 bits are float32")
+        return [(mom.m.view(p.shape), mom.v.view(p.shape)) for p, mom in zip(plan.params, plan.moments)]
+    dtype = torch.float32 if dtype is None else dtype
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("dtype must be float32 or bfloat16")
+    with _Scope(plan.device, stream) as handle:
+        out = [(torch.empty(shape, dtype=dtype, device="cuda"), torch.empty(shape, dtype=dtype, device="cuda")) for shape in plan._shapes]
+        pointers = np.array([[m.data_ptr(), v.data_ptr()] for m, v in out], dtype=np.uint64).T.copy()
+        rc = lib.spdy_adamw_moments(plan._table.ctypes.data, len(out), pointers[0].ctypes.data, pointers[1].ctypes.data, _TYPES[dtype], handle)
+    if rc:
+        binding._check(rc, "spdy_adamw_moments")
+    return out

@@ -76,3 +76,106 @@ def ref_softmax(x, temperature):
 
 def close(got, want, name):
     ref.close(got, want[name].cpu(), want[name + "_err"].cpu(), name)
+
+
+# ------------------------------------------------------------------------------------------------ AdamW
+
+def mix(x):
+    """The hash, on uint64 arrays that hold 32 bits."""
+    import numpy as np
+    m = np.uint64(0xFFFFFFFF)
+    x = np.asarray(x, dtype=np.uint64) & m
+    x = ((x ^ (x >> np.uint64(16))) * np.uint64(0x7FEB352D)) & m
+    x = ((x ^ (x >> np.uint64(15))) * np.uint64(0x846CA68B)) & m
+    return x ^ (x >> np.uint64(16))
+
+
+def random_bits(seed, step, tensor, n, first=0):
+    import numpy as np
+    key = int(mix(int(mix(int(mix(seed)) + step)) + tensor))
+    e = np.arange(first, first + n, dtype=np.uint64)
+    return torch.from_numpy(mix((e & np.uint64(0xFFFFFFFF)) + np.uint64(key) + (e >> np.uint64(32)) * np.uint64(0x9E3779B9)).astype(np.int64))
+
+
+def by_blocks(t):
+    return torch.nn.functional.pad(t, (0, -t.numel() % 32)).view(-1, 32)
+
+
+def decode(mom, signed):
+    """A moment of 8 bits as numbers, from the layout's definition."""
+    codes, E = ref_ints(mom.m if signed else mom.v), ref_ints(mom.m_exp if signed else mom.v_exp)
+    size = codes & 127 if signed else codes
+    field, mantissa = size >> 3, (size & 7).double()
+    top = 14 if signed else 30
+    value = torch.where(field > 0, torch.ldexp(1 + mantissa / 8, field - top), torch.ldexp(mantissa / 8, torch.full_like(field, 1 - top)))
+    value = torch.where((codes > 127) & torch.tensor(signed), -value, value)
+    per = E.repeat_interleave(32)[:codes.numel()]
+    value = torch.ldexp(value, per - 127)
+    return torch.where(per == 255, torch.full_like(value, math.nan), value)
+
+
+def ref_ints(t):
+    return t.detach().cpu().to(torch.int64)
+
+
+def check_codes(mom, signed, y, err, bits, what):
+    """Whether the moment is ``y`` (64 bits, off by ``err`` in the kernel) rounded with the random ``bits``: where the sum of the part cut
+    off and the random number is within the error of 1, either neighbour will do."""
+    got = decode(mom, signed)
+    E = ref_ints(mom.m_exp if signed else mom.v_exp)
+    rows, erows = by_blocks(y), by_blocks(err)
+    amax = rows.abs().amax(1)
+    bad = ~torch.isfinite(amax) | (amax >= 2.0 ** 127)
+    want_e = torch.where(bad, torch.tensor(255), (torch.frexp(amax)[1] - 1 + 127).clamp(min=1))
+    sure = ((torch.frexp(amax * (1 - 2.0 ** -20))[1] == torch.frexp(amax * (1 + 2.0 ** -20))[1]) | bad) & (amax > 2.0 ** -120)
+    assert torch.equal(E[sure], want_e[sure].long()), what
+    assert torch.isnan(got[E.repeat_interleave(32)[:got.numel()] == 255]).all(), what
+    e = E.repeat_interleave(32).view(-1, 32)
+    top, lowest = (14, -13) if signed else (30, -29)
+    fine = e != 255
+    binade = torch.maximum(torch.frexp(rows)[1] - 1, e - 127 + lowest)
+    unit = torch.ldexp(torch.ones_like(rows), binade - 3)
+    u = by_blocks(((bits & 0xFFFFF) if signed else bits >> 12).double() * 2.0 ** -20)
+    steps = rows.abs() / unit
+    slack = erows / unit + 2.0 ** -18
+    low, high = torch.floor(steps + u - slack), torch.floor(steps + u + slack)
+    if not signed:
+        low, high = (torch.where(rows > 0, t.clamp(min=1), t) for t in (low, high))
+    have = by_blocks(torch.nan_to_num(got, nan=0.0)).abs() / unit
+    ok = (have >= low) & (have <= high) | ~fine
+    assert ok.all(), (what, int((~ok).sum()))
+    assert (slack[fine & (rows.abs() > 0)] < 0.01).float().mean() > 0.9 or not (rows.abs() > 0).any(), what  # the test says something
+    neg = by_blocks(got) < 0
+    assert not (neg & (rows > 0) & fine).any(), what
+
+
+def adamw(old, g, m, v, lr, decay, betas, eps, t, keep):
+    """(param, m, v) in 64 bits and the errors of their fp32 evaluation."""
+    b1, b2 = betas
+    m1, v1 = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+    em = 2.0 ** -21 * (b1 * m.abs() + (1 - b1) * g.abs())  # two roundings of each product (its factor's and its own), one of the sum, one of g
+    ev = 2.0 ** -21 * v1 + 2.0 ** -149
+    denom = (v1 / (1 - b2 ** t)).sqrt() + eps
+    rate = lr / (1 - b1 ** t)
+    change = rate * m1 / denom
+    new = old * (1 - lr * decay) - change
+    # sqrt and quotient within 2^-21 each, half of v's error, factors
+    ep = rate * em / denom + change.abs() * (2.0 ** -19 + torch.where(v1 > 0, ev / (2 * v1), torch.zeros_like(v1))) + 2.0 ** -22 * old.abs()
+    if keep:
+        zero = old == 0
+        m1, v1, new, em, ev, ep = (torch.where(zero, torch.zeros_like(x), x) for x in (m1, v1, new, em, ev, ep))
+    return new, m1, v1, ep, em, ev
+
+
+def check_random_rounding(got, want, err, bits, what):
+    """16-bit params rounded stochastically: floor(|y| / unit + u) units, either neighbour within the error of the border."""
+    t = got.dtype
+    shift, digits, least = (16, 7, -126) if t == torch.bfloat16 else (13, 10, -14)
+    u = (((bits * 0x9E3779B1) & 0xFFFFFFFF) >> (32 - shift)).double() * 2.0 ** -shift
+    binade = (torch.frexp(want)[1] - 1).clamp(min=least)
+    unit = torch.ldexp(torch.ones_like(want), binade - digits)
+    slack = err / unit + 2.0 ** -shift
+    low, high = torch.floor(want.abs() / unit + u - slack), torch.floor(want.abs() / unit + u + slack)
+    have = ref.d64(got).abs() / unit
+    ok = (have >= low) & (have <= high)  # where the update takes the weight to almost 0, the error is more than a unit of what is left
+    assert ok.all(), (what, int((~ok).sum()))
