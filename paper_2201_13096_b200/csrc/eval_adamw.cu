@@ -59,38 +59,53 @@ SPDY_EVAL_FN uint32_t mix(uint32_t x)
 
 __device__ __forceinline__ float exponent(int field) { return __int_as_float(field << 23); }  // 2^(field - 127), 1 <= field <= 254
 
-// 2^(E - 127) of a stored byte; 255 marks a block that is not finite, 0 comes with codes of 0 only (a fresh state)
-__device__ __forceinline__ float block_scale(uint32_t E) { return E == 255 ? quiet_nan() : E == 0 ? __int_as_float(1 << 22) : exponent(static_cast<int>(E)); }
+// The two formats: the exponent field that the largest magnitude's binade gets.
+template <bool SIGNED> constexpr int kField = SIGNED ? 14 : 30;
 
-template <bool SIGNED> __device__ __forceinline__ float decode(uint32_t code, float scale)
+// Eight numbers from their codes and the block's byte.  A code's bits, four below the top of a word, are the upper bits of a float
+// whose exponent is off by a known amount: one product puts it right (two where 2^(E - 14) or 2^(E - 30) is no float).
+template <bool SIGNED> __device__ __forceinline__ void decode(uint2 codes, uint32_t E, float *y)
 {
-    constexpr float up = SIGNED ? 0x1p113f : 0x1p97f;
-    if (!SIGNED) return __uint_as_float(code << 20) * up * scale;
-    return __uint_as_float((code & 0x80u) << 24 | (code & 0x7fu) << 20) * up * scale;
+    constexpr uint32_t most = 254 - 127 + kField<SIGNED>;  // the largest E whose factor is a float
+    const float factor = E == 255 ? quiet_nan() : exponent(min(static_cast<int>(E), static_cast<int>(most)) + 127 - kField<SIGNED>);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const uint32_t top = __byte_perm(i < 4 ? codes.x : codes.y, 0, (i % 4) << 12 | 0x0444);  // the code in the highest byte
+        y[i] = (SIGNED ? __uint_as_float(static_cast<uint32_t>(static_cast<int32_t>(top) >> 4) & 0x87f00000u) : __uint_as_float(top >> 4)) * factor;
+    }
+    if (E > most && E != 255)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) y[i] *= exponent(127 + static_cast<int>(E - most));
 }
 
 // Codes of a thread's eight elements (a quarter of a block: four neighbouring lanes), and the block's byte.
-template <bool SIGNED> __device__ __forceinline__ uint2 encode(const float *y, const uint32_t *random, uint32_t &E)
+template <bool SIGNED> __device__ __forceinline__ uint2 encode(float *y, const uint32_t *random, uint32_t &E)
 {
-    uint32_t most = 0;
+    float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) most = max(most, __float_as_uint(y[i]) & 0x7fffffffu);
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-    E = max(most >> 23, 1u);
+    for (int i = 0; i < kPer; ++i) most = max_nan(most, fabsf(y[i]));
+    most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    E = max(__float_as_uint(most) >> 23, 1u);
     const bool bad = E >= 254;
-    const float down = bad ? 0.f : exponent(254 - static_cast<int>(E));
+    int field = 127 + kField<SIGNED> - static_cast<int>(E);  // of the factor
+    if (field < 1) {  // no float: the way down in two steps, of which the first is exact for all that is left after the second
+        field += 113;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) y[i] *= 0x1p-113f;
+    }
     if (bad) E = 255;
-    uint32_t w[2] = {0, 0};
+    const float factor = exponent(max(field, 1));
+    uint32_t x[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const float scaled = fabsf(y[i]) * down * (SIGNED ? 0x1p-113f : 0x1p-97f);
-        uint32_t code = (__float_as_uint(scaled) + (SIGNED ? random[i] & 0xfffffu : random[i] >> 12)) >> 20;
-        if (SIGNED) code |= __float_as_uint(y[i]) >> 24 & 0x80u;
-        else if (y[i] > 0.f) code = max(code, 1u);
-        w[i / 4] |= (bad ? 0u : code) << 8 * (i % 4);
+        x[i] = __float_as_uint(fabsf(y[i]) * factor) + (SIGNED ? random[i] & 0xfffffu : random[i] >> 12);
+        if (!SIGNED && y[i] > 0.f) x[i] = max(x[i], 1u << 20);
+        x[i] <<= 4;
+        if (SIGNED) x[i] |= __float_as_uint(y[i]) & 0x80000000u;
     }
-    return make_uint2(w[0], w[1]);
+    const auto join = [&](const uint32_t *four) { return __byte_perm(__byte_perm(four[0], four[1], 0x0073), __byte_perm(four[2], four[3], 0x0073), 0x5410); };
+    return bad ? make_uint2(0, 0) : make_uint2(join(x), join(x + 4));
 }
 
 // Eight elements from e on of a vector of n; `wide`: they may be moved 16 bytes at a time.
@@ -159,6 +174,19 @@ __device__ __forceinline__ float root_of(float x)
     asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float root_flushed(float x)
+{
+    float y;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// a / b; b is 0 or far from fp32's ends, and quotients below 2^-126 change no weight
+__device__ __forceinline__ float quotient(float a, float b)
+{
+    float y;
+    asm("div.approx.ftz.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
 
 template <class P, class G, int BITS, bool MASTER, bool RANDOM, int CAP>
 __global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ StepArgs s)
@@ -192,13 +220,11 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ 
             load8(static_cast<const float *>(t.v), e, n, true, v);
         } else {
             const uint2 cm = load_codes(static_cast<const uint8_t *>(t.m), e, n), cv = load_codes(static_cast<const uint8_t *>(t.v), e, n);
-            const float sm = e < n ? block_scale(t.m_exp[e / kBlock]) : 0.f, sv = e < n ? block_scale(t.v_exp[e / kBlock]) : 0.f;
+            decode<true>(cm, e < n ? t.m_exp[e / kBlock] : 0, m), decode<false>(cv, e < n ? t.v_exp[e / kBlock] : 0, v);
+            if (e + kPer > n)  // a block that is not finite has nothing behind the tensor's end
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                m[i] = decode<true>((i < 4 ? cm.x : cm.y) >> 8 * (i % 4) & 0xffu, sm);
-                v[i] = decode<false>((i < 4 ? cv.x : cv.y) >> 8 * (i % 4) & 0xffu, sv);
-                if (e + i >= n) m[i] = v[i] = 0.f;  // a block that is not finite has nothing behind the tensor's end
-            }
+                for (int i = 0; i < kPer; ++i)
+                    if (e + i >= n) m[i] = v[i] = 0.f;
         }
         const float decay = static_cast<float>(1.0 - lr * static_cast<double>(t.weight_decay));
         uint32_t random[kPer];
@@ -207,15 +233,28 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ 
 #pragma unroll
             for (int i = 0; i < kPer; ++i) random[i] = mix(start + i);
         }
+        float old[kPer], below[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             // every product and sum rounded by itself: the 8-bit codes below are those of the plain formula, bit for bit
-            const float old = p[i], gs = g[i] * scale;
+            const float gs = g[i] * scale;
             m[i] = m[i] * s.b1 + gs * s.g1;
             v[i] = v[i] * s.b2 + gs * s.g2 * gs;
-            p[i] = old * decay - __fdividef(m[i] * rate, root_of(v[i]) * root + s.eps);
-            if ((t.flags & kKeepZeros) && old == 0.f) p[i] = m[i] = v[i] = 0.f;
+            old[i] = p[i];
         }
+        if (s.eps >= 1e-9f) {  // roots of numbers below 2^-126 do not show beside such an eps
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) below[i] = fmaf(root_flushed(v[i]), root, s.eps);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) below[i] = fmaf(root_of(v[i]), root, s.eps);
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) p[i] = fmaf(old[i], decay, -quotient(m[i] * rate, below[i]));
+        if (t.flags & kKeepZeros)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (old[i] == 0.f) p[i] = m[i] = v[i] = 0.f;
         if (BITS == 32) {
             store8(static_cast<float *>(t.m), e, n, true, m);
             store8(static_cast<float *>(t.v), e, n, true, v);
@@ -245,13 +284,8 @@ template <class T, int CAP> __global__ void __launch_bounds__(kThreads) moments_
         const int64_t n = t.n, e = static_cast<int64_t>(chunk - t.first) * kChunk + threadIdx.x * kPer;
         if (e >= n) continue;
         const uint2 cm = load_codes(static_cast<const uint8_t *>(t.m), e, n), cv = load_codes(static_cast<const uint8_t *>(t.v), e, n);
-        const float sm = block_scale(t.m_exp[e / kBlock]), sv = block_scale(t.v_exp[e / kBlock]);
         float m[kPer], v[kPer];
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            m[i] = decode<true>((i < 4 ? cm.x : cm.y) >> 8 * (i % 4) & 0xffu, sm);
-            v[i] = decode<false>((i < 4 ? cv.x : cv.y) >> 8 * (i % 4) & 0xffu, sv);
-        }
+        decode<true>(cm, t.m_exp[e / kBlock], m), decode<false>(cv, t.v_exp[e / kBlock], v);
         store8(static_cast<T *>(t.param), e, n, t.flags & kWideParam, m);
         store8(reinterpret_cast<T *>(t.master), e, n, t.flags & kWideMaster, v);
     }

@@ -57,7 +57,7 @@ struct ProductArgs {
     int64_t ld_sums;
     void *out;                     // kGrad: the piece; kWeight: 16 bits; parts: fp32 [splits][M][ldo]
     int64_t ldo;
-    int add, sectors;              // parts: to what is there already; kWeight: rows of out start on 32 bytes
+    int add, width;                // parts: to what is there already; kWeight: 32 or 16 if every row of out starts on as many bytes, else 0
 };
 
 // Half precision keeps the gradient by the logits times a power of two that brings the largest row's to 2^13 .. 2^14: the least normal number is then
@@ -315,8 +315,13 @@ __device__ __forceinline__ void carry_store(const ProductArgs &a, uint32_t tmem,
         if (n0 + c >= a.N) continue;
 #pragma unroll
         for (int i = 0; i < 16; ++i) f[i] = ok ? f[i] * scale : quiet_nan();
-        if (!a.sectors || n0 + c + 16 > a.N) store_turned(a, m0, n0 + c, Elem<T>::pack(f), Elem<T>::pack(f + 8), turn);
-        else if (m < a.M) store32(to + 2 * c, Elem<T>::pack(f), Elem<T>::pack(f + 8));
+        const uint4 lo = Elem<T>::pack(f), hi = Elem<T>::pack(f + 8);
+        if (!a.width || n0 + c + 16 > a.N) {
+            store_turned(a, m0, n0 + c, lo, hi, turn);
+        } else if (m < a.M) {
+            if (a.width == 32) store32(to + 2 * c, lo, hi);
+            else reinterpret_cast<uint4 *>(to + 2 * c)[0] = lo, reinterpret_cast<uint4 *>(to + 2 * c)[1] = hi;
+        }
     }
 }
 
@@ -526,23 +531,54 @@ __device__ __forceinline__ void write_consts(const RowArgs &a, int64_t r, int64_
     }
 }
 
-// Joins the tiles of 32 rows, a row to a lane: each warp a part of the tiles, then the warps in their order.
-constexpr int kRowWarps = 16;
+// Joins the tiles of 32 rows, a row to a lane: each warp every 32nd tile, eight of them at a time (their loads in flight together, one
+// rescaling for all), then the warps.  2048 rows of 512 tiles: 34 us with a rescaling per tile and 16 warps, 10 this way.
+constexpr int kRowWarps = 32, kRowTiles = 8;
 __global__ void __launch_bounds__(32 * kRowWarps) rows_kernel(const RowArgs a)
 {
     __shared__ float room[kRowWarps][3][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t r = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+    // `N` sums at once; what is not there is the empty sum
+    const auto join_all = [&](Sums &sums, const float *m, const float *s, const float *t, int count) {
+        float top = sums.m;
+#pragma unroll
+        for (int i = 0; i < kRowTiles; ++i)
+            if (i < count) top = fmaxf(top, m[i]);
+        raise(sums, top, a.c);
+#pragma unroll
+        for (int i = 0; i < kRowTiles; ++i)
+            if (i < count) {
+                Sums one = {m[i], s[i], t[i]};
+                raise(one, top, a.c);
+                sums.s += one.s, sums.t += one.t;
+            }
+    };
     Sums sums = {neg_inf(), 0.f, 0.f};
-#pragma unroll 4
-    for (int tile = warp; tile < a.tiles; tile += kRowWarps) {
-        const float *from = a.partial + static_cast<int64_t>(tile) * 3 * a.padded_rows + r;
-        join(sums, {from[0], from[a.padded_rows], from[2 * a.padded_rows]}, a.c);
+    for (int tile = warp; tile < a.tiles; tile += kRowWarps * kRowTiles) {
+        float m[kRowTiles], s[kRowTiles], t[kRowTiles];
+#pragma unroll
+        for (int i = 0; i < kRowTiles; ++i) {
+            m[i] = neg_inf(), s[i] = t[i] = 0.f;
+            if (tile + i * kRowWarps < a.tiles) {
+                const float *from = a.partial + static_cast<int64_t>(tile + i * kRowWarps) * 3 * a.padded_rows + r;
+                m[i] = from[0], s[i] = from[a.padded_rows], t[i] = from[2 * a.padded_rows];
+            }
+        }
+        join_all(sums, m, s, t, kRowTiles);
     }
     room[warp][0][lane] = sums.m, room[warp][1][lane] = sums.s, room[warp][2][lane] = sums.t;
     __syncthreads();
     if (warp > 0 || r >= a.R) return;
-    for (int w = 1; w < kRowWarps; ++w) join(sums, {room[w][0][lane], room[w][1][lane], room[w][2][lane]}, a.c);
+    for (int w = 1; w < kRowWarps; w += kRowTiles) {
+        float m[kRowTiles], s[kRowTiles], t[kRowTiles];
+#pragma unroll
+        for (int i = 0; i < kRowTiles; ++i) {
+            m[i] = neg_inf(), s[i] = t[i] = 0.f;
+            if (w + i < kRowWarps) m[i] = room[w + i][0][lane], s[i] = room[w + i][1][lane], t[i] = room[w + i][2][lane];
+        }
+        join_all(sums, m, s, t, kRowTiles);
+    }
     const int64_t token = a.tokens ? token_at(a.tokens, a.index_bits, r) : -1;
     const bool empty = sums.s == 0.f;
     const float log_s = logf(sums.s), entropy = empty ? 0.f : log_s - kLn2 * (sums.t / sums.s);
@@ -567,18 +603,46 @@ __global__ void __launch_bounds__(256) saved_rows_kernel(const RowArgs a)
 }
 
 // ---------------------------------------------------------------------------------------------- sums of parts
-// out[m][n] = sum over the splits of parts[split][m][n], in their order, times 2^-scale, rounded once.
-template <class T>
-__global__ void __launch_bounds__(256) finish_kernel(const float *parts, int splits, int64_t M, int64_t N, int64_t ldp, const uint32_t *scale_bits, T *out, int64_t ldo)
+// out[m][n] = sum over the splits of parts[split][m][n], in their order, times 2^-scale, rounded once; eight columns to a thread.
+// `wide`: every row of out starts on 16 bytes.  Index: 32 bits where they are enough (a division by a 64-bit number cost more than all the rest).
+template <class T, class Index>
+__global__ void __launch_bounds__(256) finish_kernel(const float *parts, int splits, int64_t M, int64_t N, int64_t ldp, const uint32_t *scale_bits, T *out, int64_t ldo, int wide)
 {
     const float scale = power_of_two(-scale_power(scale_bits));
-    const int64_t total = M * N;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t m = i / N, n = i - m * N;
-        float sum = 0.f;
-        for (int s = 0; s < splits; ++s) sum += parts[(s * M + m) * ldp + n];
-        out[m * ldo + n] = Elem<T>::from_float(sum * scale);
+    const Index across = static_cast<Index>(ldp / 8), total = static_cast<Index>(M) * across;
+    for (Index i = static_cast<Index>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<Index>(gridDim.x) * 256) {
+        const Index row = i / across;
+        const int64_t m = row, n = static_cast<int64_t>(i - row * across) * 8;
+        float sum[8] = {};
+#pragma unroll 2
+        for (int s = 0; s < splits; ++s) {
+            uint4 lo, hi;
+            load32(parts + (s * M + m) * ldp + n, lo, hi);
+            float f[8];
+            Elem<float>::unpack(lo, f), Elem<float>::unpack(hi, f + 4);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] += f[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[k] *= scale;
+        T *to = out + m * ldo + n;
+        if (wide && n + 8 <= N) {
+            *reinterpret_cast<uint4 *>(to) = Elem<T>::pack(sum);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (n + k < N) to[k] = Elem<T>::from_float(sum[k]);
+        }
     }
+}
+template <class T> int finish(const float *parts, int splits, int64_t M, int64_t N, int64_t ldp, const uint32_t *scale_bits, T *out, int64_t ldo, cudaStream_t s)
+{
+    const int wide = aligned(out, 16) && ldo % 8 == 0;
+    const int64_t total = M * (ldp / 8), most = static_cast<int64_t>(sm_count()) * 8, want = (total + 255) / 256;
+    const unsigned blocks = static_cast<unsigned>(want < most ? want : most);
+    if (total + most * 256 < (1ll << 32)) finish_kernel<T, uint32_t><<<blocks, 256, 0, s>>>(parts, splits, M, N, ldp, scale_bits, out, ldo, wide);
+    else finish_kernel<T, uint64_t><<<blocks, 256, 0, s>>>(parts, splits, M, N, ldp, scale_bits, out, ldo, wide);
+    return finish_launch();
 }
 
 // dbias of a piece: the row groups' sums in their order, eight runs of them to a column.
@@ -610,15 +674,16 @@ struct Layout {
     int hidden_splits, weight_splits;
 };
 
-// How many parts the sum of a product of few tiles is split into, so that it fills the pairs of multiprocessors: the least estimated time in stages,
-// a part costing its share and about five more for its way in and out.
-int choose_splits(int64_t tiles, int64_t k_blocks)
+// How many parts the sum of a product of few tiles is split into, so that it fills the pairs of multiprocessors: the least estimated time in stages
+// (0.55 us each), a part costing its share, about five more for its way in and out, and the memory traffic of its M x N fp32 sums.
+int choose_splits(int64_t M, int64_t N, int64_t k_blocks)
 {
-    const int64_t pairs = sm_count() / 2;
+    const int64_t pairs = sm_count() / 2, tiles = div_up(M, kTile) * div_up(N, kTile);
+    const double traffic = static_cast<double>(M) * static_cast<double>(N) * 2.2e-6;
     int best = 1;
     double least = 1e300;
     for (int s = 1; s <= 64 && s <= k_blocks; ++s) {
-        const double time = static_cast<double>(div_up(tiles * s, pairs)) * (static_cast<double>(div_up(k_blocks, s)) + 5.0) + 0.25 * s;
+        const double time = static_cast<double>(div_up(tiles * s, pairs)) * (static_cast<double>(div_up(k_blocks, s)) + 5.0) + traffic * s;
         if (time < least) least = time, best = s;
     }
     return best;
@@ -647,9 +712,9 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
         width = div_up(div_up(V, pieces), kTile) * kTile;  // pieces of one size
         l.width = width < V ? width : div_up(V, 64) * 64;
         l.ld_parts = div_up(D, 8) * 8;
-        const int64_t across = div_up(D, kTile);
-        l.hidden_splits = choose_splits(div_up(R, kTile) * across, div_up(l.width < V ? l.width : V, kStageK));
-        l.weight_splits = choose_splits(div_up(l.width < V ? l.width : V, kTile) * across, div_up(R, kStageK));
+        const int64_t ids = l.width < V ? l.width : V;
+        l.hidden_splits = choose_splits(R, D, div_up(ids, kStageK));
+        l.weight_splits = choose_splits(ids, D, div_up(R, kStageK));
         l.consts = take(static_cast<size_t>(R) * kConsts * 4);
         l.scale = take(256);
         l.piece = take(static_cast<size_t>(R) * l.width * 2);
@@ -773,7 +838,6 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
     HEAD_TRY(map_of(&hidden_columns, h.hidden, h.ldh, R, D, h.dtype, BK));
     HEAD_TRY(map_of(&weight_columns, h.weight, h.ldw, V, D, h.dtype, BK));
     float *hidden_parts = reinterpret_cast<float *>(ws + l.parts), *weight_parts = hidden_parts + static_cast<size_t>(l.hidden_splits) * R * l.ld_parts;
-    const unsigned finish_blocks = static_cast<unsigned>(sm_count()) * 8;
     for (int64_t v0 = 0; v0 < V; v0 += l.width) {
         const int64_t n = V - v0 < l.width ? V - v0 : l.width;
         ProductArgs a = base;
@@ -800,20 +864,16 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
             T *out = static_cast<T *>(h.dweight) + v0 * h.lddw;
             if (l.weight_splits == 1) {
                 b.out = out, b.ldo = h.lddw, b.scale_bits = base.scale_bits;
-                b.sectors = aligned(out, 32) && h.lddw % 16 == 0;
+                b.width = aligned(out, 32) && h.lddw % 16 == 0 ? 32 : aligned(out, 16) && h.lddw % 8 == 0 ? 16 : 0;
                 HEAD_TRY((launch_product<T, kWeight, false>(piece_columns, hidden_columns, b, R, 8, 1, s)));
             } else {
                 b.out = weight_parts, b.ldo = l.ld_parts;
                 HEAD_TRY((launch_product<T, kWeightParts, false>(piece_columns, hidden_columns, b, R, 8, l.weight_splits, s)));
-                finish_kernel<T><<<finish_blocks, 256, 0, s>>>(weight_parts, l.weight_splits, n, D, l.ld_parts, base.scale_bits, out, h.lddw);
-                HEAD_TRY(finish_launch());
+                HEAD_TRY(finish<T>(weight_parts, l.weight_splits, n, D, l.ld_parts, base.scale_bits, out, h.lddw, s));
             }
         }
     }
-    if (h.dhidden) {
-        finish_kernel<T><<<finish_blocks, 256, 0, s>>>(hidden_parts, l.hidden_splits, R, D, l.ld_parts, base.scale_bits, static_cast<T *>(h.dhidden), h.lddh);
-        HEAD_TRY(finish_launch());
-    }
+    if (h.dhidden) HEAD_TRY(finish<T>(hidden_parts, l.hidden_splits, R, D, l.ld_parts, base.scale_bits, static_cast<T *>(h.dhidden), h.lddh, s));
     return SPDY_OK;
 }
 

@@ -170,8 +170,9 @@ static __global__ void __launch_bounds__(256) repack_kernel(const Repack p)
     const int which = blockIdx.y;
     if (!p.to[which]) return;
     const int64_t per_row = p.ldto / 8, total = p.rows[which] * per_row;
+    const bool small = total < (1ll << 32);  // a division by a 64-bit number costs more than the copy
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t r = i / per_row, k = (i - r * per_row) * 8;
+        const int64_t r = small ? static_cast<uint32_t>(i) / static_cast<uint32_t>(per_row) : i / per_row, k = (i - r * per_row) * 8;
         const uint16_t *from = p.from[which] + r * p.ld[which] + k;
         uint32_t e[8];
 #pragma unroll

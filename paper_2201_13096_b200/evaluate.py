@@ -683,8 +683,9 @@ class AdamW:
         written = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self._written() if t.numel())
         if any(a[1] > b[0] for a, b in zip(written, written[1:])):
             raise ValueError("params, masters and moments must not share memory")
-        self._grad_dtypes = self._table["grad_dtype"].tolist()
-        self._shapes = [p.shape for p in self.params]
+        self._words = self._table.view(np.uint64).reshape(count, -1)
+        self._shapes = [tuple(p.shape) for p in self.params]
+        self._strides = [p.stride() for p in self.params]
         self._dtypes = [p.dtype for p in self.params]
         self._leaves = [p for p in self.params if p.requires_grad]
 
@@ -725,26 +726,24 @@ def adamw_step(plan: AdamW, grads, lr, step, seed: int = 0, grad_scale=None, ski
     if len(grads) != len(plan.params):
         raise ValueError(f"grads must hold one entry for each of the {len(plan.params)} parameters")
     dev, f32 = plan.device, torch.float32
-    pointers, kinds = [], plan._grad_dtypes
-    for i, (g, shape, dtype) in enumerate(zip(grads, plan._shapes, plan._dtypes)):
+    pointers, wide = [], []
+    for g, shape, dtype in zip(grads, plan._shapes, plan._dtypes):
         if g is None:
             pointers.append(0)
             continue
         if g.requires_grad:
-            _refuse_gradient(f"grads[{i}]")
+            _refuse_gradient(f"grads[{len(pointers)}]")
         if g.shape != shape or g.get_device() != dev or not g.is_contiguous():
-            raise ValueError(f"grads[{i}] must be a contiguous {list(shape)} tensor on cuda:{dev}")
+            raise ValueError(f"grads[{len(pointers)}] must be a contiguous {list(shape)} tensor on cuda:{dev}")
         if g.dtype is not dtype:
             if g.dtype is not f32:
-                raise ValueError(f"grads[{i}] must be {dtype} or float32")
-            if kinds is plan._grad_dtypes:
-                kinds = list(kinds)
-            kinds[i] = 0
+                raise ValueError(f"grads[{len(pointers)}] must be {dtype} or float32")
+            wide.append(len(pointers))
         pointers.append(g.data_ptr())
-    table = plan._table.copy()  # the plan's own stays as it is: calls of several threads do not meet
-    table["grad"] = pointers
-    if kinds is not plan._grad_dtypes:
-        table["grad_dtype"] = kinds
+    words = plan._words.copy()  # the plan's own stays as it is: calls of several threads do not meet
+    words[:, 1] = pointers
+    if wide:
+        words.view(_TENSOR)["grad_dtype"][wide] = 0
     o = _AdamWOptions(0.0, *plan.betas, plan.eps, 1, seed & 0xFFFFFFFF, plan.rounding == "stochastic")
     if isinstance(lr, torch.Tensor):
         o.lr_device = _scalar(lr, "lr", f32, dev)
@@ -761,7 +760,7 @@ def adamw_step(plan: AdamW, grads, lr, step, seed: int = 0, grad_scale=None, ski
     if skip is not None:
         o.skip = _scalar(skip, "skip", f32, dev)
     with _Scope(dev, stream) as handle:
-        rc = lib.spdy_adamw_step(table.ctypes.data, len(pointers), ctypes.byref(o), handle)
+        rc = lib.spdy_adamw_step(words.ctypes.data, len(pointers), ctypes.byref(o), handle)
     if rc:
         binding._check(rc, "spdy_adamw_step")
     if plan._leaves:  # a graph that was recorded before must notice
@@ -780,9 +779,9 @@ def adamw_moments(plan: AdamW, dtype=None, stream=None):
     if dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("dtype must be float32 or bfloat16")
     with _Scope(plan.device, stream) as handle:
-        out = [(torch.empty(shape, dtype=dtype, device="cuda"), torch.empty(shape, dtype=dtype, device="cuda")) for shape in plan._shapes]
-        pointers = np.array([[m.data_ptr(), v.data_ptr()] for m, v in out], dtype=np.uint64).T.copy()
-        rc = lib.spdy_adamw_moments(plan._table.ctypes.data, len(out), pointers[0].ctypes.data, pointers[1].ctypes.data, _TYPES[dtype], handle)
+        out = [(_empty_strided(shape, strides, dtype), _empty_strided(shape, strides, dtype)) for shape, strides in zip(plan._shapes, plan._strides)]
+        firsts, seconds = (np.array([pair[k].data_ptr() for pair in out], dtype=np.uint64) for k in (0, 1))
+        rc = lib.spdy_adamw_moments(plan._table.ctypes.data, len(out), firsts.ctypes.data, seconds.ctypes.data, _TYPES[dtype], handle)
     if rc:
         binding._check(rc, "spdy_adamw_moments")
     return out

@@ -172,7 +172,7 @@ def test_gradients_that_are_not_finite(bits, bad):
 
 
 @gpu
-@pytest.mark.parametrize("scale", [1e-30, 1e-19, 1e15])
+@pytest.mark.parametrize("scale", [1e-30, 1e-19, 1e5, 1e15, 1e19])
 def test_gradients_of_any_size(scale):
     n = 4096
     p = torch.ones(n, device="cuda")
