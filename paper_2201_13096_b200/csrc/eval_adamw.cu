@@ -17,8 +17,11 @@ using namespace spdy_eval;
 
 namespace {
 
-constexpr int kThreads = 256, kPer = 8, kChunk = kThreads * kPer;  // elements a thread and a block work on at a time
-constexpr int kBlock = 32;                                        // elements that share an exponent
+// A block works on 2048 elements at a time, a thread on 8 of them, or on 16 with moments in 8 bits, where what is done per thread
+// (addresses, the tensor's entry, the blocks' exponents) weighs more than registers.
+constexpr int kChunk = 2048, kBlock = 32;                          // kBlock: elements that share an exponent
+template <int BITS> constexpr int kPer = BITS == 8 ? 16 : 8;
+template <int BITS> constexpr int kThreads = kChunk / kPer<BITS>;
 
 struct Entry {
     void *param;
@@ -28,11 +31,12 @@ struct Entry {
     uint8_t *m_exp, *v_exp;
     int64_t n;
     uint32_t first;       // chunks of the tensors before it
-    float weight_decay;
+    float weight_decay, decay;  // decay: 1 - lr weight_decay, where lr is known
     uint32_t index;       // in the caller's list
-    uint32_t flags;       // kWide*, kKeepZeros
+    uint32_t flags;
+    uint32_t unused;
 };
-enum { kWideParam = 1, kWideGrad = 2, kWideMaster = 4, kKeepZeros = 8 };
+enum { kWide = 1, kKeepZeros = 2 };  // kWide: param, grad and master start on 16 bytes
 
 struct StepArgs {
     float b1, b2, g1, g2, eps, rate, root;  // g1 = 1 - b1, rate = lr / (1 - b1^t), root = 1 / sqrt(1 - b2^t)
@@ -64,100 +68,151 @@ template <bool SIGNED> constexpr int kField = SIGNED ? 14 : 30;
 
 // Eight numbers from their codes and the block's byte.  A code's bits, four below the top of a word, are the upper bits of a float
 // whose exponent is off by a known amount: one product puts it right (two where 2^(E - 14) or 2^(E - 30) is no float).
-template <bool SIGNED> __device__ __forceinline__ void decode(uint2 codes, uint32_t E, float *y)
+template <bool SIGNED, int N> __device__ __forceinline__ void decode(const uint32_t *codes, uint32_t E, float *y)
 {
     constexpr uint32_t most = 254 - 127 + kField<SIGNED>;  // the largest E whose factor is a float
     const float factor = E == 255 ? quiet_nan() : exponent(min(static_cast<int>(E), static_cast<int>(most)) + 127 - kField<SIGNED>);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const uint32_t top = __byte_perm(i < 4 ? codes.x : codes.y, 0, (i % 4) << 12 | 0x0444);  // the code in the highest byte
+    for (int i = 0; i < N; ++i) {
+        const uint32_t top = __byte_perm(codes[i / 4], 0, (i % 4) << 12 | 0x0444);  // the code in the highest byte
         y[i] = (SIGNED ? __uint_as_float(static_cast<uint32_t>(static_cast<int32_t>(top) >> 4) & 0x87f00000u) : __uint_as_float(top >> 4)) * factor;
     }
     if (E > most && E != 255)
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) y[i] *= exponent(127 + static_cast<int>(E - most));
+        for (int i = 0; i < N; ++i) y[i] *= exponent(127 + static_cast<int>(E - most));
 }
 
-// Codes of a thread's eight elements (a quarter of a block: four neighbouring lanes), and the block's byte.
-template <bool SIGNED> __device__ __forceinline__ uint2 encode(float *y, const uint32_t *random, uint32_t &E)
+// Codes of a thread's N elements (a part of a block, which neighbouring lanes share), and the block's byte.
+template <bool SIGNED, int N> __device__ __forceinline__ void encode(float *y, const uint32_t *random, uint32_t *codes, uint32_t &E)
 {
     float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) most = max_nan(most, fabsf(y[i]));
-    most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    for (int i = 0; i < N; ++i) most = max_nan(most, fabsf(y[i]));
+#pragma unroll
+    for (int d = 1; d < kBlock / N; d *= 2) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
     E = max(__float_as_uint(most) >> 23, 1u);
     const bool bad = E >= 254;
     int field = 127 + kField<SIGNED> - static_cast<int>(E);  // of the factor
     if (field < 1) {  // no float: the way down in two steps, of which the first is exact for all that is left after the second
         field += 113;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) y[i] *= 0x1p-113f;
+        for (int i = 0; i < N; ++i) y[i] *= 0x1p-113f;
     }
     if (bad) E = 255;
     const float factor = exponent(max(field, 1));
-    uint32_t x[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        x[i] = __float_as_uint(fabsf(y[i]) * factor) + (SIGNED ? random[i] & 0xfffffu : random[i] >> 12);
-        if (!SIGNED && y[i] > 0.f) x[i] = max(x[i], 1u << 20);
-        x[i] <<= 4;
-        if (SIGNED) x[i] |= __float_as_uint(y[i]) & 0x80000000u;
+    for (int i = 0; i < N; i += 4) {
+        uint32_t x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t bits = __float_as_uint(fabsf(y[i + k]) * factor);
+            if (SIGNED) {
+                x[k] = (bits + (random[i + k] & 0xfffffu)) << 4 | (__float_as_uint(y[i + k]) & 0x80000000u);
+            } else {  // the part of `random` below its upper 20 bits lies below the code's own last bit and carries nothing
+                x[k] = (bits << 4) + (random[i + k] >> 8);
+                if (y[i + k] > 0.f) x[k] = max(x[k], 1u << 24);
+            }
+        }
+        codes[i / 4] = bad ? 0 : __byte_perm(__byte_perm(x[0], x[1], 0x0073), __byte_perm(x[2], x[3], 0x0073), 0x5410);
     }
-    const auto join = [&](const uint32_t *four) { return __byte_perm(__byte_perm(four[0], four[1], 0x0073), __byte_perm(four[2], four[3], 0x0073), 0x5410); };
-    return bad ? make_uint2(0, 0) : make_uint2(join(x), join(x + 4));
 }
 
-// Eight elements from e on of a vector of n; `wide`: they may be moved 16 bytes at a time.
-template <class T> __device__ __forceinline__ void load8(const T *p, int64_t e, int64_t n, bool wide, float *f)
+// 16 bytes of a vector of which `left` elements exist, zeros for the others; and the way back.
+template <class T> __device__ __noinline__ uint4 gather(const T *p, int left)
 {
-    if (wide && e + kPer <= n) {
-        const uint4 *q = reinterpret_cast<const uint4 *>(p + e);
-        Elem<T>::unpack(load_stream(q), f);
-        if (sizeof(T) == 4) Elem<T>::unpack(load_stream(q + 1), f + 4);
+    constexpr int bits = 8 * sizeof(T), per = 32 / bits;
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        w[j] = 0;
+#pragma unroll
+        for (int k = 0; k < per; ++k) {
+            const int i = j * per + k;
+            uint32_t x = 0;
+            if (i < left) x = bits == 32 ? reinterpret_cast<const uint32_t *>(p)[i] : bits == 16 ? reinterpret_cast<const uint16_t *>(p)[i] : reinterpret_cast<const uint8_t *>(p)[i];
+            w[j] |= x << (bits * k & 31);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <class T> __device__ __noinline__ void scatter(T *p, int left, uint4 v)
+{
+    constexpr int bits = 8 * sizeof(T), per = 32 / bits;
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int k = 0; k < per; ++k) {
+            const int i = j * per + k;
+            if (i >= left) continue;
+            const uint32_t x = w[j] >> (bits * k & 31);
+            if (bits == 32) reinterpret_cast<uint32_t *>(p)[i] = x;
+            else if (bits == 16) reinterpret_cast<uint16_t *>(p)[i] = static_cast<uint16_t>(x);
+            else reinterpret_cast<uint8_t *>(p)[i] = static_cast<uint8_t>(x);
+        }
+}
+// N elements from `p` on; `whole`: all exist, and p lies on 16 bytes.
+template <class T, int N> __device__ __forceinline__ void load(const T *p, int left, bool whole, uint4 *raw)
+{
+    constexpr int per = 16 / sizeof(T);
+    if (whole) {
+#pragma unroll
+        for (int j = 0; j < N / per; ++j) raw[j] = load_stream(p + j * per);
     } else {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) f[i] = e + i < n ? Elem<T>::to_float(p[e + i]) : 0.f;
+        for (int j = 0; j < N / per; ++j) raw[j] = gather<T>(p + j * per, left - j * per);
     }
 }
-template <class T> __device__ __forceinline__ void store8(T *p, int64_t e, int64_t n, bool wide, const float *f)
+template <class T, int N> __device__ __forceinline__ void store(T *p, int left, bool whole, const uint4 *raw)
 {
-    if (wide && e + kPer <= n) {
-        uint4 *q = reinterpret_cast<uint4 *>(p + e);
-        store_stream(q, Elem<T>::pack(f));
-        if (sizeof(T) == 4) store_stream(q + 1, Elem<T>::pack(f + 4));
+    constexpr int per = 16 / sizeof(T);
+    if (whole) {
+#pragma unroll
+        for (int j = 0; j < N / per; ++j) store_stream(p + j * per, raw[j]);
     } else {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (e + i < n) p[e + i] = Elem<T>::from_float(f[i]);
+        for (int j = 0; j < N / per; ++j) scatter<T>(p + j * per, left - j * per, raw[j]);
     }
 }
-__device__ __forceinline__ uint2 load_codes(const uint8_t *p, int64_t e, int64_t n)
+template <class T, int N> __device__ __forceinline__ void unpack(const uint4 *raw, float *f)
 {
-    if (e + kPer <= n) return *reinterpret_cast<const uint2 *>(p + e);
-    uint32_t w[2] = {0, 0};
-    for (int i = 0; i < kPer && e + i < n; ++i) w[i / 4] |= static_cast<uint32_t>(p[e + i]) << 8 * (i % 4);
-    return make_uint2(w[0], w[1]);
+#pragma unroll
+    for (int j = 0; j < N / Elem<T>::kVec; ++j) Elem<T>::unpack(raw[j], f + j * Elem<T>::kVec);
 }
-__device__ __forceinline__ void store_codes(uint8_t *p, int64_t e, int64_t n, uint2 v)
+template <class T, int N> __device__ __forceinline__ void pack(const float *f, uint4 *raw)
 {
-    if (e + kPer <= n) {
-        *reinterpret_cast<uint2 *>(p + e) = v;
-        return;
-    }
-    for (int i = 0; i < kPer && e + i < n; ++i) p[e + i] = static_cast<uint8_t>((i < 4 ? v.x : v.y) >> 8 * (i % 4));
+#pragma unroll
+    for (int j = 0; j < N / Elem<T>::kVec; ++j) raw[j] = Elem<T>::pack(f + j * Elem<T>::kVec);
 }
 
 // y to 16 bits, up with the probability of the part cut off: fp32's pattern again, brought to half precision's exponents by a power of two.
-template <class T> __device__ __forceinline__ float round_random(float y, uint32_t random)
+template <class T> __device__ __forceinline__ uint32_t round_random(float y, uint32_t random)
 {
     constexpr bool brain = std::is_same<T, __nv_bfloat16>::value;
     constexpr int shift = brain ? 16 : 13;
-    uint32_t code = (__float_as_uint(fabsf(y) * (brain ? 1.f : 0x1p-112f)) + (random >> (32 - shift))) >> shift;
-    code = min(code, brain ? 0x7f80u : 0x7c00u) | (__float_as_uint(y) >> 16 & 0x8000u);
-    const unsigned short bits = static_cast<unsigned short>(code);
-    const float rounded = brain ? __uint_as_float(code << 16) : __half2float(__ushort_as_half(bits));
-    return fabsf(y) <= 3.4028235e38f ? rounded : y;
+    const uint32_t sign = __float_as_uint(y) >> 16 & 0x8000u;
+    const uint32_t code = (__float_as_uint(fabsf(y) * (brain ? 1.f : 0x1p-112f)) + (random >> (32 - shift))) >> shift;
+    const uint32_t infinite = brain ? 0x7f80u : 0x7c00u;
+    if (!(fabsf(y) <= 3.4028235e38f)) return y == y ? sign | infinite : 0x7fffu;  // a NaN in both
+    return sign | min(code, infinite);
+}
+// N of them.  In bf16, finite numbers only need the addition: its carry ends at the exponent, and the sign stays above it.
+template <class T, int N> __device__ __forceinline__ void pack_random(const float *y, const uint32_t *random, uint4 *raw)
+{
+    uint32_t w[N / 2];
+    float odd = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) odd = fmaf(y[i], 0.f, odd);
+    if (std::is_same<T, __nv_bfloat16>::value && odd == 0.f) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2)
+            w[i / 2] = __byte_perm(__float_as_uint(y[i]) + (random[i] * 0x9e3779b1u >> 16), __float_as_uint(y[i + 1]) + (random[i + 1] * 0x9e3779b1u >> 16), 0x7632);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) w[i / 2] = round_random<T>(y[i], random[i] * 0x9e3779b1u) | round_random<T>(y[i + 1], random[i + 1] * 0x9e3779b1u) << 16;
+    }
+#pragma unroll
+    for (int j = 0; j < N / 8; ++j) raw[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
 }
 
 __device__ double power(double b, int64_t t)
@@ -189,7 +244,7 @@ __device__ __forceinline__ float quotient(float a, float b)
 }
 
 template <class P, class G, int BITS, bool MASTER, bool RANDOM, int CAP>
-__global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ StepArgs s)
+__global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_constant__ Table<CAP> table, const __grid_constant__ StepArgs s)
 {
     if (s.skip && *s.skip != 0.f) return;
     __shared__ float derived[3];
@@ -210,93 +265,106 @@ __global__ void __launch_bounds__(kThreads) step_kernel(const __grid_constant__ 
     for (uint32_t chunk = blockIdx.x; chunk < table.chunks; chunk += gridDim.x) {
         while (at + 1 < table.count && chunk >= table.e[at + 1].first) ++at;
         const Entry &t = table.e[at];
-        const int64_t n = t.n, e = static_cast<int64_t>(chunk - t.first) * kChunk + threadIdx.x * kPer;
-        float p[kPer], g[kPer], m[kPer], v[kPer];
-        if (MASTER) load8(t.master, e, n, t.flags & kWideMaster, p);
-        else load8(static_cast<const P *>(t.param), e, n, t.flags & kWideParam, p);
-        load8(static_cast<const G *>(t.grad), e, n, t.flags & kWideGrad, g);
-        if (BITS == 32) {
-            load8(static_cast<const float *>(t.m), e, n, true, m);
-            load8(static_cast<const float *>(t.v), e, n, true, v);
+        constexpr int N = kPer<BITS>;
+        using W = typename std::conditional<MASTER, float, P>::type;  // what is stepped
+        using M = typename std::conditional<BITS == 32, float, uint8_t>::type;
+        constexpr int kW = N * static_cast<int>(sizeof(W)) / 16, kG = N * static_cast<int>(sizeof(G)) / 16, kM = N * static_cast<int>(sizeof(M)) / 16;
+        const int64_t e = static_cast<int64_t>(chunk - t.first) * kChunk + threadIdx.x * N;
+        const int left = static_cast<int>(min(t.n - e, static_cast<int64_t>(N)));  // not above 0 behind the tensor's end
+        const bool all = left == N, whole = all && (t.flags & kWide);
+        W *weights = MASTER ? reinterpret_cast<W *>(t.master) : static_cast<W *>(t.param);
+        uint4 rw[kW], rg[kG], rm[kM], rv[kM];
+        load<W, N>(weights + e, left, whole, rw);
+        load<G, N>(static_cast<const G *>(t.grad) + e, left, whole, rg);
+        load<M, N>(static_cast<const M *>(t.m) + e, left, all, rm);
+        load<M, N>(static_cast<const M *>(t.v) + e, left, all, rv);
+        float p[N], m[N], v[N];
+        if constexpr (BITS == 32) {
+            unpack<float, N>(rm, m), unpack<float, N>(rv, v);
         } else {
-            const uint2 cm = load_codes(static_cast<const uint8_t *>(t.m), e, n), cv = load_codes(static_cast<const uint8_t *>(t.v), e, n);
-            decode<true>(cm, e < n ? t.m_exp[e / kBlock] : 0, m), decode<false>(cv, e < n ? t.v_exp[e / kBlock] : 0, v);
-            if (e + kPer > n)  // a block that is not finite has nothing behind the tensor's end
+            const uint32_t em = left > 0 ? t.m_exp[e / kBlock] : 0, ev = left > 0 ? t.v_exp[e / kBlock] : 0;
+            decode<true, N>(reinterpret_cast<const uint32_t *>(rm), em, m), decode<false, N>(reinterpret_cast<const uint32_t *>(rv), ev, v);
+            if (!all)  // a block that is not finite has nothing behind the tensor's end
 #pragma unroll
-                for (int i = 0; i < kPer; ++i)
-                    if (e + i >= n) m[i] = v[i] = 0.f;
+                for (int i = 0; i < N; ++i)
+                    if (i >= left) m[i] = v[i] = 0.f;
         }
-        const float decay = static_cast<float>(1.0 - lr * static_cast<double>(t.weight_decay));
-        uint32_t random[kPer];
+        const float decay = s.lr_device ? static_cast<float>(1.0 - lr * static_cast<double>(t.weight_decay)) : t.decay;
+        const bool keep = t.flags & kKeepZeros;
+        float g[N];
+        unpack<W, N>(rw, p), unpack<G, N>(rg, g);
+        if (s.grad_scale)
+#pragma unroll
+            for (int i = 0; i < N; ++i) g[i] *= scale;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            // every product and sum rounded by itself: the 8-bit codes below are those of the plain formula, bit for bit
+            m[i] = m[i] * s.b1 + g[i] * s.g1;
+            v[i] = v[i] * s.b2 + g[i] * s.g2 * g[i];
+        }
+        if (keep)  // and the weight, with m = 0, stays 0 by itself
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (p[i] == 0.f) m[i] = v[i] = 0.f;
+        if (s.eps >= 1e-9f) {  // roots of numbers below 2^-126 do not show beside such an eps
+#pragma unroll
+            for (int i = 0; i < N; ++i) p[i] = fmaf(p[i], decay, -quotient(m[i] * rate, fmaf(root_flushed(v[i]), root, s.eps)));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) p[i] = keep && p[i] == 0.f ? 0.f : fmaf(p[i], decay, -quotient(m[i] * rate, fmaf(root_of(v[i]), root, s.eps)));
+        }
+        uint32_t random[N];
         if (BITS == 8 || RANDOM) {
             const uint32_t start = mix(key + t.index) + static_cast<uint32_t>(e) + static_cast<uint32_t>(e >> 32) * 0x9e3779b9u;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) random[i] = mix(start + i);
+            for (int i = 0; i < N; ++i) random[i] = mix(start + i);
         }
-        float old[kPer], below[kPer];
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            // every product and sum rounded by itself: the 8-bit codes below are those of the plain formula, bit for bit
-            const float gs = g[i] * scale;
-            m[i] = m[i] * s.b1 + gs * s.g1;
-            v[i] = v[i] * s.b2 + gs * s.g2 * gs;
-            old[i] = p[i];
-        }
-        if (s.eps >= 1e-9f) {  // roots of numbers below 2^-126 do not show beside such an eps
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) below[i] = fmaf(root_flushed(v[i]), root, s.eps);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) below[i] = fmaf(root_of(v[i]), root, s.eps);
-        }
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) p[i] = fmaf(old[i], decay, -quotient(m[i] * rate, below[i]));
-        if (t.flags & kKeepZeros)
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (old[i] == 0.f) p[i] = m[i] = v[i] = 0.f;
-        if (BITS == 32) {
-            store8(static_cast<float *>(t.m), e, n, true, m);
-            store8(static_cast<float *>(t.v), e, n, true, v);
+        if (MASTER) store<W, N>(weights + e, left, whole, (pack<W, N>(p, rw), rw));
+        uint4 rp[N * static_cast<int>(sizeof(P)) / 16];
+        if constexpr (RANDOM) pack_random<P, N>(p, random, rp);
+        else pack<P, N>(p, rp);
+        store<P, N>(static_cast<P *>(t.param) + e, left, whole, rp);
+        if constexpr (BITS == 32) {
+            pack<float, N>(m, rm), pack<float, N>(v, rv);
         } else {
             uint32_t em, ev;
-            const uint2 cm = encode<true>(m, random, em), cv = encode<false>(v, random, ev);
-            if (e < n) {
-                store_codes(static_cast<uint8_t *>(t.m), e, n, cm), store_codes(static_cast<uint8_t *>(t.v), e, n, cv);
-                if ((threadIdx.x & 3) == 0) t.m_exp[e / kBlock] = static_cast<uint8_t>(em), t.v_exp[e / kBlock] = static_cast<uint8_t>(ev);
-            }
+            encode<true, N>(m, random, reinterpret_cast<uint32_t *>(rm), em), encode<false, N>(v, random, reinterpret_cast<uint32_t *>(rv), ev);
+            if (left > 0 && threadIdx.x % (kBlock / N) == 0) t.m_exp[e / kBlock] = static_cast<uint8_t>(em), t.v_exp[e / kBlock] = static_cast<uint8_t>(ev);
         }
-        if (MASTER) store8(t.master, e, n, t.flags & kWideMaster, p);
-        if (RANDOM)
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) p[i] = round_random<P>(p[i], random[i] * 0x9e3779b1u);
-        store8(static_cast<P *>(t.param), e, n, t.flags & kWideParam, p);
+        store<M, N>(static_cast<M *>(t.m) + e, left, all, rm);
+        store<M, N>(static_cast<M *>(t.v) + e, left, all, rv);
     }
 }
 
 // Moments in 8 bits as numbers.  param and master of the table: where the first and the second go.
-template <class T, int CAP> __global__ void __launch_bounds__(kThreads) moments_kernel(const __grid_constant__ Table<CAP> table)
+template <class T, int CAP> __global__ void __launch_bounds__(kThreads<8>) moments_kernel(const __grid_constant__ Table<CAP> table)
 {
+    constexpr int N = kPer<8>;
     uint32_t at = 0;
     for (uint32_t chunk = blockIdx.x; chunk < table.chunks; chunk += gridDim.x) {
         while (at + 1 < table.count && chunk >= table.e[at + 1].first) ++at;
         const Entry &t = table.e[at];
-        const int64_t n = t.n, e = static_cast<int64_t>(chunk - t.first) * kChunk + threadIdx.x * kPer;
-        if (e >= n) continue;
-        const uint2 cm = load_codes(static_cast<const uint8_t *>(t.m), e, n), cv = load_codes(static_cast<const uint8_t *>(t.v), e, n);
-        float m[kPer], v[kPer];
-        decode<true>(cm, t.m_exp[e / kBlock], m), decode<false>(cv, t.v_exp[e / kBlock], v);
-        store8(static_cast<T *>(t.param), e, n, t.flags & kWideParam, m);
-        store8(reinterpret_cast<T *>(t.master), e, n, t.flags & kWideMaster, v);
+        const int64_t e = static_cast<int64_t>(chunk - t.first) * kChunk + threadIdx.x * N;
+        const int left = static_cast<int>(min(t.n - e, static_cast<int64_t>(N)));
+        if (left <= 0) continue;
+        const bool all = left == N, whole = all && (t.flags & kWide);
+        uint4 rm, rv, out[N * static_cast<int>(sizeof(T)) / 16];
+        load<uint8_t, N>(static_cast<const uint8_t *>(t.m) + e, left, all, &rm), load<uint8_t, N>(static_cast<const uint8_t *>(t.v) + e, left, all, &rv);
+        float y[N];
+        decode<true, N>(reinterpret_cast<const uint32_t *>(&rm), t.m_exp[e / kBlock], y);
+        pack<T, N>(y, out);
+        store<T, N>(static_cast<T *>(t.param) + e, left, whole, out);
+        decode<false, N>(reinterpret_cast<const uint32_t *>(&rv), t.v_exp[e / kBlock], y);
+        pack<T, N>(y, out);
+        store<T, N>(reinterpret_cast<T *>(t.master) + e, left, whole, out);
     }
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-template <class K, int CAP, class... A> int launch(K kernel, const Table<CAP> &table, cudaStream_t stream, A... more)
+template <class K, int CAP, class... A> int launch(K kernel, int threads, const Table<CAP> &table, cudaStream_t stream, A... more)
 {
-    // enough blocks to fill the device eight times over a multiprocessor; the rest is walked over
-    const uint32_t most = static_cast<uint32_t>(sm_count()) * 8;
-    kernel<<<table.chunks < most ? table.chunks : most, kThreads, 0, stream>>>(table, more...);
+    const uint32_t most = static_cast<uint32_t>(sm_count()) * (2048 / threads);  // what can be resident; the rest is walked over
+    kernel<<<table.chunks < most ? table.chunks : most, threads, 0, stream>>>(table, more...);
     return finish_launch();
 }
 
@@ -337,12 +405,12 @@ template <class P, class G, int BITS, bool MASTER, bool RANDOM> int step_kind(in
     const auto fill = [&](Entry &e, int32_t i) {
         const spdy_adamw_tensor &t = tensors[i];
         e.param = t.param, e.grad = t.grad, e.master = t.master, e.m = t.m, e.v = t.v, e.m_exp = t.m_exp, e.v_exp = t.v_exp;
-        e.weight_decay = t.weight_decay;
-        e.flags = (aligned(t.param, 16) ? kWideParam : 0) | (aligned(t.grad, 16) ? kWideGrad : 0) | (aligned(t.master, 16) ? kWideMaster : 0) | (t.keep_zeros ? kKeepZeros : 0);
+        e.weight_decay = t.weight_decay, e.decay = static_cast<float>(1.0 - s.lr * static_cast<double>(t.weight_decay));
+        e.flags = (aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.master, 16) ? kWide : 0) | (t.keep_zeros ? kKeepZeros : 0);
     };
     const auto go = [&](const auto &table) {
         constexpr int cap = static_cast<int>(sizeof(table.e) / sizeof(Entry));
-        return launch(step_kernel<P, G, BITS, MASTER, RANDOM, cap>, table, stream, s);
+        return launch(step_kernel<P, G, BITS, MASTER, RANDOM, cap>, kThreads<BITS>, table, stream, s);
     };
     return all_batches(count, tensors, wanted, fill, go, go);
 }
@@ -423,11 +491,11 @@ int spdy_adamw_moments(const spdy_adamw_tensor *tensors, int32_t count, void *co
         const spdy_adamw_tensor &t = tensors[i];
         e = {};
         e.param = m_out[i], e.master = static_cast<float *>(v_out[i]), e.m = t.m, e.v = t.v, e.m_exp = t.m_exp, e.v_exp = t.v_exp;
-        e.flags = (aligned(m_out[i], 16) ? kWideParam : 0) | (aligned(v_out[i], 16) ? kWideMaster : 0);
+        e.flags = aligned(m_out[i], 16) && aligned(v_out[i], 16) ? kWide : 0;
     };
     const auto go = [&](const auto &table) {
         constexpr int cap = static_cast<int>(sizeof(table.e) / sizeof(Entry));
-        return out_dtype == SPDY_F32 ? launch(moments_kernel<float, cap>, table, stream) : launch(moments_kernel<__nv_bfloat16, cap>, table, stream);
+        return out_dtype == SPDY_F32 ? launch(moments_kernel<float, cap>, kThreads<8>, table, stream) : launch(moments_kernel<__nv_bfloat16, cap>, kThreads<8>, table, stream);
     };
     return all_batches(count, tensors, wanted, fill, go, go);
 }
