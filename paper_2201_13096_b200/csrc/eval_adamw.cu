@@ -53,6 +53,18 @@ template <int CAP> struct Table {
 };
 constexpr int kFew = 16, kMany = 360;
 
+// The tensor that a chunk belongs to.
+template <int CAP> __device__ __forceinline__ uint32_t tensor_of(const Table<CAP> &table, uint32_t chunk)
+{
+    uint32_t low = 0, high = table.count;  // first[low] <= chunk < first[high]
+    while (high - low > 1) {
+        const uint32_t mid = (low + high) / 2;
+        if (chunk >= table.e[mid].first) low = mid;
+        else high = mid;
+    }
+    return low;
+}
+
 // A hash of 32 bits: two odd multipliers, each of which carries bits up, and shifts that bring them down again.
 SPDY_EVAL_FN uint32_t mix(uint32_t x)
 {
@@ -151,13 +163,14 @@ template <class T> __device__ __noinline__ void scatter(T *p, int left, uint4 v)
             else reinterpret_cast<uint8_t *>(p)[i] = static_cast<uint8_t>(x);
         }
 }
+// Everything is read once and written once: first to leave L2 (150 M elements with fp32 states and masters 653 us without that, 614 with it).
 // N elements from `p` on; `whole`: all exist, and p lies on 16 bytes.
 template <class T, int N> __device__ __forceinline__ void load(const T *p, int left, bool whole, uint4 *raw)
 {
     constexpr int per = 16 / sizeof(T);
     if (whole) {
 #pragma unroll
-        for (int j = 0; j < N / per; ++j) raw[j] = load_stream(p + j * per);
+        for (int j = 0; j < N / per; ++j) raw[j] = load_last(p + j * per);
     } else {
 #pragma unroll
         for (int j = 0; j < N / per; ++j) raw[j] = gather<T>(p + j * per, left - j * per);
@@ -168,7 +181,7 @@ template <class T, int N> __device__ __forceinline__ void store(T *p, int left, 
     constexpr int per = 16 / sizeof(T);
     if (whole) {
 #pragma unroll
-        for (int j = 0; j < N / per; ++j) store_stream(p + j * per, raw[j]);
+        for (int j = 0; j < N / per; ++j) store_last(p + j * per, raw[j]);
     } else {
 #pragma unroll
         for (int j = 0; j < N / per; ++j) scatter<T>(p + j * per, left - j * per, raw[j]);
@@ -261,7 +274,7 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
         rate = derived[0], root = derived[1];
     }
     const float scale = s.grad_scale ? *s.grad_scale : 1.f;
-    uint32_t at = 0;
+    uint32_t at = tensor_of(table, blockIdx.x);
     for (uint32_t chunk = blockIdx.x; chunk < table.chunks; chunk += gridDim.x) {
         while (at + 1 < table.count && chunk >= table.e[at + 1].first) ++at;
         const Entry &t = table.e[at];
@@ -340,7 +353,7 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
 template <class T, int CAP> __global__ void __launch_bounds__(kThreads<8>) moments_kernel(const __grid_constant__ Table<CAP> table)
 {
     constexpr int N = kPer<8>;
-    uint32_t at = 0;
+    uint32_t at = tensor_of(table, blockIdx.x);
     for (uint32_t chunk = blockIdx.x; chunk < table.chunks; chunk += gridDim.x) {
         while (at + 1 < table.count && chunk >= table.e[at + 1].first) ++at;
         const Entry &t = table.e[at];
@@ -361,9 +374,11 @@ template <class T, int CAP> __global__ void __launch_bounds__(kThreads<8>) momen
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-template <class K, int CAP, class... A> int launch(K kernel, int threads, const Table<CAP> &table, cudaStream_t stream, A... more)
+// A block per chunk: with blocks that walk over several, fp32 states ran at 5.5 TB/s instead of 6.4 (a block's loads wait for its stores).
+// Where each block has to work out the step's numbers first, only as many as can be resident.
+template <class K, int CAP, class... A> int launch(K kernel, int threads, bool resident, const Table<CAP> &table, cudaStream_t stream, A... more)
 {
-    const uint32_t most = static_cast<uint32_t>(sm_count()) * (2048 / threads);  // what can be resident; the rest is walked over
+    const uint32_t most = resident ? static_cast<uint32_t>(sm_count()) * (2048 / threads) : 0x7fffffffu;
     kernel<<<table.chunks < most ? table.chunks : most, threads, 0, stream>>>(table, more...);
     return finish_launch();
 }
@@ -410,7 +425,7 @@ template <class P, class G, int BITS, bool MASTER, bool RANDOM> int step_kind(in
     };
     const auto go = [&](const auto &table) {
         constexpr int cap = static_cast<int>(sizeof(table.e) / sizeof(Entry));
-        return launch(step_kernel<P, G, BITS, MASTER, RANDOM, cap>, kThreads<BITS>, table, stream, s);
+        return launch(step_kernel<P, G, BITS, MASTER, RANDOM, cap>, kThreads<BITS>, s.step_device != nullptr, table, stream, s);
     };
     return all_batches(count, tensors, wanted, fill, go, go);
 }
@@ -495,7 +510,7 @@ int spdy_adamw_moments(const spdy_adamw_tensor *tensors, int32_t count, void *co
     };
     const auto go = [&](const auto &table) {
         constexpr int cap = static_cast<int>(sizeof(table.e) / sizeof(Entry));
-        return out_dtype == SPDY_F32 ? launch(moments_kernel<float, cap>, kThreads<8>, table, stream) : launch(moments_kernel<__nv_bfloat16, cap>, kThreads<8>, table, stream);
+        return out_dtype == SPDY_F32 ? launch(moments_kernel<float, cap>, kThreads<8>, false, table, stream) : launch(moments_kernel<__nv_bfloat16, cap>, kThreads<8>, false, table, stream);
     };
     return all_batches(count, tensors, wanted, fill, go, go);
 }
