@@ -6,13 +6,17 @@
 // is multiplied.  What is done with a tile differs:
 //   kStats   logits of 256 rows and ids -> per row the largest, the sum of exponentials relative to it, and the sum that the
 //            entropy needs; the given token's logit.  A second kernel joins a row's tiles in their order.
-//   kGrad    the same logits again -> the gradient by the logits, rounded to 16 bits, of one piece of the vocabulary
-//   kHidden  (the piece's gradient) x (the piece's rows of weight): fp32 sums of dhidden, added up over the pieces
-//   kWeight  (the piece's gradient)^T x hidden: the piece's rows of dweight (kWeightParts: as fp32 sums, where few tiles share
-//            their summed index among more multiprocessors)
-// The gradient's piece is the only thing of size rows x ids, and pieces are as wide as a fixed budget allows.  In the last two products
-// one or both operands have the summed index as their rows ("MN-major"); TMA brings them as boxes of 64 columns, and the matrix
-// descriptors name that order, so nothing is transposed.
+//   kLogits  the same, and the logits are kept, in 16 bits as logarithms relative to the largest of 64, for a kernel that turns them into the
+//            gradient by them in place
+//   kGrad    the logits once more -> the gradient by them, rounded to 16 bits
+//   kHidden  gradient x weight: fp32 sums of dhidden
+//   kWeight  gradient^T x hidden: dweight (kWeightParts: as fp32 sums)
+// Two plans keep what is of size rows x ids within a budget.  By ids (a backward call, whose sums are known, and where dbias is wanted,
+// whose fp32 the kept logits would not reach): the gradient of all rows for a piece of the vocabulary at a time, dhidden added up over
+// the pieces; the logits are multiplied again.  By rows (the rest of the calls that give values and gradients at once): the
+// logits of some rows and all ids at a time, dweight added up over them; each
+// product is done once.  In the last two products one or both operands have the summed index as their rows ("MN-major"); TMA brings
+// them as boxes of 64 columns, and the matrix descriptors name that order, so nothing is transposed.
 #include "eval_tensor.cuh"
 
 using namespace spdy_eval;
@@ -33,7 +37,7 @@ constexpr int kStageBytes = kSlices * kSliceBytes, kStages = 196608 / kStageByte
 constexpr int kStageK = kSlices * BK;
 constexpr int kConsts = 8;                               // floats per row that the gradient needs
 
-enum Kind { kStats, kGrad, kHidden, kWeight, kWeightParts };
+enum Kind { kStats, kLogits, kGrad, kHidden, kWeight, kWeightParts };
 
 // Which operands have the summed index as their rows.
 template <int KIND> struct Order {
@@ -43,7 +47,7 @@ template <int KIND> struct Order {
 struct ProductArgs {
     int64_t M, N;                  // rows and columns of the result that exist
     int tiles_m, tiles_n, splits, group, k_blocks;
-    int b_row0;                    // first row of the second operand
+    int a_row0, b_row0;            // first rows of the operands
     // kStats, kGrad
     const void *bias, *tokens;
     int bias_type, index_bits;
@@ -55,8 +59,11 @@ struct ProductArgs {
     const uint32_t *scale_bits;    // NULL, or the largest gradient's bits (half precision)
     float *column_sums;            // NULL, or [row groups of 32][N]
     int64_t ld_sums;
-    void *out;                     // kGrad: the piece; kWeight: 16 bits; parts: fp32 [splits][M][ldo]
+    float *tops;                   // kLogits: [ids / 64][padded_rows], what a row's 64 codes are relative to
+    void *out;                     // kLogits: codes; kGrad: the piece; kWeight: 16 bits; parts: fp32 [splits][M][ldo]
     int64_t ldo;
+    const float *sums;             // kWeight: NULL, or fp32 [M][ld_old] to add
+    int64_t ld_old;
     int add, width;                // parts: to what is there already; kWeight: 32 or 16 if every row of out starts on as many bytes, else 0
 };
 
@@ -192,6 +199,66 @@ __device__ __forceinline__ Sums carry_stats(const ProductArgs &a, uint32_t tmem,
     return sums;
 }
 
+// A kept logit: how far log2 of its exponential lies below that of the largest among the row's 64 ids of a warp, in steps of 2^-10
+// octaves over 64 octaves for bf16, 2^-11 over 32 for half precision, whose own numbers end sooner.  p comes out within 2^-11 ln 2 =
+// 3.4e-4 of itself (1.7e-4), beside the 16-bit rounding that follows of 3.9e-3 (4.9e-4).  The last code is "nothing".
+template <class T> constexpr float kSteps = std::is_same<T, __nv_bfloat16>::value ? 1024.f : 2048.f;
+constexpr uint32_t kNothing = 65535;
+
+// As carry_stats, with the codes.  The accumulator is read twice: the codes need the largest first.
+template <class T, class Ready, class Release>
+__device__ __forceinline__ Sums carry_logits(const ProductArgs &a, uint32_t tmem, int64_t m, int64_t n0, float *bias, Ready ready, Release release)
+{
+    int64_t token = -1;
+    if (m < a.M && a.token_logit) token = token_at(a.tokens, a.index_bits, m);
+    stage_bias(a, n0, bias);
+    if (!ready()) {
+        if (token >= n0 && token < n0 + kWarpColumns && token < a.N) a.token_logit[m] = quiet_nan();
+        return {0.f, quiet_nan(), quiet_nan()};  // the row's sum is NaN, and with it all that comes of its codes
+    }
+    Sums sums = {neg_inf(), 0.f, 0.f};
+#pragma unroll 1
+    for (int c = 0; c < kWarpColumns; c += 16) {
+        float f[16];
+        load_logits(a, tmem + c, n0 + c, bias + c, f);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums.m = fmaxf(sums.m, f[i]);
+    }
+    const bool inside = m < a.M && n0 < a.N;
+    if (inside) a.tops[n0 / kWarpColumns * a.padded_rows + m] = sums.m;
+    const float ref = sums.m == neg_inf() ? 0.f : sums.m;
+    uint16_t *to = static_cast<uint16_t *>(a.out) + m * a.ldo + n0;
+#pragma unroll 1
+    for (int c = 0; c < kWarpColumns; c += 16) {
+        float f[16];
+        load_logits(a, tmem + c, n0 + c, bias + c, f);
+        if (c + 16 == kWarpColumns) release();
+        const int64_t at = token - (n0 + c);
+        if (at >= 0 && at < 16 && token < a.N) {
+            float x = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x = at == i ? f[i] : x;
+            a.token_logit[m] = x;
+        }
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            uint32_t code[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float d = max_nan((f[i + k] - ref) * a.c, -200.f), e = ex2(d);  // below -200 e is 0
+                sums.s += e;
+                sums.t = fmaf(e, d, sums.t);
+                // 2^23 and a number below 2^16: rounded to a whole number, in the lower half of the pattern
+                code[k] = __float_as_uint(fmaf(fmaxf(d, -static_cast<float>(kNothing) / kSteps<T>), -kSteps<T>, 8388608.f));
+            }
+            w[i / 2] = __byte_perm(code[0], code[1], 0x5410);
+        }
+        if (inside && n0 + c < a.N) store32(to + c, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));  // ldo is a multiple of 64
+    }
+    return sums;
+}
+
 // Sums over the 32 rows of 16 columns, each lane's `f`: of column `lane / 2` in the lane, by halves of the columns that partners exchange.
 __device__ __forceinline__ float sum_columns(const float *f)
 {
@@ -212,21 +279,33 @@ __device__ __forceinline__ float sum_columns(const float *f)
     return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1);
 }
 
-// Gradient by 64 logits of a row: d = [v = token] a - p (ab + b2 y), y = log2 p = (x - ref) c - ls, rounded to 16 bits once.
-// ENT: with the entropy's gradient (b2 is not 0).
+// What the gradient by a row's logits needs: d = [v = token] hit - p (all + slope y), y = log2 p = (x - ref) c - ls.
+struct RowConsts {
+    float ref, ls, hit, all, slope;
+    int token;
+};
+__device__ __forceinline__ RowConsts row_consts(const float *consts, int64_t m, float scale)
+{
+    const float4 k = reinterpret_cast<const float4 *>(consts)[2 * m], more = reinterpret_cast<const float4 *>(consts)[2 * m + 1];
+    return {k.x, k.y, k.z * scale, k.w * scale, more.x * scale, __float_as_int(more.y)};
+}
+// -p (all + slope y).  ENT: with the entropy's gradient (slope is not 0); below -200 p is 0.
+template <bool ENT> __device__ __forceinline__ float grad_at(float y, const RowConsts &k)
+{
+    y = min_nan(y, 0.f);
+    return ENT ? -ex2(y) * fmaf(k.slope, max_nan(y, -200.f), k.all) : -ex2(y) * k.all;
+}
+template <bool ENT> __device__ __forceinline__ float grad_of(float x, const RowConsts &k, float c) { return grad_at<ENT>(fmaf(x - k.ref, c, -k.ls), k); }
+
+// Gradient by 64 logits of a row, rounded to 16 bits once.
 template <class T, bool ENT, class Ready, class Release>
 __device__ __forceinline__ void carry_grad(const ProductArgs &a, uint32_t tmem, int64_t m0, int64_t n0, float *bias, Ready ready, Release release)
 {
     const int lane = threadIdx.x & 31;
     const int64_t m = m0 + lane;
     const bool inside = m < a.M;
-    float4 k = make_float4(0.f, 0.f, 0.f, 0.f), more = make_float4(0.f, __int_as_float(-1), 0.f, 0.f);
-    if (inside) {
-        k = reinterpret_cast<const float4 *>(a.consts)[2 * m], more = reinterpret_cast<const float4 *>(a.consts)[2 * m + 1];
-        const float scale = power_of_two(scale_power(a.scale_bits));
-        k.z *= scale, k.w *= scale, more.x *= scale;
-    }
-    const int64_t token = __float_as_int(more.y);
+    RowConsts k = {0.f, 0.f, 0.f, 0.f, 0.f, -1};
+    if (inside) k = row_consts(a.consts, m, power_of_two(scale_power(a.scale_bits)));
     stage_bias(a, n0, bias);
     const bool ok = ready();
     char *to = static_cast<char *>(a.out) + (m * a.ldo + n0) * 2;
@@ -237,16 +316,12 @@ __device__ __forceinline__ void carry_grad(const ProductArgs &a, uint32_t tmem, 
         if (c + 16 == kWarpColumns) release();
         if (n0 + c >= a.N) continue;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float y = min_nan(fmaf(f[i] - k.x, a.c, -k.y), 0.f);
-            f[i] = ENT ? -ex2(y) * fmaf(more.x, max_nan(y, -200.f), k.w) : -ex2(y) * k.w;
-            if (!ok) f[i] = quiet_nan();
-        }
-        const int64_t at = token - (a.v0 + n0 + c);
+        for (int i = 0; i < 16; ++i) f[i] = ok ? grad_of<ENT>(f[i], k, a.c) : quiet_nan();
+        const int64_t at = k.token - (a.v0 + n0 + c);
         if (at >= 0 && at < 16)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (at == i) f[i] += k.z;
+                if (at == i) f[i] += k.hit;
         if (inside) store32(to + 2 * c, Elem<T>::pack(f), Elem<T>::pack(f + 8));
         if (a.column_sums) {
             if (!inside)
@@ -314,7 +389,22 @@ __device__ __forceinline__ void carry_store(const ProductArgs &a, uint32_t tmem,
         if (c + 16 == kWarpColumns) release();
         if (n0 + c >= a.N) continue;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) f[i] = ok ? f[i] * scale : quiet_nan();
+        for (int i = 0; i < 16; ++i) f[i] = ok ? f[i] : quiet_nan();
+        if (a.sums && m < a.M) {
+            const float *from = a.sums + m * a.ld_old + n0 + c;
+#pragma unroll
+            for (int h = 0; h < 16; h += 8) {
+                if (n0 + c + h >= a.N) break;  // ld_old is a multiple of 8
+                uint4 x, y;
+                float old[8];
+                load32(from + h, x, y);
+                Elem<float>::unpack(x, old), Elem<float>::unpack(y, old + 4);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[h + i] += old[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) f[i] *= scale;
         const uint4 lo = Elem<T>::pack(f), hi = Elem<T>::pack(f + 8);
         if (!a.width || n0 + c + 16 > a.N) {
             store_turned(a, m0, n0 + c, lo, hi, turn);
@@ -327,7 +417,7 @@ __device__ __forceinline__ void carry_store(const ProductArgs &a, uint32_t tmem,
 
 // ---------------------------------------------------------------------------------------------- the product
 constexpr int kBiasBytes = kEpilogueWarps * kWarpColumns * 4, kTurnBytes = kEpilogueWarps * 1024, kJoinBytes = 2 * 16 * 32 * 12;
-template <int KIND> constexpr int extra_bytes() { return KIND == kStats ? kBiasBytes + kJoinBytes : KIND == kGrad ? kBiasBytes : KIND == kWeight ? kTurnBytes : 0; }
+template <int KIND> constexpr int extra_bytes() { return KIND == kStats || KIND == kLogits ? kBiasBytes + kJoinBytes : KIND == kGrad ? kBiasBytes : KIND == kWeight ? kTurnBytes : 0; }
 template <int KIND> constexpr int smem_bytes() { return 1024 + kStages * kStageBytes + extra_bytes<KIND>(); }
 
 template <class T, int KIND, bool ENT>
@@ -382,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                         const int k = (kb * kSlices + q) * BK;
                         unsigned char *ta = to + q * kSliceBytes, *tb = ta + BM * BK * 2;
                         if (kColumnsA) tma_load_pair(ta, &map_a, m0, k, full), tma_load_pair(ta + 8192, &map_a, m0 + 64, k, full);
-                        else tma_load_pair(ta, &map_a, k, m0, full);
+                        else tma_load_pair(ta, &map_a, k, a.a_row0 + m0, full);
                         if (kColumnsB) tma_load_pair(tb, &map_b, n0, a.b_row0 + k, full), tma_load_pair(tb + 8192, &map_b, n0 + 64, a.b_row0 + k, full);
                         else tma_load_pair(tb, &map_b, k, a.b_row0 + n0, full);
                     }
@@ -465,8 +555,10 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 if (lane == 0) barrier_arrive_at(first_blocks(smem_addr(&ctl.acc_empty[acc])));
             };
             const uint32_t at = tmem + acc * kTile + group * kWarpColumns + (static_cast<uint32_t>(quarter * 32) << 16);
-            if (KIND == kStats) {
-                const Sums mine = carry_stats(a, at, m0 + lane, n0, bias, ready, release);
+            if (KIND == kStats || KIND == kLogits) {
+                Sums mine;
+                if constexpr (KIND == kLogits) mine = carry_logits<T>(a, at, m0 + lane, n0, bias, ready, release);
+                else mine = carry_stats(a, at, m0 + lane, n0, bias, ready, release);
                 // the four warps of these rows join their columns; two rooms, so that one barrier a tile is enough
                 float *room = reinterpret_cast<float *>(extra + kBiasBytes) + ((acc * 4 + quarter) * 4) * 96 + lane;
                 if (group > 0) room[group * 96] = mine.m, room[group * 96 + 32] = mine.s, room[group * 96 + 64] = mine.t;
@@ -511,7 +603,6 @@ struct RowArgs {
     float *logprob, *entropy, *lse;            // each may be NULL
     const float *grad_logprob, *grad_entropy;  // each may be NULL
     float *consts;                             // NULL without a gradient
-    uint32_t *scale_bits;                      // NULL unless half precision
 };
 
 // What carry_grad needs of a row, from the reference and base-2 logarithm of the sum relative to it.
@@ -519,16 +610,25 @@ __device__ __forceinline__ void write_consts(const RowArgs &a, int64_t r, int64_
 {
     float ga = a.grad_logprob && token >= 0 ? a.grad_logprob[r] / a.temperature : 0.f;
     float gb = a.grad_entropy ? a.grad_entropy[r] / a.temperature : 0.f;
-    if (token >= a.V && a.grad_logprob) ga = quiet_nan();
+    if ((token >= a.V && a.grad_logprob) || ls != ls) ga = quiet_nan();  // the whole row's, its kept logits tell nothing
     if (empty) ref = ls = entropy = 0.f, ga = gb = 0.f;  // nothing allowed: no gradient
     float4 *to = reinterpret_cast<float4 *>(a.consts) + 2 * r;
     const float ab = ga + (a.grad_entropy ? gb * entropy : 0.f);
     to[0] = make_float4(ref, ls, ga, ab);
     to[1] = make_float4(gb * kLn2, __int_as_float(token < 0 || token >= a.V ? -1 : static_cast<int>(token)), 0.f, 0.f);
-    if (a.scale_bits) {  // |d| <= |ga| + |gb| (p |log p| + p H), and p |log p| < 0.37
-        const float most = fabsf(ga) + fabsf(gb) * (0.37f + entropy);
-        if (most > 0.f) atomicMax(a.scale_bits, __float_as_uint(most));  // of whole numbers: the order does not matter
+}
+
+// The largest bound on a row's gradient by its logits: |d| <= |ga| + |gb| (p |log p| + p H), p |log p| < 0.37, H <= log V.
+__global__ void __launch_bounds__(256) scale_kernel(const RowArgs a, uint32_t *bits)
+{
+    float most = 0.f;
+    const float spread = 0.37f + logf(static_cast<float>(a.V));
+    for (int64_t r = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; r < a.R; r += static_cast<int64_t>(gridDim.x) * 256) {
+        const float ga = a.grad_logprob && token_at(a.tokens, a.index_bits, r) >= 0 ? fabsf(a.grad_logprob[r]) : 0.f, gb = a.grad_entropy ? fabsf(a.grad_entropy[r]) : 0.f;
+        const float bound = (ga + gb * spread) / a.temperature;
+        if (bound <= 3.4e38f) most = fmaxf(most, bound);
     }
+    if (most > 0.f) atomicMax(bits, __float_as_uint(most));  // of whole numbers: the order does not matter
 }
 
 // Joins the tiles of 32 rows, a row to a lane: each warp every 32nd tile, eight of them at a time (their loads in flight together, one
@@ -602,6 +702,52 @@ __global__ void __launch_bounds__(256) saved_rows_kernel(const RowArgs a)
     write_consts(a, r, a.tokens ? token_at(a.tokens, a.index_bits, r) : -1, lse * a.temperature, 0.f, a.in_entropy ? a.in_entropy[r] : 0.f, lse == neg_inf());
 }
 
+// ---------------------------------------------------------------------------------------------- gradient by kept logits
+// Codes into the gradient, in place: eight columns of kGradRows rows to a thread.  Memory bound: 2 bytes in, 2 out.
+constexpr int kGradRows = 8;
+template <class T, bool ENT>
+__global__ void __launch_bounds__(256) grad_kernel(uint16_t *codes, const float *tops, int64_t padded_rows, int64_t M, int64_t N, int64_t ld, const float *consts, float c,
+                                                   const uint32_t *scale_bits)
+{
+    __shared__ RowConsts rows[kGradRows];
+    const int64_t n = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+    for (int64_t m0 = static_cast<int64_t>(blockIdx.y) * kGradRows; m0 < M; m0 += static_cast<int64_t>(gridDim.y) * kGradRows) {
+        const int count = static_cast<int>(min(M - m0, static_cast<int64_t>(kGradRows)));
+        __syncthreads();
+        if (threadIdx.x < count) rows[threadIdx.x] = row_consts(consts, m0 + threadIdx.x, power_of_two(scale_power(scale_bits)));
+        __syncthreads();
+        if (n >= N) continue;
+        uint4 raw[kGradRows];
+        float top[kGradRows];
+#pragma unroll
+        for (int i = 0; i < kGradRows; ++i)
+            if (i < count) {  // ld is a multiple of 64: columns behind N are there, and nobody reads what becomes of them
+                raw[i] = load_last(codes + (m0 + i) * ld + n);
+                top[i] = tops[n / kWarpColumns * padded_rows + m0 + i];
+            }
+#pragma unroll
+        for (int i = 0; i < kGradRows; ++i) {
+            if (i >= count) break;
+            const RowConsts k = rows[i];
+            const float base = fmaf(top[i] - k.ref, c, -k.ls);
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float code = __uint_as_float(__byte_perm(w[j / 2], 0x4b000000u, j % 2 ? 0x7432 : 0x7410)) - 8388608.f;
+                const float y = code == static_cast<float>(kNothing) ? neg_inf() : fmaf(code, -1.f / kSteps<T>, base);
+                f[j] = grad_at<ENT>(y, k);
+            }
+            const int64_t at = k.token - n;
+            if (at >= 0 && at < 8)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (at == j) f[j] += k.hit;
+            *reinterpret_cast<uint4 *>(codes + (m0 + i) * ld + n) = Elem<T>::pack(f);
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------------------------- sums of parts
 // out[m][n] = sum over the splits of parts[split][m][n], in their order, times 2^-scale, rounded once; eight columns to a thread.
 // `wide`: every row of out starts on 16 bytes.  Index: 32 bits where they are enough (a division by a 64-bit number cost more than all the rest).
@@ -665,13 +811,17 @@ __global__ void __launch_bounds__(256) bias_kernel(const float *sums, int64_t gr
 int64_t div_up(int64_t x, int64_t y) { return (x + y - 1) / y; }
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// The gradient by the logits is kept for one piece of the vocabulary: as many ids as this much memory holds, 2048 at least.
+// By ids: the gradient by the logits is kept for as many ids at a time as this much memory holds, 2048 at least.
 constexpr int64_t kPieceBytes = 256ll << 20, kLeastPiece = 2048;
+// By rows: the logits, for as many rows as this much memory holds; not where that is few, since dweight's fp32 sums are read and
+// written for each.
+constexpr int64_t kLogitBytes = 512ll << 20, kLeastRows = 2048, kLeastWidth = 512;
 
 struct Layout {
-    size_t hidden, weight, partial, token_logit, consts, scale, piece, parts, sums, total;
-    int64_t padded_rows, width, ld_parts;  // width: ids of a piece
+    size_t hidden, weight, partial, token_logit, consts, scale, tops, piece, parts, weight_sums, sums, total;
+    int64_t padded_rows, rows, width, ld_piece, ld_parts;  // rows, width: what is worked on at a time
     int hidden_splits, weight_splits;
+    bool by_rows;
 };
 
 // How many parts the sum of a product of few tiles is split into, so that it fills the pairs of multiprocessors: the least estimated time in stages
@@ -689,7 +839,7 @@ int choose_splits(int64_t M, int64_t N, int64_t k_blocks)
     return best;
 }
 
-Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int64_t R, int64_t V, int64_t D, bool stats, bool grads)
+Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int64_t R, int64_t V, int64_t D, bool stats, bool grads, bool bias)
 {
     Layout l = {};
     size_t at = 0;
@@ -698,30 +848,39 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
         at += rounded(bytes);
         return here;
     };
-    l.padded_rows = div_up(R, 32) * 32;
+    l.rows = R, l.width = V;
     l.hidden = take(tma_ok(hidden, ldh) ? 0 : packed_bytes(R, D));
     l.weight = take(tma_ok(weight, ldw) ? 0 : packed_bytes(V, D));
+    if (grads) {
+        l.ld_piece = div_up(V, 64) * 64;
+        const int64_t most = kLogitBytes / 2 / l.ld_piece;  // rows
+        l.by_rows = stats && !bias && D >= kLeastWidth && (R <= most || most >= kLeastRows);
+        if (l.by_rows) {
+            const int64_t pieces = R <= most ? 1 : div_up(R, most / kTile * kTile);
+            if (pieces > 1) l.rows = div_up(div_up(R, pieces), kTile) * kTile;  // of one size
+        } else {
+            int64_t width = kPieceBytes / 2 / R / kTile * kTile;
+            if (width < kLeastPiece) width = kLeastPiece;
+            const int64_t pieces = div_up(V, width);
+            width = div_up(div_up(V, pieces), kTile) * kTile;
+            if (width < V) l.width = l.ld_piece = width;
+        }
+        const bool once = l.rows == R;
+        l.ld_parts = div_up(D, 8) * 8;
+        l.hidden_splits = choose_splits(l.rows, D, div_up(l.width, kStageK));
+        l.weight_splits = once ? choose_splits(l.width, D, div_up(l.rows, kStageK)) : 1;
+        l.consts = take(static_cast<size_t>(l.rows) * kConsts * 4);
+        l.scale = take(256);
+        if (l.by_rows) l.tops = take(static_cast<size_t>(l.ld_piece / kWarpColumns) * (div_up(l.rows, 32) * 32) * 4);
+        l.piece = take(static_cast<size_t>(l.rows) * l.ld_piece * 2);
+        l.parts = take(static_cast<size_t>(l.hidden_splits) * l.rows * l.ld_parts * 4);
+        if (!once || l.weight_splits > 1) l.weight_sums = take(static_cast<size_t>(l.weight_splits) * l.width * l.ld_parts * 4);
+        if (bias) l.sums = take(static_cast<size_t>(div_up(R, 32)) * l.ld_piece * 4);
+    }
+    l.padded_rows = div_up(l.rows, 32) * 32;
     if (stats) {
         l.partial = take(static_cast<size_t>(div_up(V, kTile)) * 3 * l.padded_rows * 4);
-        l.token_logit = take(static_cast<size_t>(R) * 4);
-    }
-    if (grads) {
-        int64_t width = kPieceBytes / 2 / R / kTile * kTile;
-        if (width < kLeastPiece) width = kLeastPiece;
-        const int64_t pieces = div_up(V, width);
-        width = div_up(div_up(V, pieces), kTile) * kTile;  // pieces of one size
-        l.width = width < V ? width : div_up(V, 64) * 64;
-        l.ld_parts = div_up(D, 8) * 8;
-        const int64_t ids = l.width < V ? l.width : V;
-        l.hidden_splits = choose_splits(R, D, div_up(ids, kStageK));
-        l.weight_splits = choose_splits(ids, D, div_up(R, kStageK));
-        l.consts = take(static_cast<size_t>(R) * kConsts * 4);
-        l.scale = take(256);
-        l.piece = take(static_cast<size_t>(R) * l.width * 2);
-        size_t parts = static_cast<size_t>(l.hidden_splits) * R * l.ld_parts * 4;
-        at = rounded(at);
-        l.parts = take(parts + (l.weight_splits > 1 ? static_cast<size_t>(l.weight_splits) * l.width * l.ld_parts * 4 : 0));
-        l.sums = take(static_cast<size_t>(l.padded_rows / 32) * l.width * 4);
+        l.token_logit = take(static_cast<size_t>(l.rows) * 4);
     }
     l.total = at;
     return l;
@@ -780,9 +939,91 @@ int group_of(int64_t K)
         if (rc__ != SPDY_OK) return rc__;  \
     } while (0)
 
+// The steps of a call on some rows (from r0) and ids (from v0).
+template <class T> struct Head {
+    const HeadArgs &h;
+    const Layout &l;
+    char *ws;
+    cudaStream_t s;
+    ProductArgs base;
+    CUtensorMap hidden, weight, hidden_columns, weight_columns;
+
+    float *floats(size_t at) const { return reinterpret_cast<float *>(ws + at); }
+
+    // Sums of rows' exponentials and what comes of them; KIND kLogits keeps the logits.
+    template <int KIND> int stats(RowArgs rows, int64_t r0)
+    {
+        ProductArgs a = base;
+        a.M = rows.R, a.N = h.V, a.a_row0 = static_cast<int>(r0);
+        a.tokens = rows.tokens;
+        a.partial = floats(l.partial), a.token_logit = rows.tokens ? floats(l.token_logit) : nullptr;
+        if (KIND == kLogits) a.out = ws + l.piece, a.ldo = l.ld_piece, a.tops = floats(l.tops);
+        HEAD_TRY((launch_product<T, KIND, true>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
+        rows.partial = a.partial, rows.token_logit = a.token_logit, rows.tiles = static_cast<int>(div_up(h.V, kTile));
+        rows_kernel<<<static_cast<unsigned>(div_up(rows.R, 32)), 32 * kRowWarps, 0, s>>>(rows);
+        return finish_launch();
+    }
+    // The gradient by the kept logits of m rows.
+    int gradient(int64_t m)
+    {
+        const int64_t down = div_up(m, kGradRows);
+        const dim3 grid(static_cast<unsigned>(div_up(h.V, 2048)), static_cast<unsigned>(down < 65535 ? down : 65535));
+        uint16_t *codes = reinterpret_cast<uint16_t *>(ws + l.piece);
+        if (h.grad_entropy) grad_kernel<T, true><<<grid, 256, 0, s>>>(codes, floats(l.tops), l.padded_rows, m, h.V, l.ld_piece, base.consts, base.c, base.scale_bits);
+        else grad_kernel<T, false><<<grid, 256, 0, s>>>(codes, floats(l.tops), l.padded_rows, m, h.V, l.ld_piece, base.consts, base.c, base.scale_bits);
+        return finish_launch();
+    }
+    // The gradient by the logits of all rows and ids v0 .. v0 + n - 1, which are multiplied again; dbias of these ids.
+    int gradient_again(int64_t n, int64_t v0)
+    {
+        ProductArgs a = base;
+        a.M = h.R, a.N = n, a.v0 = v0, a.b_row0 = static_cast<int>(v0);
+        a.out = ws + l.piece, a.ldo = l.ld_piece;
+        if (h.dbias) a.column_sums = floats(l.sums), a.ld_sums = l.ld_piece;
+        if (h.grad_entropy) HEAD_TRY((launch_product<T, kGrad, true>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
+        else HEAD_TRY((launch_product<T, kGrad, false>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
+        return h.dbias ? finish_bias(n, v0) : SPDY_OK;
+    }
+    int finish_bias(int64_t n, int64_t v0)
+    {
+        bias_kernel<<<static_cast<unsigned>(div_up(n, 32)), 256, 0, s>>>(floats(l.sums), div_up(h.R, 32), n, l.ld_piece, base.scale_bits, h.dbias + v0);
+        return finish_launch();
+    }
+    // dhidden's sums and dweight from the gradient of m rows (from r0) and n ids (from v0), added to what earlier rows or ids gave.
+    int products(int64_t m, int64_t r0, int64_t n, int64_t v0)
+    {
+        CUtensorMap piece;
+        if (h.dhidden) {
+            HEAD_TRY(map_of(&piece, ws + l.piece, l.ld_piece, m, n, h.dtype, BM));
+            ProductArgs b = {};
+            b.M = m, b.N = h.D, b.b_row0 = static_cast<int>(v0), b.out = floats(l.parts), b.ldo = l.ld_parts, b.add = v0 > 0;
+            HEAD_TRY((launch_product<T, kHidden, false>(piece, weight_columns, b, n, 8, l.hidden_splits, s)));
+        }
+        if (!h.dweight) return SPDY_OK;
+        HEAD_TRY(map_of(&piece, ws + l.piece, l.ld_piece, m, n, h.dtype, BK));
+        T *out = static_cast<T *>(h.dweight) + v0 * h.lddw;
+        ProductArgs b = {};
+        b.M = n, b.N = h.D, b.b_row0 = static_cast<int>(r0);
+        const bool last = r0 + m == h.R;
+        if (l.weight_splits > 1 || !last) {
+            b.out = floats(l.weight_sums), b.ldo = l.ld_parts, b.add = r0 > 0;
+            HEAD_TRY((launch_product<T, kWeightParts, false>(piece, hidden_columns, b, m, 8, l.weight_splits, s)));
+            return last ? finish<T>(floats(l.weight_sums), l.weight_splits, n, h.D, l.ld_parts, base.scale_bits, out, h.lddw, s) : SPDY_OK;
+        }
+        b.out = out, b.ldo = h.lddw, b.scale_bits = base.scale_bits;
+        b.width = aligned(out, 32) && h.lddw % 16 == 0 ? 32 : aligned(out, 16) && h.lddw % 8 == 0 ? 16 : 0;
+        if (r0 > 0) b.sums = floats(l.weight_sums), b.ld_old = l.ld_parts;
+        return launch_product<T, kWeight, false>(piece, hidden_columns, b, m, 8, 1, s);
+    }
+    int finish_hidden(int64_t m, int64_t r0)
+    {
+        return finish<T>(floats(l.parts), l.hidden_splits, m, h.D, l.ld_parts, base.scale_bits, static_cast<T *>(h.dhidden) + r0 * h.lddh, h.lddh, s);
+    }
+};
+
 template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
 {
-    const Layout l = lay_out(h.hidden, h.ldh, h.weight, h.ldw, h.R, h.V, h.D, h.stats, h.grads);
+    const Layout l = lay_out(h.hidden, h.ldh, h.weight, h.ldw, h.R, h.V, h.D, h.stats, h.grads, h.dbias != nullptr);
     char *ws = static_cast<char *>(workspace);
     const int64_t R = h.R, V = h.V, D = h.D;
     Repack p = {};
@@ -815,65 +1056,49 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
     if (h.grads) {
         rows.consts = reinterpret_cast<float *>(ws + l.consts);
         if (h.dtype == SPDY_F16) {
-            rows.scale_bits = reinterpret_cast<uint32_t *>(ws + l.scale);
-            SPDY_EVAL_TRY(cudaMemsetAsync(rows.scale_bits, 0, 4, s));
+            uint32_t *bits = reinterpret_cast<uint32_t *>(ws + l.scale);
+            SPDY_EVAL_TRY(cudaMemsetAsync(bits, 0, 4, s));
+            const int64_t blocks = div_up(R, 256), most = sm_count();
+            scale_kernel<<<static_cast<unsigned>(blocks < most ? blocks : most), 256, 0, s>>>(rows, bits);
+            HEAD_TRY(finish_launch());
+            base.scale_bits = bits;
         }
-        base.consts = rows.consts, base.scale_bits = rows.scale_bits;
+        base.consts = rows.consts;
     }
-    if (h.stats) {
-        ProductArgs a = base;
-        a.M = R, a.N = V;
-        a.partial = reinterpret_cast<float *>(ws + l.partial);
-        a.token_logit = h.tokens ? reinterpret_cast<float *>(ws + l.token_logit) : nullptr;
-        HEAD_TRY((launch_product<T, kStats, true>(hidden, weight, a, D, group_of(D), 1, s)));
-        rows.partial = a.partial, rows.token_logit = a.token_logit, rows.tiles = static_cast<int>(div_up(V, kTile));
-        rows_kernel<<<static_cast<unsigned>(div_up(R, 32)), 32 * kRowWarps, 0, s>>>(rows);
+    Head<T> g = {h, l, ws, s, base, hidden, weight, {}, {}};
+    if (h.grads) {
+        HEAD_TRY(map_of(&g.hidden_columns, h.hidden, h.ldh, R, D, h.dtype, BK));
+        HEAD_TRY(map_of(&g.weight_columns, h.weight, h.ldw, V, D, h.dtype, BK));
+    }
+    if (h.grads && l.by_rows) {
+        for (int64_t r0 = 0; r0 < R; r0 += l.rows) {
+            const int64_t n = R - r0 < l.rows ? R - r0 : l.rows;
+            RowArgs some = rows;
+            some.R = n;
+            const size_t token_bytes = static_cast<size_t>(h.index_bits / 8);
+            if (some.tokens) some.tokens = static_cast<const char *>(rows.tokens) + r0 * token_bytes;
+            for (float **p : {&some.logprob, &some.entropy, &some.lse}) *p = *p ? *p + r0 : nullptr;
+            for (const float **p : {&some.grad_logprob, &some.grad_entropy}) *p = *p ? *p + r0 : nullptr;
+            HEAD_TRY(g.template stats<kLogits>(some, r0));
+            HEAD_TRY(g.gradient(n));
+            HEAD_TRY(g.products(n, r0, V, 0));
+            if (h.dhidden) HEAD_TRY(g.finish_hidden(n, r0));
+        }
     } else {
-        saved_rows_kernel<<<static_cast<unsigned>(div_up(R, 256)), 256, 0, s>>>(rows);
-    }
-    HEAD_TRY(finish_launch());
-    if (!h.grads) return SPDY_OK;
-
-    CUtensorMap hidden_columns, weight_columns;
-    HEAD_TRY(map_of(&hidden_columns, h.hidden, h.ldh, R, D, h.dtype, BK));
-    HEAD_TRY(map_of(&weight_columns, h.weight, h.ldw, V, D, h.dtype, BK));
-    float *hidden_parts = reinterpret_cast<float *>(ws + l.parts), *weight_parts = hidden_parts + static_cast<size_t>(l.hidden_splits) * R * l.ld_parts;
-    for (int64_t v0 = 0; v0 < V; v0 += l.width) {
-        const int64_t n = V - v0 < l.width ? V - v0 : l.width;
-        ProductArgs a = base;
-        a.M = R, a.N = n, a.v0 = v0, a.b_row0 = static_cast<int>(v0);
-        a.out = ws + l.piece, a.ldo = l.width;
-        if (h.dbias) a.column_sums = reinterpret_cast<float *>(ws + l.sums), a.ld_sums = l.width;
-        if (h.grad_entropy) HEAD_TRY((launch_product<T, kGrad, true>(hidden, weight, a, D, group_of(D), 1, s)));
-        else HEAD_TRY((launch_product<T, kGrad, false>(hidden, weight, a, D, group_of(D), 1, s)));
-        if (h.dbias) {
-            bias_kernel<<<static_cast<unsigned>(div_up(n, 32)), 256, 0, s>>>(a.column_sums, div_up(R, 32), n, l.width, base.scale_bits, h.dbias + v0);
+        if (h.stats) {
+            HEAD_TRY(g.template stats<kStats>(rows, 0));
+        } else {
+            saved_rows_kernel<<<static_cast<unsigned>(div_up(R, 256)), 256, 0, s>>>(rows);
             HEAD_TRY(finish_launch());
         }
-        CUtensorMap piece, piece_columns;
-        if (h.dhidden) {
-            HEAD_TRY(map_of(&piece, ws + l.piece, l.width, R, n, h.dtype, BM));
-            ProductArgs b = {};
-            b.M = R, b.N = D, b.b_row0 = static_cast<int>(v0), b.out = hidden_parts, b.ldo = l.ld_parts, b.add = v0 > 0;
-            HEAD_TRY((launch_product<T, kHidden, false>(piece, weight_columns, b, n, 8, l.hidden_splits, s)));
+        if (!h.grads) return SPDY_OK;
+        for (int64_t v0 = 0; v0 < V; v0 += l.width) {
+            const int64_t n = V - v0 < l.width ? V - v0 : l.width;
+            HEAD_TRY(g.gradient_again(n, v0));
+            HEAD_TRY(g.products(R, 0, n, v0));
         }
-        if (h.dweight) {
-            HEAD_TRY(map_of(&piece_columns, ws + l.piece, l.width, R, n, h.dtype, BK));
-            ProductArgs b = {};
-            b.M = n, b.N = D;
-            T *out = static_cast<T *>(h.dweight) + v0 * h.lddw;
-            if (l.weight_splits == 1) {
-                b.out = out, b.ldo = h.lddw, b.scale_bits = base.scale_bits;
-                b.width = aligned(out, 32) && h.lddw % 16 == 0 ? 32 : aligned(out, 16) && h.lddw % 8 == 0 ? 16 : 0;
-                HEAD_TRY((launch_product<T, kWeight, false>(piece_columns, hidden_columns, b, R, 8, 1, s)));
-            } else {
-                b.out = weight_parts, b.ldo = l.ld_parts;
-                HEAD_TRY((launch_product<T, kWeightParts, false>(piece_columns, hidden_columns, b, R, 8, l.weight_splits, s)));
-                HEAD_TRY(finish<T>(weight_parts, l.weight_splits, n, D, l.ld_parts, base.scale_bits, out, h.lddw, s));
-            }
-        }
+        if (h.dhidden) HEAD_TRY(g.finish_hidden(R, 0));
     }
-    if (h.dhidden) HEAD_TRY(finish<T>(hidden_parts, l.hidden_splits, R, D, l.ld_parts, base.scale_bits, static_cast<T *>(h.dhidden), h.lddh, s));
     return SPDY_OK;
 }
 
@@ -919,7 +1144,7 @@ int run(const HeadArgs &h, void *workspace, size_t workspace_bytes, void *cuda_s
         return SPDY_OK;
     }
     if (!workspace || !aligned(workspace, 256)) return SPDY_ERR_INVALID_ARG;
-    if (workspace_bytes < lay_out(h.hidden, h.ldh, h.weight, h.ldw, h.R, h.V, h.D, h.stats, h.grads).total) return SPDY_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < lay_out(h.hidden, h.ldh, h.weight, h.ldw, h.R, h.V, h.D, h.stats, h.grads, h.dbias != nullptr).total) return SPDY_ERR_WORKSPACE_TOO_SMALL;
     return h.dtype == SPDY_BF16 ? run_head<__nv_bfloat16>(h, workspace, s) : run_head<__half>(h, workspace, s);
 }
 
@@ -940,7 +1165,7 @@ size_t spdy_linear_token_logprobs_workspace_bytes(const void *hidden, int64_t ld
                                                   int gradients)
 {
     if (!half_type(dtype) || R <= 0 || V <= 0 || D <= 0 || R > kMost || V > kMost || D > kMost) return 0;
-    return lay_out(hidden, ldh, weight, ldw, R, V, D, forward != 0, gradients != 0).total;
+    return lay_out(hidden, ldh, weight, ldw, R, V, D, forward != 0, gradients != 0, gradients == 2).total;
 }
 
 int spdy_linear_token_logprobs(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int dtype, const void *bias, int bias_dtype, const void *tokens, int index_bits,

@@ -500,7 +500,7 @@ def linear_token_logprobs_backward(hidden, weight, tokens, lse, entropy=None, gr
     vectors = _optional(R, dev, lse=lse, entropy=entropy, grad_logprob=grad_logprob, grad_entropy=grad_entropy)
     with _Scope(dev, stream) as handle:
         grads, outs = _head_grads(hidden, weight, bias, R, V, D, dev, wanted, dhidden, dweight)
-        pws, need, ws = _head_workspace(lib, query, R, V, D, 0, 1)
+        pws, need, ws = _head_workspace(lib, query, R, V, D, 0, 1 if grads.dbias is None else 2)
         rc = lib.spdy_linear_token_logprobs_backward(*head, *vectors, *outs, pws, need, handle)
     if rc:
         binding._check(rc, "spdy_linear_token_logprobs_backward")
@@ -517,7 +517,7 @@ def linear_token_logprobs_with_grad(hidden, weight, tokens, grad_logprob=None, g
     with _Scope(dev, stream) as handle:
         logprob, entropy, lse = _vectors(3, R)
         grads, outs = _head_grads(hidden, weight, bias, R, V, D, dev, wanted, dhidden, dweight)
-        pws, need, ws = _head_workspace(lib, query, R, V, D, 1, 1)
+        pws, need, ws = _head_workspace(lib, query, R, V, D, 1, 1 if grads.dbias is None else 2)
         rc = lib.spdy_linear_token_logprobs_with_grad(*head, *vectors, logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), *outs, pws,
                                                       need, handle)
     if rc:

@@ -42,16 +42,26 @@ def check(h, w, b, tokens, temperature, gl, gh, on="cpu"):
     alone = evaluate.linear_token_logprobs(h, w, tokens, b, temperature)
     out, grads = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, temperature)
     again = evaluate.linear_token_logprobs_backward(h, w, tokens, out.lse, out.entropy, gl, gh, b, temperature)
+    # without dbias (and from a width of 512 on) the logits are kept in 16 bits
+    other, kept = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, temperature, wanted=("hidden", "weight"))
     for name in ("logprob", "entropy", "lse"):
         tune.close(getattr(out, name), want, name)
-        assert torch.equal(getattr(alone, name).nan_to_num(5.0), getattr(out, name).nan_to_num(5.0)), name
-    for g in (grads, again):
-        tune.close(g.dhidden, want, "dhidden")
-        tune.close(g.dweight, want, "dweight")
-        if b is not None:
+        tune.close(getattr(other, name), want, name)
+        assert torch.equal(getattr(alone, name).nan_to_num(5.0), getattr(out, name).nan_to_num(5.0)) or (b is None and w.shape[1] >= 512), name
+    if b is not None:
+        for g in (grads, again):
+            tune.close(g.dhidden, want, "dhidden")
+            tune.close(g.dweight, want, "dweight")
             tune.close(g.dbias, want, "dbias")
-        else:
-            assert g.dbias is None
+        assert kept.dbias is None
+    else:
+        tune.close(again.dhidden, want, "dhidden")
+        tune.close(again.dweight, want, "dweight")
+        assert torch.equal(kept.dhidden, grads.dhidden) and torch.equal(kept.dweight, grads.dweight) and grads.dbias is None
+    if w.shape[1] >= 512:
+        want = tune.head(h, w, b, tokens, temperature, gl, gh, on, kept=True)
+    tune.close(kept.dhidden, want, "dhidden")
+    tune.close(kept.dweight, want, "dweight")
     evaluate.linear_check_status()
 
 
@@ -79,10 +89,28 @@ def test_against_the_formula(R, V, D, dtype, bias, temperature, entropy, padh, p
     (9000, 33000, 72, F16),       # pieces that the budget sets, the last one shorter
     (300, 20000, 520, BF16),      # the summed index of dhidden shared among multiprocessors
     (20000, 300, 40, F16),        # that of dweight
+    (9000, 40000, 512, BF16),     # two pieces of rows
+    (9001, 70001, 520, F16),      # three, odd ends
+    (700, 5003, 600, F16),        # all rows at once
+    (5, 3000, 640, BF16),
 ])
-def test_pieces_and_shares(R, V, D, dtype):
+@pytest.mark.parametrize("entropy", [False, True])
+def test_pieces_and_shares(R, V, D, dtype, entropy):
     h, w, tokens, b = head(R, V, D, dtype, F32)
-    check(h, w, b, tokens, 1.0, *weights(R, dtype, False), on="cuda")
+    check(h, w, b, tokens, 1.0, *weights(R, dtype, entropy), on="cuda")
+
+
+@gpu
+def test_rows_that_are_not_finite_in_one_of_several_pieces():
+    R, V, D = 9000, 40000, 512  # two pieces of rows
+    h, w, tokens, b = head(R, V, D, BF16)
+    gl, _ = weights(R, BF16, False)
+    clean = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl)
+    h[8000, 5] = math.nan
+    out, grads = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl)
+    rest = torch.arange(R, device="cuda") != 8000
+    assert torch.equal(out.lse[rest], clean[0].lse[rest]) and torch.equal(grads.dhidden[rest], clean[1].dhidden[rest])
+    assert torch.isnan(out.lse[8000]) and torch.isnan(grads.dhidden[8000]).all()
 
 
 @gpu
@@ -103,14 +131,15 @@ def test_tokens_that_are_none_or_beyond(bits):
 @gpu
 @pytest.mark.parametrize("entropy", [False, True])
 @pytest.mark.parametrize("low", [-INF, -1e9, -1e30, float(torch.finfo(F32).min)])
-def test_ids_that_are_not_allowed(low, entropy):
-    h, w, tokens, b = head(100, 777, 96, BF16, F32)
+@pytest.mark.parametrize("D,dtype", [(96, BF16), (512, BF16), (520, F16)])
+def test_ids_that_are_not_allowed(low, entropy, D, dtype):
+    h, w, tokens, b = head(100, 777, D, dtype, F32)
     allowed = torch.rand(777, generator=torch.Generator().manual_seed(3)) < 0.3
     allowed[256:512] = False  # a tile without any
     b = torch.where(allowed.cuda(), b, torch.full_like(b, low))
     ids = allowed.nonzero()[:, 0].cuda()
     tokens = torch.where(tokens >= 0, ids[tokens.clamp(min=0) % ids.numel()], tokens)
-    gl, gh = weights(100, BF16, entropy)
+    gl, gh = weights(100, dtype, entropy)
     check(h, w, torch.where(allowed.cuda(), b, torch.full_like(b, -INF)) if low < -1e8 else b, tokens, 1.0, gl, gh)
     got, grads = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b)
     want = tune.head(h, w, torch.where(allowed.cuda(), b, torch.full_like(b, -INF)), tokens, 1.0, gl, gh)
@@ -118,20 +147,25 @@ def test_ids_that_are_not_allowed(low, entropy):
         tune.close(getattr(got, name), want, name)
     for name in ("dhidden", "dweight", "dbias"):
         tune.close(getattr(grads, name), want, name)
-    assert (grads.dweight[~allowed.cuda()] == 0).all() and (grads.dbias[~allowed.cuda()] == 0).all()
+    kept = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, wanted=("hidden", "weight"))[1]
+    for g in (grads, kept):
+        assert (g.dweight[~allowed.cuda()] == 0).all()
+    assert (grads.dbias[~allowed.cuda()] == 0).all()
 
 
 @gpu
-def test_rows_with_nothing_left():
-    h, w, tokens, _ = head(40, 300, 64, F16)
+@pytest.mark.parametrize("D", [64, 512])
+def test_rows_with_nothing_left(D):
+    h, w, tokens, _ = head(40, 300, D, F16)
     b = torch.full((300,), -INF, device="cuda")
     gl, gh = weights(40, F16, True)
     out, grads = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b)
     again = evaluate.linear_token_logprobs_backward(h, w, tokens, out.lse, out.entropy, gl, gh, b)
     assert (out.lse == -INF).all() and (out.entropy == 0).all()
     assert (out.logprob[tokens >= 0] == -INF).all() and (out.logprob[tokens < 0] == 0).all()
-    for g in (grads, again):
-        assert (g.dhidden == 0).all() and (g.dweight == 0).all() and (g.dbias == 0).all()
+    kept = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, wanted=("hidden", "weight"))[1]
+    for g in (grads, again, kept):
+        assert (g.dhidden == 0).all() and (g.dweight == 0).all() and (g.dbias is None or (g.dbias == 0).all())
 
 
 @gpu
@@ -146,8 +180,9 @@ def test_all_ids_under_a_finite_mask():
 
 
 @gpu
-def test_values_that_are_not_finite_stay_in_their_rows():
-    h, w, tokens, b = head(70, 600, 64, BF16)
+@pytest.mark.parametrize("D", [64, 512])
+def test_values_that_are_not_finite_stay_in_their_rows(D):
+    h, w, tokens, b = head(70, 600, D, BF16)
     gl, gh = weights(70, BF16, True)
     clean = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh)
     h[5, 3], h[40, 0] = math.nan, INF
@@ -167,7 +202,7 @@ def test_values_that_are_not_finite_stay_in_their_rows():
 
 
 @gpu
-@pytest.mark.parametrize("D", [64, 72, 100])
+@pytest.mark.parametrize("D", [64, 72, 100, 520])
 def test_outputs_with_strides_leave_their_neighbours(D):
     R, V = 130, 520
     h, w, tokens, b = head(R, V, D, BF16, F32)
@@ -185,7 +220,12 @@ def test_outputs_with_strides_leave_their_neighbours(D):
         some = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, wanted=wanted)[1]
         for name in ("hidden", "weight", "bias"):
             a, c = getattr(some, "d" + name), getattr(want, "d" + name)
-            assert (a is None) if name not in wanted else torch.equal(a, c)
+            assert (a is None) if name not in wanted else torch.equal(a, c) or (D >= 512 and "bias" not in wanted)
+    for out in ({}, {"dhidden": dh, "dweight": dw}):
+        kept = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, wanted=("hidden", "weight"), **out)[1]
+        want = tune.head(h, w, b, tokens, 1.0, gl, gh, kept=D >= 512)
+        tune.close(kept.dhidden, want, "dhidden")
+        tune.close(kept.dweight, want, "dweight")
 
 
 @gpu
@@ -198,14 +238,15 @@ def test_no_rows():
 
 
 @gpu
-def test_the_same_call_gives_the_same_bits_on_any_stream_and_in_a_graph():
-    h, w, tokens, b = head(600, 9000, 128, BF16, F32)
-    gl, gh = weights(600, BF16, True)
+@pytest.mark.parametrize("D,wanted,dtype", [(128, ("hidden", "weight", "bias"), BF16), (512, ("hidden", "weight"), BF16), (520, ("weight", "hidden"), F16)])
+def test_the_same_call_gives_the_same_bits_on_any_stream_and_in_a_graph(D, wanted, dtype):
+    h, w, tokens, b = head(600, 9000, D, dtype, F32)
+    gl, gh = weights(600, dtype, True)
 
     def call(stream=None):
-        out, grads = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, stream=stream)
-        more = evaluate.linear_token_logprobs_backward(h, w, tokens, out.lse, out.entropy, gl, gh, b, stream=stream)
-        return [out.logprob, out.entropy, out.lse, *grads, *more]
+        out, grads = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, wanted=wanted, stream=stream)
+        more = evaluate.linear_token_logprobs_backward(h, w, tokens, out.lse, out.entropy, gl, gh, b, wanted=wanted, stream=stream)
+        return [t for t in (out.logprob, out.entropy, out.lse, *grads, *more) if t is not None]
 
     want = call()
     torch.cuda.synchronize()
@@ -343,6 +384,10 @@ def test_workspace_stays_bounded():
     assert need(0, 100, 64, 1, 1) == 0 and need(10, 0, 64, 1, 1) == 0
     assert need(8192, 131072, 4096, 1, 0) < 80 << 20                    # forward: 12 bytes per row and tile of 256 ids
     assert need(8192, 131072, 4096, 0, 1) < (256 + 200) << 20           # a piece of 256 MB and dhidden's fp32 sums
+    assert need(8192, 65536, 4096, 1, 1) < (512 + 1024 + 200) << 20     # some rows' logits and gradient, fp32 sums of dweight
+    assert need(4096, 65536, 4096, 1, 1) < (512 + 250) << 20            # all rows at once
+    assert need(8192, 65536, 4096, 1, 2) < (256 + 250) << 20            # with dbias: by pieces of the vocabulary
+    assert need(8192, 200000, 4096, 1, 1) < (256 + 200 + 80) << 20      # fewer than 2048 rows would fit: the same
     assert need(1 << 20, 131072, 64, 0, 1) < (4096 + 700) << 20         # 2048 ids at least
     assert need(64, 5000, 100, 1, 0, ld=101) >= need(64, 5000, 104, 1, 0) + 5000 * 100 * 2  # copies of rows that TMA cannot read
 

@@ -9,8 +9,9 @@ import eval_reference as ref
 F16 = torch.float16
 
 
-def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu"):
-    """A dict of values and, under the same name with ``_err``, of bounds on the fp32 error before the last rounding."""
+def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu", kept=False):
+    """A dict of values and, under the same name with ``_err``, of bounds on the fp32 error before the last rounding.
+    ``kept``: the gradient comes from logits kept in 16 bits, as a call keeps them that gives values and gradients but no dbias."""
     h, w = (t.detach().to(on).double() for t in (hidden, weight))
     R, D = h.shape
     V = w.shape[0]
@@ -55,7 +56,13 @@ def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu"):
     off = 3 * ez + adds + 2.0 ** -22 * (lse.abs().nan_to_num(0.0, posinf=0.0, neginf=0.0) + 4)
     share = p * (a.abs()[:, None] + b.abs()[:, None] * (logs.abs() + entropy[:, None] + 1)) / temperature
     eg = share * (off[:, None] + 2.0 ** -21 * logs.abs()) + 2.0 ** -23 * g.abs()
-    most = float(((a.abs() + b.abs() * (0.37 + entropy)) / temperature).nan_to_num(0.0).max()) if R else 0.0
+    if kept:  # log2 p in steps of 2^-10 (half precision 2^-11), off by half a step; 64 (32) octaves below a neighbour p counts as 0
+        steps, octaves = (2.0 ** -11, 32) if hidden.dtype == F16 else (2.0 ** -10, 64)
+        eg = eg + share * (steps / 2 * math.log(2) * 1.001)
+        eg = eg + 2.0 ** -octaves * (a.abs() + b.abs() * (octaves + entropy)).nan_to_num(0.0)[:, None] / temperature
+    # Half precision: a power of two brings the largest bound on a row's gradient, |a| + |b| (0.37 + log V), to 2^13 .. 2^14, where numbers below the
+    # normal ones are rounded by 2^-25: 2^-38 of that bound.
+    most = float(((a.abs() + b.abs() * (0.37 + math.log(V))) / temperature).nan_to_num(0.0).max()) if R else 0.0
     rounded = eg + ref.HALF_ULP[hidden.dtype] * 1.01 * (g.abs() + eg) + (2.0 ** -38 * most if hidden.dtype == F16 else 2.0 ** -134)
     out["dhidden"], out["dweight"], out["dbias"] = g @ w, g.T @ h, g.sum(0)
     out["dhidden_err"] = rounded @ w.abs() + (V / 8 + 16 + V / 1024) * 2.0 ** -23 * (g.abs() @ w.abs())
