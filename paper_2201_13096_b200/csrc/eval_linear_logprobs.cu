@@ -6,7 +6,7 @@
 // is multiplied.  What is done with a tile differs:
 //   kStats   logits of 256 rows and ids -> per row the largest, the sum of exponentials relative to it, and the sum that the
 //            entropy needs; the given token's logit.  A second kernel joins a row's tiles in their order.
-//   kLogits  the same, and the logits are kept, in 16 bits as logarithms relative to the largest of 64, for a kernel that turns them into the
+//   kLogits  the same, and the logits are kept, in 16 bits as logarithms relative to the largest of 32, for a kernel that turns them into the
 //            gradient by them in place
 //   kGrad    the logits once more -> the gradient by them, rounded to 16 bits
 //   kHidden  gradient x weight: fp32 sums of dhidden
@@ -59,7 +59,7 @@ struct ProductArgs {
     const uint32_t *scale_bits;    // NULL, or the largest gradient's bits (half precision)
     float *column_sums;            // NULL, or [row groups of 32][N]
     int64_t ld_sums;
-    float *tops;                   // kLogits: [ids / 64][padded_rows], what a row's 64 codes are relative to
+    float *tops;                   // kLogits: [ids / 32][padded_rows], what a row's 32 codes are relative to
     void *out;                     // kLogits: codes; kGrad: the piece; kWeight: 16 bits; parts: fp32 [splits][M][ldo]
     int64_t ldo;
     const float *sums;             // kWeight: NULL, or fp32 [M][ld_old] to add
@@ -132,6 +132,24 @@ struct Control {
     uint32_t tmem;
 };
 
+// Adds 32 logits, of which `top` is at least the largest, to the sums, which become relative to it.  `each` gets (x - top) c by pairs.
+template <class Each> __device__ __forceinline__ void add_exponentials(const float *f, float top, float c, Sums &sums, Each each)
+{
+    raise(sums, top, c);
+    const float2 from = both(top == neg_inf() ? 0.f : -top), cc = both(c);  // first the difference, so that logits of any size keep their digits
+    float2 s = both(0.f), t = both(0.f);
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+        float2 d = mul2(add2(make_float2(f[i], f[i + 1]), from), cc);
+        d = make_float2(max_nan(d.x, -200.f), max_nan(d.y, -200.f));  // below, the exponential is 0
+        const float2 e = make_float2(ex2(d.x), ex2(d.y));
+        s = add2(s, e);
+        t = fma2(e, d, t);
+        each(i, d);
+    }
+    sums.s += s.x + s.y, sums.t += t.x + t.y;
+}
+
 // ---------------------------------------------------------------------------------------------- what is done with a tile
 // Each function carries 64 columns of a warp's 32 rows, a row to a lane.  `ready` waits for the accumulator and says whether it came
 // (if not, what is written is NaN); `release` is called once the last columns have left TMEM.
@@ -144,21 +162,39 @@ __device__ __forceinline__ void stage_bias(const ProductArgs &a, int64_t n0, flo
     for (int i = lane; i < kWarpColumns; i += 32) bias[i] = a.bias && n0 + i < a.N ? value_at(a.bias, a.bias_type, a.v0 + n0 + i) : 0.f;
     __syncwarp();
 }
-// 16 logits of a row; ids beyond the vocabulary are -inf.
+// 32 logits of a row; ids beyond the vocabulary are -inf.
 __device__ __forceinline__ void load_logits(const ProductArgs &a, uint32_t tmem, int64_t n, const float *bias, float *f)
 {
-    tmem_load16(tmem, f);
+    tmem_load32(tmem, f);
     if (a.bias) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
             const float4 b = reinterpret_cast<const float4 *>(bias)[i];
-            f[4 * i] += b.x, f[4 * i + 1] += b.y, f[4 * i + 2] += b.z, f[4 * i + 3] += b.w;
+            const float2 lo = add2(make_float2(f[4 * i], f[4 * i + 1]), make_float2(b.x, b.y)), hi = add2(make_float2(f[4 * i + 2], f[4 * i + 3]), make_float2(b.z, b.w));
+            f[4 * i] = lo.x, f[4 * i + 1] = lo.y, f[4 * i + 2] = hi.x, f[4 * i + 3] = hi.y;
         }
     }
-    if (n + 16 > a.N)
+    if (n + 32 > a.N)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
+        for (int i = 0; i < 32; ++i)
             if (n + i >= a.N) f[i] = neg_inf();
+}
+// f[at], for a row in which it is one of the 32.
+__device__ __forceinline__ float pick(const float *f, int64_t at)
+{
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x = at == i ? f[i] : x;
+    return x;
+}
+__device__ __forceinline__ float largest(const float *f, float top)
+{
+    float other = f[0];
+#pragma unroll
+    for (int i = 2; i < 32; i += 2) other = fmaxf(other, f[i]);
+#pragma unroll
+    for (int i = 1; i < 32; i += 2) top = fmaxf(top, f[i]);
+    return fmaxf(top, other);
 }
 
 template <class Ready, class Release>
@@ -173,39 +209,25 @@ __device__ __forceinline__ Sums carry_stats(const ProductArgs &a, uint32_t tmem,
     }
     Sums sums = {neg_inf(), 0.f, 0.f};
 #pragma unroll 1
-    for (int c = 0; c < kWarpColumns; c += 16) {
-        float f[16];
+    for (int c = 0; c < kWarpColumns; c += 32) {
+        float f[32];
         load_logits(a, tmem + c, n0 + c, bias + c, f);
-        if (c + 16 == kWarpColumns) release();
-        float top = sums.m;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, f[i]);
-        raise(sums, top, a.c);
-        const float ref = top == neg_inf() ? 0.f : top;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float d = (f[i] - ref) * a.c, e = ex2(d);
-            sums.s += e;
-            sums.t = fmaf(e, max_nan(d, -200.f), sums.t);  // below -200 e is 0
-        }
+        if (c + 32 == kWarpColumns) release();
         const int64_t at = token - (n0 + c);
-        if (at >= 0 && at < 16 && token < a.N) {
-            float x = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x = at == i ? f[i] : x;
-            a.token_logit[m] = x;
-        }
+        if (at >= 0 && at < 32 && token < a.N) a.token_logit[m] = pick(f, at);
+        add_exponentials(f, largest(f, sums.m), a.c, sums, [](int, float2) {});
     }
     return sums;
 }
 
-// A kept logit: how far log2 of its exponential lies below that of the largest among the row's 64 ids of a warp, in steps of 2^-10
+// A kept logit: how far log2 of its exponential lies below that of the largest among 32 ids, in steps of 2^-10
 // octaves over 64 octaves for bf16, 2^-11 over 32 for half precision, whose own numbers end sooner.  p comes out within 2^-11 ln 2 =
 // 3.4e-4 of itself (1.7e-4), beside the 16-bit rounding that follows of 3.9e-3 (4.9e-4).  The last code is "nothing".
 template <class T> constexpr float kSteps = std::is_same<T, __nv_bfloat16>::value ? 1024.f : 2048.f;
 constexpr uint32_t kNothing = 65535;
 
-// As carry_stats, with the codes.  The accumulator is read twice: the codes need the largest first.
+// As carry_stats, with the codes, and per 32 of them the largest, which they are relative to.
+constexpr int kCodes = 32;
 template <class T, class Ready, class Release>
 __device__ __forceinline__ Sums carry_logits(const ProductArgs &a, uint32_t tmem, int64_t m, int64_t n0, float *bias, Ready ready, Release release)
 {
@@ -217,44 +239,29 @@ __device__ __forceinline__ Sums carry_logits(const ProductArgs &a, uint32_t tmem
         return {0.f, quiet_nan(), quiet_nan()};  // the row's sum is NaN, and with it all that comes of its codes
     }
     Sums sums = {neg_inf(), 0.f, 0.f};
-#pragma unroll 1
-    for (int c = 0; c < kWarpColumns; c += 16) {
-        float f[16];
-        load_logits(a, tmem + c, n0 + c, bias + c, f);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sums.m = fmaxf(sums.m, f[i]);
-    }
-    const bool inside = m < a.M && n0 < a.N;
-    if (inside) a.tops[n0 / kWarpColumns * a.padded_rows + m] = sums.m;
-    const float ref = sums.m == neg_inf() ? 0.f : sums.m;
     uint16_t *to = static_cast<uint16_t *>(a.out) + m * a.ldo + n0;
 #pragma unroll 1
-    for (int c = 0; c < kWarpColumns; c += 16) {
-        float f[16];
+    for (int c = 0; c < kWarpColumns; c += kCodes) {
+        float f[kCodes];
         load_logits(a, tmem + c, n0 + c, bias + c, f);
-        if (c + 16 == kWarpColumns) release();
+        if (c + kCodes == kWarpColumns) release();
         const int64_t at = token - (n0 + c);
-        if (at >= 0 && at < 16 && token < a.N) {
-            float x = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x = at == i ? f[i] : x;
-            a.token_logit[m] = x;
+        if (at >= 0 && at < kCodes && token < a.N) a.token_logit[m] = pick(f, at);
+        const float top = largest(f, neg_inf());
+        Sums here = {neg_inf(), 0.f, 0.f};
+        uint32_t w[kCodes / 2];
+        add_exponentials(f, top, a.c, here, [&](int i, float2 d) {
+            // 2^23 and a number below 2^16: rounded to a whole number, in the lower half of the pattern
+            constexpr float lowest = -static_cast<float>(kNothing) / kSteps<T>;
+            const float2 code = fma2(make_float2(fmaxf(d.x, lowest), fmaxf(d.y, lowest)), both(-kSteps<T>), both(8388608.f));
+            w[i / 2] = __byte_perm(__float_as_uint(code.x), __float_as_uint(code.y), 0x5410);
+        });
+        if (m < a.M && n0 + c < a.N) {  // ldo is a multiple of 64
+            a.tops[(n0 + c) / kCodes * a.padded_rows + m] = top;
+            store32(to + c, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
+            store32(to + c + 16, make_uint4(w[8], w[9], w[10], w[11]), make_uint4(w[12], w[13], w[14], w[15]));
         }
-        uint32_t w[8];
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-            uint32_t code[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float d = max_nan((f[i + k] - ref) * a.c, -200.f), e = ex2(d);  // below -200 e is 0
-                sums.s += e;
-                sums.t = fmaf(e, d, sums.t);
-                // 2^23 and a number below 2^16: rounded to a whole number, in the lower half of the pattern
-                code[k] = __float_as_uint(fmaf(fmaxf(d, -static_cast<float>(kNothing) / kSteps<T>), -kSteps<T>, 8388608.f));
-            }
-            w[i / 2] = __byte_perm(code[0], code[1], 0x5410);
-        }
-        if (inside && n0 + c < a.N) store32(to + c, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));  // ldo is a multiple of 64
+        join(sums, here, a.c);
     }
     return sums;
 }
@@ -295,7 +302,6 @@ template <bool ENT> __device__ __forceinline__ float grad_at(float y, const RowC
     y = min_nan(y, 0.f);
     return ENT ? -ex2(y) * fmaf(k.slope, max_nan(y, -200.f), k.all) : -ex2(y) * k.all;
 }
-template <bool ENT> __device__ __forceinline__ float grad_of(float x, const RowConsts &k, float c) { return grad_at<ENT>(fmaf(x - k.ref, c, -k.ls), k); }
 
 // Gradient by 64 logits of a row, rounded to 16 bits once.
 template <class T, bool ENT, class Ready, class Release>
@@ -310,26 +316,37 @@ __device__ __forceinline__ void carry_grad(const ProductArgs &a, uint32_t tmem, 
     const bool ok = ready();
     char *to = static_cast<char *>(a.out) + (m * a.ldo + n0) * 2;
 #pragma unroll 1
-    for (int c = 0; c < kWarpColumns; c += 16) {
-        float f[16];
+    for (int c = 0; c < kWarpColumns; c += 32) {
+        float f[32];
         load_logits(a, tmem + c, n0 + c, bias + c, f);
-        if (c + 16 == kWarpColumns) release();
+        if (c + 32 == kWarpColumns) release();
         if (n0 + c >= a.N) continue;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) f[i] = ok ? grad_of<ENT>(f[i], k, a.c) : quiet_nan();
+        for (int i = 0; i < 32; i += 2) {
+            const float2 y = fma2(add2(make_float2(f[i], f[i + 1]), both(-k.ref)), both(a.c), both(-k.ls));
+            f[i] = grad_at<ENT>(y.x, k), f[i + 1] = grad_at<ENT>(y.y, k);
+        }
         const int64_t at = k.token - (a.v0 + n0 + c);
-        if (at >= 0 && at < 16)
+        if (at >= 0 && at < 32)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < 32; ++i)
                 if (at == i) f[i] += k.hit;
-        if (inside) store32(to + 2 * c, Elem<T>::pack(f), Elem<T>::pack(f + 8));
+        if (!ok)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) f[i] = quiet_nan();
+        if (inside)  // ldo is a multiple of 64
+#pragma unroll
+            for (int i = 0; i < 32; i += 16) store32(to + 2 * (c + i), Elem<T>::pack(f + i), Elem<T>::pack(f + i + 8));
         if (a.column_sums) {
             if (!inside)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) f[i] = 0.f;
-            const float sum = sum_columns(f);
-            const int64_t n = n0 + c + (lane >> 1);
-            if (!(lane & 1) && n < a.N && m0 < a.M) a.column_sums[m0 / 32 * a.ld_sums + n] = sum;
+                for (int i = 0; i < 32; ++i) f[i] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; i += 16) {
+                const float sum = sum_columns(f + i);
+                const int64_t n = n0 + c + i + (lane >> 1);
+                if (!(lane & 1) && n < a.N && m0 < a.M) a.column_sums[m0 / 32 * a.ld_sums + n] = sum;
+            }
         }
     }
 }
@@ -723,7 +740,7 @@ __global__ void __launch_bounds__(256) grad_kernel(uint16_t *codes, const float 
         for (int i = 0; i < kGradRows; ++i)
             if (i < count) {  // ld is a multiple of 64: columns behind N are there, and nobody reads what becomes of them
                 raw[i] = load_last(codes + (m0 + i) * ld + n);
-                top[i] = tops[n / kWarpColumns * padded_rows + m0 + i];
+                top[i] = tops[n / kCodes * padded_rows + m0 + i];
             }
 #pragma unroll
         for (int i = 0; i < kGradRows; ++i) {
@@ -871,7 +888,7 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
         l.weight_splits = once ? choose_splits(l.width, D, div_up(l.rows, kStageK)) : 1;
         l.consts = take(static_cast<size_t>(l.rows) * kConsts * 4);
         l.scale = take(256);
-        if (l.by_rows) l.tops = take(static_cast<size_t>(l.ld_piece / kWarpColumns) * (div_up(l.rows, 32) * 32) * 4);
+        if (l.by_rows) l.tops = take(static_cast<size_t>(l.ld_piece / kCodes) * (div_up(l.rows, 32) * 32) * 4);
         l.piece = take(static_cast<size_t>(l.rows) * l.ld_piece * 2);
         l.parts = take(static_cast<size_t>(l.hidden_splits) * l.rows * l.ld_parts * 4);
         if (!once || l.weight_splits > 1) l.weight_sums = take(static_cast<size_t>(l.weight_splits) * l.width * l.ld_parts * 4);
