@@ -37,6 +37,14 @@ constexpr int kStageBytes = kSlices * kSliceBytes, kStages = 196608 / kStageByte
 constexpr int kStageK = kSlices * BK;
 constexpr int kConsts = 8;                               // floats per row that the gradient needs
 
+// A call's kernels follow one another by programmatic launches: each is set up while the one before still runs, waits for its end here
+// before it touches memory, and lets the next one in.
+__device__ __forceinline__ void wait_for_previous()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 enum Kind { kStats, kLogits, kGrad, kHidden, kWeight, kWeightParts };
 
 // Which operands have the summed index as their rows.
@@ -463,6 +471,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     cluster.sync();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = ctl.tmem;
+    wait_for_previous();
     const auto range = [&](int split, int &kb0, int &kb1) {
         kb0 = static_cast<int>(static_cast<int64_t>(a.k_blocks) * split / a.splits), kb1 = static_cast<int>(static_cast<int64_t>(a.k_blocks) * (split + 1) / a.splits);
     };
@@ -608,6 +617,23 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     }
 }
 
+// A launch that may begin while the kernel before it ends; every kernel here starts with wait_for_previous().
+template <class... P, class... A> int follow(void (*kernel)(P...), dim3 grid, int threads, int smem, int cluster, cudaStream_t s, A... args)
+{
+    cudaLaunchConfig_t config = {};
+    config.gridDim = grid, config.blockDim = dim3(static_cast<unsigned>(threads));
+    config.dynamicSmemBytes = static_cast<size_t>(smem);
+    config.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(cluster), attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    config.attrs = attr, config.numAttrs = cluster > 1 ? 2 : 1;
+    SPDY_EVAL_TRY(cudaLaunchKernelEx(&config, kernel, static_cast<P>(args)...));
+    return SPDY_OK;
+}
+
 // ---------------------------------------------------------------------------------------------- rows
 struct RowArgs {
     int64_t R, V, padded_rows;
@@ -638,6 +664,7 @@ __device__ __forceinline__ void write_consts(const RowArgs &a, int64_t r, int64_
 // The largest bound on a row's gradient by its logits: |d| <= |ga| + |gb| (p |log p| + p H), p |log p| < 0.37, H <= log V.
 __global__ void __launch_bounds__(256) scale_kernel(const RowArgs a, uint32_t *bits)
 {
+    wait_for_previous();
     float most = 0.f;
     const float spread = 0.37f + logf(static_cast<float>(a.V));
     for (int64_t r = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; r < a.R; r += static_cast<int64_t>(gridDim.x) * 256) {
@@ -648,12 +675,30 @@ __global__ void __launch_bounds__(256) scale_kernel(const RowArgs a, uint32_t *b
     if (most > 0.f) atomicMax(bits, __float_as_uint(most));  // of whole numbers: the order does not matter
 }
 
+// What comes of a row's sums.
+__device__ __forceinline__ void finish_row(const RowArgs &a, int64_t r, const Sums &sums)
+{
+    const int64_t token = a.tokens ? token_at(a.tokens, a.index_bits, r) : -1;
+    const bool empty = sums.s == 0.f;
+    const float log_s = logf(sums.s), entropy = empty ? 0.f : log_s - kLn2 * (sums.t / sums.s);
+    if (a.lse) a.lse[r] = sums.m / a.temperature + log_s;
+    if (a.entropy) a.entropy[r] = entropy;
+    if (a.logprob) {
+        float lp = 0.f;
+        if (token >= a.V) lp = quiet_nan();
+        else if (token >= 0) lp = empty ? neg_inf() : (a.token_logit[r] - sums.m) / a.temperature - log_s;
+        a.logprob[r] = lp;
+    }
+    if (a.consts) write_consts(a, r, token, sums.m, log2f(sums.s), entropy, empty);
+}
+
 // Joins the tiles of 32 rows, a row to a lane: each warp every 32nd tile, eight of them at a time (their loads in flight together, one
 // rescaling for all), then the warps.  2048 rows of 512 tiles: 34 us with a rescaling per tile and 16 warps, 10 this way.
 constexpr int kRowWarps = 32, kRowTiles = 8;
 __global__ void __launch_bounds__(32 * kRowWarps) rows_kernel(const RowArgs a)
 {
     __shared__ float room[kRowWarps][3][32];
+    wait_for_previous();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t r = static_cast<int64_t>(blockIdx.x) * 32 + lane;
     // `N` sums at once; what is not there is the empty sum
@@ -696,27 +741,124 @@ __global__ void __launch_bounds__(32 * kRowWarps) rows_kernel(const RowArgs a)
         }
         join_all(sums, m, s, t, kRowTiles);
     }
-    const int64_t token = a.tokens ? token_at(a.tokens, a.index_bits, r) : -1;
-    const bool empty = sums.s == 0.f;
-    const float log_s = logf(sums.s), entropy = empty ? 0.f : log_s - kLn2 * (sums.t / sums.s);
-    if (a.lse) a.lse[r] = sums.m / a.temperature + log_s;
-    if (a.entropy) a.entropy[r] = entropy;
-    if (a.logprob) {
-        float lp = 0.f;
-        if (token >= a.V) lp = quiet_nan();
-        else if (token >= 0) lp = empty ? neg_inf() : (a.token_logit[r] - sums.m) / a.temperature - log_s;
-        a.logprob[r] = lp;
-    }
-    if (a.consts) write_consts(a, r, token, sums.m, log2f(sums.s), entropy, empty);
+    finish_row(a, r, sums);
+}
+
+// The same for few rows, a block to a row, whose sums lie one behind the other.
+__global__ void __launch_bounds__(256) few_rows_kernel(const RowArgs a)
+{
+    __shared__ float room[8][3];
+    wait_for_previous();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float *from = a.partial + 3 * static_cast<int64_t>(blockIdx.x) * a.tiles;
+    Sums sums = {neg_inf(), 0.f, 0.f};
+#pragma unroll 4
+    for (int i = threadIdx.x; i < a.tiles; i += 256) join(sums, {from[i], from[a.tiles + i], from[2 * a.tiles + i]}, a.c);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) join(sums, {__shfl_xor_sync(0xffffffffu, sums.m, d), __shfl_xor_sync(0xffffffffu, sums.s, d), __shfl_xor_sync(0xffffffffu, sums.t, d)}, a.c);
+    if (lane == 0) room[warp][0] = sums.m, room[warp][1] = sums.s, room[warp][2] = sums.t;
+    __syncthreads();
+    if (threadIdx.x > 0) return;
+    for (int w = 1; w < 8; ++w) join(sums, {room[w][0], room[w][1], room[w][2]}, a.c);
+    finish_row(a, blockIdx.x, sums);
 }
 
 // The same from a forward call's lse and entropy.
 __global__ void __launch_bounds__(256) saved_rows_kernel(const RowArgs a)
 {
+    wait_for_previous();
     const int64_t r = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     if (r >= a.R) return;
     const float lse = a.in_lse[r];
     write_consts(a, r, a.tokens ? token_at(a.tokens, a.index_bits, r) : -1, lse * a.temperature, 0.f, a.in_entropy ? a.in_entropy[r] : 0.f, lse == neg_inf());
+}
+
+// ---------------------------------------------------------------------------------------------- few rows
+// Values of up to 4 rows: weight is streamed once by plain multiply-adds, four ids to a warp at a time, hidden comes from L1.  A block
+// leaves one set of sums, as a tile does.  Bound by weight's bytes: TIMES
+constexpr int kFewRows = 4, kFewIds = 4, kFewThreads = 256;
+template <class T, int ROWS, bool WIDE>
+__global__ void __launch_bounds__(kFewThreads) few_kernel(const T *hidden, int64_t ldh, const T *weight, int64_t ldw, int64_t R, int64_t V, int64_t D, const ProductArgs a)
+{
+    __shared__ float room[kFewThreads / 32][ROWS][3];
+    wait_for_previous();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kFewThreads / 32);
+    Sums sums[ROWS];
+    int64_t token[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) sums[r] = {neg_inf(), 0.f, 0.f}, token[r] = r < R && a.token_logit ? token_at(a.tokens, a.index_bits, r) : -1;
+    for (int64_t v0 = (static_cast<int64_t>(blockIdx.x) * (kFewThreads / 32) + warp) * kFewIds; v0 < V; v0 += warps * kFewIds) {
+        float acc[ROWS][kFewIds];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int c = 0; c < kFewIds; ++c) acc[r][c] = 0.f;
+        const T *w = weight + v0 * ldw;
+        if (WIDE) {
+#pragma unroll 3
+            for (int64_t k = lane * 8; k < D; k += 256) {
+                uint4 raw[kFewIds];
+#pragma unroll
+                for (int c = 0; c < kFewIds; ++c) raw[c] = v0 + c < V ? load_stream(w + c * ldw + k) : make_uint4(0, 0, 0, 0);
+                float h[ROWS][8];
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) Elem<T>::unpack(r < R ? *reinterpret_cast<const uint4 *>(hidden + r * ldh + k) : make_uint4(0, 0, 0, 0), h[r]);
+#pragma unroll
+                for (int c = 0; c < kFewIds; ++c) {
+                    float f[8];
+                    Elem<T>::unpack(raw[c], f);
+#pragma unroll
+                    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) acc[r][c] = fmaf(h[r][i], f[i], acc[r][c]);
+                }
+            }
+        } else {
+#pragma unroll 4
+            for (int64_t k = lane; k < D; k += 32) {
+                float f[kFewIds];
+#pragma unroll
+                for (int c = 0; c < kFewIds; ++c) f[c] = v0 + c < V ? Elem<T>::to_float(w[c * ldw + k]) : 0.f;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    const float h = r < R ? Elem<T>::to_float(hidden[r * ldh + k]) : 0.f;
+#pragma unroll
+                    for (int c = 0; c < kFewIds; ++c) acc[r][c] = fmaf(h, f[c], acc[r][c]);
+                }
+            }
+        }
+        const int64_t v = v0 + (lane & 3);  // the id whose logits this lane goes on with
+        const float bias = a.bias && v < V ? value_at(a.bias, a.bias_type, v) : 0.f;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            // four sums over the lanes, of which each lane keeps one
+            const bool up = lane & 1, high = lane & 2;
+            float x = (up ? acc[r][1] : acc[r][0]) + __shfl_xor_sync(0xffffffffu, up ? acc[r][0] : acc[r][1], 1);
+            const float y = (up ? acc[r][3] : acc[r][2]) + __shfl_xor_sync(0xffffffffu, up ? acc[r][2] : acc[r][3], 1);
+            x = (high ? y : x) + __shfl_xor_sync(0xffffffffu, high ? x : y, 2);
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) x += __shfl_xor_sync(0xffffffffu, x, d);
+            if (r >= R) continue;
+            x = v < V ? x + bias : neg_inf();
+            if (v == token[r] && lane < 4) a.token_logit[r] = x;
+            join(sums[r], {x, x == neg_inf() ? 0.f : 1.f, 0.f}, a.c);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+        for (int d = 1; d < 4; d *= 2)
+            join(sums[r], {__shfl_xor_sync(0xffffffffu, sums[r].m, d), __shfl_xor_sync(0xffffffffu, sums[r].s, d), __shfl_xor_sync(0xffffffffu, sums[r].t, d)}, a.c);
+        if (lane == 0) room[warp][r][0] = sums[r].m, room[warp][r][1] = sums[r].s, room[warp][r][2] = sums[r].t;
+    }
+    __syncthreads();
+    const int r = threadIdx.x;
+    if (r >= ROWS || r >= R) return;
+    Sums all = {neg_inf(), 0.f, 0.f};
+    for (int q = 0; q < kFewThreads / 32; ++q) join(all, {room[q][r][0], room[q][r][1], room[q][r][2]}, a.c);
+    float *to = a.partial + 3 * r * gridDim.x + blockIdx.x;
+    to[0] = all.m, to[gridDim.x] = all.s, to[2 * gridDim.x] = all.t;
 }
 
 // ---------------------------------------------------------------------------------------------- gradient by kept logits
@@ -727,6 +869,7 @@ __global__ void __launch_bounds__(256) grad_kernel(uint16_t *codes, const float 
                                                    const uint32_t *scale_bits)
 {
     __shared__ RowConsts rows[kGradRows];
+    wait_for_previous();
     const int64_t n = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
     for (int64_t m0 = static_cast<int64_t>(blockIdx.y) * kGradRows; m0 < M; m0 += static_cast<int64_t>(gridDim.y) * kGradRows) {
         const int count = static_cast<int>(min(M - m0, static_cast<int64_t>(kGradRows)));
@@ -771,6 +914,7 @@ __global__ void __launch_bounds__(256) grad_kernel(uint16_t *codes, const float 
 template <class T, class Index>
 __global__ void __launch_bounds__(256) finish_kernel(const float *parts, int splits, int64_t M, int64_t N, int64_t ldp, const uint32_t *scale_bits, T *out, int64_t ldo, int wide)
 {
+    wait_for_previous();
     const float scale = power_of_two(-scale_power(scale_bits));
     const Index across = static_cast<Index>(ldp / 8), total = static_cast<Index>(M) * across;
     for (Index i = static_cast<Index>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<Index>(gridDim.x) * 256) {
@@ -803,15 +947,15 @@ template <class T> int finish(const float *parts, int splits, int64_t M, int64_t
     const int wide = aligned(out, 16) && ldo % 8 == 0;
     const int64_t total = M * (ldp / 8), most = static_cast<int64_t>(sm_count()) * 8, want = (total + 255) / 256;
     const unsigned blocks = static_cast<unsigned>(want < most ? want : most);
-    if (total + most * 256 < (1ll << 32)) finish_kernel<T, uint32_t><<<blocks, 256, 0, s>>>(parts, splits, M, N, ldp, scale_bits, out, ldo, wide);
-    else finish_kernel<T, uint64_t><<<blocks, 256, 0, s>>>(parts, splits, M, N, ldp, scale_bits, out, ldo, wide);
-    return finish_launch();
+    if (total + most * 256 < (1ll << 32)) return follow(finish_kernel<T, uint32_t>, dim3(blocks), 256, 0, 1, s, parts, splits, M, N, ldp, scale_bits, out, ldo, wide);
+    return follow(finish_kernel<T, uint64_t>, dim3(blocks), 256, 0, 1, s, parts, splits, M, N, ldp, scale_bits, out, ldo, wide);
 }
 
 // dbias of a piece: the row groups' sums in their order, eight runs of them to a column.
 __global__ void __launch_bounds__(256) bias_kernel(const float *sums, int64_t groups, int64_t N, int64_t ld, const uint32_t *scale_bits, float *dbias)
 {
     __shared__ float room[8][32];
+    wait_for_previous();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t n = static_cast<int64_t>(blockIdx.x) * 32 + lane;
     float sum = 0.f;
@@ -856,6 +1000,15 @@ int choose_splits(int64_t M, int64_t N, int64_t k_blocks)
     return best;
 }
 
+// Copies of operands get rows of whole 128 bytes: TMA's boxes then touch no line twice (1021 x 50001 x 1000: 108 us with rows of 2000 bytes,
+// 84 us with 2048).
+int64_t copy_ld(int64_t D) { return div_up(D, 64) * 64; }
+size_t copy_bytes(int64_t rows, int64_t D) { return static_cast<size_t>(rows) * static_cast<size_t>(copy_ld(D)) * 2; }
+
+// Values alone of few rows need no tensor cores, and no copies of operands either.
+bool is_few(int64_t R, bool grads) { return R <= kFewRows && !grads; }
+int64_t few_blocks() { return static_cast<int64_t>(sm_count()) * 4; }
+
 Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int64_t R, int64_t V, int64_t D, bool stats, bool grads, bool bias)
 {
     Layout l = {};
@@ -866,8 +1019,14 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
         return here;
     };
     l.rows = R, l.width = V;
-    l.hidden = take(tma_ok(hidden, ldh) ? 0 : packed_bytes(R, D));
-    l.weight = take(tma_ok(weight, ldw) ? 0 : packed_bytes(V, D));
+    if (is_few(R, grads)) {
+        l.partial = take(static_cast<size_t>(few_blocks()) * 3 * R * 4);
+        l.token_logit = take(static_cast<size_t>(R) * 4);
+        l.total = at;
+        return l;
+    }
+    l.hidden = take(tma_ok(hidden, ldh) ? 0 : copy_bytes(R, D));
+    l.weight = take(tma_ok(weight, ldw) ? 0 : copy_bytes(V, D));
     if (grads) {
         l.ld_piece = div_up(V, 64) * 64;
         const int64_t most = kLogitBytes / 2 / l.ld_piece;  // rows
@@ -930,17 +1089,7 @@ template <class T, int KIND, bool ENT> int launch_product(const CUtensorMap &ma,
     const int items = a.tiles_m * a.tiles_n * splits, pairs = sm_count() / 2;
     auto *kernel = product_kernel<T, KIND, ENT>;
     SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<KIND>()));
-    cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(static_cast<unsigned>((items < pairs ? items : pairs) * 2));
-    config.blockDim = dim3(kThreads);
-    config.dynamicSmemBytes = smem_bytes<KIND>();
-    config.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    config.attrs = attr, config.numAttrs = 1;
-    SPDY_EVAL_TRY(cudaLaunchKernelEx(&config, kernel, ma, mb, a));
-    return SPDY_OK;
+    return follow(kernel, dim3(static_cast<unsigned>((items < pairs ? items : pairs) * 2)), kThreads, smem_bytes<KIND>(), 2, s, ma, mb, a);
 }
 
 // Tiles down that are worked on side by side: in a product over the width, as many as leave their rows of hidden (or of the piece) in L2.
@@ -967,6 +1116,20 @@ template <class T> struct Head {
 
     float *floats(size_t at) const { return reinterpret_cast<float *>(ws + at); }
 
+    // The values of few rows.
+    template <int ROWS> int few(RowArgs rows)
+    {
+        ProductArgs a = base;
+        a.partial = floats(l.partial), a.token_logit = rows.tokens ? floats(l.token_logit) : nullptr;
+        const int64_t want = div_up(h.V, kFewIds * (kFewThreads / 32)), most = few_blocks();
+        const unsigned blocks = static_cast<unsigned>(want < most ? want : most);
+        const T *x = static_cast<const T *>(h.hidden), *w = static_cast<const T *>(h.weight);
+        const bool wide = tma_ok(x, h.ldh) && tma_ok(w, h.ldw) && h.D % 8 == 0;
+        HEAD_TRY(follow(wide ? few_kernel<T, ROWS, true> : few_kernel<T, ROWS, false>, dim3(blocks), kFewThreads, 0, 1, s, x, h.ldh, w, h.ldw, h.R, h.V, h.D, a));
+        rows.partial = a.partial, rows.token_logit = a.token_logit, rows.tiles = static_cast<int>(blocks);
+        return follow(few_rows_kernel, dim3(static_cast<unsigned>(h.R)), 256, 0, 1, s, rows);
+    }
+
     // Sums of rows' exponentials and what comes of them; KIND kLogits keeps the logits.
     template <int KIND> int stats(RowArgs rows, int64_t r0)
     {
@@ -977,8 +1140,7 @@ template <class T> struct Head {
         if (KIND == kLogits) a.out = ws + l.piece, a.ldo = l.ld_piece, a.tops = floats(l.tops);
         HEAD_TRY((launch_product<T, KIND, true>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
         rows.partial = a.partial, rows.token_logit = a.token_logit, rows.tiles = static_cast<int>(div_up(h.V, kTile));
-        rows_kernel<<<static_cast<unsigned>(div_up(rows.R, 32)), 32 * kRowWarps, 0, s>>>(rows);
-        return finish_launch();
+        return follow(rows_kernel, dim3(static_cast<unsigned>(div_up(rows.R, 32))), 32 * kRowWarps, 0, 1, s, rows);
     }
     // The gradient by the kept logits of m rows.
     int gradient(int64_t m)
@@ -986,9 +1148,7 @@ template <class T> struct Head {
         const int64_t down = div_up(m, kGradRows);
         const dim3 grid(static_cast<unsigned>(div_up(h.V, 2048)), static_cast<unsigned>(down < 65535 ? down : 65535));
         uint16_t *codes = reinterpret_cast<uint16_t *>(ws + l.piece);
-        if (h.grad_entropy) grad_kernel<T, true><<<grid, 256, 0, s>>>(codes, floats(l.tops), l.padded_rows, m, h.V, l.ld_piece, base.consts, base.c, base.scale_bits);
-        else grad_kernel<T, false><<<grid, 256, 0, s>>>(codes, floats(l.tops), l.padded_rows, m, h.V, l.ld_piece, base.consts, base.c, base.scale_bits);
-        return finish_launch();
+        return follow(h.grad_entropy ? grad_kernel<T, true> : grad_kernel<T, false>, grid, 256, 0, 1, s, codes, floats(l.tops), l.padded_rows, m, h.V, l.ld_piece, base.consts, base.c, base.scale_bits);
     }
     // The gradient by the logits of all rows and ids v0 .. v0 + n - 1, which are multiplied again; dbias of these ids.
     int gradient_again(int64_t n, int64_t v0)
@@ -1003,8 +1163,7 @@ template <class T> struct Head {
     }
     int finish_bias(int64_t n, int64_t v0)
     {
-        bias_kernel<<<static_cast<unsigned>(div_up(n, 32)), 256, 0, s>>>(floats(l.sums), div_up(h.R, 32), n, l.ld_piece, base.scale_bits, h.dbias + v0);
-        return finish_launch();
+        return follow(bias_kernel, dim3(static_cast<unsigned>(div_up(n, 32))), 256, 0, 1, s, floats(l.sums), div_up(h.R, 32), n, l.ld_piece, base.scale_bits, h.dbias + v0);
     }
     // dhidden's sums and dweight from the gradient of m rows (from r0) and n ids (from v0), added to what earlier rows or ids gave.
     int products(int64_t m, int64_t r0, int64_t n, int64_t v0)
@@ -1043,13 +1202,14 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
     const Layout l = lay_out(h.hidden, h.ldh, h.weight, h.ldw, h.R, h.V, h.D, h.stats, h.grads, h.dbias != nullptr);
     char *ws = static_cast<char *>(workspace);
     const int64_t R = h.R, V = h.V, D = h.D;
+    const bool few = is_few(R, h.grads);
     Repack p = {};
-    p.K = D, p.ldto = packed_ld(D);
-    if (!tma_ok(h.hidden, h.ldh)) {
+    p.K = D, p.ldto = copy_ld(D);
+    if (!few && !tma_ok(h.hidden, h.ldh)) {
         p.from[0] = static_cast<const uint16_t *>(h.hidden), p.ld[0] = h.ldh, p.rows[0] = R, p.to[0] = reinterpret_cast<uint16_t *>(ws + l.hidden);
         h.hidden = ws + l.hidden, h.ldh = p.ldto;
     }
-    if (!tma_ok(h.weight, h.ldw)) {
+    if (!few && !tma_ok(h.weight, h.ldw)) {
         p.from[1] = static_cast<const uint16_t *>(h.weight), p.ld[1] = h.ldw, p.rows[1] = V, p.to[1] = reinterpret_cast<uint16_t *>(ws + l.weight);
         h.weight = ws + l.weight, h.ldw = p.ldto;
     }
@@ -1058,9 +1218,11 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
         repack_kernel<<<dim3(static_cast<unsigned>(blocks < 2368 ? blocks : 2368), 2), 256, 0, s>>>(p);
         HEAD_TRY(finish_launch());
     }
-    CUtensorMap hidden, weight;
-    HEAD_TRY(map_of(&hidden, h.hidden, h.ldh, R, D, h.dtype, BM));
-    HEAD_TRY(map_of(&weight, h.weight, h.ldw, V, D, h.dtype, BM));
+    CUtensorMap hidden = {}, weight = {};
+    if (!few) {
+        HEAD_TRY(map_of(&hidden, h.hidden, h.ldh, R, D, h.dtype, BM));
+        HEAD_TRY(map_of(&weight, h.weight, h.ldw, V, D, h.dtype, BM));
+    }
 
     RowArgs rows = {};
     rows.R = R, rows.V = V, rows.padded_rows = l.padded_rows;
@@ -1076,13 +1238,13 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
             uint32_t *bits = reinterpret_cast<uint32_t *>(ws + l.scale);
             SPDY_EVAL_TRY(cudaMemsetAsync(bits, 0, 4, s));
             const int64_t blocks = div_up(R, 256), most = sm_count();
-            scale_kernel<<<static_cast<unsigned>(blocks < most ? blocks : most), 256, 0, s>>>(rows, bits);
-            HEAD_TRY(finish_launch());
+            HEAD_TRY(follow(scale_kernel, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), 256, 0, 1, s, rows, bits));
             base.scale_bits = bits;
         }
         base.consts = rows.consts;
     }
     Head<T> g = {h, l, ws, s, base, hidden, weight, {}, {}};
+    if (few) return R == 1 ? g.template few<1>(rows) : R == 2 ? g.template few<2>(rows) : g.template few<4>(rows);
     if (h.grads) {
         HEAD_TRY(map_of(&g.hidden_columns, h.hidden, h.ldh, R, D, h.dtype, BK));
         HEAD_TRY(map_of(&g.weight_columns, h.weight, h.ldw, V, D, h.dtype, BK));
@@ -1105,8 +1267,7 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
         if (h.stats) {
             HEAD_TRY(g.template stats<kStats>(rows, 0));
         } else {
-            saved_rows_kernel<<<static_cast<unsigned>(div_up(R, 256)), 256, 0, s>>>(rows);
-            HEAD_TRY(finish_launch());
+            HEAD_TRY(follow(saved_rows_kernel, dim3(static_cast<unsigned>(div_up(R, 256))), 256, 0, 1, s, rows));
         }
         if (!h.grads) return SPDY_OK;
         for (int64_t v0 = 0; v0 < V; v0 += l.width) {

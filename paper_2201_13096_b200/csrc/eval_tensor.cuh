@@ -197,10 +197,28 @@ static __global__ void __launch_bounds__(256) repack_kernel(const Repack p)
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
         const int64_t r = small ? static_cast<uint32_t>(i) / static_cast<uint32_t>(per_row) : i / per_row, k = (i - r * per_row) * 8;
         const uint16_t *from = p.from[which] + r * p.ld[which] + k;
-        uint32_t e[8];
+        uint32_t w[4];
+        if (k > 0 && k + 8 < p.K) {  // the aligned words around them lie inside the row
+            const uintptr_t at = reinterpret_cast<uintptr_t>(from);
+            const uint32_t *q = reinterpret_cast<const uint32_t *>(at & ~static_cast<uintptr_t>(3));
+            if (at & 2) {
+                uint32_t v[5];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = k + j < p.K ? from[j] : 0;
-        *reinterpret_cast<uint4 *>(p.to[which] + r * p.ldto + k) = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+                for (int j = 0; j < 5; ++j) v[j] = q[j];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(v[j], v[j + 1], 16);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = q[j];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t lo = k + 2 * j < p.K ? from[2 * j] : 0, hi = k + 2 * j + 1 < p.K ? from[2 * j + 1] : 0;
+                w[j] = lo | hi << 16;
+            }
+        }
+        *reinterpret_cast<uint4 *>(p.to[which] + r * p.ldto + k) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 

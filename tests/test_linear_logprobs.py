@@ -47,7 +47,7 @@ def check(h, w, b, tokens, temperature, gl, gh, on="cpu"):
     for name in ("logprob", "entropy", "lse"):
         tune.close(getattr(out, name), want, name)
         tune.close(getattr(other, name), want, name)
-        assert torch.equal(getattr(alone, name).nan_to_num(5.0), getattr(out, name).nan_to_num(5.0)) or (b is None and w.shape[1] >= 512), name
+        tune.close(getattr(alone, name), want, name)  # up to four rows go their own way
     if b is not None:
         for g in (grads, again):
             tune.close(g.dhidden, want, "dhidden")
@@ -73,6 +73,7 @@ HEADS = [
     (256, 2048, 64, BF16, None, 1.0, True, 0, 0), (257, 2049, 136, F16, None, 0.5, False, 1, 1), (513, 999, 264, BF16, F32, 1.0, True, 0, 0),
     (1000, 3001, 96, BF16, "same", 1.0, False, 0, 0), (700, 64, 1000, F16, F32, 1.0, True, 22, 0), (3, 5000, 520, BF16, F32, 1.0, True, 0, 0),
     (2000, 3, 16, F16, "same", 1.0, True, 0, 0), (40, 4100, 1, BF16, None, 1.0, True, 0, 0),
+    (1, 30001, 768, BF16, F32, 1.0, False, 0, 0), (4, 20003, 264, F16, "same", 0.9, True, 8, 0), (4, 1003, 77, BF16, None, 1.0, False, 0, 3), (5, 1003, 77, BF16, None, 1.0, False, 0, 3),
 ]
 
 
@@ -199,6 +200,12 @@ def test_values_that_are_not_finite_stay_in_their_rows(D):
     b = torch.zeros(600, device="cuda")
     b[599] = INF
     assert torch.isnan(evaluate.linear_token_logprobs(h, w, tokens, b).lse).all()
+    few = evaluate.linear_token_logprobs(h[4:7], w, tokens[4:7])
+    assert torch.isnan(few.lse).tolist() == [False, True, False] and torch.isnan(few.entropy).tolist() == [False, True, False]
+    assert torch.isnan(evaluate.linear_token_logprobs(h[4:7], w, tokens[4:7], b).lse).all()
+    b.fill_(-INF)
+    few = evaluate.linear_token_logprobs(h[6:8], w, tokens[6:8].clamp(min=0), b)
+    assert (few.lse == -INF).all() and (few.logprob == -INF).all() and (few.entropy == 0).all()
 
 
 @gpu
@@ -337,7 +344,7 @@ def test_python_refusals_on_the_device():
             call(h, w, tokens, temperature=t)
     with pytest.raises(binding.SpdyError):
         evaluate.linear_token_logprobs_backward(h, w, tokens, torch.zeros(8, device="cuda"), grad_entropy=torch.ones(8, device="cuda"))
-    with pytest.raises(binding.SpdyError, match="overlap|argument"):
+    with pytest.raises(binding.SpdyError):
         call(h, w, tokens, torch.ones(8, device="cuda"), dhidden=h)
 
 
