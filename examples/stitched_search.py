@@ -7,7 +7,8 @@ The model is a stack of BERT-style feed-forward blocks over a small vocabulary w
 Every linear layer of the blocks can be pruned to each sparsity of the grid of Section 4 (the database holds its weights with the
 smallest magnitudes removed), and the search picks one sparsity per layer within a time budget.  A profile's loss
 (``eval_fn``, Section 3.4) is the distillation loss of the model stitched together for it against the dense model's most
-probable tokens.  Afterwards the last normalisation of the chosen model is tuned against the dense model for a few steps.
+probable tokens.  Afterwards the last normalisation of the chosen model is tuned against the dense model for a few steps, and with
+``--answer-steps`` it is tuned on the dense model's best tokens together with the output layer, by AdamW with moments in 8 bits.
 
     python examples/stitched_search.py [--blocks 2] [--hidden 256] [--speedup 2.5] ...
 """
@@ -50,15 +51,21 @@ class StitchedModel:
         dense = evaluate.token_logprobs(logits, logits.argmax(dim=1), top_k=top_k)
         self.top_ids, self.top_logprobs = dense.top_ids, dense.top_logprobs  # the dense model's answers, kept for good
 
-    def forward(self, profile):
-        """Logits of the model stitched together for ``profile`` (a choice per layer), and the last normalisation's input."""
+    def hidden(self, profile):
+        """What the output layer sees in the model stitched together for ``profile`` (a choice per layer), and the last normalisation's
+        input and statistics."""
         h = self.embedding[self.ids]
         for b, (weight, bias) in enumerate(self.norms):
             up, down = 2 * b, 2 * b + 1
             inner = evaluate.linear(h, self.database[up][profile[up]], bias=self.biases[up], activation="gelu")
             last = evaluate.linear(inner, self.database[down][profile[down]], bias=self.biases[down], residual=h)
             h, mean, rstd = evaluate.layer_norm(last, weight, bias)
-        return evaluate.linear(h, self.head), (last, mean, rstd)
+        return h, (last, mean, rstd)
+
+    def forward(self, profile):
+        """Logits of the stitched model, and the last normalisation's input and statistics."""
+        h, last = self.hidden(profile)
+        return evaluate.linear(h, self.head), last
 
     def loss(self, profile) -> float:
         """The search's ``eval_fn``: +inf for an infeasible profile (bytes 0xFF)."""
@@ -81,6 +88,30 @@ class StitchedModel:
             self.norms[-1] = (weight - rate * dweight, bias - rate * dbias)
         return losses
 
+    def answer_gradients(self, profile):
+        """Mean log probability of the dense model's best tokens, and the gradients of its negative by the output layer's weight and the last
+        normalisation's weight and bias.  No table of logits is made."""
+        h, (x, mean, rstd) = self.hidden([int(c) for c in profile])
+        weight, _ = self.norms[-1]
+        tokens = self.top_ids[:, 0].contiguous()
+        per_row = torch.full((self.ids.numel(),), -1.0 / self.ids.numel(), device="cuda")
+        out, grads = evaluate.linear_token_logprobs_with_grad(h, self.head, tokens, per_row)
+        _, dweight, dbias = evaluate.layer_norm_backward(grads.dhidden, x, weight, mean, rstd)
+        return out.logprob.mean(), [grads.dweight, dweight, dbias]
+
+    def tune_on_answers(self, profile, steps: int, rate: float):
+        """AdamW steps on the output layer and the last normalisation; the loss before each."""
+        weight, bias = (t.clone() for t in self.norms[-1])
+        self.norms[-1] = (weight, bias)
+        plan = evaluate.AdamW([self.head, weight, bias], bits=8, weight_decay=[0.01, 0.0, 0.0], rounding="stochastic")
+        losses = []
+        for step in range(1, steps + 1):
+            logprob, grads = self.answer_gradients(profile)
+            losses.append(-float(logprob))
+            evaluate.adamw_step(plan, grads, lr=rate, step=step, seed=step)
+        self.head_by_input = self.head.t().contiguous()
+        return losses
+
 
 def main(argv=None) -> dict:
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
@@ -95,6 +126,7 @@ def main(argv=None) -> dict:
     ap.add_argument("--budget", type=int, default=1000, help="time buckets")
     ap.add_argument("--trials", type=int, default=30)
     ap.add_argument("--tune-steps", type=int, default=10)
+    ap.add_argument("--answer-steps", type=int, default=0)
     ap.add_argument("--seed", type=int, default=0)
     a = ap.parse_args(argv)
 
@@ -111,6 +143,8 @@ def main(argv=None) -> dict:
            "budget": a.budget, "evals": found["evals"]}
     out["tuning"] = model.tune(found["profile"], a.tune_steps, rate=0.5)
     out["tuned"] = model.loss(found["profile"])
+    if a.answer_steps:
+        out["answers"] = model.tune_on_answers(found["profile"], a.answer_steps, rate=1e-3)
     return out
 
 

@@ -625,7 +625,7 @@ class AdamW:
     bits for each moment.  ``masters``: None, True (float32 copies of the 16-bit parameters are made here), or a list of float32
     tensors (None where there is no copy).  ``moments``: None (zeros), or a list of ``AdamWMoments`` to go on with, which the steps
     change in place.  ``weight_decay`` and ``keep_zeros`` (elements whose weight is 0 stay 0): one value, or one for each parameter.
-    ``rounding`` of 16-bit parameters without a master: "nearest" or "stochastic"."""
+    The tensors must keep their memory as long as the plan is used.  ``rounding`` of 16-bit parameters without a master: "nearest" or "stochastic"."""
 
     def __init__(self, params, bits: int = 32, masters=None, moments=None, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, keep_zeros=False,
                  rounding: str = "nearest"):
@@ -684,6 +684,7 @@ class AdamW:
         if any(a[1] > b[0] for a, b in zip(written, written[1:])):
             raise ValueError("params, masters and moments must not share memory")
         self._words = self._table.view(np.uint64).reshape(count, -1)
+        self._pointers = [p.data_ptr() for p in self.params]
         self._shapes = [tuple(p.shape) for p in self.params]
         self._strides = [p.stride() for p in self.params]
         self._dtypes = [p.dtype for p in self.params]
@@ -740,6 +741,8 @@ def adamw_step(plan: AdamW, grads, lr, step, seed: int = 0, grad_scale=None, ski
                 raise ValueError(f"grads[{len(pointers)}] must be {dtype} or float32")
             wide.append(len(pointers))
         pointers.append(g.data_ptr())
+    if plan._pointers != [p.data_ptr() for p in plan.params]:
+        raise ValueError("params must stay where they were when the plan was made")
     words = plan._words.copy()  # the plan's own stays as it is: calls of several threads do not meet
     words[:, 1] = pointers
     if wide:

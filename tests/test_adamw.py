@@ -258,6 +258,35 @@ def test_numbers_on_the_device_skips_streams_and_graphs(bits):
 
 
 @gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_numbers_on_the_device_with_more_chunks_than_blocks(bits):
+    sizes = (6_000_001, 33, 3_000_000)  # blocks walk over several chunks, and from one tensor into the next
+
+    def run(device):
+        params = [values(n, n % 1000).cuda().to(BF16) for n in sizes]
+        plan = evaluate.AdamW(params, bits=bits, rounding="stochastic")
+        for t in (1, 2):
+            grads = [gradient(n, t + n % 1000).cuda().to(BF16) for n in sizes]
+            if device:
+                evaluate.adamw_step(plan, grads, lr=torch.full((1,), 0.25, device="cuda"), step=torch.full((1,), t, dtype=torch.int64, device="cuda"), seed=4)
+            else:
+                evaluate.adamw_step(plan, grads, lr=0.25, step=t, seed=4)
+        return list(plan._written())
+
+    for a, b in zip(run(False), run(True)):  # 0.25 is the same in fp32
+        assert torch.equal(a, b)
+
+
+@gpu
+def test_parameters_that_moved_are_refused():
+    p = torch.ones(64, device="cuda")
+    plan = evaluate.AdamW([p])
+    p.data = torch.ones(64, device="cuda")
+    with pytest.raises(ValueError, match="stay where"):
+        evaluate.adamw_step(plan, [torch.ones(64, device="cuda")], lr=0.1, step=1)
+
+
+@gpu
 def test_leaves_of_autograd_notice_the_step():
     w = torch.nn.Parameter(torch.randn(64, device="cuda"))
     y = (w * w).sum()
