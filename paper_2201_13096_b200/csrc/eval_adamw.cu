@@ -36,7 +36,7 @@ struct Entry {
     uint32_t flags;
     uint32_t unused;
 };
-enum { kWide = 1, kKeepZeros = 2 };  // kWide: param, grad and master start on 16 bytes
+enum { kWide = 1, kWideStates = 2, kKeepZeros = 4 };  // kWide: param, grad and master start on 32 bytes; kWideStates: so do m and v
 
 struct StepArgs {
     float b1, b2, g1, g2, eps, rate, root;  // g1 = 1 - b1, rate = lr / (1 - b1^t), root = 1 / sqrt(1 - b2^t)
@@ -163,14 +163,30 @@ template <class T> __device__ __noinline__ void scatter(T *p, int left, uint4 v)
             else reinterpret_cast<uint8_t *>(p)[i] = static_cast<uint8_t>(x);
         }
 }
-// Everything is read once and written once: first to leave L2 (150 M elements with fp32 states and masters 653 us without that, 614 with it).
-// N elements from `p` on; `whole`: all exist, and p lies on 16 bytes.
+// 32 bytes, first to leave L2: everything is read once and written once (150 M elements with fp32 states and masters 653 us without that,
+// 614 with it).
+__device__ __forceinline__ void load_pair(const void *p, uint4 &lo, uint4 &hi)
+{
+    asm volatile("ld.global.L1::no_allocate.L2::evict_first.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(lo.x), "=r"(lo.y), "=r"(lo.z), "=r"(lo.w), "=r"(hi.x), "=r"(hi.y), "=r"(hi.z), "=r"(hi.w)
+                 : "l"(p)
+                 : "memory");
+}
+__device__ __forceinline__ void store_pair(void *p, uint4 lo, uint4 hi)
+{
+    asm volatile("st.global.L1::no_allocate.L2::evict_first.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(lo.x), "r"(lo.y), "r"(lo.z), "r"(lo.w), "r"(hi.x),
+                 "r"(hi.y), "r"(hi.z), "r"(hi.w)
+                 : "memory");
+}
+// N elements from `p` on; `whole`: all exist, and p lies on 32 bytes (16, where they are no more).
 template <class T, int N> __device__ __forceinline__ void load(const T *p, int left, bool whole, uint4 *raw)
 {
     constexpr int per = 16 / sizeof(T);
     if (whole) {
+        if constexpr (N / per == 1) raw[0] = load_last(p);
+        else
 #pragma unroll
-        for (int j = 0; j < N / per; ++j) raw[j] = load_last(p + j * per);
+            for (int j = 0; j < N / per; j += 2) load_pair(p + j * per, raw[j], raw[j + 1]);
     } else {
 #pragma unroll
         for (int j = 0; j < N / per; ++j) raw[j] = gather<T>(p + j * per, left - j * per);
@@ -180,8 +196,10 @@ template <class T, int N> __device__ __forceinline__ void store(T *p, int left, 
 {
     constexpr int per = 16 / sizeof(T);
     if (whole) {
+        if constexpr (N / per == 1) store_last(p, raw[0]);
+        else
 #pragma unroll
-        for (int j = 0; j < N / per; ++j) store_last(p + j * per, raw[j]);
+            for (int j = 0; j < N / per; j += 2) store_pair(p + j * per, raw[j], raw[j + 1]);
     } else {
 #pragma unroll
         for (int j = 0; j < N / per; ++j) scatter<T>(p + j * per, left - j * per, raw[j]);
@@ -289,8 +307,9 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
         uint4 rw[kW], rg[kG], rm[kM], rv[kM];
         load<W, N>(weights + e, left, whole, rw);
         load<G, N>(static_cast<const G *>(t.grad) + e, left, whole, rg);
-        load<M, N>(static_cast<const M *>(t.m) + e, left, all, rm);
-        load<M, N>(static_cast<const M *>(t.v) + e, left, all, rv);
+        const bool states = all && (BITS == 8 || (t.flags & kWideStates));
+        load<M, N>(static_cast<const M *>(t.m) + e, left, states, rm);
+        load<M, N>(static_cast<const M *>(t.v) + e, left, states, rv);
         float p[N], m[N], v[N];
         if constexpr (BITS == 32) {
             unpack<float, N>(rm, m), unpack<float, N>(rv, v);
@@ -344,8 +363,8 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
             encode<true, N>(m, random, reinterpret_cast<uint32_t *>(rm), em), encode<false, N>(v, random, reinterpret_cast<uint32_t *>(rv), ev);
             if (left > 0 && threadIdx.x % (kBlock / N) == 0) t.m_exp[e / kBlock] = static_cast<uint8_t>(em), t.v_exp[e / kBlock] = static_cast<uint8_t>(ev);
         }
-        store<M, N>(static_cast<M *>(t.m) + e, left, all, rm);
-        store<M, N>(static_cast<M *>(t.v) + e, left, all, rv);
+        store<M, N>(static_cast<M *>(t.m) + e, left, states, rm);
+        store<M, N>(static_cast<M *>(t.v) + e, left, states, rv);
     }
 }
 
@@ -421,7 +440,7 @@ template <class P, class G, int BITS, bool MASTER, bool RANDOM> int step_kind(in
         const spdy_adamw_tensor &t = tensors[i];
         e.param = t.param, e.grad = t.grad, e.master = t.master, e.m = t.m, e.v = t.v, e.m_exp = t.m_exp, e.v_exp = t.v_exp;
         e.weight_decay = t.weight_decay, e.decay = static_cast<float>(1.0 - s.lr * static_cast<double>(t.weight_decay));
-        e.flags = (aligned(t.param, 16) && aligned(t.grad, 16) && aligned(t.master, 16) ? kWide : 0) | (t.keep_zeros ? kKeepZeros : 0);
+        e.flags = (aligned(t.param, 32) && aligned(t.grad, 32) && aligned(t.master, 32) ? kWide : 0) | (aligned(t.m, 32) && aligned(t.v, 32) ? kWideStates : 0) | (t.keep_zeros ? kKeepZeros : 0);
     };
     const auto go = [&](const auto &table) {
         constexpr int cap = static_cast<int>(sizeof(table.e) / sizeof(Entry));
@@ -506,7 +525,7 @@ int spdy_adamw_moments(const spdy_adamw_tensor *tensors, int32_t count, void *co
         const spdy_adamw_tensor &t = tensors[i];
         e = {};
         e.param = m_out[i], e.master = static_cast<float *>(v_out[i]), e.m = t.m, e.v = t.v, e.m_exp = t.m_exp, e.v_exp = t.v_exp;
-        e.flags = aligned(m_out[i], 16) && aligned(v_out[i], 16) ? kWide : 0;
+        e.flags = aligned(m_out[i], 32) && aligned(v_out[i], 32) ? kWide : 0;
     };
     const auto go = [&](const auto &table) {
         constexpr int cap = static_cast<int>(sizeof(table.e) / sizeof(Entry));

@@ -94,6 +94,8 @@ def test_against_the_formula(R, V, D, dtype, bias, temperature, entropy, padh, p
     (9001, 70001, 520, F16),      # three, odd ends
     (700, 5003, 600, F16),        # all rows at once
     (5, 3000, 640, BF16),
+    (512, 30001, 96, BF16),
+    (512, 30001, 512, F16),
 ])
 @pytest.mark.parametrize("entropy", [False, True])
 def test_pieces_and_shares(R, V, D, dtype, entropy):
