@@ -52,9 +52,19 @@ template <int KIND> struct Order {
     static constexpr bool kA = KIND == kWeight || KIND == kWeightParts, kB = kA || KIND == kHidden;
 };
 
+// Division of 32-bit numbers by one that the host knows: the upper half of x ceil(2^64 / d), exact for every x.  (The tiles' and shares'
+// places took 300 instructions a tile and warp with the compiler's divisions, as many as carrying the tile on.)
+struct Divisor {
+    uint64_t m;
+    uint32_t d;
+    Divisor(uint32_t by = 1) : m(by > 1 ? ~0ull / by + 1 : 0), d(by) {}
+    __device__ __forceinline__ uint32_t of(uint32_t x) const { return d == 1 ? x : static_cast<uint32_t>(__umul64hi(x, m)); }
+};
+
 struct ProductArgs {
     int64_t M, N;                  // rows and columns of the result that exist
     int tiles_m, tiles_n, splits, group, k_blocks;
+    Divisor tiles, per_group, per_rows, per_last, per_split;  // tiles; of a group; down in a group, in the last one; splits
     int a_row0, b_row0;            // first rows of the operands
     // kStats, kGrad
     const void *bias, *tokens;
@@ -127,12 +137,13 @@ __device__ __forceinline__ uint64_t operand_by_columns(uint32_t addr)
 // The tile of an item: groups of `group` tiles down, all tiles across before the next group.
 __device__ __forceinline__ void tile_of(const ProductArgs &a, int item, int &split, int &tm, int &tn)
 {
-    const int tiles = a.tiles_m * a.tiles_n;
-    split = item / tiles;
-    const int tile = item - split * tiles, per_group = a.group * a.tiles_n, g = tile / per_group, rest = tile - g * per_group;
-    const int rows = min(a.group, a.tiles_m - g * a.group);
-    tn = rest / rows;
-    tm = g * a.group + rest - tn * rows;
+    const uint32_t x = static_cast<uint32_t>(item);
+    split = static_cast<int>(a.tiles.of(x));
+    const uint32_t tile = x - static_cast<uint32_t>(split) * a.tiles.d, g = a.per_group.of(tile), rest = tile - g * a.per_group.d;
+    const bool last = static_cast<int>((g + 1) * a.per_rows.d) > a.tiles_m;
+    const uint32_t across = last ? a.per_last.of(rest) : a.per_rows.of(rest);
+    tn = static_cast<int>(across);
+    tm = static_cast<int>(g * a.per_rows.d + rest - across * (last ? a.per_last.d : a.per_rows.d));
 }
 
 struct Control {
@@ -195,14 +206,18 @@ __device__ __forceinline__ float pick(const float *f, int64_t at)
     for (int i = 0; i < 32; ++i) x = at == i ? f[i] : x;
     return x;
 }
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
 __device__ __forceinline__ float largest(const float *f, float top)
 {
     float other = f[0];
 #pragma unroll
-    for (int i = 2; i < 32; i += 2) other = fmaxf(other, f[i]);
-#pragma unroll
-    for (int i = 1; i < 32; i += 2) top = fmaxf(top, f[i]);
-    return fmaxf(top, other);
+    for (int i = 1; i + 4 <= 32; i += 4) top = max3(top, f[i], f[i + 1]), other = max3(other, f[i + 2], f[i + 3]);
+    return fmaxf(max3(top, f[29], f[30]), fmaxf(other, f[31]));
 }
 
 template <class Ready, class Release>
@@ -473,7 +488,9 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     const uint32_t tmem = ctl.tmem;
     wait_for_previous();
     const auto range = [&](int split, int &kb0, int &kb1) {
-        kb0 = static_cast<int>(static_cast<int64_t>(a.k_blocks) * split / a.splits), kb1 = static_cast<int>(static_cast<int64_t>(a.k_blocks) * (split + 1) / a.splits);
+        kb0 = 0, kb1 = a.k_blocks;
+        if (KIND == kHidden || KIND == kWeightParts)  // below 2^24 stages, up to 64 shares
+            kb0 = static_cast<int>(a.per_split.of(static_cast<uint32_t>(a.k_blocks * split))), kb1 = static_cast<int>(a.per_split.of(static_cast<uint32_t>(a.k_blocks * (split + 1))));
     };
 
     if (warp == 0) {
@@ -1086,6 +1103,9 @@ template <class T, int KIND, bool ENT> int launch_product(const CUtensorMap &ma,
     a.group = group < a.tiles_m ? group : a.tiles_m;
     a.k_blocks = static_cast<int>(div_up(K, kStageK));
     if (static_cast<int64_t>(a.group) * a.tiles_n > 0x3fffffff) return SPDY_ERR_UNSUPPORTED;
+    a.tiles = Divisor(static_cast<uint32_t>(a.tiles_m * a.tiles_n)), a.per_group = Divisor(static_cast<uint32_t>(a.group * a.tiles_n));
+    a.per_rows = Divisor(static_cast<uint32_t>(a.group)), a.per_last = Divisor(static_cast<uint32_t>(a.tiles_m % a.group ? a.tiles_m % a.group : a.group));
+    a.per_split = Divisor(static_cast<uint32_t>(splits));
     const int items = a.tiles_m * a.tiles_n * splits, pairs = sm_count() / 2;
     auto *kernel = product_kernel<T, KIND, ENT>;
     SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<KIND>()));
