@@ -130,7 +130,8 @@ int spdy_token_logprobs_with_grad(const void *logits, int64_t ld, int dtype, con
  *   hidden [R][D], weight [V][D]: `dtype` (SPDY_BF16 or SPDY_F16), D >= 1; bias [V] of `bias_dtype` (`dtype` or SPDY_F32), may be NULL;
  *   a bias of -inf marks ids that are not allowed.  R, V and D below 2^31 - 65536.
  *   tokens, logprob, entropy, lse, rows with nothing left, NaN and infinities: as spdy_token_logprobs has them.  The tensor
- *   core's sums are cut, not rounded: a logit is off by up to about 2^-24 D / 16 of itself.
+ *   cores cut their sums where fp32 additions round; what that takes of a logit on average (1e-9 D of itself) is given back, and about
+ *   as much may be left.  Up to 4 rows are added up in fp32.
  * Gradients of sum_r grad_logprob[r] logprob[r] + grad_entropy[r] entropy[r], with g_rv the gradient by x_rv
  * (spdy_token_logprobs_backward's dlogits):
  *   dhidden[r][d] = sum_v g_rv weight[v][d],   dweight[v][d] = sum_r g_rv hidden[r][d],   dbias[v] = sum_r g_rv

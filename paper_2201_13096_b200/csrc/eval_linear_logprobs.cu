@@ -45,6 +45,12 @@ __device__ __forceinline__ void wait_for_previous()
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// The tensor core cuts its partial sums towards 0 where fp32 additions would round, so that a sum of D products ends short of itself, by
+// this much for each product: 0.75e-9 to 1.0e-9 of it in bf16, 1.0e-9 to 1.1e-9 in half precision (D 64 to 8192, operands of both signs;
+// where all products are positive, 1.2e-9 to 6.5e-9).  Logits get it back: the loss is the same for all of them, and at D = 4096 it
+// moved lse by 4e-6 of itself, and dbias, where gradients of many rows nearly cancel, by more.
+constexpr float kLoss = 0.95e-9f;
+
 enum Kind { kStats, kLogits, kGrad, kHidden, kWeight, kWeightParts };
 
 // Which operands have the summed index as their rows.
@@ -70,7 +76,7 @@ struct ProductArgs {
     const void *bias, *tokens;
     int bias_type, index_bits;
     int64_t v0;                    // the first column's id
-    float c;                       // log2(e) / T
+    float c, loss;                 // log2(e) / T; what a logit has lost of itself
     float *partial, *token_logit;  // [tiles_n][3][padded_rows], [M]
     int64_t padded_rows;
     const float *consts;           // [M][kConsts]
@@ -185,6 +191,11 @@ __device__ __forceinline__ void stage_bias(const ProductArgs &a, int64_t n0, flo
 __device__ __forceinline__ void load_logits(const ProductArgs &a, uint32_t tmem, int64_t n, const float *bias, float *f)
 {
     tmem_load32(tmem, f);
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+        const float2 x = make_float2(f[i], f[i + 1]), y = fma2(x, both(a.loss), x);
+        f[i] = y.x, f[i + 1] = y.y;
+    }
     if (a.bias) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -791,11 +802,12 @@ __global__ void __launch_bounds__(256) saved_rows_kernel(const RowArgs a)
 }
 
 // ---------------------------------------------------------------------------------------------- few rows
-// Values of up to 4 rows: weight is streamed once by plain multiply-adds, four ids to a warp at a time, hidden comes from L1.  A block
+// Logits of up to 4 rows: weight is streamed once by plain multiply-adds, four ids to a warp at a time, hidden comes from L1.  A block
 // leaves one set of sums, as a tile does.  Bound by weight's bytes: TIMES
 constexpr int kFewRows = 4, kFewIds = 4, kFewThreads = 256;
 template <class T, int ROWS, bool WIDE>
-__global__ void __launch_bounds__(kFewThreads) few_kernel(const T *hidden, int64_t ldh, const T *weight, int64_t ldw, int64_t R, int64_t V, int64_t D, const ProductArgs a)
+__global__ void __launch_bounds__(kFewThreads) few_kernel(const T *hidden, int64_t ldh, const T *weight, int64_t ldw, int64_t R, int64_t V, int64_t D, float *logits,
+                                                         int64_t ld_logits, const ProductArgs a)
 {
     __shared__ float room[kFewThreads / 32][ROWS][3];
     wait_for_previous();
@@ -859,6 +871,7 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(const T *hidden, int64
             if (r >= R) continue;
             x = v < V ? x + bias : neg_inf();
             if (v == token[r] && lane < 4) a.token_logit[r] = x;
+            if (logits && v < V && lane < 4) logits[r * ld_logits + v] = x;
             join(sums[r], {x, x == neg_inf() ? 0.f : 1.f, 0.f}, a.c);
         }
     }
@@ -876,6 +889,35 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(const T *hidden, int64
     for (int q = 0; q < kFewThreads / 32; ++q) join(all, {room[q][r][0], room[q][r][1], room[q][r][2]}, a.c);
     float *to = a.partial + 3 * r * gridDim.x + blockIdx.x;
     to[0] = all.m, to[gridDim.x] = all.s, to[2 * gridDim.x] = all.t;
+}
+
+// The gradient by few rows' logits, which are kept in fp32, and dbias; eight columns to a thread.
+template <class T, bool ENT>
+__global__ void __launch_bounds__(256) few_grad_kernel(const float *logits, int64_t R, int64_t N, int64_t ld, const float *consts, float c, const uint32_t *scale_bits, T *out,
+                                                       float *dbias)
+{
+    wait_for_previous();
+    const int64_t n = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+    if (n >= N) return;
+    const int power = scale_power(scale_bits);
+    float sum[8] = {};
+    for (int64_t r = 0; r < R; ++r) {
+        const RowConsts k = row_consts(consts, r, power_of_two(power));
+        uint4 lo, hi;
+        float f[8];
+        load32(logits + r * ld + n, lo, hi);  // ld is a multiple of 64
+        Elem<float>::unpack(lo, f), Elem<float>::unpack(hi, f + 4);
+        const int64_t at = k.token - n;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            f[j] = grad_at<ENT>(fmaf(f[j] - k.ref, c, -k.ls), k);
+            if (at == j) f[j] += k.hit;
+            sum[j] += f[j];
+        }
+        *reinterpret_cast<uint4 *>(out + r * ld + n) = Elem<T>::pack(f);
+    }
+    if (dbias)
+        for (int j = 0; j < 8 && n + j < N; ++j) dbias[n + j] = sum[j] * power_of_two(-power);
 }
 
 // ---------------------------------------------------------------------------------------------- gradient by kept logits
@@ -996,7 +1038,7 @@ constexpr int64_t kPieceBytes = 256ll << 20, kLeastPiece = 2048;
 constexpr int64_t kLogitBytes = 512ll << 20, kLeastRows = 2048, kLeastWidth = 512;
 
 struct Layout {
-    size_t hidden, weight, partial, token_logit, consts, scale, tops, piece, parts, weight_sums, sums, total;
+    size_t hidden, weight, partial, token_logit, consts, scale, logits, tops, piece, parts, weight_sums, sums, total;
     int64_t padded_rows, rows, width, ld_piece, ld_parts;  // rows, width: what is worked on at a time
     int hidden_splits, weight_splits;
     bool by_rows;
@@ -1022,8 +1064,9 @@ int choose_splits(int64_t M, int64_t N, int64_t k_blocks)
 int64_t copy_ld(int64_t D) { return div_up(D, 64) * 64; }
 size_t copy_bytes(int64_t rows, int64_t D) { return static_cast<size_t>(rows) * static_cast<size_t>(copy_ld(D)) * 2; }
 
-// Values alone of few rows need no tensor cores, and no copies of operands either.
-bool is_few(int64_t R, bool grads) { return R <= kFewRows && !grads; }
+// Logits of few rows need no tensor cores.  (Nor is fp32's own rounding then given away: with one row whose token is all but certain the
+// gradient is the small difference 1 - p.)
+bool is_few(int64_t R) { return R <= kFewRows; }
 int64_t few_blocks() { return static_cast<int64_t>(sm_count()) * 4; }
 
 Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int64_t R, int64_t V, int64_t D, bool stats, bool grads, bool bias)
@@ -1036,11 +1079,14 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
         return here;
     };
     l.rows = R, l.width = V;
-    if (is_few(R, grads)) {
+    if (is_few(R)) {
         l.partial = take(static_cast<size_t>(few_blocks()) * 3 * R * 4);
         l.token_logit = take(static_cast<size_t>(R) * 4);
-        l.total = at;
-        return l;
+        if (!grads) {
+            l.total = at;
+            return l;
+        }
+        stats = false;
     }
     l.hidden = take(tma_ok(hidden, ldh) ? 0 : copy_bytes(R, D));
     l.weight = take(tma_ok(weight, ldw) ? 0 : copy_bytes(V, D));
@@ -1048,7 +1094,9 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
         l.ld_piece = div_up(V, 64) * 64;
         const int64_t most = kLogitBytes / 2 / l.ld_piece;  // rows
         l.by_rows = stats && !bias && D >= kLeastWidth && (R <= most || most >= kLeastRows);
-        if (l.by_rows) {
+        if (is_few(R)) {
+            l.logits = take(static_cast<size_t>(R) * l.ld_piece * 4);
+        } else if (l.by_rows) {
             const int64_t pieces = R <= most ? 1 : div_up(R, most / kTile * kTile);
             if (pieces > 1) l.rows = div_up(div_up(R, pieces), kTile) * kTile;  // of one size
         } else {
@@ -1136,7 +1184,7 @@ template <class T> struct Head {
 
     float *floats(size_t at) const { return reinterpret_cast<float *>(ws + at); }
 
-    // The values of few rows.
+    // Logits of few rows, and what comes of their sums.
     template <int ROWS> int few(RowArgs rows)
     {
         ProductArgs a = base;
@@ -1145,9 +1193,17 @@ template <class T> struct Head {
         const unsigned blocks = static_cast<unsigned>(want < most ? want : most);
         const T *x = static_cast<const T *>(h.hidden), *w = static_cast<const T *>(h.weight);
         const bool wide = tma_ok(x, h.ldh) && tma_ok(w, h.ldw) && h.D % 8 == 0;
-        HEAD_TRY(follow(wide ? few_kernel<T, ROWS, true> : few_kernel<T, ROWS, false>, dim3(blocks), kFewThreads, 0, 1, s, x, h.ldh, w, h.ldw, h.R, h.V, h.D, a));
+        float *logits = h.grads ? floats(l.logits) : nullptr;
+        HEAD_TRY(follow(wide ? few_kernel<T, ROWS, true> : few_kernel<T, ROWS, false>, dim3(blocks), kFewThreads, 0, 1, s, x, h.ldh, w, h.ldw, h.R, h.V, h.D, logits, l.ld_piece, a));
+        if (!h.stats) return follow(saved_rows_kernel, dim3(1), 256, 0, 1, s, rows);
         rows.partial = a.partial, rows.token_logit = a.token_logit, rows.tiles = static_cast<int>(blocks);
         return follow(few_rows_kernel, dim3(static_cast<unsigned>(h.R)), 256, 0, 1, s, rows);
+    }
+    int few_gradient()
+    {
+        const dim3 grid(static_cast<unsigned>(div_up(h.V, 2048)));
+        return follow(h.grad_entropy ? few_grad_kernel<T, true> : few_grad_kernel<T, false>, grid, 256, 0, 1, s, floats(l.logits), h.R, h.V, l.ld_piece, base.consts, base.c,
+                      base.scale_bits, reinterpret_cast<T *>(ws + l.piece), h.dbias);
     }
 
     // Sums of rows' exponentials and what comes of them; KIND kLogits keeps the logits.
@@ -1222,14 +1278,14 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
     const Layout l = lay_out(h.hidden, h.ldh, h.weight, h.ldw, h.R, h.V, h.D, h.stats, h.grads, h.dbias != nullptr);
     char *ws = static_cast<char *>(workspace);
     const int64_t R = h.R, V = h.V, D = h.D;
-    const bool few = is_few(R, h.grads);
+    const bool few = is_few(R);
     Repack p = {};
     p.K = D, p.ldto = copy_ld(D);
-    if (!few && !tma_ok(h.hidden, h.ldh)) {
+    if ((h.grads || !few) && !tma_ok(h.hidden, h.ldh)) {
         p.from[0] = static_cast<const uint16_t *>(h.hidden), p.ld[0] = h.ldh, p.rows[0] = R, p.to[0] = reinterpret_cast<uint16_t *>(ws + l.hidden);
         h.hidden = ws + l.hidden, h.ldh = p.ldto;
     }
-    if (!few && !tma_ok(h.weight, h.ldw)) {
+    if ((h.grads || !few) && !tma_ok(h.weight, h.ldw)) {
         p.from[1] = static_cast<const uint16_t *>(h.weight), p.ld[1] = h.ldw, p.rows[1] = V, p.to[1] = reinterpret_cast<uint16_t *>(ws + l.weight);
         h.weight = ws + l.weight, h.ldw = p.ldto;
     }
@@ -1251,7 +1307,7 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
     rows.grad_logprob = h.grad_logprob, rows.grad_entropy = h.grad_entropy;
     ProductArgs base = {};
     base.bias = h.bias, base.bias_type = h.bias_type, base.tokens = h.tokens, base.index_bits = h.index_bits;
-    base.c = rows.c, base.padded_rows = l.padded_rows;
+    base.c = rows.c, base.loss = kLoss * static_cast<float>(D), base.padded_rows = l.padded_rows;
     if (h.grads) {
         rows.consts = reinterpret_cast<float *>(ws + l.consts);
         if (h.dtype == SPDY_F16) {
@@ -1264,12 +1320,17 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
         base.consts = rows.consts;
     }
     Head<T> g = {h, l, ws, s, base, hidden, weight, {}, {}};
-    if (few) return R == 1 ? g.template few<1>(rows) : R == 2 ? g.template few<2>(rows) : g.template few<4>(rows);
+    if (few) HEAD_TRY(R == 1 ? g.template few<1>(rows) : R == 2 ? g.template few<2>(rows) : g.template few<4>(rows));
+    if (!h.grads && few) return SPDY_OK;
     if (h.grads) {
         HEAD_TRY(map_of(&g.hidden_columns, h.hidden, h.ldh, R, D, h.dtype, BK));
         HEAD_TRY(map_of(&g.weight_columns, h.weight, h.ldw, V, D, h.dtype, BK));
     }
-    if (h.grads && l.by_rows) {
+    if (few) {
+        HEAD_TRY(g.few_gradient());
+        HEAD_TRY(g.products(R, 0, V, 0));
+        if (h.dhidden) HEAD_TRY(g.finish_hidden(R, 0));
+    } else if (h.grads && l.by_rows) {
         for (int64_t r0 = 0; r0 < R; r0 += l.rows) {
             const int64_t n = R - r0 < l.rows ? R - r0 : l.rows;
             RowArgs some = rows;
