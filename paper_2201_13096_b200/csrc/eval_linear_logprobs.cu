@@ -803,7 +803,8 @@ __global__ void __launch_bounds__(256) saved_rows_kernel(const RowArgs a)
 
 // ---------------------------------------------------------------------------------------------- few rows
 // Logits of up to 4 rows: weight is streamed once by plain multiply-adds, four ids to a warp at a time, hidden comes from L1.  A block
-// leaves one set of sums, as a tile does.  Bound by weight's bytes: TIMES
+// leaves one set of sums, as a tile does.  Bound by weight's bytes: 1 x 32768 x 768 12 us (the tensor cores 18), 1 x 131072 x 4096 186 (5.8 TB/s), 4 rows 217
+// (212: from there on the tensor cores)
 constexpr int kFewRows = 4, kFewIds = 4, kFewThreads = 256;
 template <class T, int ROWS, bool WIDE>
 __global__ void __launch_bounds__(kFewThreads) few_kernel(const T *hidden, int64_t ldh, const T *weight, int64_t ldw, int64_t R, int64_t V, int64_t D, float *logits,
@@ -891,33 +892,118 @@ __global__ void __launch_bounds__(kFewThreads) few_kernel(const T *hidden, int64
     to[0] = all.m, to[gridDim.x] = all.s, to[2 * gridDim.x] = all.t;
 }
 
-// The gradient by few rows' logits, which are kept in fp32, and dbias; eight columns to a thread.
-template <class T, bool ENT>
-__global__ void __launch_bounds__(256) few_grad_kernel(const float *logits, int64_t R, int64_t N, int64_t ld, const float *consts, float c, const uint32_t *scale_bits, T *out,
-                                                       float *dbias)
+// The gradient by few rows' logits, in their place and in fp32 like them, and dbias; four columns to a thread.
+template <bool ENT>
+__global__ void __launch_bounds__(256) few_grad_kernel(float *logits, int64_t R, int64_t N, int64_t ld, const float *consts, float c, float *dbias)
 {
     wait_for_previous();
-    const int64_t n = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+    const int64_t n = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
     if (n >= N) return;
-    const int power = scale_power(scale_bits);
-    float sum[8] = {};
+    float sum[4] = {};
     for (int64_t r = 0; r < R; ++r) {
-        const RowConsts k = row_consts(consts, r, power_of_two(power));
-        uint4 lo, hi;
-        float f[8];
-        load32(logits + r * ld + n, lo, hi);  // ld is a multiple of 64
-        Elem<float>::unpack(lo, f), Elem<float>::unpack(hi, f + 4);
-        const int64_t at = k.token - n;
+        const RowConsts k = row_consts(consts, r, 1.f);
+        float4 *at = reinterpret_cast<float4 *>(logits + r * ld + n);  // ld is a multiple of 64
+        float f[4] = {at->x, at->y, at->z, at->w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < 4; ++j) {
             f[j] = grad_at<ENT>(fmaf(f[j] - k.ref, c, -k.ls), k);
-            if (at == j) f[j] += k.hit;
+            if (k.token == n + j) f[j] += k.hit;
             sum[j] += f[j];
         }
-        *reinterpret_cast<uint4 *>(out + r * ld + n) = Elem<T>::pack(f);
+        *at = make_float4(f[0], f[1], f[2], f[3]);
     }
     if (dbias)
-        for (int j = 0; j < 8 && n + j < N; ++j) dbias[n + j] = sum[j] * power_of_two(-power);
+        for (int j = 0; j < 4 && n + j < N; ++j) dbias[n + j] = sum[j];
+}
+
+// dweight of few rows, and a block's share of dhidden, from the gradient in fp32 by plain multiply-adds: a block goes down a run of ids, a thread keeps
+// PER columns (8, where all rows start on 16 bytes).  weight is read and dweight written once.
+// Values and gradients, whole calls: 1 x 131072 x 4096 599 us (the tensor cores 796), 4 rows 628 (822); 4 x 32768 x 768 54 (67).
+constexpr int kFewRun = 64;  // ids whose gradients lie in shared memory
+template <class T, int ROWS, int PER>
+__global__ void __launch_bounds__(256) few_products_kernel(const float *grad, int64_t ld, const T *hidden, int64_t ldh, const T *weight, int64_t ldw, int64_t R, int64_t V, int64_t D,
+                                                           int64_t run, T *dweight, int64_t lddw, float *parts)
+{
+    __shared__ float g[ROWS][kFewRun];
+    wait_for_previous();
+    const int64_t d = (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x) * PER, first = blockIdx.x * run, end = min(first + run, V);
+    const bool mine = d < D;
+    float acc[ROWS][PER], h[ROWS][PER];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) acc[r][i] = h[r][i] = 0.f;
+        if (mine && r < R) {
+            if constexpr (PER == 8) Elem<T>::unpack(*reinterpret_cast<const uint4 *>(hidden + r * ldh + d), h[r]);
+            else h[r][0] = Elem<T>::to_float(hidden[r * ldh + d]);
+        }
+    }
+    for (int64_t v0 = first; v0 < end; v0 += kFewRun) {
+        const int count = static_cast<int>(min(end - v0, static_cast<int64_t>(kFewRun)));
+        __syncthreads();
+        for (int i = threadIdx.x; i < ROWS * kFewRun; i += blockDim.x) {
+            const int r = i / kFewRun, v = i % kFewRun;
+            g[r][v] = r < R && v < count ? grad[r * ld + v0 + v] : 0.f;
+        }
+        __syncthreads();
+        if (!mine) continue;
+        constexpr int U = 8;  // ids whose rows are on their way together (4 rows: 690 us with 4 of them, 628 with 8)
+        for (int base = 0; base < count; base += U) {
+            uint4 raw[U];
+            float single[U];
+            if (parts)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int64_t v = v0 + min(base + u, count - 1);
+                    if constexpr (PER == 8) raw[u] = load_last(weight + v * ldw + d);
+                    else single[u] = Elem<T>::to_float(weight[v * ldw + d]);
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int v = base + u;
+                if (v >= count) break;
+                float w[PER], out[PER];
+                if constexpr (PER == 8) Elem<T>::unpack(raw[u], w);
+                else w[0] = single[u];
+#pragma unroll
+                for (int i = 0; i < PER; ++i) out[i] = 0.f;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        if (parts) acc[r][i] = fmaf(g[r][v], w[i], acc[r][i]);
+                        out[i] = fmaf(g[r][v], h[r][i], out[i]);
+                    }
+                if (dweight) {
+                    T *to = dweight + (v0 + v) * lddw + d;
+                    if constexpr (PER == 8) store_last(to, Elem<T>::pack(out));
+                    else *to = Elem<T>::from_float(out[0]);
+                }
+            }
+        }
+    }
+    if (!parts || !mine) return;
+    for (int r = 0; r < ROWS && r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < PER; ++i) parts[(static_cast<int64_t>(blockIdx.x) * R + r) * D + d + i] = acc[r][i];
+}
+
+// dhidden of few rows: the blocks' shares in a fixed order, eight runs of them to a column.
+template <class T> __global__ void __launch_bounds__(256) few_finish_kernel(const float *parts, int blocks, int64_t R, int64_t D, T *dhidden, int64_t lddh)
+{
+    __shared__ float room[8][32];
+    wait_for_previous();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t d = static_cast<int64_t>(blockIdx.x) * 32 + lane, r = blockIdx.y;
+    float sum = 0.f;
+    if (d < D)
+#pragma unroll 8
+        for (int b = warp; b < blocks; b += 8) sum += parts[(b * R + r) * D + d];
+    room[warp][lane] = sum;
+    __syncthreads();
+    if (warp > 0 || d >= D) return;
+    for (int w = 1; w < 8; ++w) sum += room[w][lane];
+    dhidden[r * lddh + d] = Elem<T>::from_float(sum);
 }
 
 // ---------------------------------------------------------------------------------------------- gradient by kept logits
@@ -1064,8 +1150,8 @@ int choose_splits(int64_t M, int64_t N, int64_t k_blocks)
 int64_t copy_ld(int64_t D) { return div_up(D, 64) * 64; }
 size_t copy_bytes(int64_t rows, int64_t D) { return static_cast<size_t>(rows) * static_cast<size_t>(copy_ld(D)) * 2; }
 
-// Logits of few rows need no tensor cores.  (Nor is fp32's own rounding then given away: with one row whose token is all but certain the
-// gradient is the small difference 1 - p.)
+// Few rows need no tensor cores.  (Nor are fp32's digits then given away: with one row whose token is all but certain the gradient is the
+// small difference 1 - p.)
 bool is_few(int64_t R) { return R <= kFewRows; }
 int64_t few_blocks() { return static_cast<int64_t>(sm_count()) * 4; }
 
@@ -1082,11 +1168,14 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
     if (is_few(R)) {
         l.partial = take(static_cast<size_t>(few_blocks()) * 3 * R * 4);
         l.token_logit = take(static_cast<size_t>(R) * 4);
-        if (!grads) {
-            l.total = at;
-            return l;
+        if (grads) {
+            l.ld_piece = div_up(V, 64) * 64;
+            l.consts = take(static_cast<size_t>(R) * kConsts * 4);
+            l.logits = take(static_cast<size_t>(R) * l.ld_piece * 4);
+            l.parts = take(static_cast<size_t>(few_blocks()) * R * D * 4);
         }
-        stats = false;
+        l.total = at;
+        return l;
     }
     l.hidden = take(tma_ok(hidden, ldh) ? 0 : copy_bytes(R, D));
     l.weight = take(tma_ok(weight, ldw) ? 0 : copy_bytes(V, D));
@@ -1094,9 +1183,7 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
         l.ld_piece = div_up(V, 64) * 64;
         const int64_t most = kLogitBytes / 2 / l.ld_piece;  // rows
         l.by_rows = stats && !bias && D >= kLeastWidth && (R <= most || most >= kLeastRows);
-        if (is_few(R)) {
-            l.logits = take(static_cast<size_t>(R) * l.ld_piece * 4);
-        } else if (l.by_rows) {
+        if (l.by_rows) {
             const int64_t pieces = R <= most ? 1 : div_up(R, most / kTile * kTile);
             if (pieces > 1) l.rows = div_up(div_up(R, pieces), kTile) * kTile;  // of one size
         } else {
@@ -1184,7 +1271,7 @@ template <class T> struct Head {
 
     float *floats(size_t at) const { return reinterpret_cast<float *>(ws + at); }
 
-    // Logits of few rows, and what comes of their sums.
+    // All of few rows.
     template <int ROWS> int few(RowArgs rows)
     {
         ProductArgs a = base;
@@ -1195,15 +1282,28 @@ template <class T> struct Head {
         const bool wide = tma_ok(x, h.ldh) && tma_ok(w, h.ldw) && h.D % 8 == 0;
         float *logits = h.grads ? floats(l.logits) : nullptr;
         HEAD_TRY(follow(wide ? few_kernel<T, ROWS, true> : few_kernel<T, ROWS, false>, dim3(blocks), kFewThreads, 0, 1, s, x, h.ldh, w, h.ldw, h.R, h.V, h.D, logits, l.ld_piece, a));
-        if (!h.stats) return follow(saved_rows_kernel, dim3(1), 256, 0, 1, s, rows);
-        rows.partial = a.partial, rows.token_logit = a.token_logit, rows.tiles = static_cast<int>(blocks);
-        return follow(few_rows_kernel, dim3(static_cast<unsigned>(h.R)), 256, 0, 1, s, rows);
-    }
-    int few_gradient()
-    {
-        const dim3 grid(static_cast<unsigned>(div_up(h.V, 2048)));
-        return follow(h.grad_entropy ? few_grad_kernel<T, true> : few_grad_kernel<T, false>, grid, 256, 0, 1, s, floats(l.logits), h.R, h.V, l.ld_piece, base.consts, base.c,
-                      base.scale_bits, reinterpret_cast<T *>(ws + l.piece), h.dbias);
+        if (h.stats) {
+            rows.partial = a.partial, rows.token_logit = a.token_logit, rows.tiles = static_cast<int>(blocks);
+            HEAD_TRY(follow(few_rows_kernel, dim3(static_cast<unsigned>(h.R)), 256, 0, 1, s, rows));
+        } else {
+            HEAD_TRY(follow(saved_rows_kernel, dim3(1), 256, 0, 1, s, rows));
+        }
+        if (!h.grads) return SPDY_OK;
+        HEAD_TRY(follow(h.grad_entropy ? few_grad_kernel<true> : few_grad_kernel<false>, dim3(static_cast<unsigned>(div_up(h.V, 1024))), 256, 0, 1, s, logits, h.R, h.V, l.ld_piece,
+                        base.consts, base.c, h.dbias));
+        if (!h.dhidden && !h.dweight) return SPDY_OK;
+        T *dweight = static_cast<T *>(h.dweight);
+        const bool wide_too = wide && (!dweight || tma_ok(dweight, h.lddw));
+        const int64_t columns = div_up(h.D, wide_too ? 8 : 1), threads = columns < 256 ? div_up(columns, 32) * 32 : 256, across = div_up(columns, threads);
+        const int64_t down = most / across > 1 ? most / across : 1, run = div_up(div_up(h.V, down), 8) * 8;
+        const unsigned runs = static_cast<unsigned>(div_up(h.V, run));
+        if (across > 65535) return SPDY_ERR_UNSUPPORTED;
+        float *parts = h.dhidden ? floats(l.parts) : nullptr;
+        HEAD_TRY(follow(wide_too ? few_products_kernel<T, ROWS, 8> : few_products_kernel<T, ROWS, 1>, dim3(runs, static_cast<unsigned>(across)), static_cast<int>(threads), 0, 1, s,
+                        logits, l.ld_piece, x, h.ldh, w, h.ldw, h.R, h.V, h.D, run, dweight, h.lddw, parts));
+        if (!h.dhidden) return SPDY_OK;
+        return follow(few_finish_kernel<T>, dim3(static_cast<unsigned>(div_up(h.D, 32)), static_cast<unsigned>(h.R)), 256, 0, 1, s, parts, static_cast<int>(runs), h.R, h.D,
+                      static_cast<T *>(h.dhidden), h.lddh);
     }
 
     // Sums of rows' exponentials and what comes of them; KIND kLogits keeps the logits.
@@ -1281,11 +1381,11 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
     const bool few = is_few(R);
     Repack p = {};
     p.K = D, p.ldto = copy_ld(D);
-    if ((h.grads || !few) && !tma_ok(h.hidden, h.ldh)) {
+    if (!few && !tma_ok(h.hidden, h.ldh)) {
         p.from[0] = static_cast<const uint16_t *>(h.hidden), p.ld[0] = h.ldh, p.rows[0] = R, p.to[0] = reinterpret_cast<uint16_t *>(ws + l.hidden);
         h.hidden = ws + l.hidden, h.ldh = p.ldto;
     }
-    if ((h.grads || !few) && !tma_ok(h.weight, h.ldw)) {
+    if (!few && !tma_ok(h.weight, h.ldw)) {
         p.from[1] = static_cast<const uint16_t *>(h.weight), p.ld[1] = h.ldw, p.rows[1] = V, p.to[1] = reinterpret_cast<uint16_t *>(ws + l.weight);
         h.weight = ws + l.weight, h.ldw = p.ldto;
     }
@@ -1310,7 +1410,7 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
     base.c = rows.c, base.loss = kLoss * static_cast<float>(D), base.padded_rows = l.padded_rows;
     if (h.grads) {
         rows.consts = reinterpret_cast<float *>(ws + l.consts);
-        if (h.dtype == SPDY_F16) {
+        if (!few && h.dtype == SPDY_F16) {
             uint32_t *bits = reinterpret_cast<uint32_t *>(ws + l.scale);
             SPDY_EVAL_TRY(cudaMemsetAsync(bits, 0, 4, s));
             const int64_t blocks = div_up(R, 256), most = sm_count();
@@ -1320,17 +1420,12 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
         base.consts = rows.consts;
     }
     Head<T> g = {h, l, ws, s, base, hidden, weight, {}, {}};
-    if (few) HEAD_TRY(R == 1 ? g.template few<1>(rows) : R == 2 ? g.template few<2>(rows) : g.template few<4>(rows));
-    if (!h.grads && few) return SPDY_OK;
+    if (few) return R == 1 ? g.template few<1>(rows) : R == 2 ? g.template few<2>(rows) : g.template few<4>(rows);
     if (h.grads) {
         HEAD_TRY(map_of(&g.hidden_columns, h.hidden, h.ldh, R, D, h.dtype, BK));
         HEAD_TRY(map_of(&g.weight_columns, h.weight, h.ldw, V, D, h.dtype, BK));
     }
-    if (few) {
-        HEAD_TRY(g.few_gradient());
-        HEAD_TRY(g.products(R, 0, V, 0));
-        if (h.dhidden) HEAD_TRY(g.finish_hidden(R, 0));
-    } else if (h.grads && l.by_rows) {
+    if (h.grads && l.by_rows) {
         for (int64_t r0 = 0; r0 < R; r0 += l.rows) {
             const int64_t n = R - r0 < l.rows ? R - r0 : l.rows;
             RowArgs some = rows;
