@@ -5,8 +5,9 @@
  * SPDY's search (Section 3.3, Algorithm 4) asks its caller for the calibration loss of the model stitched together
  * for a profile (Section 3.4); the pruned model is then tuned against the dense one.  The operators here carry that
  * work on the device: linear layers with their epilogue, layer normalisation with its gradients, log probabilities
- * of given tokens with entropy and top alternatives, and the distillation loss against the dense model's top log
- * probabilities with its gradient.  spdy_linear has no backward call: its input's gradient is the product with the transposed
+ * of given tokens with entropy and top alternatives, from logits or straight from an output layer's input and weight with the
+ * gradients by both, the distillation loss against the dense model's top log probabilities with its gradient, and AdamW steps.
+ * spdy_linear has no backward call: its input's gradient is the product with the transposed
  * weight, its weight's gradient is left to the caller.
  *
  * Common rules
@@ -16,8 +17,8 @@
  *   - Matrices are row-major with unit column stride; ld... is the row stride in elements and at least the row
  *     length.  Pointers need the alignment of their element type only; wide accesses are used where the addresses
  *     allow.  Outputs may not overlap inputs except where a function says so.
- *   - Sums, statistics and gradients of parameters are held in fp32; 16-bit outputs are rounded once.  No atomics on
- *     floating-point data: the same call on the same data gives the same bits.
+ *   - Sums, statistics and gradients of parameters are held in fp32; 16-bit outputs (an output layer's dweight among them) are
+ *     rounded once.  No atomics on floating-point data: the same call on the same data gives the same bits.
  *   - Rows may be zero in number, and spdy_linear's columns: the call is a no-op (parameter gradients of no rows are written as
  *     0).  Rows of no columns (D = 0, V = 0) have no mean and no distribution: SPDY_ERR_INVALID_ARG.
  *   - At most 2^31 - 1 blocks per launch: rows beyond that number (times up to 8 for long rows) are SPDY_ERR_UNSUPPORTED.

@@ -58,19 +58,11 @@ template <int KIND> struct Order {
     static constexpr bool kA = KIND == kWeight || KIND == kWeightParts, kB = kA || KIND == kHidden;
 };
 
-// Division of 32-bit numbers by one that the host knows: the upper half of x ceil(2^64 / d), exact for every x.  (The tiles' and shares'
-// places took 300 instructions a tile and warp with the compiler's divisions, as many as carrying the tile on.)
-struct Divisor {
-    uint64_t m;
-    uint32_t d;
-    Divisor(uint32_t by = 1) : m(by > 1 ? ~0ull / by + 1 : 0), d(by) {}
-    __device__ __forceinline__ uint32_t of(uint32_t x) const { return d == 1 ? x : static_cast<uint32_t>(__umul64hi(x, m)); }
-};
-
 struct ProductArgs {
     int64_t M, N;                  // rows and columns of the result that exist
-    int tiles_m, tiles_n, splits, group, k_blocks;
-    Divisor tiles, per_group, per_rows, per_last, per_split;  // tiles; of a group; down in a group, in the last one; splits
+    Tiles tiles;                   // of the result
+    int splits, k_blocks;          // shares of the summed index, its stages
+    Divisor per_split;
     int a_row0, b_row0;            // first rows of the operands
     // kStats, kGrad
     const void *bias, *tokens;
@@ -138,18 +130,6 @@ __device__ __forceinline__ void join(Sums &a, Sums b, float c)
 __device__ __forceinline__ uint64_t operand_by_columns(uint32_t addr)
 {
     return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | 512ull << 16 | 64ull << 32 | 1ull << 46 | 2ull << 61;
-}
-
-// The tile of an item: groups of `group` tiles down, all tiles across before the next group.
-__device__ __forceinline__ void tile_of(const ProductArgs &a, int item, int &split, int &tm, int &tn)
-{
-    const uint32_t x = static_cast<uint32_t>(item);
-    split = static_cast<int>(a.tiles.of(x));
-    const uint32_t tile = x - static_cast<uint32_t>(split) * a.tiles.d, g = a.per_group.of(tile), rest = tile - g * a.per_group.d;
-    const bool last = static_cast<int>((g + 1) * a.per_rows.d) > a.tiles_m;
-    const uint32_t across = last ? a.per_last.of(rest) : a.per_rows.of(rest);
-    tn = static_cast<int>(across);
-    tm = static_cast<int>(g * a.per_rows.d + rest - across * (last ? a.per_last.d : a.per_rows.d));
 }
 
 struct Control {
@@ -481,7 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     cg::cluster_group cluster = cg::this_cluster();
     const int part = static_cast<int>(cluster.block_rank());
-    const int items = a.tiles_m * a.tiles_n * a.splits, first = static_cast<int>(blockIdx.x) / 2, step = static_cast<int>(gridDim.x) / 2;
+    const int items = static_cast<int>(a.tiles.count()) * a.splits, first = static_cast<int>(blockIdx.x) / 2, step = static_cast<int>(gridDim.x) / 2;
     constexpr bool kColumnsA = Order<KIND>::kA, kColumnsB = Order<KIND>::kB;
 
     if (threadIdx.x == 0) {
@@ -501,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     const auto range = [&](int split, int &kb0, int &kb1) {
         kb0 = 0, kb1 = a.k_blocks;
         if (KIND == kHidden || KIND == kWeightParts)  // below 2^24 stages, up to 64 shares
-            kb0 = static_cast<int>(a.per_split.of(static_cast<uint32_t>(a.k_blocks * split))), kb1 = static_cast<int>(a.per_split.of(static_cast<uint32_t>(a.k_blocks * (split + 1))));
+            kb0 = static_cast<int>(a.per_split.of(static_cast<uint32_t>(a.k_blocks) * split)), kb1 = static_cast<int>(a.per_split.of(static_cast<uint32_t>(a.k_blocks) * (split + 1)));
     };
 
     if (warp == 0) {
@@ -510,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         bool ok = true;
         for (int item = first; item < items && ok; item += step) {
             int split, tm, tn, kb0, kb1;
-            tile_of(a, item, split, tm, tn);
+            a.tiles.at(static_cast<uint32_t>(item), split, tm, tn);
             range(split, kb0, kb1);
             const int m0 = tm * kTile + part * BM, n0 = tn * kTile + part * BM;
             if (kb0 == kb1) continue;  // a share of the last, shorter piece may be empty: nothing to add
@@ -552,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             bool ok = true;
             for (int item = first; item < items && ok; item += step) {
                 int split, tm, tn, kb0, kb1;
-                tile_of(a, item, split, tm, tn);
+                a.tiles.at(static_cast<uint32_t>(item), split, tm, tn);
                 range(split, kb0, kb1);
                 if (kb0 == kb1) continue;
                 ok = __all_sync(0xffffffffu, barrier_wait(&ctl.acc_empty[acc], acc_parity ^ 1));
@@ -594,7 +574,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         bool ok = true;
         for (int item = first; item < items; item += step) {
             int split, tm, tn, kb0, kb1;
-            tile_of(a, item, split, tm, tn);
+            a.tiles.at(static_cast<uint32_t>(item), split, tm, tn);
             range(split, kb0, kb1);
             if (kb0 == kb1) continue;
             const int64_t m0 = static_cast<int64_t>(tm) * kTile + part * BM + quarter * 32, n0 = static_cast<int64_t>(tn) * kTile + group * kWarpColumns;
@@ -1234,14 +1214,9 @@ template <class T, int KIND, bool ENT> int launch_product(const CUtensorMap &ma,
 {
     const int64_t tm = div_up(a.M, kTile), tn = div_up(a.N, kTile);
     if (tm * tn * splits > 0x3fffffff) return SPDY_ERR_UNSUPPORTED;
-    a.tiles_m = static_cast<int>(tm), a.tiles_n = static_cast<int>(tn), a.splits = splits;
-    a.group = group < a.tiles_m ? group : a.tiles_m;
+    a.tiles = Tiles(static_cast<int>(tm), static_cast<int>(tn), group), a.splits = splits, a.per_split = Divisor(static_cast<uint32_t>(splits));
     a.k_blocks = static_cast<int>(div_up(K, kStageK));
-    if (static_cast<int64_t>(a.group) * a.tiles_n > 0x3fffffff) return SPDY_ERR_UNSUPPORTED;
-    a.tiles = Divisor(static_cast<uint32_t>(a.tiles_m * a.tiles_n)), a.per_group = Divisor(static_cast<uint32_t>(a.group * a.tiles_n));
-    a.per_rows = Divisor(static_cast<uint32_t>(a.group)), a.per_last = Divisor(static_cast<uint32_t>(a.tiles_m % a.group ? a.tiles_m % a.group : a.group));
-    a.per_split = Divisor(static_cast<uint32_t>(splits));
-    const int items = a.tiles_m * a.tiles_n * splits, pairs = sm_count() / 2;
+    const int items = static_cast<int>(tm * tn) * splits, pairs = sm_count() / 2;
     auto *kernel = product_kernel<T, KIND, ENT>;
     SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<KIND>()));
     return follow(kernel, dim3(static_cast<unsigned>((items < pairs ? items : pairs) * 2)), kThreads, smem_bytes<KIND>(), 2, s, ma, mb, a);

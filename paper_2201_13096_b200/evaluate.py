@@ -2,14 +2,15 @@
 
 SPDY's search asks its caller for the calibration loss of a stitched model (Section 3.4), and the pruned model is tuned
 against the dense one afterwards.  ``linear`` and ``layer_norm`` carry a block of such a model, ``token_logprobs`` scores it
-(and takes the dense model's most probable tokens), ``distill_loss`` compares it with them; the ``..._backward`` and
-``..._with_grad`` calls give the gradients of the losses and of ``layer_norm`` (``linear`` has no backward call: its input's
-gradient is ``linear`` with the weight transposed, its weight's is not here).
+(and takes the dense model's most probable tokens), ``distill_loss`` compares it with them; ``linear_token_logprobs`` scores
+an output layer without a table of logits.  The ``..._backward`` and ``..._with_grad`` calls give the gradients of the losses,
+of ``layer_norm`` and of that output layer (``linear`` has no backward call: its input's gradient is ``linear`` with the weight
+transposed, its weight's is not here), and ``adamw_step`` applies gradients to any number of tensors.
 
 Every call runs in the CUDA library on ``stream`` (default: torch's current stream of the tensors' device); PyTorch supplies
 memory and streams.  Matrices are 2-D CUDA tensors with unit column stride and any row stride.  There is no CPU fallback.
 Nothing is recorded for autograd: with gradients enabled, tensors that require one are refused (detach them, and take the
-gradient from the ``..._backward`` and ``..._with_grad`` calls).
+gradient from the ``..._backward`` and ``..._with_grad`` calls; ``AdamW`` takes leaves, and changes them in place).
 """
 from __future__ import annotations
 
