@@ -1103,9 +1103,12 @@ constexpr int64_t kPieceBytes = 256ll << 20, kLeastPiece = 2048;
 // written for each.
 constexpr int64_t kLogitBytes = 512ll << 20, kLeastRows = 2048, kLeastWidth = 512;
 
+// Sums of a row's tiles, 12 bytes each, for as many rows at a time as this much memory holds, 4096 at least.
+constexpr int64_t kPartialBytes = 32ll << 20, kLeastStats = 4096;
+
 struct Layout {
     size_t hidden, weight, partial, token_logit, consts, scale, logits, tops, piece, parts, weight_sums, sums, total;
-    int64_t padded_rows, rows, width, ld_piece, ld_parts;  // rows, width: what is worked on at a time
+    int64_t padded_rows, rows, stat_rows, width, ld_piece, ld_parts;  // rows, width: what is worked on at a time; stat_rows: for values
     int hidden_splits, weight_splits;
     bool by_rows;
 };
@@ -1185,10 +1188,15 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
         if (!once || l.weight_splits > 1) l.weight_sums = take(static_cast<size_t>(l.weight_splits) * l.width * l.ld_parts * 4);
         if (bias) l.sums = take(static_cast<size_t>(div_up(R, 32)) * l.ld_piece * 4);
     }
-    l.padded_rows = div_up(l.rows, 32) * 32;
+    l.stat_rows = l.rows;
     if (stats) {
+        if (!l.by_rows) {
+            const int64_t most = kPartialBytes / 12 / div_up(V, kTile) / kTile * kTile, rows = most > kLeastStats ? most : kLeastStats;
+            if (rows < R) l.stat_rows = div_up(div_up(R, div_up(R, rows)), kTile) * kTile;  // of one size
+        }
+        l.padded_rows = div_up(l.stat_rows, 32) * 32;
         l.partial = take(static_cast<size_t>(div_up(V, kTile)) * 3 * l.padded_rows * 4);
-        l.token_logit = take(static_cast<size_t>(l.rows) * 4);
+        l.token_logit = take(static_cast<size_t>(l.stat_rows) * 4);
     }
     l.total = at;
     return l;
@@ -1400,23 +1408,29 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
         HEAD_TRY(map_of(&g.hidden_columns, h.hidden, h.ldh, R, D, h.dtype, BK));
         HEAD_TRY(map_of(&g.weight_columns, h.weight, h.ldw, V, D, h.dtype, BK));
     }
+    const auto part = [&](int64_t r0, int64_t n) {  // the same of rows r0 .. r0 + n - 1
+        RowArgs some = rows;
+        some.R = n;
+        if (some.tokens) some.tokens = static_cast<const char *>(rows.tokens) + r0 * static_cast<int64_t>(h.index_bits / 8);
+        for (float **p : {&some.logprob, &some.entropy, &some.lse}) *p = *p ? *p + r0 : nullptr;
+        for (const float **p : {&some.grad_logprob, &some.grad_entropy}) *p = *p ? *p + r0 : nullptr;
+        return some;
+    };
     if (h.grads && l.by_rows) {
         for (int64_t r0 = 0; r0 < R; r0 += l.rows) {
             const int64_t n = R - r0 < l.rows ? R - r0 : l.rows;
-            RowArgs some = rows;
-            some.R = n;
-            const size_t token_bytes = static_cast<size_t>(h.index_bits / 8);
-            if (some.tokens) some.tokens = static_cast<const char *>(rows.tokens) + r0 * token_bytes;
-            for (float **p : {&some.logprob, &some.entropy, &some.lse}) *p = *p ? *p + r0 : nullptr;
-            for (const float **p : {&some.grad_logprob, &some.grad_entropy}) *p = *p ? *p + r0 : nullptr;
-            HEAD_TRY(g.template stats<kLogits>(some, r0));
+            HEAD_TRY(g.template stats<kLogits>(part(r0, n), r0));
             HEAD_TRY(g.gradient(n));
             HEAD_TRY(g.products(n, r0, V, 0));
             if (h.dhidden) HEAD_TRY(g.finish_hidden(n, r0));
         }
     } else {
         if (h.stats) {
-            HEAD_TRY(g.template stats<kStats>(rows, 0));
+            for (int64_t r0 = 0; r0 < R; r0 += l.stat_rows) {
+                RowArgs some = part(r0, R - r0 < l.stat_rows ? R - r0 : l.stat_rows);
+                if (some.consts) some.consts += r0 * kConsts;
+                HEAD_TRY(g.template stats<kStats>(some, r0));
+            }
         } else {
             HEAD_TRY(follow(saved_rows_kernel, dim3(static_cast<unsigned>(div_up(R, 256))), 256, 0, 1, s, rows));
         }
