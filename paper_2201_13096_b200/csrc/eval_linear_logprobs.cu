@@ -11,10 +11,9 @@
 //   kGrad    the logits once more -> the gradient by them, rounded to 16 bits
 //   kHidden  gradient x weight: fp32 sums of dhidden
 //   kWeight  gradient^T x hidden: dweight (kWeightParts: as fp32 sums)
-// Two plans keep what is of size rows x ids within a budget.  By ids (a backward call, whose sums are known, and where dbias is wanted,
-// whose fp32 the kept logits would not reach): the gradient of all rows for a piece of the vocabulary at a time, dhidden added up over
-// the pieces; the logits are multiplied again.  By rows (the rest of the calls that give values and gradients at once): the
-// logits of some rows and all ids at a time, dweight added up over them; each
+// Two plans keep what is of size rows x ids within a budget.  By ids (a backward call, whose sums are known, and narrow heads): the
+// gradient of all rows for a piece of the vocabulary at a time, dhidden added up over the pieces; the logits are multiplied again.
+// By rows (the rest of the calls that give values and gradients at once): the logits of some rows and all ids at a time, dweight added up over them; each
 // product is done once.  In the last two products one or both operands have the summed index as their rows ("MN-major"); TMA brings
 // them as boxes of 64 columns, and the matrix descriptors name that order, so nothing is transposed.
 #include "eval_tensor.cuh"
@@ -75,6 +74,7 @@ struct ProductArgs {
     const uint32_t *scale_bits;    // NULL, or the largest gradient's bits (half precision)
     float *column_sums;            // NULL, or [row groups of 32][N]
     int64_t ld_sums;
+    uint8_t *fine;                 // kLogits: NULL, or the codes' lower bits, [M][ldo]
     float *tops;                   // kLogits: [ids / 32][padded_rows], what a row's 32 codes are relative to
     void *out;                     // kLogits: codes; kGrad: the piece; kWeight: 16 bits; parts: fp32 [splits][M][ldo]
     int64_t ldo;
@@ -237,12 +237,15 @@ __device__ __forceinline__ Sums carry_stats(const ProductArgs &a, uint32_t tmem,
 // A kept logit: how far log2 of its exponential lies below that of the largest among 32 ids, in steps of 2^-10
 // octaves over 64 octaves for bf16, 2^-11 over 32 for half precision, whose own numbers end sooner.  p comes out within 2^-11 ln 2 =
 // 3.4e-4 of itself (1.7e-4), beside the 16-bit rounding that follows of 3.9e-3 (4.9e-4).  The last code is "nothing".
+// FINE, where dbias wants p to fp32's digits: another 7 bits, in bytes of their own.
 template <class T> constexpr float kSteps = std::is_same<T, __nv_bfloat16>::value ? 1024.f : 2048.f;
 constexpr uint32_t kNothing = 65535;
+template <class T, bool FINE> constexpr float kCodeSteps = kSteps<T> * (FINE ? 128.f : 1.f);
+template <bool FINE> constexpr float kLastCode = FINE ? 8388607.f : 65535.f;
 
 // As carry_stats, with the codes, and per 32 of them the largest, which they are relative to.
 constexpr int kCodes = 32;
-template <class T, class Ready, class Release>
+template <class T, bool FINE, class Ready, class Release>
 __device__ __forceinline__ Sums carry_logits(const ProductArgs &a, uint32_t tmem, int64_t m, int64_t n0, float *bias, Ready ready, Release release)
 {
     int64_t token = -1;
@@ -263,17 +266,24 @@ __device__ __forceinline__ Sums carry_logits(const ProductArgs &a, uint32_t tmem
         if (at >= 0 && at < kCodes && token < a.N) a.token_logit[m] = pick(f, at);
         const float top = largest(f, neg_inf());
         Sums here = {neg_inf(), 0.f, 0.f};
-        uint32_t w[kCodes / 2];
+        uint32_t w[kCodes / 2], low[FINE ? kCodes / 4 : 1];
         add_exponentials(f, top, a.c, here, [&](int i, float2 d) {
-            // 2^23 and a number below 2^16: rounded to a whole number, in the lower half of the pattern
-            constexpr float lowest = -static_cast<float>(kNothing) / kSteps<T>;
-            const float2 code = fma2(make_float2(fmaxf(d.x, lowest), fmaxf(d.y, lowest)), both(-kSteps<T>), both(8388608.f));
-            w[i / 2] = __byte_perm(__float_as_uint(code.x), __float_as_uint(code.y), 0x5410);
+            // 2^23 and a number below it: rounded to a whole number, in the lower part of the pattern
+            constexpr float lowest = -kLastCode<FINE> / kCodeSteps<T, FINE>;
+            const float2 code = fma2(make_float2(fmaxf(d.x, lowest), fmaxf(d.y, lowest)), both(-kCodeSteps<T, FINE>), both(8388608.f));
+            const uint32_t x = __float_as_uint(code.x), y = __float_as_uint(code.y);
+            w[i / 2] = FINE ? __byte_perm(x >> 7, y >> 7, 0x5410) : __byte_perm(x, y, 0x5410);
+            if (FINE) {
+                const uint32_t two = __byte_perm(x, y, 0x0040) & 0x7f7fu;
+                if (i % 4 == 0) low[i / 4] = two;
+                else low[i / 4] |= two << 16;
+            }
         });
         if (m < a.M && n0 + c < a.N) {  // ldo is a multiple of 64
             a.tops[(n0 + c) / kCodes * a.padded_rows + m] = top;
             store32(to + c, make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7]));
             store32(to + c + 16, make_uint4(w[8], w[9], w[10], w[11]), make_uint4(w[12], w[13], w[14], w[15]));
+            if constexpr (FINE) store32(a.fine + m * a.ldo + n0 + c, make_uint4(low[0], low[1], low[2], low[3]), make_uint4(low[4], low[5], low[6], low[7]));
         }
         join(sums, here, a.c);
     }
@@ -300,15 +310,17 @@ __device__ __forceinline__ float sum_columns(const float *f)
     return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 1);
 }
 
-// What the gradient by a row's logits needs: d = [v = token] hit - p (all + slope y), y = log2 p = (x - ref) c - ls.
+// What the gradient by a row's logits needs: d = [v = token] hit - p (all + slope y), y = log2 p = (x - ref) c - ls; `known` is d at the
+// token, from its logit in fp32: where the logits are kept in fewer bits, 1 - p of a token that is all but certain would be lost.
 struct RowConsts {
     float ref, ls, hit, all, slope;
     int token;
+    float known;
 };
 __device__ __forceinline__ RowConsts row_consts(const float *consts, int64_t m, float scale)
 {
     const float4 k = reinterpret_cast<const float4 *>(consts)[2 * m], more = reinterpret_cast<const float4 *>(consts)[2 * m + 1];
-    return {k.x, k.y, k.z * scale, k.w * scale, more.x * scale, __float_as_int(more.y)};
+    return {k.x, k.y, k.z * scale, k.w * scale, more.x * scale, __float_as_int(more.y), more.z * scale};
 }
 // -p (all + slope y).  ENT: with the entropy's gradient (slope is not 0); below -200 p is 0.
 template <bool ENT> __device__ __forceinline__ float grad_at(float y, const RowConsts &k)
@@ -324,7 +336,7 @@ __device__ __forceinline__ void carry_grad(const ProductArgs &a, uint32_t tmem, 
     const int lane = threadIdx.x & 31;
     const int64_t m = m0 + lane;
     const bool inside = m < a.M;
-    RowConsts k = {0.f, 0.f, 0.f, 0.f, 0.f, -1};
+    RowConsts k = {0.f, 0.f, 0.f, 0.f, 0.f, -1, 0.f};
     if (inside) k = row_consts(a.consts, m, power_of_two(scale_power(a.scale_bits)));
     stage_bias(a, n0, bias);
     const bool ok = ready();
@@ -451,6 +463,7 @@ constexpr int kBiasBytes = kEpilogueWarps * kWarpColumns * 4, kTurnBytes = kEpil
 template <int KIND> constexpr int extra_bytes() { return KIND == kStats || KIND == kLogits ? kBiasBytes + kJoinBytes : KIND == kGrad ? kBiasBytes : KIND == kWeight ? kTurnBytes : 0; }
 template <int KIND> constexpr int smem_bytes() { return 1024 + kStages * kStageBytes + extra_bytes<KIND>(); }
 
+// ENT: kGrad with the entropy's gradient; kLogits with the codes' lower bits.
 template <class T, int KIND, bool ENT>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ ProductArgs a)
 {
@@ -591,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             const uint32_t at = tmem + acc * kTile + group * kWarpColumns + (static_cast<uint32_t>(quarter * 32) << 16);
             if (KIND == kStats || KIND == kLogits) {
                 Sums mine;
-                if constexpr (KIND == kLogits) mine = carry_logits<T>(a, at, m0 + lane, n0, bias, ready, release);
+                if constexpr (KIND == kLogits) mine = carry_logits<T, ENT>(a, at, m0 + lane, n0, bias, ready, release);
                 else mine = carry_stats(a, at, m0 + lane, n0, bias, ready, release);
                 // the four warps of these rows join their columns; two rooms, so that one barrier a tile is enough
                 float *room = reinterpret_cast<float *>(extra + kBiasBytes) + ((acc * 4 + quarter) * 4) * 96 + lane;
@@ -657,7 +670,8 @@ struct RowArgs {
 };
 
 // What carry_grad needs of a row, from the reference and base-2 logarithm of the sum relative to it.
-__device__ __forceinline__ void write_consts(const RowArgs &a, int64_t r, int64_t token, float ref, float ls, float entropy, bool empty)
+// `x`: the token's logit, for the ones who use `known`.
+__device__ __forceinline__ void write_consts(const RowArgs &a, int64_t r, int64_t token, float ref, float ls, float entropy, bool empty, float x)
 {
     float ga = a.grad_logprob && token >= 0 ? a.grad_logprob[r] / a.temperature : 0.f;
     float gb = a.grad_entropy ? a.grad_entropy[r] / a.temperature : 0.f;
@@ -666,7 +680,8 @@ __device__ __forceinline__ void write_consts(const RowArgs &a, int64_t r, int64_
     float4 *to = reinterpret_cast<float4 *>(a.consts) + 2 * r;
     const float ab = ga + (a.grad_entropy ? gb * entropy : 0.f);
     to[0] = make_float4(ref, ls, ga, ab);
-    to[1] = make_float4(gb * kLn2, __int_as_float(token < 0 || token >= a.V ? -1 : static_cast<int>(token)), 0.f, 0.f);
+    const float y = min_nan(fmaf(x - ref, a.c, -ls), 0.f), known = ga - ex2(y) * fmaf(gb * kLn2, max_nan(y, -200.f), ab);
+    to[1] = make_float4(gb * kLn2, __int_as_float(token < 0 || token >= a.V ? -1 : static_cast<int>(token)), known, 0.f);
 }
 
 // The largest bound on a row's gradient by its logits: |d| <= |ga| + |gb| (p |log p| + p H), p |log p| < 0.37, H <= log V.
@@ -697,7 +712,7 @@ __device__ __forceinline__ void finish_row(const RowArgs &a, int64_t r, const Su
         else if (token >= 0) lp = empty ? neg_inf() : (a.token_logit[r] - sums.m) / a.temperature - log_s;
         a.logprob[r] = lp;
     }
-    if (a.consts) write_consts(a, r, token, sums.m, log2f(sums.s), entropy, empty);
+    if (a.consts) write_consts(a, r, token, sums.m, log2f(sums.s), entropy, empty, a.token_logit && token >= 0 && token < a.V ? a.token_logit[r] : 0.f);
 }
 
 // Joins the tiles of 32 rows, a row to a lane: each warp every 32nd tile, eight of them at a time (their loads in flight together, one
@@ -778,7 +793,7 @@ __global__ void __launch_bounds__(256) saved_rows_kernel(const RowArgs a)
     const int64_t r = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     if (r >= a.R) return;
     const float lse = a.in_lse[r];
-    write_consts(a, r, a.tokens ? token_at(a.tokens, a.index_bits, r) : -1, lse * a.temperature, 0.f, a.in_entropy ? a.in_entropy[r] : 0.f, lse == neg_inf());
+    write_consts(a, r, a.tokens ? token_at(a.tokens, a.index_bits, r) : -1, lse * a.temperature, 0.f, a.in_entropy ? a.in_entropy[r] : 0.f, lse == neg_inf(), 0.f);
 }
 
 // ---------------------------------------------------------------------------------------------- few rows
@@ -987,49 +1002,65 @@ template <class T> __global__ void __launch_bounds__(256) few_finish_kernel(cons
 }
 
 // ---------------------------------------------------------------------------------------------- gradient by kept logits
-// Codes into the gradient, in place: eight columns of kGradRows rows to a thread.  Memory bound: 2 bytes in, 2 out.
+// Codes into the gradient, in place: eight columns to a thread, eight rows at a time; FINE: of 32 rows, which it adds up for dbias.
+// Memory bound: 2 bytes in (3), 2 out.
 constexpr int kGradRows = 8;
-template <class T, bool ENT>
-__global__ void __launch_bounds__(256) grad_kernel(uint16_t *codes, const float *tops, int64_t padded_rows, int64_t M, int64_t N, int64_t ld, const float *consts, float c,
-                                                   const uint32_t *scale_bits)
+template <bool FINE> constexpr int kGradBlock = FINE ? 32 : kGradRows;
+template <class T, bool ENT, bool FINE>
+__global__ void __launch_bounds__(256) grad_kernel(uint16_t *codes, const uint8_t *fine, const float *tops, int64_t padded_rows, int64_t M, int64_t N, int64_t ld, const float *consts,
+                                                   float c, const uint32_t *scale_bits, float *column_sums)
 {
-    __shared__ RowConsts rows[kGradRows];
+    __shared__ RowConsts rows[kGradBlock<FINE>];
     wait_for_previous();
     const int64_t n = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
-    for (int64_t m0 = static_cast<int64_t>(blockIdx.y) * kGradRows; m0 < M; m0 += static_cast<int64_t>(gridDim.y) * kGradRows) {
-        const int count = static_cast<int>(min(M - m0, static_cast<int64_t>(kGradRows)));
+    for (int64_t m0 = static_cast<int64_t>(blockIdx.y) * kGradBlock<FINE>; m0 < M; m0 += static_cast<int64_t>(gridDim.y) * kGradBlock<FINE>) {
+        const int count = static_cast<int>(min(M - m0, static_cast<int64_t>(kGradBlock<FINE>)));
         __syncthreads();
         if (threadIdx.x < count) rows[threadIdx.x] = row_consts(consts, m0 + threadIdx.x, power_of_two(scale_power(scale_bits)));
         __syncthreads();
         if (n >= N) continue;
-        uint4 raw[kGradRows];
-        float top[kGradRows];
+        float sum[8] = {};
+#pragma unroll 1
+        for (int first = 0; first < count; first += kGradRows) {
+            uint4 raw[kGradRows];
+            uint2 low[kGradRows];
+            float top[kGradRows];
 #pragma unroll
-        for (int i = 0; i < kGradRows; ++i)
-            if (i < count) {  // ld is a multiple of 64: columns behind N are there, and nobody reads what becomes of them
-                raw[i] = load_last(codes + (m0 + i) * ld + n);
-                top[i] = tops[n / kCodes * padded_rows + m0 + i];
+            for (int i = 0; i < kGradRows; ++i)
+                if (first + i < count) {  // ld is a multiple of 64: columns behind N are there, and nobody reads what becomes of them
+                    const int64_t m = m0 + first + i;
+                    raw[i] = load_last(codes + m * ld + n);
+                    if (FINE) low[i] = *reinterpret_cast<const uint2 *>(fine + m * ld + n);
+                    top[i] = tops[n / kCodes * padded_rows + m];
+                }
+#pragma unroll
+            for (int i = 0; i < kGradRows; ++i) {
+                if (first + i >= count) break;
+                const RowConsts k = rows[first + i];
+                const float base = fmaf(top[i] - k.ref, c, -k.ls);
+                const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                float f[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t high = j % 2 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu;
+                    const uint32_t code = FINE ? high << 7 | __byte_perm(j < 4 ? low[i].x : low[i].y, 0, 0x4440 | j % 4) : high;
+                    const float steps = __uint_as_float(0x4b000000u | code) - 8388608.f;
+                    f[j] = grad_at<ENT>(high == kNothing ? neg_inf() : fmaf(steps, -1.f / kCodeSteps<T, FINE>, base), k);
+                }
+                const int64_t at = k.token - n;
+                if (at >= 0 && at < 8)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (at == j) f[j] = k.known;
+                if (FINE)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[j] += f[j];
+                *reinterpret_cast<uint4 *>(codes + (m0 + first + i) * ld + n) = Elem<T>::pack(f);
             }
-#pragma unroll
-        for (int i = 0; i < kGradRows; ++i) {
-            if (i >= count) break;
-            const RowConsts k = rows[i];
-            const float base = fmaf(top[i] - k.ref, c, -k.ls);
-            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-            float f[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float code = __uint_as_float(__byte_perm(w[j / 2], 0x4b000000u, j % 2 ? 0x7432 : 0x7410)) - 8388608.f;
-                const float y = code == static_cast<float>(kNothing) ? neg_inf() : fmaf(code, -1.f / kSteps<T>, base);
-                f[j] = grad_at<ENT>(y, k);
-            }
-            const int64_t at = k.token - n;
-            if (at >= 0 && at < 8)
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (at == j) f[j] += k.hit;
-            *reinterpret_cast<uint4 *>(codes + (m0 + i) * ld + n) = Elem<T>::pack(f);
         }
+        if (FINE)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) column_sums[m0 / 32 * ld + n + j] = sum[j];
     }
 }
 
@@ -1077,7 +1108,7 @@ template <class T> int finish(const float *parts, int splits, int64_t M, int64_t
 }
 
 // dbias of a piece: the row groups' sums in their order, eight runs of them to a column.
-__global__ void __launch_bounds__(256) bias_kernel(const float *sums, int64_t groups, int64_t N, int64_t ld, const uint32_t *scale_bits, float *dbias)
+__global__ void __launch_bounds__(256) bias_kernel(const float *sums, int64_t groups, int64_t N, int64_t ld, const uint32_t *scale_bits, float *dbias, int add)
 {
     __shared__ float room[8][32];
     wait_for_previous();
@@ -1090,7 +1121,8 @@ __global__ void __launch_bounds__(256) bias_kernel(const float *sums, int64_t gr
     __syncthreads();
     if (warp > 0 || n >= N) return;
     for (int w = 1; w < 8; ++w) sum += room[w][lane];
-    dbias[n] = sum * power_of_two(-scale_power(scale_bits));
+    sum *= power_of_two(-scale_power(scale_bits));
+    dbias[n] = add ? dbias[n] + sum : sum;
 }
 
 // ---------------------------------------------------------------------------------------------- launches
@@ -1107,7 +1139,7 @@ constexpr int64_t kLogitBytes = 512ll << 20, kLeastRows = 2048, kLeastWidth = 51
 constexpr int64_t kPartialBytes = 32ll << 20, kLeastStats = 4096;
 
 struct Layout {
-    size_t hidden, weight, partial, token_logit, consts, scale, logits, tops, piece, parts, weight_sums, sums, total;
+    size_t hidden, weight, partial, token_logit, consts, scale, logits, tops, fine, piece, parts, weight_sums, sums, total;
     int64_t padded_rows, rows, stat_rows, width, ld_piece, ld_parts;  // rows, width: what is worked on at a time; stat_rows: for values
     int hidden_splits, weight_splits;
     bool by_rows;
@@ -1164,8 +1196,8 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
     l.weight = take(tma_ok(weight, ldw) ? 0 : copy_bytes(V, D));
     if (grads) {
         l.ld_piece = div_up(V, 64) * 64;
-        const int64_t most = kLogitBytes / 2 / l.ld_piece;  // rows
-        l.by_rows = stats && !bias && D >= kLeastWidth && (R <= most || most >= kLeastRows);
+        const int64_t most = kLogitBytes / (bias ? 3 : 2) / l.ld_piece;  // rows
+        l.by_rows = stats && D >= kLeastWidth && (R <= most || most >= kLeastRows);
         if (l.by_rows) {
             const int64_t pieces = R <= most ? 1 : div_up(R, most / kTile * kTile);
             if (pieces > 1) l.rows = div_up(div_up(R, pieces), kTile) * kTile;  // of one size
@@ -1186,7 +1218,8 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
         l.piece = take(static_cast<size_t>(l.rows) * l.ld_piece * 2);
         l.parts = take(static_cast<size_t>(l.hidden_splits) * l.rows * l.ld_parts * 4);
         if (!once || l.weight_splits > 1) l.weight_sums = take(static_cast<size_t>(l.weight_splits) * l.width * l.ld_parts * 4);
-        if (bias) l.sums = take(static_cast<size_t>(div_up(R, 32)) * l.ld_piece * 4);
+        if (l.by_rows && bias) l.fine = take(static_cast<size_t>(l.rows) * l.ld_piece);
+        if (bias) l.sums = take(static_cast<size_t>(div_up(l.rows, 32)) * l.ld_piece * 4);
     }
     l.stat_rows = l.rows;
     if (stats) {
@@ -1296,18 +1329,23 @@ template <class T> struct Head {
         a.M = rows.R, a.N = h.V, a.a_row0 = static_cast<int>(r0);
         a.tokens = rows.tokens;
         a.partial = floats(l.partial), a.token_logit = rows.tokens ? floats(l.token_logit) : nullptr;
-        if (KIND == kLogits) a.out = ws + l.piece, a.ldo = l.ld_piece, a.tops = floats(l.tops);
-        HEAD_TRY((launch_product<T, KIND, true>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
+        if (KIND == kLogits) a.out = ws + l.piece, a.ldo = l.ld_piece, a.tops = floats(l.tops), a.fine = h.dbias ? reinterpret_cast<uint8_t *>(ws + l.fine) : nullptr;
+        if (KIND == kLogits && h.dbias) HEAD_TRY((launch_product<T, KIND, true>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
+        else HEAD_TRY((launch_product<T, KIND, false>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
         rows.partial = a.partial, rows.token_logit = a.token_logit, rows.tiles = static_cast<int>(div_up(h.V, kTile));
         return follow(rows_kernel, dim3(static_cast<unsigned>(div_up(rows.R, 32))), 32 * kRowWarps, 0, 1, s, rows);
     }
-    // The gradient by the kept logits of m rows.
-    int gradient(int64_t m)
+    // The gradient by the kept logits of m rows (from r0), and dbias.
+    int gradient(int64_t m, int64_t r0)
     {
-        const int64_t down = div_up(m, kGradRows);
+        const bool fine = h.dbias != nullptr;
+        const int64_t down = div_up(m, fine ? kGradBlock<true> : kGradBlock<false>);
         const dim3 grid(static_cast<unsigned>(div_up(h.V, 2048)), static_cast<unsigned>(down < 65535 ? down : 65535));
         uint16_t *codes = reinterpret_cast<uint16_t *>(ws + l.piece);
-        return follow(h.grad_entropy ? grad_kernel<T, true> : grad_kernel<T, false>, grid, 256, 0, 1, s, codes, floats(l.tops), l.padded_rows, m, h.V, l.ld_piece, base.consts, base.c, base.scale_bits);
+        const uint8_t *low = reinterpret_cast<const uint8_t *>(ws + l.fine);
+        auto *kernel = fine ? (h.grad_entropy ? grad_kernel<T, true, true> : grad_kernel<T, false, true>) : h.grad_entropy ? grad_kernel<T, true, false> : grad_kernel<T, false, false>;
+        HEAD_TRY(follow(kernel, grid, 256, 0, 1, s, codes, low, floats(l.tops), l.padded_rows, m, h.V, l.ld_piece, base.consts, base.c, base.scale_bits, floats(l.sums)));
+        return fine ? finish_bias(m, h.V, 0, r0 > 0) : SPDY_OK;
     }
     // The gradient by the logits of all rows and ids v0 .. v0 + n - 1, which are multiplied again; dbias of these ids.
     int gradient_again(int64_t n, int64_t v0)
@@ -1318,11 +1356,11 @@ template <class T> struct Head {
         if (h.dbias) a.column_sums = floats(l.sums), a.ld_sums = l.ld_piece;
         if (h.grad_entropy) HEAD_TRY((launch_product<T, kGrad, true>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
         else HEAD_TRY((launch_product<T, kGrad, false>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
-        return h.dbias ? finish_bias(n, v0) : SPDY_OK;
+        return h.dbias ? finish_bias(h.R, n, v0, false) : SPDY_OK;
     }
-    int finish_bias(int64_t n, int64_t v0)
+    int finish_bias(int64_t m, int64_t n, int64_t v0, bool add)
     {
-        return follow(bias_kernel, dim3(static_cast<unsigned>(div_up(n, 32))), 256, 0, 1, s, floats(l.sums), div_up(h.R, 32), n, l.ld_piece, base.scale_bits, h.dbias + v0);
+        return follow(bias_kernel, dim3(static_cast<unsigned>(div_up(n, 32))), 256, 0, 1, s, floats(l.sums), div_up(m, 32), n, l.ld_piece, base.scale_bits, h.dbias + v0, add);
     }
     // dhidden's sums and dweight from the gradient of m rows (from r0) and n ids (from v0), added to what earlier rows or ids gave.
     int products(int64_t m, int64_t r0, int64_t n, int64_t v0)
@@ -1420,7 +1458,7 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
         for (int64_t r0 = 0; r0 < R; r0 += l.rows) {
             const int64_t n = R - r0 < l.rows ? R - r0 : l.rows;
             HEAD_TRY(g.template stats<kLogits>(part(r0, n), r0));
-            HEAD_TRY(g.gradient(n));
+            HEAD_TRY(g.gradient(n, r0));
             HEAD_TRY(g.products(n, r0, V, 0));
             if (h.dhidden) HEAD_TRY(g.finish_hidden(n, r0));
         }

@@ -42,24 +42,26 @@ def check(h, w, b, tokens, temperature, gl, gh, on="cpu"):
     alone = evaluate.linear_token_logprobs(h, w, tokens, b, temperature)
     out, grads = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, temperature)
     again = evaluate.linear_token_logprobs_backward(h, w, tokens, out.lse, out.entropy, gl, gh, b, temperature)
-    # without dbias (and from a width of 512 on) the logits are kept in 16 bits
+    # from a width of 512 on the logits are kept, in 23 bits with dbias and in 16 without
     other, kept = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, temperature, wanted=("hidden", "weight"))
     for name in ("logprob", "entropy", "lse"):
         tune.close(getattr(out, name), want, name)
         tune.close(getattr(other, name), want, name)
         tune.close(getattr(alone, name), want, name)  # up to four rows go their own way
+    tune.close(again.dhidden, want, "dhidden")
+    tune.close(again.dweight, want, "dweight")
+    wide = w.shape[1] >= 512
     if b is not None:
-        for g in (grads, again):
-            tune.close(g.dhidden, want, "dhidden")
-            tune.close(g.dweight, want, "dweight")
-            tune.close(g.dbias, want, "dbias")
+        tune.close(again.dbias, want, "dbias")
         assert kept.dbias is None
+        fine = tune.head(h, w, b, tokens, temperature, gl, gh, on, kept=23) if wide else want
+        tune.close(grads.dhidden, fine, "dhidden")
+        tune.close(grads.dweight, fine, "dweight")
+        tune.close(grads.dbias, fine, "dbias")
     else:
-        tune.close(again.dhidden, want, "dhidden")
-        tune.close(again.dweight, want, "dweight")
         assert torch.equal(kept.dhidden, grads.dhidden) and torch.equal(kept.dweight, grads.dweight) and grads.dbias is None
-    if w.shape[1] >= 512:
-        want = tune.head(h, w, b, tokens, temperature, gl, gh, on, kept=True)
+    if wide:
+        want = tune.head(h, w, b, tokens, temperature, gl, gh, on, kept=16)
     tune.close(kept.dhidden, want, "dhidden")
     tune.close(kept.dweight, want, "dweight")
     evaluate.linear_check_status()
@@ -90,8 +92,8 @@ def test_against_the_formula(R, V, D, dtype, bias, temperature, entropy, padh, p
     (9000, 33000, 72, F16),       # pieces that the budget sets, the last one shorter
     (300, 20000, 520, BF16),      # the summed index of dhidden shared among multiprocessors
     (20000, 300, 40, F16),        # that of dweight
-    (9000, 40000, 512, BF16),     # two pieces of rows
-    (9001, 70001, 520, F16),      # three, odd ends
+    (9000, 40000, 512, BF16),     # two pieces of rows (three with dbias)
+    (9001, 70001, 520, F16),      # three (four, odd ends)
     (700, 5003, 600, F16),        # all rows at once
     (5, 3000, 640, BF16),
     (512, 30001, 96, BF16),
@@ -149,6 +151,8 @@ def test_ids_that_are_not_allowed(low, entropy, D, dtype):
     want = tune.head(h, w, torch.where(allowed.cuda(), b, torch.full_like(b, -INF)), tokens, 1.0, gl, gh)
     for name in ("logprob", "entropy", "lse"):
         tune.close(getattr(got, name), want, name)
+    if D >= 512:
+        want = tune.head(h, w, torch.where(allowed.cuda(), b, torch.full_like(b, -INF)), tokens, 1.0, gl, gh, kept=23)
     for name in ("dhidden", "dweight", "dbias"):
         tune.close(getattr(grads, name), want, name)
     kept = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, wanted=("hidden", "weight"))[1]
@@ -233,7 +237,7 @@ def test_outputs_with_strides_leave_their_neighbours(D):
             assert (a is None) if name not in wanted else torch.equal(a, c) or (D >= 512 and "bias" not in wanted)
     for out in ({}, {"dhidden": dh, "dweight": dw}):
         kept = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, wanted=("hidden", "weight"), **out)[1]
-        want = tune.head(h, w, b, tokens, 1.0, gl, gh, kept=D >= 512)
+        want = tune.head(h, w, b, tokens, 1.0, gl, gh, kept=16 if D >= 512 else 0)
         tune.close(kept.dhidden, want, "dhidden")
         tune.close(kept.dweight, want, "dweight")
 
@@ -255,6 +259,25 @@ def test_few_rows_with_all_but_certain_tokens(R, dtype):
     # products added in fp32 by 32 lanes, 64 each: within 80 roundings of magnitudes that sum to about 30 a logit, twice, and lse's own
     assert ((got - exact).abs() <= gl.cpu().double().abs() * (200 * 2.0 ** -24 * 40 + 2.0 ** -20)).all()
     tune.close(out.logprob, want, "logprob")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("entropy", [False, True])
+def test_many_rows_with_all_but_certain_tokens(dtype, entropy):
+    # the gradient at the token is 1 - p, which kept logits would not hold
+    R, V, D = 100, 3001, 512
+    h, w, tokens, b = head(R, V, D, dtype, F32)
+    tokens = tokens.clamp(min=0)
+    h.copy_((0.5 * rand(R, D, seed=5) + 1.5 * w[tokens].float()).to(dtype))
+    gl, gh = weights(R, dtype, entropy)
+    want = tune.head(h, w, b, tokens, 0.7, gl, gh)
+    assert want["logprob"].median() > -0.01
+    check(h, w, b, tokens, 0.7, gl, gh)
+    check(h, w, None, tokens, 0.7, gl, gh)
+    kept = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, 0.7, wanted=("hidden", "weight"))[1]
+    off = (kept.dhidden.cpu().double() - want["dhidden"]).norm() / want["dhidden"].norm()
+    assert off < 2.5 * ref.HALF_ULP[dtype]  # two roundings and the kept logits'
 
 
 @gpu
@@ -416,7 +439,7 @@ def test_workspace_stays_bounded():
     assert need(8192, 131072, 4096, 0, 1) < (256 + 200) << 20           # a piece of 256 MB and dhidden's fp32 sums
     assert need(8192, 65536, 4096, 1, 1) < (512 + 1024 + 200) << 20     # some rows' logits and gradient, fp32 sums of dweight
     assert need(4096, 65536, 4096, 1, 1) < (512 + 250) << 20            # all rows at once
-    assert need(8192, 65536, 4096, 1, 2) < (256 + 250) << 20            # with dbias: by pieces of the vocabulary
+    assert need(8192, 65536, 4096, 1, 2) < (512 + 1024 + 250) << 20     # with dbias
     assert need(8192, 200000, 4096, 1, 1) < (256 + 200 + 80) << 20      # fewer than 2048 rows would fit: the same
     assert need(1 << 20, 131072, 64, 0, 1) < (4096 + 700) << 20         # 2048 ids at least
     assert need(64, 5000, 100, 1, 0, ld=101) >= need(64, 5000, 104, 1, 0) + 5000 * 100 * 2  # copies of rows that TMA cannot read

@@ -58,7 +58,7 @@ def test_rows_beyond_32_bits():
         b = torch.zeros(V, device="cuda") if "bias" in wanted else None
         out, grads = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, None, b, wanted=wanted)
         rows = torch.cat([torch.arange(50, device="cuda"), torch.arange(R - tail, R, device="cuda")])
-        want = tune.head(h[rows], w, b, tokens[rows], 1.0, gl[rows], None, "cuda", kept=b is None)
+        want = tune.head(h[rows], w, b, tokens[rows], 1.0, gl[rows], None, "cuda", kept=16 if b is None else 23)
         for name in ("lse", "logprob", "entropy"):
             tune.close(getattr(out, name)[rows], want, name)
         tune.close(grads.dhidden[rows], want, "dhidden")

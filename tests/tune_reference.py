@@ -9,9 +9,10 @@ import eval_reference as ref
 F16 = torch.float16
 
 
-def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu", kept=False):
+def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu", kept=0):
     """A dict of values and, under the same name with ``_err``, of bounds on the fp32 error before the last rounding.
-    ``kept``: the gradient comes from logits kept in 16 bits, as a call keeps them that gives values and gradients but no dbias."""
+    ``kept``: the gradient comes from logits kept in so many bits, as a call that gives values and gradients keeps them: 16, or 23 with
+    dbias; the token's own is not among them."""
     h, w = (t.detach().to(on).double() for t in (hidden, weight))
     R, D = h.shape
     V = w.shape[0]
@@ -56,10 +57,12 @@ def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu", 
     off = 3 * ez + adds + 2.0 ** -22 * (lse.abs().nan_to_num(0.0, posinf=0.0, neginf=0.0) + 4)
     share = p * (a.abs()[:, None] + b.abs()[:, None] * (logs.abs() + entropy[:, None] + 1)) / temperature
     eg = share * (off[:, None] + 2.0 ** -21 * logs.abs()) + 2.0 ** -23 * g.abs()
-    if kept:  # log2 p in steps of 2^-10 (half precision 2^-11), off by half a step; 64 (32) octaves below a neighbour p counts as 0
+    if kept:  # log2 p in steps of 2^-10 (half precision 2^-11), or 2^-7 of that, off by half a step; 64 (32) octaves below a neighbour p counts as 0
         steps, octaves = (2.0 ** -11, 32) if hidden.dtype == F16 else (2.0 ** -10, 64)
-        eg = eg + share * (steps / 2 * math.log(2) * 1.001)
-        eg = eg + 2.0 ** -octaves * (a.abs() + b.abs() * (octaves + entropy)).nan_to_num(0.0)[:, None] / temperature
+        more = share * (steps * 2.0 ** (16 - kept) / 2 * math.log(2) * 1.001)
+        more = more + 2.0 ** -octaves * (a.abs() + b.abs() * (octaves + entropy)).nan_to_num(0.0)[:, None] / temperature
+        more[torch.arange(R, device=h.device)[named], tokens[named]] = 0.0
+        eg = eg + more
     # Half precision: a power of two brings the largest bound on a row's gradient, |a| + |b| (0.37 + log V), to 2^13 .. 2^14, where numbers below the
     # normal ones are rounded by 2^-25: 2^-38 of that bound.
     most = float(((a.abs() + b.abs() * (0.37 + math.log(V))) / temperature).nan_to_num(0.0).max()) if R else 0.0
