@@ -1003,16 +1003,17 @@ template <class T> __global__ void __launch_bounds__(256) few_finish_kernel(cons
 
 // ---------------------------------------------------------------------------------------------- gradient by kept logits
 // Codes into the gradient, in place: eight columns to a thread, eight rows at a time; FINE: of 32 rows, which it adds up for dbias.
-// Memory bound: 2 bytes in (3), 2 out.
-constexpr int kGradRows = 8;
+// Memory bound: 2 bytes in (3), 2 out; 4096 x 32768 97 us (5.5 TB/s).  Blocks of 128, of which small calls have enough (512 x 30001 x 768, the
+// whole call: 135 us with 256 threads, 126 with 128).
+constexpr int kGradRows = 8, kGradThreads = 128;
 template <bool FINE> constexpr int kGradBlock = FINE ? 32 : kGradRows;
 template <class T, bool ENT, bool FINE>
-__global__ void __launch_bounds__(256) grad_kernel(uint16_t *codes, const uint8_t *fine, const float *tops, int64_t padded_rows, int64_t M, int64_t N, int64_t ld, const float *consts,
+__global__ void __launch_bounds__(kGradThreads) grad_kernel(uint16_t *codes, const uint8_t *fine, const float *tops, int64_t padded_rows, int64_t M, int64_t N, int64_t ld, const float *consts,
                                                    float c, const uint32_t *scale_bits, float *column_sums)
 {
     __shared__ RowConsts rows[kGradBlock<FINE>];
     wait_for_previous();
-    const int64_t n = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+    const int64_t n = (static_cast<int64_t>(blockIdx.x) * kGradThreads + threadIdx.x) * 8;
     for (int64_t m0 = static_cast<int64_t>(blockIdx.y) * kGradBlock<FINE>; m0 < M; m0 += static_cast<int64_t>(gridDim.y) * kGradBlock<FINE>) {
         const int count = static_cast<int>(min(M - m0, static_cast<int64_t>(kGradBlock<FINE>)));
         __syncthreads();
@@ -1133,7 +1134,12 @@ size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 constexpr int64_t kPieceBytes = 256ll << 20, kLeastPiece = 2048;
 // By rows: the logits, for as many rows as this much memory holds; not where that is few, since dweight's fp32 sums are read and
 // written for each.
-constexpr int64_t kLogitBytes = 512ll << 20, kLeastRows = 2048, kLeastWidth = 512;
+constexpr int64_t kLogitBytes = 512ll << 20, kLeastRows = 2048;
+
+// Whether keeping the logits costs less than multiplying them again, which the width decides.  4096 x 32768, us by rows and by ids: width 384 466,
+// 436, 512 495, 486, 768 640, 650, 1024 730, 800; with dbias (another byte per logit) 512 630, 570, 768 797, 740, 1024 880, 860.  Few
+// logits stay in L2 and save a kernel's start: 512 x 30001 with dbias 512 134, 148, 768 140, 165, without 256 100, 108.
+bool keeps_logits(int64_t R, int64_t V, int64_t D, bool bias) { return D >= (bias && R > (1ll << 25) / V ? 1024 : 512); }
 
 // Sums of a row's tiles, 12 bytes each, for as many rows at a time as this much memory holds, 4096 at least.
 constexpr int64_t kPartialBytes = 32ll << 20, kLeastStats = 4096;
@@ -1197,7 +1203,7 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
     if (grads) {
         l.ld_piece = div_up(V, 64) * 64;
         const int64_t most = kLogitBytes / (bias ? 3 : 2) / l.ld_piece;  // rows
-        l.by_rows = stats && D >= kLeastWidth && (R <= most || most >= kLeastRows);
+        l.by_rows = stats && keeps_logits(R, V, D, bias) && (R <= most || most >= kLeastRows);
         if (l.by_rows) {
             const int64_t pieces = R <= most ? 1 : div_up(R, most / kTile * kTile);
             if (pieces > 1) l.rows = div_up(div_up(R, pieces), kTile) * kTile;  // of one size
@@ -1340,11 +1346,11 @@ template <class T> struct Head {
     {
         const bool fine = h.dbias != nullptr;
         const int64_t down = div_up(m, fine ? kGradBlock<true> : kGradBlock<false>);
-        const dim3 grid(static_cast<unsigned>(div_up(h.V, 2048)), static_cast<unsigned>(down < 65535 ? down : 65535));
+        const dim3 grid(static_cast<unsigned>(div_up(h.V, kGradThreads * 8)), static_cast<unsigned>(down < 65535 ? down : 65535));
         uint16_t *codes = reinterpret_cast<uint16_t *>(ws + l.piece);
         const uint8_t *low = reinterpret_cast<const uint8_t *>(ws + l.fine);
         auto *kernel = fine ? (h.grad_entropy ? grad_kernel<T, true, true> : grad_kernel<T, false, true>) : h.grad_entropy ? grad_kernel<T, true, false> : grad_kernel<T, false, false>;
-        HEAD_TRY(follow(kernel, grid, 256, 0, 1, s, codes, low, floats(l.tops), l.padded_rows, m, h.V, l.ld_piece, base.consts, base.c, base.scale_bits, floats(l.sums)));
+        HEAD_TRY(follow(kernel, grid, kGradThreads, 0, 1, s, codes, low, floats(l.tops), l.padded_rows, m, h.V, l.ld_piece, base.consts, base.c, base.scale_bits, floats(l.sums)));
         return fine ? finish_bias(m, h.V, 0, r0 > 0) : SPDY_OK;
     }
     // The gradient by the logits of all rows and ids v0 .. v0 + n - 1, which are multiplied again; dbias of these ids.

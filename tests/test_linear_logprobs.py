@@ -54,7 +54,7 @@ def check(h, w, b, tokens, temperature, gl, gh, on="cpu"):
     if b is not None:
         tune.close(again.dbias, want, "dbias")
         assert kept.dbias is None
-        fine = tune.head(h, w, b, tokens, temperature, gl, gh, on, kept=23) if wide else want
+        fine = tune.head(h, w, b, tokens, temperature, gl, gh, on, kept=23) if wide else want  # (from 1024 on where the logits are many)
         tune.close(grads.dhidden, fine, "dhidden")
         tune.close(grads.dweight, fine, "dweight")
         tune.close(grads.dbias, fine, "dbias")
@@ -92,8 +92,9 @@ def test_against_the_formula(R, V, D, dtype, bias, temperature, entropy, padh, p
     (9000, 33000, 72, F16),       # pieces that the budget sets, the last one shorter
     (300, 20000, 520, BF16),      # the summed index of dhidden shared among multiprocessors
     (20000, 300, 40, F16),        # that of dweight
-    (9000, 40000, 512, BF16),     # two pieces of rows (three with dbias)
-    (9001, 70001, 520, F16),      # three (four, odd ends)
+    (9000, 40000, 1024, BF16),    # two pieces of rows (three with dbias)
+    (9001, 70001, 520, F16),      # three, odd ends
+    (5000, 70001, 1032, F16),     # two with dbias
     (700, 5003, 600, F16),        # all rows at once
     (5, 3000, 640, BF16),
     (512, 30001, 96, BF16),
