@@ -73,6 +73,7 @@ SPDY_EVAL_FN uint32_t mix(uint32_t x)
     return x ^ (x >> 16);
 }
 
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float exponent(int field) { return __int_as_float(field << 23); }  // 2^(field - 127), 1 <= field <= 254
 
 // The two formats: the exponent field that the largest magnitude's binade gets.
@@ -329,10 +330,14 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
 #pragma unroll
             for (int i = 0; i < N; ++i) g[i] *= scale;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            // every product and sum rounded by itself: the 8-bit codes below are those of the plain formula, bit for bit
-            m[i] = m[i] * s.b1 + g[i] * s.g1;
-            v[i] = v[i] * s.b2 + g[i] * s.g2 * g[i];
+        for (int i = 0; i < N; i += 2) {
+            // Two elements an instruction (100 M of them in 8 bits 221 -> 210 us, bound by instructions), every product and sum
+            // rounded by itself: the 8-bit codes below are those of the plain formula, bit for bit.
+            float2 first = make_float2(m[i], m[i + 1]), second = make_float2(v[i], v[i + 1]);
+            const float2 slope = make_float2(g[i], g[i + 1]);
+            first = __fadd2_rn(__fmul2_rn(first, both(s.b1)), __fmul2_rn(slope, both(s.g1)));
+            second = __fadd2_rn(__fmul2_rn(second, both(s.b2)), __fmul2_rn(__fmul2_rn(slope, both(s.g2)), slope));
+            m[i] = first.x, m[i + 1] = first.y, v[i] = second.x, v[i + 1] = second.y;
         }
         if (keep)  // and the weight, with m = 0, stays 0 by itself
 #pragma unroll
@@ -340,7 +345,11 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
                 if (p[i] == 0.f) m[i] = v[i] = 0.f;
         if (s.eps >= 1e-9f) {  // roots of numbers below 2^-126 do not show beside such an eps
 #pragma unroll
-            for (int i = 0; i < N; ++i) p[i] = fmaf(p[i], decay, -quotient(m[i] * rate, fmaf(root_flushed(v[i]), root, s.eps)));
+            for (int i = 0; i < N; i += 2) {
+                const float2 above = __fmul2_rn(make_float2(m[i], m[i + 1]), both(rate)), below = __ffma2_rn(make_float2(root_flushed(v[i]), root_flushed(v[i + 1])), both(root), both(s.eps));
+                const float2 next = __ffma2_rn(make_float2(p[i], p[i + 1]), both(decay), make_float2(-quotient(above.x, below.x), -quotient(above.y, below.y)));
+                p[i] = next.x, p[i + 1] = next.y;
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) p[i] = keep && p[i] == 0.f ? 0.f : fmaf(p[i], decay, -quotient(m[i] * rate, fmaf(root_of(v[i]), root, s.eps)));
