@@ -680,7 +680,7 @@ template <class T, int ACT> int launch_product(LinearArgs a, void *workspace, cu
         a.w = ws, a.ldw = p.ldto;
     }
     if (p.to[0] || p.to[1]) {
-        const int64_t rows = p.rows[0] > p.rows[1] ? p.rows[0] : p.rows[1], blocks = (rows * (p.ldto / 8) + 255) / 256;
+        const int64_t rows = p.rows[0] > p.rows[1] ? p.rows[0] : p.rows[1], blocks = (rows * (p.ldto / 8) + kRepackBlock - 1) / kRepackBlock;
         repack_kernel<<<dim3(static_cast<unsigned>(blocks < 2368 ? blocks : 2368), 2), 256, 0, s>>>(p);
         const int rc = finish_launch();
         if (rc != SPDY_OK) return rc;

@@ -1417,7 +1417,7 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
         h.weight = ws + l.weight, h.ldw = p.ldto;
     }
     if (p.to[0] || p.to[1]) {
-        const int64_t rows = p.rows[0] > p.rows[1] ? p.rows[0] : p.rows[1], blocks = div_up(rows * (p.ldto / 8), 256);
+        const int64_t rows = p.rows[0] > p.rows[1] ? p.rows[0] : p.rows[1], blocks = div_up(rows * (p.ldto / 8), kRepackBlock);
         repack_kernel<<<dim3(static_cast<unsigned>(blocks < 2368 ? blocks : 2368), 2), 256, 0, s>>>(p);
         HEAD_TRY(finish_launch());
     }
