@@ -679,19 +679,15 @@ template <class T, int ACT> int launch_product(LinearArgs a, void *workspace, cu
         p.from[1] = static_cast<const uint16_t *>(a.w), p.ld[1] = a.ldw, p.rows[1] = a.N, p.to[1] = reinterpret_cast<uint16_t *>(ws);
         a.w = ws, a.ldw = p.ldto;
     }
-    if (p.to[0] || p.to[1]) {
-        const int64_t rows = p.rows[0] > p.rows[1] ? p.rows[0] : p.rows[1], blocks = (rows * (p.ldto / 8) + kRepackBlock - 1) / kRepackBlock;
-        repack_kernel<<<dim3(static_cast<unsigned>(blocks < 2368 ? blocks : 2368), 2), 256, 0, s>>>(p);
-        const int rc = finish_launch();
-        if (rc != SPDY_OK) return rc;
-    }
+    int rc = repack(p, s);
+    if (rc != SPDY_OK) return rc;
     a.k_blocks = static_cast<int>((a.K + BK * kSlices - 1) / (BK * kSlices));
     const TilePlan plan = choose_tiles<T, ACT>(a.M, a.N, a.k_blocks, sm_count());
     const int64_t rows = plan.mode == kPair ? 2 * BM : BM, tm = (a.M + rows - 1) / rows, tn = (a.N + plan.width - 1) / plan.width;
     if (tm * tn > 0x7fffffff / 8) return SPDY_ERR_UNSUPPORTED;
     a.tiles_m = static_cast<int>(tm), a.tiles_n = static_cast<int>(tn);
     CUtensorMap mx, mw;
-    int rc = make_map(&mx, a.x, a.ldx, a.M, a.K, a.dtype, BM);
+    rc = make_map(&mx, a.x, a.ldx, a.M, a.K, a.dtype, BM);
     if (rc == SPDY_OK) rc = make_map(&mw, a.w, a.ldw, a.N, a.K, a.dtype, plan.mode == kPair ? plan.width / 2 : plan.width);
     if (rc != SPDY_OK) return rc;
     if (plan.mode == kSplit) return launch_tiles<T, 64, ACT, kSplit>(mx, mw, a, plan.parts, s);

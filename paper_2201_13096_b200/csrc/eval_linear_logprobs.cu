@@ -1416,11 +1416,7 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
         p.from[1] = static_cast<const uint16_t *>(h.weight), p.ld[1] = h.ldw, p.rows[1] = V, p.to[1] = reinterpret_cast<uint16_t *>(ws + l.weight);
         h.weight = ws + l.weight, h.ldw = p.ldto;
     }
-    if (p.to[0] || p.to[1]) {
-        const int64_t rows = p.rows[0] > p.rows[1] ? p.rows[0] : p.rows[1], blocks = div_up(rows * (p.ldto / 8), kRepackBlock);
-        repack_kernel<<<dim3(static_cast<unsigned>(blocks < 2368 ? blocks : 2368), 2), 256, 0, s>>>(p);
-        HEAD_TRY(finish_launch());
-    }
+    HEAD_TRY(repack(p, s));
     CUtensorMap hidden = {}, weight = {};
     if (!few) {
         HEAD_TRY(map_of(&hidden, h.hidden, h.ldh, R, D, h.dtype, BM));

@@ -188,20 +188,21 @@ struct Repack {
     int64_t ld[2], rows[2], K, ldto;
 };
 // A thread copies eight elements of a row at a time, from the two aligned blocks of 16 bytes around them where these lie inside the matrix,
-// and two such copies together, which keeps more loads under way (50001 rows of 1000 elements, an odd stride: 53 us with words of 4 bytes,
-// 50 with blocks, 44 with two, 44 with four).  What lies behind K is whatever (TMA never reads it).  A block walks over several
-// copies: with a block for each 512 the same took 82 us.
+// and two such copies together, which keeps more loads under way.  What lies behind K is whatever (TMA never reads it).  50001 rows of
+// 1000 elements, an odd stride: 31 us, 6.4 TB/s (53 us with words of 4 bytes; 43 with the parameters not in constant memory, which
+// `which` indexes, but copied by each thread; one copy at a time cost 6 us more than two, four as much as two).
 constexpr int kRepackBlock = 512;  // copies
-static __global__ void __launch_bounds__(256) repack_kernel(const Repack p)
+// I: a division by a 64-bit number costs more than the copy, so it is done where the copies pass 32 bits only.
+template <class I> __global__ void __launch_bounds__(256) repack_kernel(const __grid_constant__ Repack p)
 {
     constexpr int kAtOnce = kRepackBlock / 256;
     const int which = blockIdx.y;
     if (!p.to[which]) return;
-    const int64_t per_row = p.ldto / 8, total = p.rows[which] * per_row, ld = p.ld[which];
+    const I per_row = static_cast<I>(p.ldto / 8), total = static_cast<I>(p.rows[which]) * per_row;
+    const int64_t ld = p.ld[which];
     const uint16_t *const matrix = p.from[which];
     const uintptr_t first = reinterpret_cast<uintptr_t>(matrix), end = first + static_cast<uint64_t>((p.rows[which] - 1) * ld + p.K) * 2;
-    const bool small = total < (1ll << 32);  // a division by a 64-bit number costs more than the copy
-    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kRepackBlock + threadIdx.x; i0 < total; i0 += static_cast<int64_t>(gridDim.x) * kRepackBlock) {
+    for (I i0 = static_cast<I>(blockIdx.x) * kRepackBlock + threadIdx.x; i0 < total; i0 += static_cast<I>(gridDim.x) * kRepackBlock) {
         uint4 a[kAtOnce], b[kAtOnce];
         const uint16_t *from[kAtOnce];
         int64_t place[kAtOnce];
@@ -209,8 +210,8 @@ static __global__ void __launch_bounds__(256) repack_kernel(const Repack p)
         bool inside[kAtOnce];
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u) {
-            const int64_t i = i0 + u * 256;
-            const int64_t r = small ? static_cast<uint32_t>(i) / static_cast<uint32_t>(per_row) : i / per_row, k = (i - r * per_row) * 8;
+            const I i = i0 + u * 256;
+            const int64_t r = i / per_row, k = static_cast<int64_t>(i - static_cast<I>(r) * per_row) * 8;
             from[u] = matrix + r * ld + k, place[u] = r * p.ldto + k;
             left[u] = i < total ? static_cast<int>(min(p.K - k, static_cast<int64_t>(8))) : 0;
             const uintptr_t at = reinterpret_cast<uintptr_t>(from[u]) & ~static_cast<uintptr_t>(15);
@@ -238,6 +239,18 @@ static __global__ void __launch_bounds__(256) repack_kernel(const Repack p)
             *reinterpret_cast<uint4 *>(p.to[which] + place[u]) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
+}
+
+// Both copies, where there are any.
+static inline int repack(const Repack &p, cudaStream_t s)
+{
+    if (!p.to[0] && !p.to[1]) return SPDY_OK;
+    constexpr int64_t most = 148 * 16;
+    const int64_t rows = p.rows[0] > p.rows[1] ? p.rows[0] : p.rows[1], copies = rows * (p.ldto / 8), want = (copies + kRepackBlock - 1) / kRepackBlock;
+    const dim3 grid(static_cast<unsigned>(want < most ? want : most), 2);
+    if (copies + (most + 1) * kRepackBlock < (1ll << 32)) repack_kernel<uint32_t><<<grid, 256, 0, s>>>(p);
+    else repack_kernel<uint64_t><<<grid, 256, 0, s>>>(p);
+    return finish_launch();
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
