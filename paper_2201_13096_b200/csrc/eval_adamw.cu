@@ -109,7 +109,7 @@ template <bool SIGNED, int N> __device__ __forceinline__ void encode(float *y, c
     if (field < 1) {  // no float: the way down in two steps, of which the first is exact for all that is left after the second
         field += 113;
 #pragma unroll
-        for (int i = 0; i < N; ++i) y[i] *= 0x1p-113f;
+        for (int i = 0; i < N; ++i) y[i] = !SIGNED && y[i] > 0.f ? fmaxf(y[i] * 0x1p-113f, 0x1p-149f) : y[i] * 0x1p-113f;  // positive stays positive, for the floor below
     }
     if (bad) E = 255;
     const float factor = exponent(max(field, 1));

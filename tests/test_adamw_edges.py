@@ -1,0 +1,33 @@
+"""AdamW steps at the edges of their formats and of autograd (include/spdy_eval.h, spdy_adamw_*)."""
+import math
+
+import pytest
+import torch
+
+import eval_reference as ref
+import tune_reference as tune
+from paper_2201_13096_b200 import build as build_mod, evaluate
+from test_adamw import gradient, snapshot, values
+
+gpu = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    build_mod.build()
+
+
+@gpu
+@pytest.mark.parametrize("large,small", [(1.0, 1e-12), (1e6, 1e-3), (1e6, 1e-12), (1e8, 1e-5), (1e12, 1e-1), (1e18, 1e-3), (1e20, 1e-18)])
+def test_second_moments_beside_large_ones_have_a_floor(large, small):
+    # 0.001 g^2 of the large one is 2^10 to 2^126: the conversion's power of two is no float of one step from 2^30 on.  The small one's is a positive
+    # number, 2^-32 of the largest or less, and has to stay one.
+    g = torch.zeros(64, device="cuda")
+    g[0], g[1], g[17], g[40] = large, small, small, small  # the last in a block of its own
+    plan = evaluate.AdamW([torch.ones(64, device="cuda")], bits=8)
+    evaluate.adamw_step(plan, [g], lr=0.0, step=1)
+    v = evaluate.adamw_moments(plan)[0][1].double()
+    assert abs(float(v[0]) / (0.001 * float(g[0].double()) ** 2) - 1) <= 2.0 ** -3  # a step of the mantissa's three bits
+    unit = 2.0 ** (math.floor(math.log2(0.001 * float(g[0].double()) ** 2)) - 32)
+    assert float(v[1]) == float(v[17]) == unit  # the least number of the block
+    assert float(v[40]) > 0 and int((v > 0).sum()) == 4
