@@ -339,10 +339,11 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
             second = __fadd2_rn(__fmul2_rn(second, both(s.b2)), __fmul2_rn(__fmul2_rn(slope, both(s.g2)), slope));
             m[i] = first.x, m[i + 1] = first.y, v[i] = second.x, v[i + 1] = second.y;
         }
-        if (keep)  // and the weight, with m = 0, stays 0 by itself
+        uint32_t zeros = 0;  // weights that stay 0, whatever the rate and the decay (0 times an infinite one would be NaN)
+        if (keep)
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (p[i] == 0.f) m[i] = v[i] = 0.f;
+                if (p[i] == 0.f) m[i] = v[i] = 0.f, zeros |= 1u << i;
         if (s.eps >= 1e-9f) {  // roots of numbers below 2^-126 do not show beside such an eps
 #pragma unroll
             for (int i = 0; i < N; i += 2) {
@@ -352,8 +353,12 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) p[i] = keep && p[i] == 0.f ? 0.f : fmaf(p[i], decay, -quotient(m[i] * rate, fmaf(root_of(v[i]), root, s.eps)));
+            for (int i = 0; i < N; ++i) p[i] = fmaf(p[i], decay, -quotient(m[i] * rate, fmaf(root_of(v[i]), root, s.eps)));
         }
+        if (zeros)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (zeros >> i & 1) p[i] = 0.f;
         uint32_t random[N];
         if (BITS == 8 || RANDOM) {
             const uint32_t start = mix(key + t.index) + static_cast<uint32_t>(e) + static_cast<uint32_t>(e >> 32) * 0x9e3779b9u;

@@ -31,3 +31,20 @@ def test_second_moments_beside_large_ones_have_a_floor(large, small):
     unit = 2.0 ** (math.floor(math.log2(0.001 * float(g[0].double()) ** 2)) - 32)
     assert float(v[1]) == float(v[17]) == unit  # the least number of the block
     assert float(v[40]) > 0 and int((v > 0).sum()) == 4
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype,master", [(torch.float32, False), (torch.bfloat16, True), (torch.float16, False)])
+@pytest.mark.parametrize("rate,decay,eps", [(math.inf, 0.0, 1e-8), (math.nan, 0.1, 1e-8), (1e30, 3e38, 1e-8), (math.inf, 0.1, 0.0), (1e30, 3e38, 0.0), (0.1, 0.1, 0.0)])
+def test_zeros_are_kept_whatever_the_rate(rate, decay, eps, dtype, master, bits):
+    for n in (77, 4096):
+        w = (values(n, 1) * (values(n, 2) > 0)).cuda().to(dtype)
+        gone = w == 0
+        plan = evaluate.AdamW([w], bits=bits, masters=True if master else None, weight_decay=decay, eps=eps, keep_zeros=True)
+        lr, step = torch.full((1,), rate, device="cuda"), torch.ones(1, dtype=torch.int64, device="cuda")
+        for given in ((lr, step), (rate, 1)) if math.isfinite(rate) else ((lr, step),):
+            evaluate.adamw_step(plan, [gradient(n, 3).cuda().to(dtype)], lr=given[0], step=given[1])
+            assert (w[gone] == 0).all() and 0 < int(gone.sum()) < n
+            for t in plan.masters + [m for pair in evaluate.adamw_moments(plan) for m in pair]:
+                assert t is None or (t[gone] == 0).all()
