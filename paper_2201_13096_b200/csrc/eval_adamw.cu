@@ -267,7 +267,7 @@ __device__ __forceinline__ float root_flushed(float x)
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// a / b; b is 0 or far from fp32's ends, and quotients below 2^-126 change no weight
+// a / b; b is 0 or a normal number far from the largest, and quotients below 2^-126 change no weight
 __device__ __forceinline__ float quotient(float a, float b)
 {
     float y;
@@ -353,7 +353,10 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) p[i] = fmaf(p[i], decay, -quotient(m[i] * rate, fmaf(root_of(v[i]), root, s.eps)));
+            for (int i = 0; i < N; ++i) {
+                const float below = fmaf(root_of(v[i]), root, s.eps), up = below < 0x1p-60f ? 0x1p60f : 1.f;  // numbers below 2^-126 would count as 0
+                p[i] = fmaf(p[i], decay, -quotient(m[i] * rate * up, below * up));
+            }
         }
         if (zeros)
 #pragma unroll
@@ -509,7 +512,8 @@ int spdy_adamw_step(const spdy_adamw_tensor *tensors, int32_t count, const spdy_
         if (!tensor_ok(tensors[i])) return SPDY_ERR_INVALID_ARG;
     StepArgs s = {};
     s.b1 = static_cast<float>(o->beta1), s.b2 = static_cast<float>(o->beta2);
-    s.g1 = static_cast<float>(1.0 - o->beta1), s.g2 = static_cast<float>(1.0 - o->beta2), s.eps = static_cast<float>(o->eps);
+    s.g1 = static_cast<float>(1.0 - o->beta1), s.g2 = static_cast<float>(1.0 - o->beta2);
+    s.eps = o->eps > 0.0 ? fmaxf(static_cast<float>(o->eps), 0x1p-149f) : 0.f;  // one that is there does not become 0: 0 / eps is 0
     s.lr = o->lr, s.beta1 = o->beta1, s.beta2 = o->beta2;
     const double t = static_cast<double>(o->step);
     s.rate = static_cast<float>(o->lr / (1.0 - pow(o->beta1, t))), s.root = static_cast<float>(1.0 / sqrt(1.0 - pow(o->beta2, t)));

@@ -48,3 +48,25 @@ def test_zeros_are_kept_whatever_the_rate(rate, decay, eps, dtype, master, bits)
             assert (w[gone] == 0).all() and 0 < int(gone.sum()) < n
             for t in plan.masters + [m for pair in evaluate.adamw_moments(plan) for m in pair]:
                 assert t is None or (t[gone] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("eps", [1e-60, 1e-45, 1e-39, 1e-37, 1e-30, 1e-12])
+def test_an_eps_below_the_normal_numbers(eps):
+    # no gradient and no moments: 0 / eps is 0, and the weights stay
+    w = values(100, 1).cuda()
+    before = w.clone()
+    plan = evaluate.AdamW([w], weight_decay=0.0, eps=eps)
+    evaluate.adamw_step(plan, [torch.zeros(100, device="cuda")], lr=0.1, step=1)
+    assert torch.equal(w, before)
+    # a moment of eps's size beside a second one of 0: m / eps, where fp32 has it.  Roundings of 0.9 m and of it times the rate, at least 2^-150 of fp32's
+    # least normal numbers each, quotient and decay as the header has them.
+    small = float(torch.tensor(eps, dtype=torch.float64).float())
+    if small < 1e-39:
+        return
+    m = torch.full((100,), 10.0, dtype=torch.float64).mul(small).float()
+    plan = evaluate.AdamW([w], weight_decay=0.0, eps=eps, moments=[evaluate.AdamWMoments(m.cuda(), torch.zeros(100, device="cuda"))])
+    evaluate.adamw_step(plan, [torch.zeros(100, device="cuda")], lr=1.0, step=100000)
+    change = 0.9 * m.double() / small
+    cut = 2 * 2.0 ** -150 / (9 * small) + 2.0 ** -21 + 2.0 ** -22
+    assert ((ref.d64(w) - (ref.d64(before) - change)).abs() <= change * cut + 2.0 ** -23 * 10).all()
