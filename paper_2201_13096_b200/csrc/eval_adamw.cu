@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 if (p[i] == 0.f) m[i] = v[i] = 0.f, zeros |= 1u << i;
-        if (s.eps >= 1e-9f) {  // roots of numbers below 2^-126 do not show beside such an eps
+        if (s.eps >= 1e-9f && s.eps >= 1e-12f * root) {  // roots of numbers below 2^-126, 2^-63 times `root`, do not show beside such an eps
 #pragma unroll
             for (int i = 0; i < N; i += 2) {
                 const float2 above = __fmul2_rn(make_float2(m[i], m[i + 1]), both(rate)), below = __ffma2_rn(make_float2(root_flushed(v[i]), root_flushed(v[i + 1])), both(root), both(s.eps));

@@ -70,3 +70,18 @@ def test_an_eps_below_the_normal_numbers(eps):
     change = 0.9 * m.double() / small
     cut = 2 * 2.0 ** -150 / (9 * small) + 2.0 ** -21 + 2.0 ** -22
     assert ((ref.d64(w) - (ref.d64(before) - change)).abs() <= change * cut + 2.0 ** -23 * 10).all()
+
+
+@gpu
+@pytest.mark.parametrize("beta2", [0.999, 1 - 1e-9, 1 - 1e-12])
+def test_second_moments_below_the_normal_numbers(beta2):
+    # a first step from 0: m / (1 - beta1) = g, and sqrt(v / (1 - beta2)) = |g| shows beside eps although v itself is below 2^-126
+    g = torch.logspace(-16, -11, 200, dtype=torch.float64).float()
+    w = torch.zeros(200, device="cuda")
+    plan = evaluate.AdamW([w], weight_decay=0.0, eps=1e-9, betas=(0.9, beta2))
+    evaluate.adamw_step(plan, [g.cuda()], lr=1.0, step=1)
+    want = -g.double() / (g.double() + 1e-9)
+    v = (1 - beta2) * g.double() ** 2
+    # v is off by up to 2^-149 (its factor's product and its own) beside the relative errors, at most all of it; the rest as in tune_reference.adamw
+    off = (2.0 ** -149 / v).clamp(max=1.0) * g.double() / (g.double() + 1e-9)
+    assert ((ref.d64(w) - want).abs() <= want.abs() * (off + 2.0 ** -18)).all()
