@@ -689,7 +689,10 @@ class AdamW:
         self._shapes = [tuple(p.shape) for p in self.params]
         self._strides = [p.stride() for p in self.params]
         self._dtypes = [p.dtype for p in self.params]
-        self._leaves = [p for p in self.params if p.requires_grad]
+        # What autograd may have saved, whether or not it requires a gradient itself: not the 8-bit codes, nor what inference mode made.
+        self._seen = [[t for t in (p, master, *mom[:2]) if t is not None and t.is_floating_point() and not t.is_inference()]
+                      for p, master, mom in zip(self.params, self.masters, self.moments)]
+        self._all_seen = [t for tensors in self._seen for t in tensors]
 
     def _fresh(self, n: int) -> AdamWMoments:
         if self.bits == 32:
@@ -767,8 +770,10 @@ def adamw_step(plan: AdamW, grads, lr, step, seed: int = 0, grad_scale=None, ski
         rc = lib.spdy_adamw_step(words.ctypes.data, len(pointers), ctypes.byref(o), handle)
     if rc:
         binding._check(rc, "spdy_adamw_step")
-    if plan._leaves:  # a graph that was recorded before must notice
-        torch.autograd.graph.increment_version(plan._leaves)
+    # A graph that was recorded before must notice, as with every operation in place.
+    seen = plan._all_seen if 0 not in pointers else [t for tensors, g in zip(plan._seen, grads) if g is not None for t in tensors]
+    if seen:
+        torch.autograd.graph.increment_version(seen)
 
 
 def adamw_moments(plan: AdamW, dtype=None, stream=None):

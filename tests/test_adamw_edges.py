@@ -85,3 +85,56 @@ def test_second_moments_below_the_normal_numbers(beta2):
     # v is off by up to 2^-149 (its factor's product and its own) beside the relative errors, at most all of it; the rest as in tune_reference.adamw
     off = (2.0 ** -149 / v).clamp(max=1.0) * g.double() / (g.double() + 1e-9)
     assert ((ref.d64(w) - want).abs() <= want.abs() * (off + 2.0 ** -18)).all()
+
+
+def _frozen(w):
+    return w
+
+
+def _detached(w):
+    return w.detach()
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("taken", [_frozen, _detached])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_graphs_notice_steps_on_weights_that_require_no_gradient(dtype, taken, bits):
+    w = torch.randn(64, 8, device="cuda").to(dtype)
+    plan = evaluate.AdamW([taken(w), torch.ones(5, device="cuda")], bits=bits, masters=[torch.zeros(64 * 8, device="cuda") if dtype != torch.float32 else None, None])
+    grads = [torch.ones(64, 8, device="cuda", dtype=dtype), None]
+    x = torch.randn(3, 8, device="cuda").to(dtype).requires_grad_()
+    saved = [w, plan.params[1]] + ([plan.masters[0]] if plan.masters[0] is not None else []) + ([plan.moments[0].m, plan.moments[0].v] if bits == 32 else [])
+    for t in saved:
+        y = (x @ t.T).sum() if t is w else (t * torch.ones_like(t).requires_grad_()).sum()
+        before = t._version
+        evaluate.adamw_step(plan, grads, lr=0.1, step=1)
+        if t is plan.params[1]:  # no gradient, no step
+            assert t._version == before
+            y.backward()
+            continue
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
+
+
+@gpu
+def test_graphs_notice_steps_on_a_weight_unfrozen_later():
+    w = torch.randn(64, device="cuda")
+    plan = evaluate.AdamW([w])
+    w.requires_grad_()
+    y = (w * w).sum()
+    evaluate.adamw_step(plan, [torch.ones(64, device="cuda")], lr=0.1, step=1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    (w * w).sum().backward()  # and after the step it is a leaf like any other
+    assert torch.equal(w.grad, 2 * w.detach())
+
+
+@gpu
+def test_tensors_of_inference_mode_can_be_stepped():
+    with torch.inference_mode():
+        w = torch.ones(64, device="cuda")
+        plan = evaluate.AdamW([w])
+        evaluate.adamw_step(plan, [torch.ones(64, device="cuda")], lr=0.1, step=1)
+    evaluate.adamw_step(plan, [torch.ones(64, device="cuda")], lr=0.1, step=2)
+    assert (w < 0.9).all()
