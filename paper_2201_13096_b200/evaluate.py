@@ -191,6 +191,14 @@ def _like(t, what: str, rows: int, cols: int, dtype, device: int) -> int:
     return ld
 
 
+def _out(t, what: str, rows: int, cols: int, dtype, device: int) -> int:
+    """The same of a matrix that the caller gives to be written: a graph that saved it before must notice."""
+    ld = _like(t, what, rows, cols, dtype, device)
+    if not t.is_inference():
+        torch.autograd.graph.increment_version(t)
+    return ld
+
+
 def _vector(t, what: str, n: int, device: int, dtype=None):
     if t.requires_grad:
         _refuse_gradient(what)
@@ -268,7 +276,7 @@ def linear(x, weight, bias=None, residual=None, activation: str = "none", out=No
         else:
             if out_dtype is not None and out.dtype != out_dtype:
                 raise ValueError("out must have out_dtype")
-            ldy = _like(out, "out", M, N, out.dtype, dev)
+            ldy = _out(out, "out", M, N, out.dtype, dev)
         ocode = _TYPES.get(out.dtype, -1)
         if ocode and ocode != code:
             raise ValueError("the result must have x's type or be float32")
@@ -314,7 +322,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=No
         if out is None:
             out, ldy = _matrix(R, D, x.dtype), D
         else:
-            ldy = _like(out, "out", R, D, x.dtype, dev)
+            ldy = _out(out, "out", R, D, x.dtype, dev)
         mean, rstd = _vectors(2, R)
         rc = lib.spdy_layer_norm(x.data_ptr(), ldx, code, _ptr(weight), _ptr(bias), kind, R, D, eps, out.data_ptr(), ldy,
                                  mean.data_ptr(), rstd.data_ptr(), handle)
@@ -337,7 +345,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, out=None, params: bool = True
         if out is None:
             out, lddx = _matrix(R, D, x.dtype), D
         else:
-            lddx = _like(out, "out", R, D, x.dtype, dev)
+            lddx = _out(out, "out", R, D, x.dtype, dev)
         dw = db = pw = pb = pws = None
         need = 0
         if params:
@@ -363,7 +371,7 @@ def _logits(logits):
 def _grads_out(out, logits, R, V, dev):
     if out is None:
         return _matrix(R, V, logits.dtype), V
-    return out, _like(out, "out", R, V, logits.dtype, dev)
+    return out, _out(out, "out", R, V, logits.dtype, dev)
 
 
 def _optional(R, dev, **vectors):
@@ -463,12 +471,12 @@ def _head_grads(hidden, weight, bias, R, V, D, dev, wanted, dhidden, dweight):
         if dhidden is None:
             dhidden = _matrix(R, D, hidden.dtype)
         else:
-            ldh = _like(dhidden, "dhidden", R, D, hidden.dtype, dev)
+            ldh = _out(dhidden, "dhidden", R, D, hidden.dtype, dev)
     if "weight" in wanted:
         if dweight is None:
             dweight = _matrix(V, D, hidden.dtype)
         else:
-            ldw = _like(dweight, "dweight", V, D, hidden.dtype, dev)
+            ldw = _out(dweight, "dweight", V, D, hidden.dtype, dev)
     dbias = _vectors(1, V)[0] if "bias" in wanted and bias is not None else None
     return LinearGrads(dhidden, dweight, dbias), (_ptr(dhidden), ldh, _ptr(dweight), ldw, _ptr(dbias))
 
