@@ -44,11 +44,17 @@ __device__ __forceinline__ void wait_for_previous()
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// The tensor core cuts its partial sums towards 0 where fp32 additions would round, so that a sum of D products ends short of itself, by
-// this much for each product: 0.75e-9 to 1.0e-9 of it in bf16, 1.0e-9 to 1.1e-9 in half precision (D 64 to 8192, operands of both signs;
-// where all products are positive, 1.2e-9 to 6.5e-9).  Logits get it back: the loss is the same for all of them, and at D = 4096 it
-// moved lse by 4e-6 of itself, and dbias, where gradients of many rows nearly cancel, by more.
-constexpr float kLoss = 0.95e-9f;
+// The tensor core cuts its partial sums towards 0 where fp32 additions would round: a sum of many products ends short of itself, by how much
+// depends on the data.  The sums that logits are go into several accumulators therefore, `most` stages to each at most, which the epilogue adds up in
+// fp32.  How far lse is off, relative, at widths 256 to 16384 (and at 4096 with positive products in half precision; the plain fp32 form 0.8e-7 to 1.1e-6):
+// 1 stage 0.9e-7 to 1.4e-7 (2.9e-7), 2 stages 1.6e-7 to 2.8e-7 (7.0e-7), 4 stages 3.3e-7 to 4.8e-7 (1.6e-6), all in one 2.2e-6 at 2624 already.  2048 x
+// 131072 x 2048 964, 887, 855 and 851 us (a slow card).  Logits take 2.
+constexpr int kPieceLogits = 2, kPieceGrad = 4;
+int piece_stages(int64_t D, int most)
+{
+    const int64_t stages = (D + kStageK - 1) / kStageK, pieces = (stages + most - 1) / most;
+    return static_cast<int>((stages + pieces - 1) / pieces);
+}
 
 enum Kind { kStats, kLogits, kGrad, kHidden, kWeight, kWeightParts };
 
@@ -56,6 +62,7 @@ enum Kind { kStats, kLogits, kGrad, kHidden, kWeight, kWeightParts };
 template <int KIND> struct Order {
     static constexpr bool kA = KIND == kWeight || KIND == kWeightParts, kB = kA || KIND == kHidden;
 };
+template <int KIND> constexpr bool kInPieces = KIND == kStats || KIND == kLogits || KIND == kGrad;
 
 struct ProductArgs {
     int64_t M, N;                  // rows and columns of the result that exist
@@ -67,7 +74,8 @@ struct ProductArgs {
     const void *bias, *tokens;
     int bias_type, index_bits;
     int64_t v0;                    // the first column's id
-    float c, loss;                 // log2(e) / T; what a logit has lost of itself
+    float c;                       // log2(e) / T
+    int piece;                     // stages of the summed index to an accumulator
     float *partial, *token_logit;  // [tiles_n][3][padded_rows], [M]
     int64_t padded_rows;
     const float *consts;           // [M][kConsts]
@@ -157,7 +165,7 @@ template <class Each> __device__ __forceinline__ void add_exponentials(const flo
 
 // ---------------------------------------------------------------------------------------------- what is done with a tile
 // Each function carries 64 columns of a warp's 32 rows, a row to a lane.  `ready` waits for the accumulator and says whether it came
-// (if not, what is written is NaN); `release` is called once the last columns have left TMEM.
+// (if not, what is written is NaN), and only then is `tmem` where it lies; `release` is called once the last columns have left TMEM.
 
 // The ids' bias in the warp's shared memory.
 __device__ __forceinline__ void stage_bias(const ProductArgs &a, int64_t n0, float *bias)
@@ -171,11 +179,6 @@ __device__ __forceinline__ void stage_bias(const ProductArgs &a, int64_t n0, flo
 __device__ __forceinline__ void load_logits(const ProductArgs &a, uint32_t tmem, int64_t n, const float *bias, float *f)
 {
     tmem_load32(tmem, f);
-#pragma unroll
-    for (int i = 0; i < 32; i += 2) {
-        const float2 x = make_float2(f[i], f[i + 1]), y = fma2(x, both(a.loss), x);
-        f[i] = y.x, f[i + 1] = y.y;
-    }
     if (a.bias) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -212,7 +215,7 @@ __device__ __forceinline__ float largest(const float *f, float top)
 }
 
 template <class Ready, class Release>
-__device__ __forceinline__ Sums carry_stats(const ProductArgs &a, uint32_t tmem, int64_t m, int64_t n0, float *bias, Ready ready, Release release)
+__device__ __forceinline__ Sums carry_stats(const ProductArgs &a, const uint32_t &tmem, int64_t m, int64_t n0, float *bias, Ready ready, Release release)
 {
     int64_t token = -1;
     if (m < a.M && a.token_logit) token = token_at(a.tokens, a.index_bits, m);
@@ -246,7 +249,7 @@ template <bool FINE> constexpr float kLastCode = FINE ? 8388607.f : 65535.f;
 // As carry_stats, with the codes, and per 32 of them the largest, which they are relative to.
 constexpr int kCodes = 32;
 template <class T, bool FINE, class Ready, class Release>
-__device__ __forceinline__ Sums carry_logits(const ProductArgs &a, uint32_t tmem, int64_t m, int64_t n0, float *bias, Ready ready, Release release)
+__device__ __forceinline__ Sums carry_logits(const ProductArgs &a, const uint32_t &tmem, int64_t m, int64_t n0, float *bias, Ready ready, Release release)
 {
     int64_t token = -1;
     if (m < a.M && a.token_logit) token = token_at(a.tokens, a.index_bits, m);
@@ -331,7 +334,7 @@ template <bool ENT> __device__ __forceinline__ float grad_at(float y, const RowC
 
 // Gradient by 64 logits of a row, rounded to 16 bits once.
 template <class T, bool ENT, class Ready, class Release>
-__device__ __forceinline__ void carry_grad(const ProductArgs &a, uint32_t tmem, int64_t m0, int64_t n0, float *bias, Ready ready, Release release)
+__device__ __forceinline__ void carry_grad(const ProductArgs &a, const uint32_t &tmem, int64_t m0, int64_t n0, float *bias, Ready ready, Release release)
 {
     const int lane = threadIdx.x & 31;
     const int64_t m = m0 + lane;
@@ -548,11 +551,15 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 a.tiles.at(static_cast<uint32_t>(item), split, tm, tn);
                 range(split, kb0, kb1);
                 if (kb0 == kb1) continue;
-                ok = __all_sync(0xffffffffu, barrier_wait(&ctl.acc_empty[acc], acc_parity ^ 1));
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t d = tmem + acc * kTile;
-                for (int kb = kb0; kb < kb1; ++kb) {
+                uint32_t d = 0;
+                for (int kb = kb0, piece = 0; kb < kb1; ++kb) {
+                    const bool begins = kInPieces<KIND> ? piece == 0 : kb == kb0, ends = (kInPieces<KIND> && ++piece == a.piece) || kb + 1 == kb1;
+                    if (begins) {
+                        ok = __all_sync(0xffffffffu, barrier_wait(&ctl.acc_empty[acc], acc_parity ^ 1));
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        d = tmem + acc * kTile;
+                    }
                     ok = __all_sync(0xffffffffu, barrier_wait(&ctl.full[stage], parity));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -564,16 +571,19 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                             const uint64_t da = kColumnsA ? operand_by_columns(pa) : operand(pa), db = kColumnsB ? operand_by_columns(pb) : operand(pb);
                             // 16 of the summed index further: 32 bytes along a row, or 16 rows of 128 bytes
 #pragma unroll
-                            for (int k = 0; k < BK / 16; ++k) mma<true>(d, da + (kColumnsA ? 128 : 2) * k, db + (kColumnsB ? 128 : 2) * k, idesc, kb > kb0 || q > 0 || k > 0);
+                            for (int k = 0; k < BK / 16; ++k) mma<true>(d, da + (kColumnsA ? 128 : 2) * k, db + (kColumnsB ? 128 : 2) * k, idesc, !begins || q > 0 || k > 0);
                         }
                         mma_commit<true>(&ctl.empty[stage]);
-                        if (kb + 1 == kb1) mma_commit<true>(&ctl.acc_full[acc]);
+                        if (ends) mma_commit<true>(&ctl.acc_full[acc]);
                     }
                     __syncwarp();
                     ++issued;
                     if (++stage == kStages) stage = 0, parity ^= 1;
+                    if (ends) {
+                        piece = 0;
+                        if (++acc == 2) acc = 0, acc_parity ^= 1;
+                    }
                 }
-                if (++acc == 2) acc = 0, acc_parity ^= 1;
             }
             // nor does a product: TMEM is freed once the last one issued is done
             if (issued > 0) barrier_wait(&ctl.empty[(issued - 1) % kStages], (issued - 1) / kStages & 1);
@@ -582,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         // warps 2 to 17: a warp reaches the quarter of TMEM's rows that its number names modulo four
         const int quarter = warp & 3, group = (warp - 2) >> 2;
         float *bias = reinterpret_cast<float *>(extra) + (warp - 2) * kWarpColumns;
-        int acc = 0;
+        int acc = 0, room_of = 0;
         uint32_t acc_parity = 0;
         bool ok = true;
         for (int item = first; item < items; item += step) {
@@ -591,7 +601,9 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             range(split, kb0, kb1);
             if (kb0 == kb1) continue;
             const int64_t m0 = static_cast<int64_t>(tm) * kTile + part * BM + quarter * 32, n0 = static_cast<int64_t>(tn) * kTile + group * kWarpColumns;
-            const auto ready = [&] {  // once a wait has run out, nothing is waited for any more
+            const auto here = [&] { return tmem + acc * kTile + group * kWarpColumns + (static_cast<uint32_t>(quarter * 32) << 16); };
+            uint32_t at = here();
+            const auto arrived = [&] {  // once a wait has run out, nothing is waited for any more
                 ok = ok && __all_sync(0xffffffffu, barrier_wait(&ctl.acc_full[acc], acc_parity));
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 return ok;
@@ -601,13 +613,40 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 __syncwarp();
                 if (lane == 0) barrier_arrive_at(first_blocks(smem_addr(&ctl.acc_empty[acc])));
             };
-            const uint32_t at = tmem + acc * kTile + group * kWarpColumns + (static_cast<uint32_t>(quarter * 32) << 16);
+            const auto next = [&] {
+                if (++acc == 2) acc = 0, acc_parity ^= 1;
+                at = here();
+            };
+            // Pieces of a sum are added up in registers, and the whole goes back to where the last one lies.
+            const auto ready = [&] {
+                if constexpr (kInPieces<KIND>) {
+                    if (a.k_blocks > a.piece) {
+                        float sum[kWarpColumns];
+#pragma unroll
+                        for (int i = 0; i < kWarpColumns; ++i) sum[i] = 0.f;
+#pragma unroll 1
+                        for (int left = a.k_blocks;; left -= a.piece) {
+                            if (!arrived()) return false;
+#pragma unroll
+                            for (int c = 0; c < kWarpColumns; c += 8) tmem_add8(at + c, sum + c);
+                            if (left <= a.piece) break;
+                            release(), next();
+                        }
+#pragma unroll
+                        for (int c = 0; c < kWarpColumns; c += 32) tmem_store32(at + c, sum + c);
+                        tmem_stores_wait();
+                        return true;
+                    }
+                }
+                return arrived();
+            };
             if (KIND == kStats || KIND == kLogits) {
                 Sums mine;
                 if constexpr (KIND == kLogits) mine = carry_logits<T, ENT>(a, at, m0 + lane, n0, bias, ready, release);
                 else mine = carry_stats(a, at, m0 + lane, n0, bias, ready, release);
                 // the four warps of these rows join their columns; two rooms, so that one barrier a tile is enough
-                float *room = reinterpret_cast<float *>(extra + kBiasBytes) + ((acc * 4 + quarter) * 4) * 96 + lane;
+                float *room = reinterpret_cast<float *>(extra + kBiasBytes) + ((room_of * 4 + quarter) * 4) * 96 + lane;
+                room_of ^= 1;
                 if (group > 0) room[group * 96] = mine.m, room[group * 96 + 32] = mine.s, room[group * 96 + 64] = mine.t;
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + quarter) : "memory");
                 if (group == 0) {
@@ -626,7 +665,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             } else {
                 carry_store<T>(a, at, m0, n0, extra + (warp - 2) * 1024, ready, release);
             }
-            if (++acc == 2) acc = 0, acc_parity ^= 1;
+            next();
         }
     }
     __syncwarp();
@@ -1360,6 +1399,7 @@ template <class T> struct Head {
         a.M = h.R, a.N = n, a.v0 = v0, a.b_row0 = static_cast<int>(v0);
         a.out = ws + l.piece, a.ldo = l.ld_piece;
         if (h.dbias) a.column_sums = floats(l.sums), a.ld_sums = l.ld_piece;
+        else a.piece = piece_stages(h.D, kPieceGrad);  // g in 16 bits shows nothing of it
         if (h.grad_entropy) HEAD_TRY((launch_product<T, kGrad, true>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
         else HEAD_TRY((launch_product<T, kGrad, false>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
         return h.dbias ? finish_bias(h.R, n, v0, false) : SPDY_OK;
@@ -1430,7 +1470,7 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
     rows.grad_logprob = h.grad_logprob, rows.grad_entropy = h.grad_entropy;
     ProductArgs base = {};
     base.bias = h.bias, base.bias_type = h.bias_type, base.tokens = h.tokens, base.index_bits = h.index_bits;
-    base.c = rows.c, base.loss = kLoss * static_cast<float>(D), base.padded_rows = l.padded_rows;
+    base.c = rows.c, base.piece = piece_stages(D, kPieceLogits), base.padded_rows = l.padded_rows;
     if (h.grads) {
         rows.consts = reinterpret_cast<float *>(ws + l.consts);
         if (!few && h.dtype == SPDY_F16) {

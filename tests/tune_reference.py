@@ -9,10 +9,11 @@ import eval_reference as ref
 F16 = torch.float16
 
 
-def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu", kept=0):
+def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu", kept=0, cut=None):
     """A dict of values and, under the same name with ``_err``, of bounds on the fp32 error before the last rounding.
     ``kept``: the gradient comes from logits kept in so many bits, as a call that gives values and gradients keeps them: 16, or 23 with
-    dbias; the token's own is not among them."""
+    dbias; the token's own is not among them.
+    ``cut``: by how much of its magnitudes a logit may be off, where that is known better than from the number of products."""
     h, w = (t.detach().to(on).double() for t in (hidden, weight))
     R, D = h.shape
     V = w.shape[0]
@@ -23,12 +24,13 @@ def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu", 
     tokens = tokens.to(on).long()
     logp, p, lse = ref_softmax(x, temperature)
     # Logits: D products added in fp32, see eval_reference.linear.  Only ids with a share count: an id's error moves lse by p times itself.
-    ez = ((D / 8 + 16) * 2.0 ** -23 * size / temperature)
+    cut = (D / 8 + 16) * 2.0 ** -23 if cut is None else cut
+    ez = (cut * size / temperature)
     ez = torch.where(p > 0, ez, torch.zeros_like(ez)).nan_to_num(0.0).amax(1)
     named = (tokens >= 0) & (tokens < V)
     at = tokens.clamp(0, V - 1)[:, None]
     lp = logp.gather(1, at)[:, 0]
-    ez_token = ((D / 8 + 16) * 2.0 ** -23 * size / temperature).gather(1, at)[:, 0]
+    ez_token = (cut * size / temperature).gather(1, at)[:, 0]
     lp = torch.where(tokens < 0, torch.zeros_like(lp), torch.where(tokens >= V, torch.full_like(lp, math.nan), lp))
     spread = torch.where(p == 0, torch.zeros_like(p), p * logp)
     entropy = -spread.sum(1)
