@@ -339,12 +339,13 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
             second = __fadd2_rn(__fmul2_rn(second, both(s.b2)), __fmul2_rn(__fmul2_rn(slope, both(s.g2)), slope));
             m[i] = first.x, m[i + 1] = first.y, v[i] = second.x, v[i + 1] = second.y;
         }
-        uint32_t zeros = 0;  // weights that stay 0, whatever the rate and the decay (0 times an infinite one would be NaN)
         if (keep)
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (p[i] == 0.f) m[i] = v[i] = 0.f, zeros |= 1u << i;
-        if (s.eps >= 1e-9f && s.eps >= 1e-12f * root) {  // roots of numbers below 2^-126, 2^-63 times `root`, do not show beside such an eps
+                if (p[i] == 0.f) m[i] = v[i] = 0.f;
+        // Roots of numbers below 2^-126, 2^-63 times `root`, do not show beside such an eps; and with finite rate and decay a weight of 0 whose m is
+        // 0 stays 0 by itself.
+        if (s.eps >= 1e-9f && s.eps >= 1e-12f * root && fabsf(rate) <= 3.4e38f && fabsf(decay) <= 3.4e38f) {
 #pragma unroll
             for (int i = 0; i < N; i += 2) {
                 const float2 above = __fmul2_rn(make_float2(m[i], m[i + 1]), both(rate)), below = __ffma2_rn(make_float2(root_flushed(v[i]), root_flushed(v[i + 1])), both(root), both(s.eps));
@@ -355,13 +356,9 @@ __global__ void __launch_bounds__(kThreads<BITS>) step_kernel(const __grid_const
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float below = fmaf(root_of(v[i]), root, s.eps), up = below < 0x1p-60f ? 0x1p60f : 1.f;  // numbers below 2^-126 would count as 0
-                p[i] = fmaf(p[i], decay, -quotient(m[i] * rate * up, below * up));
+                p[i] = keep && p[i] == 0.f ? 0.f : fmaf(p[i], decay, -quotient(m[i] * rate * up, below * up));
             }
         }
-        if (zeros)
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (zeros >> i & 1) p[i] = 0.f;
         uint32_t random[N];
         if (BITS == 8 || RANDOM) {
             const uint32_t start = mix(key + t.index) + static_cast<uint32_t>(e) + static_cast<uint32_t>(e >> 32) * 0x9e3779b9u;
