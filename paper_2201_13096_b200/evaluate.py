@@ -111,7 +111,7 @@ def library():
 # PyTorch, imported with the library (the package itself imports without it).
 torch = None
 _TYPES = {}
-_current_stream = _current_device = _empty_strided = None
+_current_stream = _current_device = _empty_strided = _new_versions = None
 
 
 def _checked(fast, plain, same):
@@ -128,8 +128,14 @@ def _same_memory(fast, plain):
     return all(f(a) == f(b) for f in (type, lambda t: t.shape, lambda t: t.stride(), lambda t: t.dtype, lambda t: t.device, lambda t: t.requires_grad))
 
 
+def _same_versions(fast, plain):
+    a, b = torch.zeros(2), torch.zeros(2)
+    fast([a, b]), plain([b])
+    return a._version == 1 and b._version == 2
+
+
 def _import_torch():
-    global torch, _current_stream, _current_device, _empty_strided
+    global torch, _current_stream, _current_device, _empty_strided, _new_versions
     import torch as t
 
     torch = t
@@ -138,6 +144,8 @@ def _import_torch():
     # uninitialised memory on the current device by (shape, strides, type), without the general call's argument parsing.
     _current_stream, _current_device = lambda i: t.cuda.current_stream(i).cuda_stream, t.cuda.current_device
     _empty_strided = lambda shape, strides, dtype: t.empty_strided(shape, strides, dtype=dtype, device="cuda")  # noqa: E731
+    # A list of tensors that have been changed in place, without a test of what it is.
+    _new_versions = _checked(getattr(t._C, "_increment_version", None), t.autograd.graph.increment_version, _same_versions)
     if t.cuda.is_available():
         _current_device = _checked(getattr(t._C, "_cuda_getDevice", None), _current_device, lambda f, p: f() == p())
         _current_stream = _checked(getattr(t._C, "_cuda_getCurrentRawStream", None), _current_stream, lambda f, p: f(_current_device()) == p(_current_device()))
@@ -195,7 +203,7 @@ def _out(t, what: str, rows: int, cols: int, dtype, device: int) -> int:
     """The same of a matrix that the caller gives to be written: a graph that saved it before must notice."""
     ld = _like(t, what, rows, cols, dtype, device)
     if not t.is_inference():
-        torch.autograd.graph.increment_version(t)
+        _new_versions([t])
     return ld
 
 
@@ -781,7 +789,7 @@ def adamw_step(plan: AdamW, grads, lr, step, seed: int = 0, grad_scale=None, ski
     # A graph that was recorded before must notice, as with every operation in place.
     seen = plan._all_seen if 0 not in pointers else [t for tensors, g in zip(plan._seen, grads) if g is not None for t in tensors]
     if seen:
-        torch.autograd.graph.increment_version(seen)
+        _new_versions(seen)
 
 
 def adamw_moments(plan: AdamW, dtype=None, stream=None):
