@@ -131,9 +131,9 @@ int spdy_token_logprobs_with_grad(const void *logits, int64_t ld, int dtype, con
  *   hidden [R][D], weight [V][D]: `dtype` (SPDY_BF16 or SPDY_F16), D >= 1; bias [V] of `bias_dtype` (`dtype` or SPDY_F32), may be NULL;
  *   a bias of -inf marks ids that are not allowed.  R, V and D below 2^31 - 65536.
  *   tokens, logprob, entropy, lse, rows with nothing left, NaN and infinities: as spdy_token_logprobs has them.  A logit is the fp32 sum
- *   of the tensor cores' sums of up to 256 products, which are cut where fp32 additions round: each is short by at most 2^-19 of its
- *   magnitudes (measured: lse by 3e-7 of itself, 7e-7 where all products are positive).  What fp32 holds exactly is exact, and columns of
- *   zeros change nothing.  Up to 4 rows are added up in fp32.
+ *   of the tensor cores' sums of up to 384 products, which are cut where fp32 additions round: each is short by at most 3e-6 of its
+ *   magnitudes (measured: lse by 4e-7 of itself, 1.2e-6 where all products are positive).  What fp32 holds exactly is exact, and columns
+ *   of zeros change nothing.  Up to 4 rows are added up in fp32.
  * Gradients of sum_r grad_logprob[r] logprob[r] + grad_entropy[r] entropy[r], with g_rv the gradient by x_rv
  * (spdy_token_logprobs_backward's dlogits):
  *   dhidden[r][d] = sum_v g_rv weight[v][d],   dweight[v][d] = sum_r g_rv hidden[r][d],   dbias[v] = sum_r g_rv

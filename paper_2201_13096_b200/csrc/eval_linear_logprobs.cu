@@ -45,16 +45,15 @@ __device__ __forceinline__ void wait_for_previous()
 }
 
 // The tensor core cuts its partial sums towards 0 where fp32 additions would round: a sum of many products ends short of itself, by how much
-// depends on the data.  The sums that logits are go into several accumulators therefore, `most` stages to each at most, which the epilogue adds up in
-// fp32.  How far lse is off, relative, at widths 256 to 16384 (and at 4096 with positive products in half precision; the plain fp32 form 0.8e-7 to 1.1e-6):
-// 1 stage 0.9e-7 to 1.4e-7 (2.9e-7), 2 stages 1.6e-7 to 2.8e-7 (7.0e-7), 4 stages 3.3e-7 to 4.8e-7 (1.6e-6), all in one 2.2e-6 at 2624 already.  2048 x
-// 131072 x 2048 964, 887, 855 and 851 us (a slow card).  Logits take 2.
-constexpr int kPieceLogits = 2, kPieceGrad = 4;
-int piece_stages(int64_t D, int most)
-{
-    const int64_t stages = (D + kStageK - 1) / kStageK, pieces = (stages + most - 1) / most;
-    return static_cast<int>((stages + pieces - 1) / pieces);
-}
+// depends on the data.  The sums that logits are go into several accumulators therefore, a few stages to each, which the epilogue adds up in fp32.
+// How far lse is off, relative, at widths 256 to 16384 (positive products in half precision): 2 stages each 1.7e-7 to 2.8e-7 (7e-7), first 3, 3, then 2
+// 1.8e-7 to 4.1e-7 (7e-7 to 1.2e-6), 4 each 2.0e-7 to 4.8e-7 (1.6e-6), all in one 2.2e-6 at 2624 already (the plain fp32 form 0.8e-7 to 1.2e-6).
+// Values of 4096 x 16384 x 1024: 107, 97, 90 and 89 us.  The first two are longer because the next tile's have to keep the tensor cores busy while the
+// epilogue is still at work on this one.
+struct Pieces {
+    int first, rest;  // stages of the first two pieces, and of each that follows
+};
+constexpr Pieces kLogitPieces = {3, 2}, kGradPieces = {4, 4};
 
 enum Kind { kStats, kLogits, kGrad, kHidden, kWeight, kWeightParts };
 
@@ -75,7 +74,7 @@ struct ProductArgs {
     int bias_type, index_bits;
     int64_t v0;                    // the first column's id
     float c;                       // log2(e) / T
-    int piece;                     // stages of the summed index to an accumulator
+    Pieces pieces;
     float *partial, *token_logit;  // [tiles_n][3][padded_rows], [M]
     int64_t padded_rows;
     const float *consts;           // [M][kConsts]
@@ -552,8 +551,10 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 range(split, kb0, kb1);
                 if (kb0 == kb1) continue;
                 uint32_t d = 0;
-                for (int kb = kb0, piece = 0; kb < kb1; ++kb) {
-                    const bool begins = kInPieces<KIND> ? piece == 0 : kb == kb0, ends = (kInPieces<KIND> && ++piece == a.piece) || kb + 1 == kb1;
+                for (int kb = kb0, left = 0, piece = 0; kb < kb1; ++kb) {
+                    const bool begins = left == 0;
+                    if (begins) left = kInPieces<KIND> ? min(kb1 - kb, piece < 2 ? a.pieces.first : a.pieces.rest) : kb1 - kb, ++piece;
+                    const bool ends = --left == 0;
                     if (begins) {
                         ok = __all_sync(0xffffffffu, barrier_wait(&ctl.acc_empty[acc], acc_parity ^ 1));
                         if (!ok) break;
@@ -579,10 +580,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                     __syncwarp();
                     ++issued;
                     if (++stage == kStages) stage = 0, parity ^= 1;
-                    if (ends) {
-                        piece = 0;
-                        if (++acc == 2) acc = 0, acc_parity ^= 1;
-                    }
+                    if (ends && ++acc == 2) acc = 0, acc_parity ^= 1;
                 }
             }
             // nor does a product: TMEM is freed once the last one issued is done
@@ -620,16 +618,17 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             // Pieces of a sum are added up in registers, and the whole goes back to where the last one lies.
             const auto ready = [&] {
                 if constexpr (kInPieces<KIND>) {
-                    if (a.k_blocks > a.piece) {
+                    if (a.k_blocks > a.pieces.first) {
                         float sum[kWarpColumns];
 #pragma unroll
                         for (int i = 0; i < kWarpColumns; ++i) sum[i] = 0.f;
 #pragma unroll 1
-                        for (int left = a.k_blocks;; left -= a.piece) {
+                        for (int left = a.k_blocks, piece = 0;; ++piece) {
                             if (!arrived()) return false;
 #pragma unroll
                             for (int c = 0; c < kWarpColumns; c += 8) tmem_add8(at + c, sum + c);
-                            if (left <= a.piece) break;
+                            left -= piece < 2 ? a.pieces.first : a.pieces.rest;
+                            if (left <= 0) break;
                             release(), next();
                         }
 #pragma unroll
@@ -1400,7 +1399,7 @@ template <class T> struct Head {
         a.M = h.R, a.N = n, a.v0 = v0, a.b_row0 = static_cast<int>(v0);
         a.out = ws + l.piece, a.ldo = l.ld_piece;
         if (h.dbias) a.column_sums = floats(l.sums), a.ld_sums = l.ld_piece;
-        else a.piece = piece_stages(h.D, kPieceGrad);  // g in 16 bits shows nothing of it
+        else a.pieces = kGradPieces;  // g in 16 bits shows nothing of it
         if (h.grad_entropy) HEAD_TRY((launch_product<T, kGrad, true>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
         else HEAD_TRY((launch_product<T, kGrad, false>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
         return h.dbias ? finish_bias(h.R, n, v0, false) : SPDY_OK;
@@ -1471,7 +1470,7 @@ template <class T> int run_head(HeadArgs h, void *workspace, cudaStream_t s)
     rows.grad_logprob = h.grad_logprob, rows.grad_entropy = h.grad_entropy;
     ProductArgs base = {};
     base.bias = h.bias, base.bias_type = h.bias_type, base.tokens = h.tokens, base.index_bits = h.index_bits;
-    base.c = rows.c, base.piece = piece_stages(D, kPieceLogits), base.padded_rows = l.padded_rows;
+    base.c = rows.c, base.pieces = kLogitPieces, base.padded_rows = l.padded_rows;
     if (h.grads) {
         rows.consts = reinterpret_cast<float *>(ws + l.consts);
         if (!few && h.dtype == SPDY_F16) {
