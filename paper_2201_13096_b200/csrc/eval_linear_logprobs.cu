@@ -1171,14 +1171,14 @@ size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 // By ids: the gradient by the logits is kept for as many ids at a time as this much memory holds, 2048 at least.
 constexpr int64_t kPieceBytes = 256ll << 20, kLeastPiece = 2048;
 // By rows: the logits, for as many rows as this much memory holds; not where that is few, since dweight's fp32 sums are read and
-// written for each.  8192 rows (bf16, ms by rows and by ids): room for 2048 (131072 ids, width 1024) 6.3, 6.5; for 1766 (151936) 8.2, 7.7, at 4096 30.2,
-// 31.3; for 1342 (200000) 11.4, 10.3, 39.8, 40.0; with dbias for 1365 (131072) 9.0, 8.2, for 1178 (151936) at 4096 33.6, 31.4.
+// written for each.  8192 rows (bf16, ms by rows and by ids): room for 2048 (131072 ids, width 1024) 6.8, 6.5; for 1766 (151936) 9.0, 7.7, at 4096 30.1,
+// 31.1; for 1342 (200000) 12.3, 10.4, at 4096 41.2, 42.4; with dbias for 1365 (131072) 9.6, 8.3, for 1178 (151936) at 4096 33.6, 31.8.
 constexpr int64_t kLogitBytes = 512ll << 20, kLeastRows = 2048;
 
-// Whether keeping the logits costs less than multiplying them again, which the width decides.  4096 x 32768 bf16, us by rows and by ids: width 512 478,
-// 457, 640 599, 617, 768 657, 672, 1024 748, 840; with dbias (another byte per logit) 512 614, 577, 640 755, 752, 768 772, 787, 1024 877, 1020.  Few
-// logits stay in L2 and save a kernel's start: 512 x 30001 with dbias 512 136, 142, 768 158, 170, without 256 91, 95.
-bool keeps_logits(int64_t R, int64_t V, int64_t D, bool bias) { return D >= (bias && R > (1ll << 25) / V ? 768 : 512); }
+// Whether keeping the logits costs less than multiplying them again, which the width decides.  4096 x 32768 bf16, us by rows and by ids: width 512 486,
+// 488, 768 700, 701, 1024 828, 844; with dbias (another byte per logit) 640 778, 700, 768 840, 771, 1024 980, 968.  Fewer logits stay in L2 in part:
+// 1021 x 50001 with dbias 768 283, 333, 1024 405, 429; 512 x 30001 with dbias 512 115, 118, 768 128, 129, without 256 95, 98.
+bool keeps_logits(int64_t R, int64_t V, int64_t D, bool bias) { return D >= (bias && R > (1ll << 26) / V ? 1024 : 512); }
 
 // Sums of a row's tiles, 12 bytes each, for as many rows at a time as this much memory holds, 4096 at least.
 constexpr int64_t kPartialBytes = 32ll << 20, kLeastStats = 4096;
