@@ -145,7 +145,8 @@ int spdy_token_logprobs_with_grad(const void *logits, int64_t ld, int dtype, con
  *   ..._backward takes lse (and entropy with grad_entropy) from the forward call, ..._with_grad computes all in one call.
  *   workspace: ..._workspace_bytes(...) bytes, 256-byte aligned, contents undefined afterwards; `forward` and `gradients` say what the
  *   call computes (gradients: 0 none, 1 without dbias, 2 with it).  Of g it holds as many ids at a time as 256 MB hold
- *   (2048 at least), or, in ..._with_grad, as many rows as 512 MB hold, and then up to 4 V D bytes of dweight's sums.
+ *   (2048 at least), or, in ..._with_grad, as many rows as 512 MB hold, and then 4 V D bytes of dweight's sums; of few
+ *   tiles (V x D small) the sums lie there in up to 64 parts.
  * spdy_linear_check_status reports for these kernels too.
  */
 size_t spdy_linear_token_logprobs_workspace_bytes(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int dtype,

@@ -65,7 +65,8 @@ template <int CAP> __device__ __forceinline__ uint32_t tensor_of(const Table<CAP
     return low;
 }
 
-// A hash of 32 bits: two odd multipliers, each of which carries bits up, and shifts that bring them down again.
+// A hash of 32 bits: "lowbias32", as Chris Wellons published it (two odd multipliers, each of which carries bits up, and shifts that bring them down
+// again; the constants are the ones found there to leave the least bias).
 SPDY_EVAL_FN uint32_t mix(uint32_t x)
 {
     x = (x ^ (x >> 16)) * 0x7feb352du;

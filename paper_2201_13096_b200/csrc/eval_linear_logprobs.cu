@@ -1041,8 +1041,8 @@ template <class T> __global__ void __launch_bounds__(256) few_finish_kernel(cons
 
 // ---------------------------------------------------------------------------------------------- gradient by kept logits
 // Codes into the gradient, in place: eight columns to a thread, eight rows at a time; FINE: of 32 rows, which it adds up for dbias.
-// Memory bound: 2 bytes in (3), 2 out; 4096 x 32768 97 us (5.5 TB/s).  Blocks of 128, of which small calls have enough (512 x 30001 x 768, the
-// whole call: 135 us with 256 threads, 126 with 128).
+// Memory bound: 2 bytes in (3), 2 out; 4096 x 32768 97 us (5.5 TB/s).  Blocks of 128, of which small calls have enough (with 256
+// threads 512 x 30001 x 768, the whole call, took 9 us longer).
 constexpr int kGradRows = 8, kGradThreads = 128;
 template <bool FINE> constexpr int kGradBlock = FINE ? 32 : kGradRows;
 template <class T, bool ENT, bool FINE>

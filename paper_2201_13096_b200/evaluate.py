@@ -10,7 +10,9 @@ transposed, its weight's is not here), and ``adamw_step`` applies gradients to a
 Every call runs in the CUDA library on ``stream`` (default: torch's current stream of the tensors' device); PyTorch supplies
 memory and streams.  Matrices are 2-D CUDA tensors with unit column stride and any row stride.  There is no CPU fallback.
 Nothing is recorded for autograd: with gradients enabled, tensors that require one are refused (detach them, and take the
-gradient from the ``..._backward`` and ``..._with_grad`` calls; ``AdamW`` takes leaves, and changes them in place).
+gradient from the ``..._backward`` and ``..._with_grad`` calls; ``AdamW`` takes leaves, and changes them in place).  Tensors that a call
+writes (``out`` and the like, what ``AdamW`` steps) get a new version, so that a graph that saved one raises, as it does for torch's own
+operations in place.
 """
 from __future__ import annotations
 
