@@ -139,8 +139,8 @@ int spdy_token_logprobs_with_grad(const void *logits, int64_t ld, int dtype, con
  *   dhidden[r][d] = sum_v g_rv weight[v][d],   dweight[v][d] = sum_r g_rv hidden[r][d],   dbias[v] = sum_r g_rv
  *   dhidden [R][D] and dweight [V][D] of `dtype`, dbias [V] fp32 (from sums in fp32); each may be NULL.  They may not overlap the inputs.
  *   g is computed in fp32 and rounded to 16 bits once, as the operand of the two products (in half precision times a power of two that
- *   brings its largest row near 2^14).  ..._with_grad may keep the logits in between, as logarithms in 16 bits (with dbias 23):
- *   p is then within 3.5e-4 of itself (half precision 1.8e-4; with dbias 2.8e-6 and 1.4e-6), and 0 where it is 2^-64 (2^-32) of a neighbouring
+ *   brings its largest row near 2^14); for up to 64 rows it is their operand as the sum of two such numbers.  ..._with_grad may keep the
+ *   logits in between, as logarithms in 16 bits (with dbias 23): p is then within 3.5e-4 of itself (half precision 1.8e-4; with dbias 2.8e-6 and 1.4e-6), and 0 where it is 2^-64 (2^-32) of a neighbouring
  *   id's; at the token g comes from its logit in fp32.  A row of hidden that is not finite spoils dweight, with or without a token.
  *   ..._backward takes lse (and entropy with grad_entropy) from the forward call, ..._with_grad computes all in one call.
  *   workspace: ..._workspace_bytes(...) bytes, 256-byte aligned, contents undefined afterwards; `forward` and `gradients` say what the

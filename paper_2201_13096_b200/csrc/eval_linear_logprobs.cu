@@ -16,6 +16,8 @@
 // By rows (the rest of the calls that give values and gradients at once): the logits of some rows and all ids at a time, dweight added up over them; each
 // product is done once.  In the last two products one or both operands have the summed index as their rows ("MN-major"); TMA brings
 // them as boxes of 64 columns, and the matrix descriptors name that order, so nothing is transposed.
+#include <limits.h>
+
 #include "eval_tensor.cuh"
 
 using namespace spdy_eval;
@@ -83,6 +85,9 @@ struct ProductArgs {
     int64_t ld_sums;
     uint8_t *fine;                 // kLogits: NULL, or the codes' lower bits, [M][ldo]
     float *tops;                   // kLogits: [ids / 32][padded_rows], what a row's 32 codes are relative to
+    int low;                       // kGrad: 0, or the row of the piece from which the lower halves lie,
+    int64_t below;                 // that many bytes behind the upper ones (as a product of the two in the kernel it was kept in registers throughout)
+    int wrap;                      // products over rows: from this one on the second operand's begin again
     void *out;                     // kLogits: codes; kGrad: the piece; kWeight: 16 bits; parts: fp32 [splits][M][ldo]
     int64_t ldo;
     const float *sums;             // kWeight: NULL, or fp32 [M][ld_old] to add
@@ -331,17 +336,28 @@ template <bool ENT> __device__ __forceinline__ float grad_at(float y, const RowC
     return ENT ? -ex2(y) * fmaf(k.slope, max_nan(y, -200.f), k.all) : -ex2(y) * k.all;
 }
 
-// Gradient by 64 logits of a row, rounded to 16 bits once.
+// What rounding to 16 bits takes from numbers, in 16 bits; nothing of ones that are not finite in them.
+template <class T> __device__ __forceinline__ uint4 lower_halves(const float *f, uint4 rounded)
+{
+    float r[8];
+    Elem<T>::unpack(rounded, r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = fabsf(r[i]) <= 3.39e38f ? f[i] - r[i] : 0.f;
+    return Elem<T>::pack(r);
+}
+
+// Gradient by 64 logits of a row, rounded to 16 bits once (or in two halves).
 template <class T, bool ENT, class Ready, class Release>
 __device__ __forceinline__ void carry_grad(const ProductArgs &a, const uint32_t &tmem, int64_t m0, int64_t n0, float *bias, Ready ready, Release release)
 {
     const int lane = threadIdx.x & 31;
     const int64_t m = m0 + lane;
     const bool inside = m < a.M;
-    RowConsts k = {0.f, 0.f, 0.f, 0.f, 0.f, -1, 0.f};
-    if (inside) k = row_consts(a.consts, m, power_of_two(scale_power(a.scale_bits)));
+    if (inside) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.consts + static_cast<int64_t>(m) * kConsts));  // no registers for them while sums are added up
     stage_bias(a, n0, bias);
     const bool ok = ready();
+    RowConsts k = {0.f, 0.f, 0.f, 0.f, 0.f, -1, 0.f};
+    if (inside) k = row_consts(a.consts, m, power_of_two(scale_power(a.scale_bits)));
     char *to = static_cast<char *>(a.out) + (m * a.ldo + n0) * 2;
 #pragma unroll 1
     for (int c = 0; c < kWarpColumns; c += 32) {
@@ -362,9 +378,17 @@ __device__ __forceinline__ void carry_grad(const ProductArgs &a, const uint32_t 
         if (!ok)
 #pragma unroll
             for (int i = 0; i < 32; ++i) f[i] = quiet_nan();
-        if (inside)  // ldo is a multiple of 64
+        if (inside) {  // ldo is a multiple of 64
 #pragma unroll
-            for (int i = 0; i < 32; i += 16) store32(to + 2 * (c + i), Elem<T>::pack(f + i), Elem<T>::pack(f + i + 8));
+            for (int i = 0; i < 32; i += 16) {
+                const uint4 x = Elem<T>::pack(f + i), y = Elem<T>::pack(f + i + 8);
+                store32(to + 2 * (c + i), x, y);
+                if (a.low) store32(to + a.below + 2 * (c + i), lower_halves<T>(f + i, x), lower_halves<T>(f + i + 8, y));
+            }
+        } else if (m < a.low) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 16) store32(to + 2 * (c + i), make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0));
+        }
         if (a.column_sums) {
             if (!inside)
 #pragma unroll
@@ -522,7 +546,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                         unsigned char *ta = to + q * kSliceBytes, *tb = ta + BM * BK * 2;
                         if (kColumnsA) tma_load_pair(ta, &map_a, m0, k, full), tma_load_pair(ta + 8192, &map_a, m0 + 64, k, full);
                         else tma_load_pair(ta, &map_a, k, a.a_row0 + m0, full);
-                        if (kColumnsB) tma_load_pair(tb, &map_b, n0, a.b_row0 + k, full), tma_load_pair(tb + 8192, &map_b, n0 + 64, a.b_row0 + k, full);
+                        const int row = a.b_row0 + (kColumnsA && k >= a.wrap ? k - a.wrap : k);
+                        if (kColumnsB) tma_load_pair(tb, &map_b, n0, row, full), tma_load_pair(tb + 8192, &map_b, n0 + 64, row, full);
                         else tma_load_pair(tb, &map_b, k, a.b_row0 + n0, full);
                     }
                 }
@@ -598,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             a.tiles.at(static_cast<uint32_t>(item), split, tm, tn);
             range(split, kb0, kb1);
             if (kb0 == kb1) continue;
-            const int64_t m0 = static_cast<int64_t>(tm) * kTile + part * BM + quarter * 32, n0 = static_cast<int64_t>(tn) * kTile + group * kWarpColumns;
+            const int m0 = tm * kTile + part * BM + quarter * 32, n0 = tn * kTile + group * kWarpColumns;  // below 2^31, see kMost
             const auto here = [&] { return tmem + acc * kTile + group * kWarpColumns + (static_cast<uint32_t>(quarter * 32) << 16); };
             uint32_t at = here();
             const auto arrived = [&] {  // once a wait has run out, nothing is waited for any more
@@ -653,7 +678,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 #pragma unroll
                     for (int g = 1; g < 4; ++g) join(sums, {room[g * 96], room[g * 96 + 32], room[g * 96 + 64]}, a.c);
                     if (m0 < a.padded_rows) {
-                        float *to = a.partial + static_cast<int64_t>(tn) * 3 * a.padded_rows + m0 + lane;
+                        float *to = a.partial + static_cast<int64_t>(n0 / kTile) * 3 * a.padded_rows + m0 + lane;
                         to[0] = sums.m, to[a.padded_rows] = sums.s, to[2 * a.padded_rows] = sums.t;
                     }
                 }
@@ -1047,13 +1072,13 @@ constexpr int kGradRows = 8, kGradThreads = 128;
 template <bool FINE> constexpr int kGradBlock = FINE ? 32 : kGradRows;
 template <class T, bool ENT, bool FINE>
 __global__ void __launch_bounds__(kGradThreads) grad_kernel(uint16_t *codes, const uint8_t *fine, const float *tops, int64_t padded_rows, int64_t M, int64_t N, int64_t ld, const float *consts,
-                                                   float c, const uint32_t *scale_bits, float *column_sums)
+                                                   float c, const uint32_t *scale_bits, float *column_sums, int64_t low)
 {
     __shared__ RowConsts rows[kGradBlock<FINE>];
     wait_for_previous();
     const int64_t n = (static_cast<int64_t>(blockIdx.x) * kGradThreads + threadIdx.x) * 8;
-    for (int64_t m0 = static_cast<int64_t>(blockIdx.y) * kGradBlock<FINE>; m0 < M; m0 += static_cast<int64_t>(gridDim.y) * kGradBlock<FINE>) {
-        const int count = static_cast<int>(min(M - m0, static_cast<int64_t>(kGradBlock<FINE>)));
+    for (int64_t m0 = static_cast<int64_t>(blockIdx.y) * kGradBlock<FINE>; m0 < max(M, low); m0 += static_cast<int64_t>(gridDim.y) * kGradBlock<FINE>) {
+        const int count = static_cast<int>(max(min(M - m0, static_cast<int64_t>(kGradBlock<FINE>)), static_cast<int64_t>(0)));
         __syncthreads();
         if (threadIdx.x < count) rows[threadIdx.x] = row_consts(consts, m0 + threadIdx.x, power_of_two(scale_power(scale_bits)));
         __syncthreads();
@@ -1062,14 +1087,14 @@ __global__ void __launch_bounds__(kGradThreads) grad_kernel(uint16_t *codes, con
 #pragma unroll 1
         for (int first = 0; first < count; first += kGradRows) {
             uint4 raw[kGradRows];
-            uint2 low[kGradRows];
+            uint2 bits[kGradRows];
             float top[kGradRows];
 #pragma unroll
             for (int i = 0; i < kGradRows; ++i)
                 if (first + i < count) {  // ld is a multiple of 64: columns behind N are there, and nobody reads what becomes of them
                     const int64_t m = m0 + first + i;
                     raw[i] = load_last(codes + m * ld + n);
-                    if (FINE) low[i] = *reinterpret_cast<const uint2 *>(fine + m * ld + n);
+                    if (FINE) bits[i] = *reinterpret_cast<const uint2 *>(fine + m * ld + n);
                     top[i] = tops[n / kCodes * padded_rows + m];
                 }
 #pragma unroll
@@ -1082,7 +1107,7 @@ __global__ void __launch_bounds__(kGradThreads) grad_kernel(uint16_t *codes, con
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const uint32_t high = j % 2 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu;
-                    const uint32_t code = FINE ? high << 7 | __byte_perm(j < 4 ? low[i].x : low[i].y, 0, 0x4440 | j % 4) : high;
+                    const uint32_t code = FINE ? high << 7 | __byte_perm(j < 4 ? bits[i].x : bits[i].y, 0, 0x4440 | j % 4) : high;
                     const float steps = __uint_as_float(0x4b000000u | code) - 8388608.f;
                     f[j] = grad_at<ENT>(high == kNothing ? neg_inf() : fmaf(steps, -1.f / kCodeSteps<T, FINE>, base), k);
                 }
@@ -1094,20 +1119,25 @@ __global__ void __launch_bounds__(kGradThreads) grad_kernel(uint16_t *codes, con
                 if (FINE)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) sum[j] += f[j];
-                *reinterpret_cast<uint4 *>(codes + (m0 + first + i) * ld + n) = Elem<T>::pack(f);
+                const uint4 rounded = Elem<T>::pack(f);
+                *reinterpret_cast<uint4 *>(codes + (m0 + first + i) * ld + n) = rounded;
+                if (low) *reinterpret_cast<uint4 *>(codes + (low + m0 + first + i) * ld + n) = lower_halves<T>(f, rounded);
             }
         }
-        if (FINE)
+        for (int64_t m = m0 + count; m < low && m < m0 + kGradBlock<FINE>; ++m) *reinterpret_cast<uint4 *>(codes + m * ld + n) = make_uint4(0, 0, 0, 0);
+        if (FINE && count > 0)
 #pragma unroll
             for (int j = 0; j < 8; ++j) column_sums[m0 / 32 * ld + n + j] = sum[j];
     }
 }
 
 // ---------------------------------------------------------------------------------------------- sums of parts
-// out[m][n] = sum over the splits of parts[split][m][n], in their order, times 2^-scale, rounded once; eight columns to a thread.
+// out[m][n] = sum over the splits of parts[split][m][n] (and, with `low`, of parts[split][low + m][n]), in their order, times 2^-scale, rounded once; eight
+// columns to a thread; `rows`: of a part.
 // `wide`: every row of out starts on 16 bytes.  Index: 32 bits where they are enough (a division by a 64-bit number cost more than all the rest).
 template <class T, class Index>
-__global__ void __launch_bounds__(256) finish_kernel(const float *parts, int splits, int64_t M, int64_t N, int64_t ldp, const uint32_t *scale_bits, T *out, int64_t ldo, int wide)
+__global__ void __launch_bounds__(256) finish_kernel(const float *parts, int splits, int64_t rows, int64_t low, int64_t M, int64_t N, int64_t ldp, const uint32_t *scale_bits, T *out, int64_t ldo,
+                                                     int wide)
 {
     wait_for_previous();
     const float scale = power_of_two(-scale_power(scale_bits));
@@ -1116,15 +1146,16 @@ __global__ void __launch_bounds__(256) finish_kernel(const float *parts, int spl
         const Index row = i / across;
         const int64_t m = row, n = static_cast<int64_t>(i - row * across) * 8;
         float sum[8] = {};
+        for (int half = 0; half < (low ? 2 : 1); ++half)
 #pragma unroll 2
-        for (int s = 0; s < splits; ++s) {
-            uint4 lo, hi;
-            load32(parts + (s * M + m) * ldp + n, lo, hi);
-            float f[8];
-            Elem<float>::unpack(lo, f), Elem<float>::unpack(hi, f + 4);
+            for (int s = 0; s < splits; ++s) {
+                uint4 lo, hi;
+                load32(parts + (s * rows + half * low + m) * ldp + n, lo, hi);
+                float f[8];
+                Elem<float>::unpack(lo, f), Elem<float>::unpack(hi, f + 4);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += f[k];
-        }
+                for (int k = 0; k < 8; ++k) sum[k] += f[k];
+            }
 #pragma unroll
         for (int k = 0; k < 8; ++k) sum[k] *= scale;
         T *to = out + m * ldo + n;
@@ -1137,13 +1168,13 @@ __global__ void __launch_bounds__(256) finish_kernel(const float *parts, int spl
         }
     }
 }
-template <class T> int finish(const float *parts, int splits, int64_t M, int64_t N, int64_t ldp, const uint32_t *scale_bits, T *out, int64_t ldo, cudaStream_t s)
+template <class T> int finish(const float *parts, int splits, int64_t rows, int64_t low, int64_t M, int64_t N, int64_t ldp, const uint32_t *scale_bits, T *out, int64_t ldo, cudaStream_t s)
 {
     const int wide = aligned(out, 16) && ldo % 8 == 0;
     const int64_t total = M * (ldp / 8), most = static_cast<int64_t>(sm_count()) * 8, want = (total + 255) / 256;
     const unsigned blocks = static_cast<unsigned>(want < most ? want : most);
-    if (total + most * 256 < (1ll << 32)) return follow(finish_kernel<T, uint32_t>, dim3(blocks), 256, 0, 1, s, parts, splits, M, N, ldp, scale_bits, out, ldo, wide);
-    return follow(finish_kernel<T, uint64_t>, dim3(blocks), 256, 0, 1, s, parts, splits, M, N, ldp, scale_bits, out, ldo, wide);
+    if (total + most * 256 < (1ll << 32)) return follow(finish_kernel<T, uint32_t>, dim3(blocks), 256, 0, 1, s, parts, splits, rows, low, M, N, ldp, scale_bits, out, ldo, wide);
+    return follow(finish_kernel<T, uint64_t>, dim3(blocks), 256, 0, 1, s, parts, splits, rows, low, M, N, ldp, scale_bits, out, ldo, wide);
 }
 
 // dbias of a piece: the row groups' sums in their order, eight runs of them to a column.
@@ -1186,6 +1217,7 @@ constexpr int64_t kPartialBytes = 32ll << 20, kLeastStats = 4096;
 struct Layout {
     size_t hidden, weight, partial, token_logit, consts, scale, logits, tops, fine, piece, parts, weight_sums, sums, total;
     int64_t padded_rows, rows, stat_rows, width, ld_piece, ld_parts;  // rows, width: what is worked on at a time; stat_rows: for values
+    int64_t low, piece_rows;  // of the piece: where the lower halves of g begin (0: it has none), all of them
     int hidden_splits, weight_splits;
     bool by_rows;
 };
@@ -1213,6 +1245,11 @@ size_t copy_bytes(int64_t rows, int64_t D) { return static_cast<size_t>(rows) * 
 // Few rows need no tensor cores.  (Nor are fp32's digits then given away: with one row whose token is all but certain the gradient is the
 // small difference 1 - p.)
 bool is_few(int64_t R) { return R <= kFewRows; }
+// The gradient of few rows goes into the products in two halves of 16 bits, the second one what rounding took from the first: with few numbers to a sum the
+// rounding of one, up to 2^-9, shows (half precision, 5 to 44 rows: dhidden and dweight were off by up to 1.6 times the last rounding alone; with more rows
+// by 1.4 times).  The halves lie below one another, at most 128 rows: one tile of dhidden's product and one stage of dweight's.  Whole calls take 1 to 18 % longer
+// (33 x 32768 x 768 64 -> 71 us, 33 x 131072 x 4096 737 -> 741; with 128 rows it would be 7 to 26 %).
+constexpr int64_t kHalvesRows = 64;
 int64_t few_blocks() { return static_cast<int64_t>(sm_count()) * 4; }
 
 Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw, int64_t R, int64_t V, int64_t D, bool stats, bool grads, bool bias)
@@ -1241,13 +1278,14 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
     l.weight = take(tma_ok(weight, ldw) ? 0 : copy_bytes(V, D));
     if (grads) {
         l.ld_piece = div_up(V, 64) * 64;
+        l.low = R <= kHalvesRows ? div_up(R, BK) * BK : 0;
         const int64_t most = kLogitBytes / (bias ? 3 : 2) / l.ld_piece;  // rows
-        l.by_rows = stats && keeps_logits(R, V, D, bias) && (R <= most || most >= kLeastRows);
+        l.by_rows = stats && keeps_logits(R, V, D, bias) && (R + l.low <= most || most >= kLeastRows);
         if (l.by_rows) {
             const int64_t pieces = R <= most ? 1 : div_up(R, most / kTile * kTile);
             if (pieces > 1) l.rows = div_up(div_up(R, pieces), kTile) * kTile;  // of one size
         } else {
-            int64_t width = kPieceBytes / 2 / R / kTile * kTile;
+            int64_t width = kPieceBytes / 2 / (R + l.low) / kTile * kTile;
             if (width < kLeastPiece) width = kLeastPiece;
             const int64_t pieces = div_up(V, width);
             width = div_up(div_up(V, pieces), kTile) * kTile;
@@ -1255,13 +1293,14 @@ Layout lay_out(const void *hidden, int64_t ldh, const void *weight, int64_t ldw,
         }
         const bool once = l.rows == R;
         l.ld_parts = div_up(D, 8) * 8;
-        l.hidden_splits = choose_splits(l.rows, D, div_up(l.width, kStageK));
-        l.weight_splits = once ? choose_splits(l.width, D, div_up(l.rows, kStageK)) : 1;
+        l.piece_rows = l.low + l.rows;
+        l.hidden_splits = choose_splits(l.piece_rows, D, div_up(l.width, kStageK));
+        l.weight_splits = once ? choose_splits(l.width, D, div_up(l.piece_rows, kStageK)) : 1;
         l.consts = take(static_cast<size_t>(l.rows) * kConsts * 4);
         l.scale = take(256);
         if (l.by_rows) l.tops = take(static_cast<size_t>(l.ld_piece / kCodes) * (div_up(l.rows, 32) * 32) * 4);
-        l.piece = take(static_cast<size_t>(l.rows) * l.ld_piece * 2);
-        l.parts = take(static_cast<size_t>(l.hidden_splits) * l.rows * l.ld_parts * 4);
+        l.piece = take(static_cast<size_t>(l.piece_rows) * l.ld_piece * 2);
+        l.parts = take(static_cast<size_t>(l.hidden_splits) * l.piece_rows * l.ld_parts * 4);
         if (!once || l.weight_splits > 1) l.weight_sums = take(static_cast<size_t>(l.weight_splits) * l.width * l.ld_parts * 4);
         if (l.by_rows && bias) l.fine = take(static_cast<size_t>(l.rows) * l.ld_piece);
         if (bias) l.sums = take(static_cast<size_t>(div_up(l.rows, 32)) * l.ld_piece * 4);
@@ -1302,6 +1341,7 @@ template <class T, int KIND, bool ENT> int launch_product(const CUtensorMap &ma,
     if (tm * tn * splits > 0x3fffffff) return SPDY_ERR_UNSUPPORTED;
     a.tiles = Tiles(static_cast<int>(tm), static_cast<int>(tn), group), a.splits = splits, a.per_split = Divisor(static_cast<uint32_t>(splits));
     a.k_blocks = static_cast<int>(div_up(K, kStageK));
+    if (a.wrap == 0) a.wrap = INT_MAX;
     const int items = static_cast<int>(tm * tn) * splits, pairs = sm_count() / 2;
     auto *kernel = product_kernel<T, KIND, ENT>;
     SPDY_EVAL_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<KIND>()));
@@ -1384,12 +1424,13 @@ template <class T> struct Head {
     int gradient(int64_t m, int64_t r0)
     {
         const bool fine = h.dbias != nullptr;
-        const int64_t down = div_up(m, fine ? kGradBlock<true> : kGradBlock<false>);
+        const int64_t down = div_up(m > l.low ? m : l.low, fine ? kGradBlock<true> : kGradBlock<false>);
         const dim3 grid(static_cast<unsigned>(div_up(h.V, kGradThreads * 8)), static_cast<unsigned>(down < 65535 ? down : 65535));
         uint16_t *codes = reinterpret_cast<uint16_t *>(ws + l.piece);
         const uint8_t *low = reinterpret_cast<const uint8_t *>(ws + l.fine);
         auto *kernel = fine ? (h.grad_entropy ? grad_kernel<T, true, true> : grad_kernel<T, false, true>) : h.grad_entropy ? grad_kernel<T, true, false> : grad_kernel<T, false, false>;
-        HEAD_TRY(follow(kernel, grid, kGradThreads, 0, 1, s, codes, low, floats(l.tops), l.padded_rows, m, h.V, l.ld_piece, base.consts, base.c, base.scale_bits, floats(l.sums)));
+        HEAD_TRY(follow(kernel, grid, kGradThreads, 0, 1, s, codes, low, floats(l.tops), l.padded_rows, m, h.V, l.ld_piece, base.consts, base.c, base.scale_bits, floats(l.sums),
+                        l.low));
         return fine ? finish_bias(m, h.V, 0, r0 > 0) : SPDY_OK;
     }
     // The gradient by the logits of all rows and ids v0 .. v0 + n - 1, which are multiplied again; dbias of these ids.
@@ -1397,7 +1438,7 @@ template <class T> struct Head {
     {
         ProductArgs a = base;
         a.M = h.R, a.N = n, a.v0 = v0, a.b_row0 = static_cast<int>(v0);
-        a.out = ws + l.piece, a.ldo = l.ld_piece;
+        a.out = ws + l.piece, a.ldo = l.ld_piece, a.low = static_cast<int>(l.low), a.below = l.low * l.ld_piece * 2;
         if (h.dbias) a.column_sums = floats(l.sums), a.ld_sums = l.ld_piece;
         else a.pieces = kGradPieces;  // g in 16 bits shows nothing of it
         if (h.grad_entropy) HEAD_TRY((launch_product<T, kGrad, true>(hidden, weight, a, h.D, group_of(h.D), 1, s)));
@@ -1411,32 +1452,33 @@ template <class T> struct Head {
     // dhidden's sums and dweight from the gradient of m rows (from r0) and n ids (from v0), added to what earlier rows or ids gave.
     int products(int64_t m, int64_t r0, int64_t n, int64_t v0)
     {
+        const int64_t rows = l.low + m;  // of the piece
         CUtensorMap piece;
         if (h.dhidden) {
-            HEAD_TRY(map_of(&piece, ws + l.piece, l.ld_piece, m, n, h.dtype, BM));
+            HEAD_TRY(map_of(&piece, ws + l.piece, l.ld_piece, rows, n, h.dtype, BM));
             ProductArgs b = {};
-            b.M = m, b.N = h.D, b.b_row0 = static_cast<int>(v0), b.out = floats(l.parts), b.ldo = l.ld_parts, b.add = v0 > 0;
+            b.M = rows, b.N = h.D, b.b_row0 = static_cast<int>(v0), b.out = floats(l.parts), b.ldo = l.ld_parts, b.add = v0 > 0;
             HEAD_TRY((launch_product<T, kHidden, false>(piece, weight_columns, b, n, 8, l.hidden_splits, s)));
         }
         if (!h.dweight) return SPDY_OK;
-        HEAD_TRY(map_of(&piece, ws + l.piece, l.ld_piece, m, n, h.dtype, BK));
+        HEAD_TRY(map_of(&piece, ws + l.piece, l.ld_piece, rows, n, h.dtype, BK));
         T *out = static_cast<T *>(h.dweight) + v0 * h.lddw;
         ProductArgs b = {};
-        b.M = n, b.N = h.D, b.b_row0 = static_cast<int>(r0);
+        b.M = n, b.N = h.D, b.b_row0 = static_cast<int>(r0), b.wrap = static_cast<int>(l.low);
         const bool last = r0 + m == h.R;
         if (l.weight_splits > 1 || !last) {
             b.out = floats(l.weight_sums), b.ldo = l.ld_parts, b.add = r0 > 0;
-            HEAD_TRY((launch_product<T, kWeightParts, false>(piece, hidden_columns, b, m, 8, l.weight_splits, s)));
-            return last ? finish<T>(floats(l.weight_sums), l.weight_splits, n, h.D, l.ld_parts, base.scale_bits, out, h.lddw, s) : SPDY_OK;
+            HEAD_TRY((launch_product<T, kWeightParts, false>(piece, hidden_columns, b, rows, 8, l.weight_splits, s)));
+            return last ? finish<T>(floats(l.weight_sums), l.weight_splits, n, 0, n, h.D, l.ld_parts, base.scale_bits, out, h.lddw, s) : SPDY_OK;
         }
         b.out = out, b.ldo = h.lddw, b.scale_bits = base.scale_bits;
         b.width = aligned(out, 32) && h.lddw % 16 == 0 ? 32 : aligned(out, 16) && h.lddw % 8 == 0 ? 16 : 0;
         if (r0 > 0) b.sums = floats(l.weight_sums), b.ld_old = l.ld_parts;
-        return launch_product<T, kWeight, false>(piece, hidden_columns, b, m, 8, 1, s);
+        return launch_product<T, kWeight, false>(piece, hidden_columns, b, rows, 8, 1, s);
     }
     int finish_hidden(int64_t m, int64_t r0)
     {
-        return finish<T>(floats(l.parts), l.hidden_splits, m, h.D, l.ld_parts, base.scale_bits, static_cast<T *>(h.dhidden) + r0 * h.lddh, h.lddh, s);
+        return finish<T>(floats(l.parts), l.hidden_splits, l.low + m, l.low, m, h.D, l.ld_parts, base.scale_bits, static_cast<T *>(h.dhidden) + r0 * h.lddh, h.lddh, s);
     }
 };
 

@@ -135,3 +135,28 @@ def test_dbias_of_few_wide_rows_from_a_saved_lse(R, V, D, dtype):
     bound = (p * gl.double().abs()[:, None] * off).sum(0).norm() + 2.0 ** -22 * g.sum(0).norm()
     got = evaluate.linear_token_logprobs_backward(h, w, tokens, lse.float(), None, gl, None, b).dbias
     assert (got.double() - g.sum(0)).norm() <= bound
+
+
+@gpu
+@pytest.mark.parametrize("R,V,D,dtype,bias,entropy", [
+    (5, 3000, 72, BF16, None, True), (6, 1764, 826, F16, None, False), (44, 1536, 1536, F16, None, False), (63, 777, 200, F16, F32, True), (64, 5003, 512, BF16, F32, False),
+    (33, 2001, 640, F16, F32, True), (32, 9000, 64, BF16, "same", True), (61, 999, 1030, BF16, None, True), (64, 4096, 256, F16, None, True), (64, 700, 1100, BF16, F32, True),
+])
+def test_gradients_of_few_rows_are_rounded_once(R, V, D, dtype, bias, entropy):
+    # up to 64 rows the gradient by the logits is the sum of two numbers of 16 bits: dhidden and dweight are as exact as their own last rounding, and what
+    # kept logits and the sums' cuts take
+    h, w, tokens, b = head(R, V, D, dtype, bias, padh=3, padw=0)
+    gl, gh = weights(R, dtype, entropy)
+    saved = evaluate.linear_token_logprobs(h, w, tokens, b)
+    again = evaluate.linear_token_logprobs_backward(h, w, tokens, saved.lse, saved.entropy, gl, gh, b)
+    want = tune.head(h, w, b, tokens, 1.0, gl, gh, on="cuda", halves=2)
+    for name in ("dhidden", "dweight"):
+        tune.close(getattr(again, name), want, name)
+    for wanted in (("hidden", "weight"), ("hidden", "weight", "bias")):
+        kept = 0 if D < 512 else 23 if b is not None and "bias" in wanted else 16
+        want = tune.head(h, w, b, tokens, 1.0, gl, gh, on="cuda", kept=kept, halves=2)
+        grads = evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, wanted=wanted)[1]
+        for name in ("dhidden", "dweight"):
+            tune.close(getattr(grads, name), want, name)
+        if grads.dbias is not None:
+            tune.close(grads.dbias, want, "dbias")

@@ -9,10 +9,11 @@ import eval_reference as ref
 F16 = torch.float16
 
 
-def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu", kept=0, cut=None):
+def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu", kept=0, cut=None, halves=1):
     """A dict of values and, under the same name with ``_err``, of bounds on the fp32 error before the last rounding.
     ``kept``: the gradient comes from logits kept in so many bits, as a call that gives values and gradients keeps them: 16, or 23 with
     dbias; the token's own is not among them.
+    ``halves``: in how many numbers of 16 bits the gradient by the logits goes into the products.
     ``cut``: by how much of its magnitudes a logit may be off, where that is known better than from the number of products."""
     h, w = (t.detach().to(on).double() for t in (hidden, weight))
     R, D = h.shape
@@ -68,7 +69,7 @@ def head(hidden, weight, bias, tokens, temperature, gl=None, gh=None, on="cpu", 
     # Half precision: a power of two brings the largest bound on a row's gradient, |a| + |b| (0.37 + log V), to 2^13 .. 2^14, where numbers below the
     # normal ones are rounded by 2^-25: 2^-38 of that bound.
     most = float(((a.abs() + b.abs() * (0.37 + math.log(V))) / temperature).nan_to_num(0.0).max()) if R else 0.0
-    rounded = eg + ref.HALF_ULP[hidden.dtype] * 1.01 * (g.abs() + eg) + (2.0 ** -38 * most if hidden.dtype == F16 else 2.0 ** -134)
+    rounded = eg + ref.HALF_ULP[hidden.dtype] ** halves * 1.01 * (g.abs() + eg) + (2.0 ** -38 * most if hidden.dtype == F16 else 2.0 ** -134)
     out["dhidden"], out["dweight"], out["dbias"] = g @ w, g.T @ h, g.sum(0)
     out["dhidden_err"] = rounded @ w.abs() + (V / 8 + 16 + V / 1024) * 2.0 ** -23 * (g.abs() @ w.abs())
     out["dweight_err"] = rounded.T @ h.abs() + (R / 8 + 16 + 64) * 2.0 ** -23 * (g.abs().T @ h.abs())
