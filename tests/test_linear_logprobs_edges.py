@@ -160,3 +160,17 @@ def test_gradients_of_few_rows_are_rounded_once(R, V, D, dtype, bias, entropy):
             tune.close(getattr(grads, name), want, name)
         if grads.dbias is not None:
             tune.close(grads.dbias, want, "dbias")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_few_rows_over_pieces_of_a_vocabulary(dtype):
+    R, V, D = 10, 2_200_001, 24  # the gradient in two halves, for 1.8 million ids at a time
+    h, w, tokens, b = head(R, V, D, dtype, F32)
+    gl, gh = weights(R, dtype, True)
+    want = tune.head(h, w, b, tokens, 1.0, gl, gh, on="cuda", halves=2)
+    saved = evaluate.linear_token_logprobs(h, w, tokens, b)
+    for grads in (evaluate.linear_token_logprobs_backward(h, w, tokens, saved.lse, saved.entropy, gl, gh, b),
+                  evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b)[1]):
+        for name in ("dhidden", "dweight", "dbias"):
+            tune.close(getattr(grads, name), want, name)
