@@ -8,8 +8,8 @@
 // are a matter of reading w once: a kernel of plain multiply-adds streams it.
 //
 // Measured, bf16, us in a graph (and the floor: the larger of bytes at 6.56 TB/s and operations at 1.68 PFLOP/s):
-// 4096 x 768 x 3072 (rows, K, columns) with bias and gelu 27.0 (11.5), without 24.7, 16384 x 1024 x 4096 with gelu 113 (82), without 103,
-// 8192 x 4096 x 1024 with residual 60 (41), 8192^3 751 to 782 (656), 512 x 1024 x 4096 12.7, 128 x 768 x 3072 9.4, 16 x 4096 x 1024 10.6.
+// 4096 x 768 x 3072 (rows, K, columns) with bias and gelu 23.0 (11.5), without 20.0, 16384 x 1024 x 4096 with gelu 105 (82), without 100,
+// 8192 x 4096 x 1024 with residual 58 (41), 8192^3 713 to 755 (656), 512 x 1024 x 4096 12.7, 128 x 768 x 3072 9.4, 16 x 4096 x 1024 10.6.
 // Bound: large products by the feed of the tensor cores (a stage's barriers and copies beside its products), the middle ones by whole rounds of tiles
 // and the last one's epilogue, the small ones by the fixed way through barriers, TMEM and the exchange of parts (about 8 us).
 #include "eval_tensor.cuh"
