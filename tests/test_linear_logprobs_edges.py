@@ -174,3 +174,30 @@ def test_few_rows_over_pieces_of_a_vocabulary(dtype):
                   evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b)[1]):
         for name in ("dhidden", "dweight", "dbias"):
             tune.close(getattr(grads, name), want, name)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("D", [64, 520])
+def test_few_rows_that_are_not_finite_stay_alone(D, dtype):
+    R, V = 40, 777
+    h, w, tokens, b = head(R, V, D, dtype, F32)
+    gl, gh = weights(R, dtype, True)
+
+    def calls():
+        saved = evaluate.linear_token_logprobs(h, w, tokens, b)  # the backward call takes what the forward call gave for the same rows
+        return (evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b, wanted=("hidden", "weight"))[1], evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, gh, b)[1],
+                evaluate.linear_token_logprobs_backward(h, w, tokens, saved.lse, saved.entropy, gl, gh, b))
+
+    clean = calls()
+    h[5, 3], h[39, 0] = float("nan"), float("inf")
+    rest = torch.ones(R, dtype=torch.bool, device="cuda")
+    rest[5] = rest[39] = False
+    for got, want in zip(calls(), clean):
+        assert torch.isnan(got.dhidden[5]).all() and not torch.isfinite(got.dhidden[39]).any()
+        assert torch.equal(got.dhidden[rest], want.dhidden[rest])
+    tokens.fill_(-1)  # padding: rows without a token and without a gradient, finite ones
+    h[5, 3], h[39, 0] = 1.0, 1.0
+    saved = evaluate.linear_token_logprobs(h, w, tokens, b)
+    for grads in (evaluate.linear_token_logprobs_with_grad(h, w, tokens, gl, None, b)[1], evaluate.linear_token_logprobs_backward(h, w, tokens, saved.lse, None, gl, None, b)):
+        assert (grads.dhidden == 0).all() and (grads.dweight == 0).all() and (grads.dbias == 0).all()
